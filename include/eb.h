@@ -53,7 +53,12 @@ extern "C" {
 typedef struct ihipStream_t* eb_stream_t; /* identical to hipStream_t */
 typedef struct ihipEvent_t* eb_event_t;   /* identical to hipEvent_t */
 
-typedef enum { EB_F32 = 0, EB_BF16 = 1 } eb_dtype;
+typedef enum {
+  EB_F32 = 0,
+  EB_BF16 = 1,
+  EB_E4M3 = 2 /* 8-bit floats (OCP E4M3: 4 exponent and 3 mantissa bits, no infinities); only as
+                 the type of a paged cache (eb_paged_kv) */
+} eb_dtype;
 
 typedef enum {
   EB_OK = 0,
@@ -127,6 +132,92 @@ eb_status eb_block_attn_dual(eb_dtype dt, const eb_ragged* r, const eb_suffix* s
                              const void* v_blk, const void* k_pre, const void* v_pre,
                              const void* k_suf, const void* v_suf, void* out, void* ws,
                              size_t ws_bytes, eb_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Paged key/value cache.  A serving program whose sequences grow block by block keeps their cached
+ * keys and values in pages of a common pool instead of one packed prefix: position p of sequence b
+ * lies in row p % page_size of page page_table[b * max_pages + p / page_size].
+ *
+ *   k, v              [n_pages, hkv, page_size, head_dim] of `dtype` (16-byte aligned)
+ *   k_scale, v_scale  [n_pages, hkv, page_size] u8, EB_E4M3 only: byte s of a row means that its
+ *                     value is 2^(s - 127) times what the 8 bits say (1 <= s <= 254)
+ *   page_table        [batch, max_pages] i32; sequences may share pages that are only read
+ *
+ * A page number outside [0, n_pages) is no page: its rows read as zeros, and rows written to it
+ * are dropped.  Table entries behind a sequence's last page are not read.
+ *
+ * Requires hkv >= 1, head_dim in {64, 128}, page_size in {16, 32, 64, 128, 256}, n_pages >= 1,
+ * max_pages >= 1 and, where cached rows are read, max_prefix <= max_pages * page_size.
+ * With EB_DEBUG_CHECKS the page numbers that a call uses have to lie in [0, n_pages).
+ * ------------------------------------------------------------------------------------- */
+typedef struct {
+  eb_dtype dtype;            /* EB_F32, EB_BF16 or EB_E4M3 */
+  int32_t hkv, head_dim;
+  int32_t n_pages, page_size;
+  int32_t max_pages;         /* columns of page_table */
+  const int32_t* page_table; /* device [batch, max_pages] */
+  void* k;
+  void* v;
+  uint8_t* k_scale; /* NULL unless EB_E4M3 */
+  uint8_t* v_scale;
+} eb_paged_kv;
+
+/* ---------------------------------------------------------------------------------------
+ * Rows into the cache.  Block row i of sequence b (rows cu_block[b] .. cu_block[b+1]-1 of k and v)
+ * goes to position
+ *
+ *   pos != NULL:  pos[i] of its sequence; a negative position leaves the row out (a position that
+ *                 is still masked, or padding)
+ *   pos == NULL:  (cached rows of b, from cu_prefix) + (i - cu_block[b]): appended in order
+ *
+ *   k, v [T, hkv, head_dim] of dtype dt;  pos [T] i32, optional
+ *
+ * dt equals the cache's dtype (rows are copied), or the cache is EB_E4M3 (dt EB_F32 or EB_BF16) and
+ * every (row, head) x[0 .. head_dim) of k and of v is quantised by itself:
+ *
+ *   a = max |x_d| over its finite values;  e = the smallest whole number with a <= 448 * 2^e, kept
+ *   in [-100, 120];  scale byte = e + 127;  8 bits = x_d * 2^-e rounded once to E4M3 (to nearest,
+ *   ties to even); infinities and NaN become NaN
+ *
+ * so that the value read back is off by at most 2^-4 of itself, or 2^-10 * 2^e where |x_d| is below
+ * 2^-6 * 2^e, and is exact in bf16.  Rows at positions past the table are dropped.  Other rows of
+ * the pages keep their contents.  No two rows of a call may go to the same row of the same page
+ * (with EB_DEBUG_CHECKS, which also refuses positions past the table, the call returns
+ * EB_ERR_INVALID).  cu_prefix and the host's prefix fields are read only where pos is NULL.
+ * ------------------------------------------------------------------------------------- */
+eb_status eb_kv_write(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, const int32_t* pos,
+                      const void* k, const void* v, eb_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Cached rows back, packed: rows cu_prefix[b] .. cu_prefix[b+1]-1 of k and v are positions
+ * 0 .. of sequence b, the k_pre / v_pre of eb_block_attn and eb_decode_step.
+ *
+ *   k, v [S, hkv, head_dim] of dtype dt, which equals the cache's, or EB_F32 or EB_BF16 for an
+ *   EB_E4M3 cache (exact in both, down to 2^-126)
+ *
+ * Of r only batch, total_prefix, max_prefix and cu_prefix are used.
+ * ------------------------------------------------------------------------------------- */
+eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, void* k, void* v,
+                     eb_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Block attention over a paged cache: eb_block_attn whose prefix rows, cu_prefix[b+1] -
+ * cu_prefix[b] of them for sequence b, are the first positions of its pages.  A block may be one
+ * row (a token at a time) or a long chunk of a prompt; the keys form a set, so the cache may hold
+ * the context left and right of the block.
+ *
+ *   q [T, hq, head_dim]    k_blk, v_blk [T, hkv, head_dim]    out [T, hq, head_dim]  (of dtype dt)
+ *
+ * dt is EB_F32 (cache EB_F32 or EB_E4M3) or EB_BF16 (cache EB_BF16 or EB_E4M3).  hkv and head_dim
+ * are the cache's; hq % hkv == 0; scale as in eb_block_attn.  Arithmetic as in eb_block_attn, on
+ * the values that the cache stands for; scores of -inf weigh nothing.
+ * ws: at least eb_block_attn_paged_workspace(...) bytes, contents ignored.
+ * ------------------------------------------------------------------------------------- */
+size_t eb_block_attn_paged_workspace(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv,
+                                     int hq);
+eb_status eb_block_attn_paged(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, int hq,
+                              float scale, const void* q, const void* k_blk, const void* v_blk,
+                              void* out, void* ws, size_t ws_bytes, eb_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------
  * Fused LM head and confidence statistics (Alg. 5: softmax of the backbone logits, top-1

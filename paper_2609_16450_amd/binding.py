@@ -16,7 +16,7 @@ import torch
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libeb.so")
 
-EB_F32, EB_BF16 = 0, 1
+EB_F32, EB_BF16, EB_E4M3 = 0, 1, 2
 EB_OK, EB_ERR_INVALID, EB_ERR_UNSUPPORTED, EB_ERR_WORKSPACE, EB_ERR_HIP = 0, 1, 2, 3, 4
 
 _P = ctypes.c_void_p
@@ -31,6 +31,13 @@ class eb_ragged(ctypes.Structure):
 class eb_suffix(ctypes.Structure):
     _fields_ = [("total_suffix", ctypes.c_int32), ("max_suffix", ctypes.c_int32),
                 ("cu_suffix", _P)]
+
+
+class eb_paged_kv(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("hkv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("page_table", _P), ("k", _P), ("v", _P),
+                ("k_scale", _P), ("v_scale", _P)]
 
 
 class eb_step_trace(ctypes.Structure):
@@ -64,6 +71,17 @@ EXPORTS = {
                                           ctypes.POINTER(eb_suffix), ctypes.c_int, ctypes.c_int,
                                           ctypes.c_int, ctypes.c_float, _P, _P, _P, _P, _P, _P,
                                           _P, _P, _P, ctypes.c_size_t, _P]),
+    "eb_kv_write": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(eb_ragged),
+                                   ctypes.POINTER(eb_paged_kv), _P, _P, _P, _P]),
+    "eb_kv_read": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(eb_ragged),
+                                  ctypes.POINTER(eb_paged_kv), _P, _P, _P]),
+    "eb_block_attn_paged_workspace": (ctypes.c_size_t, [ctypes.c_int, ctypes.POINTER(eb_ragged),
+                                                        ctypes.POINTER(eb_paged_kv),
+                                                        ctypes.c_int]),
+    "eb_block_attn_paged": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(eb_ragged),
+                                           ctypes.POINTER(eb_paged_kv), ctypes.c_int,
+                                           ctypes.c_float, _P, _P, _P, _P, _P, ctypes.c_size_t,
+                                           _P]),
     "eb_lmhead_workspace": (ctypes.c_size_t, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
                                               ctypes.c_int]),
     "eb_lmhead_confidence": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
@@ -176,6 +194,13 @@ def _dev(t: torch.Tensor, name: str, dtype=None, shape=None) -> None:
         raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def _dev_on(index: int, t: torch.Tensor, name: str, dtype=None, shape=None) -> None:
+    """As _dev, with the tensor on device `index`."""
+    _dev(t, name, dtype, shape)
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on device {t.get_device()}, the cache on {index}")
 
 
 # The current device's current stream as a handle, without building a torch.cuda.Stream (0.2
@@ -312,6 +337,135 @@ def eb_block_attn_dual(r: Ragged, cu_suffix: torch.Tensor, max_suffix: int, q, k
                                   k_pre.data_ptr(), v_pre.data_ptr(), k_suf.data_ptr(),
                                   v_suf.data_ptr(), out.data_ptr(), wp, wn, _stream(stream)),
            "eb_block_attn_dual")
+
+
+class PagedKV:
+    """A paged key/value cache (eb_paged_kv in eb.h): a pool of pages and the page table of a batch.
+
+    k, v: [n_pages, hkv, page_size, head_dim], float32, bfloat16 or float8_e4m3fn; the last with
+    k_scale, v_scale: uint8 [n_pages, hkv, page_size].  page_table: int32 [batch, max_pages].  The
+    tensors are checked once, here; they are kept, not copied, so that their contents (the table's
+    too) may change between calls.
+    """
+
+    def __init__(self, k, v, page_table, k_scale=None, v_scale=None):
+        codes = {torch.float32: EB_F32, torch.bfloat16: EB_BF16, torch.float8_e4m3fn: EB_E4M3}
+        if not isinstance(k, torch.Tensor) or k.dtype not in codes:
+            raise ValueError("k must be a float32, bfloat16 or float8_e4m3fn tensor")
+        if k.dim() != 4:
+            raise ValueError(f"k has shape {tuple(k.shape)}, expected [n_pages, hkv, page_size, "
+                             "head_dim]")
+        if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+            raise ValueError("page_table must be a tensor [batch, max_pages]")
+        _dev(k, "k")
+        self.device_index = k.get_device()
+        _dev_on(self.device_index, v, "v", k.dtype, k.shape)
+        _dev_on(self.device_index, page_table, "page_table", torch.int32)
+        if k.dtype is torch.float8_e4m3fn:
+            _dev_on(self.device_index, k_scale, "k_scale", torch.uint8, k.shape[:3])
+            _dev_on(self.device_index, v_scale, "v_scale", torch.uint8, k.shape[:3])
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("scales go with a float8_e4m3fn cache only")
+        self.k, self.v, self.page_table, self.k_scale, self.v_scale = (k, v, page_table, k_scale,
+                                                                       v_scale)
+        self.dtype = codes[k.dtype]
+        self.n_pages, self.hkv, self.page_size, self.head_dim = k.shape
+        self.batch, self.max_pages = page_table.shape
+        self._c = eb_paged_kv(self.dtype, self.hkv, self.head_dim, self.n_pages, self.page_size,
+                              self.max_pages, page_table.data_ptr(), k.data_ptr(), v.data_ptr(),
+                              _ptr(k_scale), _ptr(v_scale))
+        self._ref = ctypes.byref(self._c)
+
+    @staticmethod
+    def empty(n_pages: int, hkv: int, page_size: int, head_dim: int, page_table: torch.Tensor,
+              dtype: torch.dtype = torch.bfloat16) -> "PagedKV":
+        """A new pool on the page table's device; its pages' contents are undefined."""
+        def pool():
+            return torch.empty(n_pages, hkv, page_size, head_dim, dtype=dtype,
+                               device=page_table.device)
+
+        def scale():
+            return (torch.empty(n_pages, hkv, page_size, dtype=torch.uint8,
+                                device=page_table.device)
+                    if dtype is torch.float8_e4m3fn else None)
+
+        return PagedKV(pool(), pool(), page_table, scale(), scale())
+
+
+def _paged(r: Ragged, kv: PagedKV, stream) -> int:
+    """Checks what every call on a paged cache shares; returns the stream's handle."""
+    if not isinstance(kv, PagedKV):
+        raise TypeError("kv must be a PagedKV")
+    if kv.batch != r.batch:
+        raise ValueError(f"page_table has {kv.batch} rows, the batch {r.batch}")
+    for name, cu in (("cu_block", r.cu_block), ("cu_prefix", r.cu_prefix)):
+        _dev_on(kv.device_index, cu, name)
+    # a launch goes to the current device: refuse tensors and streams of another one
+    if torch.cuda.current_device() != kv.device_index:
+        raise ValueError(f"the cache is on device {kv.device_index}, the current device is "
+                         f"{torch.cuda.current_device()}")
+    if isinstance(stream, torch.cuda.Stream) and stream.device_index != kv.device_index:
+        raise ValueError(f"the cache is on device {kv.device_index}, the stream on "
+                         f"{stream.device_index}")
+    return _stream(stream)
+
+
+def eb_kv_write(r: Ragged, kv: PagedKV, k, v, pos=None, stream=None) -> None:
+    """Block rows k, v [T, hkv, D] into the cache's pages: at positions pos [T] int32 of their
+    sequences (negative: left out), or appended to the cached rows without pos (eb.h)."""
+    s = _paged(r, kv, stream)
+    dt = _dtype_code(k)
+    shape = (r.total_block, kv.hkv, kv.head_dim)
+    _dev_on(kv.device_index, k, "k", k.dtype, shape)
+    _dev_on(kv.device_index, v, "v", k.dtype, shape)
+    if pos is not None:
+        _dev_on(kv.device_index, pos, "pos", torch.int32, (r.total_block,))
+    rc = r.c()
+    _check(load().eb_kv_write(dt, ctypes.byref(rc), kv._ref, _ptr(pos), k.data_ptr(),
+                              v.data_ptr(), s), "eb_kv_write")
+
+
+def eb_kv_read(r: Ragged, kv: PagedKV, k, v, stream=None) -> None:
+    """k, v [S, hkv, D] <- the cached rows of every sequence (r's prefix lengths), packed as
+    eb_block_attn and eb_decode_step take them (eb.h)."""
+    s = _paged(r, kv, stream)
+    dt = _dtype_code(k)
+    shape = (r.total_prefix, kv.hkv, kv.head_dim)
+    _dev_on(kv.device_index, k, "k", k.dtype, shape)
+    _dev_on(kv.device_index, v, "v", k.dtype, shape)
+    rc = r.c()
+    _check(load().eb_kv_read(dt, ctypes.byref(rc), kv._ref, k.data_ptr(), v.data_ptr(), s),
+           "eb_kv_read")
+
+
+def eb_block_attn_paged_workspace(dtype: int, r: Ragged, kv: PagedKV, hq: int) -> int:
+    rc = r.c()
+    return int(load().eb_block_attn_paged_workspace(dtype, ctypes.byref(rc), kv._ref, hq))
+
+
+def eb_block_attn_paged(r: Ragged, kv: PagedKV, q, k_blk, v_blk, out,
+                        scale: Optional[float] = None, ws: Optional[torch.Tensor] = None,
+                        stream=None) -> None:
+    """out[T, hq, D] <- block attention of q over the cached rows (r's prefix lengths) and the block
+    keys (eb.h)."""
+    s = _paged(r, kv, stream)
+    dt = _dtype_code(q)
+    T, hq, D = q.shape
+    _dev_on(kv.device_index, q, "q", q.dtype, (r.total_block, hq, kv.head_dim))
+    _dev_on(kv.device_index, k_blk, "k_blk", q.dtype, (r.total_block, kv.hkv, kv.head_dim))
+    _dev_on(kv.device_index, v_blk, "v_blk", q.dtype, (r.total_block, kv.hkv, kv.head_dim))
+    _dev_on(kv.device_index, out, "out", q.dtype, (r.total_block, hq, kv.head_dim))
+    if ws is not None and ws.get_device() != kv.device_index:
+        raise ValueError(f"ws must be on device {kv.device_index}")
+    scale = 0.0 if scale is None else float(scale)    # 0: the library's 1/sqrt(D)
+    rc = r.c()
+    rp = ctypes.byref(rc)
+    lib = load()
+    need = int(lib.eb_block_attn_paged_workspace(dt, rp, kv._ref, hq))
+    wp, wn = _workspace(need, ws, q.device, stream)
+    _check(lib.eb_block_attn_paged(dt, rp, kv._ref, hq, scale, q.data_ptr(), k_blk.data_ptr(),
+                                   v_blk.data_ptr(), out.data_ptr(), wp, wn, s),
+           "eb_block_attn_paged")
 
 
 def eb_lmhead_workspace(dtype: int, n_rows: int, hidden: int, vocab: int) -> int:

@@ -1,0 +1,300 @@
+// Block attention over a paged key/value cache.
+//
+// Keys of a sequence are its cached rows, read through the page table, and the block's own rows.
+// The cached rows are padded to whole stages, so that a stage lies either in the cache or in the
+// block and a piece of 16 keys in one page (page sizes are multiples of 16); keys of the padding
+// get scores of -inf and values of zero, whatever the page holds there.
+#include "attn_common.hpp"
+#include "eb_common.hpp"
+#include "eb_internal.hpp"
+#include "paged.hpp"
+
+namespace eb {
+namespace {
+
+// ---------------------------------------------------------------------------------------
+// fp32 arithmetic throughout, on 16x16x4 fp32 MFMAs.
+//
+// A workgroup of kAnyWaves wavefronts per (16 query rows, K/V head, sequence, key range).  Wave w
+// takes the 16-key chunks w, w + kAnyWaves, ... of the range with an online softmax of its own; the
+// waves' results are merged through LDS and, with a key split, the ranges' by a second kernel.
+// Scores are formed transposed, S^T = K Q^T: lane l owns query l % 16 and holds keys 4 (l / 16) + r
+// of the chunk, which are the k-slots of the B operand of O^T = V^T P^T, one register per MFMA.
+// ---------------------------------------------------------------------------------------
+constexpr int kAnyWaves = 8;
+constexpr int kAnyRows = 16;
+constexpr int kAnyKeys = 16;
+constexpr int kAnyStage = kAnyWaves * kAnyKeys;  // keys that the waves take in one go
+
+struct PagedParams {
+  PagedKv kv;
+  const int32_t* cu_block;
+  const int32_t* cu_prefix;
+  int hq, group, tiles;
+  float scale;
+  const void* q;
+  const void* k_blk;
+  const void* v_blk;
+  void* out;
+  // key split, in ranges of kps keys of the padded key space; partials as in AttnParams, the
+  // maxima in natural units
+  int nsplit, kps;
+  float* o_part;
+  float* m_part;
+  float* l_part;
+};
+
+template <class T>
+__device__ __forceinline__ float widen(T x);
+template <>
+__device__ __forceinline__ float widen<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float widen<uint16_t>(uint16_t x) { return bf16_bits_to_f32(x); }
+template <>
+__device__ __forceinline__ float widen<uint8_t>(uint8_t x) { return e4m3_pair_f32<false>(x, 1.f)[0]; }
+
+template <class T>
+__device__ __forceinline__ f32x4 widen4(const T* p);
+template <>
+__device__ __forceinline__ f32x4 widen4<float>(const float* p) {
+  return *reinterpret_cast<const f32x4u*>(p);
+}
+template <>
+__device__ __forceinline__ f32x4 widen4<uint16_t>(const uint16_t* p) {
+  const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+  return f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u),
+               __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+}
+template <>
+__device__ __forceinline__ f32x4 widen4<uint8_t>(const uint8_t* p) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+  const f32x2 a = e4m3_pair_f32<false>(w, 1.f), b = e4m3_pair_f32<true>(w, 1.f);
+  return f32x4{a[0], a[1], b[0], b[1]};
+}
+__device__ __forceinline__ void store_row(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store_row(uint16_t* p, float x) { *p = f32_to_bf16_bits_rne(x); }
+
+template <int D, class T, class C>
+__global__ __launch_bounds__(kAnyWaves * 64) void attn_paged_any_kernel(PagedParams p) {
+  constexpr int kChunks = D / 16;
+  constexpr int kPitch = D + 4;
+  __shared__ __attribute__((aligned(16))) float s_o[kAnyWaves][kAnyRows * kPitch];
+  __shared__ float s_m[kAnyWaves][kAnyRows], s_l[kAnyWaves][kAnyRows];
+  const int tile = blockIdx.x % p.tiles, sp = blockIdx.x / p.tiles, g = blockIdx.y, b = blockIdx.z;
+  const int row0 = tile * kAnyRows;
+  const int bbeg = p.cu_block[b], len = p.cu_block[b + 1] - bbeg;
+  const int G = p.group, n_rows = len * G;
+  if (row0 >= n_rows) return;  // whole workgroup
+  const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
+  const int cached = (plen + kAnyKeys - 1) / kAnyKeys * kAnyKeys;  // the block's first key
+  const int n_keys = cached + len;
+  const int kbeg = sp * p.kps;
+  if (kbeg >= n_keys) return;  // whole workgroup
+  const int kend = min(n_keys, kbeg + p.kps);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int grp = lane >> 4, l16 = lane & 15;
+  auto row_at = [&](int i) {  // element offset of a query row (rows past the end repeat the last)
+    const int r = min(row0 + i, n_rows - 1);
+    return (static_cast<size_t>(bbeg + r / G) * p.hq + g * G + r % G);
+  };
+
+  f32x4 qf[kChunks], o[kChunks];
+  const T* q = static_cast<const T*>(p.q) + row_at(l16) * D + 4 * grp;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) qf[c] = widen4(q + 16 * c), o[c] = f32x4{};
+  // from the lowest finite value on: keys with scores of -inf have weights of zero
+  float m_run = -3.402823466e38f, l_run = 0.f;
+  for (int k0 = kbeg + wave * kAnyKeys; k0 < kend; k0 += kAnyStage) {
+    f32x4 kf[kChunks];
+    float vf[4][kChunks];  // V of key k0 + 4 grp + r at d = 16 c + l16
+    int valid;             // keys of this chunk
+    if (k0 < cached) {
+      valid = min(kAnyKeys, plen - k0);
+      int page = p.kv.table[static_cast<size_t>(b) * p.kv.max_pages + (k0 >> p.kv.page_shift)];
+      const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(p.kv.n_pages);
+      page = ok ? page : 0;
+      const size_t slab = ((static_cast<size_t>(page) * p.kv.hkv + g) << p.kv.page_shift) +
+                          (k0 & ((1 << p.kv.page_shift) - 1));
+      const size_t kr = slab + min(l16, valid - 1);
+      float ks = ok ? 1.f : 0.f, vs[4];
+      if (sizeof(C) == 1 && ok) ks = e8m0(p.kv.k_scale[kr]);
+      const C* kp = reinterpret_cast<const C*>(p.kv.k) + kr * D + 4 * grp;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        kf[c] = widen4(kp + 16 * c) * ks;
+        if (!ok) kf[c] = f32x4{};
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const size_t vr = slab + min(4 * grp + r, valid - 1);
+        vs[r] = 1.f;
+        if (sizeof(C) == 1) vs[r] = e8m0(p.kv.v_scale[vr]);
+        const C* vp = reinterpret_cast<const C*>(p.kv.v) + vr * D + l16;
+        const bool live = ok && 4 * grp + r < valid;  // a weight of zero times infinity is NaN
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) vf[r][c] = live ? widen<C>(vp[16 * c]) * vs[r] : 0.f;
+      }
+    } else {
+      const int j0 = k0 - cached;
+      valid = min(kAnyKeys, len - j0);
+      const size_t kr = static_cast<size_t>(bbeg + j0 + min(l16, valid - 1)) * p.kv.hkv + g;
+      const T* kp = static_cast<const T*>(p.k_blk) + kr * D + 4 * grp;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) kf[c] = widen4(kp + 16 * c);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const size_t vr =
+            static_cast<size_t>(bbeg + j0 + min(4 * grp + r, valid - 1)) * p.kv.hkv + g;
+        const T* vp = static_cast<const T*>(p.v_blk) + vr * D + l16;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+          vf[r][c] = 4 * grp + r < valid ? widen<T>(vp[16 * c]) : 0.f;
+      }
+    }
+    f32x4 acc[2] = {f32x4{}, f32x4{}};
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e & 1] = mfma16_f32(kf[c][e], qf[c][e], acc[e & 1]);
+    float sc[4], mloc = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      sc[r] = 4 * grp + r < valid ? (acc[0][r] + acc[1][r]) * p.scale : -INFINITY;
+      mloc = fmaxf(mloc, sc[r]);
+    }
+    mloc = fmaxf(mloc, __shfl_xor(mloc, 16));
+    mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
+    const float m_new = fmaxf(m_run, mloc);
+    const float alpha = expf(m_run - m_new);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) o[c] *= alpha;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float e = expf(sc[r] - m_new);
+      l_run += e;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) o[c] = mfma16_f32(vf[r][c], e, o[c]);
+    }
+  }
+  float l_tot = l_run + __shfl_xor(l_run, 16);
+  l_tot += __shfl_xor(l_tot, 32);
+  if (grp == 0) {
+    s_m[wave][l16] = m_run;
+    s_l[wave][l16] = l_tot;
+  }
+  // register r of o[c]: d = 16 c + 4 (l / 16) + r of query l % 16
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c)
+    *reinterpret_cast<f32x4*>(&s_o[wave][l16 * kPitch + 16 * c + 4 * grp]) = o[c];
+  __syncthreads();
+  // merge in wave order; a wave without keys has l = 0 and o = 0
+  for (int i = tid; i < kAnyRows * D; i += kAnyWaves * 64) {
+    const int r = i / D, d = i % D;
+    if (row0 + r >= n_rows) break;
+    float m = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < kAnyWaves; ++w) m = fmaxf(m, s_m[w][r]);
+    float l = 0.f, x = 0.f;
+#pragma unroll
+    for (int w = 0; w < kAnyWaves; ++w) {
+      const float f = expf(s_m[w][r] - m);
+      l = fmaf(f, s_l[w][r], l);
+      x = fmaf(f, s_o[w][r * kPitch + d], x);
+    }
+    const size_t at = row_at(r);
+    if (p.nsplit > 1) {
+      p.o_part[(at * p.nsplit + sp) * D + d] = x;
+      if (d == 0) p.m_part[at * p.nsplit + sp] = m, p.l_part[at * p.nsplit + sp] = l;
+    } else {
+      store_row(static_cast<T*>(p.out) + at * D + d, x / l);
+    }
+  }
+}
+
+// The ranges of one (block row, query head) per wavefront, in order.
+template <int D, class T>
+__global__ __launch_bounds__(256) void attn_paged_any_merge_kernel(PagedParams p, int batch,
+                                                                   int total) {
+  constexpr int kPer = D / 64;
+  const long rh = static_cast<long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (rh >= static_cast<long>(total) * p.hq) return;  // uniform per wavefront
+  const int b = find_sequence(p.cu_block, batch, static_cast<int>(rh / p.hq), lane);
+  const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
+  const int n_keys = (plen + kAnyKeys - 1) / kAnyKeys * kAnyKeys + p.cu_block[b + 1] - p.cu_block[b];
+  const int n = min(p.nsplit, (n_keys + p.kps - 1) / p.kps);
+  const size_t base = static_cast<size_t>(rh) * p.nsplit;
+  float m = -INFINITY, l = 0.f, x[kPer] = {};
+  for (int k = lane; k < n; k += 64) m = fmaxf(m, p.m_part[base + k]);
+  for (int mask = 32; mask >= 1; mask >>= 1) m = fmaxf(m, __shfl_xor(m, mask));
+  for (int k = 0; k < n; ++k) {
+    const float f = expf(p.m_part[base + k] - m);
+    l = fmaf(f, p.l_part[base + k], l);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      x[e] = fmaf(f, p.o_part[(base + k) * D + lane * kPer + e], x[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; ++e)
+    store_row(static_cast<T*>(p.out) + rh * D + lane * kPer + e, x[e] / l);
+}
+
+// Ranges of whole stages, enough for two workgroups per compute unit.
+SplitPlan any_plan(const PagedAttnArgs& a) {
+  const long tiles = (static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) + kAnyRows - 1) / kAnyRows;
+  const long base = tiles * a.kv.hkv * a.batch;
+  const int keys = (a.max_prefix + kAnyKeys - 1) / kAnyKeys * kAnyKeys + a.max_block;
+  const int stages = (keys + kAnyStage - 1) / kAnyStage;
+  const int want = static_cast<int>(max(1L, min((512 + base - 1) / base, static_cast<long>(stages))));
+  const int per = (stages + want - 1) / want;
+  return SplitPlan{(stages + per - 1) / per, per * kAnyStage};
+}
+
+template <int D, class T, class C>
+hipError_t launch_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
+  const SplitPlan sp = any_plan(a);
+  const size_t n = static_cast<size_t>(a.total_block) * a.hq * sp.nsplit;
+  float* o = static_cast<float*>(ws);
+  const int group = a.hq / a.kv.hkv;
+  const int tiles = static_cast<int>((static_cast<long>(a.max_block) * group + kAnyRows - 1) /
+                                     kAnyRows);
+  const PagedParams p{a.kv, a.cu_block, a.cu_prefix, a.hq, group, tiles, a.scale, a.q, a.k_blk,
+                      a.v_blk, a.out, sp.nsplit, sp.kps, o, o + n * D, o + n * D + n};
+  const dim3 grid(static_cast<unsigned>(tiles * sp.nsplit), static_cast<unsigned>(a.kv.hkv),
+                  static_cast<unsigned>(a.batch));
+  hipLaunchKernelGGL((attn_paged_any_kernel<D, T, C>), grid, dim3(kAnyWaves * 64), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sp.nsplit == 1) return e;
+  const long pairs = static_cast<long>(a.total_block) * a.hq;
+  hipLaunchKernelGGL((attn_paged_any_merge_kernel<D, T>), dim3(static_cast<unsigned>((pairs + 3) / 4)),
+                     dim3(256), 0, s, p, a.batch, a.total_block);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
+  (void)bf16;
+  if (a.total_block == 0 || a.max_block == 0) return 0;
+  const SplitPlan sp = any_plan(a);
+  if (sp.nsplit == 1) return 0;
+  return static_cast<size_t>(a.total_block) * a.hq * sp.nsplit * (a.kv.head_dim + 2) *
+         sizeof(float);
+}
+
+hipError_t attn_paged(bool bf16, const PagedAttnArgs& a, void* ws, hipStream_t s) {
+  if (a.total_block == 0 || a.max_block == 0) return hipSuccess;
+  const bool e4m3 = a.kv.type == CacheType::kE4m3;
+  if (a.kv.head_dim == 128) {
+    if (bf16) return e4m3 ? launch_any<128, uint16_t, uint8_t>(a, ws, s)
+                          : launch_any<128, uint16_t, uint16_t>(a, ws, s);
+    return e4m3 ? launch_any<128, float, uint8_t>(a, ws, s) : launch_any<128, float, float>(a, ws, s);
+  }
+  if (bf16) return e4m3 ? launch_any<64, uint16_t, uint8_t>(a, ws, s)
+                        : launch_any<64, uint16_t, uint16_t>(a, ws, s);
+  return e4m3 ? launch_any<64, float, uint8_t>(a, ws, s) : launch_any<64, float, float>(a, ws, s);
+}
+
+}  // namespace eb

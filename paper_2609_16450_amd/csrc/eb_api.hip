@@ -7,6 +7,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -42,6 +43,9 @@ eb_status hip_status(hipError_t e, const char* what) {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 constexpr size_t kWsAlign = 256;
+constexpr int kMaxGridYZ = 65535;       // second and third dimension of a launch grid
+constexpr int kMaxKeys = 1 << 30;       // of one sequence
+constexpr int kMaxPackedRows = 1 << 27; // rows that one launch of the cache kernels indexes
 constexpr int kProbeMaxGroups = 65536;
 constexpr int kProbeMaxIters = 1 << 20;
 size_t round_up(size_t n) { return (n + kWsAlign - 1) / kWsAlign * kWsAlign; }
@@ -61,6 +65,17 @@ eb_status check_ragged(const eb_ragged* r, bool need_prefix) {
                   r->total_prefix, r->max_prefix);
     if (!r->cu_prefix) return fail(EB_ERR_INVALID, "cu_prefix is NULL");
   }
+  return EB_OK;
+}
+
+// The prefix fields alone (the block's are not used).
+eb_status check_prefix(const eb_ragged* r) {
+  if (!r) return fail(EB_ERR_INVALID, "ragged descriptor is NULL");
+  if (r->batch < 1) return fail(EB_ERR_INVALID, "batch must be >= 1 (got %d)", r->batch);
+  if (r->total_prefix < 0 || r->max_prefix < 0 || r->max_prefix > r->total_prefix)
+    return fail(EB_ERR_INVALID, "bad prefix totals (total_prefix %d, max_prefix %d)",
+                r->total_prefix, r->max_prefix);
+  if (!r->cu_prefix) return fail(EB_ERR_INVALID, "cu_prefix is NULL");
   return EB_OK;
 }
 
@@ -122,6 +137,54 @@ eb_status check_unmask(const eb_ragged* r, const void* conf, const void* argmax,
   return EB_OK;
 }
 
+// The fields of a paged cache, and that dt's rows go with its type.
+eb_status check_paged(eb_dtype dt, const eb_paged_kv* kv) {
+  if (dt != EB_F32 && dt != EB_BF16) return fail(EB_ERR_INVALID, "unknown dtype %d", (int)dt);
+  if (!kv) return fail(EB_ERR_INVALID, "paged cache descriptor is NULL");
+  if (kv->dtype != EB_F32 && kv->dtype != EB_BF16 && kv->dtype != EB_E4M3)
+    return fail(EB_ERR_INVALID, "unknown cache dtype %d", (int)kv->dtype);
+  if (kv->hkv < 1 || kv->head_dim < 1 || kv->n_pages < 1 || kv->page_size < 1 || kv->max_pages < 1)
+    return fail(EB_ERR_INVALID,
+                "need hkv, head_dim, n_pages, page_size, max_pages >= 1 (got %d, %d, %d, %d, %d)",
+                kv->hkv, kv->head_dim, kv->n_pages, kv->page_size, kv->max_pages);
+  if (kv->head_dim != 64 && kv->head_dim != 128)
+    return fail(EB_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", kv->head_dim);
+  if (kv->page_size < 16 || kv->page_size > 256 || (kv->page_size & (kv->page_size - 1)))
+    return fail(EB_ERR_UNSUPPORTED, "page_size %d not supported (16, 32, 64, 128 or 256)",
+                kv->page_size);
+  if (kv->hkv > kMaxGridYZ)
+    return fail(EB_ERR_UNSUPPORTED, "hkv %d not supported (at most %d)", kv->hkv, kMaxGridYZ);
+  if (kv->dtype != EB_E4M3 && kv->dtype != dt)
+    return fail(EB_ERR_UNSUPPORTED, "rows of dtype %d with a cache of dtype %d", (int)dt,
+                (int)kv->dtype);
+  if (!kv->page_table || !kv->k || !kv->v) return fail(EB_ERR_INVALID, "NULL page_table / k / v");
+  if (!aligned16(kv->k) || !aligned16(kv->v))
+    return fail(EB_ERR_INVALID, "the cache's k and v must be 16-byte aligned");
+  if (kv->dtype == EB_E4M3 && (!kv->k_scale || !kv->v_scale))
+    return fail(EB_ERR_INVALID, "NULL k_scale / v_scale with an EB_E4M3 cache");
+  return EB_OK;
+}
+
+// The cached rows of every sequence lie within its row of the page table.
+eb_status check_paged_prefix(const eb_ragged* r, const eb_paged_kv* kv) {
+  const long capacity = static_cast<long>(kv->max_pages) * kv->page_size;
+  if (r->max_prefix > capacity)
+    return fail(EB_ERR_INVALID, "max_prefix %d does not fit %d pages of %d rows", r->max_prefix,
+                kv->max_pages, kv->page_size);
+  return EB_OK;
+}
+
+eb::PagedKv paged_args(const eb_paged_kv* kv) {
+  const eb::CacheType type = kv->dtype == EB_E4M3   ? eb::CacheType::kE4m3
+                             : kv->dtype == EB_BF16 ? eb::CacheType::kBf16
+                                                    : eb::CacheType::kF32;
+  int shift = 0;
+  while (shift < 30 && (1 << shift) < kv->page_size) ++shift;
+  return eb::PagedKv{type, kv->hkv, kv->head_dim, kv->n_pages, shift, kv->max_pages,
+                     kv->page_table, static_cast<uint8_t*>(kv->k), static_cast<uint8_t*>(kv->v),
+                     kv->k_scale, kv->v_scale};
+}
+
 // ---- optional checks of the device-array contract --------------------------------------
 // With the environment variable EB_DEBUG_CHECKS set (to anything but "0"), an entry point copies
 // its offset arrays (and tau) to the host after the work already on `stream`, and returns
@@ -133,7 +196,7 @@ bool debug_checks() {
 }
 
 template <class T>
-eb_status fetch(std::vector<T>& h, const T* d, int n, hipStream_t s) {
+eb_status fetch(std::vector<T>& h, const T* d, size_t n, hipStream_t s) {
   h.resize(n);
   hipError_t e = hipMemcpyAsync(h.data(), d, sizeof(T) * n, hipMemcpyDeviceToHost, s);
   if (e == hipSuccess) e = hipStreamSynchronize(s);
@@ -179,6 +242,59 @@ eb_status check_device(const eb_ragged* r, bool need_prefix, const float* tau, h
     st = check_cu("cu_prefix", r->cu_prefix, r->batch, r->total_prefix, r->max_prefix, s);
   if (st == EB_OK && tau) st = check_tau(tau, r->batch, s);
   return st;
+}
+
+// The pages that hold the first lens[b] positions of each sequence b have numbers in range.
+eb_status check_pages(const eb_paged_kv* kv, const std::vector<int32_t>& table, int b, int64_t n) {
+  for (int64_t j = 0; j * kv->page_size < n; ++j) {
+    const int32_t page = table[static_cast<size_t>(b) * kv->max_pages + j];
+    if (page < 0 || page >= kv->n_pages)
+      return fail(EB_ERR_INVALID, "page_table[%d][%lld] = %d is not in [0, %d)", b, (long long)j,
+                  page, kv->n_pages);
+  }
+  return EB_OK;
+}
+
+// The pages of the cached rows (cu_prefix has been checked).
+eb_status check_cached_pages(const eb_ragged* r, const eb_paged_kv* kv, hipStream_t s) {
+  std::vector<int32_t> cu, table;
+  eb_status st = fetch(cu, r->cu_prefix, r->batch + 1, s);
+  if (st == EB_OK) st = fetch(table, kv->page_table, static_cast<size_t>(r->batch) * kv->max_pages, s);
+  for (int b = 0; st == EB_OK && b < r->batch; ++b)
+    st = check_pages(kv, table, b, cu[b + 1] - cu[b]);
+  return st;
+}
+
+// Where a write's rows go: positions within the table, pages in range, no row of the pool twice.
+eb_status check_written(const eb_ragged* r, const eb_paged_kv* kv, const int32_t* pos,
+                        hipStream_t s) {
+  std::vector<int32_t> cb, cp, table, at;
+  eb_status st = fetch(cb, r->cu_block, r->batch + 1, s);
+  if (st == EB_OK && !pos) st = fetch(cp, r->cu_prefix, r->batch + 1, s);
+  if (st == EB_OK && pos) st = fetch(at, pos, r->total_block, s);
+  if (st == EB_OK) st = fetch(table, kv->page_table, static_cast<size_t>(r->batch) * kv->max_pages, s);
+  if (st != EB_OK) return st;
+  std::vector<int64_t> rows;
+  for (int b = 0; b < r->batch; ++b)
+    for (int i = cb[b]; i < cb[b + 1]; ++i) {
+      const int64_t p = pos ? at[i] : static_cast<int64_t>(cp[b + 1]) - cp[b] + i - cb[b];
+      if (p < 0) continue;
+      const int64_t j = p / kv->page_size;
+      if (j >= kv->max_pages)
+        return fail(EB_ERR_INVALID, "row %d: position %lld does not fit %d pages of %d rows", i,
+                    (long long)p, kv->max_pages, kv->page_size);
+      const int32_t page = table[static_cast<size_t>(b) * kv->max_pages + j];
+      if (page < 0 || page >= kv->n_pages)
+        return fail(EB_ERR_INVALID, "page_table[%d][%lld] = %d is not in [0, %d)", b, (long long)j,
+                    page, kv->n_pages);
+      rows.push_back(static_cast<int64_t>(page) * kv->page_size + p % kv->page_size);
+    }
+  std::sort(rows.begin(), rows.end());
+  const auto twice = std::adjacent_find(rows.begin(), rows.end());
+  if (twice != rows.end())
+    return fail(EB_ERR_INVALID, "two rows go to row %lld of page %lld",
+                (long long)(*twice % kv->page_size), (long long)(*twice / kv->page_size));
+  return EB_OK;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -318,6 +434,82 @@ eb_status eb_block_attn_dual(eb_dtype dt, const eb_ragged* r, const eb_suffix* s
                  k_pre, v_pre, out, sfx->max_suffix, sfx->cu_suffix, k_suf, v_suf};
   return hip_status(eb::block_attn(dt == EB_BF16, true, a, ws, stream),
                     "eb_block_attn_dual launch");
+}
+
+eb_status eb_kv_write(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, const int32_t* pos,
+                      const void* k, const void* v, eb_stream_t stream) {
+  eb_status st = check_ragged(r, pos == nullptr);
+  if (st == EB_OK) st = check_paged(dt, kv);
+  if (st != EB_OK) return st;
+  if (r->total_block > kMaxPackedRows)
+    return fail(EB_ERR_UNSUPPORTED, "more than %d rows in one call", kMaxPackedRows);
+  if (r->total_block > 0 && (!k || !v)) return fail(EB_ERR_INVALID, "NULL k / v");
+  if (dt == EB_BF16 && r->total_block > 0 && (!aligned16(k) || !aligned16(v)))
+    return fail(EB_ERR_INVALID, "bf16 tensors must be 16-byte aligned");
+  st = check_device(r, pos == nullptr, nullptr, stream);
+  if (st == EB_OK && debug_checks() && r->total_block > 0) st = check_written(r, kv, pos, stream);
+  if (st != EB_OK) return st;
+  return hip_status(eb::kv_write(dt == EB_BF16, paged_args(kv), r->batch, r->total_block,
+                                 r->cu_block, r->cu_prefix, pos, k, v, stream),
+                    "eb_kv_write launch");
+}
+
+eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, void* k, void* v,
+                     eb_stream_t stream) {
+  eb_status st = check_prefix(r);
+  if (st == EB_OK) st = check_paged(dt, kv);
+  if (st == EB_OK) st = check_paged_prefix(r, kv);
+  if (st != EB_OK) return st;
+  if (r->total_prefix > kMaxPackedRows)
+    return fail(EB_ERR_UNSUPPORTED, "more than %d rows in one call", kMaxPackedRows);
+  if (r->total_prefix > 0 && (!k || !v)) return fail(EB_ERR_INVALID, "NULL k / v");
+  if (dt == EB_BF16 && r->total_prefix > 0 && (!aligned16(k) || !aligned16(v)))
+    return fail(EB_ERR_INVALID, "bf16 tensors must be 16-byte aligned");
+  if (debug_checks()) {
+    st = check_cu("cu_prefix", r->cu_prefix, r->batch, r->total_prefix, r->max_prefix, stream);
+    if (st == EB_OK) st = check_cached_pages(r, kv, stream);
+    if (st != EB_OK) return st;
+  }
+  return hip_status(eb::kv_read(dt == EB_BF16, paged_args(kv), r->batch, r->total_prefix,
+                                r->cu_prefix, k, v, stream),
+                    "eb_kv_read launch");
+}
+
+size_t eb_block_attn_paged_workspace(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv,
+                                     int hq) {
+  if (!r || !kv || r->batch < 1 || hq < 1 || kv->hkv < 1 || hq % kv->hkv || r->total_block <= 0 ||
+      r->max_block <= 0 || r->max_prefix < 0 ||
+      static_cast<int64_t>(r->max_prefix) + r->max_block > kMaxKeys)
+    return 0;
+  eb::PagedAttnArgs a{r->batch, r->total_block, r->max_block, r->total_prefix, r->max_prefix,
+                      r->cu_block, r->cu_prefix, paged_args(kv), hq, 1.f, nullptr, nullptr,
+                      nullptr, nullptr};
+  return round_up(eb::attn_paged_ws_bytes(dt == EB_BF16, a));
+}
+
+eb_status eb_block_attn_paged(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, int hq,
+                              float scale, const void* q, const void* k_blk, const void* v_blk,
+                              void* out, void* ws, size_t ws_bytes, eb_stream_t stream) {
+  eb_status st = check_paged(dt, kv);
+  if (st != EB_OK) return st;
+  scale = attn_scale_or_default(scale, kv->head_dim);
+  // the cache stands in for k_pre and v_pre
+  st = check_attn(dt, r, hq, kv->hkv, kv->head_dim, scale, q, k_blk, v_blk, kv->k, kv->v, out);
+  if (st == EB_OK) st = check_paged_prefix(r, kv);
+  if (st != EB_OK) return st;
+  if (r->batch > kMaxGridYZ || static_cast<int64_t>(r->max_prefix) + r->max_block > kMaxKeys)
+    return fail(EB_ERR_UNSUPPORTED, "more than %d sequences or %d keys of a sequence", kMaxGridYZ,
+                kMaxKeys);
+  const size_t need = eb_block_attn_paged_workspace(dt, r, kv, hq);
+  if (ws_bytes < need || (need && !ws))
+    return fail(EB_ERR_WORKSPACE, "attention workspace %zu bytes < required %zu", ws_bytes, need);
+  st = check_device(r, true, nullptr, stream);
+  if (st == EB_OK && debug_checks()) st = check_cached_pages(r, kv, stream);
+  if (st != EB_OK) return st;
+  const eb::PagedAttnArgs a{r->batch, r->total_block, r->max_block, r->total_prefix,
+                            r->max_prefix, r->cu_block, r->cu_prefix, paged_args(kv), hq, scale,
+                            q, k_blk, v_blk, out};
+  return hip_status(eb::attn_paged(dt == EB_BF16, a, ws, stream), "eb_block_attn_paged launch");
 }
 
 size_t eb_lmhead_workspace(eb_dtype dt, int n_rows, int hidden, int vocab) {

@@ -48,6 +48,39 @@ size_t block_attn_ws_bytes(bool bf16, bool allow_split, int batch, int total_blo
 hipError_t block_attn(bool bf16, bool allow_split, const AttnArgs& a, void* ws, hipStream_t s,
                       bool defer_merge = false);
 
+// ---- paged cache ------------------------------------------------------------------------
+// The cache as the kernels see it (an eb_paged_kv whose fields have been checked).
+enum class CacheType { kF32, kBf16, kE4m3 };
+struct PagedKv {
+  CacheType type;
+  int hkv, head_dim;
+  int n_pages, page_shift, max_pages;  // page_size = 1 << page_shift
+  const int32_t* table;
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+};
+// bf16: the type of the rows outside the cache (else fp32); total: their number.
+hipError_t kv_write(bool bf16, const PagedKv& kv, int batch, int total, const int32_t* cu_block,
+                    const int32_t* cu_prefix, const int32_t* pos, const void* k, const void* v,
+                    hipStream_t s);
+hipError_t kv_read(bool bf16, const PagedKv& kv, int batch, int total, const int32_t* cu_prefix,
+                   void* k, void* v, hipStream_t s);
+
+struct PagedAttnArgs {
+  int batch, total_block, max_block, total_prefix, max_prefix;
+  const int32_t* cu_block;
+  const int32_t* cu_prefix;
+  PagedKv kv;
+  int hq;
+  float scale;
+  const void *q, *k_blk, *v_blk;
+  void* out;
+};
+size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a);
+hipError_t attn_paged(bool bf16, const PagedAttnArgs& a, void* ws, hipStream_t s);
+
 // LM-head partials and the block attention of `a` in one launch: the attention's workgroups are
 // queued behind the LM head's vocabulary slices (key-split partials in attn_ws, merged by
 // step_finish, which such a step always takes: its blocks have at most 64 rows x 256 slices).

@@ -1,0 +1,66 @@
+// The 8-bit values of a paged key/value cache, and the search for a packed row's sequence.
+#pragma once
+
+#include "eb_common.hpp"
+
+namespace eb {
+
+// 2^(s - 127) of a scale byte, 1 <= s <= 254.
+__device__ __forceinline__ float e8m0(uint32_t s) { return __uint_as_float(s << 23); }
+
+// Exponent of a row's scale from the bits of its largest finite magnitude a: the smallest e with
+// a <= 448 * 2^e (448 = 1.75 * 2^8 is the largest E4M3 value), kept in [-100, 120].  Within that
+// range 2^-e and every value of the row are ordinary fp32 and bf16 numbers.
+__device__ __forceinline__ int e4m3_exponent(uint32_t amax_bits) {
+  const int e = static_cast<int>(amax_bits >> 23) - 127 - 8 + ((amax_bits & 0x7fffffu) > 0x600000u);
+  return min(max(e, -100), 120);
+}
+
+// |x| as bits where x is finite, else 0.
+__device__ __forceinline__ uint32_t finite_mag(float x) {
+  const uint32_t m = __float_as_uint(x) & 0x7fffffffu;
+  return m < 0x7f800000u ? m : 0u;
+}
+
+// Four values times `inv` (a power of two, so the product is exact) as E4M3 bytes, rounded to
+// nearest even; infinities and NaN become NaN.
+__device__ __forceinline__ uint32_t pack4_e4m3(const float* x, float inv) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t b = __float_as_uint(x[i]);
+    y[i] = (b & 0x7fffffffu) < 0x7f800000u ? x[i] * inv : __uint_as_float(0x7fc00000u);
+  }
+  int w = 0;
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], w, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  return static_cast<uint32_t>(w);
+}
+
+// Two of four E4M3 bytes (the low two, or with kHigh the high two) times `scale` (a power of two)
+// as bf16, exactly; and as fp32.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <bool kHigh>
+__device__ __forceinline__ uint32_t e4m3_pair_bf16(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, kHigh));
+}
+template <bool kHigh>
+__device__ __forceinline__ f32x2 e4m3_pair_f32(uint32_t w, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, kHigh);
+}
+
+// The sequence that owns packed row `row` of a batch with offsets cu: the number of sequences that
+// end at or before it, found by the whole wavefront with one load per 64 sequences (`row` is
+// uniform).  At most batch - 1.
+__device__ __forceinline__ int find_sequence(const int32_t* cu, int batch, int row, int lane) {
+  int b = 0;
+  for (int b0 = 0; b0 < batch; b0 += 64) {
+    const bool before = b0 + lane < batch && cu[b0 + lane + 1] <= row;
+    const int n = __popcll(__ballot(before));
+    b += n;
+    if (n < 64) break;
+  }
+  return min(b, batch - 1);
+}
+
+}  // namespace eb
