@@ -5,6 +5,8 @@
 // block and a piece of 16 keys in one page (page sizes are multiples of 16); keys of the padding
 // get scores of -inf and values of zero, whatever the page holds there.
 #include "attn_common.hpp"
+#include "attn_merge.hpp"
+#include "attn_paged_few.hpp"
 #include "eb_common.hpp"
 #include "eb_internal.hpp"
 #include "paged.hpp"
@@ -273,12 +275,75 @@ hipError_t launch_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
   return hipGetLastError();
 }
 
+// ---- few query rows per K/V head, bf16 ----------------------------------------------------
+constexpr int kFewMaxRows = 64;
+#ifndef EB_FEW_TARGET
+#define EB_FEW_TARGET 1024
+#endif
+#ifndef EB_FEW_KEYS8
+#define EB_FEW_KEYS8 64
+#endif
+#ifndef EB_FEW_KEYS16
+#define EB_FEW_KEYS16 32
+#endif
+constexpr int kFewKeysE4m3 = EB_FEW_KEYS8, kFewKeysBf16 = EB_FEW_KEYS16;
+
+bool few_ok(bool bf16, const PagedAttnArgs& a) {
+  return bf16 && static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) <= kFewMaxRows;
+}
+int few_tiles(const PagedAttnArgs& a) {  // 16-row tiles per workgroup
+  return a.max_block * (a.hq / a.kv.hkv) <= kSmallTile ? 1 : 2;
+}
+int few_row_tiles(const PagedAttnArgs& a) {
+  const int per = few_tiles(a) * kSmallTile;
+  return (a.max_block * (a.hq / a.kv.hkv) + per - 1) / per;
+}
+int few_stage(const PagedAttnArgs& a) {
+  return kFewWaves * (a.kv.type == CacheType::kE4m3 ? kFewKeysE4m3 : kFewKeysBf16);
+}
+
+SplitPlan few_plan(const PagedAttnArgs& a) {
+  const long stage = few_stage(a), per_key = static_cast<long>(a.kv.hkv) * few_row_tiles(a);
+  const long keys = (a.max_prefix + stage - 1) / stage * stage + a.max_block;
+  const long base = per_key * a.batch;
+  long kps = a.total_prefix * per_key / EB_FEW_TARGET;
+  // no more ranges than eight times what equally long sequences would get
+  kps = max(kps, keys / (8 * (EB_FEW_TARGET / base + 1)));
+  kps = max(stage, (kps + stage - 1) / stage * stage);
+  return SplitPlan{static_cast<int>((keys + kps - 1) / kps), static_cast<int>(kps)};
+}
+
+template <int D, bool kE4m3, int kTiles>
+hipError_t launch_few(const PagedAttnArgs& a, void* ws, hipStream_t s) {
+  constexpr int kKeysPer = kE4m3 ? kFewKeysE4m3 : kFewKeysBf16;
+  const SplitPlan sp = few_plan(a);
+  const AttnArgs dense{a.batch, a.total_block, a.max_block, a.total_prefix, a.max_prefix,
+                       a.cu_block, a.cu_prefix, a.hq, a.kv.hkv, D, a.scale, a.q, a.k_blk, a.v_blk,
+                       nullptr, nullptr, a.out};
+  FewParams p{attn_params(dense, sp, ws), a.kv, few_row_tiles(a), a.batch * sp.nsplit * a.kv.hkv};
+  p.a.prefix_mask = kFewWaves * kKeysPer - 1;
+  const dim3 grid(static_cast<unsigned>(8 * ((p.units + 7) / 8) * p.row_tiles));
+  hipLaunchKernelGGL((attn_paged_few_kernel<D, kE4m3, kKeysPer, kTiles>), grid,
+                     dim3(kFewWaves * 64), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sp.nsplit == 1) return e;
+  launch_merge<D>(p.a, a.total_block, a.batch, s);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_few_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
+  const bool e4m3 = a.kv.type == CacheType::kE4m3;
+  if (few_tiles(a) == 1)
+    return e4m3 ? launch_few<D, true, 1>(a, ws, s) : launch_few<D, false, 1>(a, ws, s);
+  return e4m3 ? launch_few<D, true, 2>(a, ws, s) : launch_few<D, false, 2>(a, ws, s);
+}
+
 }  // namespace
 
 size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
-  (void)bf16;
   if (a.total_block == 0 || a.max_block == 0) return 0;
-  const SplitPlan sp = any_plan(a);
+  const SplitPlan sp = few_ok(bf16, a) ? few_plan(a) : any_plan(a);
   if (sp.nsplit == 1) return 0;
   return static_cast<size_t>(a.total_block) * a.hq * sp.nsplit * (a.kv.head_dim + 2) *
          sizeof(float);
@@ -286,6 +351,8 @@ size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
 
 hipError_t attn_paged(bool bf16, const PagedAttnArgs& a, void* ws, hipStream_t s) {
   if (a.total_block == 0 || a.max_block == 0) return hipSuccess;
+  if (few_ok(bf16, a))
+    return a.kv.head_dim == 128 ? launch_few_any<128>(a, ws, s) : launch_few_any<64>(a, ws, s);
   const bool e4m3 = a.kv.type == CacheType::kE4m3;
   if (a.kv.head_dim == 128) {
     if (bf16) return e4m3 ? launch_any<128, uint16_t, uint8_t>(a, ws, s)
