@@ -7,6 +7,7 @@
 #include "attn_common.hpp"
 #include "attn_merge.hpp"
 #include "attn_paged_few.hpp"
+#include "attn_tiles.hpp"
 #include "eb_common.hpp"
 #include "eb_internal.hpp"
 #include "paged.hpp"
@@ -17,18 +18,18 @@ namespace {
 // ---------------------------------------------------------------------------------------
 // fp32 arithmetic throughout, on 16x16x4 fp32 MFMAs.
 //
-// A workgroup of kAnyWaves wavefronts per (16 query rows, K/V head, sequence, key range).  Wave w
-// takes the 16-key chunks w, w + kAnyWaves, ... of the range with an online softmax of its own; the
+// A workgroup of kPf32Waves wavefronts per (16 query rows, K/V head, sequence, key range).  Wave w
+// takes the 16-key chunks w, w + kPf32Waves, ... of the range with an online softmax of its own; the
 // waves' results are merged through LDS and, with a key split, the ranges' by a second kernel.
 // Scores are formed transposed, S^T = K Q^T: lane l owns query l % 16 and holds keys 4 (l / 16) + r
 // of the chunk, which are the k-slots of the B operand of O^T = V^T P^T, one register per MFMA.
 // ---------------------------------------------------------------------------------------
-constexpr int kAnyWaves = 8;
-constexpr int kAnyRows = 16;
-constexpr int kAnyKeys = 16;
-constexpr int kAnyStage = kAnyWaves * kAnyKeys;  // keys that the waves take in one go
+constexpr int kPf32Waves = 8;
+constexpr int kPf32Rows = 16;
+constexpr int kPf32Keys = 16;
+constexpr int kPf32Stage = kPf32Waves * kPf32Keys;  // keys that the waves take in one go
 
-struct PagedParams {
+struct PagedF32Params {
   PagedKv kv;
   const int32_t* cu_block;
   const int32_t* cu_prefix;
@@ -51,8 +52,6 @@ __device__ __forceinline__ float widen(T x);
 template <>
 __device__ __forceinline__ float widen<float>(float x) { return x; }
 template <>
-__device__ __forceinline__ float widen<uint16_t>(uint16_t x) { return bf16_bits_to_f32(x); }
-template <>
 __device__ __forceinline__ float widen<uint8_t>(uint8_t x) { return e4m3_pair_f32<false>(x, 1.f)[0]; }
 
 template <class T>
@@ -62,33 +61,24 @@ __device__ __forceinline__ f32x4 widen4<float>(const float* p) {
   return *reinterpret_cast<const f32x4u*>(p);
 }
 template <>
-__device__ __forceinline__ f32x4 widen4<uint16_t>(const uint16_t* p) {
-  const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-  return f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u),
-               __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
-}
-template <>
 __device__ __forceinline__ f32x4 widen4<uint8_t>(const uint8_t* p) {
   const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
   const f32x2 a = e4m3_pair_f32<false>(w, 1.f), b = e4m3_pair_f32<true>(w, 1.f);
   return f32x4{a[0], a[1], b[0], b[1]};
 }
-__device__ __forceinline__ void store_row(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store_row(uint16_t* p, float x) { *p = f32_to_bf16_bits_rne(x); }
-
-template <int D, class T, class C>
-__global__ __launch_bounds__(kAnyWaves * 64) void attn_paged_any_kernel(PagedParams p) {
+template <int D, class C>
+__global__ __launch_bounds__(kPf32Waves * 64) void attn_paged_f32_kernel(PagedF32Params p) {
   constexpr int kChunks = D / 16;
   constexpr int kPitch = D + 4;
-  __shared__ __attribute__((aligned(16))) float s_o[kAnyWaves][kAnyRows * kPitch];
-  __shared__ float s_m[kAnyWaves][kAnyRows], s_l[kAnyWaves][kAnyRows];
+  __shared__ __attribute__((aligned(16))) float s_o[kPf32Waves][kPf32Rows * kPitch];
+  __shared__ float s_m[kPf32Waves][kPf32Rows], s_l[kPf32Waves][kPf32Rows];
   const int tile = blockIdx.x % p.tiles, sp = blockIdx.x / p.tiles, g = blockIdx.y, b = blockIdx.z;
-  const int row0 = tile * kAnyRows;
+  const int row0 = tile * kPf32Rows;
   const int bbeg = p.cu_block[b], len = p.cu_block[b + 1] - bbeg;
   const int G = p.group, n_rows = len * G;
   if (row0 >= n_rows) return;  // whole workgroup
   const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
-  const int cached = (plen + kAnyKeys - 1) / kAnyKeys * kAnyKeys;  // the block's first key
+  const int cached = (plen + kPf32Keys - 1) / kPf32Keys * kPf32Keys;  // the block's first key
   const int n_keys = cached + len;
   const int kbeg = sp * p.kps;
   if (kbeg >= n_keys) return;  // whole workgroup
@@ -101,17 +91,17 @@ __global__ __launch_bounds__(kAnyWaves * 64) void attn_paged_any_kernel(PagedPar
   };
 
   f32x4 qf[kChunks], o[kChunks];
-  const T* q = static_cast<const T*>(p.q) + row_at(l16) * D + 4 * grp;
+  const float* q = static_cast<const float*>(p.q) + row_at(l16) * D + 4 * grp;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) qf[c] = widen4(q + 16 * c), o[c] = f32x4{};
   // from the lowest finite value on: keys with scores of -inf have weights of zero
   float m_run = -3.402823466e38f, l_run = 0.f;
-  for (int k0 = kbeg + wave * kAnyKeys; k0 < kend; k0 += kAnyStage) {
+  for (int k0 = kbeg + wave * kPf32Keys; k0 < kend; k0 += kPf32Stage) {
     f32x4 kf[kChunks];
     float vf[4][kChunks];  // V of key k0 + 4 grp + r at d = 16 c + l16
     int valid;             // keys of this chunk
     if (k0 < cached) {
-      valid = min(kAnyKeys, plen - k0);
+      valid = min(kPf32Keys, plen - k0);
       int page = p.kv.table[static_cast<size_t>(b) * p.kv.max_pages + (k0 >> p.kv.page_shift)];
       const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(p.kv.n_pages);
       page = ok ? page : 0;
@@ -138,19 +128,19 @@ __global__ __launch_bounds__(kAnyWaves * 64) void attn_paged_any_kernel(PagedPar
       }
     } else {
       const int j0 = k0 - cached;
-      valid = min(kAnyKeys, len - j0);
+      valid = min(kPf32Keys, len - j0);
       const size_t kr = static_cast<size_t>(bbeg + j0 + min(l16, valid - 1)) * p.kv.hkv + g;
-      const T* kp = static_cast<const T*>(p.k_blk) + kr * D + 4 * grp;
+      const float* kp = static_cast<const float*>(p.k_blk) + kr * D + 4 * grp;
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) kf[c] = widen4(kp + 16 * c);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const size_t vr =
             static_cast<size_t>(bbeg + j0 + min(4 * grp + r, valid - 1)) * p.kv.hkv + g;
-        const T* vp = static_cast<const T*>(p.v_blk) + vr * D + l16;
+        const float* vp = static_cast<const float*>(p.v_blk) + vr * D + l16;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
-          vf[r][c] = 4 * grp + r < valid ? widen<T>(vp[16 * c]) : 0.f;
+          vf[r][c] = 4 * grp + r < valid ? vp[16 * c] : 0.f;
       }
     }
     f32x4 acc[2] = {f32x4{}, f32x4{}};
@@ -192,15 +182,15 @@ __global__ __launch_bounds__(kAnyWaves * 64) void attn_paged_any_kernel(PagedPar
     *reinterpret_cast<f32x4*>(&s_o[wave][l16 * kPitch + 16 * c + 4 * grp]) = o[c];
   __syncthreads();
   // merge in wave order; a wave without keys has l = 0 and o = 0
-  for (int i = tid; i < kAnyRows * D; i += kAnyWaves * 64) {
+  for (int i = tid; i < kPf32Rows * D; i += kPf32Waves * 64) {
     const int r = i / D, d = i % D;
     if (row0 + r >= n_rows) break;
     float m = s_m[0][r];
 #pragma unroll
-    for (int w = 1; w < kAnyWaves; ++w) m = fmaxf(m, s_m[w][r]);
+    for (int w = 1; w < kPf32Waves; ++w) m = fmaxf(m, s_m[w][r]);
     float l = 0.f, x = 0.f;
 #pragma unroll
-    for (int w = 0; w < kAnyWaves; ++w) {
+    for (int w = 0; w < kPf32Waves; ++w) {
       const float f = expf(s_m[w][r] - m);
       l = fmaf(f, s_l[w][r], l);
       x = fmaf(f, s_o[w][r * kPitch + d], x);
@@ -210,14 +200,14 @@ __global__ __launch_bounds__(kAnyWaves * 64) void attn_paged_any_kernel(PagedPar
       p.o_part[(at * p.nsplit + sp) * D + d] = x;
       if (d == 0) p.m_part[at * p.nsplit + sp] = m, p.l_part[at * p.nsplit + sp] = l;
     } else {
-      store_row(static_cast<T*>(p.out) + at * D + d, x / l);
+      static_cast<float*>(p.out)[at * D + d] = x / l;
     }
   }
 }
 
 // The ranges of one (block row, query head) per wavefront, in order.
-template <int D, class T>
-__global__ __launch_bounds__(256) void attn_paged_any_merge_kernel(PagedParams p, int batch,
+template <int D>
+__global__ __launch_bounds__(256) void attn_paged_f32_merge_kernel(PagedF32Params p, int batch,
                                                                    int total) {
   constexpr int kPer = D / 64;
   const long rh = static_cast<long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
@@ -225,7 +215,7 @@ __global__ __launch_bounds__(256) void attn_paged_any_merge_kernel(PagedParams p
   if (rh >= static_cast<long>(total) * p.hq) return;  // uniform per wavefront
   const int b = find_sequence(p.cu_block, batch, static_cast<int>(rh / p.hq), lane);
   const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
-  const int n_keys = (plen + kAnyKeys - 1) / kAnyKeys * kAnyKeys + p.cu_block[b + 1] - p.cu_block[b];
+  const int n_keys = (plen + kPf32Keys - 1) / kPf32Keys * kPf32Keys + p.cu_block[b + 1] - p.cu_block[b];
   const int n = min(p.nsplit, (n_keys + p.kps - 1) / p.kps);
   const size_t base = static_cast<size_t>(rh) * p.nsplit;
   float m = -INFINITY, l = 0.f, x[kPer] = {};
@@ -240,37 +230,37 @@ __global__ __launch_bounds__(256) void attn_paged_any_merge_kernel(PagedParams p
   }
 #pragma unroll
   for (int e = 0; e < kPer; ++e)
-    store_row(static_cast<T*>(p.out) + rh * D + lane * kPer + e, x[e] / l);
+    static_cast<float*>(p.out)[rh * D + lane * kPer + e] = x[e] / l;
 }
 
 // Ranges of whole stages, enough for two workgroups per compute unit.
-SplitPlan any_plan(const PagedAttnArgs& a) {
-  const long tiles = (static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) + kAnyRows - 1) / kAnyRows;
+SplitPlan f32_plan(const PagedAttnArgs& a) {
+  const long tiles = (static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) + kPf32Rows - 1) / kPf32Rows;
   const long base = tiles * a.kv.hkv * a.batch;
-  const int keys = (a.max_prefix + kAnyKeys - 1) / kAnyKeys * kAnyKeys + a.max_block;
-  const int stages = (keys + kAnyStage - 1) / kAnyStage;
+  const int keys = (a.max_prefix + kPf32Keys - 1) / kPf32Keys * kPf32Keys + a.max_block;
+  const int stages = (keys + kPf32Stage - 1) / kPf32Stage;
   const int want = static_cast<int>(max(1L, min((512 + base - 1) / base, static_cast<long>(stages))));
   const int per = (stages + want - 1) / want;
-  return SplitPlan{(stages + per - 1) / per, per * kAnyStage};
+  return SplitPlan{(stages + per - 1) / per, per * kPf32Stage};
 }
 
-template <int D, class T, class C>
-hipError_t launch_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
-  const SplitPlan sp = any_plan(a);
+template <int D, class C>
+hipError_t launch_f32(const PagedAttnArgs& a, void* ws, hipStream_t s) {
+  const SplitPlan sp = f32_plan(a);
   const size_t n = static_cast<size_t>(a.total_block) * a.hq * sp.nsplit;
   float* o = static_cast<float*>(ws);
   const int group = a.hq / a.kv.hkv;
-  const int tiles = static_cast<int>((static_cast<long>(a.max_block) * group + kAnyRows - 1) /
-                                     kAnyRows);
-  const PagedParams p{a.kv, a.cu_block, a.cu_prefix, a.hq, group, tiles, a.scale, a.q, a.k_blk,
+  const int tiles = static_cast<int>((static_cast<long>(a.max_block) * group + kPf32Rows - 1) /
+                                     kPf32Rows);
+  const PagedF32Params p{a.kv, a.cu_block, a.cu_prefix, a.hq, group, tiles, a.scale, a.q, a.k_blk,
                       a.v_blk, a.out, sp.nsplit, sp.kps, o, o + n * D, o + n * D + n};
   const dim3 grid(static_cast<unsigned>(tiles * sp.nsplit), static_cast<unsigned>(a.kv.hkv),
                   static_cast<unsigned>(a.batch));
-  hipLaunchKernelGGL((attn_paged_any_kernel<D, T, C>), grid, dim3(kAnyWaves * 64), 0, s, p);
+  hipLaunchKernelGGL((attn_paged_f32_kernel<D, C>), grid, dim3(kPf32Waves * 64), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.nsplit == 1) return e;
   const long pairs = static_cast<long>(a.total_block) * a.hq;
-  hipLaunchKernelGGL((attn_paged_any_merge_kernel<D, T>), dim3(static_cast<unsigned>((pairs + 3) / 4)),
+  hipLaunchKernelGGL((attn_paged_f32_merge_kernel<D>), dim3(static_cast<unsigned>((pairs + 3) / 4)),
                      dim3(256), 0, s, p, a.batch, a.total_block);
   return hipGetLastError();
 }
@@ -313,14 +303,18 @@ SplitPlan few_plan(const PagedAttnArgs& a) {
   return SplitPlan{static_cast<int>((keys + kps - 1) / kps), static_cast<int>(kps)};
 }
 
+// The call as one on packed rows whose prefix is empty, for what the kernels share.
+AttnArgs packed_args(const PagedAttnArgs& a) {
+  return AttnArgs{a.batch, a.total_block, a.max_block, a.total_prefix, a.max_prefix, a.cu_block,
+                  a.cu_prefix, a.hq, a.kv.hkv, a.kv.head_dim, a.scale, a.q, a.k_blk, a.v_blk,
+                  nullptr, nullptr, a.out};
+}
+
 template <int D, bool kE4m3, int kTiles>
 hipError_t launch_few(const PagedAttnArgs& a, void* ws, hipStream_t s) {
   constexpr int kKeysPer = kE4m3 ? kFewKeysE4m3 : kFewKeysBf16;
   const SplitPlan sp = few_plan(a);
-  const AttnArgs dense{a.batch, a.total_block, a.max_block, a.total_prefix, a.max_prefix,
-                       a.cu_block, a.cu_prefix, a.hq, a.kv.hkv, D, a.scale, a.q, a.k_blk, a.v_blk,
-                       nullptr, nullptr, a.out};
-  FewParams p{attn_params(dense, sp, ws), a.kv, few_row_tiles(a), a.batch * sp.nsplit * a.kv.hkv};
+  FewParams p{attn_params(packed_args(a), sp, ws), a.kv, few_row_tiles(a), a.batch * sp.nsplit * a.kv.hkv};
   p.a.prefix_mask = kFewWaves * kKeysPer - 1;
   const dim3 grid(static_cast<unsigned>(8 * ((p.units + 7) / 8) * p.row_tiles));
   hipLaunchKernelGGL((attn_paged_few_kernel<D, kE4m3, kKeysPer, kTiles>), grid,
@@ -339,11 +333,40 @@ hipError_t launch_few_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
   return e4m3 ? launch_few<D, true, 2>(a, ws, s) : launch_few<D, false, 2>(a, ws, s);
 }
 
+// ---- many query rows, bf16: the tile kernels of the packed prefix ---------------------------
+SplitPlan tiles_plan(const PagedAttnArgs& a) {
+  const int keys = (a.max_prefix + kKeys - 1) / kKeys * kKeys + a.max_block;
+  return split_plan(a.batch, a.max_block, keys, a.hq, a.kv.hkv);
+}
+
+template <int D, bool kE4m3>
+hipError_t launch_tiles(const PagedAttnArgs& a, void* ws, hipStream_t s) {
+  const SplitPlan sp = tiles_plan(a);
+  AttnParams p = attn_params(packed_args(a), sp, ws);
+  p.prefix_mask = kKeys - 1;
+  const PagedKeys<kE4m3> keys{a.kv};
+  const long rows = static_cast<long>(a.max_block) * p.group;
+  const int row_tiles = static_cast<int>((rows + kRowsPerWg - 1) / kRowsPerWg);
+  const int units = a.batch * sp.nsplit * a.kv.hkv;
+  const dim3 grid(
+      static_cast<unsigned>(kXcdCount * ((units + kXcdCount - 1) / kXcdCount) * row_tiles));
+  if constexpr (D == 128 && !kE4m3)
+    hipLaunchKernelGGL(attn_bf16_d128_kernel<PagedKeys<kE4m3>>, grid, dim3(kThreads), 0, s, p, keys,
+                       row_tiles, units);
+  else
+    hipLaunchKernelGGL((attn_bf16_kernel<D, PagedKeys<kE4m3>>), grid, dim3(kThreads), 0, s, p, keys,
+                       row_tiles, units);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sp.nsplit == 1) return e;
+  launch_merge<D>(p, a.total_block, a.batch, s);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
   if (a.total_block == 0 || a.max_block == 0) return 0;
-  const SplitPlan sp = few_ok(bf16, a) ? few_plan(a) : any_plan(a);
+  const SplitPlan sp = few_ok(bf16, a) ? few_plan(a) : bf16 ? tiles_plan(a) : f32_plan(a);
   if (sp.nsplit == 1) return 0;
   return static_cast<size_t>(a.total_block) * a.hq * sp.nsplit * (a.kv.head_dim + 2) *
          sizeof(float);
@@ -355,13 +378,11 @@ hipError_t attn_paged(bool bf16, const PagedAttnArgs& a, void* ws, hipStream_t s
     return a.kv.head_dim == 128 ? launch_few_any<128>(a, ws, s) : launch_few_any<64>(a, ws, s);
   const bool e4m3 = a.kv.type == CacheType::kE4m3;
   if (a.kv.head_dim == 128) {
-    if (bf16) return e4m3 ? launch_any<128, uint16_t, uint8_t>(a, ws, s)
-                          : launch_any<128, uint16_t, uint16_t>(a, ws, s);
-    return e4m3 ? launch_any<128, float, uint8_t>(a, ws, s) : launch_any<128, float, float>(a, ws, s);
+    if (bf16) return e4m3 ? launch_tiles<128, true>(a, ws, s) : launch_tiles<128, false>(a, ws, s);
+    return e4m3 ? launch_f32<128, uint8_t>(a, ws, s) : launch_f32<128, float>(a, ws, s);
   }
-  if (bf16) return e4m3 ? launch_any<64, uint16_t, uint8_t>(a, ws, s)
-                        : launch_any<64, uint16_t, uint16_t>(a, ws, s);
-  return e4m3 ? launch_any<64, float, uint8_t>(a, ws, s) : launch_any<64, float, float>(a, ws, s);
+  if (bf16) return e4m3 ? launch_tiles<64, true>(a, ws, s) : launch_tiles<64, false>(a, ws, s);
+  return e4m3 ? launch_f32<64, uint8_t>(a, ws, s) : launch_f32<64, float>(a, ws, s);
 }
 
 }  // namespace eb
