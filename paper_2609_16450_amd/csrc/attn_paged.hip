@@ -350,7 +350,7 @@ hipError_t launch_tiles(const PagedAttnArgs& a, void* ws, hipStream_t s) {
   const int units = a.batch * sp.nsplit * a.kv.hkv;
   const dim3 grid(
       static_cast<unsigned>(kXcdCount * ((units + kXcdCount - 1) / kXcdCount) * row_tiles));
-  if constexpr (D == 128 && !kE4m3)
+  if constexpr (D == 128)
     hipLaunchKernelGGL(attn_bf16_d128_kernel<PagedKeys<kE4m3>>, grid, dim3(kThreads), 0, s, p, keys,
                        row_tiles, units);
   else

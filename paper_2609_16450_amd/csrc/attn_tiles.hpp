@@ -447,8 +447,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
   constexpr int kInstPerTile = kTileBytes / 1024;            // 1 KB per load instruction
   constexpr int kInstPerWave = 2 * kInstPerTile / (kThreads / 64);
   static_assert(kInstPerTile % kInstPerWave == 0, "a wave loads K or V, not both");
-  constexpr int kPreK = 3;  // K fragment reads issued this many MFMAs ahead
-  constexpr int kPreV = 3;  // V fragment reads issued this many MFMAs ahead
+  // K and V fragment reads are issued this many MFMAs ahead (one less where a tile waits in
+  // registers: a third would spill)
+  constexpr int kPreK = Keys::kE4m3 ? 2 : 3;
+  constexpr int kPreV = Keys::kE4m3 ? 2 : 3;
   // K tiles in slots 0, 1; V tiles in slots 2, 3
   __shared__ __attribute__((aligned(16))) uint8_t smem[4 * kTileBytes];
 
@@ -515,15 +517,19 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
       plen > 0 ? (k_wave ? p.k_pre : p.v_pre) + (static_cast<size_t>(pbeg) * p.hkv + g) * D : blk0);
   const __amdgpu_buffer_rsrc_t rs_suf = make_rsrc(
       slen > 0 ? (k_wave ? p.k_suf : p.v_suf) + (static_cast<size_t>(sbeg) * p.hkv + g) * D : blk0);
+  // slot of a chunk in tile row 4 n + lane / 16 (n mod 4 = i): XORed with this
+  auto swz = [&](int lane_, int i) {
+    const int r = 4 * (i & 3) + (lane_ >> 4);
+    return k_wave ? r : 4 * (r & 3);
+  };
   int lrow[kInstPerWave];       // tile row this lane fills in instruction i
   uint32_t coff[kInstPerWave];  // byte offset of the global chunk it fetches within the row
 #pragma unroll
   for (int i = 0; i < kInstPerWave; ++i) {
     const int n = (wave * kInstPerWave + i) % kInstPerTile;
     const int r = 4 * n + (lane >> 4);
-    const int swz = k_wave ? (r & 15) : 4 * (r & 3);
     lrow[i] = r;
-    coff[i] = 16u * static_cast<uint32_t>((lane & 15) ^ swz);
+    coff[i] = 16u * static_cast<uint32_t>((lane & 15) ^ swz(lane, n));
   }
   // This wave's half (K or V) of the tile of keys kv0 .. kv0 + 63 into dst.  Keys past kend come
   // from a clamped, valid row; their scores are set to -inf.
@@ -536,9 +542,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
       // rows past it arrive as zeros.
       const uint8_t* const pool = k_wave ? keys.kv.k : keys.kv.v;
       const uint8_t* const blk = reinterpret_cast<const uint8_t*>(k_wave ? p.k_blk : p.v_blk);
-      const bool paged = kv0 < cached;
+      const bool paged = !Keys::kE4m3 && kv0 < cached;  // 8-bit tiles: fetch and place
       const uint32_t stride = paged ? kRowBytes : key_bytes;
-      const uint32_t row_off = static_cast<uint32_t>(lane >> 4) * stride;
+      int lane_ = lane;
+      if constexpr (Keys::kE4m3) asm volatile("" : "+v"(lane_));  // (as in place)
+      const uint32_t row_off = static_cast<uint32_t>(lane_ >> 4) * stride;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int at = kv0 + 32 * (wave & 1) + 16 * h;
@@ -566,7 +574,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
           const int n = (wave * kInstPerWave + 4 * h + i) % kInstPerTile;
           buffer_load_to_lds(make_rsrc(base + 4 * i * static_cast<size_t>(stride),
                                        max(bytes - 4 * i * static_cast<int>(stride), 0)),
-                             dst + n * 1024, row_off + coff[4 * h + i], 0);
+                             dst + n * 1024,
+                             row_off + 16u * static_cast<uint32_t>((lane_ & 15) ^ swz(lane_, i)), 0);
         }
       }
       return;
@@ -594,6 +603,57 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
       else
         buffer_load_to_lds(rs_suf, dst + n * 1024,
                            static_cast<uint32_t>(j - plen - len) * key_bytes + coff[i], 0);
+    }
+  };
+  // Tiles of an 8-bit cache go through registers: fetch() loads this wave's half of a tile (four
+  // loads of 16 bytes per lane, 8 rows each, and the scales of the lane's two rows per group of 16),
+  // an iteration later place() widens it to bf16, exactly, and stores it where the loads into LDS
+  // would have put it.
+  constexpr int kRawLoads = 4;
+  [[maybe_unused]] u32x4 raw[kRawLoads];
+  [[maybe_unused]] uint32_t raw_scale[2];
+  auto fetch = [&](int kv0) {
+    if constexpr (Keys::kE4m3) {
+      if (kv0 >= cached) return;
+      const uint8_t* const pool = k_wave ? keys.kv.k : keys.kv.v;
+      const uint8_t* const scale = k_wave ? keys.kv.k_scale : keys.kv.v_scale;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = kv0 + 32 * (wave & 1) + 16 * h;
+        const int entry = at >> keys.kv.page_shift;
+        window.advance(entry, lane);
+        const int page = window.uniform(entry);
+        const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(keys.kv.n_pages);
+        const size_t row = ((static_cast<size_t>(ok ? page : 0) * p.hkv + g) << keys.kv.page_shift) +
+                           (at & ((1 << keys.kv.page_shift) - 1));
+        const int rows = ok ? min(max(plen - at, 0), 16) : 0;
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(pool + row * D, rows * D);
+        // load i of the group: rows 2 (lane / 8) + i
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          raw[2 * h + i] = buffer_load16(rs, (2 * (lane >> 3) + i) * D + 16 * (lane & 7));
+        raw_scale[h] = buffer_load2(make_rsrc(scale + row, (rows + 1) & ~1), 2 * (lane >> 3));
+      }
+    }
+  };
+  auto place = [&](int kv0, uint8_t* dst) {
+    if (kv0 >= cached) {
+      issue(kv0, dst);
+      return;
+    }
+    int lane_ = lane;  // addresses formed anew per tile: kept over the loop they would spill
+    asm volatile("" : "+v"(lane_));
+#pragma unroll
+    for (int j = 0; j < kRawLoads; ++j) {
+      const int r = 32 * (wave & 1) + 16 * (j / 2) + 2 * (lane_ >> 3) + j % 2;
+      const int to = k_wave ? (r & 15) : 4 * (r & 3);
+      uint32_t s8 = j % 2 ? raw_scale[j / 2] >> 8 : raw_scale[j / 2] & 0xff;
+      if (kv0 + kDmaKeys > plen && kv0 + r >= plen) s8 = 0;  // the row's values are zeros as well
+      u32x4 lo, hi;
+      e4m3_widen(raw[j], e8m0(s8), lo, hi);
+      const int c = 2 * (lane_ & 7);
+      *reinterpret_cast<u32x4*>(dst + r * kRowBytes + 16 * (c ^ to)) = lo;
+      *reinterpret_cast<u32x4*>(dst + r * kRowBytes + 16 * ((c + 1) ^ to)) = hi;
     }
   };
   auto ktile = [&](int i) { return smem + (i & 1) * kTileBytes; };
@@ -647,7 +707,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
 
   const int n_stages = (kend - kbeg + kDmaKeys - 1) / kDmaKeys;
   // prologue: K(0), K(1), V(0); then S(0) and its maximum
-  if (k_wave) {
+  auto tile_at = [&](int st) { return kbeg + st * kDmaKeys; };
+  if constexpr (Keys::kE4m3) {
+    fetch(tile_at(0));
+    place(tile_at(0), k_wave ? ktile(0) : vtile(0));
+    if (n_stages > 1) fetch(tile_at(1));
+    if (k_wave && n_stages > 1) {
+      place(tile_at(1), ktile(1));
+      if (n_stages > 2) fetch(tile_at(2));
+    }
+  } else if (k_wave) {
     issue(kbeg, ktile(0));
     if (n_stages > 1) issue(kbeg + kDmaKeys, ktile(1));
   } else {
@@ -666,7 +735,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
     // this wave's loads of K(st + 1) and V(st) have landed; after the barrier every wave's
     // have, and every wave is done with K(st) and V(st - 1)
     wait_vm_lds_and_barrier<0>();
-    if (k_wave) {
+    if constexpr (Keys::kE4m3) {
+      const int to = st + (k_wave ? 2 : 1);  // the tile in the registers
+      if (to < n_stages) place(tile_at(to), k_wave ? ktile(st) : vtile(st + 1));
+      if (to + 1 < n_stages) fetch(tile_at(to + 1));
+    } else if (k_wave) {
       if (st + 2 < n_stages) issue(kbeg + (st + 2) * kDmaKeys, ktile(st));
     } else {
       if (st + 1 < n_stages) issue(kbeg + (st + 1) * kDmaKeys, vtile(st + 1));

@@ -49,6 +49,26 @@ __device__ __forceinline__ f32x2 e4m3_pair_f32(uint32_t w, float scale) {
   return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, kHigh);
 }
 
+// Sixteen bytes per lane, two, or one, at byte `off` of a buffer; zeros past its end.  In functions of
+// their own, like every builtin that the host pass does not know.
+__device__ __forceinline__ u32x4 buffer_load16(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
+  return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
+}
+__device__ __forceinline__ uint32_t buffer_load1(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
+  return __builtin_amdgcn_raw_buffer_load_b8(rs, off, 0, 0);
+}
+__device__ __forceinline__ uint32_t buffer_load2(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
+  return __builtin_amdgcn_raw_buffer_load_b16(rs, off, 0, 0);
+}
+
+// Sixteen E4M3 values times `scale` as sixteen bf16.
+__device__ __forceinline__ void e4m3_widen(u32x4 w, float scale, u32x4& lo, u32x4& hi) {
+  lo = u32x4{e4m3_pair_bf16<false>(w[0], scale), e4m3_pair_bf16<true>(w[0], scale),
+             e4m3_pair_bf16<false>(w[1], scale), e4m3_pair_bf16<true>(w[1], scale)};
+  hi = u32x4{e4m3_pair_bf16<false>(w[2], scale), e4m3_pair_bf16<true>(w[2], scale),
+             e4m3_pair_bf16<false>(w[3], scale), e4m3_pair_bf16<true>(w[3], scale)};
+}
+
 // The sequence that owns packed row `row` of a batch with offsets cu: the number of sequences that
 // end at or before it, found by the whole wavefront with one load per 64 sequences (`row` is
 // uniform).  At most batch - 1.
