@@ -267,16 +267,9 @@ hipError_t launch_f32(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 
 // ---- few query rows per K/V head, bf16 ----------------------------------------------------
 constexpr int kFewMaxRows = 64;
-#ifndef EB_FEW_TARGET
-#define EB_FEW_TARGET 1024
-#endif
-#ifndef EB_FEW_KEYS8
-#define EB_FEW_KEYS8 64
-#endif
-#ifndef EB_FEW_KEYS16
-#define EB_FEW_KEYS16 32
-#endif
-constexpr int kFewKeysE4m3 = EB_FEW_KEYS8, kFewKeysBf16 = EB_FEW_KEYS16;
+constexpr int kFewKeys = 32;  // keys of a piece
+constexpr int kFewStage = kFewWaves * kFewKeys;
+constexpr int kFewMaxBatch = 2048;
 
 bool few_ok(bool bf16, const PagedAttnArgs& a) {
   return bf16 && static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) <= kFewMaxRows;
@@ -284,23 +277,35 @@ bool few_ok(bool bf16, const PagedAttnArgs& a) {
 int few_tiles(const PagedAttnArgs& a) {  // 16-row tiles per workgroup
   return a.max_block * (a.hq / a.kv.hkv) <= kSmallTile ? 1 : 2;
 }
-int few_row_tiles(const PagedAttnArgs& a) {
-  const int per = few_tiles(a) * kSmallTile;
-  return (a.max_block * (a.hq / a.kv.hkv) + per - 1) / per;
-}
-int few_stage(const PagedAttnArgs& a) {
-  return kFewWaves * (a.kv.type == CacheType::kE4m3 ? kFewKeysE4m3 : kFewKeysBf16);
-}
 
-SplitPlan few_plan(const PagedAttnArgs& a) {
-  const long stage = few_stage(a), per_key = static_cast<long>(a.kv.hkv) * few_row_tiles(a);
-  const long keys = (a.max_prefix + stage - 1) / stage * stage + a.max_block;
-  const long base = per_key * a.batch;
-  long kps = a.total_prefix * per_key / EB_FEW_TARGET;
-  // no more ranges than eight times what equally long sequences would get
-  kps = max(kps, keys / (8 * (EB_FEW_TARGET / base + 1)));
-  kps = max(stage, (kps + stage - 1) / stage * stage);
-  return SplitPlan{static_cast<int>((keys + kps - 1) / kps), static_cast<int>(kps)};
+// The line of stages (attn_paged_few.hpp) in as many equal parts as workgroups that run at a time,
+// two per compute unit: one round, and all of it ends together.  Ranges of equal length for every
+// sequence, 1024 workgroups of them, took as long as their last round: 64 tokens behind 501 to 8192
+// rows 143 against 110 us (bf16), 256 behind 100 to 4000 rows 278 against 222 us, 32 blocks of 8
+// behind 1001 to 8192 rows (8 bits) 92 against 76 us (28/4 heads x 128).  768 or 1024 parts: 0-15%
+// slower.  Every workgroup looks at all sequences to find its part, so more than kFewMaxBatch
+// sequences take one workgroup each.
+struct FewPlan {
+  int row_tiles, groups, chunk;
+  size_t slots;  // partial rows of the workspace
+};
+FewPlan few_plan(const PagedAttnArgs& a) {
+  FewPlan f;
+  const int per = few_tiles(a) * kSmallTile;
+  f.row_tiles = (a.max_block * (a.hq / a.kv.hkv) + per - 1) / per;
+  const long lines = static_cast<long>(f.row_tiles) * a.kv.hkv;
+  if (a.batch > kFewMaxBatch) {
+    f.groups = a.batch, f.chunk = 0, f.slots = 0;
+    return f;
+  }
+  // stages of a line, at most
+  const long most = min(a.total_prefix / kFewStage + 2L * a.batch,
+                        a.batch * ((a.max_prefix + kFewStage - 1L) / kFewStage + 1));
+  const long chunk = (most * lines + kAttnTargetWgs - 1) / kAttnTargetWgs;
+  f.chunk = static_cast<int>(chunk);
+  f.groups = static_cast<int>((most + chunk - 1) / chunk);
+  f.slots = f.groups > 1 ? static_cast<size_t>(lines) * f.groups * 2 * per : 0;
+  return f;
 }
 
 // The call as one on packed rows whose prefix is empty, for what the kernels share.
@@ -312,16 +317,20 @@ AttnArgs packed_args(const PagedAttnArgs& a) {
 
 template <int D, bool kE4m3, int kTiles>
 hipError_t launch_few(const PagedAttnArgs& a, void* ws, hipStream_t s) {
-  constexpr int kKeysPer = kE4m3 ? kFewKeysE4m3 : kFewKeysBf16;
-  const SplitPlan sp = few_plan(a);
-  FewParams p{attn_params(packed_args(a), sp, ws), a.kv, few_row_tiles(a), a.batch * sp.nsplit * a.kv.hkv};
-  p.a.prefix_mask = kFewWaves * kKeysPer - 1;
-  const dim3 grid(static_cast<unsigned>(8 * ((p.units + 7) / 8) * p.row_tiles));
-  hipLaunchKernelGGL((attn_paged_few_kernel<D, kE4m3, kKeysPer, kTiles>), grid,
+  const FewPlan f = few_plan(a);
+  float* const o = static_cast<float*>(ws);
+  float* const m = o + f.slots * D;
+  const FewParams p{attn_params(packed_args(a), SplitPlan{1, 0}, nullptr), a.kv, a.batch,
+                    f.row_tiles, f.groups, f.chunk, o, m, m + f.slots};
+  const long units = static_cast<long>(f.groups) * a.kv.hkv;
+  const dim3 grid(static_cast<unsigned>(8 * ((units + 7) / 8) * f.row_tiles));
+  hipLaunchKernelGGL((attn_paged_few_kernel<D, kE4m3, kFewKeys, kTiles>), grid,
                      dim3(kFewWaves * 64), 0, s, p);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || sp.nsplit == 1) return e;
-  launch_merge<D>(p.a, a.total_block, a.batch, s);
+  if (e != hipSuccess || f.slots == 0) return e;
+  hipLaunchKernelGGL(attn_paged_few_merge_kernel<D>,
+                     dim3(static_cast<unsigned>(a.batch * a.kv.hkv * f.row_tiles)), dim3(512), 0, s,
+                     p, kFewStage, kTiles * kSmallTile);
   return hipGetLastError();
 }
 
@@ -366,7 +375,8 @@ hipError_t launch_tiles(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 
 size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
   if (a.total_block == 0 || a.max_block == 0) return 0;
-  const SplitPlan sp = few_ok(bf16, a) ? few_plan(a) : bf16 ? tiles_plan(a) : f32_plan(a);
+  if (few_ok(bf16, a)) return few_plan(a).slots * (a.kv.head_dim + 2) * sizeof(float);
+  const SplitPlan sp = bf16 ? tiles_plan(a) : f32_plan(a);
   if (sp.nsplit == 1) return 0;
   return static_cast<size_t>(a.total_block) * a.hq * sp.nsplit * (a.kv.head_dim + 2) *
          sizeof(float);

@@ -2,10 +2,18 @@
 // bf16.  Such calls read every cached key and value for a handful of multiply-adds: they are bound
 // by memory, and the kernel is built around its loads.
 //
-// A workgroup of four waves per (sequence, K/V head, key range, 16 kTiles query rows).  The waves
-// split the keys, not the rows: each takes every fourth piece of the range, holds all query rows
-// and keeps an online softmax of its own, so that no wave waits for another until the range ends
-// and their results are merged through LDS.
+// A workgroup is four waves.  The waves split the keys, not the rows: each takes every fourth piece,
+// holds all 16 kTiles query rows and keeps an online softmax of its own, so that no wave waits for
+// another until its keys end; their results are then merged through LDS.
+//
+// Contexts of a served batch are of very different lengths, and one launch should keep every
+// compute unit busy to its end.  So the keys of all sequences form one line, for each (K/V head,
+// tile of query rows): n_b stages for sequence b (its cached rows in stages of four pieces, and one
+// stage for the block's own rows), and workgroup w takes stages w chunk .. (w + 1) chunk - 1 of it,
+// wherever sequences begin and end in them.  A sequence that lies within one workgroup is written
+// out at once.  Otherwise each of its workgroups leaves a partial: the first in its slot 1 (the
+// sequence goes on), the others in their slot 0 (it came from before), merged by a second launch.
+// Measured against ranges of equal length for every sequence: see few_plan.
 //
 // A piece is kKeys keys.  K goes from memory straight into the registers of the MFMA's A operand
 // (S^T = K Q^T by 16x16x32: lane l holds row l % 16).  V has to be transposed for O^T = V^T P^T: it
@@ -30,11 +38,54 @@ constexpr int kFewWaves = 4;
 constexpr int kFewBlockKeys = 32;  // keys of a piece of the block's own rows
 
 struct FewParams {
-  AttnParams a;  // without the prefix segment
+  AttnParams a;  // without the prefix segment and the key split
   PagedKv kv;
-  int row_tiles;  // groups of query rows per (sequence, K/V head)
-  int units;      // batch * nsplit * hkv
+  int batch;
+  int row_tiles;  // tiles of query rows per (sequence, K/V head)
+  int groups;     // workgroups along the line of a (K/V head, tile)
+  int chunk;      // stages per workgroup; 0: workgroup w takes sequence w whole
+  // partials of (line, workgroup, slot), line = K/V head * row_tiles + tile
+  float* o_part;  // [rows of a tile, D]
+  float* m_part;  // [rows of a tile], log2 units
+  float* l_part;
 };
+
+// Stages of sequence b in the line of the tile at query row row0 (none if the tile lies past its
+// rows): its cached rows, then the block's.
+__device__ __forceinline__ int few_stages(const AttnParams& p, int b, int row0, int stage) {
+  const int len = p.cu_block[b + 1] - p.cu_block[b];
+  const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
+  return row0 < len * p.group ? (plen + stage - 1) / stage + 1 : 0;
+}
+
+// Sum of x over the lanes up to this one.
+__device__ __forceinline__ int lanes_up_to(int x, int lane) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int y = __shfl_up(x, m);
+    if (lane >= m) x += y;
+  }
+  return x;
+}
+
+// The sequence that holds stage s of the line, and its first stage, found by the whole wavefront;
+// batch if the line ends before s.
+__device__ __forceinline__ int few_find(const FewParams& fp, int row0, int stage, int s, int lane,
+                                        int& first) {
+  first = 0;
+  for (int b0 = 0; b0 < fp.batch; b0 += 64) {
+    const int n = b0 + lane < fp.batch ? few_stages(fp.a, b0 + lane, row0, stage) : 0;
+    const int upto = lanes_up_to(n, lane);
+    const uint64_t past = __ballot(first + upto > s);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      first += __shfl(upto - n, l);
+      return b0 + l;
+    }
+    first += __shfl(upto, 63);
+  }
+  return fp.batch;
+}
 
 template <int D, bool kE4m3, int kKeys, int kTiles>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewParams fp) {
@@ -53,300 +104,397 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
   __shared__ __attribute__((aligned(16))) uint8_t smem[kFewWaves * kWaveBytes];
   __shared__ float s_m[kFewWaves][kTiles * kSmallTile], s_l[kFewWaves][kTiles * kSmallTile];
 
-  // the row tiles of a unit run on one XCD, one after another (see attn_bf16_kernel)
+  // the row tiles of a unit (K/V head, workgroup of the line) run on one XCD, one after another, and
+  // read its keys from that XCD's L2
   const int xcd = blockIdx.x % 8, jx = blockIdx.x / 8;
   const int unit = 8 * (jx / fp.row_tiles) + xcd;
-  if (unit >= fp.units) return;  // whole workgroup: padding of the last round
   const int tile = jx % fp.row_tiles;
-  const int z = unit / p.hkv, g = unit % p.hkv;
-  const int b = z / p.nsplit, sp = z % p.nsplit;
+  const int w = unit / p.hkv, g = unit % p.hkv;
+  if (w >= fp.groups) return;  // whole workgroup: padding of the last round
   const int G = p.group;
-  const int bbeg = p.cu_block[b];
-  const int len = p.cu_block[b + 1] - bbeg;
-  const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
-  const int n_rows = len * G;
   const int row0 = tile * kTiles * kSmallTile;
-  const int cached = (plen + kStage - 1) / kStage * kStage;  // the block's first key
-  const int n_keys = cached + len;
-  const int kbeg = sp * p.kps;
-  if (row0 >= n_rows || kbeg >= n_keys) return;  // whole workgroup
-  const int kend = min(n_keys, kbeg + p.kps);
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = lane >> 4, l16 = lane & 15;
   uint16_t* const Vs = reinterpret_cast<uint16_t*>(smem + wave * kWaveBytes);
 
-  // Columns of lane group grp in k-step s: the contraction index is permuted so that 16 bytes of an
-  // 8-bit row hold the lane's columns of two steps.
-  auto col_of = [&](int s) { return kE4m3 ? 64 * (s / 2) + 16 * grp + 8 * (s % 2) : 32 * s + 8 * grp; };
-  bf16x8 qf[kTiles][kDSteps];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    const int r = min(row0 + t * kSmallTile + l16, n_rows - 1);
-    const uint16_t* q = p.q + (static_cast<size_t>(bbeg + r / G) * p.hq + g * G + r % G) * D;
-#pragma unroll
-    for (int s = 0; s < kDSteps; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(q + col_of(s));
+  int b, first, from, to;  // sequence, its first stage in the line, stages of this workgroup
+  if (fp.chunk) {
+    from = w * fp.chunk;
+    to = from + fp.chunk;
+    b = few_find(fp, row0, kStage, from, lane, first);
+    b = __builtin_amdgcn_readfirstlane(b);
+    first = __builtin_amdgcn_readfirstlane(first);
+  } else {
+    b = w, first = 0, from = 0, to = 1 << 30;
   }
-  f32x4 o[kTiles][kDTiles];
-  float m_run[kTiles], l_run[kTiles];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    m_run[t] = kNegBig;  // the lowest finite value: scores of -inf have weights of zero
-    l_run[t] = 0.f;
-#pragma unroll
-    for (int d = 0; d < kDTiles; ++d) o[t][d] = f32x4{};
-  }
+  for (; b < fp.batch && from < to; ++b) {
+    const int n_stages = few_stages(p, b, row0, kStage);
+    if (n_stages == 0) {
+      if (!fp.chunk) return;  // uniform, as the rest of the loop's conditions
+      continue;
+    }
+    const int bbeg = p.cu_block[b];
+    const int len = p.cu_block[b + 1] - bbeg;
+    const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
+    const int n_rows = len * G;
+    const int sbeg = from - first, send = min(to - first, n_stages);  // stages of the sequence
+    const int kbeg = sbeg * kStage, kend = min(send * kStage, plen);  // its cached rows among them
 
-  // V^T fragment of keys kbase + 4 grp + 0..3 at d = d0 + l16, as in attn_small_role
-  auto vt_read = [&](int kbase, int d0) -> v4i16 {
-    const uint16_t* a = Vs + (kbase + 4 * grp + (l16 >> 2)) * kVPitch + d0 + 4 * (l16 & 3);
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(const_cast<uint16_t*>(a)));
-  };
-  // Softmax and O^T += V^T P^T of one piece with scores sc[t][j] (16 keys each) whose first `valid`
-  // keys exist; V lies in LDS.
-  auto finish = [&](auto& sc, int valid) {
-    constexpr int kG = sizeof(sc[0]) / sizeof(f32x4);
-    u32x2 pk[kTiles][kG];
+    // Columns of lane group grp in k-step s: the contraction index is permuted so that 16 bytes of an
+    // 8-bit row hold the lane's columns of two steps.
+    auto col_of = [&](int s, int grp_) {
+      return kE4m3 ? 64 * (s / 2) + 16 * grp_ + 8 * (s % 2) : 32 * s + 8 * grp_;
+    };
+    bf16x8 qf[kTiles][kDSteps];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      if (valid < 16 * kG) {
+      const int r = min(row0 + t * kSmallTile + l16, n_rows - 1);
+      const uint16_t* q = p.q + (static_cast<size_t>(bbeg + r / G) * p.hq + g * G + r % G) * D;
+#pragma unroll
+      for (int s = 0; s < kDSteps; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(q + col_of(s, grp));
+    }
+    f32x4 o[kTiles][kDTiles];
+    float m_run[kTiles], l_run[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      m_run[t] = kNegBig;  // the lowest finite value: scores of -inf have weights of zero
+      l_run[t] = 0.f;
+#pragma unroll
+      for (int d = 0; d < kDTiles; ++d) o[t][d] = f32x4{};
+    }
+
+    // V^T fragment of keys kbase + 4 grp + 0..3 at d = d0 + l16, as in attn_small_role
+    auto vt_read = [&](int kbase, int d0) -> v4i16 {
+      const uint16_t* a = Vs + (kbase + 4 * grp + (l16 >> 2)) * kVPitch + d0 + 4 * (l16 & 3);
+      return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(const_cast<uint16_t*>(a)));
+    };
+    // Softmax and O^T += V^T P^T of one piece with scores sc[t][j] (16 keys each) whose first `valid`
+    // keys exist; V lies in LDS.
+    auto finish = [&](auto& sc, int valid) {
+      constexpr int kG = sizeof(sc[0]) / sizeof(f32x4);
+      u32x2 pk[kTiles][kG];
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        if (valid < 16 * kG) {
+#pragma unroll
+          for (int j = 0; j < kG; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (16 * j + 4 * grp + r >= valid) sc[t][j][r] = -INFINITY;
+        }
+        float mloc = -INFINITY;
 #pragma unroll
         for (int j = 0; j < kG; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (16 * j + 4 * grp + r >= valid) sc[t][j][r] = -INFINITY;
-      }
-      float mloc = -INFINITY;
+          for (int r = 0; r < 4; ++r) mloc = fmaxf(mloc, sc[t][j][r]);
+        mloc = fmaxf(mloc, __shfl_xor(mloc, 16));
+        mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
+        // scale > 0, so max(scale * s) = scale * max(s); e = 2^(scale s - m) with one FMA
+        const float m_new = fmaxf(m_run[t], mloc * p.scale_log2);
+        const float alpha = fast_exp2(m_run[t] - m_new);
+        m_run[t] = m_new;
+        float lsum = 0.f;
 #pragma unroll
-      for (int j = 0; j < kG; ++j)
+        for (int j = 0; j < kG; ++j) {
+          float e[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) mloc = fmaxf(mloc, sc[t][j][r]);
-      mloc = fmaxf(mloc, __shfl_xor(mloc, 16));
-      mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
-      // scale > 0, so max(scale * s) = scale * max(s); e = 2^(scale s - m) with one FMA
-      const float m_new = fmaxf(m_run[t], mloc * p.scale_log2);
-      const float alpha = fast_exp2(m_run[t] - m_new);
-      m_run[t] = m_new;
-      float lsum = 0.f;
-#pragma unroll
-      for (int j = 0; j < kG; ++j) {
-        float e[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          e[r] = fast_exp2(fmaf(sc[t][j][r], p.scale_log2, -m_new));
-          lsum += e[r];
+          for (int r = 0; r < 4; ++r) {
+            e[r] = fast_exp2(fmaf(sc[t][j][r], p.scale_log2, -m_new));
+            lsum += e[r];
+          }
+          pk[t][j] = u32x2{pack2_bf16(e[0], e[1]), pack2_bf16(e[2], e[3])};
         }
-        pk[t][j] = u32x2{pack2_bf16(e[0], e[1]), pack2_bf16(e[2], e[3])};
-      }
-      l_run[t] = l_run[t] * alpha + lsum;
-      if (__any(alpha != 1.0f)) {
+        l_run[t] = l_run[t] * alpha + lsum;
+        if (__any(alpha != 1.0f)) {
 #pragma unroll
-        for (int d = 0; d < kDTiles; ++d) o[t][d] *= alpha;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kG / 2; ++u)
-#pragma unroll
-      for (int d = 0; d < kDTiles; ++d) {
-        const v4i16 lo = vt_read(32 * u, 16 * d), hi = vt_read(32 * u + 16, 16 * d);
-        const bf16x8 vf = __builtin_bit_cast(
-            bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          const u32x4 w{pk[t][2 * u][0], pk[t][2 * u][1], pk[t][2 * u + 1][0], pk[t][2 * u + 1][1]};
-          o[t][d] = mfma16(vf, __builtin_bit_cast(bf16x8, w), o[t][d]);
+          for (int d = 0; d < kDTiles; ++d) o[t][d] *= alpha;
         }
       }
-  };
+#pragma unroll
+      for (int u = 0; u < kG / 2; ++u)
+#pragma unroll
+        for (int d = 0; d < kDTiles; ++d) {
+          const v4i16 lo = vt_read(32 * u, 16 * d), hi = vt_read(32 * u + 16, 16 * d);
+          const bf16x8 vf = __builtin_bit_cast(
+              bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            const u32x4 w{pk[t][2 * u][0], pk[t][2 * u][1], pk[t][2 * u + 1][0], pk[t][2 * u + 1][1]};
+            o[t][d] = mfma16(vf, __builtin_bit_cast(bf16x8, w), o[t][d]);
+          }
+        }
+    };
 
-  // ---- cached rows ----------------------------------------------------------------------
-  constexpr int kKPer = kRow / 64;             // 16-byte loads per lane of 16 rows of K
-  constexpr int kVRows = 1024 / kRow;          // rows of V per load instruction
-  constexpr int kVPer = 16 / kVRows;           // the same of V
-  constexpr int kVLanes = kRow / 16;           // lanes per row of V
-  u32x4 kraw[kGroups][kKPer], vraw[kGroups][kVPer];
-  uint32_t kscale[kGroups], vscale[kGroups][kVPer];
-  const uint32_t koff = l16 * kRow + 16 * grp;
-  const int vrow = lane / kVLanes;
-  const uint32_t voff = lane * 16;
-  const int32_t* const table = fp.kv.table + static_cast<size_t>(b) * fp.kv.max_pages;
-  const int pmask = (1 << fp.kv.page_shift) - 1;
-  // Pages of the piece at key k0 (uniform); groups past the cached rows take the last page, and no
-  // rows of it.
-  auto pages = [&](int k0, int (&page)[kGroups]) {
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j)
-      page[j] = table[min(k0 + 16 * j, plen - 1) >> fp.kv.page_shift];
-  };
-  auto load = [&](int k0, const int (&page_)[kGroups]) {
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j) {
-      const int page = __builtin_amdgcn_readfirstlane(page_[j]);
-      const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(fp.kv.n_pages);
-      const size_t row =
-          ((static_cast<size_t>(ok ? page : 0) * p.hkv + g) << fp.kv.page_shift) +
-          ((k0 + 16 * j) & pmask);
-      const int rows = ok ? min(max(plen - (k0 + 16 * j), 0), 16) : 0;
-      const __amdgpu_buffer_rsrc_t rk = make_rsrc(fp.kv.k + row * kRow, rows * kRow);
-      const __amdgpu_buffer_rsrc_t rv = make_rsrc(fp.kv.v + row * kRow, rows * kRow);
-#pragma unroll
-      for (int i = 0; i < kKPer; ++i) kraw[j][i] = buffer_load16(rk, koff + 64 * i);
-      if constexpr (kE4m3) kscale[j] = buffer_load1(make_rsrc(fp.kv.k_scale + row, rows), l16);
-#pragma unroll
-      for (int i = 0; i < kVPer; ++i) {
-        vraw[j][i] = buffer_load16(rv, voff + 1024 * i);
-        if constexpr (kE4m3)
-          vscale[j][i] = buffer_load1(make_rsrc(fp.kv.v_scale + row, rows), vrow + kVRows * i);
-      }
-    }
-  };
-  const int kcached = min(kend, cached);
-  int k0 = kbeg + wave * kKeys;
-  if (k0 < min(kcached, plen)) {
-    int page[kGroups];
-    pages(k0, page);
-    load(k0, page);
-    for (; k0 < min(kcached, plen); k0 += kStage) {
-      const int next = k0 + kStage;
-      const bool more = next < min(kcached, plen);
-      if (more) pages(next, page);
-      // V into LDS (the reads of the piece before are done: they fed the MFMAs above)
+    // ---- cached rows ----------------------------------------------------------------------
+    constexpr int kKPer = kRow / 64;             // 16-byte loads per lane of 16 rows of K
+    constexpr int kVRows = 1024 / kRow;          // rows of V per load instruction
+    constexpr int kVPer = 16 / kVRows;           // the same of V
+    constexpr int kVLanes = kRow / 16;           // lanes per row of V
+    u32x4 kraw[kGroups][kKPer], vraw[kGroups][kVPer];
+    uint32_t kscale[kGroups], vscale[kGroups][kVPer];
+    const uint32_t koff = l16 * kRow + 16 * grp;
+    const int vrow = lane / kVLanes;
+    const uint32_t voff = lane * 16;
+    const int32_t* const table = fp.kv.table + static_cast<size_t>(b) * fp.kv.max_pages;
+    const int pmask = (1 << fp.kv.page_shift) - 1;
+    // Pages of the piece at key k0 (uniform); groups past the cached rows take the last page, and no
+    // rows of it.
+    auto pages = [&](int k0, int (&page)[kGroups]) {
 #pragma unroll
       for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-        for (int i = 0; i < kVPer; ++i) {
-          uint16_t* dst = Vs + (16 * j + kVRows * i + vrow) * kVPitch;
-          if constexpr (kE4m3) {
-            u32x4 lo, hi;
-            e4m3_widen(vraw[j][i], e8m0(vscale[j][i]), lo, hi);
-            dst += 16 * (lane % kVLanes);
-            *reinterpret_cast<u32x4*>(dst) = lo;
-            *reinterpret_cast<u32x4*>(dst + 8) = hi;
-          } else {
-            *reinterpret_cast<u32x4*>(dst + 8 * (lane % kVLanes)) = vraw[j][i];
-          }
-        }
-      f32x4 sc[kTiles][kGroups];
+        page[j] = table[min(k0 + 16 * j, plen - 1) >> fp.kv.page_shift];
+    };
+    auto load = [&](int k0, const int (&page_)[kGroups]) {
 #pragma unroll
       for (int j = 0; j < kGroups; ++j) {
-        bf16x8 kf[kDSteps];
-        if constexpr (kE4m3) {
+        const int page = __builtin_amdgcn_readfirstlane(page_[j]);
+        const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(fp.kv.n_pages);
+        const size_t row =
+            ((static_cast<size_t>(ok ? page : 0) * p.hkv + g) << fp.kv.page_shift) +
+            ((k0 + 16 * j) & pmask);
+        const int rows = ok ? min(max(plen - (k0 + 16 * j), 0), 16) : 0;
+        const __amdgpu_buffer_rsrc_t rk = make_rsrc(fp.kv.k + row * kRow, rows * kRow);
+        const __amdgpu_buffer_rsrc_t rv = make_rsrc(fp.kv.v + row * kRow, rows * kRow);
 #pragma unroll
-          for (int i = 0; i < kKPer; ++i) {
-            u32x4 lo, hi;
-            e4m3_widen(kraw[j][i], e8m0(kscale[j]), lo, hi);
-            kf[2 * i] = __builtin_bit_cast(bf16x8, lo);
-            kf[2 * i + 1] = __builtin_bit_cast(bf16x8, hi);
+        for (int i = 0; i < kKPer; ++i) kraw[j][i] = buffer_load16(rk, koff + 64 * i);
+        if constexpr (kE4m3) kscale[j] = buffer_load1(make_rsrc(fp.kv.k_scale + row, rows), l16);
+#pragma unroll
+        for (int i = 0; i < kVPer; ++i) {
+          vraw[j][i] = buffer_load16(rv, voff + 1024 * i);
+          if constexpr (kE4m3)
+            vscale[j][i] = buffer_load1(make_rsrc(fp.kv.v_scale + row, rows), vrow + kVRows * i);
+        }
+      }
+    };
+    int k0 = kbeg + wave * kKeys;
+    if (k0 < kend) {
+      int page[kGroups];
+      pages(k0, page);
+      load(k0, page);
+      for (; k0 < kend; k0 += kStage) {
+        const int next = k0 + kStage;
+        const bool more = next < kend;
+        if (more) pages(next, page);
+        // V into LDS (the reads of the piece before are done: they fed the MFMAs above)
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+          for (int i = 0; i < kVPer; ++i) {
+            uint16_t* dst = Vs + (16 * j + kVRows * i + vrow) * kVPitch;
+            if constexpr (kE4m3) {
+              u32x4 lo, hi;
+              e4m3_widen(vraw[j][i], e8m0(vscale[j][i]), lo, hi);
+              dst += 16 * (lane % kVLanes);
+              *reinterpret_cast<u32x4*>(dst) = lo;
+              *reinterpret_cast<u32x4*>(dst + 8) = hi;
+            } else {
+              *reinterpret_cast<u32x4*>(dst + 8 * (lane % kVLanes)) = vraw[j][i];
+            }
           }
-        } else {
+        f32x4 sc[kTiles][kGroups];
 #pragma unroll
-          for (int i = 0; i < kKPer; ++i) kf[i] = __builtin_bit_cast(bf16x8, kraw[j][i]);
+        for (int j = 0; j < kGroups; ++j) {
+          bf16x8 kf[kDSteps];
+          if constexpr (kE4m3) {
+#pragma unroll
+            for (int i = 0; i < kKPer; ++i) {
+              u32x4 lo, hi;
+              e4m3_widen(kraw[j][i], e8m0(kscale[j]), lo, hi);
+              kf[2 * i] = __builtin_bit_cast(bf16x8, lo);
+              kf[2 * i + 1] = __builtin_bit_cast(bf16x8, hi);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < kKPer; ++i) kf[i] = __builtin_bit_cast(bf16x8, kraw[j][i]);
+          }
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            sc[t][j] = f32x4{};
+#pragma unroll
+            for (int s = 0; s < kDSteps; ++s) sc[t][j] = mfma16(kf[s], qf[t][s], sc[t][j]);
+          }
         }
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          sc[t][j] = f32x4{};
-#pragma unroll
-          for (int s = 0; s < kDSteps; ++s) sc[t][j] = mfma16(kf[s], qf[t][s], sc[t][j]);
-        }
+        if (more) load(next, page);
+        // the wave's own LDS stores before its transposing reads, and those before the next stores
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        finish(sc, plen - k0);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
-      if (more) load(next, page);
-      // the wave's own LDS stores before its transposing reads, and those before the next stores
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      finish(sc, plen - k0);
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
-  }
-  // ---- the block's own rows (bf16), pieces of 32 keys dealt to the waves ------------------
-  if (kend > cached) {
-    const int jend = kend - cached;
-    const uint32_t key_bytes = static_cast<uint32_t>(p.hkv) * 2 * D;
-    for (int j0 = max(kbeg - cached, 0) + wave * kFewBlockKeys; j0 < jend;
-         j0 += kFewWaves * kFewBlockKeys) {
-      const size_t at = (static_cast<size_t>(bbeg + j0) * p.hkv + g) * D;
-      const int rows = min(len - j0, kFewBlockKeys);
-      const uint32_t bytes = (rows - 1) * key_bytes + 2 * D;
-      const __amdgpu_buffer_rsrc_t rk = make_rsrc(p.k_blk + at, bytes);
-      const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.v_blk + at, bytes);
-      constexpr int kLanes = D / 8, kPer = kFewBlockKeys * kLanes / 64;
+    // ---- the block's own rows (bf16), pieces of 32 keys dealt to the waves ------------------
+    if (send == n_stages) {
+      const uint32_t key_bytes = static_cast<uint32_t>(p.hkv) * 2 * D;
+      int lane_ = lane;  // addresses formed here: kept over the cached rows they would spill
+      asm volatile("" : "+v"(lane_));
+      for (int j0 = wave * kFewBlockKeys; j0 < len; j0 += kFewWaves * kFewBlockKeys) {
+        const size_t at = (static_cast<size_t>(bbeg + j0) * p.hkv + g) * D;
+        const int rows = min(len - j0, kFewBlockKeys);
+        const uint32_t bytes = (rows - 1) * key_bytes + 2 * D;
+        const __amdgpu_buffer_rsrc_t rk = make_rsrc(p.k_blk + at, bytes);
+        const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.v_blk + at, bytes);
+        constexpr int kLanes = D / 8, kPer = kFewBlockKeys * kLanes / 64;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int r = i * (64 / kLanes) + lane / kLanes, c = 8 * (lane % kLanes);
-        *reinterpret_cast<u32x4*>(Vs + r * kVPitch + c) = buffer_load16(rv, r * key_bytes + 2 * c);
-      }
-      f32x4 sc[kTiles][kFewBlockKeys / 16];
-#pragma unroll
-      for (int j = 0; j < kFewBlockKeys / 16; ++j) {
-        bf16x8 kf[kDSteps];
-#pragma unroll
-        for (int s = 0; s < kDSteps; ++s)
-          kf[s] = __builtin_bit_cast(
-              bf16x8, buffer_load16(rk, (16 * j + l16) * key_bytes + 2 * col_of(s)));
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          sc[t][j] = f32x4{};
-#pragma unroll
-          for (int s = 0; s < kDSteps; ++s) sc[t][j] = mfma16(kf[s], qf[t][s], sc[t][j]);
+        for (int i = 0; i < kPer; ++i) {
+          const int r = i * (64 / kLanes) + lane_ / kLanes, c = 8 * (lane_ % kLanes);
+          *reinterpret_cast<u32x4*>(Vs + r * kVPitch + c) =
+              buffer_load16(rv, r * key_bytes + 2 * c);
         }
+        f32x4 sc[kTiles][kFewBlockKeys / 16];
+#pragma unroll
+        for (int j = 0; j < kFewBlockKeys / 16; ++j) {
+          bf16x8 kf[kDSteps];
+#pragma unroll
+          for (int s = 0; s < kDSteps; ++s)
+            kf[s] = __builtin_bit_cast(
+                bf16x8, buffer_load16(
+                            rk, (16 * j + (lane_ & 15)) * key_bytes + 2 * col_of(s, lane_ >> 4)));
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            sc[t][j] = f32x4{};
+#pragma unroll
+            for (int s = 0; s < kDSteps; ++s) sc[t][j] = mfma16(kf[s], qf[t][s], sc[t][j]);
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        finish(sc, rows);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      finish(sc, rows);
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
-  }
 
-  // ---- the waves' results, in wave order --------------------------------------------------
-  float* const so = reinterpret_cast<float*>(smem);
-  constexpr int kWaveFloats = kWaveBytes / 4;
+    // ---- the waves' results, in wave order --------------------------------------------------
+    const bool whole = sbeg == 0 && send == n_stages;
+    const size_t slot =
+        ((static_cast<size_t>(g) * fp.row_tiles + tile) * fp.groups + w) * 2 + (sbeg == 0 ? 1 : 0);
+    float* const so = reinterpret_cast<float*>(smem);
+    constexpr int kWaveFloats = kWaveBytes / 4;
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    float l = l_run[t] + __shfl_xor(l_run[t], 16);
-    l += __shfl_xor(l, 32);
-    if (grp == 0) s_m[wave][t * kSmallTile + l16] = m_run[t], s_l[wave][t * kSmallTile + l16] = l;
+    for (int t = 0; t < kTiles; ++t) {
+      float l = l_run[t] + __shfl_xor(l_run[t], 16);
+      l += __shfl_xor(l, 32);
+      if (grp == 0) s_m[wave][t * kSmallTile + l16] = m_run[t], s_l[wave][t * kSmallTile + l16] = l;
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      if (t > 0) __syncthreads();  // the tile before has been read
+      // register r of o[t][d]: column 16 d + 4 grp + r of query l16
+#pragma unroll
+      for (int d = 0; d < kDTiles; ++d)
+        *reinterpret_cast<f32x4*>(so + wave * kWaveFloats + l16 * kOPitch + 16 * d + 4 * grp) = o[t][d];
+      __syncthreads();
+      int tid_ = tid;  // (as lane_ above)
+      asm volatile("" : "+v"(tid_));
+      for (int i = tid_; i < kSmallTile * (D / 4); i += kFewWaves * 64) {
+        const int r = i / (D / 4), c = 4 * (i % (D / 4)), rt = t * kSmallTile + r;
+        const int row = row0 + rt;
+        if (row >= n_rows) break;
+        float m = s_m[0][rt];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) m = fmaxf(m, s_m[w][rt]);
+        f32x4 x{};
+        float l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) {
+          const float f = fast_exp2(s_m[w][rt] - m);
+          l = fmaf(f, s_l[w][rt], l);
+          const f32x4 y = *reinterpret_cast<const f32x4*>(so + w * kWaveFloats + r * kOPitch + c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = fmaf(f, y[e], x[e]);
+        }
+        if (whole) {
+          const size_t at = static_cast<size_t>(bbeg + row / G) * p.hq + g * G + row % G;
+          const float inv = 1.0f / l;
+          *reinterpret_cast<u32x2*>(p.out + at * D + c) =
+              u32x2{pack2_bf16(x[0] * inv, x[1] * inv), pack2_bf16(x[2] * inv, x[3] * inv)};
+        } else {
+          const size_t at = slot * kTiles * kSmallTile + rt;
+          *reinterpret_cast<f32x4*>(fp.o_part + at * D + c) = x;
+          if (c == 0) fp.m_part[at] = m, fp.l_part[at] = l;
+        }
+      }
+    }
+    __syncthreads();  // before the next sequence's values take the waves' places in LDS
+    first += n_stages;
+    from = first;
+    if (!fp.chunk) return;
   }
+}
+
+// The partials of one (sequence, K/V head, tile of query rows) per workgroup, in the order of the
+// line; a wave per query row, its lanes over kParts partials side by side.
+template <int D>
+__global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp, int stage,
+                                                                   int tile_rows) {
+  const AttnParams& p = fp.a;
+  constexpr int kCols = D / 4;          // lanes per partial row
+  constexpr int kParts = 64 / kCols;    // partials per load
+  constexpr int kBatch = 8;             // loads in flight
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int tile = blockIdx.x % fp.row_tiles, z = blockIdx.x / fp.row_tiles;
+  const int g = z % p.hkv, b = z / p.hkv;
+  const int row0 = tile * tile_rows;
+  // first stage of the sequence in the line
+  int before = 0;
+  for (int b0 = 0; b0 < b; b0 += 64)
+    before += b0 + lane < b ? few_stages(p, b0 + lane, row0, stage) : 0;
+  for (int m = 32; m >= 1; m >>= 1) before += __shfl_xor(before, m);
+  const int n = few_stages(p, b, row0, stage);
+  const int w0 = before / fp.chunk, w1 = (before + n - 1) / fp.chunk;
+  if (n == 0 || w0 == w1) return;  // nothing here, or written out by its only workgroup
+  const int bbeg = p.cu_block[b], G = p.group;
+  const int n_rows = min((p.cu_block[b + 1] - bbeg) * G - row0, tile_rows);
+  const size_t line = static_cast<size_t>(g * fp.row_tiles + tile) * fp.groups;
+  const int parts = w1 - w0 + 1;
+  const int c = 4 * (lane % kCols), sub = lane / kCols;
+  for (int r = wave; r < n_rows; r += 8) {
+    // row of partial k: slot 1 of the first workgroup, slot 0 of the others
+    auto at = [&](int k) {
+      return ((line + w0 + k) * 2 + (k == 0 ? 1 : 0)) * tile_rows + r;
+    };
+    float M = kNegBig;
+    for (int k = lane; k < parts; k += 64) M = fmaxf(M, fp.m_part[at(k)]);
+    for (int m = 32; m >= 1; m >>= 1) M = fmaxf(M, __shfl_xor(M, m));
+    f32x4 x{};
+    float l = 0.f;
+    for (int k0 = 0; k0 < parts; k0 += kBatch * kParts) {
+      f32x4 y[kBatch];
+      float mk[kBatch], lk[kBatch];
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    if (t > 0) __syncthreads();  // the tile before has been read
-    // register r of o[t][d]: column 16 d + 4 grp + r of query l16
-#pragma unroll
-    for (int d = 0; d < kDTiles; ++d)
-      *reinterpret_cast<f32x4*>(so + wave * kWaveFloats + l16 * kOPitch + 16 * d + 4 * grp) = o[t][d];
-    __syncthreads();
-    for (int i = tid; i < kSmallTile * (D / 4); i += kFewWaves * 64) {
-      const int r = i / (D / 4), c = 4 * (i % (D / 4)), rt = t * kSmallTile + r;
-      const int row = row0 + rt;
-      if (row >= n_rows) break;
-      float m = s_m[0][rt];
-#pragma unroll
-      for (int w = 1; w < kFewWaves; ++w) m = fmaxf(m, s_m[w][rt]);
-      f32x4 x{};
-      float l = 0.f;
-#pragma unroll
-      for (int w = 0; w < kFewWaves; ++w) {
-        const float f = fast_exp2(s_m[w][rt] - m);
-        l = fmaf(f, s_l[w][rt], l);
-        const f32x4 y = *reinterpret_cast<const f32x4*>(so + w * kWaveFloats + r * kOPitch + c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = fmaf(f, y[e], x[e]);
+      for (int j = 0; j < kBatch; ++j) {
+        const size_t i = at(min(k0 + j * kParts + sub, parts - 1));
+        y[j] = *reinterpret_cast<const f32x4*>(fp.o_part + i * D + c);
+        mk[j] = fp.m_part[i];
+        lk[j] = fp.l_part[i];
       }
-      const size_t at = static_cast<size_t>(bbeg + row / G) * p.hq + g * G + row % G;
-      if (p.nsplit > 1) {
-        const size_t idx = at * p.nsplit + sp;
-        *reinterpret_cast<f32x4*>(p.o_part + idx * D + c) = x;
-        if (c == 0) p.m_part[idx] = m, p.l_part[idx] = l;
-      } else {
-        const float inv = 1.0f / l;
-        *reinterpret_cast<u32x2*>(p.out + at * D + c) =
-            u32x2{pack2_bf16(x[0] * inv, x[1] * inv), pack2_bf16(x[2] * inv, x[3] * inv)};
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const float f = k0 + j * kParts + sub < parts ? fast_exp2(mk[j] - M) : 0.f;
+        if (f == 0.f) continue;  // (an infinite value of weight zero)
+        l = fmaf(f, lk[j], l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = fmaf(f, y[j][e], x[e]);
       }
+    }
+    for (int m = kCols; m < 64; m <<= 1) {
+      l += __shfl_xor(l, m);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], m);
+    }
+    if (sub == 0) {
+      const int row = row0 + r;
+      const size_t dst = static_cast<size_t>(bbeg + row / G) * p.hq + g * G + row % G;
+      const float inv = 1.0f / l;
+      *reinterpret_cast<u32x2*>(p.out + dst * D + c) =
+          u32x2{pack2_bf16(x[0] * inv, x[1] * inv), pack2_bf16(x[2] * inv, x[3] * inv)};
     }
   }
 }

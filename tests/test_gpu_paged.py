@@ -281,6 +281,15 @@ def test_attention_batches(blocks, cached, group, hkv, cache, dtype, head_dim):
     _close(*_attention(blocks, cached, 32, cache, dtype, group, head_dim, hkv=hkv), dtype)
 
 
+# More sequences than one workgroup looks through (2048), single tokens and small blocks, some empty.
+@pytest.mark.parametrize("cache,dtype", COMBOS)
+def test_attention_many_sequences(cache, dtype):
+    print(f"many {cache} {dtype}", flush=True)
+    blocks = [(i % 5) % 4 for i in range(2300)]
+    cached = [(i * 13) % 40 + (500 if i == 77 else 0) for i in range(2300)]
+    _close(*_attention(blocks, cached, 16, cache, dtype, 2, 64, hkv=1), dtype)
+
+
 @pytest.mark.parametrize("cache,dtype", COMBOS)
 @pytest.mark.parametrize("blocks,cached", [([1], [300]), ([40], [200]), ([140], [90])])
 def test_attention_scale(blocks, cached, cache, dtype):
