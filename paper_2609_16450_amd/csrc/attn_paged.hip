@@ -5,7 +5,6 @@
 // block and a piece of 16 keys in one page (page sizes are multiples of 16); keys of the padding
 // get scores of -inf and values of zero, whatever the page holds there.
 #include "attn_common.hpp"
-#include "attn_merge.hpp"
 #include "attn_paged_few.hpp"
 #include "attn_tiles.hpp"
 #include "eb_common.hpp"
@@ -266,13 +265,17 @@ hipError_t launch_f32(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 }
 
 // ---- few query rows per K/V head, bf16 ----------------------------------------------------
-constexpr int kFewMaxRows = 64;
+// Up to this many query rows per K/V head.  Over bf16 pages the tile kernel is the faster from 33
+// rows on (32 heads x 128, 16 blocks of 64 rows: 137 against 165 us); widening 8 bits costs it more
+// (28/4 heads, 64 blocks of 8: 112 against 106 us; 16/4 heads x 64, 32 blocks of 16: 67 against 48).
+constexpr int kFewRowsBf16 = 32, kFewRowsE4m3 = 64;
 constexpr int kFewKeys = 32;  // keys of a piece
 constexpr int kFewStage = kFewWaves * kFewKeys;
 constexpr int kFewMaxBatch = 2048;
 
 bool few_ok(bool bf16, const PagedAttnArgs& a) {
-  return bf16 && static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) <= kFewMaxRows;
+  const int most = a.kv.type == CacheType::kE4m3 ? kFewRowsE4m3 : kFewRowsBf16;
+  return bf16 && static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) <= most;
 }
 int few_tiles(const PagedAttnArgs& a) {  // 16-row tiles per workgroup
   return a.max_block * (a.hq / a.kv.hkv) <= kSmallTile ? 1 : 2;
@@ -343,31 +346,66 @@ hipError_t launch_few_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 }
 
 // ---- many query rows, bf16: the tile kernels of the packed prefix ---------------------------
-SplitPlan tiles_plan(const PagedAttnArgs& a) {
-  const int keys = (a.max_prefix + kKeys - 1) / kKeys * kKeys + a.max_block;
-  return split_plan(a.batch, a.max_block, keys, a.hq, a.kv.hkv);
+// Items of whole sequences (a K/V head and a tile of query rows each) up to which a launch may cut
+// sequences into ranges, for one, two or four rounds of workgroups: the fewer items, the fewer rounds
+// are needed to make them even.  With more than kSplitItems whole sequences fill the rounds (32 heads,
+// 32 blocks of 8 to 128 rows behind 2048, 1024 items: 212 us whole, 227 us with the plan).
+constexpr long kSplitItems1 = 160, kSplitItems2 = 420, kSplitItems = 900;
+
+struct TilesLaunch {
+  TilePlan plan;
+  unsigned grid;
+  size_t parts;  // items that may leave partials
+};
+TilesLaunch tiles_plan(const PagedAttnArgs& a) {
+  const long group = a.hq / a.kv.hkv, hkv = a.kv.hkv;
+  const long row_tiles = (a.max_block * group + kRowsPerWg - 1) / kRowsPerWg;
+  const long stages = (a.max_prefix + kKeys - 1L) / kKeys + (a.max_block + kKeys - 1) / kKeys;
+  // items of whole sequences, at most
+  const long whole = hkv * min(a.batch * row_tiles, a.total_block * group / kRowsPerWg + a.batch);
+  TilesLaunch t{};
+  t.plan.batch = a.batch;
+  t.plan.row_tiles = static_cast<int>(row_tiles);
+  if (a.batch <= kPlanMaxBatch && whole <= kSplitItems && stages > 1) {
+    const int rounds = whole <= kSplitItems1 ? 1 : whole <= kSplitItems2 ? 2 : 4;
+    t.plan.cap = rounds * kAttnTargetWgs;
+    t.grid = t.plan.cap;
+    t.parts = t.plan.cap;
+    return t;
+  }
+  const long base = row_tiles * hkv * a.batch;
+  const long want = max(1L, min((kAttnTargetWgs + base - 1) / base, stages));
+  const long chunk = (stages + want - 1) / want;
+  t.plan.chunk = static_cast<int>(chunk);
+  t.plan.nsplit = static_cast<int>((stages + chunk - 1) / chunk);
+  const long units = a.batch * hkv * t.plan.nsplit;
+  t.grid = static_cast<unsigned>(kXcdCount * ((units + kXcdCount - 1) / kXcdCount) * row_tiles);
+  t.parts = t.plan.nsplit > 1 ? units * row_tiles : 0;
+  return t;
 }
 
 template <int D, bool kE4m3>
 hipError_t launch_tiles(const PagedAttnArgs& a, void* ws, hipStream_t s) {
-  const SplitPlan sp = tiles_plan(a);
-  AttnParams p = attn_params(packed_args(a), sp, ws);
-  p.prefix_mask = kKeys - 1;
-  const PagedKeys<kE4m3> keys{a.kv};
-  const long rows = static_cast<long>(a.max_block) * p.group;
-  const int row_tiles = static_cast<int>((rows + kRowsPerWg - 1) / kRowsPerWg);
-  const int units = a.batch * sp.nsplit * a.kv.hkv;
-  const dim3 grid(
-      static_cast<unsigned>(kXcdCount * ((units + kXcdCount - 1) / kXcdCount) * row_tiles));
+  const TilesLaunch t = tiles_plan(a);
+  const AttnParams p = attn_params(packed_args(a), SplitPlan{1, 0}, nullptr);
+  PagedKeys<kE4m3> keys{a.kv, t.plan};
+  const size_t rows = t.parts * kRowsPerWg;
+  keys.plan.o_part = static_cast<float*>(ws);
+  keys.plan.m_part = keys.plan.o_part + rows * D;
+  keys.plan.l_part = keys.plan.m_part + rows;
+  keys.plan.found = reinterpret_cast<int32_t*>(keys.plan.l_part + rows);
   if constexpr (D == 128)
-    hipLaunchKernelGGL(attn_bf16_d128_kernel<PagedKeys<kE4m3>>, grid, dim3(kThreads), 0, s, p, keys,
-                       row_tiles, units);
+    hipLaunchKernelGGL(attn_bf16_d128_kernel<PagedKeys<kE4m3>>, dim3(t.grid), dim3(kThreads), 0, s,
+                       p, keys, 0, 0);
   else
-    hipLaunchKernelGGL((attn_bf16_kernel<D, PagedKeys<kE4m3>>), grid, dim3(kThreads), 0, s, p, keys,
-                       row_tiles, units);
+    hipLaunchKernelGGL((attn_bf16_kernel<D, PagedKeys<kE4m3>>), dim3(t.grid), dim3(kThreads), 0, s,
+                       p, keys, 0, 0);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || sp.nsplit == 1) return e;
-  launch_merge<D>(p, a.total_block, a.batch, s);
+  if (e != hipSuccess || t.parts == 0) return e;
+  const long pairs = static_cast<long>(a.total_block) * a.hq;
+  hipLaunchKernelGGL(attn_tiles_merge_kernel<D>,
+                     dim3(static_cast<unsigned>((pairs + kThreads / 64 - 1) / (kThreads / 64))),
+                     dim3(kThreads), 0, s, p, keys.plan, a.total_block);
   return hipGetLastError();
 }
 
@@ -376,7 +414,12 @@ hipError_t launch_tiles(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
   if (a.total_block == 0 || a.max_block == 0) return 0;
   if (few_ok(bf16, a)) return few_plan(a).slots * (a.kv.head_dim + 2) * sizeof(float);
-  const SplitPlan sp = bf16 ? tiles_plan(a) : f32_plan(a);
+  if (bf16) {
+    const TilesLaunch t = tiles_plan(a);
+    return t.parts * kRowsPerWg * (a.kv.head_dim + 2) * sizeof(float) +
+           (t.plan.cap ? 2 * kPlanMaxBatch * sizeof(int32_t) : 0);
+  }
+  const SplitPlan sp = f32_plan(a);
   if (sp.nsplit == 1) return 0;
   return static_cast<size_t>(a.total_block) * a.hq * sp.nsplit * (a.kv.head_dim + 2) *
          sizeof(float);

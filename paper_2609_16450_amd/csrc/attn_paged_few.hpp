@@ -28,6 +28,7 @@
 #pragma once
 
 #include "attn_common.hpp"
+#include "attn_partials.hpp"
 #include "attn_small.hpp"
 #include "paged.hpp"
 
@@ -58,16 +59,6 @@ __device__ __forceinline__ int few_stages(const AttnParams& p, int b, int row0, 
   return row0 < len * p.group ? (plen + stage - 1) / stage + 1 : 0;
 }
 
-// Sum of x over the lanes up to this one.
-__device__ __forceinline__ int lanes_up_to(int x, int lane) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int y = __shfl_up(x, m);
-    if (lane >= m) x += y;
-  }
-  return x;
-}
-
 // The sequence that holds stage s of the line, and its first stage, found by the whole wavefront;
 // batch if the line ends before s.
 __device__ __forceinline__ int few_find(const FewParams& fp, int row0, int stage, int s, int lane,
@@ -75,14 +66,14 @@ __device__ __forceinline__ int few_find(const FewParams& fp, int row0, int stage
   first = 0;
   for (int b0 = 0; b0 < fp.batch; b0 += 64) {
     const int n = b0 + lane < fp.batch ? few_stages(fp.a, b0 + lane, row0, stage) : 0;
-    const int upto = lanes_up_to(n, lane);
+    const int upto = lanes_up_to(n, 0, AddOp{});
     const uint64_t past = __ballot(first + upto > s);
     if (past) {
       const int l = __builtin_ctzll(past);
-      first += __shfl(upto - n, l);
+      first += __builtin_amdgcn_readlane(upto - n, l);
       return b0 + l;
     }
-    first += __shfl(upto, 63);
+    first += __builtin_amdgcn_readlane(upto, 63);
   }
   return fp.batch;
 }
@@ -124,8 +115,6 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
     from = w * fp.chunk;
     to = from + fp.chunk;
     b = few_find(fp, row0, kStage, from, lane, first);
-    b = __builtin_amdgcn_readfirstlane(b);
-    first = __builtin_amdgcn_readfirstlane(first);
   } else {
     b = w, first = 0, from = 0, to = 1 << 30;
   }
@@ -435,9 +424,6 @@ template <int D>
 __global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp, int stage,
                                                                    int tile_rows) {
   const AttnParams& p = fp.a;
-  constexpr int kCols = D / 4;          // lanes per partial row
-  constexpr int kParts = 64 / kCols;    // partials per load
-  constexpr int kBatch = 8;             // loads in flight
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int tile = blockIdx.x % fp.row_tiles, z = blockIdx.x / fp.row_tiles;
   const int g = z % p.hkv, b = z / p.hkv;
@@ -446,7 +432,7 @@ __global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp,
   int before = 0;
   for (int b0 = 0; b0 < b; b0 += 64)
     before += b0 + lane < b ? few_stages(p, b0 + lane, row0, stage) : 0;
-  for (int m = 32; m >= 1; m >>= 1) before += __shfl_xor(before, m);
+  before = lanes_all(before, 0, AddOp{});
   const int n = few_stages(p, b, row0, stage);
   const int w0 = before / fp.chunk, w1 = (before + n - 1) / fp.chunk;
   if (n == 0 || w0 == w1) return;  // nothing here, or written out by its only workgroup
@@ -454,48 +440,14 @@ __global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp,
   const int n_rows = min((p.cu_block[b + 1] - bbeg) * G - row0, tile_rows);
   const size_t line = static_cast<size_t>(g * fp.row_tiles + tile) * fp.groups;
   const int parts = w1 - w0 + 1;
-  const int c = 4 * (lane % kCols), sub = lane / kCols;
   for (int r = wave; r < n_rows; r += 8) {
     // row of partial k: slot 1 of the first workgroup, slot 0 of the others
     auto at = [&](int k) {
       return ((line + w0 + k) * 2 + (k == 0 ? 1 : 0)) * tile_rows + r;
     };
-    float M = kNegBig;
-    for (int k = lane; k < parts; k += 64) M = fmaxf(M, fp.m_part[at(k)]);
-    for (int m = 32; m >= 1; m >>= 1) M = fmaxf(M, __shfl_xor(M, m));
-    f32x4 x{};
-    float l = 0.f;
-    for (int k0 = 0; k0 < parts; k0 += kBatch * kParts) {
-      f32x4 y[kBatch];
-      float mk[kBatch], lk[kBatch];
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        const size_t i = at(min(k0 + j * kParts + sub, parts - 1));
-        y[j] = *reinterpret_cast<const f32x4*>(fp.o_part + i * D + c);
-        mk[j] = fp.m_part[i];
-        lk[j] = fp.l_part[i];
-      }
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        const float f = k0 + j * kParts + sub < parts ? fast_exp2(mk[j] - M) : 0.f;
-        if (f == 0.f) continue;  // (an infinite value of weight zero)
-        l = fmaf(f, lk[j], l);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = fmaf(f, y[j][e], x[e]);
-      }
-    }
-    for (int m = kCols; m < 64; m <<= 1) {
-      l += __shfl_xor(l, m);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], m);
-    }
-    if (sub == 0) {
-      const int row = row0 + r;
-      const size_t dst = static_cast<size_t>(bbeg + row / G) * p.hq + g * G + row % G;
-      const float inv = 1.0f / l;
-      *reinterpret_cast<u32x2*>(p.out + dst * D + c) =
-          u32x2{pack2_bf16(x[0] * inv, x[1] * inv), pack2_bf16(x[2] * inv, x[3] * inv)};
-    }
+    const int row = row0 + r;
+    const size_t dst = static_cast<size_t>(bbeg + row / G) * p.hq + g * G + row % G;
+    merge_partials<D>(at, parts, fp.o_part, fp.m_part, fp.l_part, lane).store(p.out + dst * D, lane);
   }
 }
 

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "attn_common.hpp"
+#include "attn_partials.hpp"
 #include "attn_small.hpp"
 #include "eb_common.hpp"
 #include "paged.hpp"
@@ -22,12 +23,6 @@ constexpr int kXcdCount = 8;  // XCDs of the chip (workgroups are dealt to them 
 struct PackedKeys {
   static constexpr bool kPaged = false, kE4m3 = false;
 };
-template <bool kBits8>
-struct PagedKeys {
-  static constexpr bool kPaged = true, kE4m3 = kBits8;
-  PagedKv kv;
-};
-
 // Page numbers of one sequence: the wave holds 64 entries of its row of the table, a lane each, and
 // the 64 behind them on their way, so that taking one costs no memory access.  Entries are asked for
 // in rising order, and none is left out by a whole window.
@@ -53,6 +48,160 @@ struct PageWindow {
   }
 };
 
+// Key ranges of a launch over pages.  A sequence's stages (its cached rows, then the block's) are cut
+// into n_b nearly equal ranges of at most `chunk` stages, and an item is one (range, K/V head, tile of
+// query rows); the row tiles of a range are neighbours, so that they run on one XCD at a time and
+// share its keys.
+// With cap > 0 every workgroup finds chunk itself, from the lengths, which the host does not know: of
+// kPlanCandidates cuts of the longest sequence the cheapest with at most cap items, by the rounds of
+// kAttnTargetWgs workgroups and the partials.  (The lanes hold a sequence each, so this is for at
+// most 64 of them, and takes a microsecond.)  Against as many ranges for every sequence as fill the
+// chip when all are as long as the longest: 28/4 heads x 128, 16 blocks of 32 to 256 rows behind 2000
+// to 16000, 576 -> 453 us; 8 of 20 to 100 behind 1000 to 8000, 71 -> 60 us; 16/4 heads x 64, the
+// same, 49 -> 32 us.  Equal lengths gain nothing (32 heads, 1000 rows behind 3000: 89 and 91 us).
+// With cap = 0 chunk is the host's, and every sequence counts as the longest, with as many row tiles.
+struct TilePlan {
+  int batch, row_tiles;
+  int cap;
+  int chunk, nsplit;  // cap = 0: stages per range, ranges per sequence
+  float* o_part;      // [items, kRowsPerWg, D], then m and l [items, kRowsPerWg]
+  float* m_part;
+  float* l_part;
+  int32_t* found;  // cap > 0: of each of kPlanMaxBatch sequences its first item, then its ranges
+};
+template <bool kBits8>
+struct PagedKeys {
+  static constexpr bool kPaged = true, kE4m3 = kBits8;
+  PagedKv kv;
+  TilePlan plan;
+};
+constexpr int kPlanMaxBatch = 64;
+constexpr int kPlanCandidates = 32;
+// Costs in stages of one of two workgroups of a compute unit: of a last round that leaves each
+// compute unit one (which is the faster for it), of a workgroup's start and end, of the merge's
+// launch, and of one row's partial, written and read.
+constexpr float kPlanHalf = 0.65f, kPlanRange = 3.f, kPlanMerge = 2.f, kPlanRow = 1.f / 8192;
+
+// Stages and row tiles of a sequence.
+__device__ __forceinline__ int tile_stages(int plen, int len) {
+  return len > 0 ? (plen + kKeys - 1) / kKeys + (len + kKeys - 1) / kKeys : 0;
+}
+__device__ __forceinline__ int tile_rows(int len, int group) {
+  return (len * group + kRowsPerWg - 1) / kRowsPerWg;
+}
+// Parts of the longest sequence that candidate j stands for: 1 .. 16, 20 .. 48, 64 .. 176.
+__device__ __forceinline__ int plan_parts(int j) {
+  return j < 16 ? j + 1 : j < 24 ? 16 + 4 * (j - 15) : 48 + 16 * (j - 23);
+}
+
+// Where sequence b's items begin, in how many ranges, with how many row tiles.
+struct SequenceItems {
+  int first, ranges, row_tiles;
+};
+
+// The lengths of a wave's sequences (lane = sequence) and the cut they get.
+struct LanePlan {
+  int ranges, items, upto;  // of the lane's sequence; upto: items of all up to it
+  int total;
+};
+__device__ __forceinline__ LanePlan lane_plan(const AttnParams& p, const TilePlan& tp, int lane) {
+  const int own = min(lane, tp.batch - 1);
+  const int len = lane < tp.batch ? p.cu_block[own + 1] - p.cu_block[own] : 0;
+  const int stages = tile_stages(p.cu_prefix[own + 1] - p.cu_prefix[own], len);
+  const int per_range = tile_rows(len, p.group) * p.hkv;
+  const int longest = max(lanes_all(stages, 0, MaxOp{}), 1);
+  const int whole = lanes_all(per_range, 0, AddOp{});
+  const int rows = lanes_all(len * p.group, 0, AddOp{});
+  // A lane per candidate, twice: lanes 0-31 add up the even sequences' items, 32-63 the odd ones'.
+  const int parts = plan_parts(lane % kPlanCandidates);
+  int chunk = (longest + parts - 1) / parts;
+  const float inv = 1.0f / chunk;
+  int items = 0;
+  for (int b = 0; b < tp.batch; b += 2) {
+    const int st0 = __builtin_amdgcn_readlane(stages, b);
+    const int st1 = __builtin_amdgcn_readlane(stages, b + 1);
+    const int per0 = __builtin_amdgcn_readlane(per_range, b);
+    const int per1 = __builtin_amdgcn_readlane(per_range, b + 1);
+    // ceil(st / chunk) = floor((st - 1) / chunk) + 1
+    const float st = static_cast<float>(lane < kPlanCandidates ? st0 : st1) - 0.5f;
+    items += (static_cast<int>(st * inv) + 1) * (lane < kPlanCandidates ? per0 : per1);
+  }
+  items += __shfl_xor(items, kPlanCandidates);
+  const int rest = items % kAttnTargetWgs;
+  float cost = items / kAttnTargetWgs +
+               (rest == 0 ? 0.f : rest <= kAttnTargetWgs / 2 ? kPlanHalf : 1.f);
+  cost *= chunk + kPlanRange;
+  if (parts > 1)
+    cost += kPlanMerge + static_cast<float>(items) * rows * p.hkv / max(whole, 1) * kPlanRow;
+  if (items > tp.cap) cost = 1e30f;
+  // the cheapest, of equals the one with fewer parts (costs are positive: their bits order them)
+  const int least = lanes_all(__float_as_int(cost), 0x7fffffff, MinOp{});
+  const uint64_t win = __ballot(__float_as_int(cost) == least);
+  chunk = __builtin_amdgcn_readlane(chunk, __builtin_ctzll(win));
+  LanePlan l;
+  auto cut = [&](int by) {
+    l.ranges = (stages + by - 1) / by;
+    l.items = l.ranges * per_range;
+    l.upto = lanes_up_to(l.items, 0, AddOp{});
+    l.total = __builtin_amdgcn_readlane(l.upto, 63);
+  };
+  cut(chunk);
+  if (l.total > tp.cap) cut(longest);  // (a count in floats was off: whole sequences always fit)
+  return l;
+}
+
+// First stage of a range.
+__device__ __forceinline__ int range_start(int stages, int range, int ranges) {
+  const int each = stages / ranges, more = stages % ranges;
+  return range * each + min(range, more);
+}
+
+// One workgroup's item.
+struct TileItem {
+  int b, g, tile, item, range, ranges;
+};
+// The item of this workgroup; false if there is none.
+__device__ __forceinline__ bool find_item(const AttnParams& p, const TilePlan& tp, int lane,
+                                          int wave, TileItem& it) {
+  const int xcd = blockIdx.x % kXcdCount, j = blockIdx.x / kXcdCount;
+  if (tp.cap == 0) {
+    const int unit = kXcdCount * (j / tp.row_tiles) + xcd;
+    it.tile = j % tp.row_tiles;
+    it.g = unit % p.hkv;
+    it.range = unit / p.hkv % tp.nsplit;
+    it.b = unit / p.hkv / tp.nsplit;
+    it.item = unit * tp.row_tiles + it.tile;
+    if (it.b >= tp.batch) return false;
+    const int stages = tile_stages(p.cu_prefix[it.b + 1] - p.cu_prefix[it.b],
+                                   p.cu_block[it.b + 1] - p.cu_block[it.b]);
+    it.ranges = (stages + tp.chunk - 1) / tp.chunk;
+    return it.range < it.ranges;
+  }
+  // The items in 8 turns equal runs, dealt to the XCDs in turn: runs of at least as many items as
+  // the longest block has row tiles, for the sharing.  turns divides 64, so that an XCD gets no more
+  // items than its share of the cap.
+  const LanePlan l = lane_plan(p, tp, lane);
+  int turns = 1;
+  while (turns < 64 && 2 * turns * kXcdCount * tp.row_tiles <= l.total) turns *= 2;
+  const int runs = turns * kXcdCount, most = (l.total + runs - 1) / runs;
+  const int run = j / most * kXcdCount + xcd;
+  it.item = run * l.total / runs + j % most;
+  if (run >= runs || it.item >= (run + 1) * l.total / runs) return false;
+  if (it.item == 0 && wave == 0) {  // for the merge
+    tp.found[lane] = l.upto - l.items;
+    tp.found[kPlanMaxBatch + lane] = l.ranges;
+  }
+  const int b = __builtin_ctzll(__ballot(l.upto > it.item));
+  const int local = it.item - __builtin_amdgcn_readlane(l.upto - l.items, b);
+  const int row_tiles = tile_rows(p.cu_block[b + 1] - p.cu_block[b], p.group);
+  it.b = b;
+  it.tile = local % row_tiles;
+  it.g = local / row_tiles % p.hkv;
+  it.range = local / row_tiles / p.hkv;
+  it.ranges = __builtin_amdgcn_readlane(l.ranges, b);
+  return true;
+}
+
 // Two workgroups per compute unit (<= 256 VGPRs per lane, no spills at D = 128), so one
 // wave's softmax arithmetic overlaps another wave's MFMAs on the same SIMD (batch 64 at
 // D = 128: 1.85 ms with one workgroup per compute unit, 1.07 ms with two).
@@ -70,14 +219,23 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnParams p, Ke
   // range) all run on one XCD, one after another: workgroups are dealt to the 8 XCDs round-robin
   // by id, and the tiles of unit u take ids 8 (row_tiles (u / 8) + tile) + u % 8.  They then read
   // the unit's K/V stages from that XCD's L2 instead of each XCD fetching them.
-  const int xcd = blockIdx.x % kXcdCount, j = blockIdx.x / kXcdCount;
-  const int unit = kXcdCount * (j / row_tiles) + xcd;
-  if (unit >= units) return;  // whole workgroup: padding of the last round
-  const int tile = j % row_tiles;
-  const int z = unit / p.hkv;
-  const int b = z / p.nsplit;
-  const int sp = z % p.nsplit;
-  const int g = unit % p.hkv;
+  [[maybe_unused]] TileItem it;
+  int b, g, sp, tile;
+  if constexpr (Keys::kPaged) {
+    if (!find_item(p, keys.plan, threadIdx.x & 63,
+                   __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), it))
+      return;  // whole workgroup
+    b = it.b, g = it.g, sp = it.range, tile = it.tile;
+  } else {
+    const int xcd = blockIdx.x % kXcdCount, j = blockIdx.x / kXcdCount;
+    const int unit = kXcdCount * (j / row_tiles) + xcd;
+    if (unit >= units) return;  // whole workgroup: padding of the last round
+    tile = j % row_tiles;
+    const int z = unit / p.hkv;
+    b = z / p.nsplit;
+    sp = z % p.nsplit;
+    g = unit % p.hkv;
+  }
   const int G = p.group;
   const int bbeg = p.cu_block[b];
   const int len = p.cu_block[b + 1] - bbeg;
@@ -90,9 +248,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnParams p, Ke
   const int slen = p.cu_suffix ? p.cu_suffix[b + 1] - sbeg : 0;
   const int cached = Keys::kPaged ? (plen + kKeys - 1) / kKeys * kKeys : plen;
   const int n_keys = cached + len + slen;
-  const int kbeg = sp * p.kps;
+  int kbeg = sp * p.kps, kend = kbeg + p.kps;
+  if constexpr (Keys::kPaged) {
+    const int stages = tile_stages(plen, len);
+    kbeg = range_start(stages, it.range, it.ranges) * kKeys;
+    kend = range_start(stages, it.range + 1, it.ranges) * kKeys;
+  }
   if (kbeg >= n_keys) return;  // whole workgroup: this key range lies past the sequence
-  const int kend = min(n_keys, kbeg + p.kps);
+  kend = min(n_keys, kend);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int half = lane >> 5, l32 = lane & 31;
@@ -374,9 +537,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnParams p, Ke
 
   const float l_tot = l_run + __shfl_xor(l_run, 32);
   if (!row_ok) return;
-  if (p.nsplit > 1) {
-    const size_t idx = (static_cast<size_t>(bbeg + pos) * p.hq + g * G + hh) * p.nsplit + sp;
-    float* dst = p.o_part + idx * D;
+  if (Keys::kPaged ? it.ranges > 1 : p.nsplit > 1) {
+    float *o_part = p.o_part, *m_part = p.m_part, *l_part = p.l_part;
+    size_t idx = (static_cast<size_t>(bbeg + pos) * p.hq + g * G + hh) * p.nsplit + sp;
+    if constexpr (Keys::kPaged) {
+      idx = static_cast<size_t>(it.item) * kRowsPerWg + wave * 32 + l32;
+      o_part = keys.plan.o_part, m_part = keys.plan.m_part, l_part = keys.plan.l_part;
+    }
+    float* dst = o_part + idx * D;
 #pragma unroll
     for (int db = 0; db < kDBlocks; ++db)
 #pragma unroll
@@ -386,8 +554,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnParams p, Ke
             f32x4{o[db][4 * q4 + 0], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
       }
     if (half == 0) {
-      p.m_part[idx] = m_run;
-      p.l_part[idx] = l_tot;
+      m_part[idx] = m_run;
+      l_part[idx] = l_tot;
     }
     return;
   }
@@ -456,14 +624,23 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
 
   // Workgroup id -> (unit, row tile) as in attn_bf16_kernel: the row tiles of one unit run on
   // one XCD, one after another, and share that XCD's L2.
-  const int xcd = blockIdx.x % kXcdCount, jx = blockIdx.x / kXcdCount;
-  const int unit = kXcdCount * (jx / row_tiles) + xcd;
-  if (unit >= units) return;  // whole workgroup: padding of the last round
-  const int tile = jx % row_tiles;
-  const int z = unit / p.hkv;
-  const int b = z / p.nsplit;
-  const int sp = z % p.nsplit;
-  const int g = unit % p.hkv;
+  [[maybe_unused]] TileItem it;
+  int b, g, sp, tile;
+  if constexpr (Keys::kPaged) {
+    if (!find_item(p, keys.plan, threadIdx.x & 63,
+                   __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), it))
+      return;  // whole workgroup
+    b = it.b, g = it.g, sp = it.range, tile = it.tile;
+  } else {
+    const int xcd = blockIdx.x % kXcdCount, jx = blockIdx.x / kXcdCount;
+    const int unit = kXcdCount * (jx / row_tiles) + xcd;
+    if (unit >= units) return;  // whole workgroup: padding of the last round
+    tile = jx % row_tiles;
+    const int z = unit / p.hkv;
+    b = z / p.nsplit;
+    sp = z % p.nsplit;
+    g = unit % p.hkv;
+  }
   const int G = p.group;
   const int bbeg = p.cu_block[b];
   const int len = p.cu_block[b + 1] - bbeg;
@@ -476,9 +653,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
   const int slen = p.cu_suffix ? p.cu_suffix[b + 1] - sbeg : 0;
   const int cached = Keys::kPaged ? (plen + kKeys - 1) / kKeys * kKeys : plen;
   const int n_keys = cached + len + slen;
-  const int kbeg = sp * p.kps;
+  int kbeg = sp * p.kps, kend = kbeg + p.kps;
+  if constexpr (Keys::kPaged) {
+    const int stages = tile_stages(plen, len);
+    kbeg = range_start(stages, it.range, it.ranges) * kKeys;
+    kend = range_start(stages, it.range + 1, it.ranges) * kKeys;
+  }
   if (kbeg >= n_keys) return;  // whole workgroup: this key range lies past the sequence
-  const int kend = min(n_keys, kbeg + p.kps);
+  kend = min(n_keys, kend);
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // uniform: scalar buffer resources
@@ -534,47 +716,59 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
   // This wave's half (K or V) of the tile of keys kv0 .. kv0 + 63 into dst.  Keys past kend come
   // from a clamped, valid row; their scores are set to -inf.
   [[maybe_unused]] PageWindow window;
-  if constexpr (Keys::kPaged) window.start(keys.kv, b, kbeg >> keys.kv.page_shift, lane);
+  [[maybe_unused]] int page_shift, page_mask;
+  [[maybe_unused]] unsigned n_pages;
+  [[maybe_unused]] size_t page_bytes;      // a page of every head
+  [[maybe_unused]] const uint8_t* pool_g;  // this head's rows of page 0
+  [[maybe_unused]] const uint8_t* scale_g;
+  [[maybe_unused]] const uint8_t* blk_g = reinterpret_cast<const uint8_t*>(blk0);
+  if constexpr (Keys::kPaged) {
+    constexpr int kHeld = Keys::kE4m3 ? D : kRowBytes;  // bytes of a cached row
+    window.start(keys.kv, b, kbeg >> keys.kv.page_shift, lane);
+    page_shift = keys.kv.page_shift;
+    page_mask = (1 << page_shift) - 1;
+    n_pages = keys.kv.n_pages;
+    page_bytes = (static_cast<size_t>(p.hkv) << page_shift) * kHeld;
+    pool_g = (k_wave ? keys.kv.k : keys.kv.v) + (static_cast<size_t>(g) << page_shift) * kHeld;
+    if constexpr (Keys::kE4m3)
+      scale_g = (k_wave ? keys.kv.k_scale : keys.kv.v_scale) + (static_cast<size_t>(g) << page_shift);
+  }
   auto issue = [&](int kv0, uint8_t* dst) {
     if constexpr (Keys::kPaged) {
       // A wave loads 32 keys in two groups of 16, each within one page (or within the block): a
       // buffer resource per load, at its first row, ends with the group's last existing row, so
       // rows past it arrive as zeros.
-      const uint8_t* const pool = k_wave ? keys.kv.k : keys.kv.v;
-      const uint8_t* const blk = reinterpret_cast<const uint8_t*>(k_wave ? p.k_blk : p.v_blk);
       const bool paged = !Keys::kE4m3 && kv0 < cached;  // 8-bit tiles: fetch and place
       const uint32_t stride = paged ? kRowBytes : key_bytes;
       int lane_ = lane;
       if constexpr (Keys::kE4m3) asm volatile("" : "+v"(lane_));  // (as in place)
       const uint32_t row_off = static_cast<uint32_t>(lane_ >> 4) * stride;
+      if (paged) window.advance(kv0 >> page_shift, lane);
+      // where the wave's rows go (formed here, not kept per load over the loop)
+      uint32_t to = static_cast<uint32_t>(dst - smem) + (wave & 1) * (kTileBytes / 2);
+      asm volatile("" : "+s"(to));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int at = kv0 + 32 * (wave & 1) + 16 * h;
         const uint8_t* base;
         int rows;
         if (paged) {
-          const int entry = at >> keys.kv.page_shift;
-          window.advance(entry, lane);
-          const int page = window.uniform(entry);
-          const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(keys.kv.n_pages);
-          base = pool + ((((static_cast<size_t>(ok ? page : 0) * p.hkv + g)
-                           << keys.kv.page_shift) +
-                          (at & ((1 << keys.kv.page_shift) - 1))) *
-                         kRowBytes);
+          const int page = window.uniform(at >> page_shift);
+          const bool ok = static_cast<unsigned>(page) < n_pages;
+          base = pool_g + (ok ? page : 0) * page_bytes + (at & page_mask) * kRowBytes;
           rows = ok ? plen - at : 0;
         } else {
           const int j = at - cached;
-          base = blk + (static_cast<size_t>(bbeg + min(j, len)) * p.hkv + g) * kRowBytes;
+          base = blk_g + min(j, len) * static_cast<size_t>(key_bytes);
           rows = len - j;
         }
         const int bytes =
             rows > 0 ? (min(rows, 16) - 1) * static_cast<int>(stride) + kRowBytes : 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int n = (wave * kInstPerWave + 4 * h + i) % kInstPerTile;
           buffer_load_to_lds(make_rsrc(base + 4 * i * static_cast<size_t>(stride),
                                        max(bytes - 4 * i * static_cast<int>(stride), 0)),
-                             dst + n * 1024,
+                             smem + to + (4 * h + i) * 1024,
                              row_off + 16u * static_cast<uint32_t>((lane_ & 15) ^ swz(lane_, i)), 0);
         }
       }
@@ -615,24 +809,21 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
   auto fetch = [&](int kv0) {
     if constexpr (Keys::kE4m3) {
       if (kv0 >= cached) return;
-      const uint8_t* const pool = k_wave ? keys.kv.k : keys.kv.v;
-      const uint8_t* const scale = k_wave ? keys.kv.k_scale : keys.kv.v_scale;
+      window.advance(kv0 >> page_shift, lane);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int at = kv0 + 32 * (wave & 1) + 16 * h;
-        const int entry = at >> keys.kv.page_shift;
-        window.advance(entry, lane);
-        const int page = window.uniform(entry);
-        const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(keys.kv.n_pages);
-        const size_t row = ((static_cast<size_t>(ok ? page : 0) * p.hkv + g) << keys.kv.page_shift) +
-                           (at & ((1 << keys.kv.page_shift) - 1));
-        const int rows = ok ? min(max(plen - at, 0), 16) : 0;
-        const __amdgpu_buffer_rsrc_t rs = make_rsrc(pool + row * D, rows * D);
-        // load i of the group: rows 2 (lane / 8) + i
+        const int page = window.uniform(at >> page_shift);
+        const bool ok = static_cast<unsigned>(page) < n_pages;
+        const size_t from = (ok ? page : 0) * page_bytes;
+        const int row = at & page_mask, rows = ok ? min(max(plen - at, 0), 16) : 0;
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(pool_g + from + row * D, rows * D);
+      // load i of the group: rows 2 (lane / 8) + i
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           raw[2 * h + i] = buffer_load16(rs, (2 * (lane >> 3) + i) * D + 16 * (lane & 7));
-        raw_scale[h] = buffer_load2(make_rsrc(scale + row, (rows + 1) & ~1), 2 * (lane >> 3));
+        raw_scale[h] = buffer_load2(make_rsrc(scale_g + from / D + row, (rows + 1) & ~1),
+                                    2 * (lane >> 3));
       }
     }
   };
@@ -739,6 +930,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
       const int to = st + (k_wave ? 2 : 1);  // the tile in the registers
       if (to < n_stages) place(tile_at(to), k_wave ? ktile(st) : vtile(st + 1));
       if (to + 1 < n_stages) fetch(tile_at(to + 1));
+    } else if constexpr (Keys::kPaged) {
+      const int to = st + (k_wave ? 2 : 1);
+      if (to < n_stages) issue(tile_at(to), k_wave ? ktile(st) : vtile(st + 1));
     } else if (k_wave) {
       if (st + 2 < n_stages) issue(kbeg + (st + 2) * kDmaKeys, ktile(st));
     } else {
@@ -835,9 +1029,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
 
   const float l_tot = l_run + __shfl_xor(l_run, 32);
   if (!row_ok) return;
-  if (p.nsplit > 1) {
-    const size_t idx = (static_cast<size_t>(bbeg + pos) * p.hq + g * G + hh) * p.nsplit + sp;
-    float* dst = p.o_part + idx * D;
+  if (Keys::kPaged ? it.ranges > 1 : p.nsplit > 1) {
+    float *o_part = p.o_part, *m_part = p.m_part, *l_part = p.l_part;
+    size_t idx = (static_cast<size_t>(bbeg + pos) * p.hq + g * G + hh) * p.nsplit + sp;
+    if constexpr (Keys::kPaged) {
+      idx = static_cast<size_t>(it.item) * kRowsPerWg + wave * 32 + l32;
+      o_part = keys.plan.o_part, m_part = keys.plan.m_part, l_part = keys.plan.l_part;
+    }
+    float* dst = o_part + idx * D;
 #pragma unroll
     for (int db = 0; db < kDBlocks; ++db)
 #pragma unroll
@@ -847,8 +1046,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
             f32x4{o[db][4 * q + 0], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
       }
     if (half == 0) {
-      p.m_part[idx] = m_run;
-      p.l_part[idx] = l_tot;
+      m_part[idx] = m_run;
+      l_part[idx] = l_tot;
     }
     return;
   }
@@ -863,6 +1062,38 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
                     pack2_bf16(o[db][4 * q + 2] * inv, o[db][4 * q + 3] * inv)};
       *reinterpret_cast<u32x2*>(dst + d) = v;
     }
+}
+
+// The ranges of every (block row, query head) of a launch over pages, in key order: a wave per pair,
+// its lanes over partials side by side.
+template <int D>
+__global__ __launch_bounds__(kThreads) void attn_tiles_merge_kernel(AttnParams p, TilePlan tp,
+                                                                    int total) {
+  const int lane = threadIdx.x & 63;
+  const long rh = static_cast<long>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  if (rh >= static_cast<long>(total) * p.hq) return;  // uniform per wavefront
+  const int row = static_cast<int>(rh / p.hq), h = static_cast<int>(rh % p.hq);
+  const int b = find_sequence(p.cu_block, tp.batch, row, lane);
+  const int len = p.cu_block[b + 1] - p.cu_block[b];
+  const int g = h / p.group, r = (row - p.cu_block[b]) * p.group + h % p.group;
+  const int tile = r / kRowsPerWg;
+  int first, ranges, row_tiles;
+  if (tp.cap > 0) {
+    first = tp.found[b];
+    ranges = tp.found[kPlanMaxBatch + b];
+    row_tiles = tile_rows(len, p.group);
+  } else {
+    row_tiles = tp.row_tiles;
+    first = b * tp.nsplit * p.hkv * row_tiles;
+    ranges = (tile_stages(p.cu_prefix[b + 1] - p.cu_prefix[b], len) + tp.chunk - 1) / tp.chunk;
+  }
+  if (ranges <= 1) return;  // written out by its only workgroup
+  auto at = [&](int k) {
+    return (first + (static_cast<size_t>(k) * p.hkv + g) * row_tiles + tile) * kRowsPerWg +
+           r % kRowsPerWg;
+  };
+  const PartialRow<D> x = merge_partials<D>(at, ranges, tp.o_part, tp.m_part, tp.l_part, lane);
+  x.store(p.out + rh * D, lane);
 }
 
 }  // namespace

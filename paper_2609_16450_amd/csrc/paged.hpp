@@ -69,6 +69,34 @@ __device__ __forceinline__ void e4m3_widen(u32x4 w, float scale, u32x4& lo, u32x
              e4m3_pair_bf16<false>(w[3], scale), e4m3_pair_bf16<true>(w[3], scale)};
 }
 
+// Reductions over the wavefront by lane shifts within rows of 16 and broadcasts between them, which
+// cost an instruction each (a shuffle goes through LDS).  `op` combines a lane's value with that of
+// lanes before it; `none` is its neutral value.  lanes_up_to: over the lanes up to this one;
+// lanes_all: over all, uniform.
+template <class Op>
+__device__ __forceinline__ int lanes_up_to(int x, int none, Op op) {
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x111, 0xf, 0xf, false));  // from lane - 1
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));  // - 2
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));  // - 4
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));  // - 8
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));  // lane 15 to row 1, 47 to 3
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));  // lane 31 to rows 2, 3
+  return x;
+}
+template <class Op>
+__device__ __forceinline__ int lanes_all(int x, int none, Op op) {
+  return __builtin_amdgcn_readlane(lanes_up_to(x, none, op), 63);
+}
+struct AddOp {
+  __device__ __forceinline__ int operator()(int a, int b) const { return a + b; }
+};
+struct MaxOp {
+  __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); }
+};
+struct MinOp {
+  __device__ __forceinline__ int operator()(int a, int b) const { return min(a, b); }
+};
+
 // The sequence that owns packed row `row` of a batch with offsets cu: the number of sequences that
 // end at or before it, found by the whole wavefront with one load per 64 sequences (`row` is
 // uniform).  At most batch - 1.
