@@ -198,6 +198,9 @@ def _dev(t: torch.Tensor, name: str, dtype=None, shape=None) -> None:
 
 def _dev_on(index: int, t: torch.Tensor, name: str, dtype=None, shape=None) -> None:
     """As _dev, with the tensor on device `index`."""
+    if (isinstance(t, torch.Tensor) and t.get_device() == index and t.is_contiguous()
+            and (dtype is None or t.dtype is dtype) and (shape is None or t.shape == shape)):
+        return
     _dev(t, name, dtype, shape)
     if t.get_device() != index:
         raise ValueError(f"{name} is on device {t.get_device()}, the cache on {index}")
@@ -392,35 +395,36 @@ class PagedKV:
         return PagedKV(pool(), pool(), page_table, scale(), scale())
 
 
-def _paged(r: Ragged, kv: PagedKV, stream) -> int:
-    """Checks what every call on a paged cache shares; returns the stream's handle."""
+def _paged(r: Ragged, kv: PagedKV, stream) -> tuple:
+    """Checks what every call on a paged cache shares; returns (eb_ragged, stream handle)."""
     if not isinstance(kv, PagedKV):
         raise TypeError("kv must be a PagedKV")
     if kv.batch != r.batch:
         raise ValueError(f"page_table has {kv.batch} rows, the batch {r.batch}")
-    for name, cu in (("cu_block", r.cu_block), ("cu_prefix", r.cu_prefix)):
-        _dev_on(kv.device_index, cu, name)
+    rc, index = r.c(), kv.device_index
+    if r.cu_block.get_device() != index or r.cu_prefix.get_device() != index:
+        raise ValueError(f"the batch's offsets and the cache (device {index}) are on different "
+                         "devices")
     # a launch goes to the current device: refuse tensors and streams of another one
-    if torch.cuda.current_device() != kv.device_index:
-        raise ValueError(f"the cache is on device {kv.device_index}, the current device is "
-                         f"{torch.cuda.current_device()}")
-    if isinstance(stream, torch.cuda.Stream) and stream.device_index != kv.device_index:
-        raise ValueError(f"the cache is on device {kv.device_index}, the stream on "
-                         f"{stream.device_index}")
-    return _stream(stream)
+    current = torch.cuda.current_device() if _get_device is None else _get_device()
+    if current != index:
+        raise ValueError(f"the cache is on device {index}, the current device is {current}")
+    if stream is not None and isinstance(stream, torch.cuda.Stream) and \
+            stream.device_index != index:
+        raise ValueError(f"the cache is on device {index}, the stream on {stream.device_index}")
+    return rc, _stream(stream)
 
 
 def eb_kv_write(r: Ragged, kv: PagedKV, k, v, pos=None, stream=None) -> None:
     """Block rows k, v [T, hkv, D] into the cache's pages: at positions pos [T] int32 of their
     sequences (negative: left out), or appended to the cached rows without pos (eb.h)."""
-    s = _paged(r, kv, stream)
+    rc, s = _paged(r, kv, stream)
     dt = _dtype_code(k)
     shape = (r.total_block, kv.hkv, kv.head_dim)
     _dev_on(kv.device_index, k, "k", k.dtype, shape)
     _dev_on(kv.device_index, v, "v", k.dtype, shape)
     if pos is not None:
         _dev_on(kv.device_index, pos, "pos", torch.int32, (r.total_block,))
-    rc = r.c()
     _check(load().eb_kv_write(dt, ctypes.byref(rc), kv._ref, _ptr(pos), k.data_ptr(),
                               v.data_ptr(), s), "eb_kv_write")
 
@@ -428,12 +432,11 @@ def eb_kv_write(r: Ragged, kv: PagedKV, k, v, pos=None, stream=None) -> None:
 def eb_kv_read(r: Ragged, kv: PagedKV, k, v, stream=None) -> None:
     """k, v [S, hkv, D] <- the cached rows of every sequence (r's prefix lengths), packed as
     eb_block_attn and eb_decode_step take them (eb.h)."""
-    s = _paged(r, kv, stream)
+    rc, s = _paged(r, kv, stream)
     dt = _dtype_code(k)
     shape = (r.total_prefix, kv.hkv, kv.head_dim)
     _dev_on(kv.device_index, k, "k", k.dtype, shape)
     _dev_on(kv.device_index, v, "v", k.dtype, shape)
-    rc = r.c()
     _check(load().eb_kv_read(dt, ctypes.byref(rc), kv._ref, k.data_ptr(), v.data_ptr(), s),
            "eb_kv_read")
 
@@ -448,21 +451,22 @@ def eb_block_attn_paged(r: Ragged, kv: PagedKV, q, k_blk, v_blk, out,
                         stream=None) -> None:
     """out[T, hq, D] <- block attention of q over the cached rows (r's prefix lengths) and the block
     keys (eb.h)."""
-    s = _paged(r, kv, stream)
+    rc, s = _paged(r, kv, stream)
     dt = _dtype_code(q)
     T, hq, D = q.shape
     _dev_on(kv.device_index, q, "q", q.dtype, (r.total_block, hq, kv.head_dim))
     _dev_on(kv.device_index, k_blk, "k_blk", q.dtype, (r.total_block, kv.hkv, kv.head_dim))
     _dev_on(kv.device_index, v_blk, "v_blk", q.dtype, (r.total_block, kv.hkv, kv.head_dim))
     _dev_on(kv.device_index, out, "out", q.dtype, (r.total_block, hq, kv.head_dim))
-    if ws is not None and ws.get_device() != kv.device_index:
-        raise ValueError(f"ws must be on device {kv.device_index}")
     scale = 0.0 if scale is None else float(scale)    # 0: the library's 1/sqrt(D)
-    rc = r.c()
     rp = ctypes.byref(rc)
     lib = load()
-    need = int(lib.eb_block_attn_paged_workspace(dt, rp, kv._ref, hq))
-    wp, wn = _workspace(need, ws, q.device, stream)
+    if ws is None:
+        need = int(lib.eb_block_attn_paged_workspace(dt, rp, kv._ref, hq))
+        wp, wn = _workspace(need, None, q.device, stream)
+    else:  # the library compares its size with what the call needs
+        _dev_on(kv.device_index, ws, "ws", torch.uint8)
+        wp, wn = ws.data_ptr(), ws.numel()
     _check(lib.eb_block_attn_paged(dt, rp, kv._ref, hq, scale, q.data_ptr(), k_blk.data_ptr(),
                                    v_blk.data_ptr(), out.data_ptr(), wp, wn, s),
            "eb_block_attn_paged")
