@@ -147,7 +147,9 @@ eb_status eb_block_attn_dual(eb_dtype dt, const eb_ragged* r, const eb_suffix* s
  * are dropped.  Table entries behind a sequence's last page are not read.
  *
  * Requires hkv >= 1, head_dim in {64, 128}, page_size in {16, 32, 64, 128, 256}, n_pages >= 1,
- * max_pages >= 1 and, where cached rows are read, max_prefix <= max_pages * page_size.
+ * max_pages >= 1 and, where cached rows are read, max_prefix <= max_pages * page_size.  One write or
+ * read moves at most 2^34 values of K.  An attention call takes at most 65535 sequences of at most
+ * 2^30 keys, and hkv at most 65535 (EB_ERR_UNSUPPORTED beyond).
  * With EB_DEBUG_CHECKS the page numbers that a call uses have to lie in [0, n_pages).
  * ------------------------------------------------------------------------------------- */
 typedef struct {

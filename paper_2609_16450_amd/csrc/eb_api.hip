@@ -45,7 +45,7 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 constexpr size_t kWsAlign = 256;
 constexpr int kMaxGridYZ = 65535;       // second and third dimension of a launch grid
 constexpr int kMaxKeys = 1 << 30;       // of one sequence
-constexpr int kMaxPackedRows = 1 << 27; // rows that one launch of the cache kernels indexes
+constexpr int64_t kMaxPackedValues = 1LL << 34;  // of K in one launch of the cache kernels
 constexpr int kProbeMaxGroups = 65536;
 constexpr int kProbeMaxIters = 1 << 20;
 size_t round_up(size_t n) { return (n + kWsAlign - 1) / kWsAlign * kWsAlign; }
@@ -171,6 +171,14 @@ eb_status check_paged_prefix(const eb_ragged* r, const eb_paged_kv* kv) {
   if (r->max_prefix > capacity)
     return fail(EB_ERR_INVALID, "max_prefix %d does not fit %d pages of %d rows", r->max_prefix,
                 kv->max_pages, kv->page_size);
+  return EB_OK;
+}
+
+// Rows that one write or read moves (a thread for 8 values; a launch has fewer than 2^32).
+eb_status check_rows(int32_t rows, const eb_paged_kv* kv) {
+  if (static_cast<int64_t>(rows) * kv->hkv * kv->head_dim > kMaxPackedValues)
+    return fail(EB_ERR_UNSUPPORTED, "%d rows of %d heads x %d in one call (at most 2^34 values)",
+                rows, kv->hkv, kv->head_dim);
   return EB_OK;
 }
 
@@ -441,8 +449,8 @@ eb_status eb_kv_write(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, co
   eb_status st = check_ragged(r, pos == nullptr);
   if (st == EB_OK) st = check_paged(dt, kv);
   if (st != EB_OK) return st;
-  if (r->total_block > kMaxPackedRows)
-    return fail(EB_ERR_UNSUPPORTED, "more than %d rows in one call", kMaxPackedRows);
+  st = check_rows(r->total_block, kv);
+  if (st != EB_OK) return st;
   if (r->total_block > 0 && (!k || !v)) return fail(EB_ERR_INVALID, "NULL k / v");
   if (dt == EB_BF16 && r->total_block > 0 && (!aligned16(k) || !aligned16(v)))
     return fail(EB_ERR_INVALID, "bf16 tensors must be 16-byte aligned");
@@ -460,8 +468,8 @@ eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, voi
   if (st == EB_OK) st = check_paged(dt, kv);
   if (st == EB_OK) st = check_paged_prefix(r, kv);
   if (st != EB_OK) return st;
-  if (r->total_prefix > kMaxPackedRows)
-    return fail(EB_ERR_UNSUPPORTED, "more than %d rows in one call", kMaxPackedRows);
+  st = check_rows(r->total_prefix, kv);
+  if (st != EB_OK) return st;
   if (r->total_prefix > 0 && (!k || !v)) return fail(EB_ERR_INVALID, "NULL k / v");
   if (dt == EB_BF16 && r->total_prefix > 0 && (!aligned16(k) || !aligned16(v)))
     return fail(EB_ERR_INVALID, "bf16 tensors must be 16-byte aligned");
