@@ -159,6 +159,7 @@ def cpu_baseline(case, budget_s: float = 15.0):
 
 
 SUFFIX_LEN = 256         # cached suffix rows per sequence on the dual-cache leg
+PAGE_SIZE = 64           # rows per page (paths paged, paged8)
 LBS_WINDOW = 512         # generation window of the LBS leg (generation length 512, App. F)
 TAU_PSI = 0.9            # LPS acceptance threshold on the lps leg
 TOP_M = 2                # per-block budget on the topm leg
@@ -211,6 +212,25 @@ def measured_peaks(torch, eb) -> dict:
                      "same box, same run")}
 
 
+def paged_cache(torch, eb, case, ds, e4m3: bool):
+    """A paged cache that holds the workload's prefixes and has room for its blocks; the pages are
+    handed out in a shuffled order, as an allocator in service leaves them."""
+    cfg = case.cfg
+    need = [-(-int(p + b) // PAGE_SIZE) for p, b in zip(case.prefix_lens, case.block_lens)]
+    order = np.random.default_rng(cfg.seed).permutation(sum(need)).astype(np.int32)
+    table = np.full((case.batch, max(need)), -1, np.int32)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    dtype = torch.float8_e4m3fn if e4m3 else ds.k_pre.dtype
+    kv = eb.PagedKV.empty(sum(need), cfg.hkv, PAGE_SIZE, cfg.head_dim,
+                          torch.from_numpy(table).to(ds.q.device), dtype)
+    eb.eb_kv_write(eb.Ragged.from_lengths(case.prefix_lens, [0] * case.batch), kv, ds.k_pre,
+                   ds.v_pre)
+    return kv
+
+
 def variant_leg(args, torch, eb, case, copies, stream) -> int:
     """The next-row paths: one JSON line with the same fields as the headline."""
     from workloads import lbs_window, router_scores, suffix_segment
@@ -240,6 +260,10 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
                 dt_code, ctypes.byref(ds.ragged.c()),
                 ctypes.byref(eb_suffix(SUFFIX_LEN * B, SUFFIX_LEN, 0)), cfg.hq, cfg.hkv,
                 cfg.head_dim))
+        if args.path in ("paged", "paged8"):
+            x["kv"] = paged_cache(torch, eb, case, ds, args.path == "paged8")
+            x["attn_ws"] = u8(eb.eb_block_attn_paged_workspace(dt_code, ds.ragged, x["kv"],
+                                                               cfg.hq))
         extra.append(x)
     if args.path == "lbs":
         m, p, xh = lbs_window(cfg.seed, B, LBS_WINDOW, cfg.vocab, cfg.vocab - 1)
@@ -260,6 +284,9 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
             eb.eb_block_attn_dual(ds.ragged, x["cu_s"], SUFFIX_LEN, ds.q, ds.k_blk, ds.v_blk,
                                   ds.k_pre, ds.v_pre, x["k_s"], x["v_s"], ds.attn_out,
                                   ws=x["attn_ws"], stream=stream)
+        elif args.path in ("paged", "paged8"):
+            eb.eb_block_attn_paged(ds.ragged, x["kv"], ds.q, ds.k_blk, ds.v_blk, ds.attn_out,
+                                   ws=x["attn_ws"], stream=stream)
         else:
             eb.eb_block_attn(ds.ragged, ds.q, ds.k_blk, ds.v_blk, ds.k_pre, ds.v_pre, ds.attn_out,
                              ws=x["attn_ws"], stream=stream)
@@ -286,6 +313,8 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
         else:
             eb.eb_unmask_select(ds.ragged, ds.conf, ds.argmax, ds.tau, ds.masked, ds.tokens,
                                 ds.unmask, ds.n_commit, ds.resolved, stream=stream)
+        if args.path in ("paged", "paged8"):  # the block's rows go into the cache
+            eb.eb_kv_write(ds.ragged, x["kv"], ds.k_blk, ds.v_blk, stream=stream)
 
     for i in range(args.warmup):
         run(i)
@@ -322,6 +351,8 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
                 "kernel_us": lm_ms * 1e3, "algorithmic_bytes": nbytes, "algorithmic_flops": flops}
         if args.path == "dual":
             config["suffix_positions"] = SUFFIX_LEN * B
+        if args.path in ("paged", "paged8"):
+            config.update(page_size=PAGE_SIZE, cache="e4m3" if args.path == "paged8" else cfg.dtype)
         if args.path == "lps":
             config["tau_psi"] = TAU_PSI
         if args.path == "topm":
@@ -526,11 +557,13 @@ def main() -> int:
                     help="write profiles/lmhead_traffic.json from rocprofv3 counter runs in DIR")
     ap.add_argument("--no-peaks", action="store_true",
                     help="skip the same-box copy and GEMM reference rates (e.g. under a profiler)")
-    ap.add_argument("--path", default="step", choices=["step", "lps", "topm", "dual", "lbs"],
+    ap.add_argument("--path", default="step", choices=["step", "lps", "topm", "dual", "lbs", "paged", "paged8"],
                     help="step: eb_decode_step (the headline); lps: attention + LM head with the "
                          "top-2 gap + LPS features + union accept rule; topm: attention + LM head "
                          "+ top-m commit; dual: dual-cache attention + LM head + unmask; lbs: the "
-                         "LBS post-pass over a 512-position generation window per sequence")
+                         "LBS post-pass over a 512-position generation window per sequence; "
+                         "paged, paged8: attention over a paged cache (paged8: of 8 bits) + LM "
+                         "head + unmask + the block's rows into the cache")
     args = ap.parse_args()
 
     if args.ingest_counters:
