@@ -138,9 +138,10 @@ eb_status eb_block_attn_dual(eb_dtype dt, const eb_ragged* r, const eb_suffix* s
  * keys and values in pages of a common pool instead of one packed prefix: position p of sequence b
  * lies in row p % page_size of page page_table[b * max_pages + p / page_size].
  *
- *   k, v              [n_pages, hkv, page_size, head_dim] of `dtype` (16-byte aligned)
+ *   k, v              [n_pages, hkv, page_size, head_dim] of `dtype`
  *   k_scale, v_scale  [n_pages, hkv, page_size] u8, EB_E4M3 only: byte s of a row means that its
  *                     value is 2^(s - 127) times what the 8 bits say (1 <= s <= 254)
+ *                     (all four 16-byte aligned)
  *   page_table        [batch, max_pages] i32; sequences may share pages that are only read
  *
  * A page number outside [0, n_pages) is no page: its rows read as zeros, and rows written to it

@@ -47,13 +47,6 @@ struct PagedF32Params {
 };
 
 template <class T>
-__device__ __forceinline__ float widen(T x);
-template <>
-__device__ __forceinline__ float widen<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float widen<uint8_t>(uint8_t x) { return e4m3_pair_f32<false>(x, 1.f)[0]; }
-
-template <class T>
 __device__ __forceinline__ f32x4 widen4(const T* p);
 template <>
 __device__ __forceinline__ f32x4 widen4<float>(const float* p) {
@@ -97,7 +90,7 @@ __global__ __launch_bounds__(kPf32Waves * 64) void attn_paged_f32_kernel(PagedF3
   float m_run = -3.402823466e38f, l_run = 0.f;
   for (int k0 = kbeg + wave * kPf32Keys; k0 < kend; k0 += kPf32Stage) {
     f32x4 kf[kChunks];
-    float vf[4][kChunks];  // V of key k0 + 4 grp + r at d = 16 c + l16
+    f32x4 vf[4][kChunks / 4];  // V of key k0 + 4 grp + r at d = kChunks l16 + 4 i + e
     int valid;             // keys of this chunk
     if (k0 < cached) {
       valid = min(kPf32Keys, plen - k0);
@@ -107,7 +100,7 @@ __global__ __launch_bounds__(kPf32Waves * 64) void attn_paged_f32_kernel(PagedF3
       const size_t slab = ((static_cast<size_t>(page) * p.kv.hkv + g) << p.kv.page_shift) +
                           (k0 & ((1 << p.kv.page_shift) - 1));
       const size_t kr = slab + min(l16, valid - 1);
-      float ks = ok ? 1.f : 0.f, vs[4];
+      float ks = ok ? 1.f : 0.f;
       if (sizeof(C) == 1 && ok) ks = e8m0(p.kv.k_scale[kr]);
       const C* kp = reinterpret_cast<const C*>(p.kv.k) + kr * D + 4 * grp;
 #pragma unroll
@@ -118,12 +111,15 @@ __global__ __launch_bounds__(kPf32Waves * 64) void attn_paged_f32_kernel(PagedF3
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const size_t vr = slab + min(4 * grp + r, valid - 1);
-        vs[r] = 1.f;
-        if (sizeof(C) == 1) vs[r] = e8m0(p.kv.v_scale[vr]);
-        const C* vp = reinterpret_cast<const C*>(p.kv.v) + vr * D + l16;
+        float vs = 1.f;
+        if (sizeof(C) == 1) vs = e8m0(p.kv.v_scale[vr]);
+        const C* vp = reinterpret_cast<const C*>(p.kv.v) + vr * D + kChunks * l16;
         const bool live = ok && 4 * grp + r < valid;  // a weight of zero times infinity is NaN
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) vf[r][c] = live ? widen<C>(vp[16 * c]) * vs[r] : 0.f;
+        for (int i = 0; i < kChunks / 4; ++i) {
+          vf[r][i] = widen4(vp + 4 * i) * vs;
+          if (!live) vf[r][i] = f32x4{};
+        }
       }
     } else {
       const int j0 = k0 - cached;
@@ -136,10 +132,12 @@ __global__ __launch_bounds__(kPf32Waves * 64) void attn_paged_f32_kernel(PagedF3
       for (int r = 0; r < 4; ++r) {
         const size_t vr =
             static_cast<size_t>(bbeg + j0 + min(4 * grp + r, valid - 1)) * p.kv.hkv + g;
-        const float* vp = static_cast<const float*>(p.v_blk) + vr * D + l16;
+        const float* vp = static_cast<const float*>(p.v_blk) + vr * D + kChunks * l16;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c)
-          vf[r][c] = 4 * grp + r < valid ? vp[16 * c] : 0.f;
+        for (int i = 0; i < kChunks / 4; ++i) {
+          vf[r][i] = widen4(vp + 4 * i);
+          if (4 * grp + r >= valid) vf[r][i] = f32x4{};
+        }
       }
     }
     f32x4 acc[2] = {f32x4{}, f32x4{}};
@@ -166,7 +164,7 @@ __global__ __launch_bounds__(kPf32Waves * 64) void attn_paged_f32_kernel(PagedF3
       const float e = expf(sc[r] - m_new);
       l_run += e;
 #pragma unroll
-      for (int c = 0; c < kChunks; ++c) o[c] = mfma16_f32(vf[r][c], e, o[c]);
+      for (int c = 0; c < kChunks; ++c) o[c] = mfma16_f32(vf[r][c / 4][c % 4], e, o[c]);
     }
   }
   float l_tot = l_run + __shfl_xor(l_run, 16);
@@ -175,10 +173,13 @@ __global__ __launch_bounds__(kPf32Waves * 64) void attn_paged_f32_kernel(PagedF3
     s_m[wave][l16] = m_run;
     s_l[wave][l16] = l_tot;
   }
-  // register r of o[c]: d = 16 c + 4 (l / 16) + r of query l % 16
+  // register r of o[c]: d = kChunks (4 (l / 16) + r) + c of query l % 16
 #pragma unroll
-  for (int c = 0; c < kChunks; ++c)
-    *reinterpret_cast<f32x4*>(&s_o[wave][l16 * kPitch + 16 * c + 4 * grp]) = o[c];
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int i = 0; i < kChunks / 4; ++i)
+      *reinterpret_cast<f32x4*>(&s_o[wave][l16 * kPitch + kChunks * (4 * grp + r) + 4 * i]) =
+          f32x4{o[4 * i][r], o[4 * i + 1][r], o[4 * i + 2][r], o[4 * i + 3][r]};
   __syncthreads();
   // merge in wave order; a wave without keys has l = 0 and o = 0
   for (int i = tid; i < kPf32Rows * D; i += kPf32Waves * 64) {
@@ -232,15 +233,18 @@ __global__ __launch_bounds__(256) void attn_paged_f32_merge_kernel(PagedF32Param
     static_cast<float*>(p.out)[rh * D + lane * kPer + e] = x[e] / l;
 }
 
-// Ranges of whole stages, enough for two workgroups per compute unit.
+// Ranges of whole stages, enough for a workgroup per compute unit (two per compute unit: 29 against 24
+// us for 4 sequences of 64 rows behind 1024, 16/4 heads x 64); up to four stages stay whole (the merge
+// takes as long).
 SplitPlan f32_plan(const PagedAttnArgs& a) {
-  const long tiles = (static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) + kPf32Rows - 1) / kPf32Rows;
+  const long tiles =
+      (static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) + kPf32Rows - 1) / kPf32Rows;
   const long base = tiles * a.kv.hkv * a.batch;
   const int keys = (a.max_prefix + kPf32Keys - 1) / kPf32Keys * kPf32Keys + a.max_block;
-  const int stages = (keys + kPf32Stage - 1) / kPf32Stage;
-  const int want = static_cast<int>(max(1L, min((512 + base - 1) / base, static_cast<long>(stages))));
-  const int per = (stages + want - 1) / want;
-  return SplitPlan{(stages + per - 1) / per, per * kPf32Stage};
+  const long stages = (keys + kPf32Stage - 1) / kPf32Stage;
+  const long want = stages <= 4 ? 1 : max(1L, min((256 + base - 1) / base, stages));
+  const long per = (stages + want - 1) / want;
+  return SplitPlan{static_cast<int>((stages + per - 1) / per), static_cast<int>(per * kPf32Stage)};
 }
 
 template <int D, class C>
@@ -272,6 +276,10 @@ constexpr int kFewRowsBf16 = 32, kFewRowsE4m3 = 64;
 constexpr int kFewKeys = 32;  // keys of a piece
 constexpr int kFewStage = kFewWaves * kFewKeys;
 constexpr int kFewMaxBatch = 2048;
+// A sequence this many stages longer than a part still takes one workgroup: the merge's launch costs
+// as much (one token behind 100 rows, 28/4 heads: 6.8 against 9.3 us; behind 1000 rows, 9 stages, 14.5
+// whole against 9.2 us).
+constexpr int kFewWhole = 5;
 
 bool few_ok(bool bf16, const PagedAttnArgs& a) {
   const int most = a.kv.type == CacheType::kE4m3 ? kFewRowsE4m3 : kFewRowsBf16;
@@ -305,6 +313,11 @@ FewPlan few_plan(const PagedAttnArgs& a) {
   const long most = min(a.total_prefix / kFewStage + 2L * a.batch,
                         a.batch * ((a.max_prefix + kFewStage - 1L) / kFewStage + 1));
   const long chunk = (most * lines + kAttnTargetWgs - 1) / kAttnTargetWgs;
+  const long longest = (a.max_prefix + kFewStage - 1L) / kFewStage + 1;
+  if (longest <= chunk + kFewWhole) {
+    f.groups = a.batch, f.chunk = 0, f.slots = 0;
+    return f;
+  }
   f.chunk = static_cast<int>(chunk);
   f.groups = static_cast<int>((most + chunk - 1) / chunk);
   f.slots = f.groups > 1 ? static_cast<size_t>(lines) * f.groups * 2 * per : 0;
@@ -351,6 +364,9 @@ hipError_t launch_few_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 // are needed to make them even.  With more than kSplitItems whole sequences fill the rounds (32 heads,
 // 32 blocks of 8 to 128 rows behind 2048, 1024 items: 212 us whole, 227 us with the plan).
 constexpr long kSplitItems1 = 160, kSplitItems2 = 420, kSplitItems = 900;
+// Up to this many stages sequences stay whole: one block of 100 rows behind 300, 28/4 heads, 7 stages,
+// 16 against 19 us; behind 600, 12 stages, 18 us either way.
+constexpr long kWholeStages = 8;
 
 struct TilesLaunch {
   TilePlan plan;
@@ -366,7 +382,7 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a) {
   TilesLaunch t{};
   t.plan.batch = a.batch;
   t.plan.row_tiles = static_cast<int>(row_tiles);
-  if (a.batch <= kPlanMaxBatch && whole <= kSplitItems && stages > 1) {
+  if (a.batch <= kPlanMaxBatch && whole <= kSplitItems && stages > kWholeStages) {
     const int rounds = whole <= kSplitItems1 ? 1 : whole <= kSplitItems2 ? 2 : 4;
     t.plan.cap = rounds * kAttnTargetWgs;
     t.grid = t.plan.cap;
@@ -374,7 +390,8 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a) {
     return t;
   }
   const long base = row_tiles * hkv * a.batch;
-  const long want = max(1L, min((kAttnTargetWgs + base - 1) / base, stages));
+  const long want =
+      stages <= kWholeStages ? 1 : max(1L, min((kAttnTargetWgs + base - 1) / base, stages));
   const long chunk = (stages + want - 1) / want;
   t.plan.chunk = static_cast<int>(chunk);
   t.plan.nsplit = static_cast<int>((stages + chunk - 1) / chunk);

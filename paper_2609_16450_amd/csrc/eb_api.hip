@@ -162,6 +162,8 @@ eb_status check_paged(eb_dtype dt, const eb_paged_kv* kv) {
     return fail(EB_ERR_INVALID, "the cache's k and v must be 16-byte aligned");
   if (kv->dtype == EB_E4M3 && (!kv->k_scale || !kv->v_scale))
     return fail(EB_ERR_INVALID, "NULL k_scale / v_scale with an EB_E4M3 cache");
+  if (kv->dtype == EB_E4M3 && (!aligned16(kv->k_scale) || !aligned16(kv->v_scale)))
+    return fail(EB_ERR_INVALID, "the cache's scales must be 16-byte aligned");
   return EB_OK;
 }
 

@@ -48,6 +48,8 @@ BAD = [
     (dict(k=None), B.EB_ERR_INVALID, "NULL"),
     (dict(v=0x208), B.EB_ERR_INVALID, "aligned"),
     (dict(dtype=B.EB_E4M3), B.EB_ERR_INVALID, "k_scale"),
+    (dict(dtype=B.EB_E4M3, k_scale=0x100), B.EB_ERR_INVALID, "v_scale"),
+    (dict(dtype=B.EB_E4M3, k_scale=0x100, v_scale=0x101), B.EB_ERR_INVALID, "aligned"),
 ]
 
 
