@@ -806,6 +806,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
   constexpr int kRawLoads = 4;
   [[maybe_unused]] u32x4 raw[kRawLoads];
   [[maybe_unused]] uint32_t raw_scale[2];
+  // where the lane's first row and chunk of a group go: row r = 2 (lane / 8), chunk 2 (lane % 8); its
+  // second chunk lies in the slot ^ 1, row r + 1 in the slot ^ 1 (K: r % 16 is XORed) or ^ 4 (V)
+  [[maybe_unused]] uint32_t raw_at =
+      2 * (lane >> 3) * kRowBytes +
+      16 * ((2 * (lane & 7)) ^ (k_wave ? 2 * (lane >> 3) : 8 * ((lane >> 3) & 1)));
   auto fetch = [&](int kv0) {
     if constexpr (Keys::kE4m3) {
       if (kv0 >= cached) return;
@@ -832,20 +837,22 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
       issue(kv0, dst);
       return;
     }
-    int lane_ = lane;  // addresses formed anew per tile: kept over the loop they would spill
-    asm volatile("" : "+v"(lane_));
+    // the tile's rows of this wave begin at a multiple of 8 KB, so slots can be XORed into addresses
+    uint32_t base = static_cast<uint32_t>(dst - smem) + (wave & 1) * (kTileBytes / 2);
+    asm volatile("" : "+s"(base));  // (formed here, not kept per slot over the loop)
+    const uint32_t row0 = raw_at + base, row1 = (row0 ^ (k_wave ? 16 : 64)) + kRowBytes;
 #pragma unroll
-    for (int j = 0; j < kRawLoads; ++j) {
-      const int r = 32 * (wave & 1) + 16 * (j / 2) + 2 * (lane_ >> 3) + j % 2;
-      const int to = k_wave ? (r & 15) : 4 * (r & 3);
-      uint32_t s8 = j % 2 ? raw_scale[j / 2] >> 8 : raw_scale[j / 2] & 0xff;
-      if (kv0 + kDmaKeys > plen && kv0 + r >= plen) s8 = 0;  // the row's values are zeros as well
-      u32x4 lo, hi;
-      e4m3_widen(raw[j], e8m0(s8), lo, hi);
-      const int c = 2 * (lane_ & 7);
-      *reinterpret_cast<u32x4*>(dst + r * kRowBytes + 16 * (c ^ to)) = lo;
-      *reinterpret_cast<u32x4*>(dst + r * kRowBytes + 16 * ((c + 1) ^ to)) = hi;
-    }
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        // (a scale byte of 255 can only come with the zeros of a row that does not exist: 254 then)
+        const uint32_t scale = min(raw_scale[h] << (i ? 15 : 23) & 0x7f800000u, 0x7f000000u);
+        u32x4 lo, hi;
+        e4m3_widen(raw[2 * h + i], __uint_as_float(scale), lo, hi);
+        uint8_t* const to = smem + h * 16 * kRowBytes;
+        *reinterpret_cast<u32x4*>(to + (i ? row1 : row0)) = lo;
+        *reinterpret_cast<u32x4*>(to + ((i ? row1 : row0) ^ 16)) = hi;
+      }
   };
   auto ktile = [&](int i) { return smem + (i & 1) * kTileBytes; };
   auto vtile = [&](int i) { return smem + (2 + (i & 1)) * kTileBytes; };
