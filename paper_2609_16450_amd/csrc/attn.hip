@@ -17,7 +17,6 @@
 
 #include "attn_common.hpp"
 #include "attn_f32.hpp"
-#include "attn_merge.hpp"
 #include "attn_small.hpp"
 #include "attn_tiles.hpp"
 #include "eb_common.hpp"
@@ -36,6 +35,26 @@ template <int D>
 __global__ __launch_bounds__(kSmallAloneThreads) void attn_small_kernel(AttnParams p) {
   attn_small_role<D, kSmallAloneThreads>(p, static_cast<int>(blockIdx.x),
                                           static_cast<int>(blockIdx.y));
+}
+
+// Combine the key-split partials of each (block row, query head), one wavefront per pair.
+template <int D, int kGroup>
+__global__ __launch_bounds__(256) void attn_merge_kernel(AttnParams p, int total_block, int batch) {
+  const int rh = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (rh >= total_block * p.hq) return;  // uniform per wavefront
+  attn_merge_pair<D, kGroup>(p, rh, batch, threadIdx.x & 63);
+}
+
+template <int D>
+void launch_merge(const AttnParams& p, int total_block, int batch, hipStream_t s) {
+  const long pairs = static_cast<long>(total_block) * p.hq;
+  const dim3 grid(static_cast<unsigned>((pairs + 3) / 4));
+  if (p.nsplit <= 4)
+    hipLaunchKernelGGL((attn_merge_kernel<D, 4>), grid, dim3(256), 0, s, p, total_block, batch);
+  else if (p.nsplit <= 8)
+    hipLaunchKernelGGL((attn_merge_kernel<D, 8>), grid, dim3(256), 0, s, p, total_block, batch);
+  else
+    hipLaunchKernelGGL((attn_merge_kernel<D, 16>), grid, dim3(256), 0, s, p, total_block, batch);
 }
 
 template <int D, int kWaves>

@@ -40,9 +40,6 @@ struct AttnParams {
   float* o_part;  // [T * hq * nsplit, D]
   float* m_part;  // [T * hq * nsplit]  running max (log2 units)
   float* l_part;  // [T * hq * nsplit]  sum of 2^(s - m)
-  // the key ranges count the prefix as rounded up to a multiple of prefix_mask + 1 keys (a paged
-  // cache, whose stages hold no other segment's keys)
-  int prefix_mask = 0;
 };
 
 struct SplitPlan {
@@ -113,9 +110,7 @@ __device__ __forceinline__ void attn_merge_pair(const AttnParams& p, int rh, int
     b += n;
     if (n < 64) break;
   }
-  const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
-  const int n_keys = ((plen + p.prefix_mask) & ~p.prefix_mask) +
-                     (p.cu_block[b + 1] - p.cu_block[b]) +
+  const int n_keys = (p.cu_prefix[b + 1] - p.cu_prefix[b]) + (p.cu_block[b + 1] - p.cu_block[b]) +
                      (p.cu_suffix ? p.cu_suffix[b + 1] - p.cu_suffix[b] : 0);
   const int nvalid = min(p.nsplit, (n_keys + p.kps - 1) / p.kps);
   float M = -INFINITY;

@@ -18,8 +18,8 @@ namespace {
 // fp32 arithmetic throughout, on 16x16x4 fp32 MFMAs.
 //
 // A workgroup of kPf32Waves wavefronts per (16 query rows, K/V head, sequence, key range).  Wave w
-// takes the 16-key chunks w, w + kPf32Waves, ... of the range with an online softmax of its own; the
-// waves' results are merged through LDS and, with a key split, the ranges' by a second kernel.
+// takes the 16-key chunks w, w + kPf32Waves, ... of the range with an online softmax of its own;
+// the waves' results are merged through LDS and, with a key split, the ranges' by a second kernel.
 // Scores are formed transposed, S^T = K Q^T: lane l owns query l % 16 and holds keys 4 (l / 16) + r
 // of the chunk, which are the k-slots of the B operand of O^T = V^T P^T, one register per MFMA.
 // ---------------------------------------------------------------------------------------
@@ -215,7 +215,8 @@ __global__ __launch_bounds__(256) void attn_paged_f32_merge_kernel(PagedF32Param
   if (rh >= static_cast<long>(total) * p.hq) return;  // uniform per wavefront
   const int b = find_sequence(p.cu_block, batch, static_cast<int>(rh / p.hq), lane);
   const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
-  const int n_keys = (plen + kPf32Keys - 1) / kPf32Keys * kPf32Keys + p.cu_block[b + 1] - p.cu_block[b];
+  const int cached = (plen + kPf32Keys - 1) / kPf32Keys * kPf32Keys;
+  const int n_keys = cached + p.cu_block[b + 1] - p.cu_block[b];
   const int n = min(p.nsplit, (n_keys + p.kps - 1) / p.kps);
   const size_t base = static_cast<size_t>(rh) * p.nsplit;
   float m = -INFINITY, l = 0.f, x[kPer] = {};
@@ -233,9 +234,9 @@ __global__ __launch_bounds__(256) void attn_paged_f32_merge_kernel(PagedF32Param
     static_cast<float*>(p.out)[rh * D + lane * kPer + e] = x[e] / l;
 }
 
-// Ranges of whole stages, enough for a workgroup per compute unit (two per compute unit: 29 against 24
-// us for 4 sequences of 64 rows behind 1024, 16/4 heads x 64); up to four stages stay whole (the merge
-// takes as long).
+// Ranges of whole stages, enough for a workgroup per compute unit (two per compute unit: 29 against
+// 24 us for 4 sequences of 64 rows behind 1024, 16/4 heads x 64); up to four stages stay whole (the
+// merge takes as long).
 SplitPlan f32_plan(const PagedAttnArgs& a) {
   const long tiles =
       (static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) + kPf32Rows - 1) / kPf32Rows;
@@ -271,14 +272,13 @@ hipError_t launch_f32(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 // ---- few query rows per K/V head, bf16 ----------------------------------------------------
 // Up to this many query rows per K/V head.  Over bf16 pages the tile kernel is the faster from 33
 // rows on (32 heads x 128, 16 blocks of 64 rows: 137 against 165 us); widening 8 bits costs it more
-// (28/4 heads, 64 blocks of 8: 112 against 106 us; 16/4 heads x 64, 32 blocks of 16: 67 against 48).
+// (28/4 heads, 64 blocks of 8: 112 against 106 us; 16/4 heads x 64, 32 blocks of 16: 67 against
+// 48).
 constexpr int kFewRowsBf16 = 32, kFewRowsE4m3 = 64;
-constexpr int kFewKeys = 32;  // keys of a piece
-constexpr int kFewStage = kFewWaves * kFewKeys;
 constexpr int kFewMaxBatch = 2048;
-// A sequence this many stages longer than a part still takes one workgroup: the merge's launch costs
-// as much (one token behind 100 rows, 28/4 heads: 6.8 against 9.3 us; behind 1000 rows, 9 stages, 14.5
-// whole against 9.2 us).
+// A sequence this many stages longer than a part still takes one workgroup: the merge's launch
+// costs as much (one token behind 100 rows, 28/4 heads: 6.8 against 9.3 us; behind 1000 rows, 9
+// stages, 14.5 whole against 9.2 us).
 constexpr int kFewWhole = 5;
 
 bool few_ok(bool bf16, const PagedAttnArgs& a) {
@@ -340,13 +340,13 @@ hipError_t launch_few(const PagedAttnArgs& a, void* ws, hipStream_t s) {
                     f.row_tiles, f.groups, f.chunk, o, m, m + f.slots};
   const long units = static_cast<long>(f.groups) * a.kv.hkv;
   const dim3 grid(static_cast<unsigned>(8 * ((units + 7) / 8) * f.row_tiles));
-  hipLaunchKernelGGL((attn_paged_few_kernel<D, kE4m3, kFewKeys, kTiles>), grid,
+  hipLaunchKernelGGL((attn_paged_few_kernel<D, kE4m3, kTiles>), grid,
                      dim3(kFewWaves * 64), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || f.slots == 0) return e;
   hipLaunchKernelGGL(attn_paged_few_merge_kernel<D>,
                      dim3(static_cast<unsigned>(a.batch * a.kv.hkv * f.row_tiles)), dim3(512), 0, s,
-                     p, kFewStage, kTiles * kSmallTile);
+                     p, kTiles * kSmallTile);
   return hipGetLastError();
 }
 
@@ -360,12 +360,13 @@ hipError_t launch_few_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 
 // ---- many query rows, bf16: the tile kernels of the packed prefix ---------------------------
 // Items of whole sequences (a K/V head and a tile of query rows each) up to which a launch may cut
-// sequences into ranges, for one, two or four rounds of workgroups: the fewer items, the fewer rounds
-// are needed to make them even.  With more than kSplitItems whole sequences fill the rounds (32 heads,
-// 32 blocks of 8 to 128 rows behind 2048, 1024 items: 212 us whole, 227 us with the plan).
+// sequences into ranges, for one, two or four rounds of workgroups: the fewer items, the fewer
+// rounds are needed to make them even.  With more than kSplitItems whole sequences fill the rounds
+// (32 heads, 32 blocks of 8 to 128 rows behind 2048, 1024 items: 212 us whole, 227 us with the
+// plan).
 constexpr long kSplitItems1 = 160, kSplitItems2 = 420, kSplitItems = 900;
-// Up to this many stages sequences stay whole: one block of 100 rows behind 300, 28/4 heads, 7 stages,
-// 16 against 19 us; behind 600, 12 stages, 18 us either way.
+// Up to this many stages sequences stay whole: one block of 100 rows behind 300, 28/4 heads, 7
+// stages, 16 against 19 us; behind 600, 12 stages, 18 us either way.
 constexpr long kWholeStages = 8;
 
 struct TilesLaunch {

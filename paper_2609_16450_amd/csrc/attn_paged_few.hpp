@@ -2,9 +2,9 @@
 // bf16.  Such calls read every cached key and value for a handful of multiply-adds: they are bound
 // by memory, and the kernel is built around its loads.
 //
-// A workgroup is four waves.  The waves split the keys, not the rows: each takes every fourth piece,
-// holds all 16 kTiles query rows and keeps an online softmax of its own, so that no wave waits for
-// another until its keys end; their results are then merged through LDS.
+// A workgroup is four waves.  The waves split the keys, not the rows: each takes every fourth
+// piece, holds all 16 kTiles query rows and keeps an online softmax of its own, so that no wave
+// waits for another until its keys end; their results are then merged through LDS.
 //
 // Contexts of a served batch are of very different lengths, and one launch should keep every
 // compute unit busy to its end.  So the keys of all sequences form one line, for each (K/V head,
@@ -15,7 +15,7 @@
 // sequence goes on), the others in their slot 0 (it came from before), merged by a second launch.
 // Measured against ranges of equal length for every sequence: see few_plan.
 //
-// A piece is kKeys keys.  K goes from memory straight into the registers of the MFMA's A operand
+// A piece is kFewKeys keys.  K goes from memory straight into the registers of the MFMA's A operand
 // (S^T = K Q^T by 16x16x32: lane l holds row l % 16).  V has to be transposed for O^T = V^T P^T: it
 // goes through the wave's own part of LDS, row-major, and comes back by transposing reads
 // (attn_small.hpp).  As soon as a piece's K is in S and its V in LDS, the loads of the wave's next
@@ -36,7 +36,8 @@ namespace eb {
 namespace {
 
 constexpr int kFewWaves = 4;
-constexpr int kFewBlockKeys = 32;  // keys of a piece of the block's own rows
+constexpr int kFewKeys = 32;  // keys of a piece
+constexpr int kFewStage = kFewWaves * kFewKeys;
 
 struct FewParams {
   AttnParams a;  // without the prefix segment and the key split
@@ -53,19 +54,19 @@ struct FewParams {
 
 // Stages of sequence b in the line of the tile at query row row0 (none if the tile lies past its
 // rows): its cached rows, then the block's.
-__device__ __forceinline__ int few_stages(const AttnParams& p, int b, int row0, int stage) {
+__device__ __forceinline__ int few_stages(const AttnParams& p, int b, int row0) {
   const int len = p.cu_block[b + 1] - p.cu_block[b];
   const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
-  return row0 < len * p.group ? (plen + stage - 1) / stage + 1 : 0;
+  return row0 < len * p.group ? (plen + kFewStage - 1) / kFewStage + 1 : 0;
 }
 
 // The sequence that holds stage s of the line, and its first stage, found by the whole wavefront;
 // batch if the line ends before s.
-__device__ __forceinline__ int few_find(const FewParams& fp, int row0, int stage, int s, int lane,
+__device__ __forceinline__ int few_find(const FewParams& fp, int row0, int s, int lane,
                                         int& first) {
   first = 0;
   for (int b0 = 0; b0 < fp.batch; b0 += 64) {
-    const int n = b0 + lane < fp.batch ? few_stages(fp.a, b0 + lane, row0, stage) : 0;
+    const int n = b0 + lane < fp.batch ? few_stages(fp.a, b0 + lane, row0) : 0;
     const int upto = lanes_up_to(n, 0, AddOp{});
     const uint64_t past = __ballot(first + upto > s);
     if (past) {
@@ -78,25 +79,23 @@ __device__ __forceinline__ int few_find(const FewParams& fp, int row0, int stage
   return fp.batch;
 }
 
-template <int D, bool kE4m3, int kKeys, int kTiles>
+template <int D, bool kE4m3, int kTiles>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewParams fp) {
   const AttnParams& p = fp.a;
   constexpr int kDSteps = D / 32;         // MFMA k-steps of S^T
   constexpr int kDTiles = D / 16;         // 16-row tiles of O^T
-  constexpr int kGroups = kKeys / 16;     // groups of 16 keys of a piece
+  constexpr int kGroups = kFewKeys / 16;     // groups of 16 keys of a piece
   constexpr int kRow = kE4m3 ? D : 2 * D; // bytes of a cached row
   constexpr int kVPitch = D + 16;         // V row pitch in LDS (see attn_small.hpp)
   constexpr int kOPitch = D + 4;          // row pitch of a wave's O in LDS (fp32)
-  constexpr int kVBytes = kKeys * kVPitch * 2;
+  constexpr int kVBytes = kFewKeys * kVPitch * 2;
   constexpr int kOBytes = kSmallTile * kOPitch * 4;
   constexpr int kWaveBytes = kVBytes > kOBytes ? kVBytes : kOBytes;
-  constexpr int kStage = kFewWaves * kKeys;
-  static_assert(kKeys >= kFewBlockKeys, "a block piece fits the wave's part of LDS");
   __shared__ __attribute__((aligned(16))) uint8_t smem[kFewWaves * kWaveBytes];
   __shared__ float s_m[kFewWaves][kTiles * kSmallTile], s_l[kFewWaves][kTiles * kSmallTile];
 
-  // the row tiles of a unit (K/V head, workgroup of the line) run on one XCD, one after another, and
-  // read its keys from that XCD's L2
+  // the row tiles of a unit (K/V head, workgroup of the line) run on one XCD, one after another,
+  // and read its keys from that XCD's L2
   const int xcd = blockIdx.x % 8, jx = blockIdx.x / 8;
   const int unit = 8 * (jx / fp.row_tiles) + xcd;
   const int tile = jx % fp.row_tiles;
@@ -114,12 +113,12 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
   if (fp.chunk) {
     from = w * fp.chunk;
     to = from + fp.chunk;
-    b = few_find(fp, row0, kStage, from, lane, first);
+    b = few_find(fp, row0, from, lane, first);
   } else {
     b = w, first = 0, from = 0, to = 1 << 30;
   }
   for (; b < fp.batch && from < to; ++b) {
-    const int n_stages = few_stages(p, b, row0, kStage);
+    const int n_stages = few_stages(p, b, row0);
     if (n_stages == 0) {
       if (!fp.chunk) return;  // uniform, as the rest of the loop's conditions
       continue;
@@ -129,10 +128,10 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
     const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
     const int n_rows = len * G;
     const int sbeg = from - first, send = min(to - first, n_stages);  // stages of the sequence
-    const int kbeg = sbeg * kStage, kend = min(send * kStage, plen);  // its cached rows among them
+    const int kbeg = sbeg * kFewStage, kend = min(send * kFewStage, plen);  // its cached rows among them
 
-    // Columns of lane group grp in k-step s: the contraction index is permuted so that 16 bytes of an
-    // 8-bit row hold the lane's columns of two steps.
+    // Columns of lane group grp in k-step s: the contraction index is permuted so that 16 bytes of
+    // an 8-bit row hold the lane's columns of two steps.
     auto col_of = [&](int s, int grp_) {
       return kE4m3 ? 64 * (s / 2) + 16 * grp_ + 8 * (s % 2) : 32 * s + 8 * grp_;
     };
@@ -142,7 +141,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
       const int r = min(row0 + t * kSmallTile + l16, n_rows - 1);
       const uint16_t* q = p.q + (static_cast<size_t>(bbeg + r / G) * p.hq + g * G + r % G) * D;
 #pragma unroll
-      for (int s = 0; s < kDSteps; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(q + col_of(s, grp));
+      for (int s = 0; s < kDSteps; ++s)
+        qf[t][s] = *reinterpret_cast<const bf16x8*>(q + col_of(s, grp));
     }
     f32x4 o[kTiles][kDTiles];
     float m_run[kTiles], l_run[kTiles];
@@ -159,8 +159,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
       const uint16_t* a = Vs + (kbase + 4 * grp + (l16 >> 2)) * kVPitch + d0 + 4 * (l16 & 3);
       return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(const_cast<uint16_t*>(a)));
     };
-    // Softmax and O^T += V^T P^T of one piece with scores sc[t][j] (16 keys each) whose first `valid`
-    // keys exist; V lies in LDS.
+    // Softmax and O^T += V^T P^T of one piece with scores sc[t][j] (16 keys each) whose first
+    // `valid` keys exist; V lies in LDS.
     auto finish = [&](auto& sc, int valid) {
       constexpr int kG = sizeof(sc[0]) / sizeof(f32x4);
       u32x2 pk[kTiles][kG];
@@ -210,7 +210,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
               bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) {
-            const u32x4 w{pk[t][2 * u][0], pk[t][2 * u][1], pk[t][2 * u + 1][0], pk[t][2 * u + 1][1]};
+            const u32x2 lo2 = pk[t][2 * u], hi2 = pk[t][2 * u + 1];
+            const u32x4 w{lo2[0], lo2[1], hi2[0], hi2[1]};
             o[t][d] = mfma16(vf, __builtin_bit_cast(bf16x8, w), o[t][d]);
           }
         }
@@ -228,8 +229,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
     const uint32_t voff = lane * 16;
     const int32_t* const table = fp.kv.table + static_cast<size_t>(b) * fp.kv.max_pages;
     const int pmask = (1 << fp.kv.page_shift) - 1;
-    // Pages of the piece at key k0 (uniform); groups past the cached rows take the last page, and no
-    // rows of it.
+    // Pages of the piece at key k0 (uniform); groups past the cached rows take the last page, and
+    // no rows of it.
     auto pages = [&](int k0, int (&page)[kGroups]) {
 #pragma unroll
       for (int j = 0; j < kGroups; ++j)
@@ -257,13 +258,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
         }
       }
     };
-    int k0 = kbeg + wave * kKeys;
+    int k0 = kbeg + wave * kFewKeys;
     if (k0 < kend) {
       int page[kGroups];
       pages(k0, page);
       load(k0, page);
-      for (; k0 < kend; k0 += kStage) {
-        const int next = k0 + kStage;
+      for (; k0 < kend; k0 += kFewStage) {
+        const int next = k0 + kFewStage;
         const bool more = next < kend;
         if (more) pages(next, page);
         // V into LDS (the reads of the piece before are done: they fed the MFMAs above)
@@ -321,22 +322,22 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
       const uint32_t key_bytes = static_cast<uint32_t>(p.hkv) * 2 * D;
       int lane_ = lane;  // addresses formed here: kept over the cached rows they would spill
       asm volatile("" : "+v"(lane_));
-      for (int j0 = wave * kFewBlockKeys; j0 < len; j0 += kFewWaves * kFewBlockKeys) {
+      for (int j0 = wave * kFewKeys; j0 < len; j0 += kFewWaves * kFewKeys) {
         const size_t at = (static_cast<size_t>(bbeg + j0) * p.hkv + g) * D;
-        const int rows = min(len - j0, kFewBlockKeys);
+        const int rows = min(len - j0, kFewKeys);
         const uint32_t bytes = (rows - 1) * key_bytes + 2 * D;
         const __amdgpu_buffer_rsrc_t rk = make_rsrc(p.k_blk + at, bytes);
         const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.v_blk + at, bytes);
-        constexpr int kLanes = D / 8, kPer = kFewBlockKeys * kLanes / 64;
+        constexpr int kLanes = D / 8, kPer = kFewKeys * kLanes / 64;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           const int r = i * (64 / kLanes) + lane_ / kLanes, c = 8 * (lane_ % kLanes);
           *reinterpret_cast<u32x4*>(Vs + r * kVPitch + c) =
               buffer_load16(rv, r * key_bytes + 2 * c);
         }
-        f32x4 sc[kTiles][kFewBlockKeys / 16];
+        f32x4 sc[kTiles][kFewKeys / 16];
 #pragma unroll
-        for (int j = 0; j < kFewBlockKeys / 16; ++j) {
+        for (int j = 0; j < kFewKeys / 16; ++j) {
           bf16x8 kf[kDSteps];
 #pragma unroll
           for (int s = 0; s < kDSteps; ++s)
@@ -378,7 +379,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
       // register r of o[t][d]: column 16 d + 4 grp + r of query l16
 #pragma unroll
       for (int d = 0; d < kDTiles; ++d)
-        *reinterpret_cast<f32x4*>(so + wave * kWaveFloats + l16 * kOPitch + 16 * d + 4 * grp) = o[t][d];
+        *reinterpret_cast<f32x4*>(so + wave * kWaveFloats + l16 * kOPitch + 16 * d + 4 * grp) =
+            o[t][d];
       __syncthreads();
       int tid_ = tid;  // (as lane_ above)
       asm volatile("" : "+v"(tid_));
@@ -421,7 +423,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
 // The partials of one (sequence, K/V head, tile of query rows) per workgroup, in the order of the
 // line; a wave per query row, its lanes over kParts partials side by side.
 template <int D>
-__global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp, int stage,
+__global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp,
                                                                    int tile_rows) {
   const AttnParams& p = fp.a;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -431,9 +433,9 @@ __global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp,
   // first stage of the sequence in the line
   int before = 0;
   for (int b0 = 0; b0 < b; b0 += 64)
-    before += b0 + lane < b ? few_stages(p, b0 + lane, row0, stage) : 0;
+    before += b0 + lane < b ? few_stages(p, b0 + lane, row0) : 0;
   before = lanes_all(before, 0, AddOp{});
-  const int n = few_stages(p, b, row0, stage);
+  const int n = few_stages(p, b, row0);
   const int w0 = before / fp.chunk, w1 = (before + n - 1) / fp.chunk;
   if (n == 0 || w0 == w1) return;  // nothing here, or written out by its only workgroup
   const int bbeg = p.cu_block[b], G = p.group;
@@ -447,7 +449,8 @@ __global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp,
     };
     const int row = row0 + r;
     const size_t dst = static_cast<size_t>(bbeg + row / G) * p.hq + g * G + row % G;
-    merge_partials<D>(at, parts, fp.o_part, fp.m_part, fp.l_part, lane).store(p.out + dst * D, lane);
+    merge_partials<D>(at, parts, fp.o_part, fp.m_part, fp.l_part, lane)
+        .store(p.out + dst * D, lane);
   }
 }
 

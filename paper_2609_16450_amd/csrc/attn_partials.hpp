@@ -1,5 +1,5 @@
-// One output row from the partials (O, running maximum in log2 units, sum of weights) of the parts of
-// its keys, by one wavefront.
+// One output row from the partials (O, running maximum in log2 units, sum of weights) of the parts
+// of its keys, by one wavefront.
 #pragma once
 
 #include "eb_common.hpp"

@@ -24,8 +24,8 @@ struct PackedKeys {
   static constexpr bool kPaged = false, kE4m3 = false;
 };
 // Page numbers of one sequence: the wave holds 64 entries of its row of the table, a lane each, and
-// the 64 behind them on their way, so that taking one costs no memory access.  Entries are asked for
-// in rising order, and none is left out by a whole window.
+// the 64 behind them on their way, so that taking one costs no memory access.  Entries are asked
+// for in rising order, and none is left out by a whole window.
 struct PageWindow {
   const int32_t* row;
   int last, first, now, next;  // last entry of the row; entries first .. first + 63 and the next 64
@@ -48,18 +48,18 @@ struct PageWindow {
   }
 };
 
-// Key ranges of a launch over pages.  A sequence's stages (its cached rows, then the block's) are cut
-// into n_b nearly equal ranges of at most `chunk` stages, and an item is one (range, K/V head, tile of
-// query rows); the row tiles of a range are neighbours, so that they run on one XCD at a time and
-// share its keys.
-// With cap > 0 every workgroup finds chunk itself, from the lengths, which the host does not know: of
-// kPlanCandidates cuts of the longest sequence the cheapest with at most cap items, by the rounds of
-// kAttnTargetWgs workgroups and the partials.  (The lanes hold a sequence each, so this is for at
-// most 64 of them, and takes a microsecond.)  Against as many ranges for every sequence as fill the
-// chip when all are as long as the longest: 28/4 heads x 128, 16 blocks of 32 to 256 rows behind 2000
-// to 16000, 576 -> 453 us; 8 of 20 to 100 behind 1000 to 8000, 71 -> 60 us; 16/4 heads x 64, the
-// same, 49 -> 32 us.  Equal lengths gain nothing (32 heads, 1000 rows behind 3000: 89 and 91 us).
-// With cap = 0 chunk is the host's, and every sequence counts as the longest, with as many row tiles.
+// Key ranges of a launch over pages.  A sequence's stages (its cached rows, then the block's) are
+// cut into n_b nearly equal ranges of at most `chunk` stages, and an item is one (range, K/V head,
+// tile of query rows); the row tiles of a range are neighbours, so that they run on one XCD at a
+// time and share its keys. With cap > 0 every workgroup finds chunk itself, from the lengths, which
+// the host does not know: of kPlanCandidates cuts of the longest sequence the cheapest with at most
+// cap items, by the rounds of kAttnTargetWgs workgroups and the partials.  (The lanes hold a
+// sequence each, so this is for at most 64 of them, and takes a microsecond.)  Against as many
+// ranges for every sequence as fill the chip when all are as long as the longest: 28/4 heads x 128,
+// 16 blocks of 32 to 256 rows behind 2000 to 16000, 576 -> 453 us; 8 of 20 to 100 behind 1000 to
+// 8000, 71 -> 60 us; 16/4 heads x 64, the same, 49 -> 32 us.  Equal lengths gain nothing (32 heads,
+// 1000 rows behind 3000: 89 and 91 us). With cap = 0 chunk is the host's, and every sequence counts
+// as the longest, with as many row tiles.
 struct TilePlan {
   int batch, row_tiles;
   int cap;
@@ -178,8 +178,8 @@ __device__ __forceinline__ bool find_item(const AttnParams& p, const TilePlan& t
     return it.range < it.ranges;
   }
   // The items in 8 turns equal runs, dealt to the XCDs in turn: runs of at least as many items as
-  // the longest block has row tiles, for the sharing.  turns divides 64, so that an XCD gets no more
-  // items than its share of the cap.
+  // the longest block has row tiles, for the sharing.  turns divides 64, so that an XCD gets no
+  // more items than its share of the cap.
   const LanePlan l = lane_plan(p, tp, lane);
   int turns = 1;
   while (turns < 64 && 2 * turns * kXcdCount * tp.row_tiles <= l.total) turns *= 2;
@@ -731,7 +731,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
     page_bytes = (static_cast<size_t>(p.hkv) << page_shift) * kHeld;
     pool_g = (k_wave ? keys.kv.k : keys.kv.v) + (static_cast<size_t>(g) << page_shift) * kHeld;
     if constexpr (Keys::kE4m3)
-      scale_g = (k_wave ? keys.kv.k_scale : keys.kv.v_scale) + (static_cast<size_t>(g) << page_shift);
+      scale_g =
+          (k_wave ? keys.kv.k_scale : keys.kv.v_scale) + (static_cast<size_t>(g) << page_shift);
   }
   auto issue = [&](int kv0, uint8_t* dst) {
     if constexpr (Keys::kPaged) {
@@ -769,7 +770,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
           buffer_load_to_lds(make_rsrc(base + 4 * i * static_cast<size_t>(stride),
                                        max(bytes - 4 * i * static_cast<int>(stride), 0)),
                              smem + to + (4 * h + i) * 1024,
-                             row_off + 16u * static_cast<uint32_t>((lane_ & 15) ^ swz(lane_, i)), 0);
+                             row_off + 16u * ((lane_ & 15) ^ swz(lane_, i)), 0);
         }
       }
       return;
@@ -800,14 +801,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
     }
   };
   // Tiles of an 8-bit cache go through registers: fetch() loads this wave's half of a tile (four
-  // loads of 16 bytes per lane, 8 rows each, and the scales of the lane's two rows per group of 16),
-  // an iteration later place() widens it to bf16, exactly, and stores it where the loads into LDS
-  // would have put it.
+  // loads of 16 bytes per lane, 8 rows each, and the scales of the lane's two rows per group of
+  // 16), an iteration later place() widens it to bf16, exactly, and stores it where the loads into
+  // LDS would have put it.
   constexpr int kRawLoads = 4;
   [[maybe_unused]] u32x4 raw[kRawLoads];
   [[maybe_unused]] uint32_t raw_scale[2];
-  // where the lane's first row and chunk of a group go: row r = 2 (lane / 8), chunk 2 (lane % 8); its
-  // second chunk lies in the slot ^ 1, row r + 1 in the slot ^ 1 (K: r % 16 is XORed) or ^ 4 (V)
+  // where the lane's first row and chunk of a group go: row r = 2 (lane / 8), chunk 2 (lane % 8);
+  // its second chunk lies in the slot ^ 1, row r + 1 in the slot ^ 1 (K: r % 16 is XORed) or ^ 4
+  // (V)
   [[maybe_unused]] uint32_t raw_at =
       2 * (lane >> 3) * kRowBytes +
       16 * ((2 * (lane & 7)) ^ (k_wave ? 2 * (lane >> 3) : 8 * ((lane >> 3) & 1)));
@@ -837,7 +839,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
       issue(kv0, dst);
       return;
     }
-    // the tile's rows of this wave begin at a multiple of 8 KB, so slots can be XORed into addresses
+    // the tile's rows of this wave begin at a multiple of 8 KB, so slots can be XORed into
+    // addresses
     uint32_t base = static_cast<uint32_t>(dst - smem) + (wave & 1) * (kTileBytes / 2);
     asm volatile("" : "+s"(base));  // (formed here, not kept per slot over the loop)
     const uint32_t row0 = raw_at + base, row1 = (row0 ^ (k_wave ? 16 : 64)) + kRowBytes;
@@ -1071,8 +1074,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
     }
 }
 
-// The ranges of every (block row, query head) of a launch over pages, in key order: a wave per pair,
-// its lanes over partials side by side.
+// The ranges of every (block row, query head) of a launch over pages, in key order: a wave per
+// pair, its lanes over partials side by side.
 template <int D>
 __global__ __launch_bounds__(kThreads) void attn_tiles_merge_kernel(AttnParams p, TilePlan tp,
                                                                     int total) {

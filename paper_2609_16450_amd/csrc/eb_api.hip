@@ -265,11 +265,16 @@ eb_status check_pages(const eb_paged_kv* kv, const std::vector<int32_t>& table, 
   return EB_OK;
 }
 
+eb_status fetch_table(std::vector<int32_t>& table, const eb_ragged* r, const eb_paged_kv* kv,
+                      hipStream_t s) {
+  return fetch(table, kv->page_table, static_cast<size_t>(r->batch) * kv->max_pages, s);
+}
+
 // The pages of the cached rows (cu_prefix has been checked).
 eb_status check_cached_pages(const eb_ragged* r, const eb_paged_kv* kv, hipStream_t s) {
   std::vector<int32_t> cu, table;
   eb_status st = fetch(cu, r->cu_prefix, r->batch + 1, s);
-  if (st == EB_OK) st = fetch(table, kv->page_table, static_cast<size_t>(r->batch) * kv->max_pages, s);
+  if (st == EB_OK) st = fetch_table(table, r, kv, s);
   for (int b = 0; st == EB_OK && b < r->batch; ++b)
     st = check_pages(kv, table, b, cu[b + 1] - cu[b]);
   return st;
@@ -282,7 +287,7 @@ eb_status check_written(const eb_ragged* r, const eb_paged_kv* kv, const int32_t
   eb_status st = fetch(cb, r->cu_block, r->batch + 1, s);
   if (st == EB_OK && !pos) st = fetch(cp, r->cu_prefix, r->batch + 1, s);
   if (st == EB_OK && pos) st = fetch(at, pos, r->total_block, s);
-  if (st == EB_OK) st = fetch(table, kv->page_table, static_cast<size_t>(r->batch) * kv->max_pages, s);
+  if (st == EB_OK) st = fetch_table(table, r, kv, s);
   if (st != EB_OK) return st;
   std::vector<int64_t> rows;
   for (int b = 0; b < r->batch; ++b)

@@ -4,12 +4,12 @@
 // many rows and by latency for few.  A row (token, K/V head) of D values is moved by D / 8 lanes of
 // 8 values each; a wavefront takes consecutive tokens of one head, which lie one behind the other
 // in a page (a line of an 8-bit cache with 64-wide heads holds two of them), while the packed side
-// sees whole rows of 128 bytes or more.  Workgroups run over the heads first: the packed rows of a few
-// tokens are then taken as one piece of memory (heads last: 5-13% slower).  Measured, read and write
-// bytes together: prompts of 501 to 2048 rows x 32 heads x 128 into 8 bits and back 98 us (4.9 TB/s,
-// as much as a large copy), the same into bf16 pages 53 us (5.0 TB/s), 64 prefixes of 1001 to 4096
-// rows x 4 heads out of 8 bits 105 us (4.7 TB/s).  Without gain: two, four or eight rows per lane, an
-// eighth of the rows to each XCD.
+// sees whole rows of 128 bytes or more.  Workgroups run over the heads first: the packed rows of a
+// few tokens are then taken as one piece of memory (heads last: 5-13% slower).  Measured, read and
+// write bytes together: prompts of 501 to 2048 rows x 32 heads x 128 into 8 bits and back 98 us
+// (4.9 TB/s, as much as a large copy), the same into bf16 pages 53 us (5.0 TB/s), 64 prefixes of
+// 1001 to 4096 rows x 4 heads out of 8 bits 105 us (4.7 TB/s).  Without gain: two, four or eight
+// rows per lane, an eighth of the rows to each XCD.
 #include "eb_internal.hpp"
 #include "paged.hpp"
 
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(PagedKv kv, const int
                                                            T* __restrict__ k, T* __restrict__ v) {
   constexpr int kLanes = D / 8;
   constexpr int kTokens = 64 / kLanes;
-  constexpr int kWords = kE4m3 ? 1 : sizeof(T) / 2;  // loads of 16 (8 bits: of 8) bytes per 8 values
+  constexpr int kWords = kE4m3 ? 1 : sizeof(T) / 2;  // loads per 8 values, 16 bytes (8 bits: 8)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int head = blockIdx.x % kv.hkv, col = (lane % kLanes) * 8;
   const int first = (blockIdx.x / kv.hkv * (kThreads / 64) + wave) * kTokens;

@@ -49,8 +49,8 @@ __device__ __forceinline__ f32x2 e4m3_pair_f32(uint32_t w, float scale) {
   return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, kHigh);
 }
 
-// Sixteen bytes per lane, two, or one, at byte `off` of a buffer; zeros past its end.  In functions of
-// their own, like every builtin that the host pass does not know.
+// Sixteen bytes per lane, two, or one, at byte `off` of a buffer; zeros past its end.  In functions
+// of their own, like every builtin that the host pass does not know.
 __device__ __forceinline__ u32x4 buffer_load16(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
   return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
 }
@@ -79,8 +79,8 @@ __device__ __forceinline__ int lanes_up_to(int x, int none, Op op) {
   x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));  // - 2
   x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));  // - 4
   x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));  // - 8
-  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));  // lane 15 to row 1, 47 to 3
-  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));  // lane 31 to rows 2, 3
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));  // lanes 15 and 47
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));  // lane 31
   return x;
 }
 template <class Op>
