@@ -53,7 +53,8 @@ class Cache:
                                 getattr(self.kv, which + "_scale").cpu().numpy())
 
     def fill(self, spans, rng, size=1.0):
-        """N(0, size^2) values in the first spans[b] positions, set from the host."""
+        """N(0, size^2) values in the first spans[b] positions, set from the host; large caches
+        repeat 9973 rows."""
         for which in "kv":
             pool = getattr(self.kv, which)
             n, hkv, page, d = pool.shape
@@ -62,14 +63,15 @@ class Cache:
             if not len(b_of):
                 continue
             pg, slot = self.table[b_of, p_of // page].astype(np.int64), p_of % page
-            rows = rng.standard_normal((len(b_of), hkv, d)) * size
+            rows = rng.standard_normal((min(len(b_of), 9973), hkv, d)) * size
+            again = torch.from_numpy(np.arange(len(b_of)) % len(rows)).cuda()
             at = (torch.from_numpy(pg).cuda(), slice(None), torch.from_numpy(slot).cuda())
             if self.e4m3:
                 codes, s = paged.quantise(rows)
-                pool.view(torch.uint8)[at] = torch.from_numpy(codes).cuda()
-                getattr(self.kv, which + "_scale")[at] = torch.from_numpy(s).cuda()
+                pool.view(torch.uint8)[at] = torch.from_numpy(codes).cuda()[again]
+                getattr(self.kv, which + "_scale")[at] = torch.from_numpy(s).cuda()[again]
             else:
-                pool[at] = torch.from_numpy(rows).to(pool.dtype).cuda()
+                pool[at] = torch.from_numpy(rows).to(pool.dtype).cuda()[again]
 
 
 def _special_rows(rows):
@@ -288,6 +290,54 @@ def test_attention_many_sequences(cache, dtype):
     blocks = [(i % 5) % 4 for i in range(2300)]
     cached = [(i * 13) % 40 + (500 if i == 77 else 0) for i in range(2300)]
     _close(*_attention(blocks, cached, 16, cache, dtype, 2, 64, hkv=1), dtype)
+
+
+# The plans of the tile kernel: more sequences than a wave has lanes, cut by the host (70 of one tile);
+# so many items that sequences stay whole, over more pages of 16 rows than a wave holds numbers of
+# (64); lengths so different that only the longest are cut; one long block, whose tiles share keys.
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("blocks,cached,hkv,group", [
+    ([34 + i % 3 * (i % 7 > 0) - 34 * (i == 9) for i in range(70)],
+     [(53 * i) % 900 for i in range(70)], 1, 2),
+    ([33 + i % 9 for i in range(58)], [1030 + 3 * i for i in range(58)], 16, 1),
+    ([70, 0, 66, 90, 65], [5000, 77, 10, 700, 0], 2, 3),
+    ([777], [1500], 1, 2)])
+def test_attention_plans(blocks, cached, hkv, group, cache, head_dim):
+    print(f"plans {len(blocks)} {max(cached)} G={group} {cache} D={head_dim}", flush=True)
+    _close(*_attention(blocks, cached, 16, cache, "bf16", group, head_dim, hkv=hkv), "bf16")
+
+
+# Rows of a K/V head at the border between the kernels: 32 and 33 over bf16 pages, 64 and 65 over 8
+# bits; 16 and 17 query rows per workgroup; sequences at the border of staying whole.
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("rows", [16, 17, 32, 33, 64, 65])
+@pytest.mark.parametrize("cached", [[640, 5], [768, 3], [2000, 900]])
+def test_attention_borders(rows, cached, cache):
+    print(f"borders {rows} {cached} {cache}", flush=True)
+    _close(*_attention([rows, rows // 2], cached, 64, cache, "bf16", 1, 128, hkv=3), "bf16")
+
+
+@pytest.mark.parametrize("cache,dtype", COMBOS)
+@pytest.mark.parametrize("blocks,cached,group", [([1, 1], [3000, 40], 2), ([50, 90], [900, 2500], 2),
+                                                 ([20], [4000], 1)])
+def test_workspace_is_enough(blocks, cached, group, cache, dtype):
+    """Nothing behind the bytes that the query asks for is written, and one byte less is refused."""
+    rng = np.random.default_rng(3)
+    c = Cache(cached, 2, 32, 128, cache, 4)
+    c.fill(cached, rng)
+    r = Ragged.from_lengths(blocks, cached)
+    dt = TYPES[dtype]
+    q, k, v = (torch.from_numpy(rng.standard_normal((sum(blocks), h, 128))).to(dt).cuda()
+               for h in (2 * group, 2, 2))
+    need = eb_block_attn_paged_workspace(0 if dtype == "f32" else EB_BF16, r, c.kv, 2 * group)
+    assert need > 0
+    ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(q)
+    eb_block_attn_paged(r, c.kv, q, k, v, out, ws=ws[:need])
+    assert (ws[need:] == 0xA5).all()
+    with pytest.raises(EbError, match="WORKSPACE"):
+        eb_block_attn_paged(r, c.kv, q, k, v, out, ws=ws[:need - 1])
 
 
 @pytest.mark.parametrize("cache,dtype", COMBOS)
