@@ -10,6 +10,8 @@
 // (4.9 TB/s, as much as a large copy), the same into bf16 pages 53 us (5.0 TB/s), 64 prefixes of
 // 1001 to 4096 rows x 4 heads out of 8 bits 105 us (4.7 TB/s).  Without gain: two, four or eight
 // rows per lane, an eighth of the rows to each XCD.
+#include <type_traits>
+
 #include "eb_internal.hpp"
 #include "paged.hpp"
 
@@ -19,23 +21,72 @@ namespace {
 constexpr int kThreads = 256;  // 4 waves
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));  // at any word
 
-// Eight values of a row, in fp32.
+// Eight values of a row, as they came.
 template <class T>
-__device__ __forceinline__ void load8(const T* p, float* x);
+struct Row8;
 template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* x) {
-  const f32x4u a = *reinterpret_cast<const f32x4u*>(p), b = *reinterpret_cast<const f32x4u*>(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
-template <>
-__device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float* x) {
-  const u32x4 a = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(a[i] << 16);
-    x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+struct Row8<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const f32x4u*>(p);
+    b = *reinterpret_cast<const f32x4u*>(p + 4);
   }
+  __device__ __forceinline__ void store(float* p) const {
+    *reinterpret_cast<f32x4*>(p) = a;
+    *reinterpret_cast<f32x4*>(p + 4) = b;
+  }
+  __device__ __forceinline__ float value(int i) const { return i < 4 ? a[i] : b[i - 4]; }
+  // largest magnitude, as bits
+  __device__ __forceinline__ uint32_t magnitude() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(value(i)) & 0x7fffffffu);
+    return m;
+  }
+  // E4M3 bytes of the values over `scale` = 2^e, all finite and at most 448 2^e
+  __device__ __forceinline__ u32x2 e4m3(float scale) const {
+    return u32x2{f32x4_to_e4m3(a, scale), f32x4_to_e4m3(b, scale)};
+  }
+};
+template <>
+struct Row8<uint16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const uint16_t* p) { w = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<u32x4*>(p) = w; }
+  __device__ __forceinline__ float value(int i) const {
+    return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ uint32_t magnitude() const {  // of bf16 pairs, two at a time
+    u16x2 m = pair(0);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, pair(i));
+    return static_cast<uint32_t>(max(m[0], m[1])) << 16;
+  }
+  __device__ __forceinline__ u32x2 e4m3(float scale) const {
+    return u32x2{bf16x4_to_e4m3(w[0], w[1], scale), bf16x4_to_e4m3(w[2], w[3], scale)};
+  }
+
+ private:
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  __device__ __forceinline__ u16x2 pair(int i) const {
+    const uint32_t x = w[i] & 0x7fff7fffu;
+    return __builtin_bit_cast(u16x2, x);
+  }
+};
+
+// Largest x of each group of kLanes lanes (8 or 16), on every lane of the group.
+template <int kLanes>
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+  auto with = [&](auto ctrl) {
+    constexpr int kCtrl = decltype(ctrl)::value;
+    x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(
+                   0, static_cast<int>(x), kCtrl, 0xf, 0xf, true)));
+  };
+  with(std::integral_constant<int, 0xb1>{});   // lane ^ 1
+  with(std::integral_constant<int, 0x4e>{});   // lane ^ 2
+  with(std::integral_constant<int, 0x141>{});  // lane ^ 7
+  if (kLanes == 16) with(std::integral_constant<int, 0x140>{});  // lane ^ 15
+  return x;
 }
 
 // Where a packed row goes to or comes from: the row's number in the pool, (page hkv + head)
@@ -70,9 +121,9 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(PagedKv kv, const in
   if (first >= total) return;  // uniform per wavefront
   const int token = min(first + lane / kLanes, total - 1);
   const size_t src = (static_cast<size_t>(token) * kv.hkv + head) * D + col;
-  float x[2][8];
-  load8(k + src, x[0]);
-  load8(v + src, x[1]);
+  Row8<T> x[2];
+  x[0].load(k + src);
+  x[1].load(v + src);
   int at = pos ? pos[token] : 0;
   const int b = lane_sequence(cu_block, batch, find_sequence(cu_block, batch, first, lane), token);
   if (!pos) at = cu_prefix[b + 1] - cu_prefix[b] + token - cu_block[b];
@@ -80,33 +131,26 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(PagedKv kv, const in
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     uint8_t* const pool = i ? kv.v : kv.k;
-    const float* const y = x[i];
     if constexpr (kE4m3) {
-      uint32_t amax = 0;
+      uint32_t amax = group_max<kLanes>(x[i].magnitude());
+      int e = e4m3_exponent(amax);
+      u32x2 w = x[i].e4m3(e8m0(e + 127));
+      if (__any(amax >= 0x7f800000u)) {  // a NaN or an infinity somewhere: its row's others count
+        amax = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) amax = max(amax, finite_mag(y[e]));
+        for (int j = 0; j < 8; ++j) amax = max(amax, finite_mag(x[i].value(j)));
+        e = e4m3_exponent(group_max<kLanes>(amax));
+        float y[8];
 #pragma unroll
-      for (int m = 1; m < kLanes; m <<= 1)
-        amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), m)));
-      const int e = e4m3_exponent(amax);
-      const float inv = e8m0(127 - e);
-      const u32x2 w{pack4_e4m3(y, inv), pack4_e4m3(y + 4, inv)};
+        for (int j = 0; j < 8; ++j) y[j] = x[i].value(j);
+        w = u32x2{pack4_e4m3(y, e8m0(127 - e)), pack4_e4m3(y + 4, e8m0(127 - e))};
+      }
       if (row >= 0) {
         *reinterpret_cast<u32x2*>(pool + row * D + col) = w;
         if (col == 0) (i ? kv.v_scale : kv.k_scale)[row] = static_cast<uint8_t>(e + 127);
       }
     } else if (row >= 0) {
-      T* const dst = reinterpret_cast<T*>(pool) + row * D + col;
-      if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<f32x4*>(dst) = f32x4{y[0], y[1], y[2], y[3]};
-        *reinterpret_cast<f32x4*>(dst + 4) = f32x4{y[4], y[5], y[6], y[7]};
-      } else {
-        u32x4 w;  // the bf16 bits as they came
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          w[e] = (__float_as_uint(y[2 * e]) >> 16) | __float_as_uint(y[2 * e + 1]);
-        *reinterpret_cast<u32x4*>(dst) = w;
-      }
+      x[i].store(reinterpret_cast<T*>(pool) + row * D + col);
     }
   }
 }

@@ -37,6 +37,23 @@ __device__ __forceinline__ uint32_t pack4_e4m3(const float* x, float inv) {
   return static_cast<uint32_t>(w);
 }
 
+// Four values over `scale` (a power of two) as E4M3 bytes, rounded once to nearest even; for finite
+// values of at most 448 scale.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t f32x4_to_e4m3(f32x4 x, float scale) {
+  s16x2 w{};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[0], x[1], scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[2], x[3], scale, true);
+  return __builtin_bit_cast(uint32_t, w);
+}
+__device__ __forceinline__ uint32_t bf16x4_to_e4m3(uint32_t lo, uint32_t hi, float scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  s16x2 w{};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, lo), scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, hi), scale, true);
+  return __builtin_bit_cast(uint32_t, w);
+}
+
 // Two of four E4M3 bytes (the low two, or with kHigh the high two) times `scale` (a power of two)
 // as bf16, exactly; and as fp32.
 typedef float f32x2 __attribute__((ext_vector_type(2)));
