@@ -5,11 +5,14 @@
 // 8 values each; a wavefront takes consecutive tokens of one head, which lie one behind the other
 // in a page (a line of an 8-bit cache with 64-wide heads holds two of them), while the packed side
 // sees whole rows of 128 bytes or more.  Workgroups run over the heads first: the packed rows of a
-// few tokens are then taken as one piece of memory (heads last: 5-13% slower).  Measured, read and
-// write bytes together: prompts of 501 to 2048 rows x 32 heads x 128 into 8 bits and back 98 us
-// (4.9 TB/s, as much as a large copy), the same into bf16 pages 53 us (5.0 TB/s), 64 prefixes of
-// 1001 to 4096 rows x 4 heads out of 8 bits 105 us (4.7 TB/s).  Without gain: two, four or eight
-// rows per lane, an eighth of the rows to each XCD.
+// few tokens are then taken as one piece of memory (heads last: 5-13% slower).
+// Quantising is a maximum over bf16 pairs and lane exchanges, and one instruction per two values,
+// exact because the scale is a power of two; rows with a NaN or an infinity take the long way.
+// Measured, bytes read and written together: prompts of 501 to 2048 rows x 32 heads x 128 into 8
+// bits and back 95 us (5.0 TB/s, as a large copy; 99 us with the values unpacked one by one), the
+// same into bf16 pages 53 us (5.0 TB/s), 64 prefixes of 1001 to 4096 rows x 4 heads out of 8 bits
+// 105 us (4.6 TB/s).  Without gain: two, four or eight rows per lane, an eighth of the rows to each
+// XCD.
 #include <type_traits>
 
 #include "eb_internal.hpp"
