@@ -195,9 +195,11 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(PagedKv kv, const int
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     T* const out = (i ? v : k) + dst;
-    if (row < 0)
+    if (row < 0) {
+      scale[i] = 127;  // (what was loaded may stand for infinity, and zero times that is NaN)
 #pragma unroll
       for (int e = 0; e < kWords; ++e) w[i][e] = u32x4{};
+    }
     if constexpr (!kE4m3) {
 #pragma unroll
       for (int e = 0; e < kWords; ++e)  // (fp32 rows may start at any float)

@@ -162,6 +162,33 @@ def test_rows_without_a_page(cache, dtype):
         np.testing.assert_array_equal(getattr(c.kv, n).view(torch.uint8).cpu().numpy(), w)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("byte", [0, 255])
+def test_no_page_at_all(byte, head_dim, dtype):
+    """Rows that have no page read as zeros whatever the pool's first row and its scale hold."""
+    table = torch.full((1, 2), -1, dtype=torch.int32, device="cuda")
+    kv = PagedKV.empty(1, 2, 16, head_dim, table, TYPES["e4m3"])
+    for t in (kv.k, kv.v):
+        t.view(torch.uint8).fill_(0x38)
+    for t in (kv.k_scale, kv.v_scale):
+        t.fill_(byte)
+    out = [torch.full((20, 2, head_dim), 7.0, dtype=TYPES[dtype], device="cuda") for _ in "kv"]
+    eb_kv_read(Ragged.from_lengths([0], [20]), kv, *out)
+    for o in out:
+        assert torch.equal(o, torch.zeros_like(o))
+    # the attention: 20 keys of zeros and the block's own, of ones
+    for rows in (1, 12, 100):
+        one = torch.ones(rows, 2, head_dim, dtype=TYPES[dtype], device="cuda")
+        q = torch.zeros(rows, 4, head_dim, dtype=TYPES[dtype], device="cuda")
+        got = torch.empty_like(q)
+        eb_block_attn_paged(Ragged.from_lengths([rows], [20]), kv, q, one, one, got)
+        want = rows / (rows + 20)
+        # weights of exactly 1, their sum exact: the division's and the output's rounding
+        tol = want * (2.0 ** -8 + 2.0 ** -20 if dtype == "bf16" else 2.0 ** -20)
+        assert (got.double() - want).abs().max().item() <= tol
+
+
 @pytest.mark.parametrize("head_dim,hkv", [(128, 2), (64, 5)])
 @pytest.mark.parametrize("cache,dtype", [("f32", "f32"), ("bf16", "bf16"), ("e4m3", "f32"),
                                          ("e4m3", "bf16")])
