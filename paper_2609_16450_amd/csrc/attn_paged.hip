@@ -369,9 +369,18 @@ constexpr long kSplitItems1 = 160, kSplitItems2 = 420, kSplitItems = 900;
 // stages, 16 against 19 us; behind 600, 12 stages, 18 us either way.
 constexpr long kWholeStages = 8;
 
+// With blocks of unlike lengths, counting every sequence as the longest leaves workgroups without an
+// item, and while these come and go the others wait: 255 tokens and a chunk of 2048 behind 1000 to
+// 4000, 28/4 heads x 128, 115000 workgroups for at most 1500 items, 1009 us, counted off 362 us
+// (32/32 heads 5125 and 1986; 64 blocks of 16 to 256 rows, 3584 for 2160, 621 and 573).  Counting
+// costs a workgroup a look at the lengths of 64 sequences at a time, about a quarter of such a
+// visit.
+constexpr long kCountBatch = 256;
+constexpr long kCountTurns = 8;  // runs per XCD, at least
+
 struct TilesLaunch {
   TilePlan plan;
-  unsigned grid;
+  long grid;
   size_t parts;  // items that may leave partials
 };
 TilesLaunch tiles_plan(const PagedAttnArgs& a) {
@@ -390,15 +399,23 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a) {
     t.parts = t.plan.cap;
     return t;
   }
-  const long base = row_tiles * hkv * a.batch;
+  const long all = row_tiles * hkv * a.batch;
+  const bool counted = all * kCountBatch > whole * (kCountBatch + a.batch);
+  const long base = counted ? whole : all;
   const long want =
       stages <= kWholeStages ? 1 : max(1L, min((kAttnTargetWgs + base - 1) / base, stages));
   const long chunk = (stages + want - 1) / want;
   t.plan.chunk = static_cast<int>(chunk);
   t.plan.nsplit = static_cast<int>((stages + chunk - 1) / chunk);
-  const long units = a.batch * hkv * t.plan.nsplit;
-  t.grid = static_cast<unsigned>(kXcdCount * ((units + kXcdCount - 1) / kXcdCount) * row_tiles);
-  t.parts = t.plan.nsplit > 1 ? units * row_tiles : 0;
+  if (counted) {
+    const long items = whole * t.plan.nsplit;
+    const long run = max(1L, min(row_tiles, items / (kXcdCount * kCountTurns)));
+    t.plan.run = static_cast<int>(run);
+    t.grid = kXcdCount * run * ((items + kXcdCount * run - 1) / (kXcdCount * run));
+  } else {
+    t.grid = kXcdCount * ((a.batch * hkv * t.plan.nsplit + kXcdCount - 1) / kXcdCount) * row_tiles;
+  }
+  t.parts = t.plan.nsplit > 1 ? t.grid : 0;
   return t;
 }
 
@@ -406,18 +423,19 @@ template <int D, bool kE4m3>
 hipError_t launch_tiles(const PagedAttnArgs& a, void* ws, hipStream_t s) {
   const TilesLaunch t = tiles_plan(a);
   const AttnParams p = attn_params(packed_args(a), SplitPlan{1, 0}, nullptr);
-  PagedKeys<kE4m3> keys{a.kv, t.plan};
+  using Keys = PagedKeys<kE4m3>;
+  Keys keys{a.kv, t.plan};
   const size_t rows = t.parts * kRowsPerWg;
   keys.plan.o_part = static_cast<float*>(ws);
   keys.plan.m_part = keys.plan.o_part + rows * D;
   keys.plan.l_part = keys.plan.m_part + rows;
   keys.plan.found = reinterpret_cast<int32_t*>(keys.plan.l_part + rows);
   if constexpr (D == 128)
-    hipLaunchKernelGGL(attn_bf16_d128_kernel<PagedKeys<kE4m3>>, dim3(t.grid), dim3(kThreads), 0, s,
-                       p, keys, 0, 0);
+    hipLaunchKernelGGL(attn_bf16_d128_kernel<Keys>, dim3(static_cast<unsigned>(t.grid)),
+                       dim3(kThreads), 0, s, p, keys, 0, 0);
   else
-    hipLaunchKernelGGL((attn_bf16_kernel<D, PagedKeys<kE4m3>>), dim3(t.grid), dim3(kThreads), 0, s,
-                       p, keys, 0, 0);
+    hipLaunchKernelGGL((attn_bf16_kernel<D, Keys>), dim3(static_cast<unsigned>(t.grid)),
+                       dim3(kThreads), 0, s, p, keys, 0, 0);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || t.parts == 0) return e;
   const long pairs = static_cast<long>(a.total_block) * a.hq;
@@ -435,7 +453,9 @@ size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
   if (bf16) {
     const TilesLaunch t = tiles_plan(a);
     return t.parts * kRowsPerWg * (a.kv.head_dim + 2) * sizeof(float) +
-           (t.plan.cap ? 2 * kPlanMaxBatch * sizeof(int32_t) : 0);
+           (t.plan.cap   ? 2 * kPlanMaxBatch * sizeof(int32_t)
+            : t.plan.run ? a.batch * sizeof(int32_t)
+                         : 0);
   }
   const SplitPlan sp = f32_plan(a);
   if (sp.nsplit == 1) return 0;

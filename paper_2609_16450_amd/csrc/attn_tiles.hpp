@@ -58,16 +58,20 @@ struct PageWindow {
 // ranges for every sequence as fill the chip when all are as long as the longest: 28/4 heads x 128,
 // 16 blocks of 32 to 256 rows behind 2000 to 16000, 576 -> 453 us; 8 of 20 to 100 behind 1000 to
 // 8000, 71 -> 60 us; 16/4 heads x 64, the same, 49 -> 32 us.  Equal lengths gain nothing (32 heads,
-// 1000 rows behind 3000: 89 and 91 us). With cap = 0 chunk is the host's, and every sequence counts
-// as the longest, with as many row tiles.
+// 1000 rows behind 3000: 89 and 91 us). With cap = 0 chunk is the host's; then either every sequence
+// counts as the longest, with as many row tiles, and many a workgroup may find nothing to do, or
+// (run > 0) the items are counted off, and a workgroup finds its own by a scan over the lengths.
 struct TilePlan {
   int batch, row_tiles;
   int cap;
   int chunk, nsplit;  // cap = 0: stages per range, ranges per sequence
+  int run;            // > 0: items counted off, dealt to the XCDs in runs of so many
   float* o_part;      // [items, kRowsPerWg, D], then m and l [items, kRowsPerWg]
   float* m_part;
   float* l_part;
-  int32_t* found;  // cap > 0: of each of kPlanMaxBatch sequences its first item, then its ranges
+  // cap > 0: of each of kPlanMaxBatch sequences its first item, then its ranges; run > 0: of each
+  // sequence with more than one range its first item
+  int32_t* found;
 };
 template <bool kBits8>
 struct PagedKeys {
@@ -160,10 +164,47 @@ __device__ __forceinline__ int range_start(int stages, int range, int ranges) {
 struct TileItem {
   int b, g, tile, item, range, ranges;
 };
+// Item number `local` of a sequence.
+__device__ __forceinline__ void place_item(TileItem& it, int local, int row_tiles, int hkv) {
+  it.tile = local % row_tiles;
+  it.g = local / row_tiles % hkv;
+  it.range = local / row_tiles / hkv;
+}
+// An item counted off (run > 0), by the whole wavefront.
+__device__ __forceinline__ bool count_off(const AttnParams& p, const TilePlan& tp, int xcd, int j,
+                                          int lane, int wave, TileItem& it) {
+  it.item = (j / tp.run * kXcdCount + xcd) * tp.run + j % tp.run;
+  int first = 0, b = tp.batch, row_tiles = 1;
+  for (int b0 = 0; b0 < tp.batch; b0 += 64) {
+    const int own = min(b0 + lane, tp.batch - 1);
+    const int len = b0 + lane < tp.batch ? p.cu_block[own + 1] - p.cu_block[own] : 0;
+    const int stages = tile_stages(p.cu_prefix[own + 1] - p.cu_prefix[own], len);
+    const int ranges = (stages + tp.chunk - 1) / tp.chunk, tiles = tile_rows(len, p.group);
+    const int n = ranges * tiles * p.hkv;
+    const int upto = lanes_up_to(n, 0, AddOp{});
+    const uint64_t past = __ballot(first + upto > it.item);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      first += __builtin_amdgcn_readlane(upto - n, l);
+      b = b0 + l;
+      it.ranges = __builtin_amdgcn_readlane(ranges, l);
+      row_tiles = __builtin_amdgcn_readlane(tiles, l);
+      break;
+    }
+    first += __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (b >= tp.batch) return false;
+  it.b = __builtin_amdgcn_readfirstlane(b);
+  place_item(it, it.item - first, row_tiles, p.hkv);
+  if (it.item == first && it.ranges > 1 && wave == 0 && lane == 0)  // for the merge
+    tp.found[b] = first;
+  return true;
+}
 // The item of this workgroup; false if there is none.
 __device__ __forceinline__ bool find_item(const AttnParams& p, const TilePlan& tp, int lane,
                                           int wave, TileItem& it) {
   const int xcd = blockIdx.x % kXcdCount, j = blockIdx.x / kXcdCount;
+  if (tp.run > 0) return count_off(p, tp, xcd, j, lane, wave, it);
   if (tp.cap == 0) {
     const int unit = kXcdCount * (j / tp.row_tiles) + xcd;
     it.tile = j % tp.row_tiles;
@@ -195,9 +236,7 @@ __device__ __forceinline__ bool find_item(const AttnParams& p, const TilePlan& t
   const int local = it.item - __builtin_amdgcn_readlane(l.upto - l.items, b);
   const int row_tiles = tile_rows(p.cu_block[b + 1] - p.cu_block[b], p.group);
   it.b = b;
-  it.tile = local % row_tiles;
-  it.g = local / row_tiles % p.hkv;
-  it.range = local / row_tiles / p.hkv;
+  place_item(it, local, row_tiles, p.hkv);
   it.ranges = __builtin_amdgcn_readlane(l.ranges, b);
   return true;
 }
@@ -1093,9 +1132,9 @@ __global__ __launch_bounds__(kThreads) void attn_tiles_merge_kernel(AttnParams p
     ranges = tp.found[kPlanMaxBatch + b];
     row_tiles = tile_rows(len, p.group);
   } else {
-    row_tiles = tp.row_tiles;
-    first = b * tp.nsplit * p.hkv * row_tiles;
     ranges = (tile_stages(p.cu_prefix[b + 1] - p.cu_prefix[b], len) + tp.chunk - 1) / tp.chunk;
+    row_tiles = tp.run > 0 ? tile_rows(len, p.group) : tp.row_tiles;
+    first = tp.run == 0 ? b * tp.nsplit * p.hkv * row_tiles : ranges > 1 ? tp.found[b] : 0;
   }
   if (ranges <= 1) return;  // written out by its only workgroup
   auto at = [&](int k) {

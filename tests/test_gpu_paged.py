@@ -335,6 +335,20 @@ def test_attention_plans(blocks, cached, hkv, group, cache, head_dim):
     _close(*_attention(blocks, cached, 16, cache, "bf16", group, head_dim, hkv=hkv), "bf16")
 
 
+# Long blocks among many short ones: key ranges of counted items, whole sequences, a batch of more
+# than 2048, the long one last, in the middle, and first; and few sequences of many heads.
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("blocks,cached,hkv,group", [
+    ([1] * 80 + [300], [(53 * i) % 900 for i in range(81)], 1, 2),
+    ([i % 4 for i in range(150)] + [500] + [2] * 130, [(91 * i) % 400 for i in range(281)], 4, 3),
+    ([200, 70] + [1] * 2300, [40, 600] + [(7 * i) % 50 for i in range(2300)], 1, 2),
+    ([600] + [1] * 39, [1000] + [9 * i for i in range(39)], 32, 1)])
+def test_attention_mixed(blocks, cached, hkv, group, cache, head_dim):
+    print(f"mixed {len(blocks)} {max(cached)} G={group} {cache} D={head_dim}", flush=True)
+    _close(*_attention(blocks, cached, 16, cache, "bf16", group, head_dim, hkv=hkv), "bf16")
+
+
 # Rows of a K/V head at the border between the kernels: 32 and 33 over bf16 pages, 64 and 65 over 8
 # bits; 16 and 17 query rows per workgroup; sequences at the border of staying whole.
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
@@ -349,6 +363,15 @@ def test_attention_borders(rows, cached, cache):
 @pytest.mark.parametrize("blocks,cached,group", [([1, 1], [3000, 40], 2), ([50, 90], [900, 2500], 2),
                                                  ([20], [4000], 1)])
 def test_workspace_is_enough(blocks, cached, group, cache, dtype):
+    _guarded(blocks, cached, group, cache, dtype)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_workspace_of_many_sequences(cache):
+    _guarded([1] * 80 + [300], [10 * i for i in range(81)], 2, cache, "bf16")
+
+
+def _guarded(blocks, cached, group, cache, dtype):
     """Nothing behind the bytes that the query asks for is written, and one byte less is refused."""
     rng = np.random.default_rng(3)
     c = Cache(cached, 2, 32, 128, cache, 4)
