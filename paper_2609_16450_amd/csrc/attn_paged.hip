@@ -281,12 +281,26 @@ constexpr int kFewMaxBatch = 2048;
 // stages, 14.5 whole against 9.2 us).
 constexpr int kFewWhole = 5;
 
-bool few_ok(bool bf16, const PagedAttnArgs& a) {
-  const int most = a.kv.type == CacheType::kE4m3 ? kFewRowsE4m3 : kFewRowsBf16;
-  return bf16 && static_cast<long>(a.max_block) * (a.hq / a.kv.hkv) <= most;
-}
-int few_tiles(const PagedAttnArgs& a) {  // 16-row tiles per workgroup
-  return a.max_block * (a.hq / a.kv.hkv) <= kSmallTile ? 1 : 2;
+// Query rows per K/V head up to which sequences of this call go to the kernel for few rows; the
+// others go to the tile kernel, in a launch of their own.  Over 8 bits that is worth two launches
+// where a long block comes with many short ones: 63 tokens and a chunk of 1024 behind 1000 to 4000
+// rows, 28/4 heads x 128, 141 us in one launch, 112 in two, 255 and a chunk of 2048 362 and 288
+// (32/32 heads 1741 and 1150, 16/4 heads x 64 244 and 167).  Over bf16 pages the tile kernel reads
+// the keys of a few rows about as fast.  The sizes of single blocks are on the device; the host
+// goes by the mean of all but the longest, and by the cached rows, whether the launch can gain more
+// than it takes (16 tokens and a chunk of 256, 28/4 heads: 42 us in one, 50 in two).
+constexpr long kFewWorth = 4096;  // cached stages of 64 rows, over the K/V heads
+long few_rows(bool bf16, const PagedAttnArgs& a) {
+  if (!bf16) return 0;
+  const bool e4m3 = a.kv.type == CacheType::kE4m3;
+  const long group = a.hq / a.kv.hkv, rows = a.max_block * group;
+  if (rows <= (e4m3 ? kFewRowsE4m3 : kFewRowsBf16)) return rows;
+  const long others = (a.total_block - a.max_block) * group;  // of batch - 1 sequences
+  const long stages = static_cast<long>(a.total_prefix) / kKeys * a.kv.hkv;
+  if (!e4m3 || a.batch == 1 || stages < kFewWorth) return 0;
+  for (long most = kSmallTile; most <= 2 * kSmallTile; most *= 2)
+    if (2 * others <= most * (a.batch - 1)) return most;
+  return 0;
 }
 
 // The line of stages (attn_paged_few.hpp) in as many equal parts as workgroups that run at a time,
@@ -297,13 +311,15 @@ int few_tiles(const PagedAttnArgs& a) {  // 16-row tiles per workgroup
 // slower.  Every workgroup looks at all sequences to find its part, so more than kFewMaxBatch
 // sequences take one workgroup each.
 struct FewPlan {
+  int most;       // query rows per K/V head
   int row_tiles, groups, chunk;
   size_t slots;  // partial rows of the workspace
 };
-FewPlan few_plan(const PagedAttnArgs& a) {
+FewPlan few_plan(const PagedAttnArgs& a, long rows) {
   FewPlan f;
-  const int per = few_tiles(a) * kSmallTile;
-  f.row_tiles = (a.max_block * (a.hq / a.kv.hkv) + per - 1) / per;
+  f.most = static_cast<int>(rows);
+  const int per = (rows <= kSmallTile ? 1 : 2) * kSmallTile;
+  f.row_tiles = (f.most + per - 1) / per;
   const long lines = static_cast<long>(f.row_tiles) * a.kv.hkv;
   if (a.batch > kFewMaxBatch) {
     f.groups = a.batch, f.chunk = 0, f.slots = 0;
@@ -332,12 +348,11 @@ AttnArgs packed_args(const PagedAttnArgs& a) {
 }
 
 template <int D, bool kE4m3, int kTiles>
-hipError_t launch_few(const PagedAttnArgs& a, void* ws, hipStream_t s) {
-  const FewPlan f = few_plan(a);
+hipError_t launch_few(const PagedAttnArgs& a, const FewPlan& f, void* ws, hipStream_t s) {
   float* const o = static_cast<float*>(ws);
   float* const m = o + f.slots * D;
   const FewParams p{attn_params(packed_args(a), SplitPlan{1, 0}, nullptr), a.kv, a.batch,
-                    f.row_tiles, f.groups, f.chunk, o, m, m + f.slots};
+                    f.row_tiles, f.groups, f.chunk, f.most, o, m, m + f.slots};
   const long units = static_cast<long>(f.groups) * a.kv.hkv;
   const dim3 grid(static_cast<unsigned>(8 * ((units + 7) / 8) * f.row_tiles));
   hipLaunchKernelGGL((attn_paged_few_kernel<D, kE4m3, kTiles>), grid,
@@ -351,11 +366,12 @@ hipError_t launch_few(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 }
 
 template <int D>
-hipError_t launch_few_any(const PagedAttnArgs& a, void* ws, hipStream_t s) {
+hipError_t launch_few_any(const PagedAttnArgs& a, long rows, void* ws, hipStream_t s) {
   const bool e4m3 = a.kv.type == CacheType::kE4m3;
-  if (few_tiles(a) == 1)
-    return e4m3 ? launch_few<D, true, 1>(a, ws, s) : launch_few<D, false, 1>(a, ws, s);
-  return e4m3 ? launch_few<D, true, 2>(a, ws, s) : launch_few<D, false, 2>(a, ws, s);
+  const FewPlan f = few_plan(a, rows);
+  if (rows <= kSmallTile)
+    return e4m3 ? launch_few<D, true, 1>(a, f, ws, s) : launch_few<D, false, 1>(a, f, ws, s);
+  return e4m3 ? launch_few<D, true, 2>(a, f, ws, s) : launch_few<D, false, 2>(a, f, ws, s);
 }
 
 // ---- many query rows, bf16: the tile kernels of the packed prefix ---------------------------
@@ -369,9 +385,9 @@ constexpr long kSplitItems1 = 160, kSplitItems2 = 420, kSplitItems = 900;
 // stages, 16 against 19 us; behind 600, 12 stages, 18 us either way.
 constexpr long kWholeStages = 8;
 
-// With blocks of unlike lengths, counting every sequence as the longest leaves workgroups without an
-// item, and while these come and go the others wait: 255 tokens and a chunk of 2048 behind 1000 to
-// 4000, 28/4 heads x 128, 115000 workgroups for at most 1500 items, 1009 us, counted off 362 us
+// With blocks of unlike lengths, counting every sequence as the longest leaves workgroups without
+// an item, and while these come and go the others wait: 255 tokens and a chunk of 2048 behind 1000
+// to 4000, 28/4 heads x 128, 115000 workgroups for at most 1500 items, 1009 us, counted off 362 us
 // (32/32 heads 5125 and 1986; 64 blocks of 16 to 256 rows, 3584 for 2160, 621 and 573).  Counting
 // costs a workgroup a look at the lengths of 64 sequences at a time, about a quarter of such a
 // visit.
@@ -383,15 +399,19 @@ struct TilesLaunch {
   long grid;
   size_t parts;  // items that may leave partials
 };
-TilesLaunch tiles_plan(const PagedAttnArgs& a) {
+// (of the sequences with more than `skip` query rows per K/V head)
+TilesLaunch tiles_plan(const PagedAttnArgs& a, long skip) {
   const long group = a.hq / a.kv.hkv, hkv = a.kv.hkv;
   const long row_tiles = (a.max_block * group + kRowsPerWg - 1) / kRowsPerWg;
   const long stages = (a.max_prefix + kKeys - 1L) / kKeys + (a.max_block + kKeys - 1) / kKeys;
   // items of whole sequences, at most
-  const long whole = hkv * min(a.batch * row_tiles, a.total_block * group / kRowsPerWg + a.batch);
+  const long rows = a.total_block * group;
+  const long sequences = min(static_cast<long>(a.batch), rows / (skip + 1));
+  const long whole = hkv * min(sequences * row_tiles, rows / kRowsPerWg + sequences);
   TilesLaunch t{};
   t.plan.batch = a.batch;
   t.plan.row_tiles = static_cast<int>(row_tiles);
+  t.plan.skip = static_cast<int>(skip);
   if (a.batch <= kPlanMaxBatch && whole <= kSplitItems && stages > kWholeStages) {
     const int rounds = whole <= kSplitItems1 ? 1 : whole <= kSplitItems2 ? 2 : 4;
     t.plan.cap = rounds * kAttnTargetWgs;
@@ -401,15 +421,19 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a) {
   }
   const long all = row_tiles * hkv * a.batch;
   const bool counted = all * kCountBatch > whole * (kCountBatch + a.batch);
-  const long base = counted ? whole : all;
+  // items of whole sequences as they are likely to be (few_rows skips short ones, not knowing them)
+  const long likely = skip ? min(whole, hkv * (rows / kRowsPerWg + 1)) : whole;
+  const long base = counted ? likely : all;
+  // (to the nearest: 400 sequences whole 89 us, halved 97; 280 of them 82 and 68, 16/4 heads x 64)
   const long want =
-      stages <= kWholeStages ? 1 : max(1L, min((kAttnTargetWgs + base - 1) / base, stages));
+      stages <= kWholeStages ? 1 : max(1L, min((kAttnTargetWgs + base / 2) / base, stages));
   const long chunk = (stages + want - 1) / want;
   t.plan.chunk = static_cast<int>(chunk);
   t.plan.nsplit = static_cast<int>((stages + chunk - 1) / chunk);
   if (counted) {
     const long items = whole * t.plan.nsplit;
-    const long run = max(1L, min(row_tiles, items / (kXcdCount * kCountTurns)));
+    const long run =
+        max(1L, min(row_tiles, likely * t.plan.nsplit / (kXcdCount * kCountTurns)));
     t.plan.run = static_cast<int>(run);
     t.grid = kXcdCount * run * ((items + kXcdCount * run - 1) / (kXcdCount * run));
   } else {
@@ -420,8 +444,8 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a) {
 }
 
 template <int D, bool kE4m3>
-hipError_t launch_tiles(const PagedAttnArgs& a, void* ws, hipStream_t s) {
-  const TilesLaunch t = tiles_plan(a);
+hipError_t launch_tiles(const PagedAttnArgs& a, long skip, void* ws, hipStream_t s) {
+  const TilesLaunch t = tiles_plan(a, skip);
   const AttnParams p = attn_params(packed_args(a), SplitPlan{1, 0}, nullptr);
   using Keys = PagedKeys<kE4m3>;
   Keys keys{a.kv, t.plan};
@@ -449,13 +473,14 @@ hipError_t launch_tiles(const PagedAttnArgs& a, void* ws, hipStream_t s) {
 
 size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
   if (a.total_block == 0 || a.max_block == 0) return 0;
-  if (few_ok(bf16, a)) return few_plan(a).slots * (a.kv.head_dim + 2) * sizeof(float);
-  if (bf16) {
-    const TilesLaunch t = tiles_plan(a);
-    return t.parts * kRowsPerWg * (a.kv.head_dim + 2) * sizeof(float) +
-           (t.plan.cap   ? 2 * kPlanMaxBatch * sizeof(int32_t)
-            : t.plan.run ? a.batch * sizeof(int32_t)
-                         : 0);
+  if (bf16) {  // one launch after the other, in the same memory
+    const long few = few_rows(bf16, a);
+    const size_t row = (a.kv.head_dim + 2) * sizeof(float);
+    const size_t bytes = few ? few_plan(a, few).slots * row : 0;
+    if (few == static_cast<long>(a.max_block) * (a.hq / a.kv.hkv)) return bytes;
+    const TilesLaunch t = tiles_plan(a, few);
+    const size_t found = t.plan.cap ? 2 * kPlanMaxBatch : t.plan.run ? a.batch : 0;
+    return max(bytes, t.parts * kRowsPerWg * row + found * sizeof(int32_t));
   }
   const SplitPlan sp = f32_plan(a);
   if (sp.nsplit == 1) return 0;
@@ -465,15 +490,20 @@ size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
 
 hipError_t attn_paged(bool bf16, const PagedAttnArgs& a, void* ws, hipStream_t s) {
   if (a.total_block == 0 || a.max_block == 0) return hipSuccess;
-  if (few_ok(bf16, a))
-    return a.kv.head_dim == 128 ? launch_few_any<128>(a, ws, s) : launch_few_any<64>(a, ws, s);
-  const bool e4m3 = a.kv.type == CacheType::kE4m3;
-  if (a.kv.head_dim == 128) {
-    if (bf16) return e4m3 ? launch_tiles<128, true>(a, ws, s) : launch_tiles<128, false>(a, ws, s);
-    return e4m3 ? launch_f32<128, uint8_t>(a, ws, s) : launch_f32<128, float>(a, ws, s);
+  const bool e4m3 = a.kv.type == CacheType::kE4m3, d128 = a.kv.head_dim == 128;
+  if (!bf16) {
+    if (d128) return e4m3 ? launch_f32<128, uint8_t>(a, ws, s) : launch_f32<128, float>(a, ws, s);
+    return e4m3 ? launch_f32<64, uint8_t>(a, ws, s) : launch_f32<64, float>(a, ws, s);
   }
-  if (bf16) return e4m3 ? launch_tiles<64, true>(a, ws, s) : launch_tiles<64, false>(a, ws, s);
-  return e4m3 ? launch_f32<64, uint8_t>(a, ws, s) : launch_f32<64, float>(a, ws, s);
+  const long few = few_rows(bf16, a);
+  if (few > 0) {
+    const hipError_t e =
+        d128 ? launch_few_any<128>(a, few, ws, s) : launch_few_any<64>(a, few, ws, s);
+    if (e != hipSuccess || few == static_cast<long>(a.max_block) * (a.hq / a.kv.hkv)) return e;
+  }
+  if (d128)
+    return e4m3 ? launch_tiles<128, true>(a, few, ws, s) : launch_tiles<128, false>(a, few, ws, s);
+  return e4m3 ? launch_tiles<64, true>(a, few, ws, s) : launch_tiles<64, false>(a, few, ws, s);
 }
 
 }  // namespace eb

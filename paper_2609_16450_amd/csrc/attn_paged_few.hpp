@@ -46,6 +46,7 @@ struct FewParams {
   int row_tiles;  // tiles of query rows per (sequence, K/V head)
   int groups;     // workgroups along the line of a (K/V head, tile)
   int chunk;      // stages per workgroup; 0: workgroup w takes sequence w whole
+  int most;       // sequences of more query rows per K/V head are another launch's
   // partials of (line, workgroup, slot), line = K/V head * row_tiles + tile
   float* o_part;  // [rows of a tile, D]
   float* m_part;  // [rows of a tile], log2 units
@@ -53,11 +54,12 @@ struct FewParams {
 };
 
 // Stages of sequence b in the line of the tile at query row row0 (none if the tile lies past its
-// rows): its cached rows, then the block's.
-__device__ __forceinline__ int few_stages(const AttnParams& p, int b, int row0) {
-  const int len = p.cu_block[b + 1] - p.cu_block[b];
+// rows, or it has too many): its cached rows, then the block's.
+__device__ __forceinline__ int few_stages(const FewParams& fp, int b, int row0) {
+  const AttnParams& p = fp.a;
+  const int rows = (p.cu_block[b + 1] - p.cu_block[b]) * p.group;
   const int plen = p.cu_prefix[b + 1] - p.cu_prefix[b];
-  return row0 < len * p.group ? (plen + kFewStage - 1) / kFewStage + 1 : 0;
+  return row0 < rows && rows <= fp.most ? (plen + kFewStage - 1) / kFewStage + 1 : 0;
 }
 
 // The sequence that holds stage s of the line, and its first stage, found by the whole wavefront;
@@ -66,7 +68,7 @@ __device__ __forceinline__ int few_find(const FewParams& fp, int row0, int s, in
                                         int& first) {
   first = 0;
   for (int b0 = 0; b0 < fp.batch; b0 += 64) {
-    const int n = b0 + lane < fp.batch ? few_stages(fp.a, b0 + lane, row0) : 0;
+    const int n = b0 + lane < fp.batch ? few_stages(fp, b0 + lane, row0) : 0;
     const int upto = lanes_up_to(n, 0, AddOp{});
     const uint64_t past = __ballot(first + upto > s);
     if (past) {
@@ -118,7 +120,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
     b = w, first = 0, from = 0, to = 1 << 30;
   }
   for (; b < fp.batch && from < to; ++b) {
-    const int n_stages = few_stages(p, b, row0);
+    const int n_stages = few_stages(fp, b, row0);
     if (n_stages == 0) {
       if (!fp.chunk) return;  // uniform, as the rest of the loop's conditions
       continue;
@@ -433,9 +435,9 @@ __global__ __launch_bounds__(512) void attn_paged_few_merge_kernel(FewParams fp,
   // first stage of the sequence in the line
   int before = 0;
   for (int b0 = 0; b0 < b; b0 += 64)
-    before += b0 + lane < b ? few_stages(p, b0 + lane, row0) : 0;
+    before += b0 + lane < b ? few_stages(fp, b0 + lane, row0) : 0;
   before = lanes_all(before, 0, AddOp{});
-  const int n = few_stages(p, b, row0);
+  const int n = few_stages(fp, b, row0);
   const int w0 = before / fp.chunk, w1 = (before + n - 1) / fp.chunk;
   if (n == 0 || w0 == w1) return;  // nothing here, or written out by its only workgroup
   const int bbeg = p.cu_block[b], G = p.group;

@@ -58,11 +58,13 @@ struct PageWindow {
 // ranges for every sequence as fill the chip when all are as long as the longest: 28/4 heads x 128,
 // 16 blocks of 32 to 256 rows behind 2000 to 16000, 576 -> 453 us; 8 of 20 to 100 behind 1000 to
 // 8000, 71 -> 60 us; 16/4 heads x 64, the same, 49 -> 32 us.  Equal lengths gain nothing (32 heads,
-// 1000 rows behind 3000: 89 and 91 us). With cap = 0 chunk is the host's; then either every sequence
-// counts as the longest, with as many row tiles, and many a workgroup may find nothing to do, or
-// (run > 0) the items are counted off, and a workgroup finds its own by a scan over the lengths.
+// 1000 rows behind 3000: 89 and 91 us). With cap = 0 chunk is the host's; then either every
+// sequence counts as the longest, with as many row tiles, and many a workgroup may find nothing to
+// do, or (run > 0) the items are counted off, and a workgroup finds its own by a scan over the
+// lengths.
 struct TilePlan {
   int batch, row_tiles;
+  int skip;  // sequences of at most this many query rows per K/V head have no items
   int cap;
   int chunk, nsplit;  // cap = 0: stages per range, ranges per sequence
   int run;            // > 0: items counted off, dealt to the XCDs in runs of so many
@@ -98,10 +100,11 @@ __device__ __forceinline__ int plan_parts(int j) {
   return j < 16 ? j + 1 : j < 24 ? 16 + 4 * (j - 15) : 48 + 16 * (j - 23);
 }
 
-// Where sequence b's items begin, in how many ranges, with how many row tiles.
-struct SequenceItems {
-  int first, ranges, row_tiles;
-};
+// Block rows of a sequence, as far as they have items here.
+__device__ __forceinline__ int tile_len(const AttnParams& p, const TilePlan& tp, int b) {
+  const int len = p.cu_block[b + 1] - p.cu_block[b];
+  return len * p.group > tp.skip ? len : 0;
+}
 
 // The lengths of a wave's sequences (lane = sequence) and the cut they get.
 struct LanePlan {
@@ -110,7 +113,7 @@ struct LanePlan {
 };
 __device__ __forceinline__ LanePlan lane_plan(const AttnParams& p, const TilePlan& tp, int lane) {
   const int own = min(lane, tp.batch - 1);
-  const int len = lane < tp.batch ? p.cu_block[own + 1] - p.cu_block[own] : 0;
+  const int len = lane < tp.batch ? tile_len(p, tp, own) : 0;
   const int stages = tile_stages(p.cu_prefix[own + 1] - p.cu_prefix[own], len);
   const int per_range = tile_rows(len, p.group) * p.hkv;
   const int longest = max(lanes_all(stages, 0, MaxOp{}), 1);
@@ -177,7 +180,7 @@ __device__ __forceinline__ bool count_off(const AttnParams& p, const TilePlan& t
   int first = 0, b = tp.batch, row_tiles = 1;
   for (int b0 = 0; b0 < tp.batch; b0 += 64) {
     const int own = min(b0 + lane, tp.batch - 1);
-    const int len = b0 + lane < tp.batch ? p.cu_block[own + 1] - p.cu_block[own] : 0;
+    const int len = b0 + lane < tp.batch ? tile_len(p, tp, own) : 0;
     const int stages = tile_stages(p.cu_prefix[own + 1] - p.cu_prefix[own], len);
     const int ranges = (stages + tp.chunk - 1) / tp.chunk, tiles = tile_rows(len, p.group);
     const int n = ranges * tiles * p.hkv;
@@ -213,8 +216,8 @@ __device__ __forceinline__ bool find_item(const AttnParams& p, const TilePlan& t
     it.b = unit / p.hkv / tp.nsplit;
     it.item = unit * tp.row_tiles + it.tile;
     if (it.b >= tp.batch) return false;
-    const int stages = tile_stages(p.cu_prefix[it.b + 1] - p.cu_prefix[it.b],
-                                   p.cu_block[it.b + 1] - p.cu_block[it.b]);
+    const int stages =
+        tile_stages(p.cu_prefix[it.b + 1] - p.cu_prefix[it.b], tile_len(p, tp, it.b));
     it.ranges = (stages + tp.chunk - 1) / tp.chunk;
     return it.range < it.ranges;
   }
@@ -1123,7 +1126,8 @@ __global__ __launch_bounds__(kThreads) void attn_tiles_merge_kernel(AttnParams p
   if (rh >= static_cast<long>(total) * p.hq) return;  // uniform per wavefront
   const int row = static_cast<int>(rh / p.hq), h = static_cast<int>(rh % p.hq);
   const int b = find_sequence(p.cu_block, tp.batch, row, lane);
-  const int len = p.cu_block[b + 1] - p.cu_block[b];
+  const int len = tile_len(p, tp, b);
+  if (len == 0) return;  // another launch's
   const int g = h / p.group, r = (row - p.cu_block[b]) * p.group + h % p.group;
   const int tile = r / kRowsPerWg;
   int first, ranges, row_tiles;

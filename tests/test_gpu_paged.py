@@ -343,7 +343,12 @@ def test_attention_plans(blocks, cached, hkv, group, cache, head_dim):
     ([1] * 80 + [300], [(53 * i) % 900 for i in range(81)], 1, 2),
     ([i % 4 for i in range(150)] + [500] + [2] * 130, [(91 * i) % 400 for i in range(281)], 4, 3),
     ([200, 70] + [1] * 2300, [40, 600] + [(7 * i) % 50 for i in range(2300)], 1, 2),
-    ([600] + [1] * 39, [1000] + [9 * i for i in range(39)], 32, 1)])
+    ([600] + [1] * 39, [1000] + [9 * i for i in range(39)], 32, 1),
+    # 8 bits: the short ones (of up to 16 and 32 rows per K/V head, some of more, some empty) in a
+    # launch of their own, of equal parts and whole
+    ([1, 0, 3, 9] * 20 + [150], [(191 * i) % 3000 + 700 for i in range(81)], 4, 3),
+    ([0, 5, 7, 2, 12] * 10 + [90], [(83 * i) % 4000 + 900 for i in range(51)], 3, 3),
+    ([1] * 2100 + [70], [(7 * i) % 90 + 80 for i in range(2101)], 2, 2)])
 def test_attention_mixed(blocks, cached, hkv, group, cache, head_dim):
     print(f"mixed {len(blocks)} {max(cached)} G={group} {cache} D={head_dim}", flush=True)
     _close(*_attention(blocks, cached, 16, cache, "bf16", group, head_dim, hkv=hkv), "bf16")
