@@ -145,12 +145,13 @@ eb_status eb_block_attn_dual(eb_dtype dt, const eb_ragged* r, const eb_suffix* s
  *   page_table        [batch, max_pages] i32; sequences may share pages that are only read
  *
  * A page number outside [0, n_pages) is no page: its rows read as zeros, and rows written to it
- * are dropped.  Table entries behind a sequence's last page are not read.
+ * are dropped.  What table entries behind a sequence's last page hold is of no account.
  *
  * Requires hkv >= 1, head_dim in {64, 128}, page_size in {16, 32, 64, 128, 256}, n_pages >= 1,
  * max_pages >= 1 and, where cached rows are read, max_prefix <= max_pages * page_size.  One write or
  * read moves at most 2^34 values of K.  An attention call takes at most 65535 sequences of at most
- * 2^30 keys, and hkv at most 65535 (EB_ERR_UNSUPPORTED beyond).
+ * 2^30 keys, hkv at most 65535, and what fits one launch of fewer than 2^32 threads
+ * (EB_ERR_UNSUPPORTED beyond).
  * With EB_DEBUG_CHECKS the page numbers that a call uses have to lie in [0, n_pages).
  * ------------------------------------------------------------------------------------- */
 typedef struct {
@@ -214,7 +215,7 @@ eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, voi
  * dt is EB_F32 (cache EB_F32 or EB_E4M3) or EB_BF16 (cache EB_BF16 or EB_E4M3).  hkv and head_dim
  * are the cache's; hq % hkv == 0; scale as in eb_block_attn.  Arithmetic as in eb_block_attn, on
  * the values that the cache stands for; scores of -inf weigh nothing.
- * ws: at least eb_block_attn_paged_workspace(...) bytes, contents ignored.
+ * ws: at least eb_block_attn_paged_workspace(...) bytes, 16-byte aligned, contents ignored.
  * ------------------------------------------------------------------------------------- */
 size_t eb_block_attn_paged_workspace(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv,
                                      int hq);

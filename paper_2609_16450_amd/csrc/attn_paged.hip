@@ -4,6 +4,8 @@
 // The cached rows are padded to whole stages, so that a stage lies either in the cache or in the
 // block and a piece of 16 keys in one page (page sizes are multiples of 16); keys of the padding
 // get scores of -inf and values of zero, whatever the page holds there.
+#include <algorithm>
+
 #include "attn_common.hpp"
 #include "attn_paged_few.hpp"
 #include "attn_tiles.hpp"
@@ -243,7 +245,7 @@ SplitPlan f32_plan(const PagedAttnArgs& a) {
   const long base = tiles * a.kv.hkv * a.batch;
   const int keys = (a.max_prefix + kPf32Keys - 1) / kPf32Keys * kPf32Keys + a.max_block;
   const long stages = (keys + kPf32Stage - 1) / kPf32Stage;
-  const long want = stages <= 4 ? 1 : max(1L, min((256 + base - 1) / base, stages));
+  const long want = stages <= 4 ? 1 : std::max(1L, std::min((256 + base - 1) / base, stages));
   const long per = (stages + want - 1) / want;
   return SplitPlan{static_cast<int>((stages + per - 1) / per), static_cast<int>(per * kPf32Stage)};
 }
@@ -290,8 +292,7 @@ constexpr int kFewWhole = 5;
 // goes by the mean of all but the longest, and by the cached rows, whether the launch can gain more
 // than it takes (16 tokens and a chunk of 256, 28/4 heads: 42 us in one, 50 in two).
 constexpr long kFewWorth = 4096;  // cached stages of 64 rows, over the K/V heads
-long few_rows(bool bf16, const PagedAttnArgs& a) {
-  if (!bf16) return 0;
+long few_rows(const PagedAttnArgs& a) {
   const bool e4m3 = a.kv.type == CacheType::kE4m3;
   const long group = a.hq / a.kv.hkv, rows = a.max_block * group;
   if (rows <= (e4m3 ? kFewRowsE4m3 : kFewRowsBf16)) return rows;
@@ -326,7 +327,7 @@ FewPlan few_plan(const PagedAttnArgs& a, long rows) {
     return f;
   }
   // stages of a line, at most
-  const long most = min(a.total_prefix / kFewStage + 2L * a.batch,
+  const long most = std::min(a.total_prefix / kFewStage + 2L * a.batch,
                         a.batch * ((a.max_prefix + kFewStage - 1L) / kFewStage + 1));
   const long chunk = (most * lines + kAttnTargetWgs - 1) / kAttnTargetWgs;
   const long longest = (a.max_prefix + kFewStage - 1L) / kFewStage + 1;
@@ -406,8 +407,8 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a, long skip) {
   const long stages = (a.max_prefix + kKeys - 1L) / kKeys + (a.max_block + kKeys - 1) / kKeys;
   // items of whole sequences, at most
   const long rows = a.total_block * group;
-  const long sequences = min(static_cast<long>(a.batch), rows / (skip + 1));
-  const long whole = hkv * min(sequences * row_tiles, rows / kRowsPerWg + sequences);
+  const long sequences = std::min(static_cast<long>(a.batch), rows / (skip + 1));
+  const long whole = hkv * std::min(sequences * row_tiles, rows / kRowsPerWg + sequences);
   TilesLaunch t{};
   t.plan.batch = a.batch;
   t.plan.row_tiles = static_cast<int>(row_tiles);
@@ -422,18 +423,18 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a, long skip) {
   const long all = row_tiles * hkv * a.batch;
   const bool counted = all * kCountBatch > whole * (kCountBatch + a.batch);
   // items of whole sequences as they are likely to be (few_rows skips short ones, not knowing them)
-  const long likely = skip ? min(whole, hkv * (rows / kRowsPerWg + 1)) : whole;
+  const long likely = skip ? std::min(whole, hkv * (rows / kRowsPerWg + 1)) : whole;
   const long base = counted ? likely : all;
   // (to the nearest: 400 sequences whole 89 us, halved 97; 280 of them 82 and 68, 16/4 heads x 64)
-  const long want =
-      stages <= kWholeStages ? 1 : max(1L, min((kAttnTargetWgs + base / 2) / base, stages));
+  const long most = std::max(1L, std::min((kAttnTargetWgs + base / 2) / base, stages));
+  const long want = stages <= kWholeStages ? 1 : most;
   const long chunk = (stages + want - 1) / want;
   t.plan.chunk = static_cast<int>(chunk);
   t.plan.nsplit = static_cast<int>((stages + chunk - 1) / chunk);
   if (counted) {
     const long items = whole * t.plan.nsplit;
     const long run =
-        max(1L, min(row_tiles, likely * t.plan.nsplit / (kXcdCount * kCountTurns)));
+        std::max(1L, std::min(row_tiles, likely * t.plan.nsplit / (kXcdCount * kCountTurns)));
     t.plan.run = static_cast<int>(run);
     t.grid = kXcdCount * run * ((items + kXcdCount * run - 1) / (kXcdCount * run));
   } else {
@@ -471,16 +472,37 @@ hipError_t launch_tiles(const PagedAttnArgs& a, long skip, void* ws, hipStream_t
 
 }  // namespace
 
+long attn_paged_threads(bool bf16, const PagedAttnArgs& a) {
+  if (a.total_block == 0 || a.max_block == 0) return 0;
+  const long group = a.hq / a.kv.hkv, rows = a.max_block * group;
+  const long merge = static_cast<long>(a.total_block) * a.hq * 64;  // a wave per query row
+  if (!bf16) {
+    const SplitPlan sp = f32_plan(a);
+    const long tiles = (rows + kPf32Rows - 1) / kPf32Rows;
+    return std::max(tiles * sp.nsplit * kPf32Waves * 64, sp.nsplit > 1 ? merge : 0);
+  }
+  long most = 0;
+  const long few = few_rows(a);
+  if (few > 0) {
+    const FewPlan f = few_plan(a, few);
+    most = std::max((static_cast<long>(f.groups) * a.kv.hkv + 7) * f.row_tiles * kFewWaves * 64,
+               f.slots ? static_cast<long>(a.batch) * a.kv.hkv * f.row_tiles * 512 : 0);
+    if (few == rows) return most;
+  }
+  const TilesLaunch t = tiles_plan(a, few);
+  return std::max(most, std::max(t.grid * kThreads, t.parts ? merge : 0));
+}
+
 size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
   if (a.total_block == 0 || a.max_block == 0) return 0;
   if (bf16) {  // one launch after the other, in the same memory
-    const long few = few_rows(bf16, a);
+    const long few = few_rows(a);
     const size_t row = (a.kv.head_dim + 2) * sizeof(float);
     const size_t bytes = few ? few_plan(a, few).slots * row : 0;
     if (few == static_cast<long>(a.max_block) * (a.hq / a.kv.hkv)) return bytes;
     const TilesLaunch t = tiles_plan(a, few);
     const size_t found = t.plan.cap ? 2 * kPlanMaxBatch : t.plan.run ? a.batch : 0;
-    return max(bytes, t.parts * kRowsPerWg * row + found * sizeof(int32_t));
+    return std::max(bytes, t.parts * kRowsPerWg * row + found * sizeof(int32_t));
   }
   const SplitPlan sp = f32_plan(a);
   if (sp.nsplit == 1) return 0;
@@ -495,7 +517,7 @@ hipError_t attn_paged(bool bf16, const PagedAttnArgs& a, void* ws, hipStream_t s
     if (d128) return e4m3 ? launch_f32<128, uint8_t>(a, ws, s) : launch_f32<128, float>(a, ws, s);
     return e4m3 ? launch_f32<64, uint8_t>(a, ws, s) : launch_f32<64, float>(a, ws, s);
   }
-  const long few = few_rows(bf16, a);
+  const long few = few_rows(a);
   if (few > 0) {
     const hipError_t e =
         d128 ? launch_few_any<128>(a, few, ws, s) : launch_few_any<64>(a, few, ws, s);

@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -205,9 +206,21 @@ bool debug_checks() {
   return v && *v && strcmp(v, "0") != 0;
 }
 
+// Host memory for n elements (a page table may be larger than that); nothing is thrown.
+template <class T>
+eb_status room(std::vector<T>& h, size_t n) {
+  try {
+    h.resize(n);
+  } catch (const std::exception&) {
+    return fail(EB_ERR_INVALID, "debug checks: no host memory for %zu elements", n);
+  }
+  return EB_OK;
+}
+
 template <class T>
 eb_status fetch(std::vector<T>& h, const T* d, size_t n, hipStream_t s) {
-  h.resize(n);
+  const eb_status st = room(h, n);
+  if (st != EB_OK) return st;
   hipError_t e = hipMemcpyAsync(h.data(), d, sizeof(T) * n, hipMemcpyDeviceToHost, s);
   if (e == hipSuccess) e = hipStreamSynchronize(s);
   return e == hipSuccess ? EB_OK : fail(EB_ERR_HIP, "debug check copy: %s", hipGetErrorString(e));
@@ -254,7 +267,7 @@ eb_status check_device(const eb_ragged* r, bool need_prefix, const float* tau, h
   return st;
 }
 
-// The pages that hold the first lens[b] positions of each sequence b have numbers in range.
+// The pages that hold the first n positions of sequence b have numbers in range.
 eb_status check_pages(const eb_paged_kv* kv, const std::vector<int32_t>& table, int b, int64_t n) {
   for (int64_t j = 0; j * kv->page_size < n; ++j) {
     const int32_t page = table[static_cast<size_t>(b) * kv->max_pages + j];
@@ -288,8 +301,10 @@ eb_status check_written(const eb_ragged* r, const eb_paged_kv* kv, const int32_t
   if (st == EB_OK && !pos) st = fetch(cp, r->cu_prefix, r->batch + 1, s);
   if (st == EB_OK && pos) st = fetch(at, pos, r->total_block, s);
   if (st == EB_OK) st = fetch_table(table, r, kv, s);
-  if (st != EB_OK) return st;
   std::vector<int64_t> rows;
+  if (st == EB_OK) st = room(rows, r->total_block);
+  if (st != EB_OK) return st;
+  size_t n = 0;
   for (int b = 0; b < r->batch; ++b)
     for (int i = cb[b]; i < cb[b + 1]; ++i) {
       const int64_t p = pos ? at[i] : static_cast<int64_t>(cp[b + 1]) - cp[b] + i - cb[b];
@@ -302,8 +317,9 @@ eb_status check_written(const eb_ragged* r, const eb_paged_kv* kv, const int32_t
       if (page < 0 || page >= kv->n_pages)
         return fail(EB_ERR_INVALID, "page_table[%d][%lld] = %d is not in [0, %d)", b, (long long)j,
                     page, kv->n_pages);
-      rows.push_back(static_cast<int64_t>(page) * kv->page_size + p % kv->page_size);
+      rows[n++] = static_cast<int64_t>(page) * kv->page_size + p % kv->page_size;
     }
+  rows.resize(n);
   std::sort(rows.begin(), rows.end());
   const auto twice = std::adjacent_find(rows.begin(), rows.end());
   if (twice != rows.end())
@@ -515,15 +531,20 @@ eb_status eb_block_attn_paged(eb_dtype dt, const eb_ragged* r, const eb_paged_kv
   if (r->batch > kMaxGridYZ || static_cast<int64_t>(r->max_prefix) + r->max_block > kMaxKeys)
     return fail(EB_ERR_UNSUPPORTED, "more than %d sequences or %d keys of a sequence", kMaxGridYZ,
                 kMaxKeys);
-  const size_t need = eb_block_attn_paged_workspace(dt, r, kv, hq);
-  if (ws_bytes < need || (need && !ws))
-    return fail(EB_ERR_WORKSPACE, "attention workspace %zu bytes < required %zu", ws_bytes, need);
-  st = check_device(r, true, nullptr, stream);
-  if (st == EB_OK && debug_checks()) st = check_cached_pages(r, kv, stream);
-  if (st != EB_OK) return st;
   const eb::PagedAttnArgs a{r->batch, r->total_block, r->max_block, r->total_prefix,
                             r->max_prefix, r->cu_block, r->cu_prefix, paged_args(kv), hq, scale,
                             q, k_blk, v_blk, out};
+  if (eb::attn_paged_threads(dt == EB_BF16, a) > UINT32_MAX)
+    return fail(EB_ERR_UNSUPPORTED, "%d block rows (at most %d of a sequence) x %d heads over %d "
+                "sequences do not fit one launch", r->total_block, r->max_block, hq, r->batch);
+  const size_t need = eb_block_attn_paged_workspace(dt, r, kv, hq);
+  if (ws_bytes < need || (need && !ws))
+    return fail(EB_ERR_WORKSPACE, "attention workspace %zu bytes < required %zu", ws_bytes, need);
+  if (need && !aligned16(ws))
+    return fail(EB_ERR_INVALID, "the attention workspace must be 16-byte aligned");
+  st = check_device(r, true, nullptr, stream);
+  if (st == EB_OK && debug_checks()) st = check_cached_pages(r, kv, stream);
+  if (st != EB_OK) return st;
   return hip_status(eb::attn_paged(dt == EB_BF16, a, ws, stream), "eb_block_attn_paged launch");
 }
 

@@ -78,6 +78,8 @@ struct PagedAttnArgs {
   const void *q, *k_blk, *v_blk;
   void* out;
 };
+// Threads of the call's largest launch (a grid's first dimension; one has fewer than 2^32).
+long attn_paged_threads(bool bf16, const PagedAttnArgs& a);
 size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a);
 hipError_t attn_paged(bool bf16, const PagedAttnArgs& a, void* ws, hipStream_t s);
 

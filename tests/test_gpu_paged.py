@@ -508,6 +508,26 @@ def test_long_pool():
 # --------------------------------------------------------------------------------------------
 # as they are used
 # --------------------------------------------------------------------------------------------
+def test_long_line():
+    """One context of 2^27 keys among 2047 empty ones: as many stages, counted for every sequence,
+    as pass 31 bits.  None of its rows has a page, so all weights are 1 and all values but the
+    block's own are zero."""
+    keys, batch = 1 << 27, 2048
+    table = torch.full((batch, keys // 256), -1, dtype=torch.int32, device="cuda")
+    kv = PagedKV.empty(1, 1, 256, 64, table, TYPES["e4m3"])
+    for t in (kv.k, kv.v, kv.k_scale, kv.v_scale):
+        t.view(torch.uint8).fill_(0xFF)
+    r = Ragged.from_lengths([1] * batch, [0] * 1000 + [keys] + [0] * 1047)
+    q = torch.zeros(batch, 1, 64, dtype=torch.bfloat16, device="cuda")
+    v = torch.from_numpy(np.random.default_rng(0).standard_normal((batch, 1, 64))).bfloat16().cuda()
+    out = torch.full_like(q, 7.0)
+    eb_block_attn_paged(r, kv, q, q, v, out)
+    want = v.double()
+    want[1000] /= keys + 1
+    # the output's rounding, and some of the sum's and the division's in fp32
+    assert ((out.double() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -18)).all()
+
+
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 def test_decoding_run(cache):
     """Blocks decoded one after another: attention over the pages, the block into the pages, and so

@@ -113,6 +113,27 @@ def test_workspace():
     assert lib.eb_block_attn_paged_workspace(B.EB_BF16, ctypes.byref(r), None, 4) == 0
 
 
+def test_workspace_alignment():
+    kv = _kv(max_pages=1 << 12, n_pages=1 << 12)
+    long = _ragged(S=60000, maxp=60000)
+    assert _attn(long, kv, ws=0x108, n=1 << 30) == B.EB_ERR_INVALID
+    assert "workspace" in B.eb_last_error()
+
+
+def test_too_much_for_one_launch():
+    """Grids of 2^32 threads and more, each kernel's own."""
+    kv = _kv(max_pages=1 << 12, n_pages=1 << 12, hkv=1 << 10)
+    rows = dict(S=0, maxp=0)
+    heads = dict(hq=1 << 10)
+    # 65000 sequences x 1024 heads of single tokens; many more rows of one head
+    assert _attn(_ragged(65000, 65000, 1, **rows), kv, **heads) == B.EB_ERR_UNSUPPORTED
+    assert "launch" in B.eb_last_error()
+    assert _attn(_ragged(60000, 1 << 28, 1 << 14, **rows), kv, **heads) == B.EB_ERR_UNSUPPORTED
+    # the tiles of the longest block for every sequence, in fp32
+    kv = _kv(dtype=B.EB_F32, hkv=1)
+    assert _attn(_ragged(1, 1 << 29, 1 << 29, **rows), kv, B.EB_F32, hq=1) == B.EB_ERR_UNSUPPORTED
+
+
 def test_too_much_for_one_call():
     kv = _kv(max_pages=1 << 27, n_pages=1 << 27)
     many = _ragged(T=1 << 28, maxb=1, S=1 << 28, maxp=1)
