@@ -348,7 +348,7 @@ class PagedKV:
     k, v: [n_pages, hkv, page_size, head_dim], float32, bfloat16 or float8_e4m3fn; the last with
     k_scale, v_scale: uint8 [n_pages, hkv, page_size].  page_table: int32 [batch, max_pages].  The
     tensors are checked once, here; they are kept, not copied, so that their contents (the table's
-    too) may change between calls.
+    too) may change between calls.  Other tensors take a new PagedKV: attributes are fixed.
     """
 
     def __init__(self, k, v, page_table, k_scale=None, v_scale=None):
@@ -378,6 +378,11 @@ class PagedKV:
                               self.max_pages, page_table.data_ptr(), k.data_ptr(), v.data_ptr(),
                               _ptr(k_scale), _ptr(v_scale))
         self._ref = ctypes.byref(self._c)
+
+    def __setattr__(self, name, value):
+        if hasattr(self, "_ref"):  # the library has the tensors' addresses already
+            raise AttributeError(f"{name}: a PagedKV's attributes are fixed")
+        super().__setattr__(name, value)
 
     @staticmethod
     def empty(n_pages: int, hkv: int, page_size: int, head_dim: int, page_table: torch.Tensor,

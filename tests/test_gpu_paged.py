@@ -672,6 +672,8 @@ def test_binding_refusals():
         PagedKV(c.kv.k, c.kv.v, c.kv.page_table, k_scale=torch.zeros(1))
     with pytest.raises(TypeError):
         eb_kv_write(r, c.kv.k, k, k)
+    with pytest.raises(AttributeError, match="fixed"):
+        c.kv.page_table = torch.zeros(1, 3, dtype=torch.int32, device="cuda")
 
 
 def test_debug_checks(monkeypatch):
