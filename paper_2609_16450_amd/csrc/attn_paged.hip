@@ -501,7 +501,7 @@ size_t attn_paged_ws_bytes(bool bf16, const PagedAttnArgs& a) {
     const size_t bytes = few ? few_plan(a, few).slots * row : 0;
     if (few == static_cast<long>(a.max_block) * (a.hq / a.kv.hkv)) return bytes;
     const TilesLaunch t = tiles_plan(a, few);
-    const size_t found = t.plan.cap ? 2 * kPlanMaxBatch : t.plan.run ? a.batch : 0;
+    const size_t found = t.plan.cap ? kFoundPlan : t.plan.run ? a.batch : 0;
     return std::max(bytes, t.parts * kRowsPerWg * row + found * sizeof(int32_t));
   }
   const SplitPlan sp = f32_plan(a);

@@ -58,10 +58,16 @@ struct PageWindow {
 // ranges for every sequence as fill the chip when all are as long as the longest: 28/4 heads x 128,
 // 16 blocks of 32 to 256 rows behind 2000 to 16000, 576 -> 453 us; 8 of 20 to 100 behind 1000 to
 // 8000, 71 -> 60 us; 16/4 heads x 64, the same, 49 -> 32 us.  Equal lengths gain nothing (32 heads,
-// 1000 rows behind 3000: 89 and 91 us). With cap = 0 chunk is the host's; then either every
-// sequence counts as the longest, with as many row tiles, and many a workgroup may find nothing to
-// do, or (run > 0) the items are counted off, and a workgroup finds its own by a scan over the
-// lengths.
+// 1000 rows behind 3000: 89 and 91 us).  Where whole sequences make more than one round of
+// workgroups, the alternative is to leave those of the full rounds whole, and to cut the few of the
+// last round into as many ranges as make it full: few partials, and no round half empty.  A chunk
+// of 2500 rows behind 8000, 28/4 heads, 440 -> 369 us; 2 of 1000 to 2048 behind 7001 to 12000
+// 507 -> 458 us; 18 blocks of 100 to 128 behind 1500, 32 heads, 8 bits, 142 -> 115 us; taken always,
+// unlike lengths suffer (5 of 300 to 500 behind 500 to 9000, 32 heads: 211 against 282 us), so the
+// costs decide here too.
+// With cap = 0 chunk is the host's; then either every sequence counts as the longest, with as many
+// row tiles, and many a workgroup may find nothing to do, or (run > 0) the items are counted off,
+// and a workgroup finds its own by a scan over the lengths.
 struct TilePlan {
   int batch, row_tiles;
   int skip;  // sequences of at most this many query rows per K/V head have no items
@@ -71,8 +77,8 @@ struct TilePlan {
   float* o_part;      // [items, kRowsPerWg, D], then m and l [items, kRowsPerWg]
   float* m_part;
   float* l_part;
-  // cap > 0: of each of kPlanMaxBatch sequences its first item, then its ranges; run > 0: of each
-  // sequence with more than one range its first item
+  // cap > 0: of each of kPlanMaxBatch sequences its first item, then its ranges, then a LastRound;
+  // run > 0: of each sequence with more than one range its first item
   int32_t* found;
 };
 template <bool kBits8>
@@ -106,10 +112,18 @@ __device__ __forceinline__ int tile_len(const AttnParams& p, const TilePlan& tp,
   return len * p.group > tp.skip ? len : 0;
 }
 
+// More items than one round has workgroups: the first `full` stay whole, each of the `rest` behind
+// them is cut into (at most) `ranges`.
+struct LastRound {
+  int full, rest, ranges;
+};
+constexpr int kFoundPlan = 2 * kPlanMaxBatch + sizeof(LastRound) / sizeof(int);
 // The lengths of a wave's sequences (lane = sequence) and the cut they get.
 struct LanePlan {
   int ranges, items, upto;  // of the lane's sequence; upto: items of all up to it
   int total;
+  int stages;
+  LastRound last;  // full > 0: in place of the sequences' ranges
 };
 __device__ __forceinline__ LanePlan lane_plan(const AttnParams& p, const TilePlan& tp, int lane) {
   const int own = min(lane, tp.batch - 1);
@@ -153,6 +167,18 @@ __device__ __forceinline__ LanePlan lane_plan(const AttnParams& p, const TilePla
     l.total = __builtin_amdgcn_readlane(l.upto, 63);
   };
   cut(chunk);
+  l.stages = stages;
+  l.last = LastRound{};
+  if (whole > kAttnTargetWgs) {
+    const int full = whole / kAttnTargetWgs, rest = whole - full * kAttnTargetWgs;
+    const int ranges = max(kAttnTargetWgs / max(rest, 1), 1);
+    const float last = static_cast<float>(longest) / ranges + kPlanRange + kPlanMerge +
+                       kAttnTargetWgs * kRowsPerWg * kPlanRow;
+    if (full * (longest + kPlanRange) + (rest ? last : 0.f) < __int_as_float(least)) {
+      cut(longest);
+      l.last = LastRound{full * kAttnTargetWgs, rest, ranges};
+    }
+  }
   if (l.total > tp.cap) cut(longest);  // (a count in floats was off: whole sequences always fit)
   return l;
 }
@@ -225,23 +251,41 @@ __device__ __forceinline__ bool find_item(const AttnParams& p, const TilePlan& t
   // the longest block has row tiles, for the sharing.  turns divides 64, so that an XCD gets no
   // more items than its share of the cap.
   const LanePlan l = lane_plan(p, tp, lane);
-  int turns = 1;
-  while (turns < 64 && 2 * turns * kXcdCount * tp.row_tiles <= l.total) turns *= 2;
-  const int runs = turns * kXcdCount, most = (l.total + runs - 1) / runs;
-  const int run = j / most * kXcdCount + xcd;
-  it.item = run * l.total / runs + j % most;
-  if (run >= runs || it.item >= (run + 1) * l.total / runs) return false;
-  if (it.item == 0 && wave == 0) {  // for the merge
+  const LastRound last = l.last;
+  if (blockIdx.x == 0 && wave == 0) {  // for the merge
     tp.found[lane] = l.upto - l.items;
     tp.found[kPlanMaxBatch + lane] = l.ranges;
+    if (lane == 0) *reinterpret_cast<LastRound*>(tp.found + 2 * kPlanMaxBatch) = last;
   }
-  const int b = __builtin_ctzll(__ballot(l.upto > it.item));
-  const int local = it.item - __builtin_amdgcn_readlane(l.upto - l.items, b);
+  // (the full rounds by themselves, in runs of a power of two of items, 64 at most, as an XCD has
+  // 64 workgroups at a time)
+  const int in_full = last.full / kXcdCount, at = j - in_full;
+  const int total = last.full ? last.rest * last.ranges : l.total;
+  if (at < 0) {
+    int run = 64;
+    while (run >= 2 * tp.row_tiles) run /= 2;
+    it.item = (j / run * kXcdCount + xcd) * run + j % run;
+  } else {
+    int turns = 1;
+    while (turns < 64 && 2 * turns * kXcdCount * tp.row_tiles <= total) turns *= 2;
+    const int runs = turns * kXcdCount, most = max((total + runs - 1) / runs, 1);
+    const int run = at / most * kXcdCount + xcd;
+    const int n = run * total / runs + at % most;
+    if (run >= runs || n >= (run + 1) * total / runs) return false;
+    it.item = last.full + n;
+  }
+  const int whole = at < 0 || !last.full ? it.item : last.full + (it.item - last.full) % last.rest;
+  const int b = __builtin_ctzll(__ballot(l.upto > whole));
+  const int local = whole - __builtin_amdgcn_readlane(l.upto - l.items, b);
   const int row_tiles = tile_rows(p.cu_block[b + 1] - p.cu_block[b], p.group);
   it.b = b;
   place_item(it, local, row_tiles, p.hkv);
   it.ranges = __builtin_amdgcn_readlane(l.ranges, b);
-  return true;
+  if (at >= 0 && last.full) {
+    it.range = (it.item - last.full) / last.rest;
+    it.ranges = min(last.ranges, __builtin_amdgcn_readlane(l.stages, b));
+  }
+  return it.range < it.ranges;
 }
 
 // Two workgroups per compute unit (<= 256 VGPRs per lane, no spills at D = 128), so one
@@ -1133,20 +1177,29 @@ __global__ __launch_bounds__(kThreads) void attn_tiles_merge_kernel(AttnParams p
   if (len == 0) return;  // another launch's
   const int g = h / p.group, r = (row - p.cu_block[b]) * p.group + h % p.group;
   const int tile = r / kRowsPerWg;
+  const int stages = tile_stages(p.cu_prefix[b + 1] - p.cu_prefix[b], len);
   int first, ranges, row_tiles;
+  long step;  // between partials
   if (tp.cap > 0) {
     first = tp.found[b];
     ranges = tp.found[kPlanMaxBatch + b];
     row_tiles = tile_rows(len, p.group);
+    const LastRound last = *reinterpret_cast<const LastRound*>(tp.found + 2 * kPlanMaxBatch);
+    step = p.hkv * row_tiles;
+    if (last.full && first + g * row_tiles + tile >= last.full) {
+      ranges = min(last.ranges, stages);
+      step = last.rest;
+    }
   } else {
-    ranges = (tile_stages(p.cu_prefix[b + 1] - p.cu_prefix[b], len) + tp.chunk - 1) / tp.chunk;
+    ranges = (stages + tp.chunk - 1) / tp.chunk;
     row_tiles = tp.run > 0 ? tile_rows(len, p.group) : tp.row_tiles;
     first = tp.run == 0 ? b * tp.nsplit * p.hkv * row_tiles : ranges > 1 ? tp.found[b] : 0;
+    step = p.hkv * row_tiles;
   }
   if (ranges <= 1) return;  // written out by its only workgroup
+  const long item = first + g * row_tiles + tile;
   auto at = [&](int k) {
-    return (first + (static_cast<size_t>(k) * p.hkv + g) * row_tiles + tile) * kRowsPerWg +
-           r % kRowsPerWg;
+    return static_cast<size_t>(item + k * step) * kRowsPerWg + r % kRowsPerWg;
   };
   const PartialRow<D> x = merge_partials<D>(at, ranges, tp.o_part, tp.m_part, tp.l_part, lane);
   x.store(p.out + rh * D, lane);

@@ -328,6 +328,11 @@ def test_attention_many_sequences(cache, dtype):
     ([34 + i % 3 * (i % 7 > 0) - 34 * (i == 9) for i in range(70)],
      [(53 * i) % 900 for i in range(70)], 1, 2),
     ([33 + i % 9 for i in range(58)], [1030 + 3 * i for i in range(58)], 16, 1),
+    # somewhat more items than workgroups that run at a time: the last ones cut, into more ranges
+    # than the shortest has stages; row tiles of one block on both sides
+    ([33 + i % 9 for i in range(40)], [1030 - 26 * i for i in range(40)], 16, 1),
+    ([34] * 33, [640 + 11 * i for i in range(33)], 16, 1),
+    ([300, 0, 200, 60], [700, 9, 300, 1500], 4, 32),
     ([70, 0, 66, 90, 65], [5000, 77, 10, 700, 0], 2, 3),
     ([777], [1500], 1, 2)])
 def test_attention_plans(blocks, cached, hkv, group, cache, head_dim):
