@@ -62,9 +62,9 @@ struct PageWindow {
 // workgroups, the alternative is to leave those of the full rounds whole, and to cut the few of the
 // last round into as many ranges as make it full: few partials, and no round half empty.  A chunk
 // of 2500 rows behind 8000, 28/4 heads, 440 -> 369 us; 2 of 1000 to 2048 behind 7001 to 12000
-// 507 -> 458 us; 18 blocks of 100 to 128 behind 1500, 32 heads, 8 bits, 142 -> 115 us; taken always,
-// unlike lengths suffer (5 of 300 to 500 behind 500 to 9000, 32 heads: 211 against 282 us), so the
-// costs decide here too.
+// 507 -> 458 us; 18 blocks of 100 to 128 behind 1500, 32 heads, 8 bits, 142 -> 115 us; taken
+// always, unlike lengths suffer (5 of 300 to 500 behind 500 to 9000, 32 heads: 211 against 282 us),
+// so the costs decide here too.
 // With cap = 0 chunk is the host's; then either every sequence counts as the longest, with as many
 // row tiles, and many a workgroup may find nothing to do, or (run > 0) the items are counted off,
 // and a workgroup finds its own by a scan over the lengths.
@@ -889,9 +889,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
   // Tiles of an 8-bit cache go through registers: fetch() loads this wave's half of a tile (four
   // loads of 16 bytes per lane, 8 rows each, and the scales of the lane's two rows per group of
   // 16), an iteration later place() widens it to bf16, exactly, and stores it where the loads into
-  // LDS would have put it.  2 chunks of 1000 to 2048 rows behind 7001 to 12000, 28/4 heads: 537 us
-  // (0.82 PFLOP/s), over bf16 pages 502.  Widening in the slots of the S loop instead, with the
-  // next tile's loads behind it: 548 us, the loads then have half the time; a swap of halves
+  // LDS would have put it.  2 chunks of 1000 to 2048 rows behind 7001 to 12000, 28/4 heads: 506 us
+  // (0.87 PFLOP/s), over bf16 pages 444.  Widening in the slots of the S loop instead, with the
+  // next tile's loads behind it: 2% slower, the loads then have half the time; a swap of halves
   // between lanes that takes away the stores' bank conflicts: no change.
   constexpr int kRawLoads = 4;
   [[maybe_unused]] u32x4 raw[kRawLoads];
@@ -1163,46 +1163,44 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
     }
 }
 
-// The ranges of every (block row, query head) of a launch over pages, in key order: a wave per
-// pair, its lanes over partials side by side.
+// The ranges of every (block row, query head) of a launch over pages, in key order: a wave per row
+// and every `waves`-th head (neighbouring heads have one K/V head and are cut alike), its lanes over
+// a head's partials side by side.
 template <int D>
 __global__ __launch_bounds__(kThreads) void attn_tiles_merge_kernel(AttnParams p, TilePlan tp,
-                                                                    int total) {
+                                                                    int total, int waves) {
   const int lane = threadIdx.x & 63;
-  const long rh = static_cast<long>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
-  if (rh >= static_cast<long>(total) * p.hq) return;  // uniform per wavefront
-  const int row = static_cast<int>(rh / p.hq), h = static_cast<int>(rh % p.hq);
+  const long unit = static_cast<long>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  if (unit >= static_cast<long>(total) * waves) return;  // uniform per wavefront
+  const int row = static_cast<int>(unit / waves), h0 = static_cast<int>(unit % waves);
   const int b = find_sequence(p.cu_block, tp.batch, row, lane);
   const int len = tile_len(p, tp, b);
   if (len == 0) return;  // another launch's
-  const int g = h / p.group, r = (row - p.cu_block[b]) * p.group + h % p.group;
-  const int tile = r / kRowsPerWg;
   const int stages = tile_stages(p.cu_prefix[b + 1] - p.cu_prefix[b], len);
-  int first, ranges, row_tiles;
-  long step;  // between partials
+  LastRound last{};
+  int first, row_tiles = tile_rows(len, p.group), ranges;
   if (tp.cap > 0) {
     first = tp.found[b];
     ranges = tp.found[kPlanMaxBatch + b];
-    row_tiles = tile_rows(len, p.group);
-    const LastRound last = *reinterpret_cast<const LastRound*>(tp.found + 2 * kPlanMaxBatch);
-    step = p.hkv * row_tiles;
-    if (last.full && first + g * row_tiles + tile >= last.full) {
-      ranges = min(last.ranges, stages);
-      step = last.rest;
-    }
+    last = *reinterpret_cast<const LastRound*>(tp.found + 2 * kPlanMaxBatch);
   } else {
     ranges = (stages + tp.chunk - 1) / tp.chunk;
-    row_tiles = tp.run > 0 ? tile_rows(len, p.group) : tp.row_tiles;
+    if (tp.run == 0) row_tiles = tp.row_tiles;
     first = tp.run == 0 ? b * tp.nsplit * p.hkv * row_tiles : ranges > 1 ? tp.found[b] : 0;
-    step = p.hkv * row_tiles;
   }
-  if (ranges <= 1) return;  // written out by its only workgroup
-  const long item = first + g * row_tiles + tile;
-  auto at = [&](int k) {
-    return static_cast<size_t>(item + k * step) * kRowsPerWg + r % kRowsPerWg;
-  };
-  const PartialRow<D> x = merge_partials<D>(at, ranges, tp.o_part, tp.m_part, tp.l_part, lane);
-  x.store(p.out + rh * D, lane);
+  for (int h = h0; h < p.hq; h += waves) {
+    const int g = h / p.group, r = (row - p.cu_block[b]) * p.group + h % p.group;
+    const long item = first + g * row_tiles + r / kRowsPerWg;
+    const bool cut = last.full && item >= last.full;  // one of the last round
+    const int n = cut ? min(last.ranges, stages) : ranges;
+    const long step = cut ? last.rest : p.hkv * row_tiles;
+    if (n <= 1) continue;  // written out by its only workgroup
+    auto at = [&](int k) {
+      return static_cast<size_t>(item + k * step) * kRowsPerWg + r % kRowsPerWg;
+    };
+    const PartialRow<D> x = merge_partials<D>(at, n, tp.o_part, tp.m_part, tp.l_part, lane);
+    x.store(p.out + (static_cast<size_t>(row) * p.hq + h) * D, lane);
+  }
 }
 
 }  // namespace
