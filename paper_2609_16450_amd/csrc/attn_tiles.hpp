@@ -1164,8 +1164,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
 }
 
 // The ranges of every (block row, query head) of a launch over pages, in key order: a wave per row
-// and every `waves`-th head (neighbouring heads have one K/V head and are cut alike), its lanes over
-// a head's partials side by side.
+// and every `waves`-th head (neighbouring heads have one K/V head and are cut alike), its lanes
+// over a head's partials side by side.
 template <int D>
 __global__ __launch_bounds__(kThreads) void attn_tiles_merge_kernel(AttnParams p, TilePlan tp,
                                                                     int total, int waves) {

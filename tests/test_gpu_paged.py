@@ -596,7 +596,8 @@ def test_decoding_run(cache):
 
 
 @pytest.mark.parametrize("cache,dtype", COMBOS)
-@pytest.mark.parametrize("blocks,cached", [([1, 1, 1], [400, 60, 999]), ([33, 90], [500, 70])])
+@pytest.mark.parametrize("blocks,cached", [([1, 1, 1], [400, 60, 999]), ([33, 90], [500, 70]),
+                                           ([1] * 64 + [80], [2100] * 65)])
 def test_captured_and_replayed(blocks, cached, cache, dtype):
     """Write, attention and read captured into one graph, replayed with eager work in between; and
     every eager run gives the same bits."""
