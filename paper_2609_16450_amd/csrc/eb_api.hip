@@ -47,6 +47,9 @@ constexpr size_t kWsAlign = 256;
 constexpr int kMaxGridYZ = 65535;       // second and third dimension of a launch grid
 constexpr int kMaxKeys = 1 << 30;       // of one sequence
 constexpr int64_t kMaxPackedValues = 1LL << 34;  // of K in one launch of the cache kernels
+// Block rows x query heads: no attention kernel takes fewer than two threads for one, and a launch
+// has fewer than 2^32.
+constexpr int64_t kMaxQueryRows = 1LL << 31;
 constexpr int kProbeMaxGroups = 65536;
 constexpr int kProbeMaxIters = 1 << 20;
 size_t round_up(size_t n) { return (n + kWsAlign - 1) / kWsAlign * kWsAlign; }
@@ -183,6 +186,17 @@ eb_status check_rows(int32_t rows, const eb_paged_kv* kv) {
     return fail(EB_ERR_UNSUPPORTED, "%d rows of %d heads x %d in one call (at most 2^34 values)",
                 rows, kv->hkv, kv->head_dim);
   return EB_OK;
+}
+
+// Sizes that the plans of the attention over pages are made for; of others a call is refused and a
+// workspace query returns 0.  (In range, every count of theirs fits 64 bits and is at least 1.)
+bool paged_attn_sizes(const eb_ragged* r, const eb_paged_kv* kv, int hq) {
+  return r->batch >= 1 && r->batch <= kMaxGridYZ && r->max_block >= 0 &&
+         r->max_block <= r->total_block && r->max_prefix >= 0 && r->max_prefix <= r->total_prefix &&
+         static_cast<int64_t>(r->max_prefix) + r->max_block <= kMaxKeys && kv->hkv >= 1 &&
+         kv->hkv <= kMaxGridYZ && hq >= 1 && hq % kv->hkv == 0 &&
+         (kv->head_dim == 64 || kv->head_dim == 128) &&
+         static_cast<int64_t>(r->total_block) * hq <= kMaxQueryRows;
 }
 
 eb::PagedKv paged_args(const eb_paged_kv* kv) {
@@ -508,10 +522,7 @@ eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, voi
 
 size_t eb_block_attn_paged_workspace(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv,
                                      int hq) {
-  if (!r || !kv || r->batch < 1 || hq < 1 || kv->hkv < 1 || hq % kv->hkv || r->total_block <= 0 ||
-      r->max_block <= 0 || r->max_prefix < 0 ||
-      static_cast<int64_t>(r->max_prefix) + r->max_block > kMaxKeys)
-    return 0;
+  if (!r || !kv || !paged_attn_sizes(r, kv, hq)) return 0;
   eb::PagedAttnArgs a{r->batch, r->total_block, r->max_block, r->total_prefix, r->max_prefix,
                       r->cu_block, r->cu_prefix, paged_args(kv), hq, 1.f, nullptr, nullptr,
                       nullptr, nullptr};
@@ -534,7 +545,7 @@ eb_status eb_block_attn_paged(eb_dtype dt, const eb_ragged* r, const eb_paged_kv
   const eb::PagedAttnArgs a{r->batch, r->total_block, r->max_block, r->total_prefix,
                             r->max_prefix, r->cu_block, r->cu_prefix, paged_args(kv), hq, scale,
                             q, k_blk, v_blk, out};
-  if (eb::attn_paged_threads(dt == EB_BF16, a) > UINT32_MAX)
+  if (!paged_attn_sizes(r, kv, hq) || eb::attn_paged_threads(dt == EB_BF16, a) > UINT32_MAX)
     return fail(EB_ERR_UNSUPPORTED, "%d block rows (at most %d of a sequence) x %d heads over %d "
                 "sequences do not fit one launch", r->total_block, r->max_block, hq, r->batch);
   const size_t need = eb_block_attn_paged_workspace(dt, r, kv, hq);

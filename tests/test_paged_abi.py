@@ -1,10 +1,15 @@
 """Paged cache: bad arguments are refused on the host, before anything is launched."""
 import ctypes
+import pathlib
+import subprocess
+import sys
 
 import pytest
 import torch
 
 from paper_2609_16450_amd import binding as B
+
+ROOT = pathlib.Path(__file__).resolve().parents[1]
 
 
 def _ragged(batch=1, T=4, maxb=4, S=20, maxp=20, cu_b=0x1000, cu_p=0x2000):
@@ -111,6 +116,38 @@ def test_workspace():
     assert need(r, _kv(page_size=0x7fffffff)) >= 0
     assert lib.eb_block_attn_paged_workspace(B.EB_BF16, None, ctypes.byref(kv), 4) == 0
     assert lib.eb_block_attn_paged_workspace(B.EB_BF16, ctypes.byref(r), None, 4) == 0
+
+
+# (batch, rows, longest block, cached rows, longest prefix), query heads, K/V heads: a longest block
+# or prefix beyond the totals, negative totals, and sizes whose products pass 64 bits
+NO_BATCH = [((70, 1, 100, 1000000, 20000), 28, 4), ((1, 1, 1, -256, 5000), 28, 4),
+            ((1, 1, 1, 4000, 5000), 28, 4), ((3, -5, -5, 100, 100), 4, 4),
+            ((1, 4, 4, 100, -1), 4, 4)]
+TOO_LARGE = [((1, 1 << 29, 1 << 29, 0, 0), 1 << 30, 1), ((1, 1 << 30, 1 << 30, 0, 0), 1 << 30, 2),
+             ((65535, 1 << 30, 1 << 15, 0, 0), 0x7fffffff, 1)]
+
+
+def test_sizes_that_no_plan_is_made_for():
+    """The query returns 0 and the call is refused, before a plan divides or multiplies by them.  (In
+    a child process, which a division by zero would end.)"""
+    sizes = NO_BATCH + TOO_LARGE
+    types = [(B.EB_F32, B.EB_F32), (B.EB_F32, B.EB_E4M3), (B.EB_BF16, B.EB_BF16),
+             (B.EB_BF16, B.EB_E4M3)]
+    code = (f"import ctypes, sys; sys.path.insert(0, {str(ROOT)!r})\n"
+            "from paper_2609_16450_amd import binding as B\n"
+            f"B._LIB_PATH = {B._LIB_PATH!r}\n"
+            f"for size, hq, hkv in {sizes}:\n"
+            f"  for dt, cache in {types}:\n"
+            "    r = B.eb_ragged(*size, 0x1000, 0x2000)\n"
+            "    kv = B.eb_paged_kv(cache, hkv, 128, 1 << 20, 256, 1 << 22, 0x1000, 0x100, 0x200,"
+            " 0x300, 0x400)\n"
+            "    a = dt, ctypes.byref(r), ctypes.byref(kv), hq\n"
+            "    print(B.load().eb_block_attn_paged_workspace(*a), B.load().eb_block_attn_paged("
+            "*a, 0.1, 0x100, 0x100, 0x100, 0x100, None, 0, None), flush=True)\n")
+    res = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    want = [f"0 {B.EB_ERR_INVALID if s in NO_BATCH else B.EB_ERR_UNSUPPORTED}"
+            for s in sizes for _ in types]
+    assert (res.returncode, res.stdout.splitlines()) == (0, want), res.stderr[-500:]
 
 
 def test_workspace_alignment():
