@@ -214,7 +214,9 @@ eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, voi
  *
  * dt is EB_F32 (cache EB_F32 or EB_E4M3) or EB_BF16 (cache EB_BF16 or EB_E4M3).  hkv and head_dim
  * are the cache's; hq % hkv == 0; scale as in eb_block_attn.  Arithmetic as in eb_block_attn, on
- * the values that the cache stands for; scores of -inf weigh nothing.
+ * the values that the cache stands for; scores of -inf weigh nothing, but an infinity or NaN among
+ * the values (an 8-bit cache holds both as NaN) makes its column infinite or NaN in every row that
+ * sees it, whatever its weight.
  * ws: at least eb_block_attn_paged_workspace(...) bytes, 16-byte aligned, contents ignored.
  * ------------------------------------------------------------------------------------- */
 size_t eb_block_attn_paged_workspace(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv,

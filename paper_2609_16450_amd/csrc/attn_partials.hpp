@@ -20,11 +20,12 @@ struct PartialRow {
   }
 };
 
-// Rescaling by 2^d with d <= 0; what has lost all weight counts nothing, infinite values included.
+// Rescaling by 2^d with d <= 0.  An infinity or NaN stays one even where 2^d is zero, as it does in
+// the kernels' own accumulators, so that no cut of the keys makes its column finite.
 __device__ __forceinline__ void rescale(f32x4& x, float& l, float d) {
   const float f = fast_exp2(d);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = f == 0.f ? 0.f : x[e] * f;
+  for (int e = 0; e < 4; ++e) x[e] *= f;
   l *= f;
 }
 
@@ -52,7 +53,8 @@ __device__ __forceinline__ PartialRow<D> merge_partials_by(At at, int n, const f
     float M_new = M;
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      if (k0 + j * kSide + sub >= n) mk[j] = -INFINITY;
+      // no such partial (what was loaded is another's, and may be infinite)
+      if (k0 + j * kSide + sub >= n) mk[j] = -INFINITY, y[j] = f32x4{};
       M_new = fmaxf(M_new, mk[j]);
     }
     rescale(x, sum, M - M_new);
@@ -62,7 +64,7 @@ __device__ __forceinline__ PartialRow<D> merge_partials_by(At at, int n, const f
       const float f = fast_exp2(mk[j] - M);
       sum = fmaf(f, lk[j], sum);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = f == 0.f ? x[e] : fmaf(f, y[j][e], x[e]);
+      for (int e = 0; e < 4; ++e) x[e] = fmaf(f, y[j][e], x[e]);
     }
   }
   for (int d = kCols; d < 64; d <<= 1) {

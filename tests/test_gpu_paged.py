@@ -444,6 +444,26 @@ def test_attention_infinities(blocks, cache, dtype):
     np.testing.assert_array_equal(others, 1.0)
 
 
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("cache,dtype", COMBOS)
+@pytest.mark.parametrize("blocks,n", [(1, 3000), (20, 2500), (40, 900), (150, 1500), (150, 70)])
+def test_attention_infinities_without_weight(blocks, n, cache, dtype, head_dim):
+    """One key takes all of the softmax's weight in 32 bits; infinities (in 8 bits NaN) at keys
+    before and behind it, in its stage, in others and in other key ranges, still leave their columns
+    infinite or NaN, as 0 times infinity is, and no other column."""
+    print(f"weightless {blocks} {n} {cache} {dtype} D={head_dim}", flush=True)
+    d = head_dim
+    at = np.unique(np.linspace(0, n + blocks - 1, d // 2).astype(int))
+    for big in (1, n // 2, n - 1, n + blocks - 1):
+        q, k, v = np.zeros((blocks, 1, d)), np.zeros((n + blocks, 1, d)), np.ones((n + blocks, 1, d))
+        q[:, 0, 0] = 64.0
+        k[big, 0, 0] = 64.0           # a score of 362 or more; the others are 0 and expf(-362) is 0
+        v[at, 0, np.arange(len(at))] = np.inf
+        got = _handmade(cache, dtype, blocks, n, d, k[:n], v[:n], k[n:], v[n:], q)
+        assert not np.isfinite(got[..., :len(at)]).any(), big
+        np.testing.assert_array_equal(got[..., len(at):], 1.0)
+
+
 @pytest.mark.parametrize("cache,dtype", COMBOS)
 @pytest.mark.parametrize("blocks,cached,group", [([1, 1], [300, 20], 2), ([30, 60], [100, 700], 3)])
 def test_attention_rising_scores(blocks, cached, group, cache, dtype):
