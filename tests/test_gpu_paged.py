@@ -310,6 +310,70 @@ def test_attention_batches(blocks, cached, group, hkv, cache, dtype, head_dim):
     _close(*_attention(blocks, cached, 32, cache, dtype, group, head_dim, hkv=hkv), dtype)
 
 
+# Every key counts exactly once, however the keys are cut: with queries of zeros all weights are 1,
+# and with values of 1 in column (position + 7 head) % D of a window of positions, 0 elsewhere, a
+# column is a count of at most 32 keys over their number.  fp32 sums of whole numbers are exact; the
+# division and the output's rounding are off by at most 2^-8 + 2^-20 of the result, a lost or doubled
+# key by 2^-5.
+COUNTS = [
+    # few query rows: single sequences over many parts, ragged ones, sequences that stay whole
+    ([1], [9001], 2, 7), ([20, 1], [5000, 1], 3, 1),
+    ([1] * 64, [(509 * i) % 8192 for i in range(64)], 2, 3),
+    ([3, 0, 2] * 30, [(91 * i) % 300 for i in range(90)], 2, 7), ([32, 16], [2100, 4000], 2, 1),
+    # more: ranges by the workgroups, the last round cut, the host's ranges, counted items
+    ([300], [2500], 1, 2), ([70], [5000], 1, 1),
+    ([70, 0, 66, 90, 65], [5000, 77, 10, 700, 0], 2, 3),
+    ([33 + i % 9 for i in range(40)], [1030 - 26 * i for i in range(40)], 16, 1),
+    ([34 + i % 3 * (i % 7 > 0) - 34 * (i == 9) for i in range(70)],
+     [(53 * i) % 900 for i in range(70)], 1, 2),
+    ([i % 4 for i in range(150)] + [500] + [2] * 130, [(91 * i) % 400 for i in range(281)], 4, 3),
+    # 8 bits: two launches
+    ([1, 0, 3, 9] * 20 + [150], [(191 * i) % 3000 + 700 for i in range(81)], 4, 3)]
+
+
+@pytest.mark.parametrize("head_dim,page", [(64, 64), (128, 16)])
+@pytest.mark.parametrize("cache,dtype", [("bf16", "bf16"), ("e4m3", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("blocks,cached,hkv,group", COUNTS)
+def test_every_key_counts_once(blocks, cached, hkv, group, cache, dtype, head_dim, page):
+    print(f"count {len(blocks)} {max(cached)} G={group} {cache} D={head_dim}", flush=True)
+    c = Cache(cached, hkv, page, head_dim, cache, 14)
+    dt, S, T = TYPES[dtype], sum(cached), sum(blocks)
+    g = torch.Generator(device="cuda").manual_seed(len(blocks))
+
+    def places(lens, first):
+        """Sequence and position of packed rows that begin at first[b] of their sequences."""
+        lens, first = (torch.tensor(x, device="cuda") for x in (lens, first))
+        seq = torch.repeat_interleave(torch.arange(len(lens), device="cuda"), lens)
+        at = torch.arange(len(seq), device="cuda") - (torch.cumsum(lens, 0) - lens)[seq]
+        return seq, at + first[seq]
+
+    seq_s, pos_s = places(cached, [0] * len(cached))
+    seq_t, pos_t = places(blocks, cached)
+    head = torch.arange(hkv, device="cuda")
+
+    def values(pos, lo, hi):
+        col = ((pos[:, None] + 7 * head) % head_dim)[..., None]
+        one = ((pos >= lo) & (pos < hi)).float()[:, None, None].expand(-1, hkv, 1)
+        return torch.zeros(len(pos), hkv, head_dim, device="cuda").scatter_(2, col, one)
+
+    k_s, k_t = (torch.randn(n, hkv, head_dim, generator=g, device="cuda").to(dt) for n in (S, T))
+    q = torch.zeros(T, hkv * group, head_dim, dtype=dt, device="cuda")
+    keys = (torch.tensor(blocks, device="cuda") + torch.tensor(cached, device="cuda")).double()
+    r, window = Ragged.from_lengths(blocks, cached), 32 * head_dim
+    for lo in range(0, int(keys.max()), window):
+        v_s, v_t = values(pos_s, lo, lo + window), values(pos_t, lo, lo + window)
+        eb_kv_write(Ragged.from_lengths(cached, [0] * len(cached)), c.kv, k_s, v_s.to(dt))
+        out = torch.full_like(q, 7.0)
+        eb_block_attn_paged(r, c.kv, q, k_t, v_t.to(dt), out)
+        want = torch.zeros(len(blocks), hkv, head_dim, dtype=torch.float64, device="cuda")
+        want.index_add_(0, seq_s, v_s.double()).index_add_(0, seq_t, v_t.double())
+        assert want.max() <= 32
+        want = (want / keys.clamp(min=1)[:, None, None])[seq_t].repeat_interleave(group, dim=1)
+        tol = 2.0 ** -20 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+        bad = (out.double() - want).abs() > tol * want
+        assert not bad.any(), (lo, torch.nonzero(bad)[:4].tolist())
+
+
 # More sequences than one workgroup looks through (2048), single tokens and small blocks, some empty.
 @pytest.mark.parametrize("cache,dtype", COMBOS)
 def test_attention_many_sequences(cache, dtype):
@@ -528,6 +592,28 @@ def test_long_pool():
                                     [0, 700], hkv, hkv)
         _close(_f64(out), ref, mag, "bf16")
         del kv
+
+
+@pytest.mark.parametrize("cache,head_dim", [("e4m3", 128), ("e4m3", 64), ("bf16", 64)])
+def test_long_pool_many_rows(cache, head_dim):
+    """The same for the kernels of many query rows (the others of them: test_long_pool)."""
+    hkv, page, n_pages, rows, cached = 8, 256, 9000 * 128 // head_dim, 100, 700
+    table = torch.tensor([[n_pages - 1, 1, n_pages - 500]], dtype=torch.int32, device="cuda")
+    kv = PagedKV.empty(n_pages, hkv, page, head_dim, table, TYPES[cache])
+    assert kv.k.numel() > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(4)
+    k, v, kb, vb, q = (torch.randn(n, hkv, head_dim, generator=g, device="cuda",
+                                   dtype=torch.bfloat16)
+                       for n in (cached, cached, rows, rows, rows))
+    eb_kv_write(Ragged.from_lengths([cached], [0]), kv, k, v)
+    out = torch.zeros_like(q)
+    eb_block_attn_paged(Ragged.from_lengths([rows], [cached]), kv, q, kb, vb, out)
+    pre = [paged.dequantise(*paged.quantise(_f64(x))) if cache == "e4m3" else _f64(x)
+           for x in (k, v)]
+    args = ([0, rows], [0, cached], hkv, hkv)
+    ref = paged.block_attention(_f64(q), _f64(kb), _f64(vb), *pre, *args)
+    mag = paged.block_attention(_f64(q), _f64(kb), np.abs(_f64(vb)), pre[0], np.abs(pre[1]), *args)
+    _close(_f64(out), ref, mag, "bf16")
 
 
 # --------------------------------------------------------------------------------------------
