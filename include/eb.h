@@ -217,7 +217,8 @@ eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, voi
  * the values that the cache stands for; scores of -inf weigh nothing, but an infinity or NaN among
  * the values (an 8-bit cache holds both as NaN) makes its column infinite or NaN in every row that
  * sees it, whatever its weight.
- * ws: at least eb_block_attn_paged_workspace(...) bytes, 16-byte aligned, contents ignored.
+ * ws: at least eb_block_attn_paged_workspace(...) bytes (at most 137 MB with up to 512 K/V heads),
+ * 16-byte aligned, contents ignored.
  * ------------------------------------------------------------------------------------- */
 size_t eb_block_attn_paged_workspace(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv,
                                      int hq);

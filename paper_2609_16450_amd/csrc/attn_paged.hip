@@ -394,6 +394,11 @@ constexpr long kWholeStages = 8;
 // visit.
 constexpr long kCountBatch = 256;
 constexpr long kCountTurns = 8;  // runs per XCD, at least
+// Items counted off that may leave partials: twice what the plan aims at.  Only where more blocks
+// than are likely have items of their own (few_rows) would there be more of them; the sequences
+// behind these stay whole.  (The host can only bound the blocks that have items, by a good ten times
+// what there usually are: a chunk of 512 among 255 tokens took 239 MB for 336 items.)
+constexpr long kMostPartials = 2 * kAttnTargetWgs;
 
 struct TilesLaunch {
   TilePlan plan;
@@ -415,7 +420,10 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a, long skip) {
   t.plan.skip = static_cast<int>(skip);
   if (a.batch <= kPlanMaxBatch && whole <= kSplitItems && stages > kWholeStages) {
     const int rounds = whole <= kSplitItems1 ? 1 : whole <= kSplitItems2 ? 2 : 4;
-    t.plan.cap = rounds * kAttnTargetWgs;
+    // no more than there are (range, K/V head, tile)s; a power of two, for find_item
+    int cap = kXcdCount;
+    while (cap < rounds * kAttnTargetWgs && cap < whole * stages) cap *= 2;
+    t.plan.cap = cap;
     t.grid = t.plan.cap;
     t.parts = t.plan.cap;
     return t;
@@ -432,15 +440,16 @@ TilesLaunch tiles_plan(const PagedAttnArgs& a, long skip) {
   t.plan.chunk = static_cast<int>(chunk);
   t.plan.nsplit = static_cast<int>((stages + chunk - 1) / chunk);
   if (counted) {
-    const long items = whole * t.plan.nsplit;
+    const long items = std::min(whole * t.plan.nsplit, whole + kMostPartials);
     const long run =
         std::max(1L, std::min(row_tiles, likely * t.plan.nsplit / (kXcdCount * kCountTurns)));
     t.plan.run = static_cast<int>(run);
+    t.plan.most = static_cast<int>(kMostPartials);
     t.grid = kXcdCount * run * ((items + kXcdCount * run - 1) / (kXcdCount * run));
   } else {
     t.grid = kXcdCount * ((a.batch * hkv * t.plan.nsplit + kXcdCount - 1) / kXcdCount) * row_tiles;
   }
-  t.parts = t.plan.nsplit > 1 ? t.grid : 0;
+  t.parts = t.plan.nsplit == 1 ? 0 : counted ? std::min(t.grid, kMostPartials) : t.grid;
   return t;
 }
 

@@ -74,11 +74,12 @@ struct TilePlan {
   int cap;
   int chunk, nsplit;  // cap = 0: stages per range, ranges per sequence
   int run;            // > 0: items counted off, dealt to the XCDs in runs of so many
+  int most;           // run > 0: items that may leave partials
   float* o_part;      // [items, kRowsPerWg, D], then m and l [items, kRowsPerWg]
   float* m_part;
   float* l_part;
   // cap > 0: of each of kPlanMaxBatch sequences its first item, then its ranges, then a LastRound;
-  // run > 0: of each sequence with more than one range its first item
+  // run > 0: of each sequence of more than `chunk` stages its first item, or -1 if it stayed whole
   int32_t* found;
 };
 template <bool kBits8>
@@ -204,11 +205,19 @@ __device__ __forceinline__ bool count_off(const AttnParams& p, const TilePlan& t
                                           int lane, int wave, TileItem& it) {
   it.item = (j / tp.run * kXcdCount + xcd) * tp.run + j % tp.run;
   int first = 0, b = tp.batch, row_tiles = 1;
+  int cut = 0;  // items so far if every sequence is cut
+  bool whole = false;
   for (int b0 = 0; b0 < tp.batch; b0 += 64) {
     const int own = min(b0 + lane, tp.batch - 1);
     const int len = b0 + lane < tp.batch ? tile_len(p, tp, own) : 0;
     const int stages = tile_stages(p.cu_prefix[own + 1] - p.cu_prefix[own], len);
-    const int ranges = (stages + tp.chunk - 1) / tp.chunk, tiles = tile_rows(len, p.group);
+    const int tiles = tile_rows(len, p.group);
+    int ranges = (stages + tp.chunk - 1) / tp.chunk;
+    if (tp.nsplit > 1) {  // (uniform) sequences are cut while the partials' places last
+      const int upto = cut + lanes_up_to(ranges * tiles * p.hkv, 0, AddOp{});
+      cut = __builtin_amdgcn_readlane(upto, 63);
+      if (upto > tp.most) ranges = min(ranges, 1);
+    }
     const int n = ranges * tiles * p.hkv;
     const int upto = lanes_up_to(n, 0, AddOp{});
     const uint64_t past = __ballot(first + upto > it.item);
@@ -217,6 +226,7 @@ __device__ __forceinline__ bool count_off(const AttnParams& p, const TilePlan& t
       first += __builtin_amdgcn_readlane(upto - n, l);
       b = b0 + l;
       it.ranges = __builtin_amdgcn_readlane(ranges, l);
+      whole = it.ranges == 1 && __builtin_amdgcn_readlane(stages, l) > tp.chunk;
       row_tiles = __builtin_amdgcn_readlane(tiles, l);
       break;
     }
@@ -225,8 +235,8 @@ __device__ __forceinline__ bool count_off(const AttnParams& p, const TilePlan& t
   if (b >= tp.batch) return false;
   it.b = __builtin_amdgcn_readfirstlane(b);
   place_item(it, it.item - first, row_tiles, p.hkv);
-  if (it.item == first && it.ranges > 1 && wave == 0 && lane == 0)  // for the merge
-    tp.found[b] = first;
+  if (it.item == first && (it.ranges > 1 || whole) && wave == 0 && lane == 0)  // for the merge
+    tp.found[b] = whole ? -1 : first;
   return true;
 }
 // The item of this workgroup; false if there is none.
@@ -1187,6 +1197,7 @@ __global__ __launch_bounds__(kThreads) void attn_tiles_merge_kernel(AttnParams p
     ranges = (stages + tp.chunk - 1) / tp.chunk;
     if (tp.run == 0) row_tiles = tp.row_tiles;
     first = tp.run == 0 ? b * tp.nsplit * p.hkv * row_tiles : ranges > 1 ? tp.found[b] : 0;
+    if (first < 0) ranges = 1;
   }
   for (int h = h0; h < p.hq; h += waves) {
     const int g = h / p.group, r = (row - p.cu_block[b]) * p.group + h % p.group;

@@ -327,8 +327,10 @@ COUNTS = [
     ([34 + i % 3 * (i % 7 > 0) - 34 * (i == 9) for i in range(70)],
      [(53 * i) % 900 for i in range(70)], 1, 2),
     ([i % 4 for i in range(150)] + [500] + [2] * 130, [(91 * i) % 400 for i in range(281)], 4, 3),
-    # 8 bits: two launches
-    ([1, 0, 3, 9] * 20 + [150], [(191 * i) % 3000 + 700 for i in range(81)], 4, 3)]
+    # 8 bits: two launches; and more blocks with items of their own than are cut into ranges
+    ([1, 0, 3, 9] * 20 + [150], [(191 * i) % 3000 + 700 for i in range(81)], 4, 3),
+    ([17, 1, 0, 1] * 100 + [70], [(191 * i) % 900 + 600 for i in range(401)], 4, 1),
+    ([70] + [0, 1, 17, 1] * 100, [(191 * i) % 900 + 600 for i in range(401)], 4, 1)]
 
 
 @pytest.mark.parametrize("head_dim,page", [(64, 64), (128, 16)])
@@ -443,6 +445,14 @@ def test_workspace_is_enough(blocks, cached, group, cache, dtype):
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 def test_workspace_of_many_sequences(cache):
     _guarded([1] * 80 + [300], [10 * i for i in range(81)], 2, cache, "bf16")
+
+
+def test_workspace_of_many_cut_sequences():
+    """More blocks with items of their own than are cut into ranges; few keys of one block, whose
+    workspace is that of its items."""
+    _guarded([17, 1, 0, 1] * 100 + [70], [(191 * i) % 900 + 600 for i in range(401)], 1, "e4m3",
+             "bf16")
+    _guarded([33], [600], 1, "bf16", "bf16")
 
 
 def _guarded(blocks, cached, group, cache, dtype):

@@ -1,6 +1,7 @@
 """Paged cache: bad arguments are refused on the host, before anything is launched."""
 import ctypes
 import pathlib
+import random
 import subprocess
 import sys
 
@@ -148,6 +149,39 @@ def test_sizes_that_no_plan_is_made_for():
     want = [f"0 {B.EB_ERR_INVALID if s in NO_BATCH else B.EB_ERR_UNSUPPORTED}"
             for s in sizes for _ in types]
     assert (res.returncode, res.stdout.splitlines()) == (0, want), res.stderr[-500:]
+
+
+def _need(blocks, cached, hq, hkv, head_dim, dt, cache):
+    r = _ragged(len(blocks), sum(blocks), max(blocks), sum(cached), max(cached))
+    kv = _kv(dtype=cache, hkv=hkv, head_dim=head_dim, n_pages=1 << 20, max_pages=1 << 20,
+             k_scale=0x100, v_scale=0x100)
+    return B.load().eb_block_attn_paged_workspace(dt, ctypes.byref(r), ctypes.byref(kv), hq)
+
+
+# a block of 33 rows behind 600: 11 ranges; a long block among many short ones, which the host can
+# not tell from blocks of 17 rows: 1024 partials of 128 rows
+@pytest.mark.parametrize("blocks,cached,hq,hkv,most", [
+    ([33], [600], 1, 1, 16), ([100], [600], 28, 4, 512), ([1] * 255 + [512], [2500] * 256, 28, 4, 1024),
+    ([1] * 199 + [64], [2500] * 200, 16, 4, 1024), ([2] * 299 + [40], [2500] * 300, 16, 4, 1024)])
+@pytest.mark.parametrize("cache", [B.EB_BF16, B.EB_E4M3])
+def test_workspace_follows_the_call(cache, blocks, cached, hq, hkv, most):
+    row = (128 + 2) * 4
+    assert _need(blocks, cached, hq, hkv, 128, B.EB_BF16, cache) <= most * 128 * row + 4096
+
+
+def test_largest_workspace():
+    """The bound that eb.h gives, over sizes of all orders."""
+    rng = random.Random(0)
+    for _ in range(4000):
+        n = int(2 ** rng.uniform(0, 10))
+        lo, hi = sorted(int(2 ** rng.uniform(0, 12)) for _ in range(2))
+        blocks = [rng.randint(lo, hi) if rng.random() < 0.5 else lo for _ in range(n)]
+        longest = int(2 ** rng.uniform(0, 17))
+        cached = [rng.randint(0, longest) for _ in range(n)]
+        hkv, group = 2 ** rng.randint(0, 9), rng.randint(1, 16)
+        for dt, cache in ((B.EB_F32, B.EB_F32), (B.EB_BF16, B.EB_BF16), (B.EB_BF16, B.EB_E4M3)):
+            if sum(blocks) * hkv * group < 2 ** 31:
+                assert _need(blocks, cached, hkv * group, hkv, 128, dt, cache) <= 137e6
 
 
 def test_workspace_alignment():
