@@ -326,6 +326,7 @@ COUNTS = [
     ([33 + i % 9 for i in range(40)], [1030 - 26 * i for i in range(40)], 16, 1),
     ([34 + i % 3 * (i % 7 > 0) - 34 * (i == 9) for i in range(70)],
      [(53 * i) % 900 for i in range(70)], 1, 2),
+    ([40 - i % 6 for i in range(64)], [(53 * i) % 900 for i in range(64)], 1, 1),
     ([i % 4 for i in range(150)] + [500] + [2] * 130, [(91 * i) % 400 for i in range(281)], 4, 3),
     # 8 bits: two launches; and more blocks with items of their own than are cut into ranges
     ([1, 0, 3, 9] * 20 + [150], [(191 * i) % 3000 + 700 for i in range(81)], 4, 3),
@@ -764,6 +765,92 @@ def test_another_stream(cache, dtype):
     _close(*_attention([1, 30], [2000, 77], 16, cache, dtype, 3, 128, stream=s), dtype)
     with torch.cuda.stream(s):
         _close(*_attention([1, 30], [2000, 77], 16, cache, dtype, 3, 128), dtype)
+
+
+@pytest.mark.parametrize("cache", ["f32", "e4m3"])
+def test_fp32_rows_at_any_float(cache):
+    """fp32 rows need not be 16-byte aligned: every one of the calls' tensors one float further."""
+    rng = np.random.default_rng(15)
+    blocks, cached, hkv, hq, d = [3, 40], [70, 500], 2, 6, 64
+    spans = [p + n for n, p in zip(blocks, cached)]
+    c = Cache(spans, hkv, 16, d, cache, 10)
+
+    def off(n, h, values=True):
+        flat = torch.zeros(n * h * d + 1, device="cuda")
+        if values:
+            flat.copy_(torch.from_numpy(rng.standard_normal(len(flat))))
+        return flat[1:].view(n, h, d)
+
+    pre = [off(sum(cached), hkv) for _ in "kv"]
+    q, k, v, out = off(43, hq), off(43, hkv), off(43, hkv), off(43, hq, False)
+    eb_kv_write(Ragged.from_lengths(cached, [0, 0]), c.kv, *pre)
+    r = Ragged.from_lengths(blocks, cached)
+    eb_block_attn_paged(r, c.kv, q, k, v, out)
+    eb_kv_write(r, c.kv, k, v)
+    back = [off(sum(spans), hkv, False) for _ in "kv"]
+    eb_kv_read(Ragged.from_lengths([0, 0], spans), c.kv, *back)
+    for which, o in zip("kv", back):
+        np.testing.assert_array_equal(_f64(o), paged.kv_read(c.values(which), c.table, spans))
+    ref = paged.paged_attention(_f64(q), _f64(k), _f64(v), c.values("k"), c.values("v"), c.table,
+                                _cu(blocks), cached, hq, hkv)
+    _close(_f64(out), ref, None, "f32")
+
+
+@pytest.mark.parametrize("cache,dtype", COMBOS)
+@pytest.mark.parametrize("blocks", [[1, 1, 2], [40, 1, 90]])
+def test_shared_pages(blocks, cache, dtype):
+    """Sequences that read the same pages (a common beginning), and one that reads a page twice."""
+    rng = np.random.default_rng(16)
+    cached, page, hkv, group, d = [200, 150, 330], 16, 2, 3, 128
+    c = Cache(cached, hkv, page, d, cache, 11)
+    c.fill(cached, rng)
+    c.table[1, :6] = c.table[0, :6]
+    c.table[2, 3:9] = c.table[2, 10]
+    c.kv.page_table.copy_(torch.from_numpy(c.table))
+    q, k, v = (torch.from_numpy(rng.standard_normal((sum(blocks), h, d))).to(TYPES[dtype])
+               for h in (hkv * group, hkv, hkv))
+    out = torch.zeros(q.shape, dtype=TYPES[dtype], device="cuda")
+    eb_block_attn_paged(Ragged.from_lengths(blocks, cached), c.kv, q.cuda(), k.cuda(), v.cuda(), out)
+    args = dict(table=c.table, cu_block=_cu(blocks), cached=cached, hq=hkv * group, hkv=hkv)
+    ref = paged.paged_attention(_f64(q), _f64(k), _f64(v), c.values("k"), c.values("v"), **args)
+    mag = paged.paged_attention(_f64(q), _f64(k), np.abs(_f64(v)), c.values("k"),
+                                np.abs(c.values("v")), **args)
+    _close(_f64(out), ref, mag, dtype)
+
+
+@pytest.mark.parametrize("cache,dtype", COMBOS)
+@pytest.mark.parametrize("blocks,cached,hkv,group,head_dim", [
+    ([1, 1], [700, 33], 1, 71, 64), ([2, 1], [100, 900], 1, 130, 128), ([1], [400], 40, 1, 128),
+    ([1, 0, 3], [90, 5, 300], 17, 5, 64)])
+def test_attention_head_layouts(blocks, cached, hkv, group, head_dim, cache, dtype):
+    """One K/V head for many query heads (a token is then many rows), many K/V heads, odd numbers."""
+    _close(*_attention(blocks, cached, 32, cache, dtype, group, head_dim, hkv=hkv), dtype)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_two_streams_at_once(cache):
+    """Two calls on one cache in flight on two streams, each with its own workspace."""
+    rng = np.random.default_rng(17)
+    cached, hkv, hq, d = [3000, 41], 2, 8, 128
+    c = Cache(cached, hkv, 64, d, cache, 12)
+    c.fill(cached, rng)
+    calls = []
+    for blocks in ([1, 1], [70, 40]):
+        r = Ragged.from_lengths(blocks, cached)
+        x = [torch.from_numpy(rng.standard_normal((sum(blocks), h, d))).bfloat16().cuda()
+             for h in (hq, hkv, hkv)]
+        ws = torch.empty(max(1, eb_block_attn_paged_workspace(EB_BF16, r, c.kv, hq)),
+                         dtype=torch.uint8, device="cuda")
+        alone, out = torch.zeros_like(x[0]), torch.zeros_like(x[0])
+        eb_block_attn_paged(r, c.kv, *x, alone, ws=ws)
+        calls.append((r, x, ws, alone, out, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for r, x, ws, _, out, s in calls:
+            eb_block_attn_paged(r, c.kv, *x, out, ws=ws, stream=s)
+    torch.cuda.synchronize()
+    for _, _, _, alone, out, _ in calls:
+        assert torch.equal(alone, out)
 
 
 def test_binding_refusals():
