@@ -265,11 +265,12 @@ def _torch_stream(stream):
 
 
 def _workspace(nbytes: int, ws: Optional[torch.Tensor], device, stream) -> tuple:
-    """(pointer, bytes) of the caller's workspace, or of a temporary one.  A temporary is
+    """(pointer, bytes, tensor) of the caller's workspace, or of a temporary one.  A temporary is
     allocated on the stream the kernels run on, so that torch's caching allocator, once the
-    tensor is dropped here, hands its memory only to later work of that same stream."""
+    tensor is dropped, hands its memory only to later work of that same stream; the caller holds
+    it until the kernels are on that stream (another thread may allocate in between)."""
     if nbytes == 0:
-        return (None if ws is None else ws.data_ptr()), (0 if ws is None else ws.numel())
+        return (None if ws is None else ws.data_ptr()), (0 if ws is None else ws.numel()), ws
     if ws is None:
         if stream is None:  # torch allocates on the current stream by itself
             ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -277,7 +278,7 @@ def _workspace(nbytes: int, ws: Optional[torch.Tensor], device, stream) -> tuple
             with torch.cuda.stream(_torch_stream(stream)):
                 ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     _dev(ws, "ws", torch.uint8)
-    return ws.data_ptr(), ws.numel()
+    return ws.data_ptr(), ws.numel(), ws
 
 
 # --------------------------------------------------------------------------------------
@@ -305,7 +306,7 @@ def eb_block_attn(r: Ragged, q, k_blk, v_blk, k_pre, v_pre, out, scale: Optional
     rc = r.c()
     lib = load()
     need = int(lib.eb_block_attn_workspace(dt, ctypes.byref(rc), hq, hkv, D))
-    wp, wn = _workspace(need, ws, q.device, stream)
+    wp, wn, ws = _workspace(need, ws, q.device, stream)
     _check(lib.eb_block_attn(dt, ctypes.byref(rc), hq, hkv, D, scale, q.data_ptr(),
                              k_blk.data_ptr(), v_blk.data_ptr(), k_pre.data_ptr(),
                              v_pre.data_ptr(), out.data_ptr(), wp, wn, _stream(stream)),
@@ -334,7 +335,7 @@ def eb_block_attn_dual(r: Ragged, cu_suffix: torch.Tensor, max_suffix: int, q, k
     sc = eb_suffix(U, int(max_suffix), cu_suffix.data_ptr())
     lib = load()
     need = int(lib.eb_block_attn_dual_workspace(dt, ctypes.byref(rc), ctypes.byref(sc), hq, hkv, D))
-    wp, wn = _workspace(need, ws, q.device, stream)
+    wp, wn, ws = _workspace(need, ws, q.device, stream)
     _check(lib.eb_block_attn_dual(dt, ctypes.byref(rc), ctypes.byref(sc), hq, hkv, D, scale,
                                   q.data_ptr(), k_blk.data_ptr(), v_blk.data_ptr(),
                                   k_pre.data_ptr(), v_pre.data_ptr(), k_suf.data_ptr(),
@@ -468,7 +469,7 @@ def eb_block_attn_paged(r: Ragged, kv: PagedKV, q, k_blk, v_blk, out,
     lib = load()
     if ws is None:
         need = int(lib.eb_block_attn_paged_workspace(dt, rp, kv._ref, hq))
-        wp, wn = _workspace(need, None, q.device, stream)
+        wp, wn, ws = _workspace(need, None, q.device, stream)
     else:  # the library compares its size with what the call needs
         _dev_on(kv.device_index, ws, "ws", torch.uint8)
         wp, wn = ws.data_ptr(), ws.numel()
@@ -496,7 +497,7 @@ def eb_lmhead_confidence(h, w, conf, entropy_nats, argmax, max_logit=None,
         _dev(max_logit, "max_logit", torch.float32, (n_rows,))
     lib = load()
     need = int(lib.eb_lmhead_workspace(dt, n_rows, hidden, vocab))
-    wp, wn = _workspace(need, ws, h.device, stream)
+    wp, wn, ws = _workspace(need, ws, h.device, stream)
     _check(lib.eb_lmhead_confidence(dt, n_rows, hidden, vocab, h.data_ptr(), w.data_ptr(),
                                     conf.data_ptr(), entropy_nats.data_ptr(), argmax.data_ptr(),
                                     _ptr(max_logit), wp, wn, _stream(stream)),
@@ -542,7 +543,7 @@ def eb_lmhead_features(h, w, conf, entropy_nats, argmax, top2_gap, max_logit=Non
         _dev(max_logit, "max_logit", torch.float32, (n_rows,))
     lib = load()
     need = int(lib.eb_lmhead_features_workspace(dt, n_rows, hidden, vocab))
-    wp, wn = _workspace(need, ws, h.device, stream)
+    wp, wn, ws = _workspace(need, ws, h.device, stream)
     _check(lib.eb_lmhead_features(dt, n_rows, hidden, vocab, h.data_ptr(), w.data_ptr(),
                                   conf.data_ptr(), entropy_nats.data_ptr(), argmax.data_ptr(),
                                   _ptr(max_logit), top2_gap.data_ptr(), wp, wn, _stream(stream)),

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from oracle import paged
+from paper_2609_16450_amd import binding
 from paper_2609_16450_amd import (EbError, PagedKV, Ragged, eb_block_attn, eb_block_attn_paged,
                                   eb_block_attn_paged_workspace, eb_decode_step, eb_kv_read,
                                   eb_kv_write, EB_BF16, StepBuffers)
@@ -851,6 +852,43 @@ def test_two_streams_at_once(cache):
     torch.cuda.synchronize()
     for _, _, _, alone, out, _ in calls:
         assert torch.equal(alone, out)
+
+
+def test_temporary_workspace_lives_until_the_launch(monkeypatch):
+    """A workspace that the binding allocates is still held when the library is called: given back
+    before, another thread's tensor could take its memory and be overwritten by the kernels."""
+    c = Cache([3000], 2, 16, 128, "bf16", 1)
+    c.fill([3000], np.random.default_rng(0))
+    r = Ragged.from_lengths([1], [3000])
+    q, k = (torch.ones(1, h, 128, dtype=torch.bfloat16, device="cuda") for h in (4, 2))
+    h, w = (torch.ones(n, 128, dtype=torch.bfloat16, device="cuda") for n in (4, 5000))
+    pre = [torch.ones(3000, 2, 128, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    conf, entropy, gap = (torch.zeros(4, device="cuda") for _ in range(3))
+    top, suffix = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (4, 2))
+    out, lib, seen = torch.zeros_like(q), binding.load(), {}
+
+    class Watched:
+        """The library, noting what a workspace query answers and the memory in use at a call."""
+
+        def __getattr__(self, name):
+            def call(*args):
+                if not name.endswith("_workspace"):
+                    seen["in use"] = torch.cuda.memory_allocated()
+                answer = getattr(lib, name)(*args)
+                if name.endswith("_workspace"):
+                    seen["need"] = answer
+                return answer
+            return call
+
+    monkeypatch.setattr(binding, "load", Watched)
+    for go in (lambda: eb_block_attn_paged(r, c.kv, q, k, k, out),
+               lambda: eb_block_attn(r, q, k, k, *pre, out),
+               lambda: binding.eb_block_attn_dual(r, suffix, 0, q, k, k, *pre, k[:0], k[:0], out),
+               lambda: binding.eb_lmhead_confidence(h, w, conf, entropy, top),
+               lambda: binding.eb_lmhead_features(h, w, conf, entropy, top, gap)):
+        before = torch.cuda.memory_allocated()
+        go()
+        assert seen["need"] > 0 and seen["in use"] >= before + seen["need"], seen
 
 
 def test_binding_refusals():
