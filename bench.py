@@ -557,7 +557,8 @@ def main() -> int:
                     help="write profiles/lmhead_traffic.json from rocprofv3 counter runs in DIR")
     ap.add_argument("--no-peaks", action="store_true",
                     help="skip the same-box copy and GEMM reference rates (e.g. under a profiler)")
-    ap.add_argument("--path", default="step", choices=["step", "lps", "topm", "dual", "lbs", "paged", "paged8"],
+    ap.add_argument("--path", default="step",
+                    choices=["step", "lps", "topm", "dual", "lbs", "paged", "paged8"],
                     help="step: eb_decode_step (the headline); lps: attention + LM head with the "
                          "top-2 gap + LPS features + union accept rule; topm: attention + LM head "
                          "+ top-m commit; dual: dual-cache attention + LM head + unmask; lbs: the "

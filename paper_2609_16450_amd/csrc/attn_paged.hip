@@ -378,9 +378,10 @@ hipError_t launch_few_any(const PagedAttnArgs& a, long rows, void* ws, hipStream
 // ---- many query rows, bf16: the tile kernels of the packed prefix ---------------------------
 // Items of whole sequences (a K/V head and a tile of query rows each) up to which a launch may cut
 // sequences into ranges, for one, two or four rounds of workgroups: the fewer items, the fewer
-// rounds are needed to make them even.  With more than kSplitItems whole sequences fill the rounds
-// (32 heads, 32 blocks of 8 to 128 rows behind 2048, 1024 items: 212 us whole, 227 us with the
-// plan).
+// rounds are needed to make them even.  With more than kSplitItems sequences stay whole (32 heads,
+// 32 blocks of 8 to 128 rows behind 2048, 1024 items, two full rounds: 212 us whole, 227 us with the
+// plan); a third round that is not full then costs as much as a full one (33, 36, 40 and 48 such
+// blocks: 254, 272, 288 and 329 us).  The borders lie between the shapes measured.
 constexpr long kSplitItems1 = 160, kSplitItems2 = 420, kSplitItems = 900;
 // Up to this many stages sequences stay whole: one block of 100 rows behind 300, 28/4 heads, 7
 // stages, 16 against 19 us; behind 600, 12 stages, 18 us either way.
@@ -396,8 +397,8 @@ constexpr long kCountBatch = 256;
 constexpr long kCountTurns = 8;  // runs per XCD, at least
 // Items counted off that may leave partials: twice what the plan aims at.  Only where more blocks
 // than are likely have items of their own (few_rows) would there be more of them; the sequences
-// behind these stay whole.  (The host can only bound the blocks that have items, by a good ten times
-// what there usually are: a chunk of 512 among 255 tokens took 239 MB for 336 items.)
+// behind these stay whole.  (The host can only bound the blocks that have items, by a good ten
+// times what there usually are: a chunk of 512 among 255 tokens took 239 MB for 336 items.)
 constexpr long kMostPartials = 2 * kAttnTargetWgs;
 
 struct TilesLaunch {

@@ -301,6 +301,11 @@ __device__ __forceinline__ bool find_item(const AttnParams& p, const TilePlan& t
 // Two workgroups per compute unit (<= 256 VGPRs per lane, no spills at D = 128), so one
 // wave's softmax arithmetic overlaps another wave's MFMAs on the same SIMD (batch 64 at
 // D = 128: 1.85 ms with one workgroup per compute unit, 1.07 ms with two).
+//
+// The probabilities are rounded to bf16 for the product with V, the MFMA's type; l sums them
+// unrounded, in fp32.  Over pages at D = 64 the result's distance from 64 bits (2-norm) is then
+// 0.0020 of it, 0.00166 with the output's rounding alone.  Holding the rest of each probability in
+// a second bf16 would take that away for twice the MFMAs of O.
 template <int D, class Keys>
 __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnParams p, Keys keys,
                                                                 int row_tiles, int units) {
@@ -692,7 +697,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnParams p, Ke
 // exceeds it by more than kAttnSlack, so probabilities 2^(s - m) stay below 2^kAttnSlack and
 // O, l are rescaled rarely.  l sums the bf16-rounded probabilities that P V multiplies, two per
 // dot instruction.  The final O / l and the split partials (m, l, O) mean the same as in
-// attn_bf16_kernel.
+// attn_bf16_kernel.  With the slack even a row's largest probability is rounded: 0.0023 from 64
+// bits (2-norm, packed or paged), 0.00166 with the output's rounding alone.
+//
+// Registers: 234 vector registers over bf16 pages, 251 over 8 bits, none of them in memory; 24 and
+// 30 scalar values do not fit and are kept in lanes of vector registers, some of those of the 8-bit
+// form read back in every iteration.
 constexpr float kAttnSlack = 8.0f;
 constexpr int kDmaKeys = 64;  // keys per tile (the schedule pairs 16 S MFMAs with 16 P words)
 static_assert(kDmaKeys == kKeys, "stages of the key-split plan");
@@ -924,7 +934,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_d128_kernel(AttnParams 
         const size_t from = (ok ? page : 0) * page_bytes;
         const int row = at & page_mask, rows = ok ? min(max(plen - at, 0), 16) : 0;
         const __amdgpu_buffer_rsrc_t rs = make_rsrc(pool_g + from + row * D, rows * D);
-      // load i of the group: rows 2 (lane / 8) + i
+        // load i of the group: rows 2 (lane / 8) + i
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           raw[2 * h + i] = buffer_load16(rs, (2 * (lane >> 3) + i) * D + 16 * (lane & 7));
