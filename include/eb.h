@@ -214,10 +214,11 @@ eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, voi
  *
  * dt is EB_F32 (cache EB_F32 or EB_E4M3) or EB_BF16 (cache EB_BF16 or EB_E4M3).  hkv and head_dim
  * are the cache's; hq % hkv == 0; scale as in eb_block_attn.  Arithmetic as in eb_block_attn, on
- * the values that the cache stands for: with bf16 rows the probabilities are rounded to bf16 for
- * the product with V (each by at most 2^-8 of itself, the result by at most about
- * 2^-7 sum_j p_j |v_j|); the denominator sums those rounded values at head_dim 128 where a block has
- * many query rows per K/V head, the unrounded ones otherwise; EB_F32 computes in fp32 throughout.
+ * the values that the cache stands for.  With bf16 rows the probabilities are held to 2^-16 for the
+ * product with V where blocks have few query rows per K/V head (up to 32, over 8 bits up to 16; single
+ * tokens), and rounded to bf16 where they have more (each by at most 2^-8 of itself, the result by
+ * at most about 2^-7 sum_j p_j |v_j|); the denominator sums those rounded values at head_dim 128
+ * from 33 (8 bits: 65) rows on, unrounded ones otherwise.  EB_F32 computes in fp32 throughout.
  * Scores of -inf weigh nothing, but an infinity or NaN among the values (an 8-bit cache holds both
  * as NaN) makes its column infinite or NaN in every row that sees it, whatever its weight.
  * ws: at least eb_block_attn_paged_workspace(...) bytes (at most 137 MB with up to 512 K/V heads),

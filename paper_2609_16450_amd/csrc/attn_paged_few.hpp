@@ -28,9 +28,13 @@
 // An 8-bit cache is converted to bf16 on the way, exactly: K rows by the lane that holds them, V
 // rows before they go to LDS.
 //
-// The probabilities are rounded to bf16 for the product with V, the MFMA's type, as in the tile
-// kernels; l sums them unrounded, in fp32, at both head dimensions.  The result's distance from 64
-// bits (2-norm) is then 0.0019 to 0.0020 of it, 0.00166 with the output's rounding alone.
+// The MFMA takes the probabilities in bf16.  Two of them hold a probability to 2^-16 and cost as
+// many MFMAs of the second product again, which wait for memory anyway: the result is then as far
+// from 64 bits (2-norm) as its own rounding makes it, 0.00166, with one bf16 0.0019 to 0.0020, and
+// no call is slower (64 tokens as above 60.4 and 61.3 us; bf16 pages, 16 blocks of 32 rows, 145 and
+// 144).  Only two tiles over 8 bits, whose widening leaves no issue slots, keep one bf16, as the
+// tile kernels do: 3 to 14% slower with two (16 blocks of 32 rows 92 against 89 us, 32 of 8 rows x 7
+// heads 70 against 65, 100 of 10 rows x 4 heads of 64 59 against 51).  l sums them in fp32.
 //
 // Every 16 keys of a piece lie in one page; a buffer resource per group of 16 ends with the last
 // cached row, so rows past it arrive as zeros, and one of no length stands for a missing page.
@@ -90,6 +94,16 @@ __device__ __forceinline__ int few_find(const FewParams& fp, int row0, int s, in
   return fp.batch;
 }
 
+// Two values >= 0, each as a bf16 below it and a bf16 of the rest, to 2^-16 of itself.  The rest is
+// made 2^-20 of the value too large, so that it is zero only where the value is: infinity times the
+// pair stays infinity.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& most, uint32_t& rest) {
+  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+  most = __builtin_amdgcn_perm(y, x, 0x07060302u);  // high halves
+  rest = pack2_bf16(fmaf(a, 0x1p-20f, a - __uint_as_float(x & 0xffff0000u)),
+                    fmaf(b, 0x1p-20f, b - __uint_as_float(y & 0xffff0000u)));
+}
+
 template <int D, bool kE4m3, int kTiles>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewParams fp) {
   const AttnParams& p = fp.a;
@@ -97,6 +111,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
   constexpr int kDTiles = D / 16;         // 16-row tiles of O^T
   constexpr int kGroups = kFewKeys / 16;     // groups of 16 keys of a piece
   constexpr int kRow = kE4m3 ? D : 2 * D; // bytes of a cached row
+  constexpr bool kTwoBf16 = !kE4m3 || kTiles == 1;  // a probability in two bf16
   constexpr int kVPitch = D + 16;         // V row pitch in LDS (see attn_small.hpp)
   constexpr int kOPitch = D + 4;          // row pitch of a wave's O in LDS (fp32)
   constexpr int kVBytes = kFewKeys * kVPitch * 2;
@@ -175,7 +190,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
     // `valid` keys exist; V lies in LDS.
     auto finish = [&](auto& sc, int valid) {
       constexpr int kG = sizeof(sc[0]) / sizeof(f32x4);
-      u32x2 pk[kTiles][kG];
+      u32x2 pk[kTiles][kG], rest[kTiles][kG];  // P in one bf16, or in two (split2)
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         if (valid < 16 * kG) {
@@ -205,7 +220,15 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
             e[r] = fast_exp2(fmaf(sc[t][j][r], p.scale_log2, -m_new));
             lsum += e[r];
           }
-          pk[t][j] = u32x2{pack2_bf16(e[0], e[1]), pack2_bf16(e[2], e[3])};
+          if constexpr (kTwoBf16) {
+            uint32_t most[2], less[2];
+            split2(e[0], e[1], most[0], less[0]);
+            split2(e[2], e[3], most[1], less[1]);
+            pk[t][j] = u32x2{most[0], most[1]};
+            rest[t][j] = u32x2{less[0], less[1]};
+          } else {
+            pk[t][j] = u32x2{pack2_bf16(e[0], e[1]), pack2_bf16(e[2], e[3])};
+          }
         }
         l_run[t] = l_run[t] * alpha + lsum;
         if (__any(alpha != 1.0f)) {
@@ -222,9 +245,12 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attn_paged_few_kernel(FewPa
               bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) {
-            const u32x2 lo2 = pk[t][2 * u], hi2 = pk[t][2 * u + 1];
-            const u32x4 w{lo2[0], lo2[1], hi2[0], hi2[1]};
-            o[t][d] = mfma16(vf, __builtin_bit_cast(bf16x8, w), o[t][d]);
+            auto weights = [&](const u32x2& lo2, const u32x2& hi2) {
+              return __builtin_bit_cast(bf16x8, u32x4{lo2[0], lo2[1], hi2[0], hi2[1]});
+            };
+            o[t][d] = mfma16(vf, weights(pk[t][2 * u], pk[t][2 * u + 1]), o[t][d]);
+            if constexpr (kTwoBf16)
+              o[t][d] = mfma16(vf, weights(rest[t][2 * u], rest[t][2 * u + 1]), o[t][d]);
           }
         }
     };

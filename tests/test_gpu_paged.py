@@ -387,6 +387,21 @@ def test_attention_many_sequences(cache, dtype):
     _close(*_attention(blocks, cached, 16, cache, dtype, 2, 64, hkv=1), dtype)
 
 
+# Few query rows per K/V head: probabilities to 2^-16, so that a result is off by its own rounding to
+# bf16 (2^-8 of itself) and, as in _close, scores that are 1.2e-4 off (twice that in a quotient) and
+# twice 2^-16 of sum_j p_j |v_j|.  Few keys, where one probability counts most.
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("cache,blocks,cached,group", [
+    *((cache, *shape) for cache in ("bf16", "e4m3") for shape in (
+        ([1] * 100, [2 + i for i in range(100)], 7), ([2] * 50, list(range(50)), 8),
+        ([1, 2], [3000, 5], 4))),
+    ("bf16", [20, 32], [10, 30], 1)])
+def test_few_rows_hold_probabilities(blocks, cached, group, cache, head_dim):
+    got, ref, mag = _attention(blocks, cached, 16, cache, "bf16", group, head_dim)
+    bound = 2.0 ** -8 * np.abs(ref) + 1.1 * (2.4e-4 + 2.0 ** -15) * mag
+    assert (np.abs(got - ref) <= bound).all(), (np.abs(got - ref) / bound).max()
+
+
 # The plans of the tile kernel: more sequences than a wave has lanes, cut by the host (70 of one tile);
 # so many items that sequences stay whole, over more pages of 16 rows than a wave holds numbers of
 # (64); lengths so different that only the longest are cut; one long block, whose tiles share keys.
