@@ -148,8 +148,8 @@ eb_status eb_block_attn_dual(eb_dtype dt, const eb_ragged* r, const eb_suffix* s
  * are dropped.  What table entries behind a sequence's last page hold is of no account.
  *
  * Requires hkv >= 1, head_dim in {64, 128}, page_size in {16, 32, 64, 128, 256}, n_pages >= 1,
- * max_pages >= 1 and, where cached rows are read, max_prefix <= max_pages * page_size.  One write or
- * read moves at most 2^34 values of K.  An attention call takes at most 65535 sequences of at most
+ * max_pages >= 1 and, where cached rows are read, max_prefix <= max_pages * page_size.  One write
+ * or read moves at most 2^34 values of K.  An attention call takes at most 65535 sequences of at most
  * 2^30 keys, hkv at most 65535, and what fits one launch of fewer than 2^32 threads
  * (EB_ERR_UNSUPPORTED beyond).
  * With EB_DEBUG_CHECKS the page numbers that a call uses have to lie in [0, n_pages).
@@ -214,10 +214,10 @@ eb_status eb_kv_read(eb_dtype dt, const eb_ragged* r, const eb_paged_kv* kv, voi
  *
  * dt is EB_F32 (cache EB_F32 or EB_E4M3) or EB_BF16 (cache EB_BF16 or EB_E4M3).  hkv and head_dim
  * are the cache's; hq % hkv == 0; scale as in eb_block_attn.  Arithmetic as in eb_block_attn, on
- * the values that the cache stands for.  With bf16 rows the probabilities are held to 2^-16 for the
- * product with V where blocks have few query rows per K/V head (up to 32, over 8 bits up to 16; single
- * tokens), and rounded to bf16 where they have more (each by at most 2^-8 of itself, the result by
- * at most about 2^-7 sum_j p_j |v_j|); the denominator sums those rounded values at head_dim 128
+ * the values that the cache stands for.  With bf16 rows the probabilities are held to 2^-16 for
+ * the product with V where blocks have few query rows per K/V head (single tokens; up to 32 rows,
+ * over 8 bits up to 16), and rounded to bf16 where they have more (each by at most 2^-8 of itself,
+ * the result by at most about 2^-7 sum_j p_j |v_j|); the denominator sums those rounded values at head_dim 128
  * from 33 (8 bits: 65) rows on, unrounded ones otherwise.  EB_F32 computes in fp32 throughout.
  * Scores of -inf weigh nothing, but an infinity or NaN among the values (an 8-bit cache holds both
  * as NaN) makes its column infinite or NaN in every row that sees it, whatever its weight.

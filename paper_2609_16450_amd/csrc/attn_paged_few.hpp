@@ -31,10 +31,11 @@
 // The MFMA takes the probabilities in bf16.  Two of them hold a probability to 2^-16 and cost as
 // many MFMAs of the second product again, which wait for memory anyway: the result is then as far
 // from 64 bits (2-norm) as its own rounding makes it, 0.00166, with one bf16 0.0019 to 0.0020, and
-// no call is slower (64 tokens as above 60.4 and 61.3 us; bf16 pages, 16 blocks of 32 rows, 145 and
-// 144).  Only two tiles over 8 bits, whose widening leaves no issue slots, keep one bf16, as the
-// tile kernels do: 3 to 14% slower with two (16 blocks of 32 rows 92 against 89 us, 32 of 8 rows x 7
-// heads 70 against 65, 100 of 10 rows x 4 heads of 64 59 against 51).  l sums them in fp32.
+// no call is slower (64 tokens as above 60.6 and 60.3 us with one, with the merge; bf16 pages, 16
+// blocks of 32 rows, 145 and 146).  Only two tiles over 8 bits, whose widening leaves no issue
+// slots, keep one bf16, as the tile kernels do: 3 to 14% slower with two (16 blocks of 32 rows 92
+// against 89 us, 32 of 8 rows x 7 heads 70 against 65, 100 of 10 rows x 4 heads of 64 59 against
+// 51).  l sums them in fp32.
 //
 // Every 16 keys of a piece lie in one page; a buffer resource per group of 16 ends with the last
 // cached row, so rows past it arrive as zeros, and one of no length stands for a missing page.

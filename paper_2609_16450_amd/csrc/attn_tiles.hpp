@@ -304,8 +304,10 @@ __device__ __forceinline__ bool find_item(const AttnParams& p, const TilePlan& t
 //
 // The probabilities are rounded to bf16 for the product with V, the MFMA's type; l sums them
 // unrounded, in fp32.  Over pages at D = 64 the result's distance from 64 bits (2-norm) is then
-// 0.0020 of it, 0.00166 with the output's rounding alone.  Holding the rest of each probability in
-// a second bf16 would take that away for twice the MFMAs of O.
+// 0.0020 of it, 0.00166 with the output's rounding alone.  A second bf16 for the rest of each
+// probability, as in the kernel for few rows, takes that away and costs 10 to 27% here, over pages
+// (16/4 heads, 32 blocks of 16 to 128 behind 2048 71 -> 86 us, 2 chunks behind 7001 and 12000 301
+// -> 382): not kept.
 template <int D, class Keys>
 __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnParams p, Keys keys,
                                                                 int row_tiles, int units) {
