@@ -40,6 +40,16 @@ class eb_paged_kv(ctypes.Structure):
                 ("k_scale", _P), ("v_scale", _P)]
 
 
+class eb_page_pool(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("page_table", _P), ("free_pages", _P),
+                ("state", _P), ("state_out", _P)]
+
+
+class eb_sample_params(ctypes.Structure):
+    _fields_ = [("temperature", _P), ("top_k", _P), ("top_p", _P), ("min_p", _P)]
+
+
 class eb_step_trace(ctypes.Structure):
     _fields_ = [("attn_begin", _P), ("attn_end", _P), ("lmhead_begin", _P), ("lmhead_end", _P),
                 ("select_begin", _P), ("select_end", _P)]
@@ -75,6 +85,8 @@ EXPORTS = {
                                    ctypes.POINTER(eb_paged_kv), _P, _P, _P, _P]),
     "eb_kv_read": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(eb_ragged),
                                   ctypes.POINTER(eb_paged_kv), _P, _P, _P]),
+    "eb_kv_assign": (ctypes.c_int, [ctypes.POINTER(eb_page_pool), ctypes.c_int32, ctypes.c_int32,
+                                    *[_P] * 10]),
     "eb_block_attn_paged_workspace": (ctypes.c_size_t, [ctypes.c_int, ctypes.POINTER(eb_ragged),
                                                         ctypes.POINTER(eb_paged_kv),
                                                         ctypes.c_int]),
@@ -87,6 +99,12 @@ EXPORTS = {
     "eb_lmhead_confidence": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
                                             ctypes.c_int, _P, _P, _P, _P, _P, _P, _P,
                                             ctypes.c_size_t, _P]),
+    "eb_lmhead_logits": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                        _P, _P, _P, _P]),
+    "eb_sample_workspace": (ctypes.c_size_t, [ctypes.c_int, ctypes.c_int, ctypes.c_int]),
+    "eb_sample": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(eb_ragged), ctypes.c_int,
+                                 ctypes.c_int64, _P, _P, ctypes.POINTER(eb_sample_params), _P, _P,
+                                 _P, _P, ctypes.c_size_t, _P]),
     "eb_unmask_select": (ctypes.c_int, [ctypes.POINTER(eb_ragged), _P, _P, _P, _P, _P, _P, _P,
                                         _P, _P]),
     "eb_lmhead_features_workspace": (ctypes.c_size_t, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
@@ -206,6 +224,16 @@ def _dev_on(index: int, t: torch.Tensor, name: str, dtype=None, shape=None) -> N
         raise ValueError(f"{name} is on device {t.get_device()}, the cache on {index}")
 
 
+def _dev_with(index: int, t: torch.Tensor, name: str, dtype=None, shape=None) -> None:
+    """As _dev, with the tensor on the call's device `index`."""
+    if (isinstance(t, torch.Tensor) and t.get_device() == index and t.is_contiguous()
+            and (dtype is None or t.dtype is dtype) and (shape is None or t.shape == shape)):
+        return
+    _dev(t, name, dtype, shape)
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on device {t.get_device()}, the call's tensors on {index}")
+
+
 # The current device's current stream as a handle, without building a torch.cuda.Stream (0.2
 # against 2 us); None where this torch has no such call.
 _get_device = getattr(torch._C, "_cuda_getDevice", None)
@@ -220,6 +248,19 @@ def _stream(stream) -> int:
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
+
+
+def _stream_on(index: int, stream) -> int:
+    """The stream's handle.  A launch goes to the current device: tensors (on device `index`) and
+    streams of another one are refused."""
+    current = torch.cuda.current_device() if _get_device is None else _get_device()
+    if current != index:
+        raise ValueError(f"the call's tensors are on device {index}, the current device is "
+                         f"{current}")
+    if isinstance(stream, torch.cuda.Stream) and stream.device_index != index:
+        raise ValueError(f"the call's tensors are on device {index}, the stream on "
+                         f"{stream.device_index}")
+    return _stream(stream)
 
 
 @dataclass
@@ -447,6 +488,67 @@ def eb_kv_read(r: Ragged, kv: PagedKV, k, v, stream=None) -> None:
            "eb_kv_read")
 
 
+class PagePool:
+    """The pages of a PagedKV that no sequence holds: a ring free_pages int32 [n_pages] and its state
+    int32 [2], the place of the first free page and their number (eb_page_pool in eb.h).  Both
+    tensors are kept, not copied."""
+
+    def __init__(self, free_pages: torch.Tensor, state: torch.Tensor):
+        if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1 or \
+                not free_pages.numel():
+            raise ValueError("free_pages must be a tensor [n_pages]")
+        _dev(free_pages, "free_pages", torch.int32)
+        _dev_with(free_pages.get_device(), state, "state", torch.int32, (2,))
+        self.free_pages, self.state = free_pages, state
+
+    @staticmethod
+    def full(n_pages: int, device="cuda") -> "PagePool":
+        """All pages of a pool, free, lowest first."""
+        return PagePool(torch.arange(n_pages, dtype=torch.int32, device=device),
+                        torch.tensor([0, n_pages], dtype=torch.int32, device=device))
+
+
+def eb_kv_assign(kv: PagedKV, pool: PagePool, cached, new_rows, cu_block, cu_prefix, pos,
+                 slot=None, done=None, shared=None, short=None, state_out=None,
+                 stream=None) -> None:
+    """Pages of `pool` into kv's page table for new_rows [B] rows behind the cached [B] ones, and back
+    for the done [B]; offsets cu_block, cu_prefix [B + 1], positions pos [n_rows] and slots of the
+    packed new rows (eb.h).  The pool's state is updated in place, or left as it is and written to
+    state_out."""
+    if not isinstance(kv, PagedKV):
+        raise TypeError("kv must be a PagedKV")
+    if not isinstance(pool, PagePool):
+        raise TypeError("pool must be a PagePool")
+    index, B = kv.device_index, kv.batch
+    if pool.free_pages.numel() != kv.n_pages:
+        raise ValueError(f"the pool's ring holds {pool.free_pages.numel()} pages, the cache "
+                         f"{kv.n_pages}")
+    if not isinstance(pos, torch.Tensor) or pos.dim() != 1:
+        raise ValueError("pos must be a tensor [n_rows]")
+    i32, n_rows = torch.int32, pos.shape[0]
+    state_out = pool.state if state_out is None else state_out
+    for name, t, dtype, shape in (("free_pages", pool.free_pages, i32, (kv.n_pages,)),
+                                  ("state", pool.state, i32, (2,)),
+                                  ("state_out", state_out, i32, (2,)),
+                                  ("cached", cached, i32, (B,)), ("new_rows", new_rows, i32, (B,)),
+                                  ("cu_block", cu_block, i32, (B + 1,)),
+                                  ("cu_prefix", cu_prefix, i32, (B + 1,)),
+                                  ("pos", pos, i32, (n_rows,)),
+                                  ("slot", slot, torch.int64, (n_rows,)),
+                                  ("done", done, torch.uint8, (B,)),
+                                  ("shared", shared, i32, (B,)),
+                                  ("short", short, torch.uint8, (B,))):
+        if t is not None or name in ("cached", "new_rows", "cu_block", "cu_prefix"):
+            _dev_with(index, t, name, dtype, shape)
+    s = _stream_on(index, stream)
+    c = eb_page_pool(kv.n_pages, kv.page_size, kv.max_pages, kv.page_table.data_ptr(),
+                     pool.free_pages.data_ptr(), pool.state.data_ptr(), state_out.data_ptr())
+    _check(load().eb_kv_assign(ctypes.byref(c), B, n_rows, cached.data_ptr(), new_rows.data_ptr(),
+                               _ptr(done), _ptr(shared), cu_block.data_ptr(),
+                               cu_prefix.data_ptr(), pos.data_ptr(), _ptr(slot), _ptr(short), s),
+           "eb_kv_assign")
+
+
 def eb_block_attn_paged_workspace(dtype: int, r: Ragged, kv: PagedKV, hq: int) -> int:
     rc = r.c()
     return int(load().eb_block_attn_paged_workspace(dtype, ctypes.byref(rc), kv._ref, hq))
@@ -502,6 +604,62 @@ def eb_lmhead_confidence(h, w, conf, entropy_nats, argmax, max_logit=None,
                                     conf.data_ptr(), entropy_nats.data_ptr(), argmax.data_ptr(),
                                     _ptr(max_logit), wp, wn, _stream(stream)),
            "eb_lmhead_confidence")
+
+
+def eb_lmhead_logits(h, w, logits, stream=None) -> None:
+    """logits [n_rows, vocab] float32 <- h [n_rows, hidden] w[vocab, hidden]^T (eb.h)."""
+    dt = _dtype_code(h)
+    n_rows, hidden = h.shape
+    vocab = w.shape[0]
+    index = h.get_device()
+    _dev(h, "h", h.dtype, (n_rows, hidden))
+    _dev_with(index, w, "w", h.dtype, (vocab, hidden))
+    _dev_with(index, logits, "logits", torch.float32, (n_rows, vocab))
+    _check(load().eb_lmhead_logits(dt, n_rows, hidden, vocab, h.data_ptr(), w.data_ptr(),
+                                   logits.data_ptr(), _stream_on(index, stream)),
+           "eb_lmhead_logits")
+
+
+def eb_sample_workspace(dtype: int, n_rows: int, vocab: int) -> int:
+    return int(load().eb_sample_workspace(dtype, n_rows, vocab))
+
+
+def eb_sample(r: Ragged, logits, uniform, token, prob=None, conf=None, temperature=None,
+              top_k=None, top_p=None, min_p=None, vocab: Optional[int] = None,
+              ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """token [T] int32 (with prob and conf [T]) <- a draw from each block row's logits [T, pitch] with
+    uniform [T], under its sequence's temperature, top_k, top_p and min_p [B] (eb.h).  vocab: the
+    columns that are tokens, all of them by default."""
+    dt = _dtype_code(logits)
+    T, B = r.total_block, r.batch
+    if logits.dim() != 2:
+        raise ValueError(f"logits has shape {tuple(logits.shape)}, expected [T, pitch]")
+    pitch = logits.shape[1]
+    vocab = pitch if vocab is None else int(vocab)
+    index = logits.get_device()
+    _dev(logits, "logits", logits.dtype, (T, pitch))
+    f32, i32 = torch.float32, torch.int32
+    _dev_with(index, uniform, "uniform", f32, (T,))
+    _dev_with(index, token, "token", i32, (T,))
+    for name, t, dtype, n in (("prob", prob, f32, T), ("conf", conf, f32, T),
+                              ("temperature", temperature, f32, B), ("top_k", top_k, i32, B),
+                              ("top_p", top_p, f32, B), ("min_p", min_p, f32, B)):
+        if t is not None:
+            _dev_with(index, t, name, dtype, (n,))
+    rc, s = r.c(), _stream_on(index, stream)
+    if r.cu_block.get_device() != index:
+        raise ValueError("the batch's offsets and the logits are on different devices")
+    lib = load()
+    if ws is None:
+        wp, wn, ws = _workspace(int(lib.eb_sample_workspace(dt, T, vocab)), None, logits.device,
+                                stream)
+    else:  # the library compares its size with what the call needs
+        _dev_with(index, ws, "ws", torch.uint8)
+        wp, wn = ws.data_ptr(), ws.numel()
+    p = eb_sample_params(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
+    _check(lib.eb_sample(dt, ctypes.byref(rc), vocab, pitch, logits.data_ptr(),
+                         uniform.data_ptr(), ctypes.byref(p), token.data_ptr(), _ptr(prob),
+                         _ptr(conf), wp, wn, s), "eb_sample")
 
 
 def eb_unmask_select(r: Ragged, conf, argmax, tau, masked, tokens, unmask, n_commit, resolved,

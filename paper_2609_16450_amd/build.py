@@ -14,7 +14,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libeb.so")
 SOURCES = ["eb_api.hip", "lmhead.hip", "attn.hip", "attn_paged.hip", "kv_cache.hip",
-           "unmask.hip", "lbs.hip", "step.hip", "probe.hip"]
+           "kv_assign.hip", "sample.hip", "unmask.hip", "lbs.hip", "step.hip", "probe.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

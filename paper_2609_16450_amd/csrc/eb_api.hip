@@ -50,6 +50,7 @@ constexpr int64_t kMaxPackedValues = 1LL << 34;  // of K in one launch of the ca
 // Block rows x query heads: no attention kernel takes fewer than two threads for one, and a launch
 // has fewer than 2^32.
 constexpr int64_t kMaxQueryRows = 1LL << 31;
+constexpr int kMaxF32HeadRows = kMaxGridYZ * 32;  // 32 rows to a workgroup of the fp32 head
 constexpr int kProbeMaxGroups = 65536;
 constexpr int kProbeMaxIters = 1 << 20;
 size_t round_up(size_t n) { return (n + kWsAlign - 1) / kWsAlign * kWsAlign; }
@@ -141,6 +142,18 @@ eb_status check_unmask(const eb_ragged* r, const void* conf, const void* argmax,
   return EB_OK;
 }
 
+eb_status check_page_size(int32_t n) {
+  if (n < 16 || n > 256 || (n & (n - 1)))
+    return fail(EB_ERR_UNSUPPORTED, "page_size %d not supported (16, 32, 64, 128 or 256)", n);
+  return EB_OK;
+}
+
+int page_shift(int32_t page_size) {
+  int shift = 0;
+  while (shift < 30 && (1 << shift) < page_size) ++shift;
+  return shift;
+}
+
 // The fields of a paged cache, and that dt's rows go with its type.
 eb_status check_paged(eb_dtype dt, const eb_paged_kv* kv) {
   if (dt != EB_F32 && dt != EB_BF16) return fail(EB_ERR_INVALID, "unknown dtype %d", (int)dt);
@@ -153,9 +166,8 @@ eb_status check_paged(eb_dtype dt, const eb_paged_kv* kv) {
                 kv->hkv, kv->head_dim, kv->n_pages, kv->page_size, kv->max_pages);
   if (kv->head_dim != 64 && kv->head_dim != 128)
     return fail(EB_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", kv->head_dim);
-  if (kv->page_size < 16 || kv->page_size > 256 || (kv->page_size & (kv->page_size - 1)))
-    return fail(EB_ERR_UNSUPPORTED, "page_size %d not supported (16, 32, 64, 128 or 256)",
-                kv->page_size);
+  const eb_status st = check_page_size(kv->page_size);
+  if (st != EB_OK) return st;
   if (kv->hkv > kMaxGridYZ)
     return fail(EB_ERR_UNSUPPORTED, "hkv %d not supported (at most %d)", kv->hkv, kMaxGridYZ);
   if (kv->dtype != EB_E4M3 && kv->dtype != dt)
@@ -203,9 +215,7 @@ eb::PagedKv paged_args(const eb_paged_kv* kv) {
   const eb::CacheType type = kv->dtype == EB_E4M3   ? eb::CacheType::kE4m3
                              : kv->dtype == EB_BF16 ? eb::CacheType::kBf16
                                                     : eb::CacheType::kF32;
-  int shift = 0;
-  while (shift < 30 && (1 << shift) < kv->page_size) ++shift;
-  return eb::PagedKv{type, kv->hkv, kv->head_dim, kv->n_pages, shift, kv->max_pages,
+  return eb::PagedKv{type, kv->hkv, kv->head_dim, kv->n_pages, page_shift(kv->page_size), kv->max_pages,
                      kv->page_table, static_cast<uint8_t*>(kv->k), static_cast<uint8_t*>(kv->v),
                      kv->k_scale, kv->v_scale};
 }
@@ -340,6 +350,80 @@ eb_status check_written(const eb_ragged* r, const eb_paged_kv* kv, const int32_t
     return fail(EB_ERR_INVALID, "two rows go to row %lld of page %lld",
                 (long long)(*twice % kv->page_size), (long long)(*twice / kv->page_size));
   return EB_OK;
+}
+
+// What an assignment's arrays have to hold: lengths whose sums fit, a ring whose free entries are
+// pages, pages given back that are pages and leave the ring no fuller than it is long.
+eb_status check_assign(const eb_page_pool* pool, int32_t batch, int32_t n_rows,
+                       const int32_t* cached, const int32_t* new_rows, const uint8_t* done,
+                       const int32_t* shared, hipStream_t s) {
+  std::vector<int32_t> held, add, keep, state, ring, table;
+  std::vector<uint8_t> gone;
+  eb_status st = fetch(held, cached, batch, s);
+  if (st == EB_OK) st = fetch(add, new_rows, batch, s);
+  if (st == EB_OK && done) st = fetch(gone, done, batch, s);
+  if (st == EB_OK && shared) st = fetch(keep, shared, batch, s);
+  if (st == EB_OK) st = fetch(state, pool->state, 2, s);
+  if (st == EB_OK) st = fetch(ring, pool->free_pages, pool->n_pages, s);
+  if (st == EB_OK && done)
+    st = fetch(table, pool->page_table, static_cast<size_t>(batch) * pool->max_pages, s);
+  if (st != EB_OK) return st;
+  if (state[0] < 0 || state[0] >= pool->n_pages || state[1] < 0 || state[1] > pool->n_pages)
+    return fail(EB_ERR_INVALID, "state (%d, %d) is not in [0, %d) x [0, %d]", state[0], state[1],
+                pool->n_pages, pool->n_pages);
+  auto is_page = [&](int32_t p) { return p >= 0 && p < pool->n_pages; };
+  for (int64_t i = 0; i < state[1]; ++i) {
+    const int64_t at = (state[0] + i) % pool->n_pages;
+    if (!is_page(ring[at]))
+      return fail(EB_ERR_INVALID, "free_pages[%lld] = %d is not in [0, %d)", (long long)at,
+                  ring[at], pool->n_pages);
+  }
+  int64_t rows = 0, prefix = 0, back = 0;
+  for (int b = 0; b < batch; ++b) {
+    if (held[b] < 0 || add[b] < 0 || (shared && keep[b] < 0))
+      return fail(EB_ERR_INVALID, "sequence %d: a negative length (%d cached, %d new, %d shared)", b,
+                  held[b], add[b], shared ? keep[b] : 0);
+    const int64_t pages = (static_cast<int64_t>(held[b]) + pool->page_size - 1) / pool->page_size;
+    if (pages > pool->max_pages)
+      return fail(EB_ERR_INVALID, "sequence %d: %d cached rows do not fit %d pages of %d rows", b,
+                  held[b], pool->max_pages, pool->page_size);
+    if (done && gone[b]) {
+      for (int64_t j = shared ? keep[b] : 0; j < pages; ++j, ++back) {
+        const int32_t page = table[static_cast<size_t>(b) * pool->max_pages + j];
+        if (!is_page(page))
+          return fail(EB_ERR_INVALID, "page_table[%d][%lld] = %d is not in [0, %d)", b,
+                      (long long)j, page, pool->n_pages);
+      }
+    } else {
+      rows += add[b];
+      prefix += held[b];
+    }
+  }
+  if (rows > n_rows || prefix > INT32_MAX)
+    return fail(EB_ERR_INVALID, "%lld new rows (n_rows %d), %lld cached rows", (long long)rows,
+                n_rows, (long long)prefix);
+  if (state[1] + back > pool->n_pages)
+    return fail(EB_ERR_INVALID, "%d free pages and %lld given back, of %d", state[1],
+                (long long)back, pool->n_pages);
+  return EB_OK;
+}
+
+// Random numbers of every row and the settings of every sequence.
+eb_status check_sample_values(const eb_ragged* r, const float* uniform, const eb_sample_params& p,
+                              hipStream_t s) {
+  auto each = [&](const char* name, const float* d, size_t n, auto ok) -> eb_status {
+    std::vector<float> h;
+    eb_status st = d ? fetch(h, d, n, s) : EB_OK;
+    for (size_t i = 0; st == EB_OK && i < h.size(); ++i)
+      if (!ok(h[i])) st = fail(EB_ERR_INVALID, "%s[%zu] = %g is out of range", name, i, (double)h[i]);
+    return st;
+  };
+  auto unit = [](float x) { return x >= 0.f && x <= 1.f; };
+  eb_status st = each("uniform", uniform, r->total_block, [](float x) { return x >= 0.f && x < 1.f; });
+  if (st == EB_OK) st = each("temperature", p.temperature, r->batch, [](float x) { return x >= 0.f; });
+  if (st == EB_OK) st = each("top_p", p.top_p, r->batch, unit);
+  if (st == EB_OK) st = each("min_p", p.min_p, r->batch, unit);
+  return st;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -559,6 +643,34 @@ eb_status eb_block_attn_paged(eb_dtype dt, const eb_ragged* r, const eb_paged_kv
   return hip_status(eb::attn_paged(dt == EB_BF16, a, ws, stream), "eb_block_attn_paged launch");
 }
 
+eb_status eb_kv_assign(const eb_page_pool* pool, int32_t batch, int32_t n_rows,
+                       const int32_t* cached, const int32_t* new_rows, const uint8_t* done,
+                       const int32_t* shared, int32_t* cu_block, int32_t* cu_prefix, int32_t* pos,
+                       int64_t* slot, uint8_t* shorted, eb_stream_t stream) {
+  if (!pool) return fail(EB_ERR_INVALID, "page pool descriptor is NULL");
+  if (batch < 1 || n_rows < 0)
+    return fail(EB_ERR_INVALID, "need batch >= 1 and n_rows >= 0 (got %d, %d)", batch, n_rows);
+  if (pool->n_pages < 1 || pool->page_size < 1 || pool->max_pages < 1)
+    return fail(EB_ERR_INVALID, "need n_pages, page_size, max_pages >= 1 (got %d, %d, %d)",
+                pool->n_pages, pool->page_size, pool->max_pages);
+  eb_status st = check_page_size(pool->page_size);
+  if (st != EB_OK) return st;
+  if (!pool->page_table || !pool->free_pages || !pool->state || !pool->state_out)
+    return fail(EB_ERR_INVALID, "NULL page_table / free_pages / state / state_out");
+  if (!cached || !new_rows || !cu_block || !cu_prefix)
+    return fail(EB_ERR_INVALID, "NULL cached / new_rows / cu_block / cu_prefix");
+  if (n_rows > 0 && !pos) return fail(EB_ERR_INVALID, "NULL pos");
+  if (debug_checks()) {
+    st = check_assign(pool, batch, n_rows, cached, new_rows, done, shared, stream);
+    if (st != EB_OK) return st;
+  }
+  const eb::KvAssign a{pool->n_pages, page_shift(pool->page_size), pool->max_pages,
+                       pool->page_table, pool->free_pages, pool->state, pool->state_out, batch,
+                       n_rows, cached, new_rows, done, shared, cu_block, cu_prefix, pos, slot,
+                       shorted};
+  return hip_status(eb::kv_assign(a, stream), "eb_kv_assign launch");
+}
+
 size_t eb_lmhead_workspace(eb_dtype dt, int n_rows, int hidden, int vocab) {
   (void)hidden;
   if (n_rows <= 0 || vocab <= 0) return 0;
@@ -608,6 +720,51 @@ eb_status eb_lmhead_features(eb_dtype dt, int n_rows, int hidden, int vocab, con
   if (n_rows > 0 && !top2_gap) return fail(EB_ERR_INVALID, "NULL top2_gap");
   return lmhead_run(dt, n_rows, hidden, vocab, h, w, conf, entropy_nats, argmax, max_logit,
                     top2_gap, ws, ws_bytes, stream);
+}
+
+eb_status eb_lmhead_logits(eb_dtype dt, int n_rows, int hidden, int vocab, const void* h,
+                           const void* w, float* logits, eb_stream_t stream) {
+  if (n_rows > 0 && !logits) return fail(EB_ERR_INVALID, "NULL logits");
+  eb_status st = check_lmhead(dt, n_rows, hidden, vocab, h, w, logits, logits, logits);
+  if (st != EB_OK) return st;
+  if (dt == EB_F32 && n_rows > kMaxF32HeadRows)
+    return fail(EB_ERR_UNSUPPORTED, "%d rows in one fp32 call (at most %d)", n_rows,
+                kMaxF32HeadRows);
+  return hip_status(eb::lmhead_logits(dt == EB_BF16, n_rows, hidden, vocab, h, w, logits, stream),
+                    "eb_lmhead_logits launch");
+}
+
+size_t eb_sample_workspace(eb_dtype dt, int n_rows, int vocab) {
+  if (n_rows <= 0 || vocab <= 0 || vocab > eb::kSampleMaxVocab) return 0;
+  return round_up(eb::sample_ws_bytes(dt == EB_BF16, n_rows, vocab));
+}
+
+eb_status eb_sample(eb_dtype dt, const eb_ragged* r, int vocab, int64_t pitch, const void* logits,
+                    const float* uniform, const eb_sample_params* params, int32_t* token,
+                    float* prob, float* conf, void* ws, size_t ws_bytes, eb_stream_t stream) {
+  if (dt != EB_F32 && dt != EB_BF16) return fail(EB_ERR_INVALID, "unknown dtype %d", (int)dt);
+  eb_status st = check_ragged(r, false);
+  if (st != EB_OK) return st;
+  if (vocab < 1 || pitch < vocab)
+    return fail(EB_ERR_INVALID, "need vocab >= 1 and pitch >= vocab (got %d, %lld)", vocab,
+                (long long)pitch);
+  if (vocab > eb::kSampleMaxVocab)
+    return fail(EB_ERR_UNSUPPORTED, "vocab %d not supported (at most %d)", vocab,
+                eb::kSampleMaxVocab);
+  if (r->total_block > 0 && (!logits || !uniform || !token))
+    return fail(EB_ERR_INVALID, "NULL logits / uniform / token");
+  const size_t need = eb_sample_workspace(dt, r->total_block, vocab);
+  if (ws_bytes < need || (need && !ws))
+    return fail(EB_ERR_WORKSPACE, "sampling workspace %zu bytes < required %zu", ws_bytes, need);
+  if (need && !aligned16(ws))
+    return fail(EB_ERR_INVALID, "the sampling workspace must be 16-byte aligned");
+  const eb_sample_params p = params ? *params : eb_sample_params{};
+  st = check_device(r, false, nullptr, stream);
+  if (st == EB_OK && debug_checks()) st = check_sample_values(r, uniform, p, stream);
+  if (st != EB_OK) return st;
+  const eb::SampleArgs a{r->batch, r->total_block, vocab, pitch, r->cu_block, logits, uniform,
+                         p.temperature, p.top_k, p.top_p, p.min_p, token, prob, conf};
+  return hip_status(eb::sample(dt == EB_BF16, a, ws, stream), "eb_sample launch");
 }
 
 eb_status eb_lps_features(const eb_ragged* r, int vocab, const float* conf,

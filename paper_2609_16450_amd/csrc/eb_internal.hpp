@@ -20,6 +20,9 @@ hipError_t lmhead_partials(bool bf16, int n_rows, int hidden, int vocab, const v
 hipError_t lmhead_combine(bool bf16, int n_rows, int vocab, const void* ws, float* conf,
                           float* entropy, int32_t* argmax, float* max_logit, float* top2_gap,
                           hipStream_t s);
+// The logits themselves, float [n_rows, vocab].
+hipError_t lmhead_logits(bool bf16, int n_rows, int hidden, int vocab, const void* h,
+                         const void* w, float* logits, hipStream_t s);
 
 // ---- block attention ------------------------------------------------------------------
 struct AttnArgs {
@@ -68,6 +71,26 @@ hipError_t kv_write(bool bf16, const PagedKv& kv, int batch, int total, const in
 hipError_t kv_read(bool bf16, const PagedKv& kv, int batch, int total, const int32_t* cu_prefix,
                    void* k, void* v, hipStream_t s);
 
+// Pages for new rows (an eb_page_pool and the arrays of eb_kv_assign, checked).
+struct KvAssign {
+  int n_pages, page_shift, max_pages;
+  int32_t* page_table;
+  int32_t* free_pages;
+  const int32_t* state;
+  int32_t* state_out;
+  int batch, n_rows;
+  const int32_t* cached;
+  const int32_t* new_rows;
+  const uint8_t* done;    // nullable
+  const int32_t* shared;  // nullable
+  int32_t* cu_block;
+  int32_t* cu_prefix;
+  int32_t* pos;
+  int64_t* slot;     // nullable
+  uint8_t* shorted;  // nullable
+};
+hipError_t kv_assign(const KvAssign& a, hipStream_t s);
+
 struct PagedAttnArgs {
   int batch, total_block, max_block, total_prefix, max_prefix;
   const int32_t* cu_block;
@@ -91,6 +114,25 @@ hipError_t attn_paged(bool bf16, const PagedAttnArgs& a, void* ws, hipStream_t s
 bool lmhead_hosts_attn(bool bf16, int n_rows, int vocab, const AttnArgs& a);
 hipError_t lmhead_partials_attn(int n_rows, int hidden, int vocab, const void* h, const void* w,
                                 void* ws, const AttnArgs& a, void* attn_ws, hipStream_t s);
+
+// ---- tokens from logits -----------------------------------------------------------------
+constexpr int kSampleMaxVocab = 1 << 21;
+struct SampleArgs {
+  int batch, n_rows, vocab;
+  int64_t pitch;  // elements from a row to the next
+  const int32_t* cu_block;
+  const void* logits;
+  const float* uniform;
+  const float* temperature;  // per sequence; nullable, as are the next three
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* token;
+  float* prob;  // nullable
+  float* conf;  // nullable
+};
+size_t sample_ws_bytes(bool bf16, int n_rows, int vocab);
+hipError_t sample(bool bf16, const SampleArgs& a, void* ws, hipStream_t s);
 
 // ---- measurement aid -------------------------------------------------------------------
 // Register-only bf16 32x32x16 MFMA loop over `groups` workgroups of 256 threads; each thread

@@ -8,6 +8,9 @@
 // Orientation: the MFMA "row" dimension is the vocabulary and the "column" dimension is the
 // block position, so every lane owns one position and reduces the logits it holds in
 // registers before a single cross-half exchange.
+//
+// The same kernels also write the logits (LmOut::kLogits, eb_lmhead_logits): another epilogue on the
+// same accumulators, so a written logit has the bits that the statistics see.
 #include <type_traits>
 
 #include "attn_small.hpp"
@@ -17,6 +20,10 @@
 
 namespace eb {
 namespace {
+
+// What a kernel does with its logits: statistics, statistics with the second-largest logit, or the
+// logits themselves.  In the last form the kernels' `part` is the output, float [n_rows, vocab].
+enum class LmOut { kStats, kTop2, kLogits };
 
 // ---------------------------------------------------------------------------------------
 // Streaming kernel for few block positions (n_rows <= 16 * NT).
@@ -121,12 +128,38 @@ __device__ __forceinline__ Partial wave_column_stats(const f32x4 (&acc)[TM][NT],
   return partial_xor_merge(p, 32, lane);
 }
 
-// kTop2: also track the second-largest logit of each (row, slice) into part2.
+// Writes the logits of a wave's natural-order 16x16 accumulator tiles (rows as in wave_column_stats,
+// columns the positions row0 + 16 nt + l % 16 below n_rows): 16 bytes per lane, 64 contiguous bytes
+// per position and tile.  A logit row starts at any float.
+template <int TM, int NT>
+__device__ __forceinline__ void store_logits(const f32x4 (&acc)[TM][NT], float* __restrict__ out,
+                                             int row0, int n_rows, int vocab, int wb, int we,
+                                             int lane) {
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = row0 + nt * 16 + (lane & 15);
+    if (row >= n_rows) continue;
+    float* const o = out + static_cast<size_t>(row) * vocab;
+#pragma unroll
+    for (int tm = 0; tm < TM; ++tm) {
+      const int v = wb + tm * 16 + 4 * (lane >> 4);
+      if (v + 4 <= we) {
+        *reinterpret_cast<f32x4u*>(o + v) = acc[tm][nt];
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (v + r < we) o[v + r] = acc[tm][nt][r];
+      }
+    }
+  }
+}
+
+// kOut = kTop2: also track the second-largest logit of each (row, slice) into part2.
 // kWaves waves per workgroup, shares of at most 8 NL vocabulary rows per wave (NL whole-line loads
 // per k-step), NT 16-position tiles.
 // kAttnD != 0: workgroups n_slices and up run the small block attention (head dimension kAttnD)
 // on unit blockIdx.x - n_slices of ap; the dispatcher starts them as the slices finish.
-template <int kWaves, int NL, int NT, int kDepth, bool kTop2, int kAttnD, bool kLines>
+template <int kWaves, int NL, int NT, int kDepth, LmOut kOut, int kAttnD, bool kLines>
 __global__ __launch_bounds__(kWaves * 64) void lmhead_stream16_kernel(
     const uint16_t* __restrict__ h, const uint16_t* __restrict__ w, int n_rows, int hidden,
     int vocab, int rows_per_wg, Partial* __restrict__ part, float* __restrict__ part2,
@@ -138,6 +171,7 @@ __global__ __launch_bounds__(kWaves * 64) void lmhead_stream16_kernel(
       return;
     }
   }
+  constexpr bool kTop2 = kOut == LmOut::kTop2;
   constexpr int TM = (NL + 1) / 2;     // 16-row tiles; the last one may lack its upper rows
   constexpr int kCols = kLines ? 64 : 32;   // columns per k-step
   constexpr int kLoads = kLines ? NL : TM;  // loads per k-step
@@ -273,6 +307,10 @@ __global__ __launch_bounds__(kWaves * 64) void lmhead_stream16_kernel(
 #pragma unroll
   for (int j = 0; j < kDepth; ++j) consume(nsteps_p - kDepth, j);
 
+  if constexpr (kOut == LmOut::kLogits) {
+    store_logits(acc, reinterpret_cast<float*>(part), 0, n_rows, vocab, wb, we, lane);
+    return;
+  }
   __syncthreads();
   Partial* red = reinterpret_cast<Partial*>(&hs[0][0]);  // [kWaves][kHRows]
   float* red2 = reinterpret_cast<float*>(red + kWaves * kHRows);
@@ -358,7 +396,7 @@ constexpr StreamForm kStreamForm = kWaves == 8 || (NL == 1 && NT <= 2) ? kWholeL
                                    : NL <= 2                           ? kHalfLines
                                                                        : kBySize;
 
-template <int kWaves, int NL, int NT, bool kTop2, int kAttnD, bool kLines>
+template <int kWaves, int NL, int NT, LmOut kOut, int kAttnD, bool kLines>
 hipError_t launch_stream_form(int n_rows, int hidden, int vocab, const StreamPlan& pl,
                               const void* h, const void* w, Partial* part, float* part2,
                               hipStream_t s, const HostedAttn& ha) {
@@ -370,20 +408,20 @@ hipError_t launch_stream_form(int n_rows, int hidden, int vocab, const StreamPla
   constexpr int D = kWaves == 8 ? 1 : (NT >= 4 ? 8 : 16) / kLoads;
   constexpr int Dp = D >= kMax ? kMax : (D >= 4 ? 4 : (D >= 2 ? 2 : 1));
   const int extra = kAttnD != 0 ? ha.units : 0;
-  hipLaunchKernelGGL((lmhead_stream16_kernel<kWaves, NL, NT, Dp, kTop2, kAttnD, kLines>),
+  hipLaunchKernelGGL((lmhead_stream16_kernel<kWaves, NL, NT, Dp, kOut, kAttnD, kLines>),
                      dim3(pl.groups + extra), dim3(kWaves * 64), 0, s,
                      static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(w), n_rows,
                      hidden, vocab, pl.rows_per_wg, part, part2, pl.groups, ha.p);
   return hipGetLastError();
 }
 
-template <int kWaves, int NL, int NT, bool kTop2, int kAttnD = 0>
+template <int kWaves, int NL, int NT, LmOut kOut, int kAttnD = 0>
 hipError_t launch_stream_nl(int n_rows, int hidden, int vocab, const StreamPlan& pl,
                             const void* h, const void* w, Partial* part, float* part2,
                             hipStream_t s, const HostedAttn& ha) {
   constexpr StreamForm form = kStreamForm<kWaves, NL, NT>;
   auto go = [&](auto lines) {
-    return launch_stream_form<kWaves, NL, NT, kTop2, kAttnD, lines.value>(
+    return launch_stream_form<kWaves, NL, NT, kOut, kAttnD, lines.value>(
         n_rows, hidden, vocab, pl, h, w, part, part2, s, ha);
   };
   if constexpr (form == kBySize) {
@@ -393,30 +431,30 @@ hipError_t launch_stream_nl(int n_rows, int hidden, int vocab, const StreamPlan&
 }
 
 // 16 waves, NL 8-row loads: the variant for the hosted attention's head dimension.
-template <int NL, int NT, bool kTop2>
+template <int NL, int NT, LmOut kOut>
 hipError_t launch_stream16(int n_rows, int hidden, int vocab, const StreamPlan& pl,
                            const void* h, const void* w, Partial* part, float* part2,
                            hipStream_t s, const HostedAttn& ha) {
-  if constexpr (!kTop2) {
+  if constexpr (kOut == LmOut::kStats) {
     if (ha.attn_d == 128)
-      return launch_stream_nl<16, NL, NT, false, 128>(n_rows, hidden, vocab, pl, h, w, part,
+      return launch_stream_nl<16, NL, NT, kOut, 128>(n_rows, hidden, vocab, pl, h, w, part,
                                                       part2, s, ha);
     if (ha.attn_d == 64)
-      return launch_stream_nl<16, NL, NT, false, 64>(n_rows, hidden, vocab, pl, h, w, part,
+      return launch_stream_nl<16, NL, NT, kOut, 64>(n_rows, hidden, vocab, pl, h, w, part,
                                                      part2, s, ha);
   }
   if (ha.attn_d != 0) return hipErrorInvalidValue;  // excluded by lmhead_hosts_attn
-  return launch_stream_nl<16, NL, NT, kTop2>(n_rows, hidden, vocab, pl, h, w, part, part2, s,
+  return launch_stream_nl<16, NL, NT, kOut>(n_rows, hidden, vocab, pl, h, w, part, part2, s,
                                              ha);
 }
 
 // NT: 16-position tiles covering n_rows.
-template <int NT, bool kTop2>
+template <int NT, LmOut kOut>
 hipError_t launch_stream(int n_rows, int hidden, int vocab, const void* h, const void* w,
                          Partial* part, float* part2, hipStream_t s, const HostedAttn& ha) {
   const StreamPlan pl = stream_plan(vocab);
   auto go16 = [&](auto nl) {
-    return launch_stream16<nl.value, NT, kTop2>(n_rows, hidden, vocab, pl, h, w, part, part2, s,
+    return launch_stream16<nl.value, NT, kOut>(n_rows, hidden, vocab, pl, h, w, part, part2, s,
                                                 ha);
   };
   if (pl.waves == 16) {
@@ -434,25 +472,25 @@ hipError_t launch_stream(int n_rows, int hidden, int vocab, const void* h, const
   // More than 48 tiles of rows per workgroup: the 8-wave shape has 7 or 8 tiles per wave.
   if constexpr (NT < 4) {
     if (pl.tm == 7)
-      return launch_stream_nl<8, 14, NT, kTop2>(n_rows, hidden, vocab, pl, h, w, part, part2, s,
+      return launch_stream_nl<8, 14, NT, kOut>(n_rows, hidden, vocab, pl, h, w, part, part2, s,
                                                 ha);
     if (pl.tm == 8)
-      return launch_stream_nl<8, 16, NT, kTop2>(n_rows, hidden, vocab, pl, h, w, part, part2, s,
+      return launch_stream_nl<8, 16, NT, kOut>(n_rows, hidden, vocab, pl, h, w, part, part2, s,
                                                 ha);
   }
   return hipErrorInvalidValue;  // excluded by use_stream
 }
 
-template <bool kTop2>
+template <LmOut kOut>
 hipError_t launch_stream_rows(int n_rows, int hidden, int vocab, const void* h, const void* w,
                               Partial* part, float* part2, hipStream_t s,
                               const HostedAttn& ha = HostedAttn{}) {
   if (n_rows <= 16)
-    return launch_stream<1, kTop2>(n_rows, hidden, vocab, h, w, part, part2, s, ha);
+    return launch_stream<1, kOut>(n_rows, hidden, vocab, h, w, part, part2, s, ha);
   if (n_rows <= 32)
-    return launch_stream<2, kTop2>(n_rows, hidden, vocab, h, w, part, part2, s, ha);
+    return launch_stream<2, kOut>(n_rows, hidden, vocab, h, w, part, part2, s, ha);
   if (n_rows <= 64)
-    return launch_stream<4, kTop2>(n_rows, hidden, vocab, h, w, part, part2, s, ha);
+    return launch_stream<4, kOut>(n_rows, hidden, vocab, h, w, part, part2, s, ha);
   return hipErrorInvalidValue;  // excluded by use_stream
 }
 
@@ -672,13 +710,28 @@ struct TileShape {
   static constexpr int kLdsBytes = kH0 + 2 * kHSlot;
 };
 
-template <int TN, bool kTop2>
+// The four values of register r = 0 .. 3 on lanes l % 16 + 16 q, as a 4 x 4 matrix over (r, q),
+// transposed in registers: lane l then holds in element j what lane l % 16 + 16 j held in register
+// l / 16.
+__device__ __forceinline__ f32x4 transpose4(const f32x4& a) {
+  const auto swap16 = [](float x, float y) {
+    return __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+  };
+  const auto lo = swap16(a[0], a[1]), hi = swap16(a[2], a[3]);
+  const auto even = __builtin_amdgcn_permlane32_swap(lo[0], hi[0], false, false);
+  const auto odd = __builtin_amdgcn_permlane32_swap(lo[1], hi[1], false, false);
+  return f32x4{__uint_as_float(even[0]), __uint_as_float(odd[0]), __uint_as_float(even[1]),
+               __uint_as_float(odd[1])};
+}
+
+template <int TN, LmOut kOut>
 __device__ __forceinline__ void tile_run(uint8_t* smem, const uint16_t* __restrict__ h,
                                          const uint16_t* __restrict__ w, int n_rows, int hidden,
                                          int vocab, int n_vtiles, int n_rtiles,
                                          Partial* __restrict__ part, float* __restrict__ part2,
                                          int s0, int step, int s_end, int wave) {
   using Shape = TileShape<TN>;
+  constexpr bool kTop2 = kOut == LmOut::kTop2;
   constexpr int BM = Shape::BM, BN = Shape::BN, BK = Shape::BK, kRowB = Shape::kRowB;
   constexpr int kWSlot = Shape::kWSlot, kHSlot = Shape::kHSlot, kH0 = Shape::kH0;
   constexpr int WM = 2, TM = kTileTM;
@@ -834,31 +887,54 @@ __device__ __forceinline__ void tile_run(uint8_t* smem, const uint16_t* __restri
     if (!pre) wait_vm_lds_and_barrier<0>();  // no DMA in flight
     acc_fence_out(acc);  // every MFMA has written its accumulator before the epilogue reads it
 
-    // Column statistics; the two halves of the vocabulary rows meet through the W slot that the
-    // last stage left, which is loaded again only in step a of the next tile's first stage.
-    Partial* red = reinterpret_cast<Partial*>(smem + w2);  // [WM][BN]
-    float* red2 = reinterpret_cast<float*>(red + WM * BN);
-    const bool full = vt * BM + BM <= vocab;
-    const int vbase = vt * BM + wm * kWaveM + q4;
+    if constexpr (kOut == LmOut::kLogits) {
+      // Lane l holds vocabulary rows 16 tm + 4 r + l / 16 of a column; transposed, 16 tm + 4 (l / 16)
+      // .. + 3: 16 bytes per lane, 64 contiguous bytes per position and 16-row block.
+      const int v0 = vt * BM + wm * kWaveM + 4 * q4;
 #pragma unroll
-    for (int tn = 0; tn < TN; ++tn) {
-      float m2 = kNegBig;
-      const Partial p = column_stats16<TM, TN, kTop2>(acc, tn, vbase, vocab, full, &m2);
-      if (lane < 16) {
-        red[wm * BN + wn * kWaveN + tn * 16 + rho] = p;
-        if (kTop2) red2[wm * BN + wn * kWaveN + tn * 16 + rho] = m2;
+      for (int tn = 0; tn < TN; ++tn) {
+        const int row = rt * BN + wn * kWaveN + tn * 16 + rho;
+        float* const o = reinterpret_cast<float*>(part) + static_cast<size_t>(row) * vocab;
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm) {
+          const f32x4 z = transpose4(acc[tm][tn]);
+          const int v = v0 + 16 * tm;
+          if (row < n_rows && v + 4 <= vocab) {
+            *reinterpret_cast<f32x4u*>(o + v) = z;
+          } else if (row < n_rows) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (v + r < vocab) o[v + r] = z[r];
+          }
+        }
       }
-    }
-    __syncthreads();
-    const int c = threadIdx.x;  // one column per thread
-    if (c < BN) {
-      const Partial p = red[c], o = red[BN + c];
-      const int row = rt * BN + c;
-      if (row < n_rows) {
-        part[static_cast<size_t>(row) * n_vtiles + vt] = partial_merge(p, o);
-        if (kTop2)
-          part2[static_cast<size_t>(row) * n_vtiles + vt] =
-              top2_merge(p.m, red2[c], o.m, red2[BN + c]);
+    } else {
+      // Column statistics; the two halves of the vocabulary rows meet through the W slot that the
+      // last stage left, which is loaded again only in step a of the next tile's first stage.
+      Partial* red = reinterpret_cast<Partial*>(smem + w2);  // [WM][BN]
+      float* red2 = reinterpret_cast<float*>(red + WM * BN);
+      const bool full = vt * BM + BM <= vocab;
+      const int vbase = vt * BM + wm * kWaveM + q4;
+#pragma unroll
+      for (int tn = 0; tn < TN; ++tn) {
+        float m2 = kNegBig;
+        const Partial p = column_stats16<TM, TN, kTop2>(acc, tn, vbase, vocab, full, &m2);
+        if (lane < 16) {
+          red[wm * BN + wn * kWaveN + tn * 16 + rho] = p;
+          if (kTop2) red2[wm * BN + wn * kWaveN + tn * 16 + rho] = m2;
+        }
+      }
+      __syncthreads();
+      const int c = threadIdx.x;  // one column per thread
+      if (c < BN) {
+        const Partial p = red[c], o = red[BN + c];
+        const int row = rt * BN + c;
+        if (row < n_rows) {
+          part[static_cast<size_t>(row) * n_vtiles + vt] = partial_merge(p, o);
+          if (kTop2)
+            part2[static_cast<size_t>(row) * n_vtiles + vt] =
+                top2_merge(p.m, red2[c], o.m, red2[BN + c]);
+        }
       }
     }
     if (!next) break;
@@ -866,12 +942,14 @@ __device__ __forceinline__ void tile_run(uint8_t* smem, const uint16_t* __restri
     vt = nvt;
     rt = nrt;
     src = nsrc;
-    __syncthreads();  // every wave is done with the reduction's slot (and, without pre, the ring)
+    // every wave is done with the reduction's slot (the logits' form takes no LDS; without pre the
+    // barrier above has freed the ring)
+    if constexpr (kOut != LmOut::kLogits) __syncthreads();
     if (!pre) start();
   }
 }
 
-template <int TN, bool kTop2>
+template <int TN, LmOut kOut>
 __global__ __launch_bounds__(256, 1) void lmhead_tile_kernel(
     const uint16_t* __restrict__ h, const uint16_t* __restrict__ w, int n_rows, int hidden,
     int vocab, int n_vtiles, int n_rtiles, Partial* __restrict__ part,
@@ -893,7 +971,7 @@ __global__ __launch_bounds__(256, 1) void lmhead_tile_kernel(
   // the wave index is the same on every lane: taken as a scalar, so the LDS destinations of the
   // loads (M0) are scalar arithmetic
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  tile_run<TN, kTop2>(smem, h, w, n_rows, hidden, vocab, n_vtiles, n_rtiles, part, part2, s0, step,
+  tile_run<TN, kOut>(smem, h, w, n_rows, hidden, vocab, n_vtiles, n_rtiles, part, part2, s0, step,
                       s_end, wave);
 }
 
@@ -904,14 +982,14 @@ __global__ __launch_bounds__(256, 1) void lmhead_tile_kernel(
 // Measured and dropped (with 32x32x16 blocks): 8 waves of 128 x 64 (10.55 ms), 256 x 128 tiles
 // with a ring of 3 at two workgroups per compute unit (11.8 ms), stages reaching LDS through
 // registers (9.65 ms), 384 x 256 tiles (384 accumulators per lane: the compiler spills).
-template <int TN, bool kTop2>
+template <int TN, LmOut kOut>
 hipError_t launch_tile_tn(int n_rows, int hidden, int vocab, const void* h, const void* w,
                           Partial* part, float* part2, hipStream_t s) {
   const int n_vtiles = tile_vtiles(vocab);
   const int n_rtiles = (n_rows + 32 * TN - 1) / (32 * TN);
   const int n_tiles = n_vtiles * n_rtiles;
   const int groups = n_tiles >= kTileGroups ? kTileGroups : n_tiles;
-  hipLaunchKernelGGL((lmhead_tile_kernel<TN, kTop2>), dim3(groups), dim3(256), 0, s,
+  hipLaunchKernelGGL((lmhead_tile_kernel<TN, kOut>), dim3(groups), dim3(256), 0, s,
                      static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(w), n_rows,
                      hidden, vocab, n_vtiles, n_rtiles, part, part2);
   return hipGetLastError();
@@ -939,11 +1017,11 @@ int tile_width(int n_rows, int vocab) {
   return best;
 }
 
-template <bool kTop2>
+template <LmOut kOut>
 hipError_t launch_tile(int n_rows, int hidden, int vocab, const void* h, const void* w,
                        Partial* part, float* part2, hipStream_t s) {
   auto go = [&](auto tn) {
-    return launch_tile_tn<tn.value, kTop2>(n_rows, hidden, vocab, h, w, part, part2, s);
+    return launch_tile_tn<tn.value, kOut>(n_rows, hidden, vocab, h, w, part, part2, s);
   };
   switch (tile_width(n_rows, vocab)) {
     case 3: return go(std::integral_constant<int, 3>{});
@@ -989,10 +1067,11 @@ __device__ __forceinline__ f32x4 load4_f32(const float* __restrict__ row, int co
   return x;
 }
 
-template <int TM, bool kTop2>
+template <int TM, LmOut kOut>
 __global__ __launch_bounds__(kF32Waves * 64) void lmhead_f32_kernel(
     const float* __restrict__ h, const float* __restrict__ w, int n_rows, int hidden, int vocab,
     int n_slices, Partial* __restrict__ part, float* __restrict__ part2) {
+  constexpr bool kTop2 = kOut == LmOut::kTop2;
   constexpr int NT = kF32NT, kRows = 16 * NT;
   __shared__ Partial red[kF32Waves][kRows];
   __shared__ float red2[kF32Waves][kRows];
@@ -1048,6 +1127,10 @@ __global__ __launch_bounds__(kF32Waves * 64) void lmhead_f32_kernel(
     for (int nt = 0; nt < NT; ++nt) b[nt] = load4_f32(hp[nt], col, hidden);
     step(a, b);
   }
+  if constexpr (kOut == LmOut::kLogits) {
+    store_logits(acc, reinterpret_cast<float*>(part), row0, n_rows, vocab, wb, we, lane);
+    return;
+  }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     float m2 = kNegBig;
@@ -1073,18 +1156,18 @@ __global__ __launch_bounds__(kF32Waves * 64) void lmhead_f32_kernel(
   }
 }
 
-template <bool kTop2>
+template <LmOut kOut>
 hipError_t launch_f32(int n_rows, int hidden, int vocab, int n_slices, const void* h,
                       const void* w, Partial* part, float* part2, hipStream_t s) {
   const dim3 grid(n_slices, (n_rows + 16 * kF32NT - 1) / (16 * kF32NT));
   const float* hp = static_cast<const float*>(h);
   const float* wp = static_cast<const float*>(w);
   if (f32_slice_rows(n_rows, vocab) == kF32SliceRows)
-    hipLaunchKernelGGL((lmhead_f32_kernel<kF32SliceRows / 64, kTop2>), grid,
+    hipLaunchKernelGGL((lmhead_f32_kernel<kF32SliceRows / 64, kOut>), grid,
                        dim3(kF32Waves * 64), 0, s, hp, wp, n_rows, hidden, vocab, n_slices, part,
                        part2);
   else
-    hipLaunchKernelGGL((lmhead_f32_kernel<kF32SmallSliceRows / 64, kTop2>), grid,
+    hipLaunchKernelGGL((lmhead_f32_kernel<kF32SmallSliceRows / 64, kOut>), grid,
                        dim3(kF32Waves * 64), 0, s, hp, wp, n_rows, hidden, vocab, n_slices, part,
                        part2);
   return hipGetLastError();
@@ -1158,6 +1241,17 @@ size_t lmhead_ws_bytes(bool bf16, int n_rows, int vocab, bool top2) {
               : max(bytes(n_rows), bytes(min(n_rows, f32_small_slice_rows(vocab))));
 }
 
+template <LmOut kOut>
+static hipError_t launch_lmhead(bool bf16, int n_rows, int hidden, int vocab, const void* h,
+                                const void* w, Partial* part, float* part2, hipStream_t s) {
+  if (!bf16)
+    return launch_f32<kOut>(n_rows, hidden, vocab, lmhead_num_slices(false, n_rows, vocab), h, w,
+                            part, part2, s);
+  if (use_stream(n_rows, vocab))
+    return launch_stream_rows<kOut>(n_rows, hidden, vocab, h, w, part, part2, s);
+  return launch_tile<kOut>(n_rows, hidden, vocab, h, w, part, part2, s);
+}
+
 hipError_t lmhead_partials(bool bf16, int n_rows, int hidden, int vocab, const void* h,
                            const void* w, void* ws, bool top2, hipStream_t s) {
   if (n_rows == 0) return hipSuccess;
@@ -1165,16 +1259,15 @@ hipError_t lmhead_partials(bool bf16, int n_rows, int hidden, int vocab, const v
   float* part2 = top2 ? reinterpret_cast<float*>(static_cast<char*>(ws) +
                                                  lmhead_part_bytes(bf16, n_rows, vocab))
                       : nullptr;
-  if (!bf16) {
-    const int n_slices = lmhead_num_slices(false, n_rows, vocab);
-    return top2 ? launch_f32<true>(n_rows, hidden, vocab, n_slices, h, w, part, part2, s)
-                : launch_f32<false>(n_rows, hidden, vocab, n_slices, h, w, part, part2, s);
-  }
-  if (use_stream(n_rows, vocab))
-    return top2 ? launch_stream_rows<true>(n_rows, hidden, vocab, h, w, part, part2, s)
-                : launch_stream_rows<false>(n_rows, hidden, vocab, h, w, part, part2, s);
-  return top2 ? launch_tile<true>(n_rows, hidden, vocab, h, w, part, part2, s)
-              : launch_tile<false>(n_rows, hidden, vocab, h, w, part, part2, s);
+  return top2 ? launch_lmhead<LmOut::kTop2>(bf16, n_rows, hidden, vocab, h, w, part, part2, s)
+              : launch_lmhead<LmOut::kStats>(bf16, n_rows, hidden, vocab, h, w, part, part2, s);
+}
+
+hipError_t lmhead_logits(bool bf16, int n_rows, int hidden, int vocab, const void* h,
+                         const void* w, float* logits, hipStream_t s) {
+  if (n_rows == 0) return hipSuccess;
+  return launch_lmhead<LmOut::kLogits>(bf16, n_rows, hidden, vocab, h, w,
+                                       reinterpret_cast<Partial*>(logits), nullptr, s);
 }
 
 bool lmhead_hosts_attn(bool bf16, int n_rows, int vocab, const AttnArgs& a) {
@@ -1186,8 +1279,8 @@ hipError_t lmhead_partials_attn(int n_rows, int hidden, int vocab, const void* h
                                 void* ws, const AttnArgs& a, void* attn_ws, hipStream_t s) {
   const SplitPlan sp = split_plan(a.batch, a.max_block, attn_max_keys(a), a.hq, a.hkv);
   const HostedAttn ha{attn_params(a, sp, attn_ws), attn_small_units(a, sp), a.head_dim};
-  return launch_stream_rows<false>(n_rows, hidden, vocab, h, w, static_cast<Partial*>(ws),
-                                   nullptr, s, ha);
+  return launch_stream_rows<LmOut::kStats>(n_rows, hidden, vocab, h, w, static_cast<Partial*>(ws),
+                                           nullptr, s, ha);
 }
 
 hipError_t lmhead_combine(bool bf16, int n_rows, int vocab, const void* ws, float* conf,

@@ -1,0 +1,550 @@
+"""eb_lmhead_logits and eb_sample on the GPU against the oracles: logits within the rounding of their
+sums, every token exactly."""
+import numpy as np
+import pytest
+import torch
+
+from oracle.sample import sample
+from paper_2609_16450_amd import (EB_BF16, EB_F32, EbError, Ragged, eb_lmhead_confidence,
+                                  eb_lmhead_logits, eb_sample, eb_sample_workspace,
+                                  eb_unmask_select)
+
+pytestmark = pytest.mark.gpu
+
+F32, I32 = torch.float32, torch.int32
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _dev(x, dtype=None):
+    t = torch.as_tensor(np.asarray(x))
+    return (t if dtype is None else t.to(dtype)).cuda()
+
+
+# --------------------------------------------------------------------------------------------
+# eb_lmhead_logits
+# --------------------------------------------------------------------------------------------
+def _head(rows, hidden, vocab, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    dt = TYPES[dtype]
+    h = torch.randn(rows, hidden, generator=g).to(dt).cuda()
+    w = (torch.randn(vocab, hidden, generator=g) / hidden ** 0.5).to(dt).cuda()
+    return h, w
+
+
+def _check_logits(h, w, guard=64):
+    """Every logit within the rounding of hidden fp32 additions and products, and not a float behind
+    the last one written."""
+    rows, hidden, vocab = h.shape[0], h.shape[1], w.shape[0]
+    buf = torch.full((rows * vocab + guard,), -7.5, device="cuda")
+    z = buf[:rows * vocab].view(rows, vocab)
+    eb_lmhead_logits(h, w, z)
+    torch.cuda.synchronize()
+    assert (buf[rows * vocab:] == -7.5).all()
+    a, b = h.double().cpu(), w.double().cpu()
+    ref = a @ b.T
+    # each of hidden products and additions is off by 2^-24 of what it gives, at most
+    bound = (hidden + 1) * 2.0 ** -24 * (a.abs() @ b.abs().T) + 1e-30
+    assert ((z.double().cpu() - ref).abs() <= bound).all()
+    return z
+
+
+@pytest.mark.parametrize("rows", [1, 15, 16, 17, 33, 64, 65, 97, 129, 200, 257, 520])
+@pytest.mark.parametrize("hidden,vocab", [(64, 1), (64, 255), (128, 1001), (192, 4099), (640, 33000)])
+def test_logits_bf16(rows, hidden, vocab):
+    print(f"logits bf16 {rows} x {hidden} x {vocab}", flush=True)
+    _check_logits(*_head(rows, hidden, vocab, "bf16", rows))
+
+
+@pytest.mark.parametrize("rows,hidden,vocab", [(1, 64, 126464), (33, 128, 152064), (64, 64, 200000),
+                                               (1, 64, 250003), (300, 64, 126465), (2, 1024, 65537)])
+def test_logits_wide_vocabulary(rows, hidden, vocab):
+    print(f"logits bf16 {rows} x {hidden} x {vocab}", flush=True)
+    _check_logits(*_head(rows, hidden, vocab, "bf16", 7))
+
+
+@pytest.mark.parametrize("rows", [1, 31, 32, 33, 150])
+@pytest.mark.parametrize("hidden,vocab", [(1, 1), (7, 63), (17, 257), (100, 2048), (256, 16400)])
+def test_logits_f32(rows, hidden, vocab):
+    print(f"logits f32 {rows} x {hidden} x {vocab}", flush=True)
+    _check_logits(*_head(rows, hidden, vocab, "f32", rows))
+
+
+@pytest.mark.parametrize("rows,hidden,vocab,dtype", [(32, 512, 50001, "bf16"), (300, 512, 5001, "bf16"),
+                                                     (40, 100, 3001, "f32")])
+def test_logits_are_those_of_the_statistics(rows, hidden, vocab, dtype):
+    """The written logits' largest is max_logit bit for bit, at the argmax, and a row's logits do not
+    depend on how many rows the call has (bf16)."""
+    h, w = _head(rows, hidden, vocab, dtype, 2)
+    z = _check_logits(h, w)
+    conf, ent, top = (torch.zeros(rows, device="cuda") for _ in range(3))
+    arg = torch.zeros(rows, dtype=I32, device="cuda")
+    eb_lmhead_confidence(h, w, conf, ent, arg, max_logit=top)
+    assert torch.equal(z.amax(1), top)
+    assert torch.equal(z.argmax(1).int(), arg)
+    few = torch.zeros(3, vocab, device="cuda")
+    eb_lmhead_logits(h[:3].contiguous(), w, few)
+    if dtype == "bf16":
+        assert torch.equal(few, z[:3])
+
+
+def test_logits_past_2_31_values():
+    """More than 2^31 logits: the last rows of a tall call are those of a short one."""
+    rows, vocab, hidden = 17000, 126465, 64
+    h, w = _head(rows, hidden, vocab, "bf16", 3)
+    z = torch.zeros(rows, vocab, device="cuda")
+    eb_lmhead_logits(h, w, z)
+    few = torch.zeros(70, vocab, device="cuda")
+    eb_lmhead_logits(h[-70:].contiguous(), w, few)
+    assert torch.equal(z[-70:], few)
+    assert float(z[-71].abs().max()) > 0
+
+
+def test_logits_infinities():
+    h, w = _head(70, 64, 300, "bf16", 4)
+    h[3, 5] = float("inf")
+    w[17, 9] = float("nan")
+    z = torch.zeros(70, 300, device="cuda")
+    eb_lmhead_logits(h, w, z)
+    assert z[:, 17].isnan().all()
+    ok = torch.ones(300, dtype=torch.bool)
+    ok[17] = False
+    assert not z[3].isfinite().any()
+    assert z[4][ok.cuda()].isfinite().all()
+
+
+def test_logits_no_rows_and_another_stream():
+    h, w = _head(40, 64, 300, "bf16", 5)
+    eb_lmhead_logits(h[:0].contiguous(), w, torch.zeros(0, 300, device="cuda"))
+    a, b = torch.zeros(40, 300, device="cuda"), torch.zeros(40, 300, device="cuda")
+    eb_lmhead_logits(h, w, a)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    eb_lmhead_logits(h, w, b, stream=s)
+    s.synchronize()
+    assert torch.equal(a, b)
+
+
+def test_logits_refusals():
+    h, w = _head(4, 64, 300, "bf16", 5)
+    with pytest.raises(ValueError, match="logits"):
+        eb_lmhead_logits(h, w, torch.zeros(4, 300, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(ValueError, match="contiguous"):
+        eb_lmhead_logits(h, w, torch.zeros(4, 301, device="cuda")[:, :300])
+    with pytest.raises(ValueError, match="w must"):
+        eb_lmhead_logits(h, w.float(), torch.zeros(4, 300, device="cuda"))
+
+
+# --------------------------------------------------------------------------------------------
+# eb_sample
+# --------------------------------------------------------------------------------------------
+class Draw:
+    """One call: rows of logits [T, V], a random number each, sequences of `blocks` rows with settings."""
+
+    def __init__(self, z, u, blocks=None, temperature=None, top_k=None, top_p=None, min_p=None,
+                 dtype="f32", pad=0):
+        self.dtype = dtype
+        t = torch.as_tensor(np.asarray(z, np.float32)).to(TYPES[dtype])
+        self.T, self.V = t.shape
+        wide = torch.full((self.T, self.V + pad), float("nan"), dtype=t.dtype)
+        wide[:, :self.V] = t
+        self.z, self.logits = t.double().numpy(), wide.cuda()
+        self.u = np.asarray(u, np.float32)
+        self.blocks = [1] * self.T if blocks is None else blocks
+        assert sum(self.blocks) == self.T
+        f = lambda x, dt: None if x is None else np.broadcast_to(np.asarray(x, dt), len(self.blocks))  # noqa: E731,E501
+        self.settings = [f(temperature, np.float32), f(top_k, np.int32), f(top_p, np.float32),
+                         f(min_p, np.float32)]
+        self.ragged = Ragged.from_lengths(self.blocks, [0] * len(self.blocks))
+
+    def run(self, ws=None, stream=None, logits=None):
+        out = [torch.full((self.T,), 99, dtype=dt, device="cuda") for dt in (I32, F32, F32)]
+        names = ("temperature", "top_k", "top_p", "min_p")
+        kw = {n: None if s is None else _dev(s.copy()) for n, s in zip(names, self.settings)}
+        torch.cuda.synchronize()
+        eb_sample(self.ragged, self.logits if logits is None else logits, _dev(self.u), out[0],
+                  prob=out[1], conf=out[2], vocab=self.V, ws=ws, stream=stream, **kw)
+        torch.cuda.synchronize()
+        return [t.cpu().numpy() for t in out]
+
+    def oracle(self):
+        b = np.repeat(np.arange(len(self.blocks)), self.blocks)
+        rows = []
+        for i in range(self.T):
+            s = [d if c is None else c[b[i]].item()
+                 for c, d in zip(self.settings, (1.0, 0, 1.0, 0.0))]
+            rows.append(sample(self.z[i], self.u[i], *s))
+        return rows
+
+    def check(self, **kw):
+        token, prob, conf = self.run(**kw)
+        for i, (t, p, c) in enumerate(self.oracle()):
+            assert token[i] == t, (i, token[i], t, prob[i], p)
+            # prob is formed in 64 bits and rounded once
+            np.testing.assert_allclose(prob[i], p, rtol=2.0 ** -24 * 1.001, atol=2.0 ** -149)
+            np.testing.assert_allclose(conf[i], c, rtol=self.conf_bound(i), atol=2.0 ** -149)
+        return token, prob, conf
+
+    def conf_bound(self, i):
+        """conf's sum: a term exp2(y) has y from a difference and a product with a rounded constant (3
+        roundings of y: 3 2^-24 |y| ln 2 of the term) and an exponential good to 2^-23; terms are added
+        in at most V / 1024 + 32 steps."""
+        z = self.z[i]
+        if not np.isfinite(z.max()):
+            return 0
+        x = z[np.isfinite(z)] - z.max()
+        p = np.exp(x)
+        p /= p.sum()
+        return (2.0 ** -24 * (3 * float((p * -x).sum()) + 2 + len(z) / 1024 + 32 + 2))
+
+
+def _logits(T, V, seed, kind="mixed"):
+    rng = np.random.default_rng(seed)
+    z = rng.standard_normal((T, V)) * rng.uniform(1, 3, (T, 1))
+    if kind == "mixed":
+        for i in range(T):
+            n = min(V, 20)
+            ids = rng.choice(V, n, replace=False)
+            z[i, ids] += np.maximum(rng.uniform(0, 15) - 1.5 * np.log(1 + np.arange(n)), 0)
+    elif kind == "ties":                                # few values: ties at every border
+        z = np.round(z)
+    return z
+
+
+SETTINGS = [
+    dict(), dict(temperature=0.0), dict(temperature=0.7), dict(top_k=1), dict(top_k=20),
+    dict(top_k=1000), dict(top_p=0.9), dict(top_p=0.0), dict(top_p=0.3), dict(top_p=0.9999),
+    dict(min_p=0.05), dict(min_p=1.0), dict(temperature=0.8, top_k=50, top_p=0.9),
+    dict(temperature=1.4, top_k=40, top_p=0.8, min_p=0.02), dict(top_p=0.95, min_p=0.001),
+    dict(temperature=100.0, top_p=0.5), dict(temperature=0.02, top_k=7, top_p=0.99),
+    dict(top_k=30000, top_p=0.97), dict(temperature=0.5, top_k=3000),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["mixed", "plain", "ties"])
+@pytest.mark.parametrize("V", [1, 2, 5, 63, 64, 257, 2047, 2048, 2049, 4100, 32003])
+def test_sample(V, kind, dtype):
+    """Every setting at every size, a few rows each; logits that tie and that do not."""
+    print(f"sample V={V} {kind} {dtype}", flush=True)
+    n = 3
+    z = _logits(n * len(SETTINGS), V, V, kind)
+    u = np.random.default_rng(V + 1).random(len(z))
+    keys = ("temperature", "top_k", "top_p", "min_p")
+    cols = {k: [s.get(k, d) for s in SETTINGS] for k, d in zip(keys, (1.0, 0, 1.0, 0.0))}
+    Draw(z, u, blocks=[n] * len(SETTINGS), dtype=dtype, pad=V % 3, **cols).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("settings", SETTINGS)
+def test_sample_one_row(settings, dtype):
+    """A single row of a large vocabulary, which the call may cut into many pieces."""
+    for seed, kind in ((1, "mixed"), (2, "plain"), (3, "ties")):
+        print(f"sample one row {settings} {dtype} {kind}", flush=True)
+        Draw(_logits(1, 152064, seed, kind), [np.random.default_rng(seed).random()], dtype=dtype,
+             **settings).check()
+
+
+@pytest.mark.parametrize("settings", SETTINGS)
+def test_sample_without_optional_arrays(settings):
+    """NULL for whatever the settings leave out, and no prob or conf."""
+    z = _logits(5, 3000, 6)
+    u = np.random.default_rng(6).random(5)
+    d = Draw(z, u, **settings)
+    d.check()
+    token = torch.zeros(5, dtype=I32, device="cuda")
+    kw = {k: _dev(np.full(5, v, np.int32 if k == "top_k" else np.float32))
+          for k, v in settings.items()}
+    eb_sample(d.ragged, d.logits, _dev(d.u), token, **kw)
+    assert token.tolist() == [t for t, _, _ in d.oracle()]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_random_numbers_at_the_ends(dtype):
+    """u = 0 takes the first kept id, the largest u the last."""
+    z = _logits(12, 5000, 8, "ties")
+    for u in (0.0, 1 - 2.0 ** -24, 2.0 ** -24, 2.0 ** -40, 0.5):
+        Draw(z, [u] * 12, dtype=dtype, top_p=np.linspace(0.1, 1, 12)).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [8, 4096, 65536])
+def test_equal_logits(V, dtype):
+    """All logits equal: sums are whole numbers, and u or top_p on a border are decided exactly; the
+    order is the ids'."""
+    u = [0.0, 0.125, 0.25, 0.375, 0.5, 0.625, 0.75, 0.875]
+    for p, n in ((1.0, V), (0.5, V // 2), (0.25, V // 4)):
+        for value in (0.0, -3.5, 1e30):
+            d = Draw(np.full((8, V), value), u, top_p=p, dtype=dtype)
+            token, prob, conf = d.check()
+            assert token.tolist() == [int(x * n) for x in u]
+            np.testing.assert_allclose(prob, 1 / n, rtol=1e-7)
+    for k in (1, 3, V - 1, V, V + 5):
+        token, _, _ = Draw(np.zeros((8, V)), u, top_k=k, dtype=dtype).check()
+        assert token.tolist() == [int(x * min(k, V)) for x in u]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_signed_zeros_tie(dtype):
+    z = np.where(np.arange(3000) % 2 == 0, -0.0, 0.0)[None].repeat(4, 0)
+    token, _, _ = Draw(z, [0.0, 0.3, 0.6, 0.9], top_k=10, dtype=dtype).check()
+    # (as fp32, 0.3 and 0.6 lie above and 0.9 below: ten times it is 8.99..)
+    assert token.tolist() == [0, 3, 6, 8]
+    token, _, _ = Draw(z, [0.9] * 4, temperature=0.0, dtype=dtype).check()
+    assert token.tolist() == [0] * 4
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("settings", SETTINGS)
+def test_masked_logits(settings, dtype):
+    """-inf in most places, in the first and the last, in all but one and in all; the lowest value of the
+    type; rows of huge spread."""
+    V, rng = 5003, np.random.default_rng(9)
+    z = _logits(9, V, 9)
+    z[0][rng.random(V) < 0.99] = -np.inf
+    z[1][:4000] = -np.inf
+    z[2][17:] = -np.inf
+    z[3][:] = -np.inf
+    z[3][4999] = -2.0
+    z[4][:] = -np.inf
+    low = float(torch.finfo(TYPES[dtype]).min)
+    z[5][rng.random(V) < 0.9] = low
+    z[6][:] = low
+    z[7] *= 1e4
+    z[8] = np.where(rng.random(V) < 0.5, 1e38, -1e38)
+    with np.errstate(invalid="ignore"):
+        token, prob, conf = Draw(z, rng.random(9), dtype=dtype, **settings).check()
+    assert token[3] == 4999 and token[4] == -1 and prob[4] == 0 and conf[4] == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nan_and_inf(dtype):
+    """A NaN or +inf anywhere: token -1, NaN; the rows beside it are as ever."""
+    V = 4100
+    for where in (0, 1, 2048, V - 1):
+        for value in (np.nan, np.inf, -np.nan):
+            z = _logits(5, V, 10)
+            z[1, where] = z[3, where] = value
+            z[3, (where + 5) % V] = -np.inf
+            for settings in (dict(), dict(temperature=0.0), dict(top_k=20, top_p=0.9), dict(min_p=0.1)):
+                d = Draw(z, [0.3] * 5, dtype=dtype, **settings)
+                token, prob, conf = d.run()
+                ref = d.oracle()
+                for i in (0, 2, 4):
+                    assert token[i] == ref[i][0]
+                for i in (1, 3):
+                    assert token[i] == -1 and np.isnan(prob[i]) and np.isnan(conf[i])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_flat_rows(dtype):
+    """Wide nuclei of a large vocabulary, whose borders are found over the whole row."""
+    for V, seed in ((126464, 1), (50001, 2)):
+        print(f"flat rows {V} {dtype}", flush=True)
+        z = np.random.default_rng(seed).standard_normal((8, V))
+        u = np.random.default_rng(seed).random(8)
+        Draw(z, u, dtype=dtype, top_p=[0.1, 0.5, 0.9, 0.99, 0.999, 0.95, 0.7, 0.3],
+             top_k=[0, 0, 0, 0, 0, 60000, 5000, 45000],
+             temperature=[1, 1, 1, 3, 1, 1, 0.5, 2], min_p=[0, 0, 0, 0, 0, 0.001, 0, 0.01]).check()
+
+
+def test_largest_vocabulary():
+    V = 1 << 21
+    z = np.random.default_rng(11).standard_normal((3, V))
+    d = Draw(z, [0.2, 0.999, 0.5], top_p=[1.0, 0.9, 0.8], top_k=[0, 0, 100000])
+    d.check()
+    with pytest.raises(EbError, match="UNSUPPORTED"):
+        eb_sample(Ragged.from_lengths([1], [0]), torch.zeros(1, V + 1, device="cuda"),
+                  torch.zeros(1, device="cuda"), torch.zeros(1, dtype=I32, device="cuda"))
+
+
+def test_rows_past_2_31_values():
+    """Logits whose offsets pass 2^31: the last rows of a tall call are those of a short one."""
+    T, V = 21500, 100003
+    z = torch.empty(T, V, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, T, 500):
+        z[i:i + 500].normal_()
+    u = torch.rand(T, device="cuda")
+    t1, t2 = torch.zeros(T, dtype=I32, device="cuda"), torch.zeros(300, dtype=I32, device="cuda")
+    eb_sample(Ragged.from_lengths([T], [0]), z, u, t1, top_k=_dev([50], I32))
+    eb_sample(Ragged.from_lengths([300], [0]), z[-300:].contiguous(), u[-300:].contiguous(), t2,
+              top_k=_dev([50], I32))
+    assert torch.equal(t1[-300:], t2)
+    assert int(t1.max()) < V and int(t1.min()) >= 0
+
+
+@pytest.mark.parametrize("T", [1, 2, 7, 31, 32, 100, 255, 256, 257, 600])
+def test_row_counts(T):
+    """However many rows, a row's token, prob and conf are the same."""
+    V = 20011
+    z = _logits(600, V, 12)
+    u = np.random.default_rng(12).random(600)
+    kw = dict(top_p=0.9, temperature=0.9)
+    if not hasattr(test_row_counts, "ref"):
+        test_row_counts.ref = Draw(z, u, **kw).check()
+    for got, want in zip(Draw(z[:T], u[:T], **kw).run(), test_row_counts.ref):
+        np.testing.assert_array_equal(got, want[:T])
+
+
+def test_ragged_batch():
+    """Settings go by sequence, through empty blocks, over more than 64 sequences."""
+    rng = np.random.default_rng(13)
+    blocks = [int(x) for x in rng.integers(0, 4, 150)]
+    T = sum(blocks)
+    Draw(_logits(T, 700, 13), rng.random(T), blocks=blocks, temperature=rng.uniform(0, 2, 150),
+         top_k=rng.integers(-1, 900, 150), top_p=rng.uniform(0, 1.1, 150),
+         min_p=rng.uniform(-0.1, 0.2, 150)).check()
+
+
+def test_no_rows():
+    r = Ragged.from_lengths([0, 0], [0, 0])
+    eb_sample(r, torch.zeros(0, 50, device="cuda"), torch.zeros(0, device="cuda"),
+              torch.zeros(0, dtype=I32, device="cuda"))
+
+
+@pytest.mark.parametrize("T,V", [(1, 152064), (5, 32003), (300, 9001)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_workspace_is_enough(T, V, dtype):
+    """Exactly the workspace that the query gives, with bytes of garbage inside and a guard behind; the
+    answer is the same in a larger one and in none given."""
+    z, u = _logits(T, V, 14), np.random.default_rng(14).random(T)
+    d = Draw(z, u, dtype=dtype, top_p=0.9, top_k=40000)
+    need = eb_sample_workspace(EB_BF16 if dtype == "bf16" else EB_F32, T, V)
+    want = d.run()
+    for fill in (0, 0xFF, 0x7F):
+        buf = torch.full((need + 256,), fill, dtype=torch.uint8, device="cuda")
+        buf[need:] = 0x5A
+        got = d.run(ws=buf[:need])
+        assert (buf[need:] == 0x5A).all()
+        for a, b in zip(got, want):
+            np.testing.assert_array_equal(a, b)
+    if need:
+        with pytest.raises(EbError, match="WORKSPACE"):
+            d.run(ws=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+
+
+def test_logits_at_any_element():
+    """Logits that begin at any element of their storage, with rows of any pitch."""
+    for dtype in ("f32", "bf16"):
+        for off, pitch in ((1, 2051), (3, 2048), (5, 3000)):
+            d = Draw(_logits(6, 2047, 15), np.random.default_rng(15).random(6), dtype=dtype,
+                     top_p=0.8)
+            store = torch.full((off + 6 * pitch,), float("nan"), dtype=TYPES[dtype], device="cuda")
+            view = store[off:].view(6, pitch)
+            view[:, :2047] = d.logits[:, :2047]
+            token, _, _ = d.run(logits=view)
+            assert token.tolist() == [t for t, _, _ in d.oracle()]
+
+
+def test_another_stream_and_two_at_once():
+    d = [Draw(_logits(40, 30011, 16 + i), np.random.default_rng(i).random(40), top_p=0.9)
+         for i in range(2)]
+    want = [x.check()[0] for x in d]
+    streams = [torch.cuda.Stream() for _ in d]
+    assert d[0].run(stream=streams[0])[0].tolist() == want[0].tolist()
+    out = [torch.zeros(40, dtype=I32, device="cuda") for _ in d]
+    args = [(x.ragged, x.logits, _dev(x.u), o, _dev(x.settings[2].copy()))
+            for x, o in zip(d, out)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (r, z, u, o, p), s in zip(args, streams):
+            eb_sample(r, z, u, o, top_p=p, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(out, want):
+        assert o.tolist() == w.tolist()
+
+
+@pytest.mark.parametrize("T,V", [(1, 152064), (40, 9001), (300, 3001)])
+def test_captured_and_replayed(T, V):
+    """Logits, draw and commit in one graph; two graphs that share a workspace; replays with new inputs in
+    the same tensors and eager work in between."""
+    print(f"graph {T} {V}", flush=True)
+    h, w = _head(T, 64, V, "bf16", 17)
+    r = Ragged.from_lengths([T], [0])
+    u = torch.rand(T, device="cuda")
+    z, conf = torch.zeros(T, V, device="cuda"), torch.zeros(T, device="cuda")
+    ws = torch.empty(max(1, eb_sample_workspace(EB_F32, T, V)), dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for kw in (dict(top_p=_dev([0.9], F32)), dict(top_k=_dev([30], I32), temperature=_dev([0.7], F32))):
+        tok = torch.zeros(T, dtype=I32, device="cuda")
+        state = [torch.ones(T, dtype=torch.uint8, device="cuda"), torch.zeros(T, dtype=I32, device="cuda"),
+                 torch.zeros(T, dtype=torch.uint8, device="cuda"),
+                 torch.zeros(1, dtype=I32, device="cuda"), torch.zeros(1, dtype=torch.uint8, device="cuda")]
+        tau = torch.full((1,), 0.01, device="cuda")
+
+        def go(tok=tok, kw=kw, state=state, tau=tau):
+            state[0].fill_(1)
+            eb_lmhead_logits(h, w, z)
+            eb_sample(r, z, u, tok, conf=conf, ws=ws, **kw)
+            eb_unmask_select(r, conf, tok, tau, *state)
+
+        go()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            go()
+        graphs.append((g, go))
+        outs.append([tok, *state])
+    for i in range(3):
+        h.normal_()
+        u.uniform_()
+        for (g, go), out in zip(graphs, outs):
+            for t in out:
+                t.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            got = [t.clone() for t in out]
+            (h.float() @ h.float().t()).sum().item()
+            go()
+            torch.cuda.synchronize()
+            for a, b in zip(got, out):
+                assert torch.equal(a, b), i
+
+
+def test_draws_follow_the_distribution():
+    """Evenly spaced random numbers draw every id as often as its probability says."""
+    z = np.log(np.array([1.0, 2, 3, 4, 6, 16]))
+    n = 3200
+    token, _, _ = Draw(np.repeat(z[None], n, 0), (np.arange(n) + 0.5) / n).run()
+    assert np.bincount(token).tolist() == [100, 200, 300, 400, 600, 1600]
+
+
+def test_sample_refusals():
+    d = Draw(_logits(3, 100, 18), [0.5] * 3)
+    z, u, r = d.logits, _dev(d.u), d.ragged
+    tok = torch.zeros(3, dtype=I32, device="cuda")
+    with pytest.raises(ValueError, match="uniform"):
+        eb_sample(r, z, u[:2], tok)
+    with pytest.raises(ValueError, match="token"):
+        eb_sample(r, z, u, tok.long())
+    with pytest.raises(ValueError, match="dtype"):
+        eb_sample(r, z.half(), u, tok)
+    with pytest.raises(ValueError, match="logits"):
+        eb_sample(r, z[:2].contiguous(), u, tok)
+    with pytest.raises(ValueError, match="contiguous"):
+        eb_sample(r, z.t().contiguous().t(), u, tok)
+    with pytest.raises(ValueError, match="top_k"):
+        eb_sample(r, z, u, tok, top_k=torch.zeros(3, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError, match="min_p"):
+        eb_sample(r, z, u, tok, min_p=torch.zeros(2, device="cuda"))
+    with pytest.raises(EbError, match="pitch"):
+        eb_sample(r, z, u, tok, vocab=101)
+    with pytest.raises(EbError, match="vocab"):
+        eb_sample(r, z, u, tok, vocab=0)
+
+
+def test_debug_checks(monkeypatch):
+    monkeypatch.setenv("EB_DEBUG_CHECKS", "1")
+    z, ok = _logits(3, 100, 19), [0.0, 0.5, 1 - 2.0 ** -24]
+    Draw(z, ok, temperature=0.0, top_p=1.0, min_p=1.0).check()
+    for bad in (dict(u=[0.0, 1.0, 0.5]), dict(u=[0.0, np.nan, 0.5]), dict(u=[-0.1, 0.0, 0.5])):
+        with pytest.raises(EbError, match="uniform"):
+            Draw(z, bad["u"]).run()
+    for name, value in (("temperature", -1.0), ("temperature", np.nan), ("top_p", 1.5),
+                        ("min_p", -0.5)):
+        with pytest.raises(EbError, match=name):
+            Draw(z, ok, **{name: value}).run()
+    d = Draw(z, ok, blocks=[1, 2])
+    d.ragged.cu_block = _dev([0, 2, 3], I32)
+    d.ragged.max_block = 1
+    with pytest.raises(EbError, match="cu_block"):
+        d.run()
