@@ -735,8 +735,9 @@ eb_status eb_lmhead_logits(eb_dtype dt, int n_rows, int hidden, int vocab, const
 }
 
 size_t eb_sample_workspace(eb_dtype dt, int n_rows, int vocab) {
+  (void)dt;
   if (n_rows <= 0 || vocab <= 0 || vocab > eb::kSampleMaxVocab) return 0;
-  return round_up(eb::sample_ws_bytes(dt == EB_BF16, n_rows, vocab));
+  return round_up(eb::sample_ws_bytes(n_rows, vocab));
 }
 
 eb_status eb_sample(eb_dtype dt, const eb_ragged* r, int vocab, int64_t pitch, const void* logits,
@@ -751,6 +752,9 @@ eb_status eb_sample(eb_dtype dt, const eb_ragged* r, int vocab, int64_t pitch, c
   if (vocab > eb::kSampleMaxVocab)
     return fail(EB_ERR_UNSUPPORTED, "vocab %d not supported (at most %d)", vocab,
                 eb::kSampleMaxVocab);
+  if (eb::sample_threads(r->total_block, vocab) > UINT32_MAX)
+    return fail(EB_ERR_UNSUPPORTED, "%d rows of %d logits do not fit one launch", r->total_block,
+                vocab);
   if (r->total_block > 0 && (!logits || !uniform || !token))
     return fail(EB_ERR_INVALID, "NULL logits / uniform / token");
   const size_t need = eb_sample_workspace(dt, r->total_block, vocab);

@@ -131,7 +131,9 @@ struct SampleArgs {
   float* prob;  // nullable
   float* conf;  // nullable
 };
-size_t sample_ws_bytes(bool bf16, int n_rows, int vocab);
+size_t sample_ws_bytes(int n_rows, int vocab);
+// Threads of the call's largest launch (a launch has fewer than 2^32).
+long sample_threads(int n_rows, int vocab);
 hipError_t sample(bool bf16, const SampleArgs& a, void* ws, hipStream_t s);
 
 // ---- measurement aid -------------------------------------------------------------------
