@@ -331,7 +331,7 @@ eb_status eb_lmhead_logits(eb_dtype dt, int n_rows, int hidden, int vocab, const
  *              where it is the top-1 token; with token the conf and argmax of eb_unmask_select
  *
  * temperature[b] <= 0 takes the first of the order (prob 1).  An id whose logit is -inf, or whose w
- * underflows in 64 bits, is never drawn.  A row with no logit above -inf gets token -1 and prob and
+ * is below 2^-980, is never drawn.  A row with no logit above -inf gets token -1 and prob and
  * conf 0; one with a NaN or +inf token -1 and NaN.
  *
  *   logits [T, pitch] of dtype dt, of which the first vocab columns are read (pitch >= vocab, in

@@ -35,10 +35,13 @@ constexpr int kSegment = 2048;         // ids that a wave takes at a time
 constexpr int kGroup = kSegment / 64;  // of them a lane's
 constexpr int kScanThreads = 256;
 constexpr int kScanWaves = kScanThreads / 64;
-constexpr int kThreads = 1024;  // of the workgroup that picks
+constexpr int kPickThreads = 256;
+constexpr int kPickWaves = kPickThreads / 64;
+constexpr int kPickList = kPickThreads;  // ids that the second launch settles a row among
+constexpr int kThreads = 1024;           // of a workgroup that searches
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxSegments = kThreads;
-constexpr int kList = kThreads;  // ids that are sorted in LDS
+constexpr int kList = kThreads;  // ids that it sorts in LDS
 constexpr int kBins = 2048;
 static_assert(kMaxSegments * kSegment >= kSampleMaxVocab, "a thread per segment");
 
@@ -55,31 +58,39 @@ __device__ __forceinline__ int id_in_segment(int i, int lane) {
   return (i * 64 + lane) * kVec<T>;
 }
 
-// Logits at .. at + kVec - 1 of a row; -inf behind its end.
-__device__ __forceinline__ void load_logits(const float* row, int at, int vocab, float (&z)[4]) {
-  if (at + 4 <= vocab) {
-    const f32x4 x = *reinterpret_cast<const f32x4u*>(row + at);
+// Logits at .. at + kVec - 1 of a row, as they came; -inf behind its end.
+template <class T>
+struct Chunk;
+template <>
+struct Chunk<float> {
+  f32x4 x;
+  __device__ __forceinline__ void load(const float* row, int at, int vocab) {
+    if (at + 4 <= vocab) {
+      x = *reinterpret_cast<const f32x4u*>(row + at);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = x[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = at + e < vocab ? row[at + e] : -INFINITY;
-  }
-}
-__device__ __forceinline__ void load_logits(const uint16_t* row, int at, int vocab, float (&z)[8]) {
-  if (at + 8 <= vocab) {
-    const u32x4 x = *reinterpret_cast<const u32x4h*>(row + at);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t w = x[e / 2];
-      z[e] = __uint_as_float(e % 2 ? w & 0xffff0000u : w << 16);
+      for (int e = 0; e < 4; ++e) x[e] = at + e < vocab ? row[at + e] : -INFINITY;
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      z[e] = at + e < vocab ? bf16_bits_to_f32(row[at + e]) : -INFINITY;
   }
-}
+  __device__ __forceinline__ float operator[](int e) const { return x[e]; }
+};
+template <>
+struct Chunk<uint16_t> {
+  u32x4 x;
+  __device__ __forceinline__ void load(const uint16_t* row, int at, int vocab) {
+    if (at + 8 <= vocab) {
+      x = *reinterpret_cast<const u32x4h*>(row + at);
+    } else {
+      auto bits = [&](int e) -> uint32_t { return at + e < vocab ? row[at + e] : 0xff80u; };
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = bits(2 * i) | bits(2 * i + 1) << 16;
+    }
+  }
+  __device__ __forceinline__ float operator[](int e) const {
+    const uint32_t w = x[e / 2];
+    return __uint_as_float(e % 2 ? w & 0xffff0000u : w << 16);
+  }
+};
 __device__ __forceinline__ float load_logit(const float* row, int id) { return row[id]; }
 __device__ __forceinline__ float load_logit(const uint16_t* row, int id) {
   return bf16_bits_to_f32(row[id]);
@@ -94,39 +105,64 @@ __device__ __forceinline__ float key_logit(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
-// 2^(i / 16)
-__constant__ const double kPow16[16] = {
-    0x1.0000000000000p+0, 0x1.0b5586cf9890fp+0, 0x1.172b83c7d517bp+0, 0x1.2387a6e756238p+0,
-    0x1.306fe0a31b715p+0, 0x1.3dea64c123422p+0, 0x1.4bfdad5362a27p+0, 0x1.5ab07dd485429p+0,
-    0x1.6a09e667f3bcdp+0, 0x1.7a11473eb0187p+0, 0x1.8ace5422aa0dbp+0, 0x1.9c49182a3f090p+0,
-    0x1.ae89f995ad3adp+0, 0x1.c199bdd85529cp+0, 0x1.d5818dcfba487p+0, 0x1.ea4afa2a490dap+0};
+// 2^(i / 64)
+__constant__ const double kPow64[64] = {
+    0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0e3ec32d3d1a2p+0, 0x1.11301d0125b51p+0, 0x1.1429aaea92de0p+0,
+    0x1.172b83c7d517bp+0, 0x1.1a35beb6fcb75p+0, 0x1.1d4873168b9aap+0, 0x1.2063b88628cd6p+0,
+    0x1.2387a6e756238p+0, 0x1.26b4565e27cddp+0, 0x1.29e9df51fdee1p+0, 0x1.2d285a6e4030bp+0,
+    0x1.306fe0a31b715p+0, 0x1.33c08b26416ffp+0, 0x1.371a7373aa9cbp+0, 0x1.3a7db34e59ff7p+0,
+    0x1.3dea64c123422p+0, 0x1.4160a21f72e2ap+0, 0x1.44e086061892dp+0, 0x1.486a2b5c13cd0p+0,
+    0x1.4bfdad5362a27p+0, 0x1.4f9b2769d2ca7p+0, 0x1.5342b569d4f82p+0, 0x1.56f4736b527dap+0,
+    0x1.5ab07dd485429p+0, 0x1.5e76f15ad2148p+0, 0x1.6247eb03a5585p+0, 0x1.6623882552225p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6dfb23c651a2fp+0, 0x1.71f75e8ec5f74p+0, 0x1.75feb564267c9p+0,
+    0x1.7a11473eb0187p+0, 0x1.7e2f336cf4e62p+0, 0x1.82589994cce13p+0, 0x1.868d99b4492edp+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8f1ae99157736p+0, 0x1.93737b0cdc5e5p+0, 0x1.97d829fde4e50p+0,
+    0x1.9c49182a3f090p+0, 0x1.a0c667b5de565p+0, 0x1.a5503b23e255dp+0, 0x1.a9e6b5579fdbfp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b33a2b84f15fbp+0, 0x1.b7f76f2fb5e47p+0, 0x1.bcc1e904bc1d2p+0,
+    0x1.c199bdd85529cp+0, 0x1.c67f12e57d14bp+0, 0x1.cb720dcef9069p+0, 0x1.d072d4a07897cp+0,
+    0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
+    0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0};
 
-// exp((z - top) / temperature) in 64 bits.  With y = (z - top) 16 log2(e) / temperature and n the
-// whole number nearest to y, it is 2^(n / 16) 2^((y - n) / 16): a table (of 16 values, which the
-// lanes of a wave read from LDS without a conflict) and the power series of the exponential to the fifth
-// term, |y - n| <= 1/2, which leaves less than 2^-42 of the value.  A weight's error of that size moves
-// a border of the draw by as much of the sum at most, and one in 10^10 draws across it.
+// exp((z - top) / temperature) in 64 bits.  With y = (z - top) 64 log2(e) / temperature and n the
+// whole number nearest to y, it is 2^(n / 64) 2^((y - n) / 64): a table in LDS and a polynomial in
+// y - n (|y - n| <= 1/2) of the third degree, 1 at 0 and otherwise as near as one comes, which leaves
+// 2^-37 of the value at most.  (A weight's error of that size moves a border of the draw by as much
+// of the weight: one in 10^8 draws from 100000 ids of like weight across it.)  n comes from the low
+// bits of y + 1.5 2^52, and 2^(n / 64 rounded down) goes into the result's exponent.
+// What a pass over a row costs is its weights: with 16 table values and a fifth degree 41 us for 131072 on
+// one compute unit, 20 us of them the weights.
 struct Weights {
-  const double* pow16;  // LDS
-  double top, rate;     // largest logit; 16 log2(e) / temperature
-  __device__ __forceinline__ double operator()(float z) const {
-    constexpr double c1 = 0x1.62e42fefa39efp-5, c2 = 0x1.ebfbdff82c58fp-11,
-                     c3 = 0x1.c6b08d704a0c0p-17, c4 = 0x1.3b2ab6fba4e77p-23,
-                     c5 = 0x1.5d87fe78a6731p-30;  // (ln 2 / 16)^k / k!
-    // (z = -inf ends at the lower bound, whose power is 0)
-    const double y = fmax((static_cast<double>(z) - top) * rate, -20000.0);
-    const double n = rint(y), r = y - n;
-    const int k = static_cast<int>(n);
-    const double p = fma(r, fma(r, fma(r, fma(r, fma(r, c5, c4), c3), c2), c1), 1.0);
-    return ldexp(pow16[k & 15] * p, k >> 4);
+  const double* pow64;  // LDS
+  double top, rate;     // largest logit; 64 log2(e) / temperature
+  // Not 0 but 2^-1000 or so where that is the value or less, -inf among it.
+  __device__ __forceinline__ double normal(float z) const {
+    // the power series of exp(x ln 2 / 64) with the fourth term's best parabola in place of it
+    constexpr double c1 = 0x1.62e42fefa39efp-7, c2 = 0x1.ebfc213e1c4f7p-15,
+                     c3 = 0x1.c6b08d704a0c0p-23;
+    constexpr double kRound = 0x1.8p52;
+    const double y = fmax((static_cast<double>(z) - top) * rate, kLeast);
+    const double shifted = y + kRound, r = y - (shifted - kRound);
+    const int k = static_cast<int>(__double_as_longlong(shifted));  // low word
+    const double p = fma(r, fma(r, fma(r, c3, c2), c1), 1.0);
+    const uint64_t x = __double_as_longlong(pow64[k & 63] * p);
+    return __longlong_as_double(x + (static_cast<uint64_t>(static_cast<uint32_t>(k >> 6)) << 52));
   }
+  __device__ __forceinline__ double operator()(float z) const {
+    const double x = normal(z);
+    return x > kNothing ? x : 0.0;
+  }
+  static constexpr double kLeast = -64000.0;  // in y
+  // Weights up to this one are 0; what normal() gives for those below 2^-1000, a segment of them
+  // summed up too.
+  static constexpr double kNothing = 0x1p-980;
 };
 __device__ __forceinline__ double weight_rate(float temperature) {
-  return 0x1.71547652b82fep+4 / static_cast<double>(temperature);  // 16 log2(e) / t
+  return 0x1.71547652b82fep+6 / static_cast<double>(temperature);  // 64 log2(e) / t
 }
 // Weights as whole numbers of 1 / scale, a power of two; one that is not 0 counts at least 1.
 __device__ __forceinline__ uint64_t whole(double w, double scale) {
-  return w > 0.0 ? max(static_cast<uint64_t>(rint(w * scale)), uint64_t{1}) : 0;
+  return w > Weights::kNothing ? max(static_cast<uint64_t>(rint(w * scale)), uint64_t{1}) : 0;
 }
 
 // Kept: above key, or equal to it with an id of at most last.
@@ -151,11 +187,19 @@ struct alignas(8) SegmentStats {
 };
 static_assert(sizeof(SegmentStats) == 24, "packed");
 
-// A row's settings and whether it is one of few kept ids by count.
+// Top-k small enough to be settled by the second launch: half the list, so that the ids which the
+// groups' largest logits let through besides fit as well.
+constexpr int kFewIds = kPickList / 2;
+
+// A row's settings.
 struct Settings {
   float temperature, top_p, min_p;
   int32_t top_k;  // 0: no limit
   __device__ __forceinline__ bool greedy() const { return !(temperature > 0.f); }
+  __device__ __forceinline__ bool few() const { return top_k > 0 && top_k <= kFewIds; }
+  __device__ __forceinline__ bool limited() const {
+    return top_k > 0 || top_p < 1.f || min_p > 0.f;
+  }
 };
 __device__ __forceinline__ Settings settings(const SampleArgs& a, int b) {
   Settings s;
@@ -166,15 +210,28 @@ __device__ __forceinline__ Settings settings(const SampleArgs& a, int b) {
   s.top_k = k > 0 && k < a.vocab ? k : 0;
   return s;
 }
-// Top-k small enough to be settled in LDS: half the list, so that the ids which the groups' largest
-// logits let through besides fit as well.
-constexpr int kFewIds = kList / 2;
-
 struct Workspace {
   SegmentStats* stats;  // [n_rows, segments]
   float* group_top;     // [n_rows, segments, 64]: largest logit of a lane's ids
+  uint32_t* pending;    // [n_rows]: the second launch has left it to the third
   int segments;
 };
+
+// x, which is the same on every lane, as a scalar: what depends on it alone takes no vector registers,
+// and branches on it no lane masks.
+template <class V>
+__device__ __forceinline__ V uniform(V x) {
+  static_assert(sizeof(V) == 4 || sizeof(V) == 8, "one or two words");
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(
+        V, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int32_t, x)));
+  } else {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(b));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(b >> 32));
+    return __builtin_bit_cast(V, static_cast<uint64_t>(hi) << 32 | lo);
+  }
+}
 
 template <class V, class Op>
 __device__ __forceinline__ V wave_reduce(V x, Op op) {
@@ -201,17 +258,17 @@ struct Min {
 // ---------------------------------------------------------------------------------------
 template <class T>
 __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(SampleArgs a, Workspace ws) {
-  __shared__ double pow16[16];
+  __shared__ double pow64[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int parts = (ws.segments + kScanWaves - 1) / kScanWaves;
   const int r = blockIdx.x / parts;
   const int g = (blockIdx.x - r * parts) * kScanWaves + wave;
   const T* const row = static_cast<const T*>(a.logits) + static_cast<size_t>(r) * a.pitch;
-  float z[kLoads<T>][kVec<T>];
+  Chunk<T> z[kLoads<T>];
 #pragma unroll
   for (int i = 0; i < kLoads<T>; ++i)
-    load_logits(row, g * kSegment + id_in_segment<T>(i, lane), a.vocab, z[i]);
-  if (threadIdx.x < 16) pow16[threadIdx.x] = kPow16[threadIdx.x];
+    z[i].load(row, g * kSegment + id_in_segment<T>(i, lane), a.vocab);
+  if (threadIdx.x < 64) pow64[threadIdx.x] = kPow64[threadIdx.x];
   const Settings st = settings(a, find_sequence(a.cu_block, a.batch, r, lane));
   __syncthreads();
   if (g >= ws.segments) return;
@@ -233,28 +290,452 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(SampleArgs a,
   bad = __any(bad);
   SegmentStats out{bad ? NAN : top, low, 0.f, 0.f, 0.0};
   if (top > -INFINITY && !bad) {  // (else every difference would be NaN)
-    if (a.conf) {
+    // rows of few ids by count, and greedy ones, take no sum over all
+    const bool sum = !st.greedy() && !st.few();
+    if (sum) {
+      const Weights w{pow64, static_cast<double>(top), weight_rate(st.temperature)};
+#pragma unroll
+      for (int i = 0; i < kLoads<T>; ++i)
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e) out.sum += w.normal(z[i][e]);
+      out.sum = wave_reduce(out.sum, Add{});
+      out.soft = static_cast<float>(out.sum);  // (at temperature 1)
+    }
+    if (a.conf && !(sum && st.temperature == 1.f)) {
+      out.soft = 0.f;
 #pragma unroll
       for (int i = 0; i < kLoads<T>; ++i)
 #pragma unroll
         for (int e = 0; e < kVec<T>; ++e) out.soft += fast_exp2((z[i][e] - top) * kLog2e);
       out.soft = wave_reduce(out.soft, Add{});
     }
-    // rows of few ids by count, and greedy ones, take no sum over all
-    if (!st.greedy() && (st.top_k == 0 || st.top_k > kFewIds)) {
-      const Weights w{pow16, static_cast<double>(top), weight_rate(st.temperature)};
-#pragma unroll
-      for (int i = 0; i < kLoads<T>; ++i)
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) out.sum += w(z[i][e]);
-      out.sum = wave_reduce(out.sum, Add{});
-    }
   }
   if (lane == 0) ws.stats[at] = out;
 }
 
 // ---------------------------------------------------------------------------------------
-// Second launch: a workgroup per row.
+// What the later launches share.
+// ---------------------------------------------------------------------------------------
+__device__ __forceinline__ int wave_index() {
+  return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+}
+
+// x over the kN waves of the workgroup, on every thread; `slots` [kN] is free again behind the next
+// barrier.
+template <int kN, class V, class Op>
+__device__ __forceinline__ V block_reduce(V x, V* slots, Op op) {
+  x = wave_reduce(x, op);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = x;
+  __syncthreads();
+  V y = slots[0];
+#pragma unroll
+  for (int w = 1; w < kN; ++w) y = op(y, slots[w]);
+  return uniform(y);
+}
+
+// Sum of x over this lane and the lanes before it.
+template <class V>
+__device__ __forceinline__ V wave_scan(V x) {
+  const int lane = threadIdx.x & 63;
+  for (int n = 1; n < 64; n <<= 1) {
+    const V o = __shfl_up(x, n);
+    if (lane >= n) x += o;
+  }
+  return x;
+}
+
+// Sum of x over the threads before this one; `total` over all.
+template <int kN, class V>
+__device__ __forceinline__ V block_scan(V x, V* slots, V& total) {
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  const V sum = wave_scan(x);
+  __syncthreads();
+  if (lane == 63) slots[wave] = sum;
+  __syncthreads();
+  V before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kN; ++w) {
+    if (w == wave) before = all;
+    all += slots[w];
+  }
+  total = uniform(all);
+  return before + sum - x;
+}
+
+// floor(sum * x) for x in [0, 1) (bits of x below 2^-64 are left out).
+__device__ __forceinline__ uint64_t part_of(uint64_t sum, float x) {
+  return __umul64hi(sum, static_cast<uint64_t>(static_cast<double>(x) * 0x1p64));
+}
+// The least whole number >= max(sum * p, 1), for p < 1.
+__device__ __forceinline__ uint64_t share_of(uint64_t sum, float p) {
+  const uint64_t q = static_cast<uint64_t>(static_cast<double>(fmaxf(p, 0.f)) * 0x1p64);
+  return max(__umul64hi(sum, q) + (sum * q != 0), uint64_t{1});
+}
+
+// A list's entry: (key, ~id), so that the order is that of falling entries.
+__device__ __forceinline__ uint64_t entry_of(float z, int id) {
+  return static_cast<uint64_t>(order_key(z)) << 32 | ~static_cast<uint32_t>(id);
+}
+__device__ __forceinline__ uint32_t entry_key(uint64_t x) { return static_cast<uint32_t>(x >> 32); }
+__device__ __forceinline__ int entry_id(uint64_t x) {
+  return static_cast<int>(~static_cast<uint32_t>(x));
+}
+
+// A row, as a workgroup of any size sees it.  Every wave reduces the segments' statistics by itself,
+// without barriers, and all come to the same bits.
+template <class T>
+struct Row {
+  const T* logits;
+  const SegmentStats* stats;
+  const float* group_top;
+  int r, vocab, segments;
+  Settings st;
+  float top, low;
+  Weights w;
+  double scale;
+  uint64_t whole_sum;  // of all weights, as whole numbers
+
+  // False where the row has a NaN or +inf, or nothing to draw from; its outputs are then written.
+  __device__ __forceinline__ bool open(const SampleArgs& a, const Workspace& ws, int row,
+                                       const double* pow64) {
+    const int lane = threadIdx.x & 63;
+    r = row;
+    logits = static_cast<const T*>(a.logits) + static_cast<size_t>(r) * a.pitch;
+    stats = ws.stats + static_cast<size_t>(r) * ws.segments;
+    group_top = ws.group_top + static_cast<size_t>(r) * ws.segments * 64;
+    vocab = a.vocab;
+    segments = ws.segments;
+    float hi = -INFINITY, lo = INFINITY;
+    bool bad = false;
+    for (int g = lane; g < segments; g += 64) {
+      bad |= stats[g].top != stats[g].top;
+      hi = fmaxf(hi, stats[g].top);
+      lo = fminf(lo, stats[g].low);
+    }
+    st = settings(a, find_sequence(a.cu_block, a.batch, r, lane));
+    top = uniform(wave_reduce(hi, Max{}));
+    low = uniform(wave_reduce(lo, Min{}));
+    bad = __any(bad);
+    w = Weights{pow64, static_cast<double>(top), weight_rate(st.temperature)};
+    if (!bad && top > -INFINITY) return true;
+    if (threadIdx.x == 0) {
+      a.token[r] = -1;
+      const float none = bad ? NAN : 0.f;
+      if (a.prob) a.prob[r] = none;
+      if (a.conf) a.conf[r] = none;
+      ws.pending[r] = 0;
+    }
+    return false;
+  }
+  // (once the table of powers is there)
+  __device__ __forceinline__ double segment_weight(int g) const {
+    const SegmentStats& x = stats[g];
+    return x.top > -INFINITY ? x.sum * w(x.top) : 0.0;
+  }
+  __device__ __forceinline__ uint64_t segment_whole(int g) const {
+    return g < segments ? whole(segment_weight(g), scale) : 0;
+  }
+  __device__ __forceinline__ void set_scale(double sum) { scale = ldexp(1.0, 61 - ilogb(sum)); }
+  // scale and whole_sum from the segments' sums
+  __device__ __forceinline__ void sum_segments() {
+    const int lane = threadIdx.x & 63;
+    double x = 0.0;
+    for (int g = lane; g < segments; g += 64) x += segment_weight(g);
+    set_scale(uniform(wave_reduce(x, Add{})));
+    uint64_t n = 0;
+    for (int g = lane; g < segments; g += 64) n += segment_whole(g);
+    whole_sum = uniform(wave_reduce(n, Add{}));
+  }
+  // Where the running sum of parts(g) first exceeds x: the segment, with the sum before it.
+  template <class F>
+  __device__ __forceinline__ int find_segment(uint64_t x, F parts, uint64_t& before) const {
+    const int lane = threadIdx.x & 63;
+    uint64_t base = 0;
+    for (int g0 = 0; g0 < segments; g0 += 64) {
+      const uint64_t part = parts(g0 + lane), upto = base + wave_scan(part);
+      const uint64_t hit = __ballot(upto > x);
+      if (hit) {
+        const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+        before = uniform(__shfl(upto - part, l));
+        return g0 + l;
+      }
+      base = uniform(__shfl(upto, 63));
+    }
+    before = base;
+    return segments - 1;
+  }
+  // The id whose running sum of f, over the ids of segment g in order and what lies before it, first
+  // exceeds x.  Where the segment's sum of f comes out a little less than the sum that has led to it
+  // (one of the first launch's), its last id with f > 0.
+  template <int kN, class S, class F>
+  __device__ __forceinline__ int find_id(S& s, int g, uint64_t before, uint64_t x, F f) const {
+    constexpr int kIds = kSegment / (64 * kN);  // of a thread
+    const int at = g * kSegment + static_cast<int>(threadIdx.x) * kIds;
+    uint64_t v[kIds], mine = 0;
+#pragma unroll
+    for (int e = 0; e < kIds; ++e) {
+      v[e] = at + e < vocab ? f(load_logit(logits, at + e), at + e) : 0;
+      mine += v[e];
+    }
+    if (threadIdx.x == 0) s.found_id = -1;
+    uint64_t total;
+    uint64_t run = before + block_scan<kN>(mine, s.slots64, total);
+    if (run <= x && run + mine > x) {
+      int id = at;
+#pragma unroll
+      for (int e = 0; e < kIds - 1; ++e) {
+        run += v[e];
+        if (run <= x) id = at + e + 1;
+      }
+      s.found_id = id;
+    }
+    __syncthreads();
+    const int id = uniform(s.found_id);
+    if (id >= 0) return id;
+    uint32_t last = 0;  // id + 1
+#pragma unroll
+    for (int e = 0; e < kIds; ++e)
+      if (v[e]) last = at + e + 1;
+    last = block_reduce<kN>(last, s.slots32, Max{});
+    return last ? static_cast<int>(last) - 1 : g * kSegment;
+  }
+  // Row r's outputs, by the calling thread (soft: model_sum(), by its whole wave); sum: of the kept
+  // weights.
+  __device__ __forceinline__ float model_sum(const SampleArgs& a) const {
+    float soft = 0.f;
+    if (a.conf)
+      for (int g = threadIdx.x & 63; g < segments; g += 64)
+        soft += stats[g].soft * fast_exp2((stats[g].top - top) * kLog2e);
+    return wave_reduce(soft, Add{});
+  }
+  __device__ __forceinline__ void write(const SampleArgs& a, int token, double sum,
+                                        float soft) const {
+    const float z = load_logit(logits, token);
+    a.token[r] = token;
+    if (a.prob) a.prob[r] = st.greedy() ? 1.f : static_cast<float>(w(z) / sum);
+    if (a.conf) a.conf[r] = static_cast<float>(Weights{w.pow64, w.top, weight_rate(1.f)}(z)) / soft;
+  }
+};
+
+__device__ __forceinline__ float random_number(const SampleArgs& a, int r) {
+  return fminf(fmaxf(a.uniform[r], 0.f), 0x1.fffffep-1f);
+}
+
+// ---------------------------------------------------------------------------------------
+// Second launch: a workgroup of four waves per row settles it where that takes one segment, or at
+// most kPickList ids.
+// ---------------------------------------------------------------------------------------
+struct PickShared {
+  double pow64[64];
+  uint64_t list[kPickList][2];  // entry, weight
+  alignas(16) uint32_t bins[kPickThreads];
+  uint32_t groups[kPickList];
+  uint64_t slots64[kPickWaves];
+  uint32_t slots32[kPickWaves];
+  uint64_t sum_of_k, sum_of_list;
+  uint32_t n_list, n_groups;
+  uint32_t past_min_p;
+  int32_t found_id;
+};
+
+// The first ids of the order into s.list: at least `want` of them, by way of the groups whose largest
+// logit lies in the first so many bins of these; all ids above -inf (then `complete`) where there are
+// at most kPickList.  Returns their number, or -1 where they are more than that.
+template <class T>
+__device__ __forceinline__ int gather(const Row<T>& row, PickShared& s, uint32_t want,
+                                      bool& complete) {
+  const int t = threadIdx.x, lane = t & 63, n_groups = row.segments * 64;
+  // largest logits of groups t, t + kPickThreads, ..: kept in registers for up to 163840 ids
+  constexpr int kHeld = 20;
+  float held[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = t + j * kPickThreads;
+    held[j] = i < n_groups ? row.group_top[i] : -INFINITY;
+  }
+  auto each_group = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) f(held[j], t + j * kPickThreads);
+    for (int i = t + kHeld * kPickThreads; i < n_groups; i += kPickThreads) f(row.group_top[i], i);
+  };
+  // (what weighs less than e^-48 of the largest needs no bin of its own; halves: no overflow)
+  const float from = fmaxf(row.low, row.top - 48.f * row.st.temperature);
+  const float per = fminf((kPickThreads - 1) / (0.5f * row.top - 0.5f * from), FLT_MAX);
+  auto bin = [&](float z) {
+    return static_cast<int>(fminf((0.5f * row.top - 0.5f * z) * per, kPickThreads - 1.f));
+  };
+  s.bins[t] = 0;
+  if (t == 0) s.n_list = s.n_groups = 0;
+  __syncthreads();
+  each_group([&](float z, int) {
+    if (z > -INFINITY) atomicAdd(&s.bins[bin(z)], 1u);
+  });
+  __syncthreads();
+  // the bin that the want-th group lies in; every wave for itself, four bins a lane
+  int last = kPickThreads - 1;
+  uint32_t finite;
+  {
+    const u32x4 c = *reinterpret_cast<const u32x4*>(&s.bins[4 * lane]);
+    const uint32_t mine = c[0] + c[1] + c[2] + c[3], upto = wave_scan(mine);
+    finite = uniform(__shfl(upto, 63));
+    const uint64_t hit = __ballot(upto >= want);
+    if (hit) {
+      const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+      uint32_t n = upto - mine;
+      int b = 4 * lane;
+#pragma unroll
+      for (int e = 0; e < 3; ++e) {
+        n += c[e];
+        if (n < want) b = 4 * lane + e + 1;
+      }
+      last = uniform(__shfl(b, l));
+    }
+  }
+  complete = row.vocab <= kPickList || finite * kGroup <= kPickList;
+  if (complete) last = kPickThreads - 1;
+  auto taken = [&](float z) { return z > -INFINITY && bin(z) <= last; };
+  each_group([&](float z, int i) {
+    if (!taken(z)) return;
+    const uint32_t at = atomicAdd(&s.n_groups, 1u);
+    if (at < kPickList) s.groups[at] = static_cast<uint32_t>(i);
+  });
+  __syncthreads();
+  const int found = static_cast<int>(uniform(s.n_groups));
+  if (found > kPickList) return -1;  // (each holds one such id at least)
+  for (int i = t; i < found * kLoads<T>; i += kPickThreads) {
+    const int group = static_cast<int>(s.groups[i / kLoads<T>]);
+    const int at = (group >> 6) * kSegment + id_in_segment<T>(i % kLoads<T>, group & 63);
+    Chunk<T> z;
+    z.load(row.logits, at, row.vocab);
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e)
+      if (taken(z[e])) {
+        const uint32_t j = atomicAdd(&s.n_list, 1u);
+        if (j < kPickList) s.list[j][0] = entry_of(z[e], at + e);
+      }
+  }
+  __syncthreads();
+  const uint32_t n = uniform(s.n_list);
+  return n <= kPickList ? static_cast<int>(n) : -1;
+}
+
+// Cuts and draws from the n ids of s.list, the first n of the order, an id a thread; false where what
+// is kept may go on behind them.  An id's place in the order, the weight before it, and then the weight
+// up to it in the order of ids come from one walk each over the list, which all lanes read at once:
+// no sorting, and no sums across waves.
+template <class T>
+__device__ __forceinline__ bool pick_from_list(const SampleArgs& a, const Row<T>& row,
+                                               PickShared& s, int n, bool complete) {
+  const int t = threadIdx.x;
+  const Settings& st = row.st;
+  const bool active = t < n;
+  const uint64_t entry = active ? s.list[t][0] : 0;
+  const double x = active ? row.w(key_logit(entry_key(entry))) : 0.0;
+  const uint64_t mass = whole(x, row.scale);
+  if (active) s.list[t][1] = mass;
+  __syncthreads();
+  uint64_t before = 0;
+  int place = 0;
+  if (wave_index() * 64 < n)
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+      const bool ahead = s.list[j][0] > entry;
+      place += ahead;
+      before += ahead ? s.list[j][1] : 0;
+    }
+  if (st.top_k > n && !complete) return false;
+  const int keep = st.top_k > 0 ? min(st.top_k, n) : n;
+  if (active && place == keep - 1) s.sum_of_k = before + mass;
+  if (active && place == n - 1) {
+    s.sum_of_list = before + mass;
+    s.past_min_p = !(x >= st.min_p);
+  }
+  __syncthreads();
+  const uint64_t of_list = uniform(s.sum_of_list);
+  bool closed = complete || st.top_k > 0;  // nothing behind the list can be kept
+  bool kept = active && place < keep;
+  if (st.top_p < 1.f) {
+    const uint64_t all = st.top_k > 0 ? uniform(s.sum_of_k) : complete ? of_list : row.whole_sum;
+    const uint64_t target = share_of(all, st.top_p);
+    closed |= of_list >= target;
+    kept &= before < target;
+  }
+  if (st.min_p > 0.f) {
+    closed |= uniform(s.past_min_p) != 0;
+    kept &= x >= st.min_p;
+  }
+  if (!closed) return false;
+  if (active && !kept) s.list[t][1] = 0;
+  __syncthreads();
+  if (wave_index() * 64 >= n) return true;
+  uint64_t upto = 0, total = 0;
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) {
+    const uint64_t m = s.list[j][1];
+    total += m;
+    // (~id falls as the id rises)
+    upto += static_cast<uint32_t>(s.list[j][0]) >= static_cast<uint32_t>(entry) ? m : 0;
+  }
+  const uint64_t at = part_of(total, random_number(a, row.r));
+  const float soft = row.model_sum(a);
+  if (kept && upto > at && upto - mass <= at)
+    row.write(a, entry_id(entry), static_cast<double>(total) / row.scale, soft);
+  return true;
+}
+
+template <class T>
+__global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a, Workspace ws) {
+  __shared__ PickShared s;
+  const int t = threadIdx.x;
+  if (t < 64) s.pow64[t] = kPow64[t];
+  Row<T> row;
+  if (!row.open(a, ws, blockIdx.x, s.pow64)) return;
+  __syncthreads();
+  if (row.st.greedy() || !row.st.limited()) {
+    int token;
+    double sum = 1.0;
+    if (row.st.greedy()) {
+      const float top = row.top;
+      uint64_t before;
+      const int g = row.find_segment(
+          0, [&](int i) -> uint64_t { return i < row.segments && row.stats[i].top == top; }, before);
+      const uint32_t key = order_key(top);
+      token = row.template find_id<kPickWaves>(
+          s, g, 0, 0, [&](float z, int) -> uint64_t { return order_key(z) == key; });
+    } else {
+      row.sum_segments();
+      uint64_t before;
+      const uint64_t at = part_of(row.whole_sum, random_number(a, row.r));
+      const int g = row.find_segment(at, [&](int i) { return row.segment_whole(i); }, before);
+      token = row.template find_id<kPickWaves>(
+          s, g, before, at, [&](float z, int) { return whole(row.w(z), row.scale); });
+      sum = static_cast<double>(row.whole_sum) / row.scale;
+    }
+    const float soft = row.model_sum(a);
+    if (t == 0) {
+      row.write(a, token, sum, soft);
+      ws.pending[row.r] = 0;
+    }
+    return;
+  }
+  if (row.st.few()) {
+    row.scale = 0x1p52;  // (at most kPickList weights of at most 1 are summed)
+    row.whole_sum = 0;
+  } else {
+    row.sum_segments();
+  }
+  bool done = false;
+  if (row.st.few() || row.st.top_k == 0) {
+    bool complete;
+    const int n = gather(row, s, row.st.few() ? row.st.top_k : kFewIds, complete);
+    done = n > 0 && pick_from_list(a, row, s, n, complete);
+  }
+  if (t == 0) ws.pending[row.r] = !done;
+}
+
+// ---------------------------------------------------------------------------------------
+// Third launch: a workgroup of 16 waves for each row that the second has left.
 // ---------------------------------------------------------------------------------------
 struct Shared {
   uint64_t segment[kMaxSegments];  // a sum per segment, then the sum before it
@@ -266,50 +747,15 @@ struct Shared {
     uint64_t bin_mass[kBins];
   };
   uint32_t bins[kBins];
-  double pow16[16];
+  double pow64[64];
   uint64_t slots64[kWaves];
   double slots_d[kWaves];
   float slots_f[kWaves];
   uint32_t slots32[kWaves];
-  uint32_t n_list, found, found_count, found_before;
+  uint32_t n_list, n_groups, found, found_count, found_before;
   uint64_t found_mass, found_mass_before;
   int32_t found_id;
 };
-
-// x over all threads, on every thread; `slots` [kWaves] is free again behind the next barrier.
-template <class V, class Op>
-__device__ __forceinline__ V block_reduce(V x, V* slots, Op op) {
-  x = wave_reduce(x, op);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = x;
-  __syncthreads();
-  V y = slots[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) y = op(y, slots[w]);
-  return y;
-}
-
-// Sum of x over the threads before this one; `total` over all.
-template <class V>
-__device__ __forceinline__ V block_scan(V x, V* slots, V& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  V sum = x;
-  for (int n = 1; n < 64; n <<= 1) {
-    const V o = __shfl_up(sum, n);
-    if (lane >= n) sum += o;
-  }
-  __syncthreads();
-  if (lane == 63) slots[wave] = sum;
-  __syncthreads();
-  V before = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w == wave) before = total;
-    total += slots[w];
-  }
-  return before + sum - x;
-}
 
 // Sorts list[0 .. n) falling, in place: a value per thread, exchanged between lanes for distances
 // below 64 and through LDS beyond.
@@ -338,39 +784,45 @@ __device__ __forceinline__ void sort_falling(uint64_t* list, int n) {
   __syncthreads();
 }
 
-// floor(sum * x) for x in [0, 1) (bits of x below 2^-64 are left out).
-__device__ __forceinline__ uint64_t part_of(uint64_t sum, float x) {
-  return __umul64hi(sum, static_cast<uint64_t>(static_cast<double>(x) * 0x1p64));
-}
-// The least whole number >= max(sum * p, 1), for p < 1.
-__device__ __forceinline__ uint64_t share_of(uint64_t sum, float p) {
-  const uint64_t q = static_cast<uint64_t>(static_cast<double>(fmaxf(p, 0.f)) * 0x1p64);
-  return max(__umul64hi(sum, q) + (sum * q != 0), uint64_t{1});
-}
-
 template <class T>
-struct Picker {
-  const SampleArgs& a;
-  const Workspace& ws;
+struct Searcher {
+  Row<T>& row;
   Shared& s;
-  const T* row;
-  int r;
-  Settings st;
-  Weights w;
-  double scale;
-  int segments;
 
   // ---- the row's segments, wave by wave -----------------------------------------------
-  // f(z, id) for every id of segment g that this lane holds (ids behind the end as -inf).
-  template <class F>
-  __device__ __forceinline__ void visit(int g, F f) const {
+  // f(z, id) for every id that this lane holds of segments wave, wave + kWaves, .. for which
+  // wanted(g); then each_segment(g) (by the whole wave) for these and the others.  Two loads at a time,
+  // the next two under way meanwhile, worked on by two ids (with more of them under way the kernel
+  // spilled).
+  template <class Wanted, class F, class End>
+  __device__ __forceinline__ void visit(Wanted wanted, F f, End each_segment) const {
+    const int lane = threadIdx.x & 63;
+    constexpr int kAtOnce = 2;
+    for (int g = wave_index(); g < row.segments; g += kWaves) {
+      if (wanted(g)) {
+        Chunk<T> x[kAtOnce], next[kAtOnce];
+        auto load = [&](int i0, Chunk<T> (&c)[kAtOnce]) {
 #pragma unroll
-    for (int i = 0; i < kLoads<T>; ++i) {
-      const int at = g * kSegment + id_in_segment<T>(i, threadIdx.x & 63);
-      float z[kVec<T>];
-      load_logits(row, at, a.vocab, z);
+          for (int i = 0; i < kAtOnce; ++i)
+            c[i].load(row.logits, g * kSegment + id_in_segment<T>(i0 + i, lane), row.vocab);
+        };
+        load(0, x);
+#pragma unroll 1
+        for (int i0 = 0; i0 < kLoads<T>; i0 += kAtOnce) {
+          if (i0 + kAtOnce < kLoads<T>) load(i0 + kAtOnce, next);
 #pragma unroll
-      for (int e = 0; e < kVec<T>; ++e) f(z[e], at + e);
+          for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+            for (int e = 0; e < kVec<T>; ++e) {
+              if (e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+              f(x[i][e], g * kSegment + id_in_segment<T>(i0 + i, lane) + e);
+            }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) x[i] = next[i];
+        }
+      }
+      each_segment(g);
     }
   }
   // s.segment[g] <- sum of f(z, id) over the segments whose largest logit has a key of at least
@@ -378,228 +830,63 @@ struct Picker {
   template <class F>
   __device__ __forceinline__ void segment_sums(uint32_t key_low, F f) const {
     __syncthreads();
-    for (int g = threadIdx.x >> 6; g < segments; g += kWaves) {
-      uint64_t sum = 0;
-      if (order_key(s.segment_top[g]) >= key_low)
-        visit(g, [&](float z, int id) { sum += f(z, id); });
-      sum = wave_reduce(sum, Add{});
-      if ((threadIdx.x & 63) == 0) s.segment[g] = sum;
-    }
+    uint64_t sum = 0;
+    visit([&](int g) { return order_key(uniform(s.segment_top[g])) >= key_low; },
+          [&](float z, int id) { sum += f(z, id); },
+          [&](int g) {
+            sum = wave_reduce(sum, Add{});
+            if ((threadIdx.x & 63) == 0) s.segment[g] = sum;
+            sum = 0;
+          });
     __syncthreads();
   }
-  // s.segment[g] <- the sum before segment g; returns the sum of all.
-  __device__ __forceinline__ uint64_t segments_before() const {
-    __syncthreads();
-    const int t = threadIdx.x;
-    uint64_t total;
-    const uint64_t before = block_scan(t < segments ? s.segment[t] : 0, s.slots64, total);
-    __syncthreads();
-    s.segment[t] = before;
-    __syncthreads();
-    return total;
+  // Sum of s.segment, as every wave finds it.
+  __device__ __forceinline__ uint64_t sum_of_segments() const {
+    uint64_t n = 0;
+    for (int g = threadIdx.x & 63; g < row.segments; g += 64) n += s.segment[g];
+    return uniform(wave_reduce(n, Add{}));
   }
-  // The id whose running sum of f, over all ids in order, first exceeds x, from s.segment as
-  // segments_before leaves it (x < the sum of all).  Where the segment's sum of f comes out a little
-  // less than s.segment says (a sum of the first launch), its last id with f > 0.
+  // The id whose running sum of f, over all ids in order, first exceeds x, from f's sums in s.segment.
   template <class F>
   __device__ __forceinline__ int find(uint64_t x, F f) const {
-    const int t = threadIdx.x;
-    if (t == 0) s.found_id = -1;
-    if (t < segments && s.segment[t] <= x && (t + 1 == segments || s.segment[t + 1] > x))
-      s.found = static_cast<uint32_t>(t);
-    __syncthreads();
-    const int g = min(static_cast<int>(s.found), segments - 1);
-    // two ids a thread
-    const int at = g * kSegment + 2 * t;
-    uint64_t v[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) v[e] = at + e < a.vocab ? f(load_logit(row, at + e), at + e) : 0;
-    uint64_t total;
-    const uint64_t before = s.segment[g] + block_scan(v[0] + v[1], s.slots64, total);
-    if (before <= x && before + v[0] > x)
-      s.found_id = at;
-    else if (before + v[0] <= x && before + v[0] + v[1] > x)
-      s.found_id = at + 1;
-    __syncthreads();
-    if (s.found_id < 0) {  // uniform
-      const uint32_t mine = v[1] ? at + 2 : v[0] ? at + 1 : 0;  // id + 1
-      const uint32_t last = block_reduce(mine, s.slots32, Max{});
-      return last ? static_cast<int>(last) - 1 : g * kSegment;
-    }
-    return s.found_id;
-  }
-
-  // ---- few ids, in LDS ------------------------------------------------------------------
-  // Puts every id whose logit is at least `least` into s.list as (key, ~id), by way of the groups
-  // whose largest logit is; returns their number, or -1 where they are more than kList.
-  __device__ __forceinline__ int gather(float least) const {
-    const int t = threadIdx.x, n_groups = segments * 64;
-    const float* const tops = ws.group_top + static_cast<size_t>(r) * n_groups;
-    uint32_t* const groups = s.bins;  // kBins of them at most
-    __syncthreads();
-    if (t == 0) s.n_list = s.found = 0;
-    __syncthreads();
-    for (int i = t; i < n_groups; i += kThreads)
-      if (tops[i] >= least) {
-        const uint32_t at = atomicAdd(&s.found, 1u);
-        if (at < kList) groups[at] = static_cast<uint32_t>(i);
-      }
-    __syncthreads();
-    const int found = static_cast<int>(s.found);
-    if (found > kList) return -1;  // (each holds one such id at least)
-    for (int i = t; i < found * kLoads<T>; i += kThreads) {
-      const int group = static_cast<int>(groups[i / kLoads<T>]);
-      const int at = (group >> 6) * kSegment + id_in_segment<T>(i % kLoads<T>, group & 63);
-      float z[kVec<T>];
-      load_logits(row, at, a.vocab, z);
-#pragma unroll
-      for (int e = 0; e < kVec<T>; ++e)
-        if (z[e] >= least) {
-          const uint32_t j = atomicAdd(&s.n_list, 1u);
-          if (j < kList)
-            s.list[j] = static_cast<uint64_t>(order_key(z[e])) << 32 | ~static_cast<uint32_t>(at + e);
-        }
-    }
-    __syncthreads();
-    return s.n_list <= kList ? static_cast<int>(s.n_list) : -1;
-  }
-  static __device__ __forceinline__ uint32_t entry_key(uint64_t x) {
-    return static_cast<uint32_t>(x >> 32);
-  }
-  static __device__ __forceinline__ int entry_id(uint64_t x) {
-    return static_cast<int>(~static_cast<uint32_t>(x));
-  }
-  __device__ __forceinline__ double entry_weight(uint64_t x) const {
-    return w(key_logit(entry_key(x)));
-  }
-
-  // A logit such that at least `want` groups have a larger one or it, and not many more: the lowest in
-  // the first so many bins of the groups' largest.  The lowest finite value when all groups above
-  // -inf together hold at most kList ids.
-  __device__ __forceinline__ float few_limit(uint32_t want, float top) const {
-    const int t = threadIdx.x, n_groups = segments * 64;
-    const float* const tops = ws.group_top + static_cast<size_t>(r) * n_groups;
-    float low = INFINITY;
-    uint32_t finite = 0;
-    for (int i = t; i < n_groups; i += kThreads) {
-      const float z = tops[i];
-      if (z > -INFINITY) {
-        low = fminf(low, z);
-        ++finite;
-      }
-    }
-    low = block_reduce(low, s.slots_f, Min{});
-    finite = block_reduce(finite, s.slots32, Add{});
-    if (finite * kGroup <= kList) return -FLT_MAX;
-    // (what weighs less than e^-48 of the largest needs no bin of its own; halves: no overflow)
-    const float from = fmaxf(low, top - 48.f * st.temperature);
-    const float per = (kThreads - 1) / (0.5f * top - 0.5f * from);
-    if (!(per < FLT_MAX)) return low;
-    auto bin = [&](float z) {
-      return static_cast<int>(fminf((0.5f * top - 0.5f * z) * per, kThreads - 1.f));
-    };
-    s.bins[t] = 0;
-    if (t == 0) s.found = kThreads - 1;
-    __syncthreads();
-    for (int i = t; i < n_groups; i += kThreads)
-      if (tops[i] > -INFINITY) atomicAdd(&s.bins[bin(tops[i])], 1u);
-    __syncthreads();
-    uint32_t total;
-    const uint32_t mine = s.bins[t];
-    const uint32_t before = block_scan(mine, s.slots32, total);
-    if (before < want && before + mine >= want) s.found = static_cast<uint32_t>(t);
-    __syncthreads();
-    const int b = static_cast<int>(s.found);
-    float edge = INFINITY;
-    for (int i = t; i < n_groups; i += kThreads)
-      if (tops[i] > -INFINITY && bin(tops[i]) <= b) edge = fminf(edge, tops[i]);
-    return block_reduce(edge, s.slots_f, Min{});
-  }
-
-  // Cuts and draws from the n ids of s.list, which are the first n of the order; false where what is
-  // kept may go on behind them.  whole_sum: the sum of all weights where no top-k limits it.
-  __device__ __forceinline__ bool pick_from_list(int n, bool complete, uint64_t whole_sum, float u,
-                                                 int& token, double& sum) const {
-    const int t = threadIdx.x;
-    sort_falling(s.list, n);
-    const uint64_t entry = t < n ? s.list[t] : 0;
-    const double x = t < n ? entry_weight(entry) : 0.0;
-    const uint64_t mass = whole(x, scale);
-    uint64_t total;
-    const uint64_t before = block_scan(mass, s.slots64, total);
-    int keep = n;
-    bool closed = complete;  // nothing behind the list can be kept
-    if (st.top_k > 0) {
-      if (st.top_k > n && !complete) return false;
-      keep = min(st.top_k, n);
-      closed = true;
-    }
-    if (st.top_p < 1.f) {
-      if (st.top_k > 0) {
-        if (t == keep - 1) s.mass[0] = before + mass;
-        __syncthreads();
-        whole_sum = s.mass[0];
-      } else if (complete) {
-        whole_sum = total;
-      }
-      const uint64_t target = share_of(whole_sum, st.top_p);
-      if (t == 0) s.found = n;
-      __syncthreads();
-      if (t < n && before < target && before + mass >= target) s.found = static_cast<uint32_t>(t);
-      __syncthreads();
-      if (static_cast<int>(s.found) < n) {
-        keep = min(keep, static_cast<int>(s.found) + 1);
-        closed = true;
-      }
-    }
-    if (st.min_p > 0.f) {
-      const uint32_t above =
-          block_reduce(static_cast<uint32_t>(t < n && x >= st.min_p), s.slots32, Add{});
-      if (static_cast<int>(above) < n) closed = true;
-      keep = min(keep, static_cast<int>(above));
-    }
-    if (!closed) return false;
-    // the kept ones in the order of their ids
-    __syncthreads();
-    if (t < n) s.mass[t] = mass;
-    if (t < keep)
-      s.list[t] = static_cast<uint64_t>(static_cast<uint32_t>(entry)) << 32 | static_cast<uint32_t>(t);
-    __syncthreads();
-    sort_falling(s.list, keep);  // (~id falls)
-    const uint64_t by_id = t < keep ? s.list[t] : 0;
-    const uint64_t m = t < keep ? s.mass[static_cast<uint32_t>(by_id)] : 0;
-    const uint64_t up_to = block_scan(m, s.slots64, total);
-    const uint64_t at = part_of(total, u);
-    if (up_to <= at && at < up_to + m) s.found_id = static_cast<int>(~static_cast<uint32_t>(by_id >> 32));
-    __syncthreads();
-    token = s.found_id;
-    sum = static_cast<double>(total) / scale;
-    return true;
+    uint64_t before;
+    const int g = row.find_segment(
+        x, [&](int i) { return i < row.segments ? s.segment[i] : uint64_t{0}; }, before);
+    return row.template find_id<kWaves>(s, g, before, x, f);
   }
 
   // ---- a cut anywhere in the row -----------------------------------------------------------
-  // Puts the kept ids' sums into s.segment.
-  __device__ __forceinline__ void sum_kept(const Cut& cut, uint32_t key_low) const {
-    segment_sums(max(cut.key, key_low), [&](float z, int id) -> uint64_t {
-      if (!cut.keeps(order_key(z), id)) return 0;
-      const double x = w(z);
-      return x >= st.min_p ? whole(x, scale) : 0;
-    });
+  // s.segment <- sums of the kept ids' weights, none of which has a key below key_low.
+  __device__ __forceinline__ void sum_kept(const Cut& cut, uint32_t key_low, float min_p) const {
+    const uint32_t least = max(cut.key, key_low);
+    double sum = 0.0;
+    __syncthreads();
+    visit([&](int g) { return order_key(uniform(s.segment_top[g])) >= least; },
+          [&](float z, int id) {
+            const double x = row.w(z);
+            if (cut.keeps(order_key(z), id) && x >= min_p) sum += x;
+          },
+          [&](int g) {
+            sum = wave_reduce(sum, Add{});
+            if ((threadIdx.x & 63) == 0) s.segment[g] = whole(sum, row.scale);
+            sum = 0.0;
+          });
+    __syncthreads();
   }
 
-  // The cut behind the first `target` ids of the order (kMass false), or behind the fewest whose
-  // weights come to `target` (true).  `summed`: s.segment holds the sums of what it keeps.
+  // The cut behind the first `target` ids of the order (by_mass false), or behind the fewest whose
+  // weights come to `target` (true), and in s.segment the sums of what it keeps; false where this
+  // does not find it.
   //
   // A histogram over [low, top] by value, of counts, or of weights in 32 bits, which is only to find
   // the bin; then the exact sums above the bin, segment by segment, with the bin's ids into the
   // list.  Where the histogram's rounding has led to the bin next to the right one, the exact sums say
   // so.
-  template <bool kMass>
-  __device__ __forceinline__ Cut search(uint64_t target, float low, float top, bool& summed) const {
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    summed = false;
+  __device__ __forceinline__ bool search(bool by_mass, uint64_t target, float low, float top,
+                                         Cut& cut) const {
+    const int t = threadIdx.x, lane = t & 63;
     const float per = (kBins - 1) / (0.5f * top - 0.5f * low);  // (halves: no overflow)
-    if (!(per < FLT_MAX)) return search_bits<kMass>(target);
+    if (!(per < FLT_MAX)) return false;
     auto bin = [&](float z) {
       return static_cast<int>(fminf((0.5f * top - 0.5f * z) * per, kBins - 1.f));
     };
@@ -607,17 +894,17 @@ struct Picker {
     for (int i = t; i < kBins; i += kThreads) s.bins[i] = 0;
     if (t == 0) s.found = kBins - 1;
     __syncthreads();
-    float* const fbins = reinterpret_cast<float*>(s.bins);
-    const float rate = static_cast<float>(w.rate / 16.0);
-    for (int g = wave; g < segments; g += kWaves)
-      if (s.segment_top[g] > -INFINITY)
-        visit(g, [&](float z, int) {
-          if (!(z > -INFINITY)) return;
-          if (kMass)
-            atomicAdd(&fbins[bin(z)], fast_exp2((z - top) * rate));
-          else
-            atomicAdd(&s.bins[bin(z)], 1u);
-        });
+    // weights as whole numbers of 2^-31 of (at most) their sum (a float's atomic sum takes 8 times as long
+    // in LDS)
+    const float rate2 = static_cast<float>(row.w.rate / 64.0);
+    const float unit = static_cast<float>(ilogb(row.scale) - 31);
+    visit([&](int g) { return uniform(s.segment_top[g]) > -INFINITY; },
+          [&](float z, int) {
+            if (!(z > -INFINITY)) return;
+            const uint32_t n = by_mass ? static_cast<uint32_t>(fast_exp2((z - top) * rate2 + unit)) : 1u;
+            atomicAdd(&s.bins[bin(z)], n);
+          },
+          [](int) {});
     __syncthreads();
     auto take = [&](auto before, auto x0, auto x1, auto want) {
       if (before < want && before + x0 >= want)
@@ -625,86 +912,78 @@ struct Picker {
       else if (before + x0 < want && before + x0 + x1 >= want)
         s.found = 2 * t + 1;
     };
-    if (kMass) {
-      const double x0 = fbins[2 * t], x1 = fbins[2 * t + 1];
-      double all;
-      const double before = block_scan(x0 + x1, s.slots_d, all);
-      take(before, x0, x1, static_cast<double>(target) / scale);
-    } else {
+    {
       const uint64_t x0 = s.bins[2 * t], x1 = s.bins[2 * t + 1];
       uint64_t all;
-      const uint64_t before = block_scan(x0 + x1, s.slots64, all);
-      take(before, x0, x1, target);
+      const uint64_t before = block_scan<kWaves>(x0 + x1, s.slots64, all);
+      take(before, x0, x1, by_mass ? max(target >> 31, uint64_t{1}) : target);
     }
     __syncthreads();
-    int at_bin = static_cast<int>(s.found);
+    int at_bin = static_cast<int>(uniform(s.found));
 
     uint64_t above;
-    for (int last_step = 0;;) {
+    for (int tries = 0;; ++tries) {
       __syncthreads();
       if (t == 0) s.n_list = 0;
       __syncthreads();
       uint64_t n_above = 0, m_inside = 0;
-      for (int g = wave; g < segments; g += kWaves) {
-        uint64_t sum = 0;
-        if (s.segment_top[g] > -INFINITY && bin(s.segment_top[g]) <= at_bin)
-          visit(g, [&](float z, int id) {
-            if (!(z > -INFINITY)) return;
-            const int b = bin(z);
-            if (b > at_bin) return;
-            const uint64_t m = whole(w(z), scale);
-            if (b < at_bin) {
-              sum += m;
-              ++n_above;
-              return;
-            }
-            m_inside += m;
-            const uint32_t j = atomicAdd(&s.n_list, 1u);
-            if (j < kList)
-              s.list[j] = static_cast<uint64_t>(order_key(z)) << 32 | ~static_cast<uint32_t>(id);
-          });
-        sum = wave_reduce(sum, Add{});
-        if (lane == 0) s.segment[g] = sum;
-      }
-      uint64_t inside = block_reduce(kMass ? m_inside : uint64_t{0}, s.slots64, Add{});
-      above = kMass ? (t < segments ? s.segment[t] : 0) : n_above;
-      above = block_reduce(above, s.slots64, Add{});
-      if (!kMass) inside = s.n_list;
+      double sum = 0.0;
+      visit([&](int g) { return uniform(s.segment_top[g]) > -INFINITY && uniform(bin(s.segment_top[g])) <= at_bin; },
+            [&](float z, int id) {
+              const int b = bin(z);
+              if (b > at_bin || !(z > -INFINITY)) return;
+              const double x = row.w.normal(z);
+              if (b < at_bin) {
+                sum += x;
+                if (!by_mass) ++n_above;
+                return;
+              }
+              if (by_mass) m_inside += whole(x, row.scale);
+              const uint32_t j = atomicAdd(&s.n_list, 1u);
+              if (j < kList)
+                s.list[j] = entry_of(z, id);
+            },
+            [&](int g) {
+              sum = wave_reduce(sum, Add{});
+              if (lane == 0) s.segment[g] = whole(sum, row.scale);
+              sum = 0.0;
+            });
+      __syncthreads();
+      uint64_t inside = block_reduce<kWaves>(by_mass ? m_inside : uint64_t{0}, s.slots64, Add{});
+      above = by_mass ? (t < row.segments ? s.segment[t] : 0) : n_above;
+      above = block_reduce<kWaves>(above, s.slots64, Add{});
+      if (!by_mass) inside = uniform(s.n_list);
       int step = 0;
       if (above >= target)
         step = -1;
       else if (above + inside < target)
         step = 1;
-      // (a step back after one in the other direction, or off the end: by bits)
       if (step == 0) break;
-      if (step == -last_step || at_bin + step < 0 || at_bin + step >= kBins)
-        return search_bits<kMass>(target);
-      last_step = step;
       at_bin += step;
+      if (tries == 2 || at_bin < 0 || at_bin >= kBins) return false;
     }
-    const int n = static_cast<int>(s.n_list);
-    if (n > kList) return search_bits<kMass>(target);
+    const int n = static_cast<int>(uniform(s.n_list));
+    if (n > kList) return false;
     sort_falling(s.list, n);
     const uint64_t entry = t < n ? s.list[t] : 0;
-    const uint64_t mass = t < n ? whole(entry_weight(entry), scale) : 0;
+    const uint64_t mass = t < n ? whole(row.w(key_logit(entry_key(entry))), row.scale) : 0;
     uint64_t total;
-    const uint64_t unit = kMass ? mass : t < n ? 1 : 0;
-    const uint64_t before = above + block_scan(unit, s.slots64, total);
+    const uint64_t step = by_mass ? mass : t < n ? 1 : 0;
+    const uint64_t before = above + block_scan<kWaves>(step, s.slots64, total);
     if (t < n && before < target) {  // kept
       atomicAdd(reinterpret_cast<unsigned long long*>(&s.segment[entry_id(entry) / kSegment]),
                 static_cast<unsigned long long>(mass));
-      if (before + unit >= target) s.found = static_cast<uint32_t>(t);
+      if (before + step >= target) s.found = static_cast<uint32_t>(t);
     }
     __syncthreads();
-    const uint64_t last = s.list[s.found];
-    summed = true;
-    return Cut{entry_key(last), entry_id(last)};
+    const uint64_t last = uniform(s.list[s.found]);
+    cut = Cut{entry_key(last), entry_id(last)};
+    return true;
   }
 
   // The same by three rounds over the row, which fix 11, 11 and 10 bits of the key, with exact sums;
   // then, where not all ids of that key are kept, their last one.
-  template <bool kMass>
-  __device__ __forceinline__ Cut search_bits(uint64_t target) const {
+  __device__ __forceinline__ Cut search_bits(bool by_mass, uint64_t target) const {
     const int t = threadIdx.x;
     uint32_t prefix = 0;
     uint64_t n_before = 0, m_before = 0;
@@ -718,26 +997,26 @@ struct Picker {
       }
       if (t == 0) s.found_count = 0;
       __syncthreads();
-      for (int g = t >> 6; g < segments; g += kWaves)
-        if (s.segment_top[g] > -INFINITY)
-          visit(g, [&](float z, int) {
-            const uint32_t key = order_key(z);
-            if (!(z > -INFINITY) || (level > 0 && (key >> above) != prefix)) return;
-            const uint32_t bin = (key >> shift) & mask;
-            atomicAdd(&s.bins[bin], 1u);
-            atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin_mass[bin]),
-                      static_cast<unsigned long long>(whole(w(z), scale)));
-          });
+      visit([&](int g) { return uniform(s.segment_top[g]) > -INFINITY; },
+            [&](float z, int) {
+              const uint32_t key = order_key(z);
+              if (!(z > -INFINITY) || (level > 0 && (key >> above) != prefix)) return;
+              const uint32_t bin = (key >> shift) & mask;
+              atomicAdd(&s.bins[bin], 1u);
+              atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin_mass[bin]),
+                        static_cast<unsigned long long>(whole(row.w(z), row.scale)));
+            },
+            [](int) {});
       __syncthreads();
       // bins from the highest down, two a thread
       const int hi = kBins - 1 - 2 * t;
       const uint64_t c0 = s.bins[hi], c1 = s.bins[hi - 1], m0 = s.bin_mass[hi],
                      m1 = s.bin_mass[hi - 1];
       uint64_t all;
-      const uint64_t n0 = n_before + block_scan(c0 + c1, s.slots64, all);
-      const uint64_t p0 = m_before + block_scan(m0 + m1, s.slots64, all);
+      const uint64_t n0 = n_before + block_scan<kWaves>(c0 + c1, s.slots64, all);
+      const uint64_t p0 = m_before + block_scan<kWaves>(m0 + m1, s.slots64, all);
       auto take = [&](int bin, uint64_t c, uint64_t m, uint64_t n, uint64_t p) {
-        const uint64_t from = kMass ? p : n, to = kMass ? p + m : n + c;
+        const uint64_t from = by_mass ? p : n, to = by_mass ? p + m : n + c;
         if (from < target && target <= to) {
           s.found = static_cast<uint32_t>(bin);
           s.found_count = static_cast<uint32_t>(c);
@@ -749,138 +1028,83 @@ struct Picker {
       take(hi, c0, m0, n0, p0);
       take(hi - 1, c1, m1, n0 + c0, p0 + m0);
       __syncthreads();
-      if (s.found_count == 0) return kKeepAll;  // fewer ids, or less weight, than the target
-      prefix = level == 0 ? s.found : (prefix << (level == 1 ? 11 : 10)) | s.found;
-      n_before = s.found_before;
-      m_before = s.found_mass_before;
+      if (uniform(s.found_count) == 0) return kKeepAll;  // fewer ids, or less weight, than the target
+      const uint32_t bin = uniform(s.found);
+      prefix = level == 0 ? bin : (prefix << (level == 1 ? 11 : 10)) | bin;
+      n_before = uniform(s.found_before);
+      m_before = uniform(s.found_mass_before);
     }
     // every id of the last bin has the same key and weight
-    const uint64_t equal = s.found_count, each = s.found_mass / equal;
-    const uint64_t keep = kMass ? (target - m_before + each - 1) / each : target - n_before;
+    const uint64_t equal = uniform(s.found_count), each = uniform(s.found_mass) / equal;
+    const uint64_t keep = by_mass ? (target - m_before + each - 1) / each : target - n_before;
     Cut cut{prefix, INT32_MAX};
     if (keep < equal) {
       auto ties = [&](float z, int id) -> uint64_t {
-        return id < a.vocab && order_key(z) == cut.key ? 1 : 0;
+        return id < row.vocab && order_key(z) == cut.key ? 1 : 0;
       };
       segment_sums(cut.key, ties);
-      segments_before();
       cut.last = find(keep - 1, ties);
     }
     return cut;
   }
 };
 
+// The rows that sample_pick_kernel has left.
 template <class T>
-__global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, Workspace ws) {
+__global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, Workspace ws) {
   __shared__ Shared s;
   const int t = threadIdx.x, r = blockIdx.x;
-  const Settings st = settings(a, find_sequence(a.cu_block, a.batch, r, t & 63));
-  const float u = fminf(fmaxf(a.uniform[r], 0.f), 0x1.fffffep-1f);
-  SegmentStats mine{-INFINITY, INFINITY, 0.f, 0.f, 0.0};
-  if (t < ws.segments) mine = ws.stats[static_cast<size_t>(r) * ws.segments + t];
-  s.segment_top[t] = mine.top;
-  if (t < 16) s.pow16[t] = kPow16[t];
-  const bool bad = __syncthreads_or(mine.top != mine.top);
-  const float top = block_reduce(mine.top, s.slots_f, Max{});
-  if (bad || top == -INFINITY) {  // a NaN or +inf; or nothing to draw from
-    if (t == 0) {
-      a.token[r] = -1;
-      const float none = bad ? NAN : 0.f;
-      if (a.prob) a.prob[r] = none;
-      if (a.conf) a.conf[r] = none;
-    }
-    return;
-  }
-  Picker<T> p{a, ws, s, static_cast<const T*>(a.logits) + static_cast<size_t>(r) * a.pitch, r, st,
-              Weights{s.pow16, static_cast<double>(top), weight_rate(st.temperature)}, 0.0,
-              ws.segments};
-  int token;
-  double sum = 1.0;  // of the kept weights
-  if (st.greedy()) {
-    const uint32_t key = order_key(top);
-    s.segment[t] = mine.top == top;
-    p.segments_before();
-    token = p.find(0, [&](float z, int) -> uint64_t { return order_key(z) == key; });
+  if (!uniform(ws.pending[r])) return;
+  if (t < 64) s.pow64[t] = kPow64[t];
+  Row<T> row;
+  if (!row.open(a, ws, r, s.pow64)) return;
+  s.segment_top[t] = t < row.segments ? row.stats[t].top : -INFINITY;
+  __syncthreads();
+  const Settings& st = row.st;
+  Searcher<T> p{row, s};
+  if (st.few()) {  // (for which the first launch forms no sums)
+    double x = 0.0;
+    p.visit([&](int g) { return uniform(s.segment_top[g]) > -INFINITY; },
+            [&](float z, int) { x += row.w.normal(z); }, [](int) {});
+    row.set_scale(block_reduce<kWaves>(x, s.slots_d, Add{}));
   } else {
-    const bool few = st.top_k > 0 && st.top_k <= kFewIds;
-    uint64_t whole_sum = 0;
-    // s.segment <- the segments' sums as whole numbers of 1 / scale, from sums relative to their own top
-    auto scale_sums = [&](double x) {
-      const double all = block_reduce(x, s.slots_d, Add{});
-      p.scale = ldexp(1.0, 61 - ilogb(all));
-      const uint64_t part = whole(x, p.scale);
-      s.segment[t] = part;
-      whole_sum = block_reduce(part, s.slots64, Add{});
-    };
-    if (few)
-      p.scale = 0x1p51;  // (at most kList weights of at most 1 are summed)
-    else
-      scale_sums(mine.top > -INFINITY ? mine.sum * p.w(mine.top) : 0.0);
-    const bool limited = st.top_k > 0 || st.top_p < 1.f || st.min_p > 0.f;
-    bool done = false;
-    if (limited && (few || st.top_k == 0)) {
-      const float least = p.few_limit(few ? st.top_k : kFewIds / 2, top);
-      const int n = p.gather(least);
-      done = n >= 0 && p.pick_from_list(n, least == -FLT_MAX, whole_sum, u, token, sum);
-    }
-    if (!done) {
-      if (few) {  // the list has not done, and the sums have not been formed
-        double x = 0.0;
-        for (int g = t >> 6; g < ws.segments; g += kWaves)
-          p.visit(g, [&](float z, int) { x += p.w(z); });
-        scale_sums(x);
-      }
-      Cut cut = kKeepAll;
-      bool summed = !limited;
-      if (limited) {
-        const float low = block_reduce(mine.low, s.slots_f, Min{});
-        if (st.top_k > 0) {
-          cut = p.template search<false>(static_cast<uint64_t>(st.top_k), low, top, summed);
-          if (st.top_p < 1.f) {
-            if (!summed) {
-              p.segment_sums(cut.key, [&](float z, int id) -> uint64_t {
-                return cut.keeps(order_key(z), id) ? whole(p.w(z), p.scale) : 0;
-              });
-              summed = true;
-            }
-            whole_sum = block_reduce(t < ws.segments ? s.segment[t] : uint64_t{0}, s.slots64, Add{});
-          }
-        }
-        if (st.top_p < 1.f) {
-          bool sums_of_it;
-          const Cut c = p.template search<true>(share_of(whole_sum, st.top_p),
-                                                fmaxf(low, top - 64.f * st.temperature), top,
-                                                sums_of_it);
-          summed = c.tighter(cut) && sums_of_it;
-          if (c.tighter(cut)) cut = c;
-        }
-        uint32_t key_low = 0;
-        if (st.min_p > 0.f) {
-          // the cut may keep ids below min_p: none below this key is kept
-          if (cut.key == 0 || p.w(key_logit(cut.key)) < st.min_p) summed = false;
-          const double least = top + static_cast<double>(st.temperature) * log(static_cast<double>(st.min_p));
-          key_low = order_key(static_cast<float>(least - 1e-6 * (1.0 + fabs(least))));
-        }
-        if (!summed) p.sum_kept(cut, key_low);
-      }
-      const uint64_t total = p.segments_before();
-      token = p.find(part_of(total, u), [&](float z, int id) -> uint64_t {
-        if (!cut.keeps(order_key(z), id)) return 0;
-        const double x = p.w(z);
-        return x >= st.min_p ? whole(x, p.scale) : 0;
-      });
-      sum = static_cast<double>(total) / p.scale;
-    }
+    row.sum_segments();
   }
-  float soft = 0.f;
-  if (a.conf)
-    soft = block_reduce(mine.soft * fast_exp2((mine.top - top) * kLog2e), s.slots_f, Add{});
-  if (t == 0) {
-    const float z = load_logit(p.row, token);
-    a.token[r] = token;
-    if (a.prob) a.prob[r] = st.greedy() ? 1.f : static_cast<float>(p.w(z) / sum);
-    if (a.conf) a.conf[r] = static_cast<float>(exp(static_cast<double>(z) - top) / soft);
+  uint64_t sum = row.whole_sum;
+  Cut cut = kKeepAll;
+  bool summed = false;
+  for (int kind = 0; kind < 2; ++kind) {  // top-k, then top-p of what it keeps
+    if (kind == 0 ? st.top_k == 0 : st.top_p >= 1.f) continue;
+    if (kind == 1 && st.top_k > 0) {
+      if (!summed) p.sum_kept(cut, 0, 0.f);
+      summed = true;
+      sum = p.sum_of_segments();
+    }
+    const uint64_t target = kind == 1 ? share_of(sum, st.top_p) : st.top_k;
+    const float from = kind == 1 ? fmaxf(row.low, row.top - 64.f * st.temperature) : row.low;
+    Cut c;
+    const bool found = p.search(kind == 1, target, from, row.top, c);
+    if (!found) c = p.search_bits(kind == 1, target);
+    summed = c.tighter(cut) && found;
+    if (c.tighter(cut)) cut = c;
   }
+  uint32_t key_low = 0;
+  if (st.min_p > 0.f) {
+    // the cut may keep ids below min_p: none below this key is kept
+    if (cut.key == 0 || row.w(key_logit(cut.key)) < st.min_p) summed = false;
+    const double least =
+        row.top + static_cast<double>(st.temperature) * log(static_cast<double>(st.min_p));
+    key_low = order_key(static_cast<float>(least - 1e-6 * (1.0 + fabs(least))));
+  }
+  if (!summed) p.sum_kept(cut, key_low, st.min_p);
+  const uint64_t total = p.sum_of_segments();
+  const int token = p.find(part_of(total, random_number(a, r)), [&](float z, int id) -> uint64_t {
+    if (!cut.keeps(order_key(z), id)) return 0;
+    const double x = row.w(z);
+    return x >= st.min_p ? whole(x, row.scale) : 0;
+  });
+  const float soft = row.model_sum(a);
+  if (t == 0) row.write(a, token, static_cast<double>(total) / row.scale, soft);
 }
 
 int segments_of(int vocab) { return (vocab + kSegment - 1) / kSegment; }
@@ -888,24 +1112,29 @@ size_t stats_bytes(int n_rows, int vocab) {
   const size_t n = static_cast<size_t>(n_rows) * segments_of(vocab) * sizeof(SegmentStats);
   return (n + 255) / 256 * 256;
 }
+size_t tops_bytes(int n_rows, int vocab) {
+  return static_cast<size_t>(n_rows) * segments_of(vocab) * 64 * sizeof(float);
+}
 
 template <class T>
 hipError_t launch(const SampleArgs& a, void* ws, hipStream_t s) {
   const int segments = segments_of(a.vocab);
-  const Workspace w{static_cast<SegmentStats*>(ws),
-                    reinterpret_cast<float*>(static_cast<char*>(ws) + stats_bytes(a.n_rows, a.vocab)),
-                    segments};
+  char* const tops = static_cast<char*>(ws) + stats_bytes(a.n_rows, a.vocab);
+  const Workspace w{static_cast<SegmentStats*>(ws), reinterpret_cast<float*>(tops),
+                    reinterpret_cast<uint32_t*>(tops + tops_bytes(a.n_rows, a.vocab)), segments};
   const int parts = (segments + kScanWaves - 1) / kScanWaves;
   hipLaunchKernelGGL(sample_scan_kernel<T>, dim3(a.n_rows * parts), dim3(kScanThreads), 0, s, a, w);
-  hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.n_rows), dim3(kThreads), 0, s, a, w);
+  hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.n_rows), dim3(kPickThreads), 0, s, a, w);
+  // rows are left only where something limits them and the list does not hold them whole
+  if ((a.top_k || a.top_p || a.min_p) && a.vocab > kPickList)
+    hipLaunchKernelGGL(sample_search_kernel<T>, dim3(a.n_rows), dim3(kThreads), 0, s, a, w);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t sample_ws_bytes(int n_rows, int vocab) {
-  return stats_bytes(n_rows, vocab) +
-         static_cast<size_t>(n_rows) * segments_of(vocab) * 64 * sizeof(float);
+  return stats_bytes(n_rows, vocab) + tops_bytes(n_rows, vocab) + n_rows * sizeof(uint32_t);
 }
 
 long sample_threads(int n_rows, int vocab) {

@@ -267,6 +267,19 @@ def test_random_numbers_at_the_ends(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("settings", [dict(), dict(top_p=0.999), dict(top_k=3000), dict(min_p=1e-30)])
+def test_weights_that_vanish(settings, dtype):
+    """Low temperatures: whole segments whose weights are 0 in 64 bits, before the ids that are drawn."""
+    z = np.full((6, 9000), -40.0)
+    z[:, 5000:5010] = np.linspace(0, 1, 10)
+    z[:, 7000] = -0.5
+    u = [0.0, 0.2, 0.4, 0.6, 0.8, 1 - 2.0 ** -24]
+    for t in (0.05, 0.01, 0.002):
+        token, _, _ = Draw(z, u, dtype=dtype, temperature=t, **settings).check()
+        assert (token >= 5000).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [8, 4096, 65536])
 def test_equal_logits(V, dtype):
     """All logits equal: sums are whole numbers, and u or top_p on a border are decided exactly; the
