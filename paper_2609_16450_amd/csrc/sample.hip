@@ -20,6 +20,7 @@
 // more ids than the list (logits that tie, or a few that lie far off the others), the cut's key is
 // found bit by bit instead.
 #include <float.h>
+#include <stddef.h>
 
 #include <type_traits>
 
@@ -43,6 +44,7 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kMaxSegments = kThreads;
 constexpr int kList = kThreads;  // ids that it sorts in LDS
 constexpr int kBins = 2048;
+constexpr int kSearchVocab = 32768;  // rows of more ids are searched by many workgroups
 static_assert(kMaxSegments * kSegment >= kSampleMaxVocab, "a thread per segment");
 
 typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));  // at any 2 bytes
@@ -210,11 +212,25 @@ __device__ __forceinline__ Settings settings(const SampleArgs& a, int b) {
   s.top_k = k > 0 && k < a.vocab ? k : 0;
   return s;
 }
+// What the launches that search a row leave one another; zeroed by the second launch.
+struct SearchState {
+  uint32_t count[kBins], mass[kBins];  // ids and weights (of 2^-31 of their sum) per bin
+  uint64_t between;                    // weight between `first` and bin_k
+  uint32_t n_list[2];
+  int32_t first, bin_k, bin_m;  // the cut's bin; top-k's and min-p's (kBins: no limit)
+  uint32_t before_k;            // ids in the bins before bin_k
+  uint64_t list[2][kList];      // ids of bin `first`, of bin_k
+};
+static_assert(sizeof(SearchState) % 16 == 0, "whole 16-byte words");
+
 struct Workspace {
   SegmentStats* stats;  // [n_rows, segments]
   float* group_top;     // [n_rows, segments, 64]: largest logit of a lane's ids
-  uint32_t* pending;    // [n_rows]: the second launch has left it to the third
+  uint32_t* pending;    // [n_rows]: the second launch has left it to the next ones
+  uint64_t* kept;       // [n_rows, segments]: sums above a cut's bin
+  SearchState* states;  // [n_rows]
   int segments;
+  int parts;  // workgroups per row of the launches that search
 };
 
 // x, which is the same on every lane, as a scalar: what depends on it alone takes no vector registers,
@@ -732,27 +748,263 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
     done = n > 0 && pick_from_list(a, row, s, n, complete);
   }
   if (t == 0) ws.pending[row.r] = !done;
+  if (!done && row.vocab > kSearchVocab) {  // (all but the lists)
+    u32x4* const state = reinterpret_cast<u32x4*>(&ws.states[row.r]);
+    for (int i = t; i < static_cast<int>(offsetof(SearchState, list) / 16); i += kPickThreads)
+      state[i] = u32x4{};
+  }
 }
 
 // ---------------------------------------------------------------------------------------
-// Third launch: a workgroup of 16 waves for each row that the second has left.
+// The rows that the second launch has left: cuts anywhere.  Of more than kSearchVocab ids, three
+// launches: a histogram of a row by its parts' workgroups, which tells the bin that the cut lies in;
+// the exact sums above the bin, segment by segment, with the bin's ids put into a list, by
+// workgroups again; and a workgroup that sorts the list, cuts and draws.  The last one alone also does
+// rows of fewer ids, and those that the others have not found the cut of.
 // ---------------------------------------------------------------------------------------
+constexpr int kPartThreads = 256;
+constexpr int kPartWaves = kPartThreads / 64;
+
+// f(z, id) for every id that this lane holds of segments first + wave, first + wave + kN, .. below
+// `end` for which wanted(g); then each_segment(g) (by the whole wave) for these and the others.
+// kAtOnce loads at a time, the next ones under way meanwhile, worked on by two ids: with more of them
+// under way the kernels of 16 waves spill.
+template <int kN, int kAtOnce, class T, class Wanted, class F, class End>
+__device__ __forceinline__ void visit(const Row<T>& row, int first, int end, Wanted wanted, F f,
+                                      End each_segment) {
+  const int lane = threadIdx.x & 63;
+  for (int g = first + wave_index(); g < end; g += kN) {
+    if (wanted(g)) {
+      Chunk<T> x[kAtOnce], next[kAtOnce];
+      auto load = [&](int i0, Chunk<T> (&c)[kAtOnce]) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          c[i].load(row.logits, g * kSegment + id_in_segment<T>(i0 + i, lane), row.vocab);
+      };
+      load(0, x);
+#pragma unroll 1
+      for (int i0 = 0; i0 < kLoads<T>; i0 += kAtOnce) {
+        if (i0 + kAtOnce < kLoads<T>) load(i0 + kAtOnce, next);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+          for (int e = 0; e < kVec<T>; ++e) {
+            if (e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            f(x[i][e], g * kSegment + id_in_segment<T>(i0 + i, lane) + e);
+          }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) x[i] = next[i];
+      }
+    }
+    each_segment(g);
+  }
+}
+
+// Bins of equal width from a row's largest logit down, the last one for all that lies lower; a higher
+// logit never has a higher bin.
+struct Bins {
+  float half_top, per;
+  template <class T>
+  __device__ __forceinline__ explicit Bins(const Row<T>& row) {
+    // (what weighs less than e^-64 of the largest needs no bin of its own; halves: no overflow)
+    const float from = fmaxf(row.low, row.top - 64.f * row.st.temperature);
+    half_top = 0.5f * row.top;
+    per = (kBins - 1) / (half_top - 0.5f * from);
+  }
+  __device__ __forceinline__ bool usable() const { return per < FLT_MAX; }
+  __device__ __forceinline__ int operator()(float z) const {
+    return static_cast<int>(fminf((half_top - 0.5f * z) * per, kBins - 1.f));
+  }
+};
+
+// The least logit whose weight is at least min_p: from its formula, then, as the weights themselves
+// round, by steps to the next float.
+template <class T>
+__device__ __forceinline__ float min_p_logit(const Row<T>& row) {
+  const double z = row.top + static_cast<double>(row.st.temperature) *
+                                 log(static_cast<double>(row.st.min_p));
+  uint32_t key = order_key(fminf(fmaxf(static_cast<float>(z), -FLT_MAX), row.top));
+  auto reaches = [&](uint32_t k) { return row.w(key_logit(k)) >= row.st.min_p; };
+  for (int i = 0; i < 8 && !reaches(key); ++i) ++key;
+  for (int i = 0; i < 8 && reaches(key - 1); ++i) --key;
+  return key_logit(key);
+}
+
+// Whether the launches over parts have to do with a row (of those left).
+template <class T>
+__device__ __forceinline__ bool in_parts(const Row<T>& row) {
+  return row.vocab > kSearchVocab && !row.st.few() && Bins(row).usable();
+}
+
+__device__ __forceinline__ int part_begin(int part, int parts, int segments) {
+  return static_cast<int>(static_cast<long>(segments) * part / parts);
+}
+
+template <class T>
+__global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a, Workspace ws) {
+  __shared__ uint32_t count[kBins], mass[kBins];
+  __shared__ double pow64[64];
+  const int t = threadIdx.x, r = blockIdx.x / ws.parts, part = blockIdx.x - r * ws.parts;
+  if (!uniform(ws.pending[r])) return;
+  if (t < 64) pow64[t] = kPow64[t];
+  for (int i = t; i < kBins; i += kPartThreads) count[i] = mass[i] = 0;
+  Row<T> row;
+  if (!row.open(a, ws, r, pow64) || !in_parts(row)) return;
+  const bool by_count = row.st.top_k > 0, by_mass = row.st.top_p < 1.f;
+  if (!by_count && !by_mass) return;
+  __syncthreads();
+  row.sum_segments();
+  // weights as whole numbers of 2^-31 of (at most) their sum (a float's atomic sum takes 8 times as
+  // long in LDS)
+  const float rate = static_cast<float>(row.w.rate / 64.0);
+  const float unit = static_cast<float>(ilogb(row.scale) - 31);
+  const float top = row.top;
+  const Bins bin(row);
+  visit<kPartWaves, 4>(
+      row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
+      [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
+      [&](float z, int) {
+        if (!(z > -INFINITY)) return;
+        const int b = bin(z);
+        if (by_count) atomicAdd(&count[b], 1u);
+        if (by_mass)
+          atomicAdd(&mass[b], static_cast<uint32_t>(fast_exp2((z - top) * rate + unit)));
+      },
+      [](int) {});
+  __syncthreads();
+  SearchState& state = ws.states[r];
+  for (int i = t; i < kBins; i += kPartThreads) {
+    if (by_count && count[i]) atomicAdd(&state.count[i], count[i]);
+    if (by_mass && mass[i]) atomicAdd(&state.mass[i], mass[i]);
+  }
+}
+
+// The bin in which the running sum of x (kBins / kPartThreads bins a thread) reaches `target`, with the
+// sum before it and its own; kBins where none does.
+struct FoundBin {
+  int bin;
+  uint64_t before, own;
+};
+__device__ __forceinline__ FoundBin find_bin(const uint32_t* x, uint64_t target, uint64_t* slots,
+                                             FoundBin* found) {
+  constexpr int kEach = kBins / kPartThreads;
+  const int t = threadIdx.x;
+  uint32_t v[kEach];
+  uint64_t mine = 0, total;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    v[e] = x[t * kEach + e];
+    mine += v[e];
+  }
+  __syncthreads();  // (what an earlier call has found has been read)
+  if (t == 0) *found = FoundBin{kBins, 0, 0};
+  uint64_t run = block_scan<kPartWaves>(mine, slots, total);
+  if (run < target && run + mine >= target) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      if (run < target && run + v[e] >= target) *found = FoundBin{t * kEach + e, run, v[e]};
+      run += v[e];
+    }
+  }
+  __syncthreads();
+  return FoundBin{uniform(found->bin), uniform(found->before), uniform(found->own)};
+}
+
+template <class T>
+__global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a, Workspace ws) {
+  __shared__ double pow64[64];
+  __shared__ uint64_t slots64[kPartWaves];
+  __shared__ FoundBin found;
+  const int t = threadIdx.x, r = blockIdx.x / ws.parts, part = blockIdx.x - r * ws.parts;
+  if (!uniform(ws.pending[r])) return;
+  if (t < 64) pow64[t] = kPow64[t];
+  Row<T> row;
+  if (!row.open(a, ws, r, pow64) || !in_parts(row)) return;
+  __syncthreads();
+  row.sum_segments();
+  const Settings& st = row.st;
+  const Bins bin(row);
+  SearchState& state = ws.states[r];
+  // the bin of each limit, kBins where it limits nothing; the first of them holds the cut
+  int bin_k = kBins, bin_p = kBins, bin_m = kBins;
+  uint64_t before_k = 0;
+  if (st.top_k > 0) {
+    const FoundBin f = find_bin(state.count, static_cast<uint64_t>(st.top_k), slots64, &found);
+    bin_k = f.bin;
+    before_k = f.before;
+  }
+  if (st.top_p < 1.f) {
+    uint64_t all = row.whole_sum >> 31;
+    if (bin_k < kBins) {  // the weight of the bins up to bin_k, about that of the first top_k ids
+      uint64_t x = 0;
+      for (int i = t; i <= bin_k; i += kPartThreads) x += state.mass[i];
+      all = block_reduce<kPartWaves>(x, slots64, Add{});
+    }
+    const uint64_t target = max(share_of(all, st.top_p), uint64_t{1});
+    bin_p = find_bin(state.mass, target, slots64, &found).bin;
+  }
+  if (st.min_p > 0.f) bin_m = bin(min_p_logit(row));
+  const int first = min(min(bin_k, bin_p), bin_m);
+  const bool between = st.top_p < 1.f && bin_k < kBins && bin_k > first;
+  const int last = between ? bin_k : first;
+  if (part == 0 && t == 0) {
+    state.first = first;
+    state.bin_k = bin_k;
+    state.bin_m = bin_m;
+    state.before_k = static_cast<uint32_t>(before_k);
+  }
+  auto append = [&](int which, float z, int id) {
+    const uint32_t j = atomicAdd(&state.n_list[which], 1u);
+    if (j < kList) state.list[which][j] = entry_of(z, id);
+  };
+  double sum = 0.0, sum_between = 0.0;
+  const int last_of_row = last;
+  visit<kPartWaves, 4>(
+      row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
+      [&](int g) {
+        const float top = uniform(row.stats[g].top);
+        return top > -INFINITY && uniform(bin(top)) <= last_of_row;
+      },
+      [&](float z, int id) {
+        const int b = bin(z);
+        if (b > last || !(z > -INFINITY)) return;
+        if (b == first) {
+          append(0, z, id);
+        } else if (b < first) {
+          sum += row.w.normal(z);
+        } else if (b < bin_k) {
+          sum_between += row.w.normal(z);
+        } else {
+          append(1, z, id);
+        }
+      },
+      [&](int g) {
+        sum = wave_reduce(sum, Add{});
+        if ((t & 63) == 0)
+          ws.kept[static_cast<size_t>(r) * ws.segments + g] = whole(sum, row.scale);
+        sum = 0.0;
+      });
+  if (between) {
+    sum_between = wave_reduce(sum_between, Add{});
+    if ((t & 63) == 0)
+      atomicAdd(reinterpret_cast<unsigned long long*>(&state.between),
+                static_cast<unsigned long long>(whole(sum_between, row.scale)));
+  }
+}
+
 struct Shared {
-  uint64_t segment[kMaxSegments];  // a sum per segment, then the sum before it
-  float segment_top[kMaxSegments];
+  uint64_t segment[kMaxSegments];
   union {
-    struct {
-      uint64_t list[kList], mass[kList];
-    };
+    uint64_t list[kList];
     uint64_t bin_mass[kBins];
   };
   uint32_t bins[kBins];
   double pow64[64];
   uint64_t slots64[kWaves];
   double slots_d[kWaves];
-  float slots_f[kWaves];
   uint32_t slots32[kWaves];
-  uint32_t n_list, n_groups, found, found_count, found_before;
+  uint32_t found, found_count, found_before;
   uint64_t found_mass, found_mass_before;
   int32_t found_id;
 };
@@ -789,55 +1041,21 @@ struct Searcher {
   Row<T>& row;
   Shared& s;
 
-  // ---- the row's segments, wave by wave -----------------------------------------------
-  // f(z, id) for every id that this lane holds of segments wave, wave + kWaves, .. for which
-  // wanted(g); then each_segment(g) (by the whole wave) for these and the others.  Two loads at a time,
-  // the next two under way meanwhile, worked on by two ids (with more of them under way the kernel
-  // spilled).
-  template <class Wanted, class F, class End>
-  __device__ __forceinline__ void visit(Wanted wanted, F f, End each_segment) const {
-    const int lane = threadIdx.x & 63;
-    constexpr int kAtOnce = 2;
-    for (int g = wave_index(); g < row.segments; g += kWaves) {
-      if (wanted(g)) {
-        Chunk<T> x[kAtOnce], next[kAtOnce];
-        auto load = [&](int i0, Chunk<T> (&c)[kAtOnce]) {
-#pragma unroll
-          for (int i = 0; i < kAtOnce; ++i)
-            c[i].load(row.logits, g * kSegment + id_in_segment<T>(i0 + i, lane), row.vocab);
-        };
-        load(0, x);
-#pragma unroll 1
-        for (int i0 = 0; i0 < kLoads<T>; i0 += kAtOnce) {
-          if (i0 + kAtOnce < kLoads<T>) load(i0 + kAtOnce, next);
-#pragma unroll
-          for (int i = 0; i < kAtOnce; ++i)
-#pragma unroll
-            for (int e = 0; e < kVec<T>; ++e) {
-              if (e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-              f(x[i][e], g * kSegment + id_in_segment<T>(i0 + i, lane) + e);
-            }
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int i = 0; i < kAtOnce; ++i) x[i] = next[i];
-        }
-      }
-      each_segment(g);
-    }
-  }
   // s.segment[g] <- sum of f(z, id) over the segments whose largest logit has a key of at least
   // key_low, 0 for the others.
   template <class F>
   __device__ __forceinline__ void segment_sums(uint32_t key_low, F f) const {
     __syncthreads();
     uint64_t sum = 0;
-    visit([&](int g) { return order_key(uniform(s.segment_top[g])) >= key_low; },
-          [&](float z, int id) { sum += f(z, id); },
-          [&](int g) {
-            sum = wave_reduce(sum, Add{});
-            if ((threadIdx.x & 63) == 0) s.segment[g] = sum;
-            sum = 0;
-          });
+    visit<kWaves, 2>(
+        row, 0, row.segments,
+        [&](int g) { return order_key(uniform(row.stats[g].top)) >= key_low; },
+        [&](float z, int id) { sum += f(z, id); },
+        [&](int g) {
+          sum = wave_reduce(sum, Add{});
+          if ((threadIdx.x & 63) == 0) s.segment[g] = sum;
+          sum = 0;
+        });
     __syncthreads();
   }
   // Sum of s.segment, as every wave finds it.
@@ -854,135 +1072,106 @@ struct Searcher {
         x, [&](int i) { return i < row.segments ? s.segment[i] : uint64_t{0}; }, before);
     return row.template find_id<kWaves>(s, g, before, x, f);
   }
-
-  // ---- a cut anywhere in the row -----------------------------------------------------------
   // s.segment <- sums of the kept ids' weights, none of which has a key below key_low.
   __device__ __forceinline__ void sum_kept(const Cut& cut, uint32_t key_low, float min_p) const {
     const uint32_t least = max(cut.key, key_low);
     double sum = 0.0;
     __syncthreads();
-    visit([&](int g) { return order_key(uniform(s.segment_top[g])) >= least; },
-          [&](float z, int id) {
-            const double x = row.w(z);
-            if (cut.keeps(order_key(z), id) && x >= min_p) sum += x;
-          },
-          [&](int g) {
-            sum = wave_reduce(sum, Add{});
-            if ((threadIdx.x & 63) == 0) s.segment[g] = whole(sum, row.scale);
-            sum = 0.0;
-          });
+    visit<kWaves, 2>(
+        row, 0, row.segments,
+        [&](int g) { return order_key(uniform(row.stats[g].top)) >= least; },
+        [&](float z, int id) {
+          const double x = row.w(z);
+          if (cut.keeps(order_key(z), id) && x >= min_p) sum += x;
+        },
+        [&](int g) {
+          sum = wave_reduce(sum, Add{});
+          if ((threadIdx.x & 63) == 0) s.segment[g] = whole(sum, row.scale);
+          sum = 0.0;
+        });
     __syncthreads();
   }
 
-  // The cut behind the first `target` ids of the order (by_mass false), or behind the fewest whose
-  // weights come to `target` (true), and in s.segment the sums of what it keeps; false where this
-  // does not find it.
-  //
-  // A histogram over [low, top] by value, of counts, or of weights in 32 bits, which is only to find
-  // the bin; then the exact sums above the bin, segment by segment, with the bin's ids into the
-  // list.  Where the histogram's rounding has led to the bin next to the right one, the exact sums say
-  // so.
-  __device__ __forceinline__ bool search(bool by_mass, uint64_t target, float low, float top,
-                                         Cut& cut) const {
-    const int t = threadIdx.x, lane = t & 63;
-    const float per = (kBins - 1) / (0.5f * top - 0.5f * low);  // (halves: no overflow)
-    if (!(per < FLT_MAX)) return false;
-    auto bin = [&](float z) {
-      return static_cast<int>(fminf((0.5f * top - 0.5f * z) * per, kBins - 1.f));
-    };
+  // One of a state's lists, sorted: this thread's entry with its weight, and the weights of the list
+  // before it.
+  __device__ __forceinline__ int sorted_list(const SearchState& state, int which, uint64_t& entry,
+                                             double& x, uint64_t& mass, uint64_t& before,
+                                             uint64_t& total) const {
+    const int t = threadIdx.x, n = static_cast<int>(uniform(state.n_list[which]));
     __syncthreads();
-    for (int i = t; i < kBins; i += kThreads) s.bins[i] = 0;
-    if (t == 0) s.found = kBins - 1;
+    if (t < n) s.list[t] = state.list[which][t];
     __syncthreads();
-    // weights as whole numbers of 2^-31 of (at most) their sum (a float's atomic sum takes 8 times as long
-    // in LDS)
-    const float rate2 = static_cast<float>(row.w.rate / 64.0);
-    const float unit = static_cast<float>(ilogb(row.scale) - 31);
-    visit([&](int g) { return uniform(s.segment_top[g]) > -INFINITY; },
-          [&](float z, int) {
-            if (!(z > -INFINITY)) return;
-            const uint32_t n = by_mass ? static_cast<uint32_t>(fast_exp2((z - top) * rate2 + unit)) : 1u;
-            atomicAdd(&s.bins[bin(z)], n);
-          },
-          [](int) {});
-    __syncthreads();
-    auto take = [&](auto before, auto x0, auto x1, auto want) {
-      if (before < want && before + x0 >= want)
-        s.found = 2 * t;
-      else if (before + x0 < want && before + x0 + x1 >= want)
-        s.found = 2 * t + 1;
-    };
-    {
-      const uint64_t x0 = s.bins[2 * t], x1 = s.bins[2 * t + 1];
-      uint64_t all;
-      const uint64_t before = block_scan<kWaves>(x0 + x1, s.slots64, all);
-      take(before, x0, x1, by_mass ? max(target >> 31, uint64_t{1}) : target);
-    }
-    __syncthreads();
-    int at_bin = static_cast<int>(uniform(s.found));
-
-    uint64_t above;
-    for (int tries = 0;; ++tries) {
-      __syncthreads();
-      if (t == 0) s.n_list = 0;
-      __syncthreads();
-      uint64_t n_above = 0, m_inside = 0;
-      double sum = 0.0;
-      visit([&](int g) { return uniform(s.segment_top[g]) > -INFINITY && uniform(bin(s.segment_top[g])) <= at_bin; },
-            [&](float z, int id) {
-              const int b = bin(z);
-              if (b > at_bin || !(z > -INFINITY)) return;
-              const double x = row.w.normal(z);
-              if (b < at_bin) {
-                sum += x;
-                if (!by_mass) ++n_above;
-                return;
-              }
-              if (by_mass) m_inside += whole(x, row.scale);
-              const uint32_t j = atomicAdd(&s.n_list, 1u);
-              if (j < kList)
-                s.list[j] = entry_of(z, id);
-            },
-            [&](int g) {
-              sum = wave_reduce(sum, Add{});
-              if (lane == 0) s.segment[g] = whole(sum, row.scale);
-              sum = 0.0;
-            });
-      __syncthreads();
-      uint64_t inside = block_reduce<kWaves>(by_mass ? m_inside : uint64_t{0}, s.slots64, Add{});
-      above = by_mass ? (t < row.segments ? s.segment[t] : 0) : n_above;
-      above = block_reduce<kWaves>(above, s.slots64, Add{});
-      if (!by_mass) inside = uniform(s.n_list);
-      int step = 0;
-      if (above >= target)
-        step = -1;
-      else if (above + inside < target)
-        step = 1;
-      if (step == 0) break;
-      at_bin += step;
-      if (tries == 2 || at_bin < 0 || at_bin >= kBins) return false;
-    }
-    const int n = static_cast<int>(uniform(s.n_list));
-    if (n > kList) return false;
     sort_falling(s.list, n);
-    const uint64_t entry = t < n ? s.list[t] : 0;
-    const uint64_t mass = t < n ? whole(row.w(key_logit(entry_key(entry))), row.scale) : 0;
-    uint64_t total;
-    const uint64_t step = by_mass ? mass : t < n ? 1 : 0;
-    const uint64_t before = above + block_scan<kWaves>(step, s.slots64, total);
-    if (t < n && before < target) {  // kept
+    entry = t < n ? s.list[t] : 0;
+    x = t < n ? row.w(key_logit(entry_key(entry))) : 0.0;
+    mass = whole(x, row.scale);
+    before = block_scan<kWaves>(mass, s.slots64, total);
+    return n;
+  }
+
+  // The cut from what the launches over parts have found, with the kept ids' sums in s.segment; false
+  // where a list has run over, or a rounding of the histogram has led to a bin without the cut.
+  __device__ __forceinline__ bool cut_from_lists(const SearchState& state, const uint64_t* kept_sums,
+                                                 Cut& cut) const {
+    const int t = threadIdx.x;
+    const Settings& st = row.st;
+    const int first = uniform(state.first), bin_k = uniform(state.bin_k);
+    if (first >= kBins || uniform(state.n_list[0]) > kList || uniform(state.n_list[1]) > kList)
+      return false;
+    for (int g = t; g < row.segments; g += kThreads) s.segment[g] = kept_sums[g];
+    const int n_k = st.top_k - static_cast<int>(uniform(state.before_k));  // of bin_k's ids
+    uint64_t entry, mass, before, in_list, of_k = 0;
+    double x;
+    if (st.top_p < 1.f && bin_k < kBins && bin_k > first) {
+      sorted_list(state, 1, entry, x, mass, before, in_list);
+      if (t == n_k - 1) s.found_mass = before + mass;
+      __syncthreads();
+      of_k = uniform(s.found_mass) + uniform(state.between);
+    }
+    const int n = sorted_list(state, 0, entry, x, mass, before, in_list);
+    const uint64_t above = sum_of_segments();
+    bool kept = t < n, closed = false;
+    const bool by_min_p = uniform(state.bin_m) == first;
+    if (bin_k == first) {
+      kept &= t < n_k;
+      closed = true;
+    }
+    if (st.top_p < 1.f) {
+      uint64_t all = row.whole_sum;
+      if (bin_k == first) {
+        if (t == n_k - 1) s.found_mass = before + mass;
+        __syncthreads();
+        all = above + uniform(s.found_mass);
+      } else if (bin_k < kBins) {
+        all = above + in_list + of_k;
+      }
+      const uint64_t target = share_of(all, st.top_p);
+      if (above >= target) return false;
+      kept &= above + before < target;
+      closed |= above + in_list >= target;
+    }
+    if (st.min_p > 0.f) {
+      kept &= x >= st.min_p;
+      closed |= by_min_p;
+    }
+    if (!closed) return false;
+    if (n == 0) {  // nothing between the bins above and min_p
+      cut = kKeepAll;
+      return by_min_p;
+    }
+    if (kept)
       atomicAdd(reinterpret_cast<unsigned long long*>(&s.segment[entry_id(entry) / kSegment]),
                 static_cast<unsigned long long>(mass));
-      if (before + step >= target) s.found = static_cast<uint32_t>(t);
-    }
-    __syncthreads();
-    const uint64_t last = uniform(s.list[s.found]);
-    cut = Cut{entry_key(last), entry_id(last)};
+    // (the kept ones of the list are its first)
+    const uint32_t n_kept = block_reduce<kWaves>(static_cast<uint32_t>(kept), s.slots32, Add{});
+    const uint64_t last = uniform(s.list[n_kept ? n_kept - 1 : 0]);
+    cut = Cut{entry_key(last), entry_id(last) - (n_kept ? 0 : 1)};
     return true;
   }
 
-  // The same by three rounds over the row, which fix 11, 11 and 10 bits of the key, with exact sums;
-  // then, where not all ids of that key are kept, their last one.
+  // The cut behind the first `target` ids of the order (by_mass false), or behind the fewest whose
+  // weights come to `target` (true), by three rounds over the row, which fix 11, 11 and 10 bits of the
+  // key; then, where not all ids of that key are kept, their last one.
   __device__ __forceinline__ Cut search_bits(bool by_mass, uint64_t target) const {
     const int t = threadIdx.x;
     uint32_t prefix = 0;
@@ -997,16 +1186,18 @@ struct Searcher {
       }
       if (t == 0) s.found_count = 0;
       __syncthreads();
-      visit([&](int g) { return uniform(s.segment_top[g]) > -INFINITY; },
-            [&](float z, int) {
-              const uint32_t key = order_key(z);
-              if (!(z > -INFINITY) || (level > 0 && (key >> above) != prefix)) return;
-              const uint32_t bin = (key >> shift) & mask;
-              atomicAdd(&s.bins[bin], 1u);
+      visit<kWaves, 2>(
+          row, 0, row.segments, [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
+          [&](float z, int) {
+            const uint32_t key = order_key(z);
+            if (!(z > -INFINITY) || (level > 0 && (key >> above) != prefix)) return;
+            const uint32_t bin = (key >> shift) & mask;
+            atomicAdd(&s.bins[bin], 1u);
+            if (by_mass)
               atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin_mass[bin]),
                         static_cast<unsigned long long>(whole(row.w(z), row.scale)));
-            },
-            [](int) {});
+          },
+          [](int) {});
       __syncthreads();
       // bins from the highest down, two a thread
       const int hi = kBins - 1 - 2 * t;
@@ -1035,7 +1226,7 @@ struct Searcher {
       m_before = uniform(s.found_mass_before);
     }
     // every id of the last bin has the same key and weight
-    const uint64_t equal = uniform(s.found_count), each = uniform(s.found_mass) / equal;
+    const uint64_t equal = uniform(s.found_count), each = uniform(s.found_mass) / equal;  // (if by_mass)
     const uint64_t keep = by_mass ? (target - m_before + each - 1) / each : target - n_before;
     Cut cut{prefix, INT32_MAX};
     if (keep < equal) {
@@ -1049,7 +1240,6 @@ struct Searcher {
   }
 };
 
-// The rows that sample_pick_kernel has left.
 template <class T>
 __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, Workspace ws) {
   __shared__ Shared s;
@@ -1058,45 +1248,34 @@ __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, W
   if (t < 64) s.pow64[t] = kPow64[t];
   Row<T> row;
   if (!row.open(a, ws, r, s.pow64)) return;
-  s.segment_top[t] = t < row.segments ? row.stats[t].top : -INFINITY;
   __syncthreads();
   const Settings& st = row.st;
-  Searcher<T> p{row, s};
-  if (st.few()) {  // (for which the first launch forms no sums)
-    double x = 0.0;
-    p.visit([&](int g) { return uniform(s.segment_top[g]) > -INFINITY; },
-            [&](float z, int) { x += row.w.normal(z); }, [](int) {});
-    row.set_scale(block_reduce<kWaves>(x, s.slots_d, Add{}));
-  } else {
-    row.sum_segments();
-  }
-  uint64_t sum = row.whole_sum;
+  const Searcher<T> p{row, s};
+  if (!st.few()) row.sum_segments();
   Cut cut = kKeepAll;
-  bool summed = false;
-  for (int kind = 0; kind < 2; ++kind) {  // top-k, then top-p of what it keeps
-    if (kind == 0 ? st.top_k == 0 : st.top_p >= 1.f) continue;
-    if (kind == 1 && st.top_k > 0) {
-      if (!summed) p.sum_kept(cut, 0, 0.f);
-      summed = true;
-      sum = p.sum_of_segments();
+  if (!in_parts(row) ||
+      !p.cut_from_lists(ws.states[r], ws.kept + static_cast<size_t>(r) * ws.segments, cut)) {
+    if (st.few()) {  // (for which the first launch forms no sums)
+      double x = 0.0;
+      visit<kWaves, 2>(
+          row, 0, row.segments, [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
+          [&](float z, int) { x += row.w.normal(z); }, [](int) {});
+      row.set_scale(block_reduce<kWaves>(x, s.slots_d, Add{}));
     }
-    const uint64_t target = kind == 1 ? share_of(sum, st.top_p) : st.top_k;
-    const float from = kind == 1 ? fmaxf(row.low, row.top - 64.f * st.temperature) : row.low;
-    Cut c;
-    const bool found = p.search(kind == 1, target, from, row.top, c);
-    if (!found) c = p.search_bits(kind == 1, target);
-    summed = c.tighter(cut) && found;
-    if (c.tighter(cut)) cut = c;
+    uint64_t sum = row.whole_sum;
+    cut = kKeepAll;
+    for (int kind = 0; kind < 2; ++kind) {  // top-k, then top-p of what it keeps
+      if (kind == 0 ? st.top_k == 0 : st.top_p >= 1.f) continue;
+      if (kind == 1 && st.top_k > 0) {
+        p.sum_kept(cut, 0, 0.f);
+        sum = p.sum_of_segments();
+      }
+      const Cut c = p.search_bits(kind == 1, kind == 1 ? share_of(sum, st.top_p) : st.top_k);
+      if (c.tighter(cut)) cut = c;
+    }
+    p.sum_kept(cut, st.min_p > 0.f ? order_key(min_p_logit(row)) : 0, st.min_p);
   }
-  uint32_t key_low = 0;
-  if (st.min_p > 0.f) {
-    // the cut may keep ids below min_p: none below this key is kept
-    if (cut.key == 0 || row.w(key_logit(cut.key)) < st.min_p) summed = false;
-    const double least =
-        row.top + static_cast<double>(st.temperature) * log(static_cast<double>(st.min_p));
-    key_low = order_key(static_cast<float>(least - 1e-6 * (1.0 + fabs(least))));
-  }
-  if (!summed) p.sum_kept(cut, key_low, st.min_p);
+  __syncthreads();
   const uint64_t total = p.sum_of_segments();
   const int token = p.find(part_of(total, random_number(a, r)), [&](float z, int id) -> uint64_t {
     if (!cut.keeps(order_key(z), id)) return 0;
@@ -1108,38 +1287,65 @@ __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, W
 }
 
 int segments_of(int vocab) { return (vocab + kSegment - 1) / kSegment; }
-size_t stats_bytes(int n_rows, int vocab) {
-  const size_t n = static_cast<size_t>(n_rows) * segments_of(vocab) * sizeof(SegmentStats);
-  return (n + 255) / 256 * 256;
-}
-size_t tops_bytes(int n_rows, int vocab) {
-  return static_cast<size_t>(n_rows) * segments_of(vocab) * 64 * sizeof(float);
+
+// Where a call's intermediate results lie in its workspace.
+struct Layout {
+  size_t tops, pending, kept, states, bytes;
+  Layout(int n_rows, int vocab) {
+    const size_t n = n_rows, segments = segments_of(vocab);
+    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    tops = up(n * segments * sizeof(SegmentStats));
+    pending = tops + up(n * segments * 64 * sizeof(float));
+    kept = pending + up(n * sizeof(uint32_t));
+    states = bytes = kept;
+    if (vocab > kSearchVocab) {
+      states = kept + up(n * segments * sizeof(uint64_t));
+      bytes = states + n * sizeof(SearchState);
+    }
+  }
+};
+
+// Workgroups per row of the launches over parts: about 2048 in all, at most 16 of a row (a wave has a
+// segment of its own then, at 2^17 ids).
+int parts_of(int n_rows, int vocab) {
+  return max(1, min(min(2048 / n_rows, 16), (segments_of(vocab) + kPartWaves - 1) / kPartWaves));
 }
 
 template <class T>
 hipError_t launch(const SampleArgs& a, void* ws, hipStream_t s) {
   const int segments = segments_of(a.vocab);
-  char* const tops = static_cast<char*>(ws) + stats_bytes(a.n_rows, a.vocab);
-  const Workspace w{static_cast<SegmentStats*>(ws), reinterpret_cast<float*>(tops),
-                    reinterpret_cast<uint32_t*>(tops + tops_bytes(a.n_rows, a.vocab)), segments};
-  const int parts = (segments + kScanWaves - 1) / kScanWaves;
-  hipLaunchKernelGGL(sample_scan_kernel<T>, dim3(a.n_rows * parts), dim3(kScanThreads), 0, s, a, w);
+  const Layout at(a.n_rows, a.vocab);
+  char* const base = static_cast<char*>(ws);
+  const Workspace w{reinterpret_cast<SegmentStats*>(base),
+                    reinterpret_cast<float*>(base + at.tops),
+                    reinterpret_cast<uint32_t*>(base + at.pending),
+                    reinterpret_cast<uint64_t*>(base + at.kept),
+                    reinterpret_cast<SearchState*>(base + at.states),
+                    segments,
+                    parts_of(a.n_rows, a.vocab)};
+  const int groups = (segments + kScanWaves - 1) / kScanWaves;
+  hipLaunchKernelGGL(sample_scan_kernel<T>, dim3(a.n_rows * groups), dim3(kScanThreads), 0, s, a, w);
   hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.n_rows), dim3(kPickThreads), 0, s, a, w);
   // rows are left only where something limits them and the list does not hold them whole
-  if ((a.top_k || a.top_p || a.min_p) && a.vocab > kPickList)
+  if ((a.top_k || a.top_p || a.min_p) && a.vocab > kPickList) {
+    if (a.vocab > kSearchVocab) {
+      const dim3 grid(a.n_rows * w.parts);
+      if (a.top_k || a.top_p)
+        hipLaunchKernelGGL(sample_bins_kernel<T>, grid, dim3(kPartThreads), 0, s, a, w);
+      hipLaunchKernelGGL(sample_sums_kernel<T>, grid, dim3(kPartThreads), 0, s, a, w);
+    }
     hipLaunchKernelGGL(sample_search_kernel<T>, dim3(a.n_rows), dim3(kThreads), 0, s, a, w);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t sample_ws_bytes(int n_rows, int vocab) {
-  return stats_bytes(n_rows, vocab) + tops_bytes(n_rows, vocab) + n_rows * sizeof(uint32_t);
-}
+size_t sample_ws_bytes(int n_rows, int vocab) { return Layout(n_rows, vocab).bytes; }
 
 long sample_threads(int n_rows, int vocab) {
-  const long parts = (segments_of(vocab) + kScanWaves - 1) / kScanWaves;
-  return max(parts * kScanThreads, static_cast<long>(kThreads)) * n_rows;
+  const long groups = (segments_of(vocab) + kScanWaves - 1) / kScanWaves;
+  return max(groups * kScanThreads, static_cast<long>(kThreads)) * n_rows;
 }
 
 hipError_t sample(bool bf16, const SampleArgs& a, void* ws, hipStream_t s) {
