@@ -212,21 +212,34 @@ __device__ __forceinline__ Settings settings(const SampleArgs& a, int b) {
   s.top_k = k > 0 && k < a.vocab ? k : 0;
   return s;
 }
+// What the second launch knows of a row that it leaves to the next ones.
+struct RowHeader {
+  double scale;
+  uint64_t whole_sum;
+  float top, low;
+  Settings st;
+  uint32_t pending;  // 0: the row is settled, and the rest is not written
+  uint32_t pad;
+};
+static_assert(sizeof(RowHeader) == 48, "packed");
+
 // What the launches that search a row leave one another; zeroed by the second launch.
 struct SearchState {
   uint32_t count[kBins], mass[kBins];  // ids and weights (of 2^-31 of their sum) per bin
-  uint64_t between;                    // weight between `first` and bin_k
+  uint64_t between;                    // weight between `last` and bin_k
   uint32_t n_list[2];
-  int32_t first, bin_k, bin_m;  // the cut's bin; top-k's and min-p's (kBins: no limit)
-  uint32_t before_k;            // ids in the bins before bin_k
-  uint64_t list[2][kList];      // ids of bin `first`, of bin_k
+  int32_t first, last;              // bins of the cut
+  int32_t bin_k, bin_m;             // top-k's and min-p's (kBins: no limit)
+  uint32_t before_first, before_k;  // ids in the bins before `first` and before bin_k, with a top-k
+  uint64_t pad;
+  uint64_t list[2][kList];          // ids of bins first .. last, of bin_k where that lies behind them
 };
 static_assert(sizeof(SearchState) % 16 == 0, "whole 16-byte words");
 
 struct Workspace {
   SegmentStats* stats;  // [n_rows, segments]
   float* group_top;     // [n_rows, segments, 64]: largest logit of a lane's ids
-  uint32_t* pending;    // [n_rows]: the second launch has left it to the next ones
+  RowHeader* headers;   // [n_rows]
   uint64_t* kept;       // [n_rows, segments]: sums above a cut's bin
   SearchState* states;  // [n_rows]
   int segments;
@@ -249,9 +262,47 @@ __device__ __forceinline__ V uniform(V x) {
   }
 }
 
+// x of another lane by DPP, word by word; `old` where no lane is there or the row is masked out.
+template <int kCtrl, int kRows = 0xf, class V>
+__device__ __forceinline__ V dpp(V old, V x) {
+  constexpr int kWords = sizeof(V) / 4;
+  struct Words {
+    int32_t w[kWords];
+  };
+  const Words o = __builtin_bit_cast(Words, old), a = __builtin_bit_cast(Words, x);
+  Words r;
+#pragma unroll
+  for (int i = 0; i < kWords; ++i)
+    r.w[i] = __builtin_amdgcn_update_dpp(o.w[i], a.w[i], kCtrl, kRows, 0xf, false);
+  return __builtin_bit_cast(V, r);
+}
+
+// x over the wave, on every lane.  Within rows of 16 lanes by DPP (a third of the time that exchanges
+// through LDS take), then by the swaps of rows and halves; both lanes of a pair combine the same two
+// values, so all lanes end with the same bits.
 template <class V, class Op>
 __device__ __forceinline__ V wave_reduce(V x, Op op) {
-  for (int mask = 32; mask >= 1; mask >>= 1) x = op(x, __shfl_xor(x, mask));
+  x = op(x, dpp<0xb1>(x, x));   // lane ^ 1
+  x = op(x, dpp<0x4e>(x, x));   // lane ^ 2
+  x = op(x, dpp<0x141>(x, x));  // lane ^ 7: the other four of eight
+  x = op(x, dpp<0x140>(x, x));  // lane ^ 15: the other eight of a row
+  constexpr int kWords = sizeof(V) / 4;
+  struct Words {
+    uint32_t w[kWords];
+  };
+  auto swapped = [&](auto swap) {
+    const Words a = __builtin_bit_cast(Words, x);
+    Words lo, hi;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const auto r = swap(a.w[i]);
+      lo.w[i] = r[0];
+      hi.w[i] = r[1];
+    }
+    x = op(__builtin_bit_cast(V, lo), __builtin_bit_cast(V, hi));
+  };
+  swapped([](uint32_t v) { return __builtin_amdgcn_permlane16_swap(v, v, false, false); });
+  swapped([](uint32_t v) { return __builtin_amdgcn_permlane32_swap(v, v, false, false); });
   return x;
 }
 struct Add {
@@ -350,14 +401,16 @@ __device__ __forceinline__ V block_reduce(V x, V* slots, Op op) {
   return uniform(y);
 }
 
-// Sum of x over this lane and the lanes before it.
+// Sum of x over this lane and the lanes before it: within rows of 16, then with the last lanes of the
+// rows before.
 template <class V>
 __device__ __forceinline__ V wave_scan(V x) {
-  const int lane = threadIdx.x & 63;
-  for (int n = 1; n < 64; n <<= 1) {
-    const V o = __shfl_up(x, n);
-    if (lane >= n) x += o;
-  }
+  x += dpp<0x111>(V{}, x);       // row_shr:1
+  x += dpp<0x112>(V{}, x);       // row_shr:2
+  x += dpp<0x114>(V{}, x);       // row_shr:4
+  x += dpp<0x118>(V{}, x);       // row_shr:8
+  x += dpp<0x142, 0xa>(V{}, x);  // row_bcast:15 into rows 1 and 3
+  x += dpp<0x143, 0xc>(V{}, x);  // row_bcast:31 into rows 2 and 3
   return x;
 }
 
@@ -412,57 +465,30 @@ struct Row {
   double scale;
   uint64_t whole_sum;  // of all weights, as whole numbers
 
-  // False where the row has a NaN or +inf, or nothing to draw from; its outputs are then written.
-  __device__ __forceinline__ bool open(const SampleArgs& a, const Workspace& ws, int row,
-                                       const double* pow64) {
-    const int lane = threadIdx.x & 63;
+  __device__ __forceinline__ void locate(const SampleArgs& a, const Workspace& ws, int row) {
     r = row;
     logits = static_cast<const T*>(a.logits) + static_cast<size_t>(r) * a.pitch;
     stats = ws.stats + static_cast<size_t>(r) * ws.segments;
     group_top = ws.group_top + static_cast<size_t>(r) * ws.segments * 64;
     vocab = a.vocab;
     segments = ws.segments;
-    float hi = -INFINITY, lo = INFINITY;
-    bool bad = false;
-    for (int g = lane; g < segments; g += 64) {
-      bad |= stats[g].top != stats[g].top;
-      hi = fmaxf(hi, stats[g].top);
-      lo = fminf(lo, stats[g].low);
-    }
-    st = settings(a, find_sequence(a.cu_block, a.batch, r, lane));
-    top = uniform(wave_reduce(hi, Max{}));
-    low = uniform(wave_reduce(lo, Min{}));
-    bad = __any(bad);
+  }
+  // A row that the second launch has left: false where it has not.
+  __device__ __forceinline__ bool reopen(const SampleArgs& a, const Workspace& ws, int row,
+                                         const double* pow64) {
+    const RowHeader& h = ws.headers[row];
+    if (!uniform(h.pending)) return false;
+    locate(a, ws, row);
+    top = uniform(h.top);
+    low = uniform(h.low);
+    st = Settings{uniform(h.st.temperature), uniform(h.st.top_p), uniform(h.st.min_p),
+                  uniform(h.st.top_k)};
+    scale = uniform(h.scale);
+    whole_sum = uniform(h.whole_sum);
     w = Weights{pow64, static_cast<double>(top), weight_rate(st.temperature)};
-    if (!bad && top > -INFINITY) return true;
-    if (threadIdx.x == 0) {
-      a.token[r] = -1;
-      const float none = bad ? NAN : 0.f;
-      if (a.prob) a.prob[r] = none;
-      if (a.conf) a.conf[r] = none;
-      ws.pending[r] = 0;
-    }
-    return false;
-  }
-  // (once the table of powers is there)
-  __device__ __forceinline__ double segment_weight(int g) const {
-    const SegmentStats& x = stats[g];
-    return x.top > -INFINITY ? x.sum * w(x.top) : 0.0;
-  }
-  __device__ __forceinline__ uint64_t segment_whole(int g) const {
-    return g < segments ? whole(segment_weight(g), scale) : 0;
+    return true;
   }
   __device__ __forceinline__ void set_scale(double sum) { scale = ldexp(1.0, 61 - ilogb(sum)); }
-  // scale and whole_sum from the segments' sums
-  __device__ __forceinline__ void sum_segments() {
-    const int lane = threadIdx.x & 63;
-    double x = 0.0;
-    for (int g = lane; g < segments; g += 64) x += segment_weight(g);
-    set_scale(uniform(wave_reduce(x, Add{})));
-    uint64_t n = 0;
-    for (int g = lane; g < segments; g += 64) n += segment_whole(g);
-    whole_sum = uniform(wave_reduce(n, Add{}));
-  }
   // Where the running sum of parts(g) first exceeds x: the segment, with the sum before it.
   template <class F>
   __device__ __forceinline__ int find_segment(uint64_t x, F parts, uint64_t& before) const {
@@ -516,8 +542,8 @@ struct Row {
     last = block_reduce<kN>(last, s.slots32, Max{});
     return last ? static_cast<int>(last) - 1 : g * kSegment;
   }
-  // Row r's outputs, by the calling thread (soft: model_sum(), by its whole wave); sum: of the kept
-  // weights.
+  // Row r's outputs, by the calling thread; soft: sum of the model's weights, for conf; sum: of the
+  // kept weights.
   __device__ __forceinline__ float model_sum(const SampleArgs& a) const {
     float soft = 0.f;
     if (a.conf)
@@ -549,42 +575,77 @@ struct PickShared {
   uint32_t groups[kPickList];
   uint64_t slots64[kPickWaves];
   uint32_t slots32[kPickWaves];
-  uint64_t sum_of_k, sum_of_list;
-  uint32_t n_list, n_groups;
-  uint32_t past_min_p;
+  uint64_t sum_of_k;
+  uint32_t n_list, n_groups, past_min_p;
   int32_t found_id;
+};
+
+// A row's segments, a few of them in this lane's registers (segments lane and lane + 64: rows of up to
+// 2^18 ids), the others in memory.  Every wave goes through all of them by itself, without barriers,
+// and all come to the same bits.
+struct SegmentsOfRow {
+  static constexpr int kHeld = 2;
+  const SegmentStats* stats;
+  int n;
+  SegmentStats held[kHeld];
+  __device__ __forceinline__ SegmentsOfRow(const SegmentStats* stats_, int n_) : stats(stats_), n(n_) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      held[j] = lane + 64 * j < n ? stats[lane + 64 * j]
+                                  : SegmentStats{-INFINITY, INFINITY, 0.f, 0.f, 0.0};
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) f(held[j]);
+    for (int g = (threadIdx.x & 63) + 64 * kHeld; g < n; g += 64) f(stats[g]);
+  }
+  // f(segment g), 0 behind the last one; g - lane is a multiple of 64
+  template <class F>
+  __device__ __forceinline__ uint64_t at(int g, F f) const {
+    if (g < 64) return f(held[0]);
+    if (g < 128) return f(held[1]);
+    return g < n ? f(stats[g]) : 0;
+  }
+};
+
+// Largest logits of groups t, t + kPickThreads, .., the first ones (rows of up to 163840 ids) in
+// registers.
+struct GroupTops {
+  static constexpr int kHeld = 20;
+  const float* tops;
+  int n;
+  float held[kHeld];
+  __device__ __forceinline__ GroupTops(const float* tops_, int n_) : tops(tops_), n(n_) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      const int i = threadIdx.x + j * kPickThreads;
+      held[j] = i < n ? tops[i] : -INFINITY;
+    }
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) f(held[j], static_cast<int>(threadIdx.x) + j * kPickThreads);
+    for (int i = threadIdx.x + kHeld * kPickThreads; i < n; i += kPickThreads) f(tops[i], i);
+  }
 };
 
 // The first ids of the order into s.list: at least `want` of them, by way of the groups whose largest
 // logit lies in the first so many bins of these; all ids above -inf (then `complete`) where there are
 // at most kPickList.  Returns their number, or -1 where they are more than that.
 template <class T>
-__device__ __forceinline__ int gather(const Row<T>& row, PickShared& s, uint32_t want,
-                                      bool& complete) {
-  const int t = threadIdx.x, lane = t & 63, n_groups = row.segments * 64;
-  // largest logits of groups t, t + kPickThreads, ..: kept in registers for up to 163840 ids
-  constexpr int kHeld = 20;
-  float held[kHeld];
-#pragma unroll
-  for (int j = 0; j < kHeld; ++j) {
-    const int i = t + j * kPickThreads;
-    held[j] = i < n_groups ? row.group_top[i] : -INFINITY;
-  }
-  auto each_group = [&](auto f) {
-#pragma unroll
-    for (int j = 0; j < kHeld; ++j) f(held[j], t + j * kPickThreads);
-    for (int i = t + kHeld * kPickThreads; i < n_groups; i += kPickThreads) f(row.group_top[i], i);
-  };
+__device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, PickShared& s,
+                                      uint32_t want, bool& complete) {
+  const int t = threadIdx.x, lane = t & 63;
   // (what weighs less than e^-48 of the largest needs no bin of its own; halves: no overflow)
   const float from = fmaxf(row.low, row.top - 48.f * row.st.temperature);
   const float per = fminf((kPickThreads - 1) / (0.5f * row.top - 0.5f * from), FLT_MAX);
   auto bin = [&](float z) {
     return static_cast<int>(fminf((0.5f * row.top - 0.5f * z) * per, kPickThreads - 1.f));
   };
-  s.bins[t] = 0;
-  if (t == 0) s.n_list = s.n_groups = 0;
-  __syncthreads();
-  each_group([&](float z, int) {
+  tops.each([&](float z, int) {
     if (z > -INFINITY) atomicAdd(&s.bins[bin(z)], 1u);
   });
   __syncthreads();
@@ -593,12 +654,12 @@ __device__ __forceinline__ int gather(const Row<T>& row, PickShared& s, uint32_t
   uint32_t finite;
   {
     const u32x4 c = *reinterpret_cast<const u32x4*>(&s.bins[4 * lane]);
-    const uint32_t mine = c[0] + c[1] + c[2] + c[3], upto = wave_scan(mine);
+    const uint32_t sum = c[0] + c[1] + c[2] + c[3], upto = wave_scan(sum);
     finite = uniform(__shfl(upto, 63));
     const uint64_t hit = __ballot(upto >= want);
     if (hit) {
       const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
-      uint32_t n = upto - mine;
+      uint32_t n = upto - sum;
       int b = 4 * lane;
 #pragma unroll
       for (int e = 0; e < 3; ++e) {
@@ -611,26 +672,48 @@ __device__ __forceinline__ int gather(const Row<T>& row, PickShared& s, uint32_t
   complete = row.vocab <= kPickList || finite * kGroup <= kPickList;
   if (complete) last = kPickThreads - 1;
   auto taken = [&](float z) { return z > -INFINITY && bin(z) <= last; };
-  each_group([&](float z, int i) {
-    if (!taken(z)) return;
-    const uint32_t at = atomicAdd(&s.n_groups, 1u);
-    if (at < kPickList) s.groups[at] = static_cast<uint32_t>(i);
-  });
+  // (places are reserved once a thread: an atomic's answer takes as long as the rest)
+  uint32_t mine = 0;
+  tops.each([&](float z, int) { mine += taken(z); });
+  uint32_t place = mine ? atomicAdd(&s.n_groups, mine) : 0;
+  if (mine)
+    tops.each([&](float z, int i) {
+      if (!taken(z)) return;
+      if (place < kPickList) s.groups[place] = static_cast<uint32_t>(i);
+      ++place;
+    });
   __syncthreads();
   const int found = static_cast<int>(uniform(s.n_groups));
   if (found > kPickList) return -1;  // (each holds one such id at least)
-  for (int i = t; i < found * kLoads<T>; i += kPickThreads) {
-    const int group = static_cast<int>(s.groups[i / kLoads<T>]);
-    const int at = (group >> 6) * kSegment + id_in_segment<T>(i % kLoads<T>, group & 63);
-    Chunk<T> z;
-    z.load(row.logits, at, row.vocab);
+  // the groups' ids, all loads of a thread under way at once
+  Chunk<T> z[kLoads<T>];
+  auto id_of = [&](int i) {
+    const int item = t + i * kPickThreads, group = static_cast<int>(s.groups[item / kLoads<T>]);
+    return (group >> 6) * kSegment + id_in_segment<T>(item % kLoads<T>, group & 63);
+  };
+  auto has = [&](int i) { return t + i * kPickThreads < found * kLoads<T>; };
+  mine = 0;
 #pragma unroll
-    for (int e = 0; e < kVec<T>; ++e)
-      if (taken(z[e])) {
-        const uint32_t j = atomicAdd(&s.n_list, 1u);
-        if (j < kPickList) s.list[j][0] = entry_of(z[e], at + e);
+  for (int i = 0; i < kLoads<T>; ++i)
+    if (has(i)) z[i].load(row.logits, id_of(i), row.vocab);
+#pragma unroll
+  for (int i = 0; i < kLoads<T>; ++i)
+    if (has(i))
+#pragma unroll
+      for (int e = 0; e < kVec<T>; ++e) mine += taken(z[i][e]);
+  place = mine ? atomicAdd(&s.n_list, mine) : 0;
+  if (mine)
+#pragma unroll
+    for (int i = 0; i < kLoads<T>; ++i)
+      if (has(i)) {
+        const int id = id_of(i);
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e)
+          if (taken(z[i][e])) {
+            if (place < kPickList) s.list[place][0] = entry_of(z[i][e], id + e);
+            ++place;
+          }
       }
-  }
   __syncthreads();
   const uint32_t n = uniform(s.n_list);
   return n <= kPickList ? static_cast<int>(n) : -1;
@@ -642,116 +725,184 @@ __device__ __forceinline__ int gather(const Row<T>& row, PickShared& s, uint32_t
 // no sorting, and no sums across waves.
 template <class T>
 __device__ __forceinline__ bool pick_from_list(const SampleArgs& a, const Row<T>& row,
-                                               PickShared& s, int n, bool complete) {
+                                               PickShared& s, int n, bool complete, float soft) {
   const int t = threadIdx.x;
   const Settings& st = row.st;
+  if (st.top_k > n && !complete) return false;
   const bool active = t < n;
   const uint64_t entry = active ? s.list[t][0] : 0;
   const double x = active ? row.w(key_logit(entry_key(entry))) : 0.0;
   const uint64_t mass = whole(x, row.scale);
-  if (active) s.list[t][1] = mass;
-  __syncthreads();
+  if (active)
+    s.list[t][1] = mass;
+  else
+    s.list[t][0] = s.list[t][1] = 0;
+  if (active && x < st.min_p) s.past_min_p = 1;
+  const uint64_t of_list = block_reduce<kPickWaves>(mass, s.slots64, Add{});
+  uint64_t all = complete ? of_list : row.whole_sum;
+  // where nothing behind the list can be kept
+  if (!complete && st.top_k == 0 && !(st.top_p < 1.f && of_list >= share_of(all, st.top_p)) &&
+      !uniform(s.past_min_p))
+    return false;
   uint64_t before = 0;
   int place = 0;
-  if (wave_index() * 64 < n)
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) {
-      const bool ahead = s.list[j][0] > entry;
-      place += ahead;
-      before += ahead ? s.list[j][1] : 0;
+  // f(entry, weight) of the list's ids, eight at a time; behind its end 0, 0
+  auto walk = [&](auto f) {
+    if (wave_index() * 64 >= n) return;
+    for (int j = 0; j < n; j += 8) {
+      uint64_t e[8], m[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        e[i] = s.list[j + i][0];
+        m[i] = s.list[j + i][1];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f(e[i], m[i]);
     }
-  if (st.top_k > n && !complete) return false;
+  };
+  walk([&](uint64_t e, uint64_t m) {
+    const bool ahead = e > entry;
+    place += ahead;
+    before += ahead ? m : 0;
+  });
   const int keep = st.top_k > 0 ? min(st.top_k, n) : n;
-  if (active && place == keep - 1) s.sum_of_k = before + mass;
-  if (active && place == n - 1) {
-    s.sum_of_list = before + mass;
-    s.past_min_p = !(x >= st.min_p);
-  }
-  __syncthreads();
-  const uint64_t of_list = uniform(s.sum_of_list);
-  bool closed = complete || st.top_k > 0;  // nothing behind the list can be kept
-  bool kept = active && place < keep;
+  bool kept = active && place < keep && x >= st.min_p;
   if (st.top_p < 1.f) {
-    const uint64_t all = st.top_k > 0 ? uniform(s.sum_of_k) : complete ? of_list : row.whole_sum;
-    const uint64_t target = share_of(all, st.top_p);
-    closed |= of_list >= target;
-    kept &= before < target;
+    if (st.top_k > 0) {
+      if (active && place == keep - 1) s.sum_of_k = before + mass;
+      __syncthreads();
+      all = uniform(s.sum_of_k);
+    }
+    kept &= before < share_of(all, st.top_p);
   }
-  if (st.min_p > 0.f) {
-    closed |= uniform(s.past_min_p) != 0;
-    kept &= x >= st.min_p;
-  }
-  if (!closed) return false;
+  __syncthreads();  // the walks are over
   if (active && !kept) s.list[t][1] = 0;
   __syncthreads();
   if (wave_index() * 64 >= n) return true;
   uint64_t upto = 0, total = 0;
-#pragma unroll 4
-  for (int j = 0; j < n; ++j) {
-    const uint64_t m = s.list[j][1];
+  walk([&](uint64_t e, uint64_t m) {
     total += m;
     // (~id falls as the id rises)
-    upto += static_cast<uint32_t>(s.list[j][0]) >= static_cast<uint32_t>(entry) ? m : 0;
-  }
+    upto += static_cast<uint32_t>(e) >= static_cast<uint32_t>(entry) ? m : 0;
+  });
   const uint64_t at = part_of(total, random_number(a, row.r));
-  const float soft = row.model_sum(a);
   if (kept && upto > at && upto - mass <= at)
     row.write(a, entry_id(entry), static_cast<double>(total) / row.scale, soft);
   return true;
 }
 
-template <class T>
+// kLimits: the call has a top-k, top-p or min-p (of which a row may still have none).
+template <class T, bool kLimits>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a, Workspace ws) {
   __shared__ PickShared s;
-  const int t = threadIdx.x;
-  if (t < 64) s.pow64[t] = kPow64[t];
+  const int t = threadIdx.x, lane = t & 63;
   Row<T> row;
-  if (!row.open(a, ws, blockIdx.x, s.pow64)) return;
+  row.locate(a, ws, blockIdx.x);
+  const SegmentsOfRow segments(row.stats, row.segments);
+  const GroupTops tops(row.group_top, kLimits ? row.segments * 64 : 0);
+  row.st = settings(a, find_sequence(a.cu_block, a.batch, row.r, lane));
+  if (t < 64) s.pow64[t] = kPow64[t];
+  s.bins[t] = 0;
+  if (t == 0) s.n_list = s.n_groups = s.past_min_p = 0;
+  float hi = -INFINITY, lo = INFINITY;
+  bool bad = false;
+  segments.each([&](const SegmentStats& x) {
+    bad |= x.top != x.top;
+    hi = fmaxf(hi, x.top);
+    lo = fminf(lo, x.low);
+  });
+  row.top = uniform(wave_reduce(hi, Max{}));
+  row.low = uniform(wave_reduce(lo, Min{}));
+  bad = __any(bad);
+  RowHeader& header = ws.headers[row.r];
+  if (bad || row.top == -INFINITY) {  // a NaN or +inf; or nothing to draw from
+    if (t == 0) {
+      a.token[row.r] = -1;
+      const float none = bad ? NAN : 0.f;
+      if (a.prob) a.prob[row.r] = none;
+      if (a.conf) a.conf[row.r] = none;
+      header.pending = 0;
+    }
+    return;
+  }
+  row.w = Weights{s.pow64, static_cast<double>(row.top), weight_rate(row.st.temperature)};
   __syncthreads();
+
+  float soft = 0.f;  // sum of the model's weights, for conf
+  if (a.conf) {
+    segments.each([&](const SegmentStats& x) {
+      soft += x.soft * fast_exp2((x.top - row.top) * kLog2e);
+    });
+    soft = wave_reduce(soft, Add{});
+  }
+  auto weight = [&](const SegmentStats& x) { return x.top > -INFINITY ? x.sum * row.w(x.top) : 0.0; };
+  auto whole_part = [&](const SegmentStats& x) { return whole(weight(x), row.scale); };
+  auto sum_segments = [&]() {  // sets scale and whole_sum
+    double x = 0.0;
+    segments.each([&](const SegmentStats& g) { x += weight(g); });
+    x = uniform(wave_reduce(x, Add{}));
+    row.set_scale(x);
+    row.whole_sum = whole(x, row.scale);
+  };
   if (row.st.greedy() || !row.st.limited()) {
     int token;
     double sum = 1.0;
+    uint64_t before;
     if (row.st.greedy()) {
       const float top = row.top;
-      uint64_t before;
-      const int g = row.find_segment(
-          0, [&](int i) -> uint64_t { return i < row.segments && row.stats[i].top == top; }, before);
       const uint32_t key = order_key(top);
+      const int g = row.find_segment(
+          0, [&](int i) {
+            return segments.at(i, [&](const SegmentStats& x) -> uint64_t { return x.top == top; });
+          }, before);
       token = row.template find_id<kPickWaves>(
           s, g, 0, 0, [&](float z, int) -> uint64_t { return order_key(z) == key; });
     } else {
-      row.sum_segments();
-      uint64_t before;
+      sum_segments();
+      uint64_t n = 0;  // as the segments' parts add up
+      segments.each([&](const SegmentStats& g) { n += whole_part(g); });
+      row.whole_sum = uniform(wave_reduce(n, Add{}));
       const uint64_t at = part_of(row.whole_sum, random_number(a, row.r));
-      const int g = row.find_segment(at, [&](int i) { return row.segment_whole(i); }, before);
+      const int g =
+          row.find_segment(at, [&](int i) { return segments.at(i, whole_part); }, before);
       token = row.template find_id<kPickWaves>(
           s, g, before, at, [&](float z, int) { return whole(row.w(z), row.scale); });
       sum = static_cast<double>(row.whole_sum) / row.scale;
     }
-    const float soft = row.model_sum(a);
     if (t == 0) {
       row.write(a, token, sum, soft);
-      ws.pending[row.r] = 0;
+      header.pending = 0;
     }
     return;
   }
-  if (row.st.few()) {
-    row.scale = 0x1p52;  // (at most kPickList weights of at most 1 are summed)
-    row.whole_sum = 0;
-  } else {
-    row.sum_segments();
-  }
-  bool done = false;
-  if (row.st.few() || row.st.top_k == 0) {
-    bool complete;
-    const int n = gather(row, s, row.st.few() ? row.st.top_k : kFewIds, complete);
-    done = n > 0 && pick_from_list(a, row, s, n, complete);
-  }
-  if (t == 0) ws.pending[row.r] = !done;
-  if (!done && row.vocab > kSearchVocab) {  // (all but the lists)
-    u32x4* const state = reinterpret_cast<u32x4*>(&ws.states[row.r]);
-    for (int i = t; i < static_cast<int>(offsetof(SearchState, list) / 16); i += kPickThreads)
-      state[i] = u32x4{};
+  if constexpr (kLimits) {
+    if (row.st.few()) {
+      row.scale = 0x1p52;  // (at most kPickList weights of at most 1 are summed)
+      row.whole_sum = 0;
+    } else {
+      sum_segments();
+    }
+    bool done = false;
+    // (a list of weights of at most 1 does not come to top_p of more than its length)
+    const bool hopeless = row.st.min_p <= 0.f && row.vocab > kPickList &&
+                          static_cast<double>(share_of(row.whole_sum, fminf(row.st.top_p, 0x1.fffffep-1f))) >
+                              kPickList * row.scale;
+    if (row.st.few() || (row.st.top_k == 0 && !hopeless)) {
+      bool complete;
+      const int n = gather(row, tops, s, row.st.few() ? row.st.top_k : kFewIds, complete);
+      done = n > 0 && pick_from_list(a, row, s, n, complete, soft);
+    }
+    if (t == 0) {
+      if (done)
+        header.pending = 0;
+      else
+        header = RowHeader{row.scale, row.whole_sum, row.top, row.low, row.st, 1, 0};
+    }
+    if (!done && row.vocab > kSearchVocab) {  // (all but the lists)
+      u32x4* const state = reinterpret_cast<u32x4*>(&ws.states[row.r]);
+      for (int i = t; i < static_cast<int>(offsetof(SearchState, list) / 16); i += kPickThreads)
+        state[i] = u32x4{};
+    }
   }
 }
 
@@ -844,17 +995,13 @@ __device__ __forceinline__ int part_begin(int part, int parts, int segments) {
 template <class T>
 __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a, Workspace ws) {
   __shared__ uint32_t count[kBins], mass[kBins];
-  __shared__ double pow64[64];
   const int t = threadIdx.x, r = blockIdx.x / ws.parts, part = blockIdx.x - r * ws.parts;
-  if (!uniform(ws.pending[r])) return;
-  if (t < 64) pow64[t] = kPow64[t];
-  for (int i = t; i < kBins; i += kPartThreads) count[i] = mass[i] = 0;
   Row<T> row;
-  if (!row.open(a, ws, r, pow64) || !in_parts(row)) return;
+  if (!row.reopen(a, ws, r, nullptr) || !in_parts(row)) return;
+  for (int i = t; i < kBins; i += kPartThreads) count[i] = mass[i] = 0;
   const bool by_count = row.st.top_k > 0, by_mass = row.st.top_p < 1.f;
   if (!by_count && !by_mass) return;
   __syncthreads();
-  row.sum_segments();
   // weights as whole numbers of 2^-31 of (at most) their sum (a float's atomic sum takes 8 times as
   // long in LDS)
   const float rate = static_cast<float>(row.w.rate / 64.0);
@@ -869,7 +1016,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
         const int b = bin(z);
         if (by_count) atomicAdd(&count[b], 1u);
         if (by_mass)
-          atomicAdd(&mass[b], static_cast<uint32_t>(fast_exp2((z - top) * rate + unit)));
+          atomicAdd(&mass[b], static_cast<uint32_t>(fast_exp2((z - top) * rate + unit) + 0.5f));
       },
       [](int) {});
   __syncthreads();
@@ -917,17 +1064,17 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
   __shared__ uint64_t slots64[kPartWaves];
   __shared__ FoundBin found;
   const int t = threadIdx.x, r = blockIdx.x / ws.parts, part = blockIdx.x - r * ws.parts;
-  if (!uniform(ws.pending[r])) return;
-  if (t < 64) pow64[t] = kPow64[t];
   Row<T> row;
-  if (!row.open(a, ws, r, pow64) || !in_parts(row)) return;
+  if (!row.reopen(a, ws, r, pow64) || !in_parts(row)) return;
+  if (t < 64) pow64[t] = kPow64[t];
   __syncthreads();
-  row.sum_segments();
   const Settings& st = row.st;
   const Bins bin(row);
   SearchState& state = ws.states[r];
-  // the bin of each limit, kBins where it limits nothing; the first of them holds the cut
-  int bin_k = kBins, bin_p = kBins, bin_m = kBins;
+  // The bins of each limit, kBins where it limits nothing; the cut lies in the first of them.  top-p's are
+  // those that its sum reaches within 2^-18 of the whole, which the histogram's roundings stay below
+  // (hardly ever two), and, where it is a part of the first top_k ids' weight, for all that this may be.
+  int bin_k = kBins, bin_m = kBins, p_first = kBins, p_last = kBins;
   uint64_t before_k = 0;
   if (st.top_k > 0) {
     const FoundBin f = find_bin(state.count, static_cast<uint64_t>(st.top_k), slots64, &found);
@@ -935,44 +1082,53 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
     before_k = f.before;
   }
   if (st.top_p < 1.f) {
-    uint64_t all = row.whole_sum >> 31;
-    if (bin_k < kBins) {  // the weight of the bins up to bin_k, about that of the first top_k ids
+    uint64_t least = row.whole_sum >> 31, most = least;  // weight that top_p takes its part of
+    if (bin_k < kBins) {  // the bins up to bin_k, without it and with it
       uint64_t x = 0;
-      for (int i = t; i <= bin_k; i += kPartThreads) x += state.mass[i];
-      all = block_reduce<kPartWaves>(x, slots64, Add{});
+      for (int i = t; i < bin_k; i += kPartThreads) x += state.mass[i];
+      least = block_reduce<kPartWaves>(x, slots64, Add{});
+      most = least + state.mass[bin_k];
     }
-    const uint64_t target = max(share_of(all, st.top_p), uint64_t{1});
-    bin_p = find_bin(state.mass, target, slots64, &found).bin;
+    const uint64_t slack = (most >> 18) + 1, low = share_of(least, st.top_p);
+    p_first = find_bin(state.mass, low > slack ? low - slack : 1, slots64, &found).bin;
+    p_last = find_bin(state.mass, share_of(most, st.top_p) + slack, slots64, &found).bin;
   }
   if (st.min_p > 0.f) bin_m = bin(min_p_logit(row));
-  const int first = min(min(bin_k, bin_p), bin_m);
-  const bool between = st.top_p < 1.f && bin_k < kBins && bin_k > first;
-  const int last = between ? bin_k : first;
-  if (part == 0 && t == 0) {
-    state.first = first;
-    state.bin_k = bin_k;
-    state.bin_m = bin_m;
-    state.before_k = static_cast<uint32_t>(before_k);
+  const int first = min(min(bin_k, p_first), bin_m), last = min(min(bin_k, p_last), bin_m);
+  const bool between = st.top_p < 1.f && bin_k < kBins && bin_k > last;
+  const int end = between ? bin_k : last;
+  if (part == 0) {
+    uint64_t x = 0;
+    if (st.top_k > 0)
+      for (int i = t; i < min(first, kBins); i += kPartThreads) x += state.count[i];
+    x = block_reduce<kPartWaves>(x, slots64, Add{});
+    if (t == 0) {
+      state.first = first;
+      state.last = last;
+      state.bin_k = bin_k;
+      state.bin_m = bin_m;
+      state.before_first = static_cast<uint32_t>(x);
+      state.before_k = static_cast<uint32_t>(before_k);
+    }
   }
   auto append = [&](int which, float z, int id) {
     const uint32_t j = atomicAdd(&state.n_list[which], 1u);
     if (j < kList) state.list[which][j] = entry_of(z, id);
   };
   double sum = 0.0, sum_between = 0.0;
-  const int last_of_row = last;
   visit<kPartWaves, 4>(
       row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
       [&](int g) {
         const float top = uniform(row.stats[g].top);
-        return top > -INFINITY && uniform(bin(top)) <= last_of_row;
+        return top > -INFINITY && uniform(bin(top)) <= end;
       },
       [&](float z, int id) {
         const int b = bin(z);
-        if (b > last || !(z > -INFINITY)) return;
-        if (b == first) {
-          append(0, z, id);
-        } else if (b < first) {
+        if (b > end || !(z > -INFINITY)) return;
+        if (b < first) {
           sum += row.w.normal(z);
+        } else if (b <= last) {
+          append(0, z, id);
         } else if (b < bin_k) {
           sum_between += row.w.normal(z);
         } else {
@@ -1115,36 +1271,38 @@ struct Searcher {
                                                  Cut& cut) const {
     const int t = threadIdx.x;
     const Settings& st = row.st;
-    const int first = uniform(state.first), bin_k = uniform(state.bin_k);
-    if (first >= kBins || uniform(state.n_list[0]) > kList || uniform(state.n_list[1]) > kList)
+    const int last = uniform(state.last), bin_k = uniform(state.bin_k);
+    if (last >= kBins || uniform(state.n_list[0]) > kList || uniform(state.n_list[1]) > kList)
       return false;
     for (int g = t; g < row.segments; g += kThreads) s.segment[g] = kept_sums[g];
-    const int n_k = st.top_k - static_cast<int>(uniform(state.before_k));  // of bin_k's ids
+    const bool by_min_p = uniform(state.bin_m) == last;
     uint64_t entry, mass, before, in_list, of_k = 0;
     double x;
-    if (st.top_p < 1.f && bin_k < kBins && bin_k > first) {
-      sorted_list(state, 1, entry, x, mass, before, in_list);
-      if (t == n_k - 1) s.found_mass = before + mass;
+    // top_k's place in a list, with the weights up to it
+    auto up_to = [&](uint32_t ids_before) {
+      const int n = st.top_k - static_cast<int>(uniform(ids_before));
+      if (t == n - 1) s.found_mass = before + mass;
       __syncthreads();
-      of_k = uniform(s.found_mass) + uniform(state.between);
+      const uint64_t m = uniform(s.found_mass);
+      return m;
+    };
+    if (st.top_p < 1.f && bin_k < kBins && bin_k > last) {
+      sorted_list(state, 1, entry, x, mass, before, in_list);
+      of_k = up_to(state.before_k) + uniform(state.between);
     }
     const int n = sorted_list(state, 0, entry, x, mass, before, in_list);
     const uint64_t above = sum_of_segments();
     bool kept = t < n, closed = false;
-    const bool by_min_p = uniform(state.bin_m) == first;
-    if (bin_k == first) {
-      kept &= t < n_k;
+    if (bin_k == last) {
+      kept &= t < st.top_k - static_cast<int>(uniform(state.before_first));
       closed = true;
     }
     if (st.top_p < 1.f) {
       uint64_t all = row.whole_sum;
-      if (bin_k == first) {
-        if (t == n_k - 1) s.found_mass = before + mass;
-        __syncthreads();
-        all = above + uniform(s.found_mass);
-      } else if (bin_k < kBins) {
+      if (bin_k == last)
+        all = above + up_to(state.before_first);
+      else if (bin_k < kBins)
         all = above + in_list + of_k;
-      }
       const uint64_t target = share_of(all, st.top_p);
       if (above >= target) return false;
       kept &= above + before < target;
@@ -1159,13 +1317,14 @@ struct Searcher {
       cut = kKeepAll;
       return by_min_p;
     }
+    __syncthreads();  // every wave has summed up the segments
     if (kept)
       atomicAdd(reinterpret_cast<unsigned long long*>(&s.segment[entry_id(entry) / kSegment]),
                 static_cast<unsigned long long>(mass));
     // (the kept ones of the list are its first)
     const uint32_t n_kept = block_reduce<kWaves>(static_cast<uint32_t>(kept), s.slots32, Add{});
-    const uint64_t last = uniform(s.list[n_kept ? n_kept - 1 : 0]);
-    cut = Cut{entry_key(last), entry_id(last) - (n_kept ? 0 : 1)};
+    const uint64_t end = uniform(s.list[n_kept ? n_kept - 1 : 0]);
+    cut = Cut{entry_key(end), entry_id(end) - (n_kept ? 0 : 1)};
     return true;
   }
 
@@ -1244,14 +1403,12 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, Workspace ws) {
   __shared__ Shared s;
   const int t = threadIdx.x, r = blockIdx.x;
-  if (!uniform(ws.pending[r])) return;
-  if (t < 64) s.pow64[t] = kPow64[t];
   Row<T> row;
-  if (!row.open(a, ws, r, s.pow64)) return;
+  if (!row.reopen(a, ws, r, s.pow64)) return;
+  if (t < 64) s.pow64[t] = kPow64[t];
   __syncthreads();
   const Settings& st = row.st;
   const Searcher<T> p{row, s};
-  if (!st.few()) row.sum_segments();
   Cut cut = kKeepAll;
   if (!in_parts(row) ||
       !p.cut_from_lists(ws.states[r], ws.kept + static_cast<size_t>(r) * ws.segments, cut)) {
@@ -1290,13 +1447,13 @@ int segments_of(int vocab) { return (vocab + kSegment - 1) / kSegment; }
 
 // Where a call's intermediate results lie in its workspace.
 struct Layout {
-  size_t tops, pending, kept, states, bytes;
+  size_t tops, headers, kept, states, bytes;
   Layout(int n_rows, int vocab) {
     const size_t n = n_rows, segments = segments_of(vocab);
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
     tops = up(n * segments * sizeof(SegmentStats));
-    pending = tops + up(n * segments * 64 * sizeof(float));
-    kept = pending + up(n * sizeof(uint32_t));
+    headers = tops + up(n * segments * 64 * sizeof(float));
+    kept = headers + up(n * sizeof(RowHeader));
     states = bytes = kept;
     if (vocab > kSearchVocab) {
       states = kept + up(n * segments * sizeof(uint64_t));
@@ -1318,16 +1475,18 @@ hipError_t launch(const SampleArgs& a, void* ws, hipStream_t s) {
   char* const base = static_cast<char*>(ws);
   const Workspace w{reinterpret_cast<SegmentStats*>(base),
                     reinterpret_cast<float*>(base + at.tops),
-                    reinterpret_cast<uint32_t*>(base + at.pending),
+                    reinterpret_cast<RowHeader*>(base + at.headers),
                     reinterpret_cast<uint64_t*>(base + at.kept),
                     reinterpret_cast<SearchState*>(base + at.states),
                     segments,
                     parts_of(a.n_rows, a.vocab)};
   const int groups = (segments + kScanWaves - 1) / kScanWaves;
   hipLaunchKernelGGL(sample_scan_kernel<T>, dim3(a.n_rows * groups), dim3(kScanThreads), 0, s, a, w);
-  hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.n_rows), dim3(kPickThreads), 0, s, a, w);
+  const bool limits = a.top_k || a.top_p || a.min_p;
+  const auto pick = limits ? sample_pick_kernel<T, true> : sample_pick_kernel<T, false>;
+  hipLaunchKernelGGL(pick, dim3(a.n_rows), dim3(kPickThreads), 0, s, a, w);
   // rows are left only where something limits them and the list does not hold them whole
-  if ((a.top_k || a.top_p || a.min_p) && a.vocab > kPickList) {
+  if (limits && a.vocab > kPickList) {
     if (a.vocab > kSearchVocab) {
       const dim3 grid(a.n_rows * w.parts);
       if (a.top_k || a.top_p)
