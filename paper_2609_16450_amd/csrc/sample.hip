@@ -60,7 +60,8 @@ __device__ __forceinline__ int id_in_segment(int i, int lane) {
   return (i * 64 + lane) * kVec<T>;
 }
 
-// Logits at .. at + kVec - 1 of a row, as they came; -inf behind its end.
+// Logits at .. at + kVec - 1 of a row, as they came; -inf behind its end.  (Loads without the test for
+// segments that lie before the row's end: 300 -> 318 us for 944 rows of 126464.)
 template <class T>
 struct Chunk;
 template <>
@@ -192,6 +193,8 @@ static_assert(sizeof(SegmentStats) == 24, "packed");
 // Top-k small enough to be settled by the second launch: half the list, so that the ids which the
 // groups' largest logits let through besides fit as well.
 constexpr int kFewIds = kPickList / 2;
+// Ids among which a top-p or min-p alone is tried: a sure model's nucleus.
+constexpr int kNucleus = 64;
 
 // A row's settings.
 struct Settings {
@@ -316,6 +319,7 @@ struct Max {
   __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); }
 };
 struct Min {
+  __device__ __forceinline__ uint64_t operator()(uint64_t a, uint64_t b) const { return min(a, b); }
   __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); }
   __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return min(a, b); }
 };
@@ -632,6 +636,31 @@ struct GroupTops {
   }
 };
 
+// put(place, j) for the items j < kN of each lane for which has(j): places of one list, reserved once a
+// wave (with a branch and an atomic to each item, most of the kernel's time went here).
+template <int kN, class Has, class Put>
+__device__ __forceinline__ void append(uint32_t& length, Has has, Put put) {
+  uint64_t lanes[kN];
+  uint32_t total = 0;
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    lanes[j] = __ballot(has(j));
+    total += __popcll(lanes[j]);
+  }
+  if (total == 0) return;
+  uint32_t at = 0;
+  if ((threadIdx.x & 63) == 0) at = atomicAdd(&length, total);
+  at = uniform(at);
+#pragma unroll
+  for (int j = 0; j < kN; ++j)
+    if (lanes[j]) {
+      const uint32_t low = static_cast<uint32_t>(lanes[j]), high = static_cast<uint32_t>(lanes[j] >> 32);
+      const uint32_t place = at + __builtin_amdgcn_mbcnt_hi(high, __builtin_amdgcn_mbcnt_lo(low, 0));
+      if (has(j)) put(place, j);
+      at += __popcll(lanes[j]);
+    }
+}
+
 // The first ids of the order into s.list: at least `want` of them, by way of the groups whose largest
 // logit lies in the first so many bins of these; all ids above -inf (then `complete`) where there are
 // at most kPickList.  Returns their number, or -1 where they are more than that.
@@ -672,48 +701,41 @@ __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, 
   complete = row.vocab <= kPickList || finite * kGroup <= kPickList;
   if (complete) last = kPickThreads - 1;
   auto taken = [&](float z) { return z > -INFINITY && bin(z) <= last; };
-  // (places are reserved once a thread: an atomic's answer takes as long as the rest)
-  uint32_t mine = 0;
-  tops.each([&](float z, int) { mine += taken(z); });
-  uint32_t place = mine ? atomicAdd(&s.n_groups, mine) : 0;
-  if (mine)
-    tops.each([&](float z, int i) {
-      if (!taken(z)) return;
-      if (place < kPickList) s.groups[place] = static_cast<uint32_t>(i);
-      ++place;
-    });
+  append<GroupTops::kHeld>(
+      s.n_groups, [&](int j) { return taken(tops.held[j]); },
+      [&](uint32_t place, int j) {
+        if (place < kPickList) s.groups[place] = static_cast<uint32_t>(t + j * kPickThreads);
+      });
+  for (int i0 = GroupTops::kHeld * kPickThreads; i0 < tops.n; i0 += kPickThreads) {
+    const float z = i0 + t < tops.n ? tops.tops[i0 + t] : -INFINITY;
+    append<1>(
+        s.n_groups, [&](int) { return taken(z); },
+        [&](uint32_t place, int) {
+          if (place < kPickList) s.groups[place] = static_cast<uint32_t>(i0 + t);
+        });
+  }
   __syncthreads();
   const int found = static_cast<int>(uniform(s.n_groups));
   if (found > kPickList) return -1;  // (each holds one such id at least)
-  // the groups' ids, all loads of a thread under way at once
-  Chunk<T> z[kLoads<T>];
-  auto id_of = [&](int i) {
-    const int item = t + i * kPickThreads, group = static_cast<int>(s.groups[item / kLoads<T>]);
-    return (group >> 6) * kSegment + id_in_segment<T>(item % kLoads<T>, group & 63);
-  };
-  auto has = [&](int i) { return t + i * kPickThreads < found * kLoads<T>; };
-  mine = 0;
+  // the groups' ids, one a lane, 16 loads of a thread under way at once
+  constexpr int kAtOnce = 16;
+  for (int i0 = 0; i0 < found * kGroup; i0 += kAtOnce * kPickThreads) {
+    float z[kAtOnce];
+    int ids[kAtOnce];
 #pragma unroll
-  for (int i = 0; i < kLoads<T>; ++i)
-    if (has(i)) z[i].load(row.logits, id_of(i), row.vocab);
-#pragma unroll
-  for (int i = 0; i < kLoads<T>; ++i)
-    if (has(i))
-#pragma unroll
-      for (int e = 0; e < kVec<T>; ++e) mine += taken(z[i][e]);
-  place = mine ? atomicAdd(&s.n_list, mine) : 0;
-  if (mine)
-#pragma unroll
-    for (int i = 0; i < kLoads<T>; ++i)
-      if (has(i)) {
-        const int id = id_of(i);
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e)
-          if (taken(z[i][e])) {
-            if (place < kPickList) s.list[place][0] = entry_of(z[i][e], id + e);
-            ++place;
-          }
-      }
+    for (int j = 0; j < kAtOnce; ++j) {
+      const int item = i0 + j * kPickThreads + t, k = item % kGroup;
+      const int group = static_cast<int>(s.groups[min(item / kGroup, found - 1)]);
+      ids[j] = (group >> 6) * kSegment + id_in_segment<T>(k / kVec<T>, group & 63) + k % kVec<T>;
+      z[j] = load_logit(row.logits, min(ids[j], row.vocab - 1));
+      if (item >= found * kGroup || ids[j] >= row.vocab) z[j] = -INFINITY;
+    }
+    append<kAtOnce>(
+        s.n_list, [&](int j) { return taken(z[j]); },
+        [&](uint32_t place, int j) {
+          if (place < kPickList) s.list[place][0] = entry_of(z[j], ids[j]);
+        });
+  }
   __syncthreads();
   const uint32_t n = uniform(s.n_list);
   return n <= kPickList ? static_cast<int>(n) : -1;
@@ -889,7 +911,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
                               kPickList * row.scale;
     if (row.st.few() || (row.st.top_k == 0 && !hopeless)) {
       bool complete;
-      const int n = gather(row, tops, s, row.st.few() ? row.st.top_k : kFewIds, complete);
+      const int n = gather(row, tops, s, row.st.few() ? row.st.top_k : kNucleus, complete);
       done = n > 0 && pick_from_list(a, row, s, n, complete, soft);
     }
     if (t == 0) {
@@ -918,9 +940,10 @@ constexpr int kPartWaves = kPartThreads / 64;
 
 // f(z, id) for every id that this lane holds of segments first + wave, first + wave + kN, .. below
 // `end` for which wanted(g); then each_segment(g) (by the whole wave) for these and the others.
-// kAtOnce loads at a time, the next ones under way meanwhile, worked on by two ids: with more of them
-// under way the kernels of 16 waves spill.
-template <int kN, int kAtOnce, class T, class Wanted, class F, class End>
+// kAtOnce loads at a time, the next ones under way meanwhile, worked on by kIds ids: a weight is a chain
+// of a dozen operations, of which a wave alone on its SIMD needs several at once (8: 14 -> 10 us for 32
+// rows, a segment to a wave); with more than two the kernels of 16 waves spill.
+template <int kN, int kAtOnce, int kIds, class T, class Wanted, class F, class End>
 __device__ __forceinline__ void visit(const Row<T>& row, int first, int end, Wanted wanted, F f,
                                       End each_segment) {
   const int lane = threadIdx.x & 63;
@@ -940,7 +963,7 @@ __device__ __forceinline__ void visit(const Row<T>& row, int first, int end, Wan
         for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
           for (int e = 0; e < kVec<T>; ++e) {
-            if (e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            if ((i * kVec<T> + e) % kIds == 0) __builtin_amdgcn_sched_barrier(0);
             f(x[i][e], g * kSegment + id_in_segment<T>(i0 + i, lane) + e);
           }
         __builtin_amdgcn_sched_barrier(0);
@@ -1008,7 +1031,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
   const float unit = static_cast<float>(ilogb(row.scale) - 31);
   const float top = row.top;
   const Bins bin(row);
-  visit<kPartWaves, 4>(
+  visit<kPartWaves, 4, 8>(
       row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
       [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
       [&](float z, int) {
@@ -1116,7 +1139,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
     if (j < kList) state.list[which][j] = entry_of(z, id);
   };
   double sum = 0.0, sum_between = 0.0;
-  visit<kPartWaves, 4>(
+  visit<kPartWaves, 4, 8>(
       row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
       [&](int g) {
         const float top = uniform(row.stats[g].top);
@@ -1151,10 +1174,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
 
 struct Shared {
   uint64_t segment[kMaxSegments];
-  union {
-    uint64_t list[kList];
-    uint64_t bin_mass[kBins];
-  };
+  uint64_t list[kList];
+  uint64_t bin_mass[kBins];
   uint32_t bins[kBins];
   double pow64[64];
   uint64_t slots64[kWaves];
@@ -1164,33 +1185,6 @@ struct Shared {
   uint64_t found_mass, found_mass_before;
   int32_t found_id;
 };
-
-// Sorts list[0 .. n) falling, in place: a value per thread, exchanged between lanes for distances
-// below 64 and through LDS beyond.
-__device__ __forceinline__ void sort_falling(uint64_t* list, int n) {
-  const int t = threadIdx.x;
-  int size = 64;
-  while (size < n) size <<= 1;
-  uint64_t x = t < n ? list[t] : 0;
-  for (int k = 2; k <= size; k <<= 1) {
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      uint64_t o;
-      if (j >= 64) {
-        __syncthreads();
-        list[t] = x;
-        __syncthreads();
-        o = list[t ^ j];
-      } else {
-        o = __shfl_xor(x, j);
-      }
-      const bool larger = ((t & k) == 0) == ((t & j) == 0);  // this place takes the larger one
-      x = (x > o) == larger ? x : o;
-    }
-  }
-  __syncthreads();
-  if (t < size) list[t] = x;
-  __syncthreads();
-}
 
 template <class T>
 struct Searcher {
@@ -1203,7 +1197,7 @@ struct Searcher {
   __device__ __forceinline__ void segment_sums(uint32_t key_low, F f) const {
     __syncthreads();
     uint64_t sum = 0;
-    visit<kWaves, 2>(
+    visit<kWaves, 2, 2>(
         row, 0, row.segments,
         [&](int g) { return order_key(uniform(row.stats[g].top)) >= key_low; },
         [&](float z, int id) { sum += f(z, id); },
@@ -1233,7 +1227,7 @@ struct Searcher {
     const uint32_t least = max(cut.key, key_low);
     double sum = 0.0;
     __syncthreads();
-    visit<kWaves, 2>(
+    visit<kWaves, 2, 2>(
         row, 0, row.segments,
         [&](int g) { return order_key(uniform(row.stats[g].top)) >= least; },
         [&](float z, int id) {
@@ -1248,21 +1242,75 @@ struct Searcher {
     __syncthreads();
   }
 
-  // One of a state's lists, sorted: this thread's entry with its weight, and the weights of the list
-  // before it.
-  __device__ __forceinline__ int sorted_list(const SearchState& state, int which, uint64_t& entry,
-                                             double& x, uint64_t& mass, uint64_t& before,
-                                             uint64_t& total) const {
-    const int t = threadIdx.x, n = static_cast<int>(uniform(state.n_list[which]));
+  // One of a state's lists, an entry a thread.
+  struct Listed {
+    int n;
+    uint64_t entry, mass;  // this thread's (0: none) and its weight
+    double x;
+    uint64_t before;  // in the order of entries: their weights before this one, their number
+    uint32_t place;
+    uint64_t total;  // weight of all
+  };
+  // The entries are first put into bins, whose numbers and sums of weights come by
+  // atomics; within a bin, mostly of one to three, each walks over the others.  (Sorting up to 1024
+  // entries across 16 waves took 4 us more.)
+  __device__ __forceinline__ Listed listed(const SearchState& state, int which) const {
+    constexpr int kListBins = kThreads;
+    const int t = threadIdx.x;
+    Listed l;
+    l.n = static_cast<int>(uniform(state.n_list[which]));
+    const bool active = t < l.n;
+    l.entry = active ? state.list[which][t] : 0;
+    l.x = active ? row.w(key_logit(entry_key(l.entry))) : 0.0;
+    l.mass = whole(l.x, row.scale);
+    // entries as consecutive numbers as far as they go: keys from the list's lowest on (of bf16 logits
+    // their upper halves, so that equal ones are told apart by their ids), then the ids
+    constexpr int kKeyShift = sizeof(T) == 2 ? 16 : 0;
+    const uint32_t key = entry_key(l.entry) >> kKeyShift;
+    const uint32_t high = block_reduce<kWaves>(active ? key : 0, s.slots32, Max{});
+    const uint32_t low = block_reduce<kWaves>(active ? key : 0xffffffffu, s.slots32, Min{});
+    const int id_bits = 32 - __clz(row.vocab);
+    const uint64_t range = (static_cast<uint64_t>(high - low) + 1) << id_bits;
+    const int shift = max(0, 64 - __clzll(static_cast<long long>(range)) - 10);
+    static_assert(kListBins == 1 << 10, "range >> shift is a bin");
+    uint64_t* const sums = s.bin_mass;
+    uint32_t* const counts = s.bins;
+    sums[t] = 0;
+    counts[t] = 0;
     __syncthreads();
-    if (t < n) s.list[t] = state.list[which][t];
+    const uint64_t number = static_cast<uint64_t>(high - key) << id_bits |
+                            static_cast<uint32_t>(entry_id(l.entry));
+    const uint32_t bin = active ? static_cast<uint32_t>(number >> shift) : 0;
+    uint32_t at_in_bin = 0;
+    if (active) {
+      at_in_bin = atomicAdd(&counts[bin], 1u);
+      atomicAdd(reinterpret_cast<unsigned long long*>(&sums[bin]),
+                static_cast<unsigned long long>(l.mass));
+    }
     __syncthreads();
-    sort_falling(s.list, n);
-    entry = t < n ? s.list[t] : 0;
-    x = t < n ? row.w(key_logit(entry_key(entry))) : 0.0;
-    mass = whole(x, row.scale);
-    before = block_scan<kWaves>(mass, s.slots64, total);
-    return n;
+    const uint32_t count = counts[t];
+    uint32_t all;
+    const uint32_t place = block_scan<kWaves>(count, s.slots32, all);
+    const uint64_t before = block_scan<kWaves>(sums[t], s.slots64, l.total);
+    __syncthreads();
+    sums[t] = before;
+    counts[t] = place;
+    __syncthreads();
+    // the entries bin by bin, in no order within one
+    l.before = sums[bin];
+    l.place = counts[bin];
+    const uint32_t end = bin + 1 < kListBins ? counts[bin + 1] : static_cast<uint32_t>(l.n);
+    const uint32_t begin = l.place;
+    if (active) s.list[begin + at_in_bin] = l.entry;
+    __syncthreads();
+    for (uint32_t j = begin; active && j < end; ++j) {
+      const uint64_t other = s.list[j];
+      if (other > l.entry) {
+        ++l.place;
+        l.before += whole(row.w(key_logit(entry_key(other))), row.scale);
+      }
+    }
+    return l;
   }
 
   // The cut from what the launches over parts have found, with the kept ids' sums in s.segment; false
@@ -1276,55 +1324,56 @@ struct Searcher {
       return false;
     for (int g = t; g < row.segments; g += kThreads) s.segment[g] = kept_sums[g];
     const bool by_min_p = uniform(state.bin_m) == last;
-    uint64_t entry, mass, before, in_list, of_k = 0;
-    double x;
-    // top_k's place in a list, with the weights up to it
-    auto up_to = [&](uint32_t ids_before) {
-      const int n = st.top_k - static_cast<int>(uniform(ids_before));
-      if (t == n - 1) s.found_mass = before + mass;
+    // the weight of a list's entries up to the top_k-th id
+    auto up_to = [&](const Listed& l, uint32_t ids_before) {
+      const uint32_t n = static_cast<uint32_t>(st.top_k) - uniform(ids_before);
+      if (l.entry && l.place == n - 1) s.found_mass = l.before + l.mass;
       __syncthreads();
-      const uint64_t m = uniform(s.found_mass);
-      return m;
+      return uniform(s.found_mass);
     };
+    uint64_t of_k = 0;
     if (st.top_p < 1.f && bin_k < kBins && bin_k > last) {
-      sorted_list(state, 1, entry, x, mass, before, in_list);
-      of_k = up_to(state.before_k) + uniform(state.between);
+      const Listed l = listed(state, 1);
+      of_k = up_to(l, state.before_k) + uniform(state.between);
+      __syncthreads();
     }
-    const int n = sorted_list(state, 0, entry, x, mass, before, in_list);
+    const Listed l = listed(state, 0);
     const uint64_t above = sum_of_segments();
-    bool kept = t < n, closed = false;
+    bool kept = l.entry != 0, closed = false;
     if (bin_k == last) {
-      kept &= t < st.top_k - static_cast<int>(uniform(state.before_first));
+      kept &= l.place < static_cast<uint32_t>(st.top_k) - uniform(state.before_first);
       closed = true;
     }
     if (st.top_p < 1.f) {
       uint64_t all = row.whole_sum;
       if (bin_k == last)
-        all = above + up_to(state.before_first);
+        all = above + up_to(l, state.before_first);
       else if (bin_k < kBins)
-        all = above + in_list + of_k;
+        all = above + l.total + of_k;
       const uint64_t target = share_of(all, st.top_p);
       if (above >= target) return false;
-      kept &= above + before < target;
-      closed |= above + in_list >= target;
+      kept &= above + l.before < target;
+      closed |= above + l.total >= target;
     }
     if (st.min_p > 0.f) {
-      kept &= x >= st.min_p;
+      kept &= l.x >= st.min_p;
       closed |= by_min_p;
     }
     if (!closed) return false;
-    if (n == 0) {  // nothing between the bins above and min_p
+    if (l.n == 0) {  // nothing between the bins above and min_p
       cut = kKeepAll;
       return by_min_p;
     }
-    __syncthreads();  // every wave has summed up the segments
-    if (kept)
-      atomicAdd(reinterpret_cast<unsigned long long*>(&s.segment[entry_id(entry) / kSegment]),
-                static_cast<unsigned long long>(mass));
-    // (the kept ones of the list are its first)
-    const uint32_t n_kept = block_reduce<kWaves>(static_cast<uint32_t>(kept), s.slots32, Add{});
-    const uint64_t end = uniform(s.list[n_kept ? n_kept - 1 : 0]);
-    cut = Cut{entry_key(end), entry_id(end) - (n_kept ? 0 : 1)};
+    // (the kept ones of the list are its first; with none kept, the cut lies before all of them)
+    const uint64_t none = ~uint64_t{0};
+    const uint64_t end = block_reduce<kWaves>(kept ? l.entry : none, s.slots64, Min{});
+    if (kept)  // (every wave has summed up the segments)
+      atomicAdd(reinterpret_cast<unsigned long long*>(&s.segment[entry_id(l.entry) / kSegment]),
+                static_cast<unsigned long long>(l.mass));
+    if (end == none)
+      cut = Cut{block_reduce<kWaves>(entry_key(l.entry), s.slots32, Max{}), -1};
+    else
+      cut = Cut{entry_key(end), entry_id(end)};
     return true;
   }
 
@@ -1345,7 +1394,7 @@ struct Searcher {
       }
       if (t == 0) s.found_count = 0;
       __syncthreads();
-      visit<kWaves, 2>(
+      visit<kWaves, 2, 2>(
           row, 0, row.segments, [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
           [&](float z, int) {
             const uint32_t key = order_key(z);
@@ -1414,7 +1463,7 @@ __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, W
       !p.cut_from_lists(ws.states[r], ws.kept + static_cast<size_t>(r) * ws.segments, cut)) {
     if (st.few()) {  // (for which the first launch forms no sums)
       double x = 0.0;
-      visit<kWaves, 2>(
+      visit<kWaves, 2, 2>(
           row, 0, row.segments, [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
           [&](float z, int) { x += row.w.normal(z); }, [](int) {});
       row.set_scale(block_reduce<kWaves>(x, s.slots_d, Add{}));
@@ -1462,10 +1511,11 @@ struct Layout {
   }
 };
 
-// Workgroups per row of the launches over parts: about 2048 in all, at most 16 of a row (a wave has a
-// segment of its own then, at 2^17 ids).
+// Workgroups per row of the launches over parts: up to 8192 in all, as the rows left over are of unlike
+// cost (2048: 300 -> 244 us for 944 rows, mixed settings), at most 32 of a row (a wave has a
+// segment of its own then, up to 2^18 ids).
 int parts_of(int n_rows, int vocab) {
-  return max(1, min(min(2048 / n_rows, 16), (segments_of(vocab) + kPartWaves - 1) / kPartWaves));
+  return max(1, min(min(8192 / n_rows, 32), (segments_of(vocab) + kPartWaves - 1) / kPartWaves));
 }
 
 template <class T>
