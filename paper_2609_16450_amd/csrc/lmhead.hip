@@ -678,8 +678,7 @@ __device__ __forceinline__ void band_tile(int s, int n_vtiles, int n_rtiles, int
 // computing a sequence of tiles of 256 vocabulary rows x BN = 32 TN block positions.  The launch
 // sequence is cut into 8 contiguous segments, one per XCD (workgroup g runs on XCD g % 8 and
 // takes every 32nd tile of its XCD's segment), so each XCD gets the same number of tiles and
-// its 32 resident workgroups share a few W and h tiles in its L2.  With fewer tiles than
-// workgroups, workgroup g computes tile g.
+// its 32 resident workgroups share a few W and h tiles in its L2.
 //
 // Per tile: 4 waves form a 2 x 2 grid of 128 x 16 TN sub-tiles, each 8 x TN blocks of 16x16x32
 // bf16 MFMAs (32 TN accumulator registers per lane).  A stage is 64 hidden columns, two MFMA k
@@ -959,13 +958,9 @@ __global__ __launch_bounds__(256, 1) void lmhead_tile_kernel(
   // this workgroup's tiles: s0, s0 + step, ... below s_end
   const int n_tiles = n_vtiles * n_rtiles;
   const int g = blockIdx.x, groups = gridDim.x;
-  int s0 = g, step = groups, s_end = n_tiles;
-  if (groups == kTileGroups) {
-    const int x = g % kXcds;
-    s_end = static_cast<int>(static_cast<long long>(n_tiles) * (x + 1) / kXcds);
-    s0 = static_cast<int>(static_cast<long long>(n_tiles) * x / kXcds) + g / kXcds;
-    step = kTileGroups / kXcds;
-  }
+  const int x = g % kXcds, step = groups / kXcds;
+  const int s_end = static_cast<int>(static_cast<long long>(n_tiles) * (x + 1) / kXcds);
+  const int s0 = static_cast<int>(static_cast<long long>(n_tiles) * x / kXcds) + g / kXcds;
   if (s0 >= s_end) return;  // whole workgroup
 
   // the wave index is the same on every lane: taken as a scalar, so the LDS destinations of the
@@ -988,7 +983,8 @@ hipError_t launch_tile_tn(int n_rows, int hidden, int vocab, const void* h, cons
   const int n_vtiles = tile_vtiles(vocab);
   const int n_rtiles = (n_rows + 32 * TN - 1) / (32 * TN);
   const int n_tiles = n_vtiles * n_rtiles;
-  const int groups = n_tiles >= kTileGroups ? kTileGroups : n_tiles;
+  // (a multiple of kXcds: every XCD's segment of the launch sequence has its workgroups)
+  const int groups = min(kTileGroups, (n_tiles + kXcds - 1) / kXcds * kXcds);
   hipLaunchKernelGGL((lmhead_tile_kernel<TN, kOut>), dim3(groups), dim3(256), 0, s,
                      static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(w), n_rows,
                      hidden, vocab, n_vtiles, n_rtiles, part, part2);
