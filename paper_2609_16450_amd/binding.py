@@ -234,6 +234,15 @@ def _dev_with(index: int, t: torch.Tensor, name: str, dtype=None, shape=None) ->
         raise ValueError(f"{name} is on device {t.get_device()}, the call's tensors on {index}")
 
 
+def _ok(index: int, t, dtype, shape) -> bool:
+    """What _dev_with checks, without saying what is wrong (half its time; None is no tensor)."""
+    try:
+        return (t.dtype is dtype and t.shape == shape and t.get_device() == index
+                and t.is_contiguous())
+    except AttributeError:
+        return False
+
+
 # The current device's current stream as a handle, without building a torch.cuda.Stream (0.2
 # against 2 us); None where this torch has no such call.
 _get_device = getattr(torch._C, "_cuda_getDevice", None)
@@ -527,19 +536,28 @@ def eb_kv_assign(kv: PagedKV, pool: PagePool, cached, new_rows, cu_block, cu_pre
         raise ValueError("pos must be a tensor [n_rows]")
     i32, n_rows = torch.int32, pos.shape[0]
     state_out = pool.state if state_out is None else state_out
-    for name, t, dtype, shape in (("free_pages", pool.free_pages, i32, (kv.n_pages,)),
-                                  ("state", pool.state, i32, (2,)),
-                                  ("state_out", state_out, i32, (2,)),
-                                  ("cached", cached, i32, (B,)), ("new_rows", new_rows, i32, (B,)),
-                                  ("cu_block", cu_block, i32, (B + 1,)),
-                                  ("cu_prefix", cu_prefix, i32, (B + 1,)),
-                                  ("pos", pos, i32, (n_rows,)),
-                                  ("slot", slot, torch.int64, (n_rows,)),
-                                  ("done", done, torch.uint8, (B,)),
-                                  ("shared", shared, i32, (B,)),
-                                  ("short", short, torch.uint8, (B,))):
-        if t is not None or name in ("cached", "new_rows", "cu_block", "cu_prefix"):
-            _dev_with(index, t, name, dtype, shape)
+    of_batch, offsets, of_rows = (B,), (B + 1,), (n_rows,)
+    if not (_ok(index, cached, i32, of_batch) and _ok(index, new_rows, i32, of_batch)
+            and _ok(index, cu_block, i32, offsets) and _ok(index, cu_prefix, i32, offsets)
+            and _ok(index, pos, i32, of_rows) and _ok(index, state_out, i32, (2,))
+            and pool.free_pages.get_device() == index
+            and (slot is None or _ok(index, slot, torch.int64, of_rows))
+            and (done is None or _ok(index, done, torch.uint8, of_batch))
+            and (shared is None or _ok(index, shared, i32, of_batch))
+            and (short is None or _ok(index, short, torch.uint8, of_batch))):
+        for name, t, dtype, shape in (("free_pages", pool.free_pages, i32, (kv.n_pages,)),
+                                      ("state_out", state_out, i32, (2,)),
+                                      ("cached", cached, i32, of_batch),
+                                      ("new_rows", new_rows, i32, of_batch),
+                                      ("cu_block", cu_block, i32, offsets),
+                                      ("cu_prefix", cu_prefix, i32, offsets),
+                                      ("pos", pos, i32, of_rows),
+                                      ("slot", slot, torch.int64, of_rows),
+                                      ("done", done, torch.uint8, of_batch),
+                                      ("shared", shared, i32, of_batch),
+                                      ("short", short, torch.uint8, of_batch)):
+            if t is not None or name in ("cached", "new_rows", "cu_block", "cu_prefix"):
+                _dev_with(index, t, name, dtype, shape)
     s = _stream_on(index, stream)
     c = eb_page_pool(kv.n_pages, kv.page_size, kv.max_pages, kv.page_table.data_ptr(),
                      pool.free_pages.data_ptr(), pool.state.data_ptr(), state_out.data_ptr())
@@ -639,13 +657,23 @@ def eb_sample(r: Ragged, logits, uniform, token, prob=None, conf=None, temperatu
     index = logits.get_device()
     _dev(logits, "logits", logits.dtype, (T, pitch))
     f32, i32 = torch.float32, torch.int32
-    _dev_with(index, uniform, "uniform", f32, (T,))
-    _dev_with(index, token, "token", i32, (T,))
-    for name, t, dtype, n in (("prob", prob, f32, T), ("conf", conf, f32, T),
-                              ("temperature", temperature, f32, B), ("top_k", top_k, i32, B),
-                              ("top_p", top_p, f32, B), ("min_p", min_p, f32, B)):
-        if t is not None:
-            _dev_with(index, t, name, dtype, (n,))
+    of_rows, of_batch = (T,), (B,)
+    if not (_ok(index, uniform, f32, of_rows) and _ok(index, token, i32, of_rows)
+            and (prob is None or _ok(index, prob, f32, of_rows))
+            and (conf is None or _ok(index, conf, f32, of_rows))
+            and (temperature is None or _ok(index, temperature, f32, of_batch))
+            and (top_k is None or _ok(index, top_k, i32, of_batch))
+            and (top_p is None or _ok(index, top_p, f32, of_batch))
+            and (min_p is None or _ok(index, min_p, f32, of_batch))):
+        _dev_with(index, uniform, "uniform", f32, of_rows)
+        _dev_with(index, token, "token", i32, of_rows)
+        for name, t, dtype, shape in (("prob", prob, f32, of_rows), ("conf", conf, f32, of_rows),
+                                      ("temperature", temperature, f32, of_batch),
+                                      ("top_k", top_k, i32, of_batch),
+                                      ("top_p", top_p, f32, of_batch),
+                                      ("min_p", min_p, f32, of_batch)):
+            if t is not None:
+                _dev_with(index, t, name, dtype, shape)
     rc, s = r.c(), _stream_on(index, stream)
     if r.cu_block.get_device() != index:
         raise ValueError("the batch's offsets and the logits are on different devices")

@@ -10,6 +10,7 @@
 // behind it (length, table or ring, then the stores), not by memory.
 #include "eb_common.hpp"
 #include "eb_internal.hpp"
+#include "wave_ops.hpp"
 
 namespace eb {
 namespace {
@@ -24,11 +25,8 @@ struct Sums {
   __device__ __forceinline__ Sums operator+(const Sums& o) const {
     return Sums{rows + o.rows, prefix + o.prefix, need + o.need, back + o.back};
   }
+  __device__ __forceinline__ Sums& operator+=(const Sums& o) { return *this = *this + o; }
 };
-__device__ __forceinline__ Sums shfl_up(const Sums& s, int n) {
-  return Sums{__shfl_up(s.rows, n), __shfl_up(s.prefix, n), __shfl_up(s.need, n),
-              __shfl_up(s.back, n)};
-}
 
 // Last index t in [0, n) with first[t] <= x, where first[0] <= x and first never decreases.
 __device__ __forceinline__ int last_at_or_before(const uint32_t* first, int n, uint32_t x) {
@@ -80,18 +78,15 @@ __device__ __forceinline__ void assign(const KvAssign& a, bool write_state) {
         own.need = fits ? static_cast<uint32_t>(want - held) : 0;
       }
     }
-    Sums sum = own;  // inclusive, over the wave, then over the waves before
-    for (int n = 1; n < 64; n <<= 1) {
-      const Sums o = shfl_up(sum, n);
-      if (lane >= n) sum = sum + o;
-    }
+    Sums sum = wave_scan(own);  // then over the waves before
     __syncthreads();  // the round before is done with its arrays
     if (lane == 63) wave_sum[wave] = sum;
     __syncthreads();
     Sums total = before;
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      if (w == wave) sum = sum + total;
-      total = total + wave_sum[w];
+      if (w == wave) sum += total;
+      total += wave_sum[w];
     }
     const bool served = fits && (own.need == 0 || sum.need <= free_pages);
     row_first[tid] = sum.rows - own.rows;
