@@ -10,15 +10,21 @@
 // numbers of 2^-62 of (at least) their sum: the sums are exact in any order, also by atomics, and the
 // one rounding of a weight is off by 2^-63 of the sum, less than a sum in 64-bit floats would lose.
 //
-// Two launches.  sample_scan_kernel reads every logit once and leaves, per segment of 2048 ids, its
-// largest and lowest logit and its sums of weights, and the largest of each of its 64 groups of 32 ids.
-// sample_pick_kernel, a workgroup per row, cuts and draws from these: with a temperature alone it
-// reads the one segment that the draw falls into; with a top-k, or where the nucleus is small, the
-// groups that can hold what is kept (their largest logits say which), at most kList ids, sorted
-// in LDS; and otherwise the row again, twice per cut: once for a histogram that finds the bin which
-// the cut lies in, once for the exact sums above that bin and the ids within it.  Where that bin holds
-// more ids than the list (logits that tie, or a few that lie far off the others), the cut's key is
-// found bit by bit instead.
+// sample_scan_kernel reads every logit once and leaves, per segment of 2048 ids, its largest and lowest
+// logit and its sums of weights, and the largest of each of its 64 groups of 32 ids.
+// sample_pick_kernel, a workgroup per row, cuts and draws from these alone where that can be done: with
+// a temperature only it reads the one segment that the draw falls into; with a small top-k, or where
+// the nucleus is small, the groups that can hold what is kept (their largest logits say which), at
+// most kPickList ids in LDS.  The rows left over are read again.  Of a large vocabulary,
+// sample_bins_kernel makes a histogram which finds the few bins that the cut lies in, and
+// sample_sums_kernel the exact sums above them and a list of the ids within, many workgroups to a row;
+// sample_search_kernel, one workgroup to a row, orders the list, cuts and draws.  Rows of a smaller
+// vocabulary, and those whose bins hold more ids than the list (logits that tie, or a few that lie
+// far off the others), it cuts by itself, the key found bit by bit.
+//
+// Bounds: many rows are bound by reading the logits, once in the scan (944 fp32 rows of 126464, mixed
+// settings: 110 us, 4.3 TB/s), and once or twice more where they are left over; few rows by one
+// dependent step after another (a single row with a temperature or a small top-k: 20 us, two launches).
 #include <float.h>
 #include <stddef.h>
 
@@ -62,7 +68,7 @@ __device__ __forceinline__ int id_in_segment(int i, int lane) {
 }
 
 // Logits at .. at + kVec - 1 of a row, as they came; -inf behind its end.  (Loads without the test for
-// segments that lie before the row's end: 300 -> 318 us for 944 rows of 126464.)
+// segments that lie before the row's end: 108 -> 123 us for 944 rows of 126464.)
 template <class T>
 struct Chunk;
 template <>
@@ -284,7 +290,7 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(SampleArgs a,
   if (threadIdx.x < 64) pow64[threadIdx.x] = kPow64[threadIdx.x];
   const Settings st = settings(a, find_sequence(a.cu_block, a.batch, r, lane));
   __syncthreads();
-  if (g >= ws.segments) return;
+  if (g >= ws.segments || r >= a.cu_block[a.batch]) return;
 
   float top = -INFINITY, low = INFINITY;
   bool bad = false;
@@ -766,6 +772,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
   row.low = uniform(wave_reduce(lo, Min{}));
   bad = __any(bad);
   RowHeader& header = ws.headers[row.r];
+  if (row.r >= a.cu_block[a.batch]) {  // behind the last sequence
+    if (t == 0) header.pending = 0;
+    return;
+  }
   if (bad || row.top == -INFINITY) {  // a NaN or +inf; or nothing to draw from
     if (t == 0) {
       a.token[row.r] = -1;
@@ -869,12 +879,13 @@ constexpr int kPartWaves = kPartThreads / 64;
 
 // f(z, id) for every id that this lane holds of segments first + wave, first + wave + kN, .. below
 // `end` for which wanted(g); then each_segment(g) (by the whole wave) for these and the others.
-// kAtOnce loads at a time, the next ones under way meanwhile, worked on by kIds ids: a weight is a chain
-// of a dozen operations, of which a wave alone on its SIMD needs several at once (8: 14 -> 10 us for 32
-// rows, a segment to a wave); with more than two the kernels of 16 waves spill.
-template <int kN, int kAtOnce, int kIds, class T, class Wanted, class F, class End>
+// Two loads at a time, the next two under way meanwhile (four: 232 -> 237 us for 944 rows of 126464, mixed
+// settings), worked on by two ids (with more the kernels of 16 waves, which have 128 registers a lane,
+// spill; the others take the same time with eight).
+template <int kN, class T, class Wanted, class F, class End>
 __device__ __forceinline__ void visit(const Row<T>& row, int first, int end, Wanted wanted, F f,
                                       End each_segment) {
+  constexpr int kAtOnce = 2, kIds = 2;
   const int lane = threadIdx.x & 63;
   for (int g = first + wave_index(); g < end; g += kN) {
     if (wanted(g)) {
@@ -960,7 +971,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
   const float unit = static_cast<float>(ilogb(row.scale) - 31);
   const float top = row.top;
   const Bins bin(row);
-  visit<kPartWaves, 4, 8>(
+  visit<kPartWaves>(
       row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
       [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
       [&](float z, int) {
@@ -980,10 +991,10 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
 }
 
 // The bin in which the running sum of x (kBins / kPartThreads bins a thread) reaches `target`, with the
-// sum before it and its own; kBins where none does.
+// sum before it; kBins where none does.
 struct FoundBin {
   int bin;
-  uint64_t before, own;
+  uint64_t before;
 };
 __device__ __forceinline__ FoundBin find_bin(const uint32_t* x, uint64_t target, uint64_t* slots,
                                              FoundBin* found) {
@@ -997,17 +1008,17 @@ __device__ __forceinline__ FoundBin find_bin(const uint32_t* x, uint64_t target,
     mine += v[e];
   }
   __syncthreads();  // (what an earlier call has found has been read)
-  if (t == 0) *found = FoundBin{kBins, 0, 0};
+  if (t == 0) *found = FoundBin{kBins, 0};
   uint64_t run = block_scan<kPartWaves>(mine, slots, total);
   if (run < target && run + mine >= target) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      if (run < target && run + v[e] >= target) *found = FoundBin{t * kEach + e, run, v[e]};
+      if (run < target && run + v[e] >= target) *found = FoundBin{t * kEach + e, run};
       run += v[e];
     }
   }
   __syncthreads();
-  return FoundBin{uniform(found->bin), uniform(found->before), uniform(found->own)};
+  return FoundBin{uniform(found->bin), uniform(found->before)};
 }
 
 template <class T>
@@ -1068,7 +1079,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
     if (j < kList) state.list[which][j] = entry_of(z, id);
   };
   double sum = 0.0, sum_between = 0.0;
-  visit<kPartWaves, 4, 8>(
+  visit<kPartWaves>(
       row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
       [&](int g) {
         const float top = uniform(row.stats[g].top);
@@ -1126,7 +1137,7 @@ struct Searcher {
   __device__ __forceinline__ void segment_sums(uint32_t key_low, F f) const {
     __syncthreads();
     uint64_t sum = 0;
-    visit<kWaves, 2, 2>(
+    visit<kWaves>(
         row, 0, row.segments,
         [&](int g) { return order_key(uniform(row.stats[g].top)) >= key_low; },
         [&](float z, int id) { sum += f(z, id); },
@@ -1156,7 +1167,7 @@ struct Searcher {
     const uint32_t least = max(cut.key, key_low);
     double sum = 0.0;
     __syncthreads();
-    visit<kWaves, 2, 2>(
+    visit<kWaves>(
         row, 0, row.segments,
         [&](int g) { return order_key(uniform(row.stats[g].top)) >= least; },
         [&](float z, int id) {
@@ -1323,7 +1334,7 @@ struct Searcher {
       }
       if (t == 0) s.found_count = 0;
       __syncthreads();
-      visit<kWaves, 2, 2>(
+      visit<kWaves>(
           row, 0, row.segments, [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
           [&](float z, int) {
             const uint32_t key = order_key(z);
@@ -1392,7 +1403,7 @@ __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, W
       !p.cut_from_lists(ws.states[r], ws.kept + static_cast<size_t>(r) * ws.segments, cut)) {
     if (st.few()) {  // (for which the first launch forms no sums)
       double x = 0.0;
-      visit<kWaves, 2, 2>(
+      visit<kWaves>(
           row, 0, row.segments, [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
           [&](float z, int) { x += row.w.normal(z); }, [](int) {});
       row.set_scale(block_reduce<kWaves>(x, s.slots_d, Add{}));

@@ -521,6 +521,101 @@ def test_draws_follow_the_distribution():
     assert np.bincount(token).tolist() == [100, 200, 300, 400, 600, 1600]
 
 
+def test_padded_batch():
+    """Rows behind the last sequence's: not used, whatever they hold, and their outputs left as they were;
+    the others as without them.  In a batch of which every row is padding nothing changes."""
+    rng = np.random.default_rng(20)
+    for V in (300, 5000, 40011):
+        z, u = _logits(12, V, 20), rng.random(12)
+        for settings in (dict(), dict(top_k=20), dict(top_p=0.9), dict(temperature=0.0, top_k=3)):
+            d = Draw(z[:7], u[:7], blocks=[3, 0, 4], **settings)
+            want = d.check()
+            p = Draw(np.concatenate([z[:7], np.full((5, V), np.nan)]), u, blocks=[3, 0, 9], **settings)
+            for end, n in (([3, 3, 7], 7), ([0, 0, 0], 0)):
+                p.ragged.cu_block = _dev([0, *end], I32)
+                got = p.run()
+                for g, w in zip(got, want):
+                    np.testing.assert_array_equal(g[:n], w[:n])
+                    assert (g[n:] == 99).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_repeated_calls_give_the_same_bits(dtype):
+    """Wide nuclei by atomics in any order, over many rows: the same bits each time."""
+    T, V = 96, 50021
+    d = Draw(_logits(T, V, 21, "plain"), np.random.default_rng(21).random(T), dtype=dtype,
+             temperature=np.linspace(0.5, 2, T), top_k=np.where(np.arange(T) % 3 == 0, 20000, 0),
+             top_p=np.linspace(0.5, 0.999, T), min_p=np.where(np.arange(T) % 4 == 0, 1e-4, 0))
+    want = d.check()
+    ws = torch.empty(eb_sample_workspace(EB_BF16 if dtype == "bf16" else EB_F32, T, V),
+                     dtype=torch.uint8, device="cuda")
+    for i in range(30):
+        ws.fill_(i * 37 % 256)
+        for got, w in zip(d.run(ws=ws), want):
+            np.testing.assert_array_equal(got, w, err_msg=str(i))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [256, 257, 2048, 32768, 32769, 34817, 40960])
+def test_vocabularies_at_borders(V, dtype):
+    """Sizes at which a call takes other launches, or a row's parts end with a segment."""
+    z = _logits(2 * len(SETTINGS), V, 22, "plain")
+    u = np.random.default_rng(V).random(len(z))
+    keys = ("temperature", "top_k", "top_p", "min_p")
+    cols = {k: [s.get(k, d) for s in SETTINGS] for k, d in zip(keys, (1.0, 0, 1.0, 0.0))}
+    Draw(z, u, blocks=[2] * len(SETTINGS), dtype=dtype, **cols).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [3001, 40011])
+def test_more_ties_than_a_list_holds(V, dtype):
+    """Borders inside thousands of equal logits, above them and below them, and logits far off the rest."""
+    rng = np.random.default_rng(23)
+    z = np.round(rng.standard_normal((12, V)) * 0.5)
+    z[4:8, rng.choice(V, 9, replace=False)] += 40.0
+    z[8:10, 5] = 1e6
+    z[10:, 7] = -1e30
+    u = rng.random(12)
+    for settings in (dict(top_k=3), dict(top_k=100), dict(top_k=V // 2), dict(top_k=V - 1), dict(top_p=0.01),
+                     dict(top_p=0.5), dict(top_p=0.97), dict(top_k=V // 2, top_p=0.6), dict(min_p=0.3),
+                     dict(top_k=70, top_p=0.6, min_p=0.1), dict(top_p=0.999, min_p=1e-9, temperature=3.0)):
+        Draw(z, u, dtype=dtype, **settings).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 5000, 40011])
+def test_extreme_temperatures(V, dtype):
+    """From the smallest number to infinity: the top id alone, or all ids above -inf alike."""
+    rng = np.random.default_rng(24)
+    z = _logits(4, V, 24, "plain")
+    z[2, ::3] = -np.inf
+    z[3] = np.where(rng.random(V) < 0.5, 3e38, -3e38)
+    u = rng.random(4)
+    with np.errstate(invalid="ignore", over="ignore"):
+        for t in (1e-45, 1e-38, 1e-3, 1e3, 1e30, 3e38):
+            for settings in (dict(), dict(top_k=5), dict(top_k=250), dict(top_p=0.9), dict(min_p=0.9)):
+                Draw(z, u, dtype=dtype, temperature=t, **settings).check()
+        # infinity, for which the formula gives 0 times infinity
+        for settings in (dict(), dict(top_k=5), dict(top_p=0.9), dict(min_p=0.9)):
+            got = Draw(z[:3], u[:3], dtype=dtype, temperature=np.inf, **settings).run()
+            want = Draw(z[:3], u[:3], dtype=dtype, temperature=3e38, **settings).run()
+            np.testing.assert_array_equal(got[0], want[0])
+
+
+def test_more_rows_than_parts():
+    """So many rows that each is one part; and counts at which a row's parts change."""
+    V = 34000
+    z, u = _logits(64, V, 25, "plain"), np.random.default_rng(25).random(64)
+    want = Draw(z, u, top_p=0.9).check()
+    for n in (129, 150):                                # 64 rows each: 8256 and 9600
+        r = Ragged.from_lengths([64 * n], [0])
+        out = [torch.zeros(64 * n, dtype=dt, device="cuda") for dt in (I32, F32)]
+        eb_sample(r, _dev(z.astype(np.float32)).repeat(n, 1), _dev(u.astype(np.float32)).repeat(n), out[0],
+                  prob=out[1], top_p=_dev([0.9], F32))
+        for got, w in zip(out, want):
+            np.testing.assert_array_equal(got.view(n, 64).cpu().numpy(), np.broadcast_to(w, (n, 64)))
+
+
 def test_sample_refusals():
     d = Draw(_logits(3, 100, 18), [0.5] * 3)
     z, u, r = d.logits, _dev(d.u), d.ragged
