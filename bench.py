@@ -159,7 +159,8 @@ def cpu_baseline(case, budget_s: float = 15.0):
 
 
 SUFFIX_LEN = 256         # cached suffix rows per sequence on the dual-cache leg
-PAGE_SIZE = 64           # rows per page (paths paged, paged8)
+PAGE_SIZE = 64           # rows per page (paths paged, paged8, sample)
+TEMPERATURE, TOP_P = 0.8, 0.95  # of every sequence on the sample leg
 LBS_WINDOW = 512         # generation window of the LBS leg (generation length 512, App. F)
 TAU_PSI = 0.9            # LPS acceptance threshold on the lps leg
 TOP_M = 2                # per-block budget on the topm leg
@@ -231,6 +232,19 @@ def paged_cache(torch, eb, case, ds, e4m3: bool):
     return kv
 
 
+def free_pages(torch, eb, case, kv):
+    """A pool of the pages that paged_cache has set aside for the workload's blocks."""
+    table = kv.page_table.cpu().numpy()
+    free = [table[b, -(-int(p) // PAGE_SIZE):-(-int(p + n) // PAGE_SIZE)]
+            for b, (p, n) in enumerate(zip(case.prefix_lens, case.block_lens))]
+    free = np.concatenate(free).astype(np.int32)
+    ring = np.zeros(kv.n_pages, np.int32)
+    ring[:len(free)] = free
+    dev = kv.page_table.device
+    return eb.PagePool(torch.from_numpy(ring).to(dev),
+                       torch.tensor([0, len(free)], dtype=torch.int32, device=dev))
+
+
 def variant_leg(args, torch, eb, case, copies, stream) -> int:
     """The next-row paths: one JSON line with the same fields as the headline."""
     from workloads import lbs_window, router_scores, suffix_segment
@@ -260,10 +274,20 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
                 dt_code, ctypes.byref(ds.ragged.c()),
                 ctypes.byref(eb_suffix(SUFFIX_LEN * B, SUFFIX_LEN, 0)), cfg.hq, cfg.hkv,
                 cfg.head_dim))
-        if args.path in ("paged", "paged8"):
+        if args.path in ("paged", "paged8", "sample"):
             x["kv"] = paged_cache(torch, eb, case, ds, args.path == "paged8")
             x["attn_ws"] = u8(eb.eb_block_attn_paged_workspace(dt_code, ds.ragged, x["kv"],
                                                                cfg.hq))
+        if args.path == "sample":
+            i32 = dict(dtype=torch.int32, device=dev)
+            x.update(pool=free_pages(torch, eb, case, x["kv"]),
+                     cached=torch.tensor(case.prefix_lens, **i32),
+                     new=torch.tensor(case.block_lens, **i32), pos=torch.empty(T, **i32),
+                     state_out=torch.empty(2, **i32), logits=torch.empty((T, cfg.vocab), device=dev),
+                     token=torch.empty(T, **i32), uniform=torch.rand(T, device=dev),
+                     temperature=torch.full((B,), TEMPERATURE, device=dev),
+                     top_p=torch.full((B,), TOP_P, device=dev),
+                     sample_ws=u8(eb.eb_sample_workspace(eb.EB_F32, T, cfg.vocab)))
         extra.append(x)
     if args.path == "lbs":
         m, p, xh = lbs_window(cfg.seed, B, LBS_WINDOW, cfg.vocab, cfg.vocab - 1)
@@ -280,11 +304,14 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
             eb.eb_lbs_select(L["m"], L["p"], L["x"], cfg.vocab - 1, 4, 32, 5, L["block"],
                              L["size"], L["first"], stream=stream)
             return
+        if args.path == "sample":  # offsets and pages of the step; the pool stays as it is
+            eb.eb_kv_assign(x["kv"], x["pool"], x["cached"], x["new"], ds.ragged.cu_block,
+                            ds.ragged.cu_prefix, x["pos"], state_out=x["state_out"], stream=stream)
         if args.path == "dual":
             eb.eb_block_attn_dual(ds.ragged, x["cu_s"], SUFFIX_LEN, ds.q, ds.k_blk, ds.v_blk,
                                   ds.k_pre, ds.v_pre, x["k_s"], x["v_s"], ds.attn_out,
                                   ws=x["attn_ws"], stream=stream)
-        elif args.path in ("paged", "paged8"):
+        elif args.path in ("paged", "paged8", "sample"):
             eb.eb_block_attn_paged(ds.ragged, x["kv"], ds.q, ds.k_blk, ds.v_blk, ds.attn_out,
                                    ws=x["attn_ws"], stream=stream)
         else:
@@ -295,12 +322,20 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
         if args.path == "lps":
             eb.eb_lmhead_features(ds.h, ds.w, ds.conf, ds.entropy, ds.argmax, x["gap"],
                                   ds.max_logit, ws=x["lm_ws"], stream=stream)
+        elif args.path == "sample":
+            eb.eb_lmhead_logits(ds.h, ds.w, x["logits"], stream=stream)
         else:
             eb.eb_lmhead_confidence(ds.h, ds.w, ds.conf, ds.entropy, ds.argmax, ds.max_logit,
                                     ws=x["lm_ws"], stream=stream)
         if lm_events:
             lm_events[1].record(stream)
-        if args.path == "lps":
+        if args.path == "sample":
+            eb.eb_sample(ds.ragged, x["logits"], x["uniform"], x["token"], conf=ds.conf,
+                         temperature=x["temperature"], top_p=x["top_p"], ws=x["sample_ws"],
+                         stream=stream)
+            eb.eb_unmask_select(ds.ragged, ds.conf, x["token"], ds.tau, ds.masked, ds.tokens,
+                                ds.unmask, ds.n_commit, ds.resolved, stream=stream)
+        elif args.path == "lps":
             eb.eb_lps_features(ds.ragged, cfg.vocab, ds.conf, ds.entropy, x["gap"], ds.masked,
                                x["feat"], x["pos"], x["rho"], stream=stream)
             eb.eb_unmask_select_lps(ds.ragged, ds.conf, ds.argmax, ds.tau, x["p_psi"], TAU_PSI,
@@ -313,8 +348,9 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
         else:
             eb.eb_unmask_select(ds.ragged, ds.conf, ds.argmax, ds.tau, ds.masked, ds.tokens,
                                 ds.unmask, ds.n_commit, ds.resolved, stream=stream)
-        if args.path in ("paged", "paged8"):  # the block's rows go into the cache
-            eb.eb_kv_write(ds.ragged, x["kv"], ds.k_blk, ds.v_blk, stream=stream)
+        if args.path in ("paged", "paged8", "sample"):  # the block's rows go into the cache
+            eb.eb_kv_write(ds.ragged, x["kv"], ds.k_blk, ds.v_blk,
+                           pos=x["pos"] if args.path == "sample" else None, stream=stream)
 
     for i in range(args.warmup):
         run(i)
@@ -349,9 +385,16 @@ def variant_leg(args, torch, eb, case, copies, stream) -> int:
                 "frac": achieved / peak, "traffic": None,
                 "kernel": lmhead_kernel_name(cfg.dtype, T) + " + lmhead_combine_kernel",
                 "kernel_us": lm_ms * 1e3, "algorithmic_bytes": nbytes, "algorithmic_flops": flops}
+        if args.path == "sample":  # the logits are written as well; no combining launch
+            nbytes += 4 * T * cfg.vocab - 12 * T
+            roof.update(kernel=lmhead_kernel_name(cfg.dtype, T), algorithmic_bytes=nbytes)
+            if bound == "hbm":
+                achieved = nbytes / (lm_ms * 1e-3) / 1e9
+                roof.update(achieved=achieved, frac=achieved / peak)
+            config.update(temperature=TEMPERATURE, top_p=TOP_P)
         if args.path == "dual":
             config["suffix_positions"] = SUFFIX_LEN * B
-        if args.path in ("paged", "paged8"):
+        if args.path in ("paged", "paged8", "sample"):
             config.update(page_size=PAGE_SIZE, cache="e4m3" if args.path == "paged8" else cfg.dtype)
         if args.path == "lps":
             config["tau_psi"] = TAU_PSI
@@ -558,13 +601,15 @@ def main() -> int:
     ap.add_argument("--no-peaks", action="store_true",
                     help="skip the same-box copy and GEMM reference rates (e.g. under a profiler)")
     ap.add_argument("--path", default="step",
-                    choices=["step", "lps", "topm", "dual", "lbs", "paged", "paged8"],
+                    choices=["step", "lps", "topm", "dual", "lbs", "paged", "paged8", "sample"],
                     help="step: eb_decode_step (the headline); lps: attention + LM head with the "
                          "top-2 gap + LPS features + union accept rule; topm: attention + LM head "
                          "+ top-m commit; dual: dual-cache attention + LM head + unmask; lbs: the "
                          "LBS post-pass over a 512-position generation window per sequence; "
                          "paged, paged8: attention over a paged cache (paged8: of 8 bits) + LM "
-                         "head + unmask + the block's rows into the cache")
+                         "head + unmask + the block's rows into the cache; sample: pages for the "
+                         "block's rows + attention over a paged cache + logits + a draw under a "
+                         "temperature and top-p + unmask + the rows into the cache")
     args = ap.parse_args()
 
     if args.ingest_counters:

@@ -11,6 +11,9 @@
  *   3. threshold commit kappa >= tau with the anti-stall fallback inside each block
  *                                                          -> eb_unmask_select
  *   4. all of the above on one stream                      -> eb_decode_step
+ * For serving, the cached rows may live in pages (eb_paged_kv, eb_kv_write, eb_kv_read,
+ * eb_block_attn_paged), which eb_kv_assign hands out and takes back on the device; and tokens may be
+ * drawn instead of taken greedily: eb_lmhead_logits writes the logits out, eb_sample draws.
  *
  * Conventions shared by every entry point
  *   - Every pointer argument is a DEVICE pointer owned by the caller unless stated
