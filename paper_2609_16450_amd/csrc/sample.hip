@@ -200,7 +200,7 @@ static_assert(sizeof(SegmentStats) == 24, "packed");
 // Top-k small enough to be settled by the second launch: half the list, so that the ids which the
 // groups' largest logits let through besides fit as well.
 constexpr int kFewIds = kPickList / 2;
-// Ids among which a top-p or min-p alone is tried: a sure model's nucleus.
+// Ids among which a top-p or min-p is tried otherwise: a sure model's nucleus.
 constexpr int kNucleus = 64;
 
 // A row's settings.
@@ -438,10 +438,10 @@ struct Row {
       const uint64_t hit = __ballot(upto > x);
       if (hit) {
         const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
-        before = uniform(__shfl(upto - part, l));
+        before = of_lane(upto - part, l);
         return g0 + l;
       }
-      base = uniform(__shfl(upto, 63));
+      base = of_lane(upto, 63);
     }
     before = base;
     return segments - 1;
@@ -514,8 +514,9 @@ struct PickShared {
   uint32_t groups[kPickList];
   uint64_t slots64[kPickWaves];
   uint32_t slots32[kPickWaves];
+  float slots_f[kPickWaves];
   uint64_t sum_of_k;
-  uint32_t n_list, n_groups, past_min_p;
+  uint32_t n_list, n_groups, past_min_p, unsure;
   int32_t found_id;
 };
 
@@ -549,105 +550,126 @@ struct SegmentsOfRow {
   }
 };
 
-// Largest logits of groups t, t + kPickThreads, .., the first ones (rows of up to 163840 ids) in
-// registers.
+// Largest logits of a row's groups: thread t has groups 4 t .. 4 t + 3 of every 4 kPickThreads, the first
+// ones (rows of up to 163840 ids) in registers.
 struct GroupTops {
-  static constexpr int kHeld = 20;
+  static constexpr int kHeld = 5, kPass = 4 * kPickThreads;
   const float* tops;
-  int n;
-  float held[kHeld];
+  int n;  // a multiple of 64
+  f32x4 held[kHeld];
   __device__ __forceinline__ GroupTops(const float* tops_, int n_) : tops(tops_), n(n_) {
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
-      const int i = threadIdx.x + j * kPickThreads;
-      held[j] = i < n ? tops[i] : -INFINITY;
+      const int i = j * kPass + 4 * static_cast<int>(threadIdx.x);
+      held[j] = i < n ? *reinterpret_cast<const f32x4*>(tops + i)
+                      : f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     }
+  }
+  // Number of this thread's first group of a pass.
+  static __device__ __forceinline__ int first(int pass) {
+    return pass * kPass + 4 * static_cast<int>(threadIdx.x);
   }
   template <class F>
   __device__ __forceinline__ void each(F f) const {
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) f(held[j], static_cast<int>(threadIdx.x) + j * kPickThreads);
-    for (int i = threadIdx.x + kHeld * kPickThreads; i < n; i += kPickThreads) f(tops[i], i);
+    for (int j = 0; j < kHeld; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(held[j][e]);
+    for (int i = first(kHeld); i < n; i += kPass)
+      for (int e = 0; e < 4; ++e) f(tops[i + e]);
   }
 };
 
-// put(place, j) for the items j < kN of each lane for which has(j): places of one list, reserved once a
-// wave (with a branch and an atomic to each item, most of the kernel's time went here).
-template <int kN, class Has, class Put>
-__device__ __forceinline__ void append(uint32_t& length, Has has, Put put) {
-  uint64_t lanes[kN];
-  uint32_t total = 0;
-#pragma unroll
-  for (int j = 0; j < kN; ++j) {
-    lanes[j] = __ballot(has(j));
-    total += __popcll(lanes[j]);
-  }
-  if (total == 0) return;
+// The first of `mine` places in a list for this lane; reserved once a wave.  (With a branch and an atomic
+// to each item most of the kernel's time went here.)
+__device__ __forceinline__ uint32_t reserve(uint32_t& length, uint32_t mine) {
+  const uint32_t upto = wave_scan(mine), total = of_lane(upto, 63);
   uint32_t at = 0;
-  if ((threadIdx.x & 63) == 0) at = atomicAdd(&length, total);
-  at = uniform(at);
-#pragma unroll
-  for (int j = 0; j < kN; ++j)
-    if (lanes[j]) {
-      const uint32_t low = static_cast<uint32_t>(lanes[j]), high = static_cast<uint32_t>(lanes[j] >> 32);
-      const uint32_t place = at + __builtin_amdgcn_mbcnt_hi(high, __builtin_amdgcn_mbcnt_lo(low, 0));
-      if (has(j)) put(place, j);
-      at += __popcll(lanes[j]);
-    }
+  if (total && (threadIdx.x & 63) == 0) at = atomicAdd(&length, total);
+  return uniform(at) + upto - mine;
 }
 
-// The first ids of the order into s.list: at least `want` of them, by way of the groups whose largest
-// logit lies in the first so many bins of these; all ids above -inf (then `complete`) where there are
-// at most kPickList.  Returns their number, or -1 where they are more than that.
+// The first ids of the order into s.list, by way of the groups whose largest logits are the first of
+// these; all ids above -inf (then `complete`) where there are at most kPickList.  By count: at least
+// `want` of them.  Otherwise about as many, less where the rest weighs less than e^-48 of the largest.
+// Returns their number, or -1 where they are more than kPickList.
+//
+// (What a row costs here is its code, which every launch fetches anew: about 0.6 us per 1000 bytes.  So
+// there is one comparison to an item, with a logit, once that has been found.)
 template <class T>
 __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, PickShared& s,
-                                      uint32_t want, bool& complete) {
+                                      uint32_t want, bool by_count, bool& complete) {
+  constexpr int kLevels = 3;
   const int t = threadIdx.x, lane = t & 63;
-  // (what weighs less than e^-48 of the largest needs no bin of its own; halves: no overflow)
-  const float from = fmaxf(row.low, row.top - 48.f * row.st.temperature);
-  const float per = fminf((kPickThreads - 1) / (0.5f * row.top - 0.5f * from), FLT_MAX);
-  auto bin = [&](float z) {
-    return static_cast<int>(fminf((0.5f * row.top - 0.5f * z) * per, kPickThreads - 1.f));
-  };
-  tops.each([&](float z, int) {
-    if (z > -INFINITY) atomicAdd(&s.bins[bin(z)], 1u);
-  });
-  __syncthreads();
-  // the bin that the want-th group lies in; every wave for itself, four bins a lane
-  int last = kPickThreads - 1;
-  uint32_t finite;
-  {
+  float hi = row.top, lo = fmaxf(row.low, row.top - 48.f * row.st.temperature);
+  float least = row.low;  // that has a bin
+  float cut;              // least logit that is taken
+  // The bin of [lo, hi] that the want-th group lies in, the last one for what lies lower as well.  Where
+  // the groups up to it are more than the list, the bins are laid over that bin's: a sure row's one
+  // logit far above all others, then perhaps a mask's far below them.
+  uint32_t ahead = 0;  // groups above hi
+  for (int level = 0;; ++level) {
+    // (halves: no overflow)
+    const float per = fminf((kPickThreads - 1) / (0.5f * hi - 0.5f * lo), FLT_MAX);
+    auto bin = [&](float z) {
+      return static_cast<int>(fminf((0.5f * hi - 0.5f * z) * per, kPickThreads - 1.f));
+    };
+    tops.each([&](float z) {
+      if (z >= least && z <= hi) atomicAdd(&s.bins[bin(z)], 1u);
+    });
+    __syncthreads();
+    // every wave for itself, four bins a lane
     const u32x4 c = *reinterpret_cast<const u32x4*>(&s.bins[4 * lane]);
-    const uint32_t sum = c[0] + c[1] + c[2] + c[3], upto = wave_scan(sum);
-    finite = uniform(__shfl(upto, 63));
+    const uint32_t sum = c[0] + c[1] + c[2] + c[3], upto = ahead + wave_scan(sum);
+    uint32_t through = of_lane(upto, 63), before = through;
+    if (level == 0) complete = row.vocab <= kPickList || through * kGroup <= kPickList;
+    int last = kPickThreads - 1;
     const uint64_t hit = __ballot(upto >= want);
-    if (hit) {
+    if (hit && !complete) {
       const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
-      uint32_t n = upto - sum;
-      int b = 4 * lane;
-#pragma unroll
-      for (int e = 0; e < 3; ++e) {
-        n += c[e];
-        if (n < want) b = 4 * lane + e + 1;
-      }
-      last = uniform(__shfl(b, l));
+      before = of_lane(upto - sum, l);
+      last = 4 * l;
+      through = before + of_lane(c[0], l);
+      if (through < want) ++last, before = through, through += of_lane(c[1], l);
+      if (through < want) ++last, before = through, through += of_lane(c[2], l);
+      if (through < want) ++last, before = through, through += of_lane(c[3], l);
     }
+    if (!by_count && !complete && lo > row.low) last = min(last, kPickThreads - 2);
+    // (a bin lower than the one found, for the roundings of both)
+    cut = last == kPickThreads - 1 ? least : fmaxf(2.f * (0.5f * hi - (last + 2) / per), least);
+    if (!by_count || complete || through <= kPickList || level == kLevels - 1) break;
+    float a = -INFINITY, b = INFINITY;
+    tops.each([&](float z) {
+      const bool in = z >= least && z <= hi && bin(z) == last;
+      a = fmaxf(a, in ? z : -INFINITY);
+      b = fminf(b, in ? z : INFINITY);
+    });
+    a = block_reduce<kPickWaves>(a, s.slots_f, Max{});
+    s.bins[t] = 0;  // (every wave has read them)
+    b = block_reduce<kPickWaves>(b, s.slots_f, Min{});
+    hi = a;
+    least = lo = b;
+    ahead = before;
   }
-  complete = row.vocab <= kPickList || finite * kGroup <= kPickList;
-  if (complete) last = kPickThreads - 1;
-  auto taken = [&](float z) { return z > -INFINITY && bin(z) <= last; };
-  append<GroupTops::kHeld>(
-      s.n_groups, [&](int j) { return taken(tops.held[j]); },
-      [&](uint32_t place, int j) {
-        if (place < kPickList) s.groups[place] = static_cast<uint32_t>(t + j * kPickThreads);
-      });
-  for (int i0 = GroupTops::kHeld * kPickThreads; i0 < tops.n; i0 += kPickThreads) {
-    const float z = i0 + t < tops.n ? tops.tops[i0 + t] : -INFINITY;
-    append<1>(
-        s.n_groups, [&](int) { return taken(z); },
-        [&](uint32_t place, int) {
-          if (place < kPickList) s.groups[place] = static_cast<uint32_t>(i0 + t);
-        });
+  uint32_t taken = 0;  // bit 4 j + e: held[j][e]
+#pragma unroll
+  for (int j = 0; j < GroupTops::kHeld; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) taken |= static_cast<uint32_t>(tops.held[j][e] >= cut) << (4 * j + e);
+  auto put_groups = [&](int pass) {
+    uint32_t place = reserve(s.n_groups, __popc(taken));
+    for (; taken; taken &= taken - 1) {
+      const int bit = __ffs(taken) - 1;
+      if (place < kPickList)
+        s.groups[place++] = static_cast<uint32_t>(GroupTops::first(pass + bit / 4) + bit % 4);
+    }
+  };
+  put_groups(0);
+  for (int pass = GroupTops::kHeld; pass * GroupTops::kPass < tops.n; ++pass) {
+    const int i = GroupTops::first(pass);
+    for (int e = 0; e < 4; ++e)
+      if (i < tops.n && tops.tops[i + e] >= cut) taken |= 1u << e;
+    put_groups(pass);
   }
   __syncthreads();
   const int found = static_cast<int>(uniform(s.n_groups));
@@ -657,6 +679,7 @@ __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, 
   for (int i0 = 0; i0 < found * kGroup; i0 += kAtOnce * kPickThreads) {
     float z[kAtOnce];
     int ids[kAtOnce];
+    uint32_t mine = 0;
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
       const int item = i0 + j * kPickThreads + t, k = item % kGroup;
@@ -665,11 +688,12 @@ __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, 
       z[j] = load_logit(row.logits, min(ids[j], row.vocab - 1));
       if (item >= found * kGroup || ids[j] >= row.vocab) z[j] = -INFINITY;
     }
-    append<kAtOnce>(
-        s.n_list, [&](int j) { return taken(z[j]); },
-        [&](uint32_t place, int j) {
-          if (place < kPickList) s.list[place][0] = entry_of(z[j], ids[j]);
-        });
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) mine += z[j] >= cut;
+    uint32_t place = reserve(s.n_list, mine);
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j)
+      if (z[j] >= cut && place < kPickList) s.list[place++][0] = entry_of(z[j], ids[j]);
   }
   __syncthreads();
   const uint32_t n = uniform(s.n_list);
@@ -685,7 +709,8 @@ __device__ __forceinline__ bool pick_from_list(const SampleArgs& a, const Row<T>
                                                PickShared& s, int n, bool complete, float soft) {
   const int t = threadIdx.x;
   const Settings& st = row.st;
-  if (st.top_k > n && !complete) return false;
+  const bool open = !complete && !(st.top_k > 0 && st.top_k <= n);  // what limits it may lie behind
+  if (open && st.few()) return false;
   const bool active = t < n;
   const uint64_t entry = active ? s.list[t][0] : 0;
   const double x = active ? row.w(key_logit(entry_key(entry))) : 0.0;
@@ -697,9 +722,8 @@ __device__ __forceinline__ bool pick_from_list(const SampleArgs& a, const Row<T>
   if (active && x < st.min_p) s.past_min_p = 1;
   const uint64_t of_list = block_reduce<kPickWaves>(mass, s.slots64, Add{});
   uint64_t all = complete ? of_list : row.whole_sum;
-  // where nothing behind the list can be kept
-  if (!complete && st.top_k == 0 && !(st.top_p < 1.f && of_list >= share_of(all, st.top_p)) &&
-      !uniform(s.past_min_p))
+  // unless nothing behind the list can be kept
+  if (open && !(st.top_p < 1.f && of_list >= share_of(all, st.top_p)) && !uniform(s.past_min_p))
     return false;
   uint64_t before = 0;
   int place = 0;
@@ -725,14 +749,19 @@ __device__ __forceinline__ bool pick_from_list(const SampleArgs& a, const Row<T>
   const int keep = st.top_k > 0 ? min(st.top_k, n) : n;
   bool kept = active && place < keep && x >= st.min_p;
   if (st.top_p < 1.f) {
-    if (st.top_k > 0) {
+    if (st.top_k > 0 && !open) {
       if (active && place == keep - 1) s.sum_of_k = before + mass;
       __syncthreads();
       all = uniform(s.sum_of_k);
     }
+    // (of a top-k behind the list: its ids weigh no less than the list and no more than all)
+    if (st.top_k > 0 && open && kept && before < share_of(all, st.top_p) &&
+        before >= share_of(of_list, st.top_p))
+      s.unsure = 1;
     kept &= before < share_of(all, st.top_p);
   }
   __syncthreads();  // the walks are over
+  if (uniform(s.unsure)) return false;
   if (active && !kept) s.list[t][1] = 0;
   __syncthreads();
   if (wave_index() * 64 >= n) return true;
@@ -760,7 +789,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
   row.st = settings(a, find_sequence(a.cu_block, a.batch, row.r, lane));
   if (t < 64) s.pow64[t] = kPow64[t];
   s.bins[t] = 0;
-  if (t == 0) s.n_list = s.n_groups = s.past_min_p = 0;
+  if (t == 0) s.n_list = s.n_groups = s.past_min_p = s.unsure = 0;
   float hi = -INFINITY, lo = INFINITY;
   bool bad = false;
   segments.each([&](const SegmentStats& x) {
@@ -848,9 +877,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
     const bool hopeless = row.st.min_p <= 0.f && row.vocab > kPickList &&
                           static_cast<double>(share_of(row.whole_sum, fminf(row.st.top_p, 0x1.fffffep-1f))) >
                               kPickList * row.scale;
-    if (row.st.few() || (row.st.top_k == 0 && !hopeless)) {
+    if (row.st.few() || ((row.st.top_p < 1.f || row.st.min_p > 0.f) && !hopeless)) {
       bool complete;
-      const int n = gather(row, tops, s, row.st.few() ? row.st.top_k : kNucleus, complete);
+      const int n = gather(row, tops, s, row.st.few() ? row.st.top_k : kNucleus, row.st.few(),
+                           complete);
       done = n > 0 && pick_from_list(a, row, s, n, complete, soft);
     }
     if (t == 0) {
@@ -915,20 +945,29 @@ __device__ __forceinline__ void visit(const Row<T>& row, int first, int end, Wan
   }
 }
 
-// Bins of equal width from a row's largest logit down, the last one for all that lies lower; a higher
-// logit never has a higher bin.
+// Bins from a row's largest logit down; a higher logit never has a higher bin.  They are of equal width
+// down to what weighs e^-64 of the largest, and the last one holds all that lies lower; but with a
+// top-k, which counts that too, half of them are laid over it.
 struct Bins {
-  float half_top, per;
+  static constexpr int kLower = kBins / 2 - 1;
+  float half_top, per, half_from, per_lower, upper;
   template <class T>
   __device__ __forceinline__ explicit Bins(const Row<T>& row) {
-    // (what weighs less than e^-64 of the largest needs no bin of its own; halves: no overflow)
+    // (halves: no overflow)
     const float from = fmaxf(row.low, row.top - 64.f * row.st.temperature);
+    const bool split = row.st.top_k > 0 && from > row.low;
+    upper = split ? kBins - 1 - kLower : kBins - 1;
     half_top = 0.5f * row.top;
-    per = (kBins - 1) / (half_top - 0.5f * from);
+    half_from = 0.5f * from;
+    per = upper / (half_top - half_from);
+    per_lower = split ? kLower / (half_from - 0.5f * row.low) : 0.f;
   }
   __device__ __forceinline__ bool usable() const { return per < FLT_MAX; }
   __device__ __forceinline__ int operator()(float z) const {
-    return static_cast<int>(fminf((half_top - 0.5f * z) * per, kBins - 1.f));
+    const float x = fminf((half_top - 0.5f * z) * per, upper);
+    // (a NaN, of 0 times infinity, becomes 0)
+    const float y = fminf(fmaxf((half_from - 0.5f * z) * per_lower, 0.f), kLower);
+    return static_cast<int>(x + y);
   }
 };
 
@@ -957,7 +996,7 @@ __device__ __forceinline__ int part_begin(int part, int parts, int segments) {
 
 template <class T>
 __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a, Workspace ws) {
-  __shared__ uint32_t count[kBins], mass[kBins];
+  __shared__ uint32_t count[kBins], mass[kBins + 64];
   const int t = threadIdx.x, r = blockIdx.x / ws.parts, part = blockIdx.x - r * ws.parts;
   Row<T> row;
   if (!row.reopen(a, ws, r, nullptr) || !in_parts(row)) return;
@@ -978,8 +1017,11 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
         if (!(z > -INFINITY)) return;
         const int b = bin(z);
         if (by_count) atomicAdd(&count[b], 1u);
-        if (by_mass)
-          atomicAdd(&mass[b], static_cast<uint32_t>(fast_exp2((z - top) * rate + unit) + 0.5f));
+        if (by_mass) {
+          // (most of a sure row's are 0, and in one bin: these go to a place of the lane's own)
+          const uint32_t m = static_cast<uint32_t>(fast_exp2((z - top) * rate + unit) + 0.5f);
+          atomicAdd(&mass[m ? b : kBins + (t & 63)], m);
+        }
       },
       [](int) {});
   __syncthreads();

@@ -22,6 +22,20 @@ __device__ __forceinline__ V uniform(V x) {
   }
 }
 
+// x of lane l, which is the same on every lane, as a scalar.
+template <class V>
+__device__ __forceinline__ V of_lane(V x, int l) {
+  static_assert(sizeof(V) == 4 || sizeof(V) == 8, "one or two words");
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int32_t, x), l));
+  } else {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(b), l);
+    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(b >> 32), l);
+    return __builtin_bit_cast(V, static_cast<uint64_t>(hi) << 32 | lo);
+  }
+}
+
 // x of another lane by DPP, word by word; `old` where no lane is there or the row is masked out.
 template <int kCtrl, int kRows = 0xf, class V>
 __device__ __forceinline__ V dpp(V old, V x) {

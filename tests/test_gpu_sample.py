@@ -602,6 +602,40 @@ def test_extreme_temperatures(V, dtype):
             np.testing.assert_array_equal(got[0], want[0])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [2500, 126464])
+def test_sure_rows(V, dtype):
+    """One logit, or a few, far above all others, alone and with the type's lowest value far below them: each
+    setting, small and large top-k among them."""
+    rng = np.random.default_rng(26)
+    z = _logits(8, V, 26, "plain")
+    low = float(torch.finfo(TYPES[dtype]).min)
+    z[:4, V // 3] = 128.0
+    z[2:6, rng.choice(V, 5, replace=False)] += np.array([60.0, 30.0, 25.0, 15.0, 14.5])
+    z[1, V // 2:], z[3, ::2], z[5, 40:] = low, low, -np.inf
+    z[6, :V // 3] = low
+    u = rng.random(8)
+    u[4] = 1 - 2.0 ** -24
+    with np.errstate(over="ignore", invalid="ignore"):
+        for settings in SETTINGS + [dict(top_k=k, top_p=p, min_p=m) for k in (2, 40, 128, 129, 200, 256, 257, V - 2)
+                                    for p, m in ((1.0, 0.0), (0.9, 0.0), (1.0, 1e-3), (0.999, 1e-12))]:
+            Draw(z, u, dtype=dtype, **settings).check()
+
+
+def test_nucleus_inside_a_longer_top_k():
+    """A top-p whose share of the first top_k ids' weight ends near a step of the sums: the rows for which
+    the list tells, and those for which the sum over all top_k ids has to be known."""
+    V = 9000
+    w = np.concatenate([2.0 ** -np.arange(12), np.full(V - 12, 2.0 ** -20)])
+    rng = np.random.default_rng(27)
+    order = rng.permutation(V)
+    z = np.full((40, V), 0.0)
+    z[:, order] = np.log(w)
+    p = np.concatenate([np.linspace(0.5, 0.999, 20), 0.995 + np.arange(20) * 2.0 ** -12])
+    Draw(z, rng.random(40), top_p=p, top_k=[300 + 200 * (i % 30) for i in range(40)],
+         min_p=[0, 2.0 ** -19] * 20).check()
+
+
 def test_more_rows_than_parts():
     """So many rows that each is one part; and counts at which a row's parts change."""
     V = 34000
