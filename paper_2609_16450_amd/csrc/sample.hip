@@ -594,8 +594,9 @@ __device__ __forceinline__ uint32_t reserve(uint32_t& length, uint32_t mine) {
 // `want` of them.  Otherwise about as many, less where the rest weighs less than e^-48 of the largest.
 // Returns their number, or -1 where they are more than kPickList.
 //
-// (What a row costs here is its code, which every launch fetches anew: about 0.6 us per 1000 bytes.  So
-// there is one comparison to an item, with a logit, once that has been found.)
+// (Much of what a row costs here is the fetching of its code: with a bin and a branch to each item, 41 KB
+// in the kernel, 16.0 us for 32 rows; with one comparison, with the lowest logit that is taken, 31 KB and
+// 12.4 us.)
 template <class T>
 __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, PickShared& s,
                                       uint32_t want, bool by_count, bool& complete) {
@@ -1032,14 +1033,14 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
   }
 }
 
-// The bin in which the running sum of x (kBins / kPartThreads bins a thread) reaches `target`, with the
-// sum before it; kBins where none does.
-struct FoundBin {
-  int bin;
+// The bins in which the running sum of x (kBins / kPartThreads bins a thread) reaches a first and a second
+// target, kBins where none does, with the sum before the first of them.
+struct FoundBins {
+  int first, second;
   uint64_t before;
 };
-__device__ __forceinline__ FoundBin find_bin(const uint32_t* x, uint64_t target, uint64_t* slots,
-                                             FoundBin* found) {
+__device__ __forceinline__ FoundBins find_bins(const uint32_t* x, uint64_t first, uint64_t second,
+                                               uint64_t* slots, FoundBins* found) {
   constexpr int kEach = kBins / kPartThreads;
   const int t = threadIdx.x;
   uint32_t v[kEach];
@@ -1050,24 +1051,26 @@ __device__ __forceinline__ FoundBin find_bin(const uint32_t* x, uint64_t target,
     mine += v[e];
   }
   __syncthreads();  // (what an earlier call has found has been read)
-  if (t == 0) *found = FoundBin{kBins, 0};
+  if (t == 0) *found = FoundBins{kBins, kBins, 0};
   uint64_t run = block_scan<kPartWaves>(mine, slots, total);
-  if (run < target && run + mine >= target) {
+  if ((run < first && run + mine >= first) || (run < second && run + mine >= second)) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      if (run < target && run + v[e] >= target) *found = FoundBin{t * kEach + e, run};
-      run += v[e];
+      const uint64_t upto = run + v[e];
+      if (run < first && upto >= first) found->first = t * kEach + e, found->before = run;
+      if (run < second && upto >= second) found->second = t * kEach + e;
+      run = upto;
     }
   }
   __syncthreads();
-  return FoundBin{uniform(found->bin), uniform(found->before)};
+  return FoundBins{uniform(found->first), uniform(found->second), uniform(found->before)};
 }
 
 template <class T>
 __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a, Workspace ws) {
   __shared__ double pow64[64];
   __shared__ uint64_t slots64[kPartWaves];
-  __shared__ FoundBin found;
+  __shared__ FoundBins found;
   const int t = threadIdx.x, r = blockIdx.x / ws.parts, part = blockIdx.x - r * ws.parts;
   Row<T> row;
   if (!row.reopen(a, ws, r, pow64) || !in_parts(row)) return;
@@ -1081,22 +1084,31 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
   // (hardly ever two), and, where it is a part of the first top_k ids' weight, for all that this may be.
   int bin_k = kBins, bin_m = kBins, p_first = kBins, p_last = kBins;
   uint64_t before_k = 0;
-  if (st.top_k > 0) {
-    const FoundBin f = find_bin(state.count, static_cast<uint64_t>(st.top_k), slots64, &found);
-    bin_k = f.bin;
-    before_k = f.before;
-  }
-  if (st.top_p < 1.f) {
-    uint64_t least = row.whole_sum >> 31, most = least;  // weight that top_p takes its part of
-    if (bin_k < kBins) {  // the bins up to bin_k, without it and with it
-      uint64_t x = 0;
-      for (int i = t; i < bin_k; i += kPartThreads) x += state.mass[i];
-      least = block_reduce<kPartWaves>(x, slots64, Add{});
-      most = least + state.mass[bin_k];
+#pragma unroll 1
+  for (int by_mass = 0; by_mass < 2; ++by_mass) {
+    if (by_mass ? st.top_p >= 1.f : st.top_k == 0) continue;
+    uint64_t low = static_cast<uint64_t>(st.top_k), high = low;
+    if (by_mass) {
+      uint64_t least = row.whole_sum >> 31, most = least;  // weight that top_p takes its part of
+      if (bin_k < kBins) {  // the bins up to bin_k, without it and with it
+        uint64_t x = 0;
+        for (int i = t; i < bin_k; i += kPartThreads) x += state.mass[i];
+        least = block_reduce<kPartWaves>(x, slots64, Add{});
+        most = least + state.mass[bin_k];
+      }
+      const uint64_t slack = (most >> 18) + 1;
+      low = share_of(least, st.top_p);
+      low = low > slack ? low - slack : 1;
+      high = share_of(most, st.top_p) + slack;
     }
-    const uint64_t slack = (most >> 18) + 1, low = share_of(least, st.top_p);
-    p_first = find_bin(state.mass, low > slack ? low - slack : 1, slots64, &found).bin;
-    p_last = find_bin(state.mass, share_of(most, st.top_p) + slack, slots64, &found).bin;
+    const FoundBins f = find_bins(by_mass ? state.mass : state.count, low, high, slots64, &found);
+    if (by_mass) {
+      p_first = f.first;
+      p_last = f.second;
+    } else {
+      bin_k = f.first;
+      before_k = f.before;
+    }
   }
   if (st.min_p > 0.f) bin_m = bin(min_p_logit(row));
   const int first = min(min(bin_k, p_first), bin_m), last = min(min(bin_k, p_last), bin_m);
@@ -1116,10 +1128,6 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
       state.before_k = static_cast<uint32_t>(before_k);
     }
   }
-  auto append = [&](int which, float z, int id) {
-    const uint32_t j = atomicAdd(&state.n_list[which], 1u);
-    if (j < kList) state.list[which][j] = entry_of(z, id);
-  };
   double sum = 0.0, sum_between = 0.0;
   visit<kPartWaves>(
       row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
@@ -1132,12 +1140,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
         if (b > end || !(z > -INFINITY)) return;
         if (b < first) {
           sum += row.w.normal(z);
-        } else if (b <= last) {
-          append(0, z, id);
-        } else if (b < bin_k) {
+        } else if (b > last && b < bin_k) {
           sum_between += row.w.normal(z);
         } else {
-          append(1, z, id);
+          const int which = b <= last ? 0 : 1;
+          const uint32_t j = atomicAdd(&state.n_list[which], 1u);
+          if (j < kList) state.list[which][j] = entry_of(z, id);
         }
       },
       [&](int g) {
