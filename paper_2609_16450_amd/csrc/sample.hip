@@ -15,12 +15,11 @@
 // sample_pick_kernel, a workgroup per row, cuts and draws from these alone where that can be done: with
 // a temperature only it reads the one segment that the draw falls into; with a small top-k, or where
 // the nucleus is small, the groups that can hold what is kept (their largest logits say which), at
-// most kPickList ids in LDS.  The rows left over are read again.  Of a large vocabulary,
-// sample_bins_kernel makes a histogram which finds the few bins that the cut lies in, and
+// most kPickList ids in LDS.  The rows left over are read again: sample_bins_kernel makes a histogram which finds the few bins that the cut lies in, and
 // sample_sums_kernel the exact sums above them and a list of the ids within, many workgroups to a row;
-// sample_search_kernel, one workgroup to a row, orders the list, cuts and draws.  Rows of a smaller
-// vocabulary, and those whose bins hold more ids than the list (logits that tie, or a few that lie
-// far off the others), it cuts by itself, the key found bit by bit.
+// sample_search_kernel, one workgroup to a row, orders the list, cuts and draws.  Rows whose bins hold
+// more ids than the list (logits that tie, or a few that lie far off the others) it cuts by itself, the
+// key found bit by bit.
 //
 // Bounds: many rows are bound by reading the logits, once in the scan (944 fp32 rows of 126464, mixed
 // settings: 110 us, 4.3 TB/s), and once or twice more where they are left over; few rows by one
@@ -51,7 +50,6 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kMaxSegments = kThreads;
 constexpr int kList = kThreads;  // ids that it sorts in LDS
 constexpr int kBins = 2048;
-constexpr int kSearchVocab = 32768;  // rows of more ids are searched by many workgroups
 static_assert(kMaxSegments * kSegment >= kSampleMaxVocab, "a thread per segment");
 
 typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));  // at any 2 bytes
@@ -208,7 +206,11 @@ struct Settings {
   float temperature, top_p, min_p;
   int32_t top_k;  // 0: no limit
   __device__ __forceinline__ bool greedy() const { return !(temperature > 0.f); }
-  __device__ __forceinline__ bool few() const { return top_k > 0 && top_k <= kFewIds; }
+  // (the top_k largest of n groups let at most about -n ln(1 - top_k / n) ids through, 214 of 128 groups)
+  __device__ __forceinline__ bool few(int vocab) const {
+    const int groups = (vocab + kSegment - 1) / kSegment * 64;
+    return top_k > 0 && top_k <= kFewIds && (vocab <= kPickList || 16 * top_k <= 13 * groups);
+  }
   __device__ __forceinline__ bool limited() const {
     return top_k > 0 || top_p < 1.f || min_p > 0.f;
   }
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(SampleArgs a,
   SegmentStats out{bad ? NAN : top, low, 0.f, 0.f, 0.0};
   if (top > -INFINITY && !bad) {  // (else every difference would be NaN)
     // rows of few ids by count, and greedy ones, take no sum over all
-    const bool sum = !st.greedy() && !st.few();
+    const bool sum = !st.greedy() && !st.few(a.vocab);
     if (sum) {
       const Weights w{pow64, static_cast<double>(top), weight_rate(st.temperature)};
 #pragma unroll
@@ -711,7 +713,7 @@ __device__ __forceinline__ bool pick_from_list(const SampleArgs& a, const Row<T>
   const int t = threadIdx.x;
   const Settings& st = row.st;
   const bool open = !complete && !(st.top_k > 0 && st.top_k <= n);  // what limits it may lie behind
-  if (open && st.few()) return false;
+  if (open && st.few(row.vocab)) return false;
   const bool active = t < n;
   const uint64_t entry = active ? s.list[t][0] : 0;
   const double x = active ? row.w(key_logit(entry_key(entry))) : 0.0;
@@ -867,7 +869,8 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
     return;
   }
   if constexpr (kLimits) {
-    if (row.st.few()) {
+    const bool few = row.st.few(row.vocab);
+    if (few) {
       row.scale = 0x1p52;  // (at most kPickList weights of at most 1 are summed)
       row.whole_sum = 0;
     } else {
@@ -878,10 +881,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
     const bool hopeless = row.st.min_p <= 0.f && row.vocab > kPickList &&
                           static_cast<double>(share_of(row.whole_sum, fminf(row.st.top_p, 0x1.fffffep-1f))) >
                               kPickList * row.scale;
-    if (row.st.few() || ((row.st.top_p < 1.f || row.st.min_p > 0.f) && !hopeless)) {
+    if (few || ((row.st.top_p < 1.f || row.st.min_p > 0.f) && !hopeless)) {
       bool complete;
-      const int n = gather(row, tops, s, row.st.few() ? row.st.top_k : kNucleus, row.st.few(),
-                           complete);
+      const int n = gather(row, tops, s, few ? row.st.top_k : kNucleus, few, complete);
       done = n > 0 && pick_from_list(a, row, s, n, complete, soft);
     }
     if (t == 0) {
@@ -890,7 +892,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
       else
         header = RowHeader{row.scale, row.whole_sum, row.top, row.low, row.st, 1, 0};
     }
-    if (!done && row.vocab > kSearchVocab) {  // (all but the lists)
+    if (!done) {  // (all but the lists)
       u32x4* const state = reinterpret_cast<u32x4*>(&ws.states[row.r]);
       for (int i = t; i < static_cast<int>(offsetof(SearchState, list) / 16); i += kPickThreads)
         state[i] = u32x4{};
@@ -899,11 +901,12 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
 }
 
 // ---------------------------------------------------------------------------------------
-// The rows that the second launch has left: cuts anywhere.  Of more than kSearchVocab ids, three
-// launches: a histogram of a row by its parts' workgroups, which tells the bin that the cut lies in;
-// the exact sums above the bin, segment by segment, with the bin's ids put into a list, by
-// workgroups again; and a workgroup that sorts the list, cuts and draws.  The last one alone also does
-// rows of fewer ids, and those that the others have not found the cut of.
+// The rows that the second launch has left: cuts anywhere.  Three launches: a histogram of a row by its
+// parts' workgroups, which tells the bin that the cut lies in; the exact sums above the bin, segment by
+// segment, with the bin's ids put into a list, by workgroups again; and a workgroup that orders the list,
+// cuts and draws.  The last one alone also does the rows that the others have not found the cut of.
+// (That workgroup alone for rows of up to 32768 ids: 40 -> 48 us for a row of 9000, 588 -> 970 us for 4096
+// rows of 32000, wide nuclei.)
 // ---------------------------------------------------------------------------------------
 constexpr int kPartThreads = 256;
 constexpr int kPartWaves = kPartThreads / 64;
@@ -988,7 +991,7 @@ __device__ __forceinline__ float min_p_logit(const Row<T>& row) {
 // Whether the launches over parts have to do with a row (of those left).
 template <class T>
 __device__ __forceinline__ bool in_parts(const Row<T>& row) {
-  return row.vocab > kSearchVocab && !row.st.few() && Bins(row).usable();
+  return !row.st.few(row.vocab) && Bins(row).usable();
 }
 
 __device__ __forceinline__ int part_begin(int part, int parts, int segments) {
@@ -1451,7 +1454,7 @@ __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, W
   Cut cut = kKeepAll;
   if (!in_parts(row) ||
       !p.cut_from_lists(ws.states[r], ws.kept + static_cast<size_t>(r) * ws.segments, cut)) {
-    if (st.few()) {  // (for which the first launch forms no sums)
+    if (st.few(row.vocab)) {  // (for which the first launch forms no sums)
       double x = 0.0;
       visit<kWaves>(
           row, 0, row.segments, [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
@@ -1494,7 +1497,7 @@ struct Layout {
     headers = tops + up(n * segments * 64 * sizeof(float));
     kept = headers + up(n * sizeof(RowHeader));
     states = bytes = kept;
-    if (vocab > kSearchVocab) {
+    if (vocab > kPickList) {
       states = kept + up(n * segments * sizeof(uint64_t));
       bytes = states + n * sizeof(SearchState);
     }
@@ -1527,12 +1530,10 @@ hipError_t launch(const SampleArgs& a, void* ws, hipStream_t s) {
   hipLaunchKernelGGL(pick, dim3(a.n_rows), dim3(kPickThreads), 0, s, a, w);
   // rows are left only where something limits them and the list does not hold them whole
   if (limits && a.vocab > kPickList) {
-    if (a.vocab > kSearchVocab) {
-      const dim3 grid(a.n_rows * w.parts);
-      if (a.top_k || a.top_p)
-        hipLaunchKernelGGL(sample_bins_kernel<T>, grid, dim3(kPartThreads), 0, s, a, w);
-      hipLaunchKernelGGL(sample_sums_kernel<T>, grid, dim3(kPartThreads), 0, s, a, w);
-    }
+    const dim3 grid(a.n_rows * w.parts);
+    if (a.top_k || a.top_p)
+      hipLaunchKernelGGL(sample_bins_kernel<T>, grid, dim3(kPartThreads), 0, s, a, w);
+    hipLaunchKernelGGL(sample_sums_kernel<T>, grid, dim3(kPartThreads), 0, s, a, w);
     hipLaunchKernelGGL(sample_search_kernel<T>, dim3(a.n_rows), dim3(kThreads), 0, s, a, w);
   }
   return hipGetLastError();
