@@ -10,7 +10,9 @@
 // registers before a single cross-half exchange.
 //
 // The same kernels also write the logits (LmOut::kLogits, eb_lmhead_logits): another epilogue on the
-// same accumulators, so a written logit has the bits that the statistics see.
+// same accumulators, so a written logit has the bits that the statistics see.  32 rows of 126464 x 4096:
+// 178 us (statistics 176), bound by W; 1024 rows: 807 us (753), bound by the MFMAs, and what comes on
+// top is the stores of 518 MB.
 #include <type_traits>
 
 #include "attn_small.hpp"
@@ -983,7 +985,9 @@ hipError_t launch_tile_tn(int n_rows, int hidden, int vocab, const void* h, cons
   const int n_vtiles = tile_vtiles(vocab);
   const int n_rtiles = (n_rows + 32 * TN - 1) / (32 * TN);
   const int n_tiles = n_vtiles * n_rtiles;
-  // (a multiple of kXcds: every XCD's segment of the launch sequence has its workgroups)
+  // (a multiple of kXcds: every XCD's segment of the launch sequence has its workgroups.  With fewer
+  // tiles than compute units and workgroup g at tile g, as before: 47 us for the logits of 201 rows of
+  // 32003 x 2048, W in the cache in front of HBM; 33 us with the segments)
   const int groups = min(kTileGroups, (n_tiles + kXcds - 1) / kXcds * kXcds);
   hipLaunchKernelGGL((lmhead_tile_kernel<TN, kOut>), dim3(groups), dim3(256), 0, s,
                      static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(w), n_rows,
