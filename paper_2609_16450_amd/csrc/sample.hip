@@ -236,15 +236,18 @@ struct RowHeader {
 static_assert(sizeof(RowHeader) == 48, "packed");
 
 // What the launches that search a row leave one another; zeroed by the second launch.
-struct SearchState {
-  uint32_t count[kBins], mass[kBins];  // ids and weights (of 2^-31 of their sum) per bin
-  uint64_t between;                    // weight between `last` and bin_k
+struct Border {
+  uint64_t between;  // weight between `last` and bin_k
   uint32_t n_list[2];
   int32_t first, last;              // bins of the cut
   int32_t bin_k, bin_m;             // top-k's and min-p's (kBins: no limit)
   uint32_t before_first, before_k;  // ids in the bins before `first` and before bin_k, with a top-k
+};
+struct SearchState {
+  uint32_t count[kBins], mass[kBins];  // ids and weights (of 2^-31 of their sum) per bin
+  Border border;
   uint64_t pad;
-  uint64_t list[2][kList];          // ids of bins first .. last, of bin_k where that lies behind them
+  uint64_t list[2][kList];  // ids of bins first .. last, of bin_k where that lies behind them
 };
 static_assert(sizeof(SearchState) % 16 == 0, "whole 16-byte words");
 
@@ -1074,10 +1077,13 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
   __shared__ double pow64[64];
   __shared__ uint64_t slots64[kPartWaves];
   __shared__ FoundBins found;
+  __shared__ uint64_t list[2][kList];
+  __shared__ uint32_t n_list[2], list_at[2];
   const int t = threadIdx.x, r = blockIdx.x / ws.parts, part = blockIdx.x - r * ws.parts;
   Row<T> row;
   if (!row.reopen(a, ws, r, pow64) || !in_parts(row)) return;
   if (t < 64) pow64[t] = kPow64[t];
+  if (t < 2) n_list[t] = 0;
   __syncthreads();
   const Settings& st = row.st;
   const Bins bin(row);
@@ -1123,12 +1129,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
       for (int i = t; i < min(first, kBins); i += kPartThreads) x += state.count[i];
     x = block_reduce<kPartWaves>(x, slots64, Add{});
     if (t == 0) {
-      state.first = first;
-      state.last = last;
-      state.bin_k = bin_k;
-      state.bin_m = bin_m;
-      state.before_first = static_cast<uint32_t>(x);
-      state.before_k = static_cast<uint32_t>(before_k);
+      state.border.first = first;
+      state.border.last = last;
+      state.border.bin_k = bin_k;
+      state.border.bin_m = bin_m;
+      state.border.before_first = static_cast<uint32_t>(x);
+      state.border.before_k = static_cast<uint32_t>(before_k);
     }
   }
   double sum = 0.0, sum_between = 0.0;
@@ -1147,8 +1153,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
           sum_between += row.w.normal(z);
         } else {
           const int which = b <= last ? 0 : 1;
-          const uint32_t j = atomicAdd(&state.n_list[which], 1u);
-          if (j < kList) state.list[which][j] = entry_of(z, id);
+          const uint32_t j = atomicAdd(&n_list[which], 1u);
+          if (j < kList) list[which][j] = entry_of(z, id);
         }
       },
       [&](int g) {
@@ -1157,10 +1163,18 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
           ws.kept[static_cast<size_t>(r) * ws.segments + g] = whole(sum, row.scale);
         sum = 0.0;
       });
+  // The listed ids by one reservation a workgroup.  (An atomic on the state for each took a wave 4 us.)
+  __syncthreads();
+  if (t < 2 && n_list[t]) list_at[t] = atomicAdd(&state.border.n_list[t], n_list[t]);
+  __syncthreads();
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+    for (uint32_t j = t; j < min(n_list[which], uint32_t{kList}); j += kPartThreads)
+      if (list_at[which] + j < kList) state.list[which][list_at[which] + j] = list[which][j];
   if (between) {
     sum_between = wave_reduce(sum_between, Add{});
     if ((t & 63) == 0)
-      atomicAdd(reinterpret_cast<unsigned long long*>(&state.between),
+      atomicAdd(reinterpret_cast<unsigned long long*>(&state.border.between),
                 static_cast<unsigned long long>(whole(sum_between, row.scale)));
   }
 }
@@ -1247,13 +1261,13 @@ struct Searcher {
   // The entries are first put into bins, whose numbers and sums of weights come by
   // atomics; within a bin, mostly of one to three, each walks over the others.  (Sorting up to 1024
   // entries across 16 waves took 4 us more.)
-  __device__ __forceinline__ Listed listed(const SearchState& state, int which) const {
+  __device__ __forceinline__ Listed listed(uint32_t n, uint64_t entry) const {
     constexpr int kListBins = kThreads;
     const int t = threadIdx.x;
     Listed l;
-    l.n = static_cast<int>(uniform(state.n_list[which]));
+    l.n = static_cast<int>(uniform(n));
     const bool active = t < l.n;
-    l.entry = active ? state.list[which][t] : 0;
+    l.entry = active ? entry : 0;
     l.x = active ? row.w(key_logit(entry_key(l.entry))) : 0.0;
     l.mass = whole(l.x, row.scale);
     // entries as consecutive numbers as far as they go: keys from the list's lowest on (of bf16 logits
@@ -1308,15 +1322,17 @@ struct Searcher {
 
   // The cut from what the launches over parts have found, with the kept ids' sums in s.segment; false
   // where a list has run over, or a rounding of the histogram has led to a bin without the cut.
-  __device__ __forceinline__ bool cut_from_lists(const SearchState& state, const uint64_t* kept_sums,
+  // first_list, kept_sum: this thread's entry of the state's first list and segment's sum above the bins.
+  __device__ __forceinline__ bool cut_from_lists(const Border& border, uint64_t first_list,
+                                                 const uint64_t* second_list, uint64_t kept_sum,
                                                  Cut& cut) const {
     const int t = threadIdx.x;
     const Settings& st = row.st;
-    const int last = uniform(state.last), bin_k = uniform(state.bin_k);
-    if (last >= kBins || uniform(state.n_list[0]) > kList || uniform(state.n_list[1]) > kList)
+    const int last = uniform(border.last), bin_k = uniform(border.bin_k);
+    if (last >= kBins || uniform(border.n_list[0]) > kList || uniform(border.n_list[1]) > kList)
       return false;
-    for (int g = t; g < row.segments; g += kThreads) s.segment[g] = kept_sums[g];
-    const bool by_min_p = uniform(state.bin_m) == last;
+    if (t < row.segments) s.segment[t] = kept_sum;
+    const bool by_min_p = uniform(border.bin_m) == last;
     // the weight of a list's entries up to the top_k-th id
     auto up_to = [&](const Listed& l, uint32_t ids_before) {
       const uint32_t n = static_cast<uint32_t>(st.top_k) - uniform(ids_before);
@@ -1326,21 +1342,21 @@ struct Searcher {
     };
     uint64_t of_k = 0;
     if (st.top_p < 1.f && bin_k < kBins && bin_k > last) {
-      const Listed l = listed(state, 1);
-      of_k = up_to(l, state.before_k) + uniform(state.between);
+      const Listed l = listed(border.n_list[1], second_list[t]);
+      of_k = up_to(l, border.before_k) + uniform(border.between);
       __syncthreads();
     }
-    const Listed l = listed(state, 0);
+    const Listed l = listed(border.n_list[0], first_list);
     const uint64_t above = sum_of_segments();
     bool kept = l.entry != 0, closed = false;
     if (bin_k == last) {
-      kept &= l.place < static_cast<uint32_t>(st.top_k) - uniform(state.before_first);
+      kept &= l.place < static_cast<uint32_t>(st.top_k) - uniform(border.before_first);
       closed = true;
     }
     if (st.top_p < 1.f) {
       uint64_t all = row.whole_sum;
       if (bin_k == last)
-        all = above + up_to(l, state.before_first);
+        all = above + up_to(l, border.before_first);
       else if (bin_k < kBins)
         all = above + l.total + of_k;
       const uint64_t target = share_of(all, st.top_p);
@@ -1446,6 +1462,12 @@ __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, W
   __shared__ Shared s;
   const int t = threadIdx.x, r = blockIdx.x;
   Row<T> row;
+  // (read before it is known whether the row is left over: no waiting for one load after another)
+  const SearchState& state = ws.states[r];
+  const Border border = state.border;
+  const uint64_t first_list = state.list[0][t];
+  const uint64_t kept_sum =
+      t < ws.segments ? ws.kept[static_cast<size_t>(r) * ws.segments + t] : uint64_t{0};
   if (!row.reopen(a, ws, r, s.pow64)) return;
   if (t < 64) s.pow64[t] = kPow64[t];
   __syncthreads();
@@ -1453,7 +1475,7 @@ __global__ __launch_bounds__(kThreads) void sample_search_kernel(SampleArgs a, W
   const Searcher<T> p{row, s};
   Cut cut = kKeepAll;
   if (!in_parts(row) ||
-      !p.cut_from_lists(ws.states[r], ws.kept + static_cast<size_t>(r) * ws.segments, cut)) {
+      !p.cut_from_lists(border, first_list, state.list[1], kept_sum, cut)) {
     if (st.few(row.vocab)) {  // (for which the first launch forms no sums)
       double x = 0.0;
       visit<kWaves>(
