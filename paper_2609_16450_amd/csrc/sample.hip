@@ -271,6 +271,12 @@ struct Max {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
   __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); }
 };
+struct MaxOfBoth {  // of the two halves, each by itself
+  __device__ __forceinline__ uint64_t operator()(uint64_t a, uint64_t b) const {
+    const uint32_t hi = max(static_cast<uint32_t>(a >> 32), static_cast<uint32_t>(b >> 32));
+    return static_cast<uint64_t>(hi) << 32 | max(static_cast<uint32_t>(a), static_cast<uint32_t>(b));
+  }
+};
 struct Min {
   __device__ __forceinline__ uint64_t operator()(uint64_t a, uint64_t b) const { return min(a, b); }
   __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); }
@@ -913,6 +919,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
 // ---------------------------------------------------------------------------------------
 constexpr int kPartThreads = 256;
 constexpr int kPartWaves = kPartThreads / 64;
+// The histogram's workgroups do two parts each: what few rows wait for is its atomics on the row's state
+// (4 waves: 14.6 us for 32 rows, 8: 11.0, 16: 10.2; but of 944 rows in all 199, 196 and 197 us).
+constexpr int kBinThreads = 2 * kPartThreads;
+__host__ __device__ constexpr int bin_parts(int parts) { return (parts + 1) / 2; }
 
 // f(z, id) for every id that this lane holds of segments first + wave, first + wave + kN, .. below
 // `end` for which wanted(g); then each_segment(g) (by the whole wave) for these and the others.
@@ -1002,12 +1012,13 @@ __device__ __forceinline__ int part_begin(int part, int parts, int segments) {
 }
 
 template <class T>
-__global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a, Workspace ws) {
+__global__ __launch_bounds__(kBinThreads) void sample_bins_kernel(SampleArgs a, Workspace ws) {
   __shared__ uint32_t count[kBins], mass[kBins + 64];
-  const int t = threadIdx.x, r = blockIdx.x / ws.parts, part = blockIdx.x - r * ws.parts;
+  const int parts = bin_parts(ws.parts);
+  const int t = threadIdx.x, r = blockIdx.x / parts, part = blockIdx.x - r * parts;
   Row<T> row;
   if (!row.reopen(a, ws, r, nullptr) || !in_parts(row)) return;
-  for (int i = t; i < kBins; i += kPartThreads) count[i] = mass[i] = 0;
+  for (int i = t; i < kBins; i += kBinThreads) count[i] = mass[i] = 0;
   const bool by_count = row.st.top_k > 0, by_mass = row.st.top_p < 1.f;
   if (!by_count && !by_mass) return;
   __syncthreads();
@@ -1017,8 +1028,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
   const float unit = static_cast<float>(ilogb(row.scale) - 31);
   const float top = row.top;
   const Bins bin(row);
-  visit<kPartWaves>(
-      row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
+  visit<kBinThreads / 64>(
+      row, part_begin(part, parts, ws.segments), part_begin(part + 1, parts, ws.segments),
       [&](int g) { return uniform(row.stats[g].top) > -INFINITY; },
       [&](float z, int) {
         if (!(z > -INFINITY)) return;
@@ -1033,7 +1044,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
       [](int) {});
   __syncthreads();
   SearchState& state = ws.states[r];
-  for (int i = t; i < kBins; i += kPartThreads) {
+  for (int i = t; i < kBins; i += kBinThreads) {
     if (by_count && count[i]) atomicAdd(&state.count[i], count[i]);
     if (by_mass && mass[i]) atomicAdd(&state.mass[i], mass[i]);
   }
@@ -1274,8 +1285,9 @@ struct Searcher {
     // their upper halves, so that equal ones are told apart by their ids), then the ids
     constexpr int kKeyShift = sizeof(T) == 2 ? 16 : 0;
     const uint32_t key = entry_key(l.entry) >> kKeyShift;
-    const uint32_t high = block_reduce<kWaves>(active ? key : 0, s.slots32, Max{});
-    const uint32_t low = block_reduce<kWaves>(active ? key : 0xffffffffu, s.slots32, Min{});
+    const uint64_t ends = block_reduce<kWaves>(
+        active ? static_cast<uint64_t>(key) << 32 | ~key : uint64_t{0}, s.slots64, MaxOfBoth{});
+    const uint32_t high = static_cast<uint32_t>(ends >> 32), low = ~static_cast<uint32_t>(ends);
     const int id_bits = 32 - __clz(row.vocab);
     const uint64_t range = (static_cast<uint64_t>(high - low) + 1) << id_bits;
     const int shift = max(0, 64 - __clzll(static_cast<long long>(range)) - 10);
@@ -1552,10 +1564,11 @@ hipError_t launch(const SampleArgs& a, void* ws, hipStream_t s) {
   hipLaunchKernelGGL(pick, dim3(a.n_rows), dim3(kPickThreads), 0, s, a, w);
   // rows are left only where something limits them and the list does not hold them whole
   if (limits && a.vocab > kPickList) {
-    const dim3 grid(a.n_rows * w.parts);
     if (a.top_k || a.top_p)
-      hipLaunchKernelGGL(sample_bins_kernel<T>, grid, dim3(kPartThreads), 0, s, a, w);
-    hipLaunchKernelGGL(sample_sums_kernel<T>, grid, dim3(kPartThreads), 0, s, a, w);
+      hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(a.n_rows * bin_parts(w.parts)), dim3(kBinThreads),
+                         0, s, a, w);
+    hipLaunchKernelGGL(sample_sums_kernel<T>, dim3(a.n_rows * w.parts), dim3(kPartThreads), 0, s, a,
+                       w);
     hipLaunchKernelGGL(sample_search_kernel<T>, dim3(a.n_rows), dim3(kThreads), 0, s, a, w);
   }
   return hipGetLastError();
