@@ -17,7 +17,7 @@
 namespace eb {
 namespace {
 
-constexpr int kThreads = 1024;  // sequences per round, and rows per workgroup and turn
+constexpr int kThreads = 1024;  // sequences per pass, and rows per workgroup and turn
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxGroups = 2048;
 
@@ -56,9 +56,9 @@ __device__ __forceinline__ void assign(const KvAssign& a, bool write_state) {
   const uint32_t tail = (head + free_pages) % n_pages;
   if (tid == 0) taken_pages = 0;
 
-  Sums before{0, 0, 0, 0};  // of the sequences of earlier rounds
+  Sums before{0, 0, 0, 0};  // of the sequences of earlier passes
   for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
-    const int b = b0 + tid, in_round = min(kThreads, a.batch - b0);
+    const int b = b0 + tid, in_pass = min(kThreads, a.batch - b0);
     Sums own{0, 0, 0, 0};
     int32_t cached = 0, held = 0, keep = 0;
     bool fits = true;
@@ -81,7 +81,7 @@ __device__ __forceinline__ void assign(const KvAssign& a, bool write_state) {
       }
     }
     Sums sum = wave_scan(own);  // then over the waves before
-    __syncthreads();  // the round before is done with its arrays
+    __syncthreads();  // the pass before is done with its arrays
     if (lane == 63) wave_sum[wave] = sum;
     __syncthreads();
     Sums total = before;
@@ -108,12 +108,12 @@ __device__ __forceinline__ void assign(const KvAssign& a, bool write_state) {
     __syncthreads();
     if constexpr (!kStateOnly) {
       const uint32_t stride = gridDim.x * kThreads;
-      // rows of this round's sequences
+      // rows of this pass's sequences
       const uint32_t r_end = min(total.rows, static_cast<uint32_t>(a.n_rows));
       uint32_t r = blockIdx.x * kThreads + tid;
       if (r < before.rows) r += (before.rows - r + stride - 1) / stride * stride;
       for (; r < r_end; r += stride) {
-        const int t = last_at_or_before(row_first, in_round, r);
+        const int t = last_at_or_before(row_first, in_pass, r);
         const int64_t at = static_cast<int64_t>(cached_rows[t]) + (r - row_first[t]);
         const int64_t j = at >> a.page_shift;  // page of the sequence
         int32_t* const entry = a.page_table + static_cast<size_t>(b0 + t) * a.max_pages + j;
@@ -134,11 +134,11 @@ __device__ __forceinline__ void assign(const KvAssign& a, bool write_state) {
                           ? (static_cast<int64_t>(number) << a.page_shift) + (at & (page - 1))
                           : -1;
       }
-      // pages that this round's finished sequences give back
+      // pages that this pass's finished sequences give back
       uint32_t p = blockIdx.x * kThreads + tid;
       if (p < before.back) p += (before.back - p + stride - 1) / stride * stride;
       for (; p < total.back; p += stride) {
-        const int t = last_at_or_before(back_first, in_round, p);
+        const int t = last_at_or_before(back_first, in_pass, p);
         const uint32_t j = p - back_first[t] + static_cast<uint32_t>(shared_pages[t]);
         a.free_pages[(tail + p % n_pages) % n_pages] =
             a.page_table[static_cast<size_t>(b0 + t) * a.max_pages + j];
