@@ -886,11 +886,15 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
       sum_segments();
     }
     bool done = false;
+    // A list that holds the whole row settles it whatever limits it, and has to: such a call makes no
+    // later launches, and its workspace has no states for them.
+    const bool held = row.vocab <= kPickList;
     // (a list of weights of at most 1 does not come to top_p of more than its length)
-    const bool hopeless = row.st.min_p <= 0.f && row.vocab > kPickList &&
-                          static_cast<double>(share_of(row.whole_sum, fminf(row.st.top_p, 0x1.fffffep-1f))) >
-                              kPickList * row.scale;
-    if (few || ((row.st.top_p < 1.f || row.st.min_p > 0.f) && !hopeless)) {
+    const bool hopeless =
+        row.st.min_p <= 0.f &&
+        static_cast<double>(share_of(row.whole_sum, fminf(row.st.top_p, 0x1.fffffep-1f))) >
+            kPickList * row.scale;
+    if (few || held || ((row.st.top_p < 1.f || row.st.min_p > 0.f) && !hopeless)) {
       bool complete;
       const int n = gather(row, tops, s, few ? row.st.top_k : kNucleus, few, complete);
       done = n > 0 && pick_from_list(a, row, s, n, complete, soft);
@@ -901,7 +905,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
       else
         header = RowHeader{row.scale, row.whole_sum, row.top, row.low, row.st, 1, 0};
     }
-    if (!done) {  // (all but the lists)
+    if (!done && !held) {  // (all but the lists)
       u32x4* const state = reinterpret_cast<u32x4*>(&ws.states[row.r]);
       for (int i = t; i < static_cast<int>(offsetof(SearchState, list) / 16); i += kPickThreads)
         state[i] = u32x4{};

@@ -567,6 +567,34 @@ def test_vocabularies_at_borders(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [129, 130, 200, 255, 256])
+def test_vocabularies_that_a_list_holds(V, dtype):
+    """A call whose rows fit the second launch's list makes no later ones: every row is settled, with
+    limits of any kind, alone and beside others, and nothing behind the workspace is written."""
+    many = [127, 128, 129, 200, V - 2, V - 1, V, V + 1]
+    rows = [dict(top_k=k) for k in many] + [dict(top_k=k, **more) for k in many for more in
+            (dict(top_p=0.9), dict(min_p=0.01), dict(temperature=0.0), dict(temperature=3.0))]
+    rows += [dict(top_p=0.5), dict(top_p=0.999), dict(min_p=1e-6), dict(), dict(top_k=1)]
+    keys = ("temperature", "top_k", "top_p", "min_p")
+    cols = {k: [s.get(k, d) for s in rows] for k, d in zip(keys, (1.0, 0, 1.0, 0.0))}
+    for seed, kind in ((30, "plain"), (31, "mixed"), (32, "ties")):
+        T = 2 * len(rows)
+        z, u = _logits(T, V, seed, kind), np.random.default_rng(seed).random(T)
+        z[1::6, ::3] = -np.inf
+        d = Draw(z, u, blocks=[2] * len(rows), dtype=dtype, pad=seed % 3, **cols)
+        need = eb_sample_workspace(EB_BF16 if dtype == "bf16" else EB_F32, T, V)
+        buf = torch.full((need + T * (1 << 16),), 0x5A, dtype=torch.uint8, device="cuda")
+        d.check(ws=buf[:need])
+        assert (buf[need:] == 0x5A).all()
+    for k in many:                                      # top-k by itself: the other arrays are NULL
+        d = Draw(z[:3], u[:3], dtype=dtype, top_k=k)
+        need = eb_sample_workspace(EB_BF16 if dtype == "bf16" else EB_F32, 3, V)
+        buf = torch.full((need + 3 * (1 << 16),), 0x5A, dtype=torch.uint8, device="cuda")
+        d.check(ws=buf[:need])
+        assert (buf[need:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [3001, 40011])
 def test_more_ties_than_a_list_holds(V, dtype):
     """Borders inside thousands of equal logits, above them and below them, and logits far off the rest."""
