@@ -1152,7 +1152,9 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
       state.border.before_k = static_cast<uint32_t>(before_k);
     }
   }
+  // (whole numbers from each segment's sums: which segments are a wave's depends on the call's rows)
   double sum = 0.0, sum_between = 0.0;
+  uint64_t weight_between = 0;
   visit<kPartWaves>(
       row, part_begin(part, ws.parts, ws.segments), part_begin(part + 1, ws.parts, ws.segments),
       [&](int g) {
@@ -1177,6 +1179,10 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
         if ((t & 63) == 0)
           ws.kept[static_cast<size_t>(r) * ws.segments + g] = whole(sum, row.scale);
         sum = 0.0;
+        if (between) {
+          weight_between += whole(wave_reduce(sum_between, Add{}), row.scale);
+          sum_between = 0.0;
+        }
       });
   // The listed ids by one reservation a workgroup.  (With an atomic on the
   // state for each 14.5 us for 32 wide nuclei, so 11.9.)
@@ -1187,12 +1193,9 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
   for (int which = 0; which < 2; ++which)
     for (uint32_t j = t; j < min(n_list[which], uint32_t{kList}); j += kPartThreads)
       if (list_at[which] + j < kList) state.list[which][list_at[which] + j] = list[which][j];
-  if (between) {
-    sum_between = wave_reduce(sum_between, Add{});
-    if ((t & 63) == 0)
-      atomicAdd(reinterpret_cast<unsigned long long*>(&state.border.between),
-                static_cast<unsigned long long>(whole(sum_between, row.scale)));
-  }
+  if (between && (t & 63) == 0)
+    atomicAdd(reinterpret_cast<unsigned long long*>(&state.border.between),
+              static_cast<unsigned long long>(weight_between));
 }
 
 struct Shared {

@@ -398,6 +398,71 @@ def test_row_counts(T):
         np.testing.assert_array_equal(got, want[:T])
 
 
+@pytest.mark.parametrize("settings", [dict(top_k=15000, top_p=0.9), dict(top_k=100, top_p=0.9),
+                                      dict(top_p=0.97, min_p=1e-4), dict(temperature=1.1)])
+def test_row_counts_under_other_limits(settings):
+    """As test_row_counts, for a top-p inside a longer top-k and other limits."""
+    V = 20011
+    z = _logits(600, V, 12)
+    u = np.random.default_rng(12).random(600)
+    want = Draw(z, u, **settings).check()
+    for T in (1, 7, 32, 257):
+        for got, w in zip(Draw(z[:T], u[:T], **settings).run(), want):
+            np.testing.assert_array_equal(got, w[:T])
+
+
+def test_a_sum_inside_a_top_k_is_cut_alike_for_all_row_counts():
+    """Four ids of weight 1, and so much weight behind them that a top-p of one half ends within a few units
+    of the sums of the third: how many are kept hangs on the last bits of the weight of all top_k ids.
+    The rows differ by a step of one small weight each; the border lies at the same one whether the
+    call has 201 rows or so many that a row is one part."""
+    V, n = 24576, 20000
+    rng = np.random.default_rng(33)
+    ids = rng.permutation(V)
+    top, bulk, c1, c2, tail = np.split(ids[:n + 506], [4, n + 4, n + 5, n + 6])
+    top, c1, c2 = np.sort(top), c1[0], c2[0]
+    b = 0.2 * rng.standard_normal(n)
+    row = np.full(V, -np.inf, np.float32)
+    row[top] = 0.0
+    row[bulk] = b + np.log((2 - 5e-7) / np.exp(b).sum())
+    row[tail], row[c1], row[c2] = -40.0, -39.0, -39.0
+    row, top_k = torch.from_numpy(row).cuda(), n + 6 + 250
+
+    def kept_all(column, steps, repeat=1):
+        """Whether all four ids are kept, for each value (the bits of a float, as a whole number)."""
+        values = torch.from_numpy(np.asarray(steps, np.int64).astype(np.uint32).view(np.float32)).cuda()
+        z = row.repeat(len(steps) * repeat, 1)
+        z[:, column] = values.repeat(repeat)
+        T = len(z)
+        token = torch.zeros(T, dtype=I32, device="cuda")
+        eb_sample(Ragged.from_lengths([T], [0]), z, torch.full((T,), 0.99, device="cuda"), token,
+                  top_k=_dev([top_k], I32), top_p=_dev([0.5], F32))
+        token = token.cpu().numpy()
+        assert np.isin(token, top[2:]).all()
+        return token == top[3]
+
+    def border(column):
+        """The lowest float (as bits: negative floats fall) with which the fourth is kept."""
+        bits = lambda x: int(np.float32(x).view(np.uint32))  # noqa: E731
+        least, most = bits(-39.0), bits(-12.0)
+        assert kept_all(column, [least, most]).tolist() == [False, True]
+        while least - most > 1:
+            steps = np.unique(np.linspace(most, least, 66).astype(np.int64))
+            kept = kept_all(column, steps)
+            last = int(np.flatnonzero(kept)[-1])
+            most, least = int(steps[last]), int(steps[last + 1])
+        return most
+
+    row[c1] = torch.from_numpy(np.array([border(c1) + 1], np.uint32).view(np.float32)).cuda()[0]
+    at = border(c2)
+    steps = np.arange(at - 100, at + 101)
+    few = kept_all(c2, steps)
+    assert few.any() and not few.all()
+    for repeat in (2, 5, 21, 45):                       # 45 * 201 = 9045 rows: one part each
+        many = kept_all(c2, steps, repeat).reshape(repeat, -1)
+        np.testing.assert_array_equal(many, np.broadcast_to(few, many.shape))
+
+
 def test_ragged_batch():
     """Settings go by sequence, through empty blocks, over more than 64 sequences."""
     rng = np.random.default_rng(13)
