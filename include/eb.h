@@ -346,8 +346,8 @@ eb_status eb_lmhead_logits(eb_dtype dt, int n_rows, int hidden, int vocab, const
  * token does not depend on how a row is cut and equal inputs give equal tokens; conf's sum is in
  * 32 bits.  vocab <= 2097152 (EB_ERR_UNSUPPORTED beyond).  Of r only batch, total_block, max_block
  * and cu_block are used; in a batch padded to T rows, those behind cu_block[batch] are not used and
- * their outputs left as they were.  With EB_DEBUG_CHECKS, uniform, temperature (not negative, no
- * NaN), top_p and min_p ([0, 1]) are checked as well.
+ * their outputs left as they were.  With EB_DEBUG_CHECKS, uniform (of the rows that are used),
+ * temperature (not negative, no NaN), top_p and min_p ([0, 1]) are checked as well.
  * ws: at least eb_sample_workspace(...) bytes, 16-byte aligned, contents ignored; enough for
  * every smaller number of rows, too.
  * ------------------------------------------------------------------------------------- */

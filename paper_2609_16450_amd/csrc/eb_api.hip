@@ -409,7 +409,8 @@ eb_status check_assign(const eb_page_pool* pool, int32_t batch, int32_t n_rows,
   return EB_OK;
 }
 
-// Random numbers of every row and the settings of every sequence.
+// Random numbers of the rows in use (a batch may be padded behind them) and the settings of every
+// sequence.
 eb_status check_sample_values(const eb_ragged* r, const float* uniform, const eb_sample_params& p,
                               hipStream_t s) {
   auto each = [&](const char* name, const float* d, size_t n, auto ok) -> eb_status {
@@ -420,7 +421,10 @@ eb_status check_sample_values(const eb_ragged* r, const float* uniform, const eb
     return st;
   };
   auto unit = [](float x) { return x >= 0.f && x <= 1.f; };
-  eb_status st = each("uniform", uniform, r->total_block, [](float x) { return x >= 0.f && x < 1.f; });
+  std::vector<int32_t> used;  // (checked to lie in [0, total_block])
+  eb_status st = fetch(used, r->cu_block + r->batch, 1, s);
+  if (st == EB_OK)
+    st = each("uniform", uniform, used[0], [](float x) { return x >= 0.f && x < 1.f; });
   if (st == EB_OK) st = each("temperature", p.temperature, r->batch, [](float x) { return x >= 0.f; });
   if (st == EB_OK) st = each("top_p", p.top_p, r->batch, unit);
   if (st == EB_OK) st = each("min_p", p.min_p, r->batch, unit);

@@ -783,3 +783,23 @@ def test_debug_checks(monkeypatch):
     d.ragged.max_block = 1
     with pytest.raises(EbError, match="cu_block"):
         d.run()
+
+
+def test_debug_checks_leave_padding_alone(monkeypatch):
+    """Random numbers of rows behind the last sequence's are not used, and not checked either."""
+    monkeypatch.setenv("EB_DEBUG_CHECKS", "1")
+    z, u = _logits(12, 300, 34), np.random.default_rng(34).random(12).astype(np.float32)
+    want = Draw(z[:7], u[:7], blocks=[3, 4], top_p=0.9).check()
+    u[7:] = [np.nan, -1.0, 1.0, np.inf, 2.0]
+    for end, n in (([3, 7], 7), ([0, 0], 0)):
+        d = Draw(z, u, blocks=[3, 9], top_p=0.9)
+        d.ragged.cu_block = _dev([0, *end], I32)
+        got = d.run()
+        for g, w in zip(got, want):
+            np.testing.assert_array_equal(g[:n], w[:n])
+            assert (g[n:] == 99).all()
+    u[6] = np.nan                                       # the last row that is used
+    d = Draw(z, u, blocks=[3, 9], top_p=0.9)
+    d.ragged.cu_block = _dev([0, 3, 7], I32)
+    with pytest.raises(EbError, match="uniform"):
+        d.run()
