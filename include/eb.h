@@ -263,8 +263,11 @@ eb_status eb_block_attn_paged(eb_dtype dt, const eb_ragged* r, const eb_paged_kv
  *
  * n_rows >= the sum of the new rows; lengths and sums of lengths lie in [0, 2^31).  Table entries of
  * pages that are not handed out, and a finished sequence's row, keep their contents.  Integers
- * only; the same inputs give the same pages.  With EB_DEBUG_CHECKS the lengths, the ring's state, the
- * rings' free entries, the pages given back and that they fit the ring are checked.
+ * only; the same inputs give the same pages.  An eb_ragged over these offsets holds exact totals
+ * and maxima all the same, except for eb_sample, whose batch may be padded: a graph of calls that
+ * take an eb_ragged is for the lengths that it was captured with.
+ * With EB_DEBUG_CHECKS the lengths, the ring's state and its free entries, the pages given back and
+ * that they fit the ring are checked.
  * ------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t n_pages, page_size; /* as in eb_paged_kv */

@@ -341,3 +341,95 @@ def test_serving_run():
             seen_short += int(ref["short"][b])
             at += live[b]
     assert seen_short and ended
+
+
+@pytest.mark.parametrize("cached,new,dtype", [([5, 70, 33], [9, 1, 20], torch.float32),
+                                              ([0, 400, 129, 31], [32, 16, 64, 1], torch.bfloat16)])
+def test_step_captured_and_replayed(cached, new, dtype):
+    """A whole step in one graph: pages for its rows, attention over the pages, the rows into them, logits, a
+    draw, the commit.  The lengths are the capture's; every replay takes other pages, until there are too
+    few, and other values, and leaves what the same calls leave eagerly, bit for bit."""
+    page, hq, hkv, d, hidden, V = 16, 4, 2, 64, 64, 300
+    B, T = len(cached), sum(new)
+    held, wide = [-(-c // page) for c in cached], 40
+    takes = sum(-(-(c + n) // page) for c, n in zip(cached, new)) - sum(held)
+    replays = 4
+    n_pages = sum(held) + takes * (replays + 1)         # the eager run before, then all but the last
+    table = torch.full((B, wide), -1, dtype=torch.int32)
+    for b in range(B):
+        table[b, :held[b]] = torch.arange(sum(held[:b]), sum(held[:b + 1]))
+    u8, f32, i32 = torch.uint8, torch.float32, torch.int32
+    w = torch.randn(V, hidden, device="cuda").to(dtype)
+
+    class Side:
+        """All that one side of the comparison reads and writes."""
+
+        def __init__(self):
+            self.kv = PagedKV.empty(n_pages, hkv, page, d, table.cuda(), dtype)
+            for t in (self.kv.k, self.kv.v):
+                t.copy_(torch.randn(t.shape, generator=torch.Generator().manual_seed(5)))
+            self.pool = PagePool(torch.arange(sum(held), sum(held) + n_pages, device="cuda",
+                                              dtype=i32) % n_pages,
+                                 _dev([0, n_pages - sum(held)]))
+            z = lambda shape, dt: torch.zeros(shape, dtype=dt, device="cuda")  # noqa: E731
+            self.cu, self.cp, self.pos = z(B + 1, i32), z(B + 1, i32), z(T, i32)
+            self.short = z(B, u8)
+            self.q, self.k, self.v = z((T, hq, d), dtype), z((T, hkv, d), dtype), z((T, hkv, d), dtype)
+            self.h, self.u, self.out = z((T, hidden), dtype), z(T, f32), z((T, hq, d), dtype)
+            self.logits, self.token = z((T, V), f32), z(T, i32)
+            self.prob, self.conf = z(T, f32), z(T, f32)
+            self.masked, self.tokens, self.unmask = z(T, u8), z(T, i32), z(T, u8)
+            self.nc, self.res = z(B, i32), z(B, u8)
+            self.ragged = Ragged.from_lengths(new, cached)
+            self.ragged.cu_block, self.ragged.cu_prefix = self.cu, self.cp
+            self.ins = (_dev(cached), _dev(new))
+            self.limits = dict(temperature=_dev([0.8] * B, f32), top_p=_dev([0.9] * B, f32))
+            self.tau = torch.full((B,), 0.02, device="cuda")
+
+        def fill(self, seed):
+            g = torch.Generator().manual_seed(seed)
+            for t in (self.q, self.k, self.v, self.h):
+                t.copy_(torch.randn(t.shape, generator=g))
+            self.u.copy_(torch.rand(T, generator=g))
+            self.masked.fill_(1)
+            self.tokens.fill_(-1)
+
+        def step(self):
+            eb_kv_assign(self.kv, self.pool, *self.ins, self.cu, self.cp, self.pos, short=self.short)
+            eb_block_attn_paged(self.ragged, self.kv, self.q, self.k, self.v, self.out)
+            eb_kv_write(self.ragged, self.kv, self.k, self.v, pos=self.pos)
+            eb_lmhead_logits(self.h, w, self.logits)
+            eb_sample(self.ragged, self.logits, self.u, self.token, prob=self.prob, conf=self.conf,
+                      **self.limits)
+            eb_unmask_select(self.ragged, self.conf, self.token, self.tau, self.masked, self.tokens,
+                             self.unmask, self.nc, self.res)
+
+        def results(self):
+            return dict(table=self.kv.page_table, state=self.pool.state, k=self.kv.k, v=self.kv.v,
+                        cu=self.cu, cp=self.cp, pos=self.pos, short=self.short, out=self.out,
+                        logits=self.logits, token=self.token, prob=self.prob, conf=self.conf,
+                        masked=self.masked, tokens=self.tokens, unmask=self.unmask, nc=self.nc,
+                        res=self.res)
+
+    captured, eager = Side(), Side()
+    for x in (captured, eager):
+        x.fill(0)
+        x.step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured.step()
+    print(f"step captured {cached} {new}", flush=True)
+    short = []
+    for i in range(1, replays + 2):
+        captured.fill(i)
+        g.replay()
+        torch.cuda.synchronize()
+        (w.float() @ w.float().t()).sum().item()
+        eager.fill(i)
+        eager.step()
+        torch.cuda.synchronize()
+        for (name, a), b in zip(captured.results().items(), eager.results().values()):
+            assert torch.equal(a, b), (i, name)
+        short.append(int(captured.short.sum()))
+    assert not any(short[:-1]) and short[-1]
