@@ -1103,9 +1103,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
   const Settings& st = row.st;
   const Bins bin(row);
   SearchState& state = ws.states[r];
-  // The bins of each limit, kBins where it limits nothing; the cut lies in the first of them.  top-p's are
-  // those that its sum reaches within 2^-18 of the whole, which the histogram's roundings stay below
-  // (hardly ever two), and, where it is a part of the first top_k ids' weight, for all that this may be.
+  // The bins of each limit, kBins where it limits nothing; the cut lies in the first of them.  top-p's
+  // are those that its sum reaches within 2^-18 of the whole (hardly ever two) and, where it is a part of
+  // the first top_k ids' weight, for all that this may be.  The histogram is mostly nearer than 2^-18,
+  // but not always: each id's weight is off by up to half of 2^-31 of the sum, all of a long tail to the
+  // same side perhaps (2^-15 of the sum for 126464 ids).  What has led to a bin beside the cut's is
+  // found by the exact sums (cut_from_lists), and such a row is searched by one workgroup.
   int bin_k = kBins, bin_m = kBins, p_first = kBins, p_last = kBins;
   uint64_t before_k = 0;
 #pragma unroll 1

@@ -87,6 +87,16 @@ def test_logits_are_those_of_the_statistics(rows, hidden, vocab, dtype):
         assert torch.equal(few, z[:3])
 
 
+@pytest.mark.parametrize("rows,hidden,vocab", [(40, 100, 3001), (70, 256, 16400), (600, 64, 2048)])
+def test_logits_f32_do_not_depend_on_the_row_count(rows, hidden, vocab):
+    h, w = _head(rows, hidden, vocab, "f32", 6)
+    z = _check_logits(h, w)
+    for first, n in ((0, 1), (3, 3), (1, 33), (rows - 2, 2)):
+        few = torch.zeros(n, vocab, device="cuda")
+        eb_lmhead_logits(h[first:first + n].contiguous(), w, few)
+        assert torch.equal(few, z[first:first + n])
+
+
 def test_logits_past_2_31_values():
     """More than 2^31 logits: the last rows of a tall call are those of a short one."""
     rows, vocab, hidden = 17000, 126465, 64
@@ -673,6 +683,46 @@ def test_more_ties_than_a_list_holds(V, dtype):
                      dict(top_p=0.5), dict(top_p=0.97), dict(top_k=V // 2, top_p=0.6), dict(min_p=0.3),
                      dict(top_k=70, top_p=0.6, min_p=0.1), dict(top_p=0.999, min_p=1e-9, temperature=3.0)):
         Draw(z, u, dtype=dtype, **settings).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,wide", [(20011, 0.24), (126464, 0.05), (400003, 0.05)])
+def test_tails_that_the_histogram_rounds_away(V, wide, dtype):
+    """One id far above a long tail whose weights lie about half a unit of the histogram (2^-31 of the sum
+    each, a half rounding to 0 or to 1): nuclei that end in the tail, which the histogram never
+    reaches or reaches too early or late."""
+    rng = np.random.default_rng(35)
+    tails = np.log(2.0 ** -30 * np.array([0.25, 0.38, 0.45, 0.505, 0.9, 1.45, 1.505]))
+    z = tails[:, None] + wide * rng.random((7, V))      # (the sum lies between 1 and 2)
+    z[:, V // 3] = 0.0
+    z[::2, V // 2] = -5.0
+    p = np.exp(z)
+    all_ids = p.sum(1)
+    part = all_ids - p[:, V // 3] - np.where(np.arange(7) % 2, 0, p[:, V // 2])
+    end = 1 - 2.0 ** -24                                # (as fp32 the next one is 1)
+    for share in (0.01, 0.2, 0.5, 0.97):                # of the tail that is kept
+        top_p = 1 - (1 - share) * part / all_ids
+        for u, more in ((min(1 - 0.3 * share * part.min(), end), {}), (end, {}),
+                        (end, dict(top_k=V - 7, min_p=1e-12))):
+            Draw(z, [u] * 7, dtype=dtype, top_p=top_p, **more).check()
+
+
+@pytest.mark.parametrize("off", [0.45, 0.55])
+def test_short_lists_that_the_histogram_misses(off):
+    """Thousands of ids above the border whose weights the histogram rounds all down, or all up: it leads to
+    a bin beside the border's, whose ids the list holds."""
+    V = 51203
+    rng = np.random.default_rng(36)
+    w = np.concatenate([[1.0], np.full(30000, 2.0 ** -30 * (40 + off)),
+                        2.0 ** -30 * 20 * np.exp(0.24 * rng.random(V - 30001))])
+    order = rng.permutation(V)
+    z = np.zeros((24, V))
+    z[:, order] = np.log(w)
+    before = np.cumsum(np.sort(w)[::-1])
+    top_p = before[30500 + 800 * np.arange(24)] / before[-1]
+    for u in (0.5, 1 - 2.0 ** -10, 1 - 2.0 ** -24):
+        Draw(z, [u] * 24, top_p=top_p).check()
+        Draw(z, [u] * 24, top_p=top_p, top_k=V - 500).check()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
