@@ -500,7 +500,8 @@ def eb_kv_read(r: Ragged, kv: PagedKV, k, v, stream=None) -> None:
 class PagePool:
     """The pages of a PagedKV that no sequence holds: a ring free_pages int32 [n_pages] and its state
     int32 [2], the place of the first free page and their number (eb_page_pool in eb.h).  Both
-    tensors are kept, not copied."""
+    tensors are checked once, here, and kept, not copied: their contents change, other tensors take
+    a new PagePool."""
 
     def __init__(self, free_pages: torch.Tensor, state: torch.Tensor):
         if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1 or \
@@ -508,7 +509,13 @@ class PagePool:
             raise ValueError("free_pages must be a tensor [n_pages]")
         _dev(free_pages, "free_pages", torch.int32)
         _dev_with(free_pages.get_device(), state, "state", torch.int32, (2,))
-        self.free_pages, self.state = free_pages, state
+        self.free_pages = free_pages
+        self.state = state
+
+    def __setattr__(self, name, value):
+        if hasattr(self, "state"):  # a tensor set here would reach the kernel unchecked
+            raise AttributeError(f"{name}: a PagePool's attributes are fixed")
+        super().__setattr__(name, value)
 
     @staticmethod
     def full(n_pages: int, device="cuda") -> "PagePool":

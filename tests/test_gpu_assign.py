@@ -234,6 +234,17 @@ def test_binding_refusals():
         eb_kv_assign(kv, pool, cached, new, cu, cp, pos, state_out=cu)
 
 
+def test_pool_attributes_are_fixed():
+    """A tensor set behind the checks of the constructor would reach the kernel unchecked."""
+    pool = PagePool.full(8)
+    ring, state = pool.free_pages, pool.state
+    for name, t in (("state", torch.zeros(1, dtype=torch.int32)), ("free_pages", ring.long())):
+        with pytest.raises(AttributeError, match="fixed"):
+            setattr(pool, name, t)
+    assert pool.free_pages is ring and pool.state is state
+    assert ring.tolist() == list(range(8)) and state.tolist() == [0, 8]
+
+
 def test_debug_checks(monkeypatch):
     monkeypatch.setenv("EB_DEBUG_CHECKS", "1")
 
