@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void kv_assign_state_kernel(KvAssign a) {
 }  // namespace
 
 hipError_t kv_assign(const KvAssign& a, hipStream_t s) {
-  const int groups = max(1, min(kMaxGroups, (a.n_rows + kThreads - 1) / kThreads));
+  const int groups = max(1, min(kMaxGroups, a.n_rows / kThreads + (a.n_rows % kThreads != 0)));
   const bool apart = groups > 1 && a.state_out == a.state;
   hipLaunchKernelGGL(kv_assign_kernel, dim3(groups), dim3(kThreads), 0, s, a, !apart);
   if (apart) hipLaunchKernelGGL(kv_assign_state_kernel, dim3(1), dim3(kThreads), 0, s, a);
