@@ -12,8 +12,8 @@
  *                                                          -> eb_unmask_select
  *   4. all of the above on one stream                      -> eb_decode_step
  * For serving, the cached rows may live in pages (eb_paged_kv, eb_kv_write, eb_kv_read,
- * eb_block_attn_paged), which eb_kv_assign hands out and takes back on the device; and tokens may be
- * drawn instead of taken greedily: eb_lmhead_logits writes the logits out, eb_sample draws.
+ * eb_block_attn_paged), which eb_kv_assign hands out and takes back on the device; and tokens may
+ * be drawn instead of taken greedily: eb_lmhead_logits writes the logits out, eb_sample draws.
  *
  * Conventions shared by every entry point
  *   - Every pointer argument is a DEVICE pointer owned by the caller unless stated
@@ -234,35 +234,38 @@ eb_status eb_block_attn_paged(eb_dtype dt, const eb_ragged* r, const eb_paged_kv
                               void* out, void* ws, size_t ws_bytes, eb_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------
- * Pages for the rows that the next calls add, from the sequences' lengths, on the device.  The pages
- * that no sequence holds lie in a ring: state[1] of them, the first at free_pages[state[0]], the
- * next behind it, free_pages[0] behind free_pages[n_pages - 1].
+ * Pages for the rows that the next calls add, from the sequences' lengths, on the device.  The
+ * pages that no sequence holds lie in a ring: state[1] of them, the first at free_pages[state[0]],
+ * the next behind it, free_pages[0] behind free_pages[n_pages - 1].
  *
  * Sequence b holds cached[b] rows, in the first ceil(cached[b] / page_size) pages of its row of
  * page_table, and gets new_rows[b] more.  In order b = 0, 1, ..:
  *
  *   not finished   its new rows begin at position cached[b]; the pages that they need beyond those
  *                  held come from the front of the ring into its row of the table.  Where the ring
- *                  has too few left for it and everyone before (pages that were refused to one are
- *                  counted as well), or its row of the table has too few columns, shorted[b] = 1, none of
- *                  its rows gets a place and its new pages' entries become -1 (no page)
- *   done[b] != 0   no rows; the pages it holds, but for the first shared[b] of them (pages that other
- *                  sequences read too), go behind the ring's last, where later calls take them
+ *                  has too few left for it and everyone before (pages that the ring refused to one
+ *                  are counted as well), or its row of the table has too few columns,
+ *                  shorted[b] = 1, none of its rows gets a place and its new pages' entries become
+ *                  -1 (no page)
+ *   done[b] != 0   no rows; the pages it holds, but for the first shared[b] of them (pages that
+ *                  other sequences read too), go behind the ring's last, where later calls take
+ *                  them
  *
  *   cached, new_rows [batch] i32;  done [batch] u8, optional;  shared [batch] i32, optional (0)
  *   cu_block, cu_prefix [batch + 1] i32: offsets of the new and the cached rows (finished sequences
- *                  have none of both, sequences that got no pages have theirs), as eb_ragged takes them
- *   pos [n_rows] i32, slot [n_rows] i64 (optional): of packed row i its position in its sequence, as
- *                  eb_kv_write takes it, and its place in a head's rows of the pool, page *
+ *                  have none of both, sequences that got no pages have theirs), as eb_ragged takes
+ *                  them
+ *   pos [n_rows] i32, slot [n_rows] i64 (optional): of packed row i its position in its sequence,
+ *                  as eb_kv_write takes it, and its place in a head's rows of the pool, page *
  *                  page_size + row (-1: no page); both -1 for rows that get no place and for rows
  *                  behind the last sequence's (a batch padded to n_rows)
  *   shorted [batch] u8, optional
- *   state_out [2] i32: the ring's state behind the call.  It may be `state` itself.  While it is not,
- *                  and the table's entries of the new pages are all that is read from it, the same
- *                  call can be made again.
+ *   state_out [2] i32: the ring's state behind the call.  It may be `state` itself.  While it is
+ *                  not, and the table's entries of the new pages are all that is read from it, the
+ *                  same call can be made again.
  *
- * n_rows >= the sum of the new rows; lengths and sums of lengths lie in [0, 2^31).  Table entries of
- * pages that are not handed out, and a finished sequence's row, keep their contents.  Integers
+ * n_rows >= the sum of the new rows; lengths and sums of lengths lie in [0, 2^31).  Table entries
+ * of pages that are not handed out, and a finished sequence's row, keep their contents.  Integers
  * only; the same inputs give the same pages.  An eb_ragged over these offsets holds exact totals
  * and maxima all the same, except for eb_sample, whose batch may be padded: a graph of calls that
  * take an eb_ragged is for the lengths that it was captured with.
@@ -310,8 +313,8 @@ eb_status eb_lmhead_confidence(eb_dtype dt, int n_rows, int hidden, int vocab, c
 /* ---------------------------------------------------------------------------------------
  * The LM head's logits, written out:  logits[i, v] = sum_k h[i, k] w[v, k]  in fp32, the same bits
  * that eb_lmhead_confidence forms its statistics from.  For callers that draw tokens (eb_sample) or
- * change logits; 4 bytes per row and vocabulary entry, so a large batch may want to go a part of its
- * rows at a time (a row's logits do not depend on the others').
+ * change logits; 4 bytes per row and vocabulary entry, so a large batch may want to go a part of
+ * its rows at a time (a row's logits do not depend on the others').
  *
  *   h [n_rows, hidden]   w [vocab, hidden] of dtype dt   logits [n_rows, vocab] f32
  *
@@ -321,8 +324,9 @@ eb_status eb_lmhead_logits(eb_dtype dt, int n_rows, int hidden, int vocab, const
                            const void* w, float* logits, eb_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------
- * A token per block row, drawn from its logits with a given random number, under a temperature, top-k,
- * top-p and min-p of its sequence.  For row i of sequence b, z = logits[i, 0 .. vocab), m = max z:
+ * A token per block row, drawn from its logits with a given random number, under a temperature,
+ * top-k, top-p and min-p of its sequence.  For row i of sequence b, z = logits[i, 0 .. vocab) and
+ * m = max z:
  *
  *   w_v = exp((z_v - m) / temperature[b]);  the order: z falling, equal z (also -0 and +0) by id
  *   kept: the first n ids of the order, n the least of
@@ -330,8 +334,8 @@ eb_status eb_lmhead_logits(eb_dtype dt, int n_rows, int hidden, int vocab, const
  *     the fewest whose w come to >= top_p[b] * (sum of w over the first top_k[b]), at least one
  *                                               (top_p[b] >= 1: no limit)
  *     how many have w >= min_p[b]               (min_p[b] <= 0: no limit; above 1 as 1)
- *   token[i] = the lowest kept id with  sum of w over the kept ids up to it > uniform[i] * (sum of w
- *              over all kept ids)
+ *   token[i] = the lowest kept id with
+ *                sum of w over the kept ids up to it > uniform[i] * (sum of w over all kept ids)
  *   prob[i]  = w of the token / (sum of w over all kept ids): what it was drawn with
  *   conf[i]  = exp(z of the token - m) / sum_v exp(z_v - m): its probability under the model, kappa
  *              where it is the top-1 token; with token the conf and argmax of eb_unmask_select
@@ -342,15 +346,19 @@ eb_status eb_lmhead_logits(eb_dtype dt, int n_rows, int hidden, int vocab, const
  *
  *   logits [T, pitch] of dtype dt, of which the first vocab columns are read (pitch >= vocab, in
  *   elements; rows start at any element)   uniform [T] f32 in [0, 1)   token [T] i32
- *   prob, conf [T] f32, optional           temperature, top_p, min_p [batch] f32, top_k [batch] i32,
- *                                          each optional (NULL: 1, 1, 0, 0)
+ *   prob, conf [T] f32, optional
+ *   temperature, top_p, min_p [batch] f32, top_k [batch] i32, each optional (NULL: 1, 1, 0, 0)
  *
- * The weights are formed in 64 bits and summed as whole numbers of about 2^-62 of their sum, so the
- * token does not depend on how a row is cut and equal inputs give equal tokens; conf's sum is in
- * 32 bits.  vocab <= 2097152 (EB_ERR_UNSUPPORTED beyond).  Of r only batch, total_block, max_block
- * and cu_block are used; in a batch padded to T rows, those behind cu_block[batch] are not used and
- * their outputs left as they were.  With EB_DEBUG_CHECKS, uniform (of the rows that are used),
- * temperature (not negative, no NaN), top_p and min_p ([0, 1]) are checked as well.
+ * A weight is formed in 64 bits, right to 2^-37 of itself; with 100000 ids of like weight about one
+ * draw in 10^8 falls to the id beside the one that exact weights give.  Weights are summed in 64
+ * bits over 2048 ids at a time, always the same ones, and beyond that as whole numbers of about
+ * 2^-62 of their sum (where a top_k of at most 128 settles a row: 2^-52 of the largest), so a row's
+ * token does not depend on how the row is cut or on the other rows, and equal inputs give equal
+ * tokens.  prob is rounded to 32 bits once; conf's sum is in 32 bits.  vocab <= 2097152
+ * (EB_ERR_UNSUPPORTED beyond).  Of r only batch, total_block, max_block and cu_block are used; in a
+ * batch padded to T rows, those behind cu_block[batch] are not used and their outputs left as they
+ * were.  With EB_DEBUG_CHECKS, uniform (of the rows that are used), temperature (not negative, no
+ * NaN), top_p and min_p ([0, 1]) are checked as well.
  * ws: at least eb_sample_workspace(...) bytes, 16-byte aligned, contents ignored; enough for
  * every smaller number of rows, too.
  * ------------------------------------------------------------------------------------- */

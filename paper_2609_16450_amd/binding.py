@@ -498,8 +498,8 @@ def eb_kv_read(r: Ragged, kv: PagedKV, k, v, stream=None) -> None:
 
 
 class PagePool:
-    """The pages of a PagedKV that no sequence holds: a ring free_pages int32 [n_pages] and its state
-    int32 [2], the place of the first free page and their number (eb_page_pool in eb.h).  Both
+    """The pages of a PagedKV that no sequence holds: a ring free_pages int32 [n_pages] and its
+    state int32 [2], the place of the first free page and their number (eb_page_pool in eb.h).  Both
     tensors are checked once, here, and kept, not copied: their contents change, other tensors take
     a new PagePool."""
 
@@ -527,10 +527,10 @@ class PagePool:
 def eb_kv_assign(kv: PagedKV, pool: PagePool, cached, new_rows, cu_block, cu_prefix, pos,
                  slot=None, done=None, shared=None, short=None, state_out=None,
                  stream=None) -> None:
-    """Pages of `pool` into kv's page table for new_rows [B] rows behind the cached [B] ones, and back
-    for the done [B]; offsets cu_block, cu_prefix [B + 1], positions pos [n_rows] and slots of the
-    packed new rows (eb.h).  The pool's state is updated in place, or left as it is and written to
-    state_out."""
+    """Pages of `pool` into kv's page table for new_rows [B] rows behind the cached [B] ones, and
+    back for the done [B]; offsets cu_block, cu_prefix [B + 1], positions pos [n_rows] and slots of
+    the packed new rows (eb.h).  The pool's state is updated in place, or left as it is and written
+    to state_out."""
     if not isinstance(kv, PagedKV):
         raise TypeError("kv must be a PagedKV")
     if not isinstance(pool, PagePool):
@@ -652,9 +652,9 @@ def eb_sample_workspace(dtype: int, n_rows: int, vocab: int) -> int:
 def eb_sample(r: Ragged, logits, uniform, token, prob=None, conf=None, temperature=None,
               top_k=None, top_p=None, min_p=None, vocab: Optional[int] = None,
               ws: Optional[torch.Tensor] = None, stream=None) -> None:
-    """token [T] int32 (with prob and conf [T]) <- a draw from each block row's logits [T, pitch] with
-    uniform [T], under its sequence's temperature, top_k, top_p and min_p [B] (eb.h).  vocab: the
-    columns that are tokens, all of them by default."""
+    """token [T] int32 (with prob and conf [T]) <- a draw from each block row's logits [T, pitch]
+    with uniform [T], under its sequence's temperature, top_k, top_p and min_p [B] (eb.h).  vocab:
+    the columns that are tokens, all of them by default."""
     dt = _dtype_code(logits)
     T, B = r.total_block, r.batch
     if logits.dim() != 2:

@@ -215,9 +215,9 @@ eb::PagedKv paged_args(const eb_paged_kv* kv) {
   const eb::CacheType type = kv->dtype == EB_E4M3   ? eb::CacheType::kE4m3
                              : kv->dtype == EB_BF16 ? eb::CacheType::kBf16
                                                     : eb::CacheType::kF32;
-  return eb::PagedKv{type, kv->hkv, kv->head_dim, kv->n_pages, page_shift(kv->page_size), kv->max_pages,
-                     kv->page_table, static_cast<uint8_t*>(kv->k), static_cast<uint8_t*>(kv->v),
-                     kv->k_scale, kv->v_scale};
+  return eb::PagedKv{type, kv->hkv, kv->head_dim, kv->n_pages, page_shift(kv->page_size),
+                     kv->max_pages, kv->page_table, static_cast<uint8_t*>(kv->k),
+                     static_cast<uint8_t*>(kv->v), kv->k_scale, kv->v_scale};
 }
 
 // ---- optional checks of the device-array contract --------------------------------------
@@ -382,8 +382,8 @@ eb_status check_assign(const eb_page_pool* pool, int32_t batch, int32_t n_rows,
   int64_t rows = 0, prefix = 0, back = 0;
   for (int b = 0; b < batch; ++b) {
     if (held[b] < 0 || add[b] < 0 || (shared && keep[b] < 0))
-      return fail(EB_ERR_INVALID, "sequence %d: a negative length (%d cached, %d new, %d shared)", b,
-                  held[b], add[b], shared ? keep[b] : 0);
+      return fail(EB_ERR_INVALID, "sequence %d: a negative length (%d cached, %d new, %d shared)",
+                  b, held[b], add[b], shared ? keep[b] : 0);
     const int64_t pages = (static_cast<int64_t>(held[b]) + pool->page_size - 1) / pool->page_size;
     if (pages > pool->max_pages)
       return fail(EB_ERR_INVALID, "sequence %d: %d cached rows do not fit %d pages of %d rows", b,
@@ -417,7 +417,8 @@ eb_status check_sample_values(const eb_ragged* r, const float* uniform, const eb
     std::vector<float> h;
     eb_status st = d ? fetch(h, d, n, s) : EB_OK;
     for (size_t i = 0; st == EB_OK && i < h.size(); ++i)
-      if (!ok(h[i])) st = fail(EB_ERR_INVALID, "%s[%zu] = %g is out of range", name, i, (double)h[i]);
+      if (!ok(h[i]))
+        st = fail(EB_ERR_INVALID, "%s[%zu] = %g is out of range", name, i, (double)h[i]);
     return st;
   };
   auto unit = [](float x) { return x >= 0.f && x <= 1.f; };
@@ -425,7 +426,8 @@ eb_status check_sample_values(const eb_ragged* r, const float* uniform, const eb
   eb_status st = fetch(used, r->cu_block + r->batch, 1, s);
   if (st == EB_OK)
     st = each("uniform", uniform, used[0], [](float x) { return x >= 0.f && x < 1.f; });
-  if (st == EB_OK) st = each("temperature", p.temperature, r->batch, [](float x) { return x >= 0.f; });
+  if (st == EB_OK)
+    st = each("temperature", p.temperature, r->batch, [](float x) { return x >= 0.f; });
   if (st == EB_OK) st = each("top_p", p.top_p, r->batch, unit);
   if (st == EB_OK) st = each("min_p", p.min_p, r->batch, unit);
   return st;

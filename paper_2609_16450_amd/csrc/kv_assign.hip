@@ -3,13 +3,14 @@
 // Everything follows from exclusive sums over the sequences: of their new rows (where a sequence's
 // rows begin), of the pages that they need (which of the free pages are theirs) and of the pages
 // that finished ones give back (where in the ring those go).  One launch does all of it: every
-// workgroup forms the sums of all sequences for itself, kThreads sequences at a time, which costs it
-// less than a second launch would, and then writes its own rows' positions and slots; a new page's
-// first row also writes the page's number into the table, and given-back pages are spread over all
-// workgroups.  A few thousand integers: bound by the launch and the three or four dependent loads
-// behind it (length, table or ring, then the stores), not by memory: 4.3 us for one sequence, 6.2 us for
-// 64 with 16 to 256 rows each, 9.0 us for 1024 with 205000 rows (of a copy of their 2.5 MB: 0.5 us).
-// Running sums by DPP: 5.3 -> 4.3, 7.1 -> 6.2 and 10.0 -> 9.0 us against exchanges through LDS.
+// workgroup forms the sums of all sequences for itself, kThreads sequences at a time, which costs
+// it less than a second launch would, and then writes its own rows' positions and slots; a new
+// page's first row also writes the page's number into the table, and given-back pages are spread
+// over all workgroups.  A few thousand integers: bound by the launch and the three or four
+// dependent loads behind it (length, table or ring, then the stores), not by memory: 4.3 us for one
+// sequence, 6.2 us for 64 with 16 to 256 rows each, 9.0 us for 1024 with 205000 rows (of a copy of
+// their 2.5 MB: 0.5 us).  Running sums by DPP: 5.3 -> 4.3, 7.1 -> 6.2 and 10.0 -> 9.0 us against
+// exchanges through LDS.
 #include "eb_common.hpp"
 #include "eb_internal.hpp"
 #include "wave_ops.hpp"
@@ -38,8 +39,8 @@ __device__ __forceinline__ int last_at_or_before(const uint32_t* first, int n, u
   return lo;
 }
 
-// write_state false: the call's state_out is its state, which other workgroups may still be reading,
-// and kv_assign_state_kernel writes it behind this launch.
+// write_state false: the call's state_out is its state, which other workgroups may still be
+// reading, and kv_assign_state_kernel writes it behind this launch.
 template <bool kStateOnly>
 __device__ __forceinline__ void assign(const KvAssign& a, bool write_state) {
   __shared__ uint32_t row_first[kThreads], need_first[kThreads], back_first[kThreads];

@@ -9,10 +9,10 @@
 // block position, so every lane owns one position and reduces the logits it holds in
 // registers before a single cross-half exchange.
 //
-// The same kernels also write the logits (LmOut::kLogits, eb_lmhead_logits): another epilogue on the
-// same accumulators, so a written logit has the bits that the statistics see.  32 rows of 126464 x 4096:
-// 178 us (statistics 176), bound by W; 1024 rows: 807 us (753), bound by the MFMAs, and what comes on
-// top is the stores of 518 MB.
+// The same kernels also write the logits (LmOut::kLogits, eb_lmhead_logits): another epilogue on
+// the same accumulators, so a written logit has the bits that the statistics see.  32 rows of
+// 126464 x 4096: 178 us (statistics 176), bound by W; 1024 rows: 807 us (753), bound by the MFMAs,
+// and what comes on top is the stores of 518 MB.
 #include <type_traits>
 
 #include "attn_small.hpp"
@@ -130,9 +130,9 @@ __device__ __forceinline__ Partial wave_column_stats(const f32x4 (&acc)[TM][NT],
   return partial_xor_merge(p, 32, lane);
 }
 
-// Writes the logits of a wave's natural-order 16x16 accumulator tiles (rows as in wave_column_stats,
-// columns the positions row0 + 16 nt + l % 16 below n_rows): 16 bytes per lane, 64 contiguous bytes
-// per position and tile.  A logit row starts at any float.
+// Writes the logits of a wave's natural-order 16x16 accumulator tiles (rows as in
+// wave_column_stats, columns the positions row0 + 16 nt + l % 16 below n_rows): 16 bytes per lane,
+// 64 contiguous bytes per position and tile.  A logit row starts at any float.
 template <int TM, int NT>
 __device__ __forceinline__ void store_logits(const f32x4 (&acc)[TM][NT], float* __restrict__ out,
                                              int row0, int n_rows, int vocab, int wb, int we,
@@ -889,8 +889,9 @@ __device__ __forceinline__ void tile_run(uint8_t* smem, const uint16_t* __restri
     acc_fence_out(acc);  // every MFMA has written its accumulator before the epilogue reads it
 
     if constexpr (kOut == LmOut::kLogits) {
-      // Lane l holds vocabulary rows 16 tm + 4 r + l / 16 of a column; transposed, 16 tm + 4 (l / 16)
-      // .. + 3: 16 bytes per lane, 64 contiguous bytes per position and 16-row block.
+      // Lane l holds vocabulary rows 16 tm + 4 r + l / 16 of a column; transposed,
+      // 16 tm + 4 (l / 16) .. + 3: 16 bytes per lane, 64 contiguous bytes per position and 16-row
+      // block.
       const int v0 = vt * BM + wm * kWaveM + 4 * q4;
 #pragma unroll
       for (int tn = 0; tn < TN; ++tn) {
@@ -972,22 +973,22 @@ __global__ __launch_bounds__(256, 1) void lmhead_tile_kernel(
                       s_end, wave);
 }
 
-// Tile kernel of the large-batch path: 4 waves, one workgroup per compute unit.  1000 positions of a
-// 126464 x 4096 head take 768 us, against 900 us with stages of 32 columns (64 contiguous bytes per
-// row and load: twice the L2 requests), 2048 positions of 126464 x 2048 811 against 949 us.  With two
-// waves loading W and two loading h, and the body once per role, it was 781 and 827 us.
-// Measured and dropped (with 32x32x16 blocks): 8 waves of 128 x 64 (10.55 ms), 256 x 128 tiles
-// with a ring of 3 at two workgroups per compute unit (11.8 ms), stages reaching LDS through
-// registers (9.65 ms), 384 x 256 tiles (384 accumulators per lane: the compiler spills).
+// Tile kernel of the large-batch path: 4 waves, one workgroup per compute unit.  1000 positions of
+// a 126464 x 4096 head take 768 us, against 900 us with stages of 32 columns (64 contiguous bytes
+// per row and load: twice the L2 requests), 2048 positions of 126464 x 2048 811 against 949 us.
+// With two waves loading W and two loading h, and the body once per role, it was 781 and 827 us.
+// Measured and dropped (with 32x32x16 blocks): 8 waves of 128 x 64 (10.55 ms), 256 x 128 tiles with
+// a ring of 3 at two workgroups per compute unit (11.8 ms), stages reaching LDS through registers
+// (9.65 ms), 384 x 256 tiles (384 accumulators per lane: the compiler spills).
 template <int TN, LmOut kOut>
 hipError_t launch_tile_tn(int n_rows, int hidden, int vocab, const void* h, const void* w,
                           Partial* part, float* part2, hipStream_t s) {
   const int n_vtiles = tile_vtiles(vocab);
   const int n_rtiles = (n_rows + 32 * TN - 1) / (32 * TN);
   const int n_tiles = n_vtiles * n_rtiles;
-  // (a multiple of kXcds: every XCD's segment of the launch sequence has its workgroups.  With fewer
-  // tiles than compute units and workgroup g at tile g, as before: 47 us for the logits of 201 rows of
-  // 32003 x 2048, W in the cache in front of HBM; 33 us with the segments)
+  // (A multiple of kXcds: every XCD's segment of the launch sequence has its workgroups.  201 rows
+  // of 32003 x 2048, fewer tiles than compute units, against workgroup g at tile g: logits 50.0 ->
+  // 47.4 us, statistics 47.6 -> 43.5; 45.8 -> 34.5 both with W in the cache in front of HBM.)
   const int groups = min(kTileGroups, (n_tiles + kXcds - 1) / kXcds * kXcds);
   hipLaunchKernelGGL((lmhead_tile_kernel<TN, kOut>), dim3(groups), dim3(256), 0, s,
                      static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(w), n_rows,

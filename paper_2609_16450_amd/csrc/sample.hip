@@ -1,30 +1,36 @@
 // A token per row from its logits and a given random number: temperature, top-k, top-p, min-p.
 //
-// With w_v = exp((z_v - m) / t) and the vocabulary in the order (z falling, id rising), every filter
-// keeps a prefix of that order, so what is kept is one cut: all ids whose logit lies above a value,
-// and of those that equal it the lowest ids up to one.  The token is the lowest kept id whose running
-// sum, over the kept ids in rising order, exceeds u times the sum of all of them.
+// With w_v = exp((z_v - m) / t) and the vocabulary in the order (z falling, id rising), every
+// filter keeps a prefix of that order, so what is kept is one cut: all ids whose logit lies above a
+// value, and of those that equal it the lowest ids up to one.  The token is the lowest kept id
+// whose running sum, over the kept ids in rising order, exceeds u times the sum of all of them.
 //
 // The drawn id depends on sums over up to the whole vocabulary next to a border, and has to be the
-// same whatever cuts the sums into pieces.  So weights are formed in 64 bits and held as whole
-// numbers of 2^-62 of (at least) their sum: the sums are exact in any order, also by atomics, and the
-// one rounding of a weight is off by 2^-63 of the sum, less than a sum in 64-bit floats would lose.
+// same whatever cuts the sums into pieces.  So a weight is formed in 64 bits (to 2^-37 of itself,
+// see Weights).  Within a segment of 2048 ids weights are summed as 64-bit floats, always the same
+// ones in the same order.  Beyond that, and id by id next to a border, sums are of whole numbers of
+// 2^-62 of (at least) the sum of all weights (in rows of a small top-k, of 2^-52 of the largest
+// one): they are exact in any order, also by atomics, whichever segments a workgroup has.  A whole
+// number is off by at most half a unit, a segment's sum by less than 2^-47 of itself, far below
+// what the weights are off by.
 //
-// sample_scan_kernel reads every logit once and leaves, per segment of 2048 ids, its largest and lowest
-// logit and its sums of weights, and the largest of each of its 64 groups of 32 ids.
-// sample_pick_kernel, a workgroup per row, cuts and draws from these alone where that can be done: with
-// a temperature only it reads the one segment that the draw falls into; with a small top-k, or where
-// the nucleus is small, the groups that can hold what is kept (their largest logits say which), at
-// most kPickList ids in LDS.  The rows left over are read again: sample_bins_kernel makes a histogram which finds the few bins that the cut lies in, and
-// sample_sums_kernel the exact sums above them and a list of the ids within, many workgroups to a row;
-// sample_search_kernel, one workgroup to a row, orders the list, cuts and draws.  Rows whose bins hold
-// more ids than the list (logits that tie, or a few that lie far off the others) it cuts by itself, the
-// key found bit by bit.
+// sample_scan_kernel reads every logit once and leaves, per segment of 2048 ids, its largest and
+// lowest logit and its sums of weights, and the largest of each of its 64 groups of 32 ids.
+// sample_pick_kernel, a workgroup per row, cuts and draws from these alone where that can be done:
+// with a temperature only it reads the one segment that the draw falls into; with a small top-k, or
+// where the nucleus is small, the groups that can hold what is kept (their largest logits say
+// which), at most kPickList ids in LDS.  The rows left over (none of a vocabulary that the list
+// holds whole) are read again: sample_bins_kernel makes a histogram which finds the few bins that
+// the cut lies in, and sample_sums_kernel the exact sums above them and a list of the ids within,
+// many workgroups to a row; sample_search_kernel, one workgroup to a row, orders the list, cuts and
+// draws.  Rows whose bins hold more ids than the list it cuts by itself, the key found bit by bit:
+// logits that tie; a few that lie far off the others, so that these share few bins; more than some
+// 300000 ids, of which one bin holds too many.
 //
-// Bounds: many rows are bound by reading the logits, once in the scan (944 fp32 rows of 126464, mixed
-// settings: 110 us, 4.3 TB/s), and once or twice more where they are left over; few rows by one
-// dependent step after another (a single row with a small top-k: 20 us; two launches, and three that find
-// nothing to do).
+// Bounds: many rows are bound by reading the logits, once in the scan (944 fp32 rows of 126464,
+// mixed settings: 110 us, 4.3 TB/s), and once or twice more where they are left over; few rows by
+// one dependent step after another (a single row with a small top-k: 20 us; two launches, and three
+// that find nothing to do).
 #include <float.h>
 #include <stddef.h>
 
@@ -66,8 +72,8 @@ __device__ __forceinline__ int id_in_segment(int i, int lane) {
   return (i * 64 + lane) * kVec<T>;
 }
 
-// Logits at .. at + kVec - 1 of a row, as they came; -inf behind its end.  (Loads without the test for
-// segments that lie before the row's end: 108 -> 123 us for 944 rows of 126464.)
+// Logits at .. at + kVec - 1 of a row, as they came; -inf behind its end.  (Loads without the test
+// for segments that lie before the row's end: 108 -> 123 us for 944 rows of 126464.)
 template <class T>
 struct Chunk;
 template <>
@@ -135,12 +141,12 @@ __constant__ const double kPow64[64] = {
 
 // exp((z - top) / temperature) in 64 bits.  With y = (z - top) 64 log2(e) / temperature and n the
 // whole number nearest to y, it is 2^(n / 64) 2^((y - n) / 64): a table in LDS and a polynomial in
-// y - n (|y - n| <= 1/2) of the third degree, 1 at 0 and otherwise as near as one comes, which leaves
-// 2^-37 of the value at most.  (A weight's error of that size moves a border of the draw by as much
-// of the weight: one in 10^8 draws from 100000 ids of like weight across it.)  n comes from the low
-// bits of y + 1.5 2^52, and 2^(n / 64 rounded down) goes into the result's exponent.
-// What a pass over a row costs is its weights: with 16 table values and a fifth degree 41 us for 131072 on
-// one compute unit, 20 us of them the weights.
+// y - n (|y - n| <= 1/2) of the third degree, 1 at 0 and otherwise as near as one comes, which
+// leaves 2^-37 of the value at most.  (A weight's error of that size moves a border of the draw by
+// as much of the weight: one in 10^8 draws from 100000 ids of like weight across it.)  n comes from
+// the low bits of y + 1.5 2^52, and 2^(n / 64 rounded down) goes into the result's exponent.  What
+// a pass over a row costs is its weights: with 16 table values and a fifth degree 41 us for 131072
+// on one compute unit, 20 us of them the weights.
 struct Weights {
   const double* pow64;  // LDS
   double top, rate;     // largest logit; 64 log2(e) / temperature
@@ -207,7 +213,8 @@ struct Settings {
   float temperature, top_p, min_p;
   int32_t top_k;  // 0: no limit
   __device__ __forceinline__ bool greedy() const { return !(temperature > 0.f); }
-  // (the top_k largest of n groups let at most about -n ln(1 - top_k / n) ids through, 214 of 128 groups)
+  // (the top_k largest of n groups let at most about -n ln(1 - top_k / n) ids through, 214 of 128
+  // groups)
   __device__ __forceinline__ bool few(int vocab) const {
     const int groups = (vocab + kSegment - 1) / kSegment * 64;
     return top_k > 0 && top_k <= kFewIds && (vocab <= kPickList || 16 * top_k <= 13 * groups);
@@ -275,7 +282,8 @@ struct Max {
 struct MaxOfBoth {  // of the two halves, each by itself
   __device__ __forceinline__ uint64_t operator()(uint64_t a, uint64_t b) const {
     const uint32_t hi = max(static_cast<uint32_t>(a >> 32), static_cast<uint32_t>(b >> 32));
-    return static_cast<uint64_t>(hi) << 32 | max(static_cast<uint32_t>(a), static_cast<uint32_t>(b));
+    const uint32_t lo = max(static_cast<uint32_t>(a), static_cast<uint32_t>(b));
+    return static_cast<uint64_t>(hi) << 32 | lo;
   }
 };
 struct Min {
@@ -401,8 +409,8 @@ __device__ __forceinline__ int entry_id(uint64_t x) {
   return static_cast<int>(~static_cast<uint32_t>(x));
 }
 
-// A row, as a workgroup of any size sees it.  Every wave reduces the segments' statistics by itself,
-// without barriers, and all come to the same bits.
+// A row, as a workgroup of any size sees it.  Every wave reduces the segments' statistics by
+// itself, without barriers, and all come to the same bits.
 template <class T>
 struct Row {
   const T* logits;
@@ -457,9 +465,9 @@ struct Row {
     before = base;
     return segments - 1;
   }
-  // The id whose running sum of f, over the ids of segment g in order and what lies before it, first
-  // exceeds x.  Where the segment's sum of f comes out a little less than the sum that has led to it
-  // (one of the first launch's), its last id with f > 0.
+  // The id whose running sum of f, over the ids of segment g in order and what lies before it,
+  // first exceeds x.  Where the segment's sum of f comes out a little less than the sum that has
+  // led to it (one of the first launch's), its last id with f > 0.
   template <int kN, class S, class F>
   __device__ __forceinline__ int find_id(S& s, int g, uint64_t before, uint64_t x, F f) const {
     constexpr int kIds = kSegment / (64 * kN);  // of a thread
@@ -531,15 +539,16 @@ struct PickShared {
   int32_t found_id;
 };
 
-// A row's segments, a few of them in this lane's registers (segments lane and lane + 64: rows of up to
-// 2^18 ids), the others in memory.  Every wave goes through all of them by itself, without barriers,
-// and all come to the same bits.
+// A row's segments, a few of them in this lane's registers (segments lane and lane + 64: rows of up
+// to 2^18 ids), the others in memory.  Every wave goes through all of them by itself, without
+// barriers, and all come to the same bits.
 struct SegmentsOfRow {
   static constexpr int kHeld = 2;
   const SegmentStats* stats;
   int n;
   SegmentStats held[kHeld];
-  __device__ __forceinline__ SegmentsOfRow(const SegmentStats* stats_, int n_) : stats(stats_), n(n_) {
+  __device__ __forceinline__ SegmentsOfRow(const SegmentStats* stats_, int n_)
+      : stats(stats_), n(n_) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
@@ -561,8 +570,8 @@ struct SegmentsOfRow {
   }
 };
 
-// Largest logits of a row's groups: thread t has groups 4 t .. 4 t + 3 of every 4 kPickThreads, the first
-// ones (rows of up to 163840 ids) in registers.
+// Largest logits of a row's groups: thread t has groups 4 t .. 4 t + 3 of every 4 kPickThreads, the
+// first ones (rows of up to 163840 ids) in registers.
 struct GroupTops {
   static constexpr int kHeld = 5, kPass = 4 * kPickThreads;
   const float* tops;
@@ -591,8 +600,8 @@ struct GroupTops {
   }
 };
 
-// The first of `mine` places in a list for this lane; reserved once a wave.  (With a branch and an atomic
-// to each item most of the kernel's time went here.)
+// The first of `mine` places in a list for this lane; reserved once a wave.  (With a branch and an
+// atomic to each item most of the kernel's time went here.)
 __device__ __forceinline__ uint32_t reserve(uint32_t& length, uint32_t mine) {
   const uint32_t upto = wave_scan(mine), total = of_lane(upto, 63);
   uint32_t at = 0;
@@ -600,14 +609,14 @@ __device__ __forceinline__ uint32_t reserve(uint32_t& length, uint32_t mine) {
   return uniform(at) + upto - mine;
 }
 
-// The first ids of the order into s.list, by way of the groups whose largest logits are the first of
-// these; all ids above -inf (then `complete`) where there are at most kPickList.  By count: at least
-// `want` of them.  Otherwise about as many, less where the rest weighs less than e^-48 of the largest.
-// Returns their number, or -1 where they are more than kPickList.
+// The first ids of the order into s.list, by way of the groups whose largest logits are the first
+// of these; all ids above -inf (then `complete`) where there are at most kPickList.  By count: at
+// least `want` of them.  Otherwise about as many, less where the rest weighs less than e^-48 of the
+// largest.  Returns their number, or -1 where they are more than kPickList.
 //
-// (Much of what a row costs here is the fetching of its code: with a bin and a branch to each item, 41 KB
-// in the kernel, 16.0 us for 32 rows; with one comparison, with the lowest logit that is taken, 31 KB and
-// 12.4 us.)
+// (Much of what a row costs here is the fetching of its code: with a bin and a branch to each item,
+// 41 KB in the kernel, 16.0 us for 32 rows; with one comparison, with the lowest logit that is
+// taken, 31 KB and 12.4 us.)
 template <class T>
 __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, PickShared& s,
                                       uint32_t want, bool by_count, bool& complete) {
@@ -616,9 +625,9 @@ __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, 
   float hi = row.top, lo = fmaxf(row.low, row.top - 48.f * row.st.temperature);
   float least = row.low;  // that has a bin
   float cut;              // least logit that is taken
-  // The bin of [lo, hi] that the want-th group lies in, the last one for what lies lower as well.  Where
-  // the groups up to it are more than the list, the bins are laid over that bin's: a sure row's one
-  // logit far above all others, then perhaps a mask's far below them.
+  // The bin of [lo, hi] that the want-th group lies in, the last one for what lies lower as well.
+  // Where the groups up to it are more than the list, the bins are laid over that bin's: a sure
+  // row's one logit far above all others, then perhaps a mask's far below them.
   uint32_t ahead = 0;  // groups above hi
   for (int level = 0;; ++level) {
     // (halves: no overflow)
@@ -667,7 +676,8 @@ __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, 
 #pragma unroll
   for (int j = 0; j < GroupTops::kHeld; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) taken |= static_cast<uint32_t>(tops.held[j][e] >= cut) << (4 * j + e);
+    for (int e = 0; e < 4; ++e)
+      taken |= static_cast<uint32_t>(tops.held[j][e] >= cut) << (4 * j + e);
   auto put_groups = [&](int pass) {
     uint32_t place = reserve(s.n_groups, __popc(taken));
     for (; taken; taken &= taken - 1) {
@@ -712,10 +722,10 @@ __device__ __forceinline__ int gather(const Row<T>& row, const GroupTops& tops, 
   return n <= kPickList ? static_cast<int>(n) : -1;
 }
 
-// Cuts and draws from the n ids of s.list, the first n of the order, an id a thread; false where what
-// is kept may go on behind them.  An id's place in the order, the weight before it, and then the weight
-// up to it in the order of ids come from one walk each over the list, which all lanes read at once:
-// no sorting, and no sums across waves.
+// Cuts and draws from the n ids of s.list, the first n of the order, an id a thread; false where
+// what is kept may go on behind them.  An id's place in the order, the weight before it, and then
+// the weight up to it in the order of ids come from one walk each over the list, which all lanes
+// read at once: no sorting, and no sums across waves.
 template <class T>
 __device__ __forceinline__ bool pick_from_list(const SampleArgs& a, const Row<T>& row,
                                                PickShared& s, int n, bool complete, float soft) {
@@ -837,7 +847,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
     });
     soft = wave_reduce(soft, Add{});
   }
-  auto weight = [&](const SegmentStats& x) { return x.top > -INFINITY ? x.sum * row.w(x.top) : 0.0; };
+  auto weight = [&](const SegmentStats& x) {
+    return x.top > -INFINITY ? x.sum * row.w(x.top) : 0.0;
+  };
   auto whole_part = [&](const SegmentStats& x) { return whole(weight(x), row.scale); };
   auto sum_segments = [&]() {  // sets scale and whole_sum
     double x = 0.0;
@@ -886,8 +898,8 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
       sum_segments();
     }
     bool done = false;
-    // A list that holds the whole row settles it whatever limits it, and has to: such a call makes no
-    // later launches, and its workspace has no states for them.
+    // A list that holds the whole row settles it whatever limits it, and has to: such a call makes
+    // no later launches, and its workspace has no states for them.
     const bool held = row.vocab <= kPickList;
     // (a list of weights of at most 1 does not come to top_p of more than its length)
     const bool hopeless =
@@ -914,25 +926,26 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
 }
 
 // ---------------------------------------------------------------------------------------
-// The rows that the second launch has left: cuts anywhere.  Three launches: a histogram of a row by its
-// parts' workgroups, which tells the bin that the cut lies in; the exact sums above the bin, segment by
-// segment, with the bin's ids put into a list, by workgroups again; and a workgroup that orders the list,
-// cuts and draws.  The last one alone also does the rows that the others have not found the cut of.
-// (That workgroup alone for rows of up to 32768 ids: 40 -> 48 us for a row of 9000, 588 -> 970 us for 4096
-// rows of 32000, wide nuclei.)
+// The rows that the second launch has left: cuts anywhere.  Three launches: a histogram of a row by
+// its parts' workgroups, which tells the bin that the cut lies in; the exact sums above the bin,
+// segment by segment, with the bin's ids put into a list, by workgroups again; and a workgroup that
+// orders the list, cuts and draws.  The last one alone also does the rows that the others have not
+// found the cut of.  (That workgroup alone for rows of up to 32768 ids: 40 -> 48 us for a row of
+// 9000, 588 -> 970 us for 4096 rows of 32000, wide nuclei.)
 // ---------------------------------------------------------------------------------------
 constexpr int kPartThreads = 256;
 constexpr int kPartWaves = kPartThreads / 64;
-// The histogram's workgroups do two parts each: what few rows wait for is its atomics on the row's state
-// (4 waves: 14.6 us for 32 rows, 8: 11.0, 16: 10.2; but of 944 rows in all 199, 196 and 197 us).
+// The histogram's workgroups do two parts each: what few rows wait for is its atomics on the row's
+// state (4 waves: 14.6 us for 32 rows, 8: 11.0, 16: 10.2; but of 944 rows in all 199, 196 and 197
+// us).
 constexpr int kBinThreads = 2 * kPartThreads;
 __host__ __device__ constexpr int bin_parts(int parts) { return (parts + 1) / 2; }
 
 // f(z, id) for every id that this lane holds of segments first + wave, first + wave + kN, .. below
 // `end` for which wanted(g); then each_segment(g) (by the whole wave) for these and the others.
-// Two loads at a time, the next two under way meanwhile (four: 232 -> 237 us for 944 rows of 126464, mixed
-// settings), worked on by two ids (with more the kernels of 16 waves, which have 128 registers a lane,
-// spill; the others take the same time with eight).
+// Two loads at a time, the next two under way meanwhile (four: 232 -> 237 us for 944 rows of
+// 126464, mixed settings), worked on by two ids (with more the kernels of 16 waves, which have 128
+// registers a lane, spill; the others take the same time with eight).
 template <int kN, class T, class Wanted, class F, class End>
 __device__ __forceinline__ void visit(const Row<T>& row, int first, int end, Wanted wanted, F f,
                                       End each_segment) {
@@ -966,9 +979,9 @@ __device__ __forceinline__ void visit(const Row<T>& row, int first, int end, Wan
   }
 }
 
-// Bins from a row's largest logit down; a higher logit never has a higher bin.  They are of equal width
-// down to what weighs e^-64 of the largest, and the last one holds all that lies lower; but with a
-// top-k, which counts that too, half of them are laid over it.
+// Bins from a row's largest logit down; a higher logit never has a higher bin.  They are of equal
+// width down to what weighs e^-64 of the largest, and the last one holds all that lies lower; but
+// with a top-k, which counts that too, half of them are laid over it.
 struct Bins {
   static constexpr int kLower = kBins / 2 - 1;
   float half_top, per, half_from, per_lower, upper;
@@ -1054,8 +1067,8 @@ __global__ __launch_bounds__(kBinThreads) void sample_bins_kernel(SampleArgs a, 
   }
 }
 
-// The bins in which the running sum of x (kBins / kPartThreads bins a thread) reaches a first and a second
-// target, kBins where none does, with the sum before the first of them.
+// The bins in which the running sum of x (kBins / kPartThreads bins a thread) reaches a first and a
+// second target, kBins where none does, with the sum before the first of them.
 struct FoundBins {
   int first, second;
   uint64_t before;
@@ -1103,12 +1116,13 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
   const Settings& st = row.st;
   const Bins bin(row);
   SearchState& state = ws.states[r];
-  // The bins of each limit, kBins where it limits nothing; the cut lies in the first of them.  top-p's
-  // are those that its sum reaches within 2^-18 of the whole (hardly ever two) and, where it is a part of
-  // the first top_k ids' weight, for all that this may be.  The histogram is mostly nearer than 2^-18,
-  // but not always: each id's weight is off by up to half of 2^-31 of the sum, all of a long tail to the
-  // same side perhaps (2^-15 of the sum for 126464 ids).  What has led to a bin beside the cut's is
-  // found by the exact sums (cut_from_lists), and such a row is searched by one workgroup.
+  // The bins of each limit, kBins where it limits nothing; the cut lies in the first of them.
+  // top-p's are those that its sum reaches within 2^-18 of the whole (hardly ever two) and, where
+  // it is a part of the first top_k ids' weight, for all that this may be.  The histogram is mostly
+  // nearer than 2^-18, but not always: each id's weight is off by up to half of 2^-31 of the sum,
+  // all of a long tail to the same side perhaps (2^-15 of the sum for 126464 ids).  What has led to
+  // a bin beside the cut's is found by the exact sums (cut_from_lists), and such a row is searched
+  // by one workgroup.
   int bin_k = kBins, bin_m = kBins, p_first = kBins, p_last = kBins;
   uint64_t before_k = 0;
 #pragma unroll 1
@@ -1155,7 +1169,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_sums_kernel(SampleArgs a,
       state.border.before_k = static_cast<uint32_t>(before_k);
     }
   }
-  // (whole numbers from each segment's sums: which segments are a wave's depends on the call's rows)
+  // (whole numbers from each segment's sums: which segments are a wave's depends on the call's
+  // rows)
   double sum = 0.0, sum_between = 0.0;
   uint64_t weight_between = 0;
   visit<kPartWaves>(
@@ -1243,7 +1258,8 @@ struct Searcher {
     for (int g = threadIdx.x & 63; g < row.segments; g += 64) n += s.segment[g];
     return uniform(wave_reduce(n, Add{}));
   }
-  // The id whose running sum of f, over all ids in order, first exceeds x, from f's sums in s.segment.
+  // The id whose running sum of f, over all ids in order, first exceeds x, from f's sums in
+  // s.segment.
   template <class F>
   __device__ __forceinline__ int find(uint64_t x, F f) const {
     uint64_t before;
@@ -1292,8 +1308,8 @@ struct Searcher {
     l.entry = active ? entry : 0;
     l.x = active ? row.w(key_logit(entry_key(l.entry))) : 0.0;
     l.mass = whole(l.x, row.scale);
-    // entries as consecutive numbers as far as they go: keys from the list's lowest on (of bf16 logits
-    // their upper halves, so that equal ones are told apart by their ids), then the ids
+    // entries as consecutive numbers as far as they go: keys from the list's lowest on (of bf16
+    // logits their upper halves, so that equal ones are told apart by their ids), then the ids
     constexpr int kKeyShift = sizeof(T) == 2 ? 16 : 0;
     const uint32_t key = entry_key(l.entry) >> kKeyShift;
     const uint64_t ends = block_reduce<kWaves>(
@@ -1343,9 +1359,10 @@ struct Searcher {
     return l;
   }
 
-  // The cut from what the launches over parts have found, with the kept ids' sums in s.segment; false
-  // where a list has run over, or a rounding of the histogram has led to a bin without the cut.
-  // first_list, kept_sum: this thread's entry of the state's first list and segment's sum above the bins.
+  // The cut from what the launches over parts have found, with the kept ids' sums in s.segment;
+  // false where a list has run over, or a rounding of the histogram has led to a bin without the
+  // cut. first_list, kept_sum: this thread's entry of the state's first list and segment's sum
+  // above the bins.
   __device__ __forceinline__ bool cut_from_lists(const Border& border, uint64_t first_list,
                                                  const uint64_t* second_list, uint64_t kept_sum,
                                                  Cut& cut) const {
@@ -1410,8 +1427,8 @@ struct Searcher {
   }
 
   // The cut behind the first `target` ids of the order (by_mass false), or behind the fewest whose
-  // weights come to `target` (true), by three rounds over the row, which fix 11, 11 and 10 bits of the
-  // key; then, where not all ids of that key are kept, their last one.
+  // weights come to `target` (true), by three rounds over the row, which fix 11, 11 and 10 bits of
+  // the key; then, where not all ids of that key are kept, their last one.
   __device__ __forceinline__ Cut search_bits(bool by_mass, uint64_t target) const {
     const int t = threadIdx.x;
     uint32_t prefix = 0;
@@ -1459,14 +1476,16 @@ struct Searcher {
       take(hi, c0, m0, n0, p0);
       take(hi - 1, c1, m1, n0 + c0, p0 + m0);
       __syncthreads();
-      if (uniform(s.found_count) == 0) return kKeepAll;  // fewer ids, or less weight, than the target
+      // (fewer ids, or less weight, than the target)
+      if (uniform(s.found_count) == 0) return kKeepAll;
       const uint32_t bin = uniform(s.found);
       prefix = level == 0 ? bin : (prefix << (level == 1 ? 11 : 10)) | bin;
       n_before = uniform(s.found_before);
       m_before = uniform(s.found_mass_before);
     }
     // every id of the last bin has the same key and weight
-    const uint64_t equal = uniform(s.found_count), each = uniform(s.found_mass) / equal;  // (if by_mass)
+    const uint64_t equal = uniform(s.found_count);
+    const uint64_t each = uniform(s.found_mass) / equal;  // (if by_mass)
     const uint64_t keep = by_mass ? (target - m_before + each - 1) / each : target - n_before;
     Cut cut{prefix, INT32_MAX};
     if (keep < equal) {
@@ -1549,8 +1568,8 @@ struct Layout {
   }
 };
 
-// Workgroups per row of the launches over parts: up to 8192 in all, as the rows left over are of unlike
-// cost (2048: 300 -> 244 us for 944 rows, mixed settings), at most 32 of a row (a wave has a
+// Workgroups per row of the launches over parts: up to 8192 in all, as the rows left over are of
+// unlike cost (2048: 300 -> 244 us for 944 rows, mixed settings), at most 32 of a row (a wave has a
 // segment of its own then, up to 2^18 ids).
 int parts_of(int n_rows, int vocab) {
   return max(1, min(min(8192 / n_rows, 32), (segments_of(vocab) + kPartWaves - 1) / kPartWaves));
@@ -1569,15 +1588,16 @@ hipError_t launch(const SampleArgs& a, void* ws, hipStream_t s) {
                     segments,
                     parts_of(a.n_rows, a.vocab)};
   const int groups = (segments + kScanWaves - 1) / kScanWaves;
-  hipLaunchKernelGGL(sample_scan_kernel<T>, dim3(a.n_rows * groups), dim3(kScanThreads), 0, s, a, w);
+  hipLaunchKernelGGL(sample_scan_kernel<T>, dim3(a.n_rows * groups), dim3(kScanThreads), 0, s, a,
+                     w);
   const bool limits = a.top_k || a.top_p || a.min_p;
   const auto pick = limits ? sample_pick_kernel<T, true> : sample_pick_kernel<T, false>;
   hipLaunchKernelGGL(pick, dim3(a.n_rows), dim3(kPickThreads), 0, s, a, w);
   // rows are left only where something limits them and the list does not hold them whole
   if (limits && a.vocab > kPickList) {
     if (a.top_k || a.top_p)
-      hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(a.n_rows * bin_parts(w.parts)), dim3(kBinThreads),
-                         0, s, a, w);
+      hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(a.n_rows * bin_parts(w.parts)),
+                         dim3(kBinThreads), 0, s, a, w);
     hipLaunchKernelGGL(sample_sums_kernel<T>, dim3(a.n_rows * w.parts), dim3(kPartThreads), 0, s, a,
                        w);
     hipLaunchKernelGGL(sample_search_kernel<T>, dim3(a.n_rows), dim3(kThreads), 0, s, a, w);

@@ -6,8 +6,8 @@
 
 namespace eb {
 
-// x, which is the same on every lane, as a scalar: what depends on it alone takes no vector registers,
-// and branches on it no lane masks.
+// x, which is the same on every lane, as a scalar: what depends on it alone takes no vector
+// registers, and branches on it no lane masks.
 template <class V>
 __device__ __forceinline__ V uniform(V x) {
   static_assert(sizeof(V) == 4 || sizeof(V) == 8, "one or two words");
@@ -51,9 +51,9 @@ __device__ __forceinline__ V dpp(V old, V x) {
   return __builtin_bit_cast(V, r);
 }
 
-// x over the wave, on every lane.  Within rows of 16 lanes by DPP (a third of the time that exchanges
-// through LDS take), then by the swaps of rows and halves; both lanes of a pair combine the same two
-// values, so all lanes end with the same bits.
+// x over the wave, on every lane.  Within rows of 16 lanes by DPP (a third of the time that
+// exchanges through LDS take), then by the swaps of rows and halves; both lanes of a pair combine
+// the same two values, so all lanes end with the same bits.
 template <class V, class Op>
 __device__ __forceinline__ V wave_reduce(V x, Op op) {
   x = op(x, dpp<0xb1>(x, x));   // lane ^ 1
@@ -79,8 +79,8 @@ __device__ __forceinline__ V wave_reduce(V x, Op op) {
   swapped([](uint32_t v) { return __builtin_amdgcn_permlane32_swap(v, v, false, false); });
   return x;
 }
-// Sum of x over this lane and the lanes before it: within rows of 16, then with the last lanes of the
-// rows before.
+// Sum of x over this lane and the lanes before it: within rows of 16, then with the last lanes of
+// the rows before.
 template <class V>
 __device__ __forceinline__ V wave_scan(V x) {
   x += dpp<0x111>(V{}, x);       // row_shr:1

@@ -357,15 +357,15 @@ def test_serving_run():
 @pytest.mark.parametrize("cached,new,dtype", [([5, 70, 33], [9, 1, 20], torch.float32),
                                               ([0, 400, 129, 31], [32, 16, 64, 1], torch.bfloat16)])
 def test_step_captured_and_replayed(cached, new, dtype):
-    """A whole step in one graph: pages for its rows, attention over the pages, the rows into them, logits, a
-    draw, the commit.  The lengths are the capture's; every replay takes other pages, until there are too
-    few, and other values, and leaves what the same calls leave eagerly, bit for bit."""
+    """A whole step in one graph: pages for its rows, attention over the pages, the rows into them,
+    logits, a draw, the commit.  The lengths are the capture's; every replay takes other pages, until
+    there are too few, and other values, and leaves what the same calls leave eagerly, bit for bit."""
     page, hq, hkv, d, hidden, V = 16, 4, 2, 64, 64, 300
     B, T = len(cached), sum(new)
     held, wide = [-(-c // page) for c in cached], 40
     takes = sum(-(-(c + n) // page) for c, n in zip(cached, new)) - sum(held)
     replays = 4
-    n_pages = sum(held) + takes * (replays + 1)         # the eager run before, then all but the last
+    n_pages = sum(held) + takes * (replays + 1)         # an eager run, then all replays but one
     table = torch.full((B, wide), -1, dtype=torch.int32)
     for b in range(B):
         table[b, :held[b]] = torch.arange(sum(held[:b]), sum(held[:b + 1]))
@@ -385,7 +385,7 @@ def test_step_captured_and_replayed(cached, new, dtype):
             z = lambda shape, dt: torch.zeros(shape, dtype=dt, device="cuda")  # noqa: E731
             self.cu, self.cp, self.pos = z(B + 1, i32), z(B + 1, i32), z(T, i32)
             self.short = z(B, u8)
-            self.q, self.k, self.v = z((T, hq, d), dtype), z((T, hkv, d), dtype), z((T, hkv, d), dtype)
+            self.q, self.k, self.v = (z((T, n, d), dtype) for n in (hq, hkv, hkv))
             self.h, self.u, self.out = z((T, hidden), dtype), z(T, f32), z((T, hq, d), dtype)
             self.logits, self.token = z((T, V), f32), z(T, i32)
             self.prob, self.conf = z(T, f32), z(T, f32)
@@ -406,7 +406,8 @@ def test_step_captured_and_replayed(cached, new, dtype):
             self.tokens.fill_(-1)
 
         def step(self):
-            eb_kv_assign(self.kv, self.pool, *self.ins, self.cu, self.cp, self.pos, short=self.short)
+            eb_kv_assign(self.kv, self.pool, *self.ins, self.cu, self.cp, self.pos,
+                         short=self.short)
             eb_block_attn_paged(self.ragged, self.kv, self.q, self.k, self.v, self.out)
             eb_kv_write(self.ragged, self.kv, self.k, self.v, pos=self.pos)
             eb_lmhead_logits(self.h, w, self.logits)

@@ -422,8 +422,8 @@ def test_row_counts_under_other_limits(settings):
 
 
 def test_a_sum_inside_a_top_k_is_cut_alike_for_all_row_counts():
-    """Four ids of weight 1, and so much weight behind them that a top-p of one half ends within a few units
-    of the sums of the third: how many are kept hangs on the last bits of the weight of all top_k ids.
+    """Four ids of weight 1, and so much weight behind them that a top-p of one half ends within a few
+    units of the sums of the third: how many are kept hangs on the last bits of all top_k ids' weight.
     The rows differ by a step of one small weight each; the border lies at the same one whether the
     call has 201 rows or so many that a row is one part."""
     V, n = 24576, 20000
@@ -439,8 +439,8 @@ def test_a_sum_inside_a_top_k_is_cut_alike_for_all_row_counts():
     row, top_k = torch.from_numpy(row).cuda(), n + 6 + 250
 
     def kept_all(column, steps, repeat=1):
-        """Whether all four ids are kept, for each value (the bits of a float, as a whole number)."""
-        values = torch.from_numpy(np.asarray(steps, np.int64).astype(np.uint32).view(np.float32)).cuda()
+        """Whether all four are kept, for each value (the bits of a float, as a whole number)."""
+        values = _dev(np.asarray(steps, np.int64).astype(np.uint32).view(np.float32))
         z = row.repeat(len(steps) * repeat, 1)
         z[:, column] = values.repeat(repeat)
         T = len(z)
@@ -644,8 +644,8 @@ def test_vocabularies_at_borders(V, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [129, 130, 200, 255, 256])
 def test_vocabularies_that_a_list_holds(V, dtype):
-    """A call whose rows fit the second launch's list makes no later ones: every row is settled, with
-    limits of any kind, alone and beside others, and nothing behind the workspace is written."""
+    """A call whose rows fit the second launch's list makes no later ones: every row is settled,
+    with limits of any kind, alone and beside others, and nothing behind the workspace is written."""
     many = [127, 128, 129, 200, V - 2, V - 1, V, V + 1]
     rows = [dict(top_k=k) for k in many] + [dict(top_k=k, **more) for k in many for more in
             (dict(top_p=0.9), dict(min_p=0.01), dict(temperature=0.0), dict(temperature=3.0))]
@@ -688,8 +688,8 @@ def test_more_ties_than_a_list_holds(V, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V,wide", [(20011, 0.24), (126464, 0.05), (400003, 0.05)])
 def test_tails_that_the_histogram_rounds_away(V, wide, dtype):
-    """One id far above a long tail whose weights lie about half a unit of the histogram (2^-31 of the sum
-    each, a half rounding to 0 or to 1): nuclei that end in the tail, which the histogram never
+    """One id far above a long tail whose weights lie about half a unit of the histogram (2^-31 of the
+    sum each, a half rounding to 0 or to 1): nuclei that end in the tail, which the histogram never
     reaches or reaches too early or late."""
     rng = np.random.default_rng(35)
     tails = np.log(2.0 ** -30 * np.array([0.25, 0.38, 0.45, 0.505, 0.9, 1.45, 1.505]))
@@ -709,8 +709,8 @@ def test_tails_that_the_histogram_rounds_away(V, wide, dtype):
 
 @pytest.mark.parametrize("off", [0.45, 0.55])
 def test_short_lists_that_the_histogram_misses(off):
-    """Thousands of ids above the border whose weights the histogram rounds all down, or all up: it leads to
-    a bin beside the border's, whose ids the list holds."""
+    """Thousands of ids above the border whose weights the histogram rounds all down, or all up: it
+    leads to a bin beside the border's, whose ids the list holds."""
     V = 51203
     rng = np.random.default_rng(36)
     w = np.concatenate([[1.0], np.full(30000, 2.0 ** -30 * (40 + off)),

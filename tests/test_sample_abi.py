@@ -111,8 +111,8 @@ def test_assign_refuses(change, status, word):
 @pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are never read without a GPU")
 @pytest.mark.parametrize("rows", [1, 1024, 1025, (1 << 21) + 1, (1 << 31) - 1024, (1 << 31) - 1])
 def test_assign_launch_shapes(rows):
-    """Up to the largest number of rows the launch's shape is formed without overflow (which the build with
-    sanitizers reports); here the launch itself finds no device."""
+    """Up to the largest number of rows the launch's shape is formed without overflow (which the
+    build with sanitizers reports); here the launch itself finds no device."""
     assert _assign(n_rows=rows) == B.EB_ERR_HIP
 
 
